@@ -426,6 +426,151 @@ int symar_check_selftest(symheap_t *heap, void *cuda_stream);
 /* Text of the last CUDA error seen by the library on this thread (host string). */
 const char *symar_last_cuda_error(void);
 
+/* ---- operators between the AllReduces of a decoder layer -------------------------
+ *
+ * A tensor-parallel layer runs, per rank: a product that makes queries, keys and values; rotation and
+ * storage of the new keys and values; attention over what is stored; a product whose partial sums
+ * allreduce() adds; and the same again around the feed-forward part.  These calls are that path on one
+ * card, for all P emulated ranks at once: the heads of all ranks lie side by side, and symar_linear()
+ * takes one matrix per rank and may write straight into the ranks' heap segments.
+ *
+ * Conventions.  Plain device pointers; every stride is in ELEMENTS of the tensor it belongs to and the
+ * innermost axis is contiguous.  Strides may be larger than the extent they cover, and 0 where an operand
+ * is shared.  Calls enqueue on `cuda_stream`, return a status and may be captured in a CUDA graph; they
+ * allocate nothing.  Results are deterministic: no sum depends on the order in which blocks run.       */
+
+typedef enum {
+    SYMAR_ACT_NONE = 0, SYMAR_ACT_RELU = 1,
+    SYMAR_ACT_GELU = 2,          /* y/2 (1 + erf(y / sqrt 2))                                  */
+    SYMAR_ACT_GELU_TANH = 3,     /* y/2 (1 + tanh(sqrt(2/pi) (y + 0.044715 y^3)))              */
+    SYMAR_ACT_SILU = 4           /* y / (1 + exp(-y))                                          */
+} symar_act_t;
+
+/* out_g = act(x_g w_g^T + bias_g) + residual_g  for g = 0 .. groups-1 (one per rank).
+ *   x_g [m][k] and w_g [n][k] bf16 (w as a linear layer keeps it); bias_g [n] bf16 or NULL;
+ *   residual_g and out_g [m][n] of out_dtype (residual may be NULL, and may be out itself).
+ * Sums and epilogue are binary32, rounded once to out_dtype.  With out_dtype = SYMAR_F32 the partial sums of
+ * the tensor cores, whose additions truncate, are added up in IEEE binary32 every 128 products.
+ * root: the one group that adds bias and residual; -1 = every group.  (Of P partial products that an AllReduce
+ * will add, one rank carries the bias and the residual.)
+ * group strides of 0 share an operand; an out_group of 0 is an error where groups > 1.  m, n or k of 0 is allowed
+ * (k = 0: the product is 0).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
+ * are read by the copy engine, others element by element.                                       */
+typedef struct {
+    const void *x;        int64_t x_ld, x_group;
+    const void *w;        int64_t w_ld, w_group;
+    const void *bias;     int64_t bias_group;
+    const void *residual; int64_t residual_ld, residual_group;
+    void       *out;      int64_t out_ld, out_group;
+    int32_t     groups, m, n, k;
+    int32_t     out_dtype;        /* symar_dtype_t */
+    int32_t     act;              /* symar_act_t   */
+    int32_t     root;
+} symar_linear_t;
+int symar_linear(const symar_linear_t *args, void *cuda_stream);
+
+/* The paged 4-bit cache.  `pages` holds num_pages pages of
+ *     [kv_heads][ K codes [page_size][D/2] u8 | V codes [page_size][D/2] u8 |
+ *                 K words [page_size][D/64] u32 | V words [page_size][D/64] u32 ]
+ * 16-byte aligned; D = head_dim is 64, 128 or 256, page_size 16, 32, 64, 128 or 256 tokens.  Channel c of a token is
+ * nibble c, low nibble first.  Each 64 channels share a word: a binary32 scale s >= 0 whose four lowest bits hold the
+ * zero point z; code n stands for s (n - z).  A group x is stored with lo = min(0, x), hi = max(0, x),
+ * s = hi/15 - lo/15 (each product rounded, 1/15 being the binary32 nearest to it; the difference's four lowest bits
+ * cleared), z = rint(-lo r), n = clamp(rint(x r) + z, 0, 15), r = 1/s.  Where s < 2^-126 the group reads back as zeros;
+ * a group with a value that is not finite reads back as NaN.                                     */
+enum { SYMAR_KV_GROUP = 64, SYMAR_KV_MAX_SEQS = 4096 };
+typedef struct {
+    void    *pages;
+    int64_t  num_pages;
+    int32_t  kv_heads, head_dim, page_size;
+} symar_kv_cache_t;
+
+/* The sequences of a call; all pointers are device pointers to int32.
+ *   lengths [seqs]           tokens of each sequence, the new ones included (0: an idle slot)
+ *   token_start [seqs + 1]   sequence b's new tokens are rows token_start[b] .. token_start[b+1]-1 of q, k and v, and
+ *                            the last ones of the sequence; NULL: one new token per sequence, row b (tokens == seqs)
+ *   page_table [seqs][table_ld]  token t of sequence b lies in page page_table[b][t / page_size]           */
+typedef struct {
+    const int32_t *lengths;
+    const int32_t *token_start;
+    const int32_t *page_table;
+    int64_t        table_ld;
+    int32_t        seqs, tokens;
+} symar_kv_batch_t;
+
+/* Context of the cache operators: partial results of sequences that several blocks share, and a status word.
+ * One stream and one host thread at a time, like a heap.  symar_kv_create() allocates (synchronously), the
+ * _on form takes caller memory of symar_kv_required_bytes() bytes, 256-byte aligned.                   */
+typedef struct symar_kv symar_kv_t;
+size_t symar_kv_required_bytes(void);
+int symar_kv_create(symar_kv_t **kv);
+int symar_kv_create_on(symar_kv_t **kv, void *device_mem, size_t device_bytes);
+int symar_kv_destroy(symar_kv_t *kv);
+/* Clear the status word and the context's counters (asynchronous). */
+int symar_kv_reset(symar_kv_t *kv, void *cuda_stream);
+/* Synchronous read: *code is SYMAR_OK, or SYMAR_ERR_INVAL once a call met a page number outside the pool, a position
+ * beyond the page table's row or beyond the table of rotations; *seq and *position say where first.  Such a token
+ * is neither written nor seen; the calls themselves return normally.  Out pointers may be NULL.          */
+int symar_kv_status(symar_kv_t *kv, int *code, int *seq, int *position);
+/* Bytes of one page; 0 for an unsupported shape. */
+size_t symar_kv_page_bytes(int kv_heads, int head_dim, int page_size);
+
+/* Rotations of positions 0 .. rows-1: table [rows][rot_dim/2][2] binary32 (cos, sin) of position * f_i, computed in
+ * binary64 from f_i = base^(-2i/rot_dim), scaled for contexts longer than the model was trained on:
+ *   SYMAR_ROPE_PLAIN     f_i
+ *   SYMAR_ROPE_LINEAR    f_i / factor
+ *   SYMAR_ROPE_BASE      base replaced by base * factor^(rot_dim / (rot_dim - 2))
+ *   SYMAR_ROPE_BY_PARTS  with r = original / (2 pi / f_i) turns over the original context:
+ *                        (1 - g) f_i / factor + g f_i,  g = clamp((r - low) / (high - low), 0, 1)
+ * and cos and sin multiplied by `magnitude` (0 counts as 1).                                      */
+typedef enum { SYMAR_ROPE_PLAIN = 0, SYMAR_ROPE_LINEAR = 1, SYMAR_ROPE_BASE = 2, SYMAR_ROPE_BY_PARTS = 3 } symar_rope_t;
+typedef struct {
+    double  base, factor, original, low, high, magnitude;
+    int32_t kind, rot_dim;
+} symar_rope_scaling_t;
+int symar_rope_table(void *table, int64_t rows, const symar_rope_scaling_t *scaling, void *cuda_stream);
+
+/* Rotate and store.  k, v [tokens][kv_heads][D], q [tokens][q_heads][D] (may be NULL) -> q_out (may be q); all of
+ * `dtype`, with token stride _ld and head stride _head.  The first rot_dim channels of q and k are turned by the
+ * token's position: channels 2i and 2i+1 are a pair where interleaved is 1, i and i + rot_dim/2 where it is 0;
+ * products and sum are each rounded to binary32.  rotations = NULL: no rotation.  A token of an idle slot (position < 0)
+ * is not stored and its q is copied as it is.                                                */
+typedef struct {
+    const void *q;     int64_t q_ld, q_head;
+    void       *q_out; int64_t q_out_ld, q_out_head;
+    const void *k;     int64_t k_ld, k_head;
+    const void *v;     int64_t v_ld, v_head;
+    const void *rotations;
+    int64_t     rotation_rows;
+    int32_t     rot_dim, interleaved, q_heads, dtype;
+} symar_kv_append_t;
+int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch,
+                    const symar_kv_append_t *args, void *cuda_stream);
+
+/* The batch's new tokens as the cache holds them: k, v [tokens][kv_heads][D] of `dtype` (either may be NULL); zeros
+ * for a token of an idle slot.                                                                */
+typedef struct {
+    void   *k; int64_t k_ld, k_head;
+    void   *v; int64_t v_ld, v_head;
+    int32_t dtype;
+} symar_kv_read_t;
+int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch,
+                  const symar_kv_read_t *args, void *cuda_stream);
+
+/* Attention of the batch's new tokens (already stored) over the cache:
+ *   out[t][h] = sum_j softmax_j(scale q[t][h] . K[j][h / share]) V[j][h / share],  share = q_heads / kv_heads,
+ * over the tokens j up to t's own position and, where window > 0, more than position - window.  A row that sees no token
+ * is zeros.  q, out [tokens][q_heads][D] bf16; scale 0 counts as 1 / sqrt(D).  Scores, softmax and sums are binary32; the
+ * probabilities, times the scale of their V group, are rounded to bf16 for the tensor cores.               */
+typedef struct {
+    const void *q;   int64_t q_ld, q_head;
+    void       *out; int64_t out_ld, out_head;
+    float       scale;
+    int32_t     q_heads, window, dtype;
+} symar_kv_attention_t;
+int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch,
+                       const symar_kv_attention_t *args, void *cuda_stream);
+
 /* ---- speed-of-light probes (Sec. VI: L_SoL = 2 L_L2_RTT + L_remote_store) ----
  *
  * Building blocks of the latency bound, measured on the box:

@@ -53,7 +53,7 @@ struct DevicePlace { bool tried = false, ok = false; uint64_t sm_half[4] = {0, 0
 static DevicePlace g_place[kMaxDevices];
 static std::mutex  g_place_mutex;
 
-static int cuda_fail(cudaError_t e, const char *what)
+int cuda_fail(cudaError_t e, const char *what)
 {
     g_last_cuda_error = std::string(what) + ": " + cudaGetErrorString(e);
     return SYMAR_ERR_CUDA;

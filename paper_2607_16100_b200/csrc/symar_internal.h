@@ -6,6 +6,9 @@
 
 namespace symar {
 
+// Keeps the text that symar_last_cuda_error() returns; gives SYMAR_ERR_CUDA.
+int cuda_fail(cudaError_t e, const char *what);
+
 using KernelFn = void (*)(const KArgs);
 
 // Kernel instantiation for (algorithm, element type, ranks); dbg selects the

@@ -1,0 +1,524 @@
+// The paged 4-bit key/value cache: context, append with rotation, read-back, and the table of rotations.
+// The formats and formulas are those stated in include/symar.h.
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "symar_ops.h"
+
+namespace symar {
+namespace {
+
+constexpr int kThreads   = 256;
+constexpr int kMaxTokens = 8;       // tokens that one block of append or read takes
+
+// ---- eight channels of a row, in binary32 ------------------------------------------
+template <typename T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+__device__ __forceinline__ void load8(const float *p, bool vec, float (&x)[8])
+{
+    if (vec) {
+        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, bool vec, float (&x)[8])
+{
+    if (vec) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i]     = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
+    }
+}
+__device__ __forceinline__ void store8(float *p, bool vec, const float (&x)[8])
+{
+    if (vec) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = x[i];
+    }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, bool vec, const float (&x)[8])
+{
+    if (vec) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<uint32_t *>(&h);
+        }
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __float2bfloat16_rn(x[i]);
+    }
+}
+
+// ---- where a new token goes ---------------------------------------------------------
+struct Place {
+    int     seq, pos;       // pos < 0: an idle slot's token
+    int64_t page;           // -1: nowhere
+};
+
+__device__ Place place_of(const KvView &c, const KvBatch &b, int *status, int token)
+{
+    Place p{token, -1, -1};
+    if (b.token_start) {
+        int lo = 0, hi = b.seqs;                      // first sequence whose tokens end beyond `token`
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (b.token_start[mid + 1] > token) hi = mid;
+            else lo = mid + 1;
+        }
+        p.seq = lo;
+        if (lo >= b.seqs) return p;                   // a row of no sequence
+        p.pos = b.lengths[lo] - (b.token_start[lo + 1] - token);
+    } else {
+        p.pos = b.lengths[token] - 1;
+    }
+    if (p.pos >= 0) p.page = kv_page_of(c, b, status, p.seq, p.pos);
+    return p;
+}
+
+struct Rows {
+    char   *p;
+    int64_t ld, head;       // elements
+    int     vec;            // 16-byte accesses allowed
+};
+struct AppendArgs {
+    KvView  c;
+    KvBatch b;
+    Rows    q, qo, k, v;
+    const float2 *table;
+    int64_t table_rows;
+    int     rot, interleaved, q_heads;
+    int    *status;
+    int     tokens_per_block;
+};
+
+// One unit is one head of one token: dim/8 lanes of a warp, eight channels each.  The partner channels of the
+// half layout are read again from global memory (they are in L1: another lane of the same warp reads them too),
+// before any lane of the warp writes, so that q may be rotated in place.
+template <typename T>
+__device__ __forceinline__ void rotate8(float (&x)[8], const T *row, bool vec, int c0, int rot, bool interleaved,
+                                        const float2 *cs)
+{
+    if (c0 >= rot) return;
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int ch = c0 + 2 * i;
+            if (ch < rot) {
+                const float2 t = cs[ch >> 1];
+                const float a = x[2 * i], b = x[2 * i + 1];
+                x[2 * i]     = __fsub_rn(__fmul_rn(a, t.x), __fmul_rn(b, t.y));
+                x[2 * i + 1] = __fadd_rn(__fmul_rn(b, t.x), __fmul_rn(a, t.y));
+            }
+        }
+        return;
+    }
+    const int h = rot >> 1;
+    float y[8];
+    if ((h & 7) == 0) {                                // the whole chunk lies in one half
+        load8(row + (c0 < h ? c0 + h : c0 - h), vec, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int ch = c0 + i;
+            y[i] = ch < rot ? to_f32(row[ch < h ? ch + h : ch - h]) : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int ch = c0 + i;
+        if (ch < rot) {
+            const float2 t = cs[ch < h ? ch : ch - h];
+            const float a = __fmul_rn(x[i], t.x), b = __fmul_rn(y[i], t.y);
+            x[i] = ch < h ? __fsub_rn(a, b) : __fadd_rn(a, b);
+        }
+    }
+}
+
+// Codes and word of a group of 64 channels held by eight neighbouring lanes.  Returns this lane's eight codes.
+__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &word)
+{
+    float lo = 0.0f, hi = 0.0f, odd = 0.0f;            // odd: NaN once a value is not finite
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo  = fminf(lo, x[i]);
+        hi  = fmaxf(hi, x[i]);
+        odd = __fadd_rn(odd, __fmul_rn(x[i], 0.0f));
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+        lo  = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi  = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+        odd = __fadd_rn(odd, __shfl_xor_sync(0xffffffffu, odd, d));
+    }
+    const float fifteenth = 1.0f / 15.0f;
+    const uint32_t bits = __float_as_uint(__fsub_rn(__fmul_rn(hi, fifteenth), __fmul_rn(lo, fifteenth))) & ~15u;
+    const float s = __uint_as_float(bits);
+    if (odd != odd) {
+        word = 0x7fc00000u;
+        return 0u;
+    }
+    if (!(s >= 1.17549435e-38f)) {
+        word = 0u;
+        return 0u;
+    }
+    const float inv = __fdiv_rn(1.0f, s);
+    const float z   = rintf(__fmul_rn(-lo, inv));
+    word            = bits | (uint32_t)z;
+    uint32_t codes  = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float n = fminf(fmaxf(__fadd_rn(rintf(__fmul_rn(x[i], inv)), z), 0.0f), 15.0f);
+        codes |= (uint32_t)n << (4 * i);
+    }
+    return codes;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
+{
+    __shared__ Place at[kMaxTokens];
+    const int first = (int)blockIdx.x * a.tokens_per_block;
+    const int mine  = min(a.tokens_per_block, a.b.tokens - first);
+    if ((int)threadIdx.x < mine) at[threadIdx.x] = place_of(a.c, a.b, a.status, first + threadIdx.x);
+    __syncthreads();
+
+    const int lanes = a.c.dim / 8, per_pass = kThreads / lanes;
+    const int heads = a.q_heads + 2 * a.c.kv_heads, units = mine * heads;
+    const int lane  = (int)threadIdx.x & (lanes - 1), c0 = lane * 8;
+    // every warp makes the same number of trips: the shuffles and the barrier below take whole warps
+    for (int u0 = (int)blockIdx.y * per_pass; u0 < units; u0 += (int)gridDim.y * per_pass) {
+        const int  u   = u0 + (int)threadIdx.x / lanes;
+        const bool on  = u < units;
+        const int  t   = on ? u / heads : 0, h = on ? u - t * heads : 0;
+        const Place p  = at[t];
+        const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.c.kv_heads;
+        const int  hh   = is_q ? h : (is_k ? h - a.q_heads : h - a.q_heads - a.c.kv_heads);
+        const Rows &r   = is_q ? a.q : (is_k ? a.k : a.v);
+        const T *row    = reinterpret_cast<const T *>(r.p) + (int64_t)(first + t) * r.ld + (int64_t)hh * r.head;
+        float x[8] = {};
+        if (on) {
+            load8(row + c0, r.vec, x);
+            if ((is_q || is_k) && a.table && p.pos >= 0) {
+                if (p.pos < a.table_rows) rotate8(x, row, r.vec, c0, a.rot, a.interleaved, a.table + (int64_t)p.pos * (a.rot >> 1));
+                else if (lane == 0) kv_record(a.status, p.seq, p.pos);
+            }
+        }
+        __syncwarp();
+        if (is_q && on)
+            store8(reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + t) * a.qo.ld + (int64_t)hh * a.qo.head + c0, a.qo.vec, x);
+        uint32_t word;
+        const uint32_t codes = quantise8(x, word);
+        if (on && !is_q && p.page >= 0 && !(a.table && p.pos >= a.table_rows)) {
+            const int slot = p.pos & ((1 << a.c.page_shift) - 1), ps = 1 << a.c.page_shift;
+            unsigned char *base = a.c.pages + p.page * a.c.page_bytes + hh * a.c.head_bytes;
+            *reinterpret_cast<uint32_t *>(base + ((is_k ? 0 : ps) + slot) * (a.c.dim / 2) + lane * 4) = codes;
+            if ((lane & 7) == 0)
+                reinterpret_cast<uint32_t *>(base + ps * a.c.dim)[((is_k ? 0 : ps) + slot) * a.c.groups + (lane >> 3)] = word;
+        }
+    }
+}
+
+struct ReadArgs {
+    KvView  c;
+    KvBatch b;
+    Rows    k, v;
+    int    *status;
+    int     tokens_per_block;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
+{
+    __shared__ Place at[kMaxTokens];
+    const int first = (int)blockIdx.x * a.tokens_per_block;
+    const int mine  = min(a.tokens_per_block, a.b.tokens - first);
+    if ((int)threadIdx.x < mine) at[threadIdx.x] = place_of(a.c, a.b, a.status, first + threadIdx.x);
+    __syncthreads();
+
+    const int lanes = a.c.dim / 8, per_pass = kThreads / lanes;
+    const int heads = 2 * a.c.kv_heads, units = mine * heads, ps = 1 << a.c.page_shift;
+    const int lane  = (int)threadIdx.x & (lanes - 1);
+    for (int u = (int)blockIdx.y * per_pass + (int)threadIdx.x / lanes; u < units; u += (int)gridDim.y * per_pass) {
+        const int  t = u / heads, h = u - t * heads;
+        const bool is_k = h < a.c.kv_heads;
+        const int  hh   = is_k ? h : h - a.c.kv_heads;
+        const Rows &r   = is_k ? a.k : a.v;
+        if (!r.p) continue;
+        const Place p = at[t];
+        float x[8] = {};
+        if (p.page >= 0) {
+            const int at_row = (is_k ? 0 : ps) + (p.pos & (ps - 1));
+            const unsigned char *base = a.c.pages + p.page * a.c.page_bytes + hh * a.c.head_bytes;
+            const uint32_t codes = *reinterpret_cast<const uint32_t *>(base + at_row * (a.c.dim / 2) + lane * 4);
+            const uint32_t word  = reinterpret_cast<const uint32_t *>(base + ps * a.c.dim)[at_row * a.c.groups + (lane >> 3)];
+            const float s = kv_scale(word);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __fmul_rn((float)((int)(codes >> (4 * i) & 15u) - kv_zero(word)), s);
+        }
+        store8(reinterpret_cast<T *>(r.p) + (int64_t)(first + t) * r.ld + (int64_t)hh * r.head + lane * 8, r.vec, x);
+    }
+}
+
+struct TableArgs {
+    float2 *table;
+    int64_t rows;
+    int     half, kind;
+    double  log2_base, inv_factor, original, low, high, magnitude;
+};
+
+__global__ void __launch_bounds__(kThreads) table_kernel(const TableArgs a)
+{
+    const int64_t n = a.rows * a.half;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / a.half;
+        const int pair    = (int)(i - row * a.half);
+        double f = exp2(-a.log2_base * pair / a.half);
+        if (a.kind == SYMAR_ROPE_LINEAR) {
+            f *= a.inv_factor;
+        } else if (a.kind == SYMAR_ROPE_BY_PARTS) {
+            const double turns = a.original * f / 6.283185307179586476925287;
+            const double g = fmin(fmax((turns - a.low) / (a.high - a.low), 0.0), 1.0);
+            f = (1.0 - g) * f * a.inv_factor + g * f;
+        }
+        double s, c;
+        sincos((double)row * f, &s, &c);
+        a.table[i] = make_float2((float)(c * a.magnitude), (float)(s * a.magnitude));
+    }
+}
+
+bool make_rows(Rows *r, const void *p, int64_t ld, int64_t head, int dtype)
+{
+    const int64_t vec = dtype == SYMAR_F32 ? 4 : 8;
+    if ((uintptr_t)p % (dtype == SYMAR_F32 ? 4 : 2)) return false;
+    r->p    = (char *)const_cast<void *>(p);
+    r->ld   = ld;
+    r->head = head;
+    r->vec  = (uintptr_t)p % 16 == 0 && ld % vec == 0 && head % vec == 0;
+    return true;
+}
+
+// Blocks of append and read: few tokens take one head per thread group, many take up to eight tokens per block.
+dim3 token_grid(int tokens, int heads, int lanes, int num_sms, int *tokens_per_block)
+{
+    const int per_pass = kThreads / lanes;
+    const int64_t passes = ((int64_t)tokens * heads + per_pass - 1) / per_pass;
+    int tpb = 1;
+    while (tpb < kMaxTokens && passes / tpb > 16ll * num_sms) tpb *= 2;
+    *tokens_per_block = tpb;
+    const int units = tpb * heads;
+    const int split = passes > 64ll * num_sms ? 1 : (units + per_pass - 1) / per_pass;
+    return dim3((unsigned)((tokens + tpb - 1) / tpb), (unsigned)split, 1);
+}
+
+}  // namespace
+
+int kv_check(const symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch, KvView *c, KvBatch *b)
+{
+    if (!kv || !cache || !batch) return SYMAR_ERR_INVAL;
+    if (!symar_kv_page_bytes(cache->kv_heads, cache->head_dim, cache->page_size)) return SYMAR_ERR_UNSUPPORTED;
+    if (!cache->pages || (uintptr_t)cache->pages % 16 || cache->num_pages < 1) return SYMAR_ERR_INVAL;
+    if (batch->seqs < 0 || batch->tokens < 0 || batch->table_ld < 0) return SYMAR_ERR_INVAL;
+    if (batch->seqs > SYMAR_KV_MAX_SEQS) return SYMAR_ERR_UNSUPPORTED;
+    if (batch->tokens > 0) {
+        if (!batch->lengths || !batch->page_table || batch->seqs == 0) return SYMAR_ERR_INVAL;
+        if (((uintptr_t)batch->lengths | (uintptr_t)batch->page_table | (uintptr_t)batch->token_start) % 4) return SYMAR_ERR_INVAL;
+        if (!batch->token_start && batch->tokens != batch->seqs) return SYMAR_ERR_INVAL;
+    }
+    c->pages      = (unsigned char *)cache->pages;
+    c->num_pages  = cache->num_pages;
+    c->kv_heads   = cache->kv_heads;
+    c->dim        = cache->head_dim;
+    c->groups     = cache->head_dim / 64;
+    c->page_shift = 4;
+    while ((1 << c->page_shift) < cache->page_size) ++c->page_shift;
+    c->head_bytes = kv_head_bytes(cache->head_dim, cache->page_size);
+    c->page_bytes = c->head_bytes * cache->kv_heads;
+    *b = KvBatch{batch->lengths, batch->token_start, batch->page_table, batch->table_ld, batch->seqs, batch->tokens};
+    return SYMAR_OK;
+}
+
+}  // namespace symar
+
+using namespace symar;
+
+extern "C" {
+
+size_t symar_kv_page_bytes(int kv_heads, int head_dim, int page_size)
+{
+    if (kv_heads < 1 || kv_heads > 4096 || (head_dim != 64 && head_dim != 128 && head_dim != 256)) return 0;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return 0;
+    return (size_t)kv_heads * (size_t)kv_head_bytes(head_dim, page_size);
+}
+
+size_t symar_kv_required_bytes(void)
+{
+    return kKvPartOff + (size_t)2 * kAttnMaxBlocks * kAttnMaxRows * (kAttnMaxDim + 2) * sizeof(float);
+}
+
+int symar_kv_create_on(symar_kv_t **kv, void *device_mem, size_t device_bytes)
+{
+    if (!kv || !device_mem || (uintptr_t)device_mem % 256) return SYMAR_ERR_INVAL;
+    if (device_bytes < symar_kv_required_bytes()) return SYMAR_ERR_NOMEM;
+    symar_kv *h = new (std::nothrow) symar_kv;
+    if (!h) return SYMAR_ERR_NOMEM;
+    h->mem      = (char *)device_mem;
+    h->status   = (int *)h->mem;
+    h->counters = (unsigned *)(h->mem + kKvCtrOff);
+    h->partials = (float *)(h->mem + kKvPartOff);
+    cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
+    if (e == cudaSuccess) e = cudaMemset(h->mem, 0, kKvPartOff);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) {
+        delete h;
+        return cuda_fail(e, "symar_kv_create");
+    }
+    *kv = h;
+    return SYMAR_OK;
+}
+
+int symar_kv_create(symar_kv_t **kv)
+{
+    if (!kv) return SYMAR_ERR_INVAL;
+    void *p = nullptr;
+    cudaError_t e = cudaMalloc(&p, symar_kv_required_bytes());
+    if (e == cudaErrorMemoryAllocation) {
+        (void)cudaGetLastError();
+        return SYMAR_ERR_NOMEM;
+    }
+    if (e != cudaSuccess) return cuda_fail(e, "cudaMalloc");
+    const int rc = symar_kv_create_on(kv, p, symar_kv_required_bytes());
+    if (rc != SYMAR_OK) (void)cudaFree(p);
+    else (*kv)->owns = true;
+    return rc;
+}
+
+int symar_kv_destroy(symar_kv_t *kv)
+{
+    if (!kv) return SYMAR_ERR_INVAL;
+    int rc = SYMAR_OK;
+    if (kv->owns) {
+        cudaError_t e = cudaFree(kv->mem);
+        if (e != cudaSuccess) rc = cuda_fail(e, "cudaFree");
+    }
+    delete kv;
+    return rc;
+}
+
+int symar_kv_reset(symar_kv_t *kv, void *cuda_stream)
+{
+    if (!kv) return SYMAR_ERR_INVAL;
+    cudaError_t e = cudaMemsetAsync(kv->mem, 0, kKvPartOff, (cudaStream_t)cuda_stream);
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "cudaMemsetAsync");
+}
+
+int symar_kv_status(symar_kv_t *kv, int *code, int *seq, int *position)
+{
+    if (!kv) return SYMAR_ERR_INVAL;
+    int w[3] = {0, 0, 0};
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(w, kv->status, sizeof w, cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return cuda_fail(e, "symar_kv_status");
+    if (code) *code = w[0];
+    if (seq) *seq = w[1];
+    if (position) *position = w[2];
+    return SYMAR_OK;
+}
+
+int symar_rope_table(void *table, int64_t rows, const symar_rope_scaling_t *s, void *cuda_stream)
+{
+    if (!s || rows < 0 || s->rot_dim < 2 || s->rot_dim % 2 || s->rot_dim > 256) return SYMAR_ERR_INVAL;
+    if (!(s->base > 0.0) || s->kind < SYMAR_ROPE_PLAIN || s->kind > SYMAR_ROPE_BY_PARTS) return SYMAR_ERR_INVAL;
+    if (s->kind != SYMAR_ROPE_PLAIN && !(s->factor > 0.0)) return SYMAR_ERR_INVAL;
+    if (s->kind == SYMAR_ROPE_BASE && s->rot_dim < 4) return SYMAR_ERR_INVAL;
+    if (s->kind == SYMAR_ROPE_BY_PARTS && (!(s->original > 0.0) || !(s->high > s->low))) return SYMAR_ERR_INVAL;
+    if (rows == 0) return SYMAR_OK;
+    if (!table || (uintptr_t)table % 8) return SYMAR_ERR_INVAL;
+    TableArgs a;
+    a.table      = (float2 *)table;
+    a.rows       = rows;
+    a.half       = s->rot_dim / 2;
+    a.kind       = s->kind;
+    a.inv_factor = s->kind == SYMAR_ROPE_PLAIN ? 1.0 : 1.0 / s->factor;
+    const double base = s->kind == SYMAR_ROPE_BASE ? s->base * std::pow(s->factor, (double)s->rot_dim / (s->rot_dim - 2)) : s->base;
+    a.log2_base  = std::log2(base);
+    a.original   = s->original;
+    a.low        = s->low;
+    a.high       = s->high;
+    a.magnitude  = s->magnitude == 0.0 ? 1.0 : s->magnitude;
+    const int64_t blocks = (rows * a.half + kThreads - 1) / kThreads;
+    table_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_rope_table");
+}
+
+int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch,
+                    const symar_kv_append_t *args, void *cuda_stream)
+{
+    AppendArgs a;
+    const int rc = kv_check(kv, cache, batch, &a.c, &a.b);
+    if (rc != SYMAR_OK) return rc;
+    if (!args || (args->dtype != SYMAR_F32 && args->dtype != SYMAR_BF16)) return SYMAR_ERR_INVAL;
+    if (args->q_heads < 0 || args->q_heads > 65536 || (args->interleaved != 0 && args->interleaved != 1)) return SYMAR_ERR_INVAL;
+    if (args->rotations && (args->rot_dim < 2 || args->rot_dim % 2 || args->rot_dim > cache->head_dim || args->rotation_rows < 0 ||
+                            (uintptr_t)args->rotations % 8))
+        return SYMAR_ERR_INVAL;
+    if (batch->tokens == 0) return SYMAR_OK;
+    a.q_heads = args->q ? args->q_heads : 0;
+    if (!args->k || !args->v || (a.q_heads > 0 && !args->q_out)) return SYMAR_ERR_INVAL;
+    if (!make_rows(&a.q, args->q, args->q_ld, args->q_head, args->dtype) ||
+        !make_rows(&a.qo, args->q_out, args->q_out_ld, args->q_out_head, args->dtype) ||
+        !make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
+        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype))
+        return SYMAR_ERR_INVAL;
+    a.table       = (const float2 *)args->rotations;
+    a.table_rows  = args->rotation_rows;
+    a.rot         = args->rotations ? args->rot_dim : 0;
+    a.interleaved = args->interleaved;
+    a.status      = kv->status;
+    const dim3 grid = token_grid(batch->tokens, a.q_heads + 2 * a.c.kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
+    if (args->dtype == SYMAR_F32) append_kernel<float><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    else append_kernel<__nv_bfloat16><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_append");
+}
+
+int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch, const symar_kv_read_t *args,
+                  void *cuda_stream)
+{
+    ReadArgs a;
+    const int rc = kv_check(kv, cache, batch, &a.c, &a.b);
+    if (rc != SYMAR_OK) return rc;
+    if (!args || (args->dtype != SYMAR_F32 && args->dtype != SYMAR_BF16)) return SYMAR_ERR_INVAL;
+    if (batch->tokens == 0 || (!args->k && !args->v)) return SYMAR_OK;
+    if (!make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
+        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype))
+        return SYMAR_ERR_INVAL;
+    a.status = kv->status;
+    const dim3 grid = token_grid(batch->tokens, 2 * a.c.kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
+    if (args->dtype == SYMAR_F32) read_kernel<float><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    else read_kernel<__nv_bfloat16><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_read");
+}
+
+}  // extern "C"

@@ -8,7 +8,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_double, c_int, c_size_t, c_uint, c_void_p
+from ctypes import (POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint,
+                    c_void_p)
 from pathlib import Path
 
 _PKG = Path(__file__).resolve().parent
@@ -82,6 +83,18 @@ SIGNATURES = [
     ("symar_probe_barrier", c_int, [c_int, c_int, c_int, POINTER(c_double)]),
     ("symar_llbuffer_bytes", c_size_t, [c_int, c_size_t, c_size_t, c_int, c_int]),
     ("symar_llbuffer_init_sentinel", c_int, [c_void_p, c_size_t, c_void_p]),
+    ("symar_linear", c_int, [c_void_p, c_void_p]),
+    ("symar_kv_required_bytes", c_size_t, []),
+    ("symar_kv_create", c_int, [POINTER(c_void_p)]),
+    ("symar_kv_create_on", c_int, [POINTER(c_void_p), c_void_p, c_size_t]),
+    ("symar_kv_destroy", c_int, [c_void_p]),
+    ("symar_kv_reset", c_int, [c_void_p, c_void_p]),
+    ("symar_kv_status", c_int, [c_void_p, POINTER(c_int), POINTER(c_int), POINTER(c_int)]),
+    ("symar_kv_page_bytes", c_size_t, [c_int, c_int, c_int]),
+    ("symar_rope_table", c_int, [c_void_p, c_int64, c_void_p, c_void_p]),
+    ("symar_kv_append", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    ("symar_kv_read", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    ("symar_kv_attention", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("symar_probe_pingpong_blocks", c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int)]),
 ]
 
@@ -362,6 +375,307 @@ def allreduce_static(in_ptr: int, out_ptr: int, rank_pitch_bytes: int, P: int, c
     library allocates nothing.  Returns the raw status code."""
     return int(load().allreduce_static(in_ptr, out_ptr, rank_pitch_bytes, P, count, dtype,
                                        status_ptr or None, stream))
+
+
+# -- operators between the AllReduces of a decoder layer --
+#
+# These take torch tensors (device memory, strides, dtypes and the current stream); everything is computed in the
+# library's kernels.  Innermost axes must be contiguous; all other strides are free.
+
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
+KV_GROUP, KV_MAX_SEQS = 64, 4096
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [
+        ("x", c_void_p), ("x_ld", c_int64), ("x_group", c_int64),
+        ("w", c_void_p), ("w_ld", c_int64), ("w_group", c_int64),
+        ("bias", c_void_p), ("bias_group", c_int64),
+        ("residual", c_void_p), ("residual_ld", c_int64), ("residual_group", c_int64),
+        ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
+        ("groups", c_int32), ("m", c_int32), ("n", c_int32), ("k", c_int32),
+        ("out_dtype", c_int32), ("act", c_int32), ("root", c_int32),
+    ]
+
+
+class KVCacheArgs(ctypes.Structure):
+    _fields_ = [("pages", c_void_p), ("num_pages", c_int64), ("kv_heads", c_int32), ("head_dim", c_int32),
+                ("page_size", c_int32)]
+
+
+class KVBatchArgs(ctypes.Structure):
+    _fields_ = [("lengths", c_void_p), ("token_start", c_void_p), ("page_table", c_void_p), ("table_ld", c_int64),
+                ("seqs", c_int32), ("tokens", c_int32)]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("base", c_double), ("factor", c_double), ("original", c_double), ("low", c_double), ("high", c_double),
+                ("magnitude", c_double), ("kind", c_int32), ("rot_dim", c_int32)]
+
+
+class KVAppendArgs(ctypes.Structure):
+    _fields_ = [
+        ("q", c_void_p), ("q_ld", c_int64), ("q_head", c_int64),
+        ("q_out", c_void_p), ("q_out_ld", c_int64), ("q_out_head", c_int64),
+        ("k", c_void_p), ("k_ld", c_int64), ("k_head", c_int64),
+        ("v", c_void_p), ("v_ld", c_int64), ("v_head", c_int64),
+        ("rotations", c_void_p), ("rotation_rows", c_int64),
+        ("rot_dim", c_int32), ("interleaved", c_int32), ("q_heads", c_int32), ("dtype", c_int32),
+    ]
+
+
+class KVReadArgs(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("k_ld", c_int64), ("k_head", c_int64),
+                ("v", c_void_p), ("v_ld", c_int64), ("v_head", c_int64), ("dtype", c_int32)]
+
+
+class KVAttentionArgs(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("q_ld", c_int64), ("q_head", c_int64),
+                ("out", c_void_p), ("out_ld", c_int64), ("out_head", c_int64),
+                ("scale", c_float), ("q_heads", c_int32), ("window", c_int32), ("dtype", c_int32)]
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dtype_code(t, where: str) -> int:
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise SymarError(ERR_UNSUPPORTED, f"{where}: dtype {t.dtype}")
+
+
+def _bad(where: str, what: str):
+    raise SymarError(ERR_INVAL, f"{where}: {what}")
+
+
+def _on_device(t, stream):
+    """(context manager that makes t's device current or None, stream handle)."""
+    torch = _torch()
+    index = t.device.index
+    if stream is None:
+        stream = torch.cuda.current_stream(index).cuda_stream
+    return (None if index == torch.cuda.current_device() else torch.cuda.device(index)), stream
+
+
+def _call(fn, where, t, stream, *args) -> None:
+    guard, stream = _on_device(t, stream)
+    if guard is None:
+        _ck(fn(*args, stream), where)
+    else:
+        with guard:
+            _ck(fn(*args, stream), where)
+
+
+def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, stream=None):
+    """``act(x @ w.T + bias) + residual`` (``symar_linear``).
+
+    x [m, k] or [groups, m, k] and w [n, k] or [groups, n, k] bfloat16; bias [n] or [groups, n]; residual and the
+    result [m, n] or [groups, m, n] of ``out_dtype`` (bfloat16 unless said or given by ``out``).  Operands of two
+    dimensions (or expanded ones) are shared by all groups.  ``root``: the one group that adds bias and residual,
+    -1 = every group."""
+    torch = _torch()
+    where = "symar_linear"
+    bf16 = torch.bfloat16
+    if x.dtype is not bf16 or w.dtype is not bf16 or (bias is not None and bias.dtype is not bf16):
+        raise SymarError(ERR_UNSUPPORTED, f"{where}: operands are bfloat16")
+    if not x.is_cuda or x.dim() not in (2, 3) or w.dim() not in (2, 3) or act not in ACTS:
+        _bad(where, "x, w are CUDA tensors of two or three dimensions, act is one of " + ", ".join(ACTS))
+    grouped = x.dim() == 3 or w.dim() == 3
+    groups = x.shape[0] if x.dim() == 3 else (w.shape[0] if grouped else 1)
+    (m, k), n = x.shape[-2:], w.shape[-2]
+    shape = (groups, m, n) if grouped else (m, n)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype or bf16, device=x.device)
+    elif out_dtype is not None and out.dtype is not out_dtype:
+        _bad(where, "out is not of out_dtype")
+    xs, ws, os = x.stride(), w.stride(), out.stride()
+    if w.shape[-1] != k or (w.dim() == 3 and w.shape[0] != groups) or out.shape != shape:
+        _bad(where, f"shapes of x {tuple(x.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)}")
+    if (k > 1 and (xs[-1] != 1 or ws[-1] != 1)) or (n > 1 and os[-1] != 1):
+        _bad(where, "the innermost axis is contiguous")
+    bp = bg = rp = rl = rg = 0
+    if bias is not None:
+        if bias.shape not in ((n,), (groups, n)) or (n > 1 and bias.stride(-1) != 1) or bias.device != x.device:
+            _bad(where, f"bias of shape {tuple(bias.shape)}")
+        bp, bg = bias.data_ptr(), bias.stride(0) if bias.dim() == 2 else 0
+    if residual is not None:
+        if residual.shape not in (shape, (m, n)) or residual.dtype is not out.dtype or (n > 1 and residual.stride(-1) != 1) or \
+                residual.device != x.device:
+            _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
+        rs = residual.stride()
+        rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
+    if w.device != x.device or out.device != x.device:
+        _bad(where, "all tensors are on one device")
+    args = LinearArgs(x.data_ptr(), xs[-2], xs[0] if len(xs) == 3 else 0, w.data_ptr(), ws[-2],
+                      ws[0] if len(ws) == 3 else 0, bp, bg, rp, rl, rg, out.data_ptr(), os[-2],
+                      os[0] if len(os) == 3 else 0, groups, m, n, k, _dtype_code(out, where), ACTS[act], root)
+    _call(load().symar_linear, where, x, stream, byref(args))
+    return out
+
+
+def rope_table(rows: int, rot_dim: int, *, base: float = 10000.0, kind: str = "plain", factor: float = 1.0,
+               original: float = 0.0, low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, device="cuda",
+               stream=None):
+    """[rows, rot_dim/2, 2] float32 (cos, sin) of every position and pair (``symar_rope_table``)."""
+    torch = _torch()
+    if kind not in ROPE_KINDS or rows < 0:
+        _bad("symar_rope_table", f"rows {rows}, kind {kind!r}")
+    table = torch.empty(rows, rot_dim // 2, 2, dtype=torch.float32, device=device)
+    how = RopeScaling(base, factor, original, low, high, magnitude, ROPE_KINDS[kind], rot_dim)
+    _call(load().symar_rope_table, "symar_rope_table", table, stream, table.data_ptr(), rows, byref(how))
+    return table
+
+
+class PagedKV:
+    """A pool of 4-bit key/value pages in a torch uint8 tensor [pages, kv_heads, bytes of one head's page]."""
+
+    def __init__(self, pages, head_dim: int, page_size: int):
+        torch = _torch()
+        each = int(load().symar_kv_page_bytes(1, head_dim, page_size))
+        if not each:
+            raise SymarError(ERR_UNSUPPORTED, f"PagedKV: head_dim {head_dim}, page_size {page_size}")
+        if pages.dtype is not torch.uint8 or pages.dim() != 3 or pages.shape[2] != each or not pages.is_contiguous() or \
+                not pages.is_cuda:
+            _bad("PagedKV", f"pages are a contiguous CUDA uint8 tensor [pages, kv_heads, {each}]")
+        self.pages, self.head_dim, self.page_size, self.kv_heads = pages, head_dim, page_size, pages.shape[1]
+        self.args = KVCacheArgs(pages.data_ptr(), pages.shape[0], pages.shape[1], head_dim, page_size)
+
+    @classmethod
+    def zeros(cls, pages: int, kv_heads: int, head_dim: int, page_size: int, device="cuda") -> "PagedKV":
+        torch = _torch()
+        each = int(load().symar_kv_page_bytes(1, head_dim, page_size))
+        return cls(torch.zeros(pages, kv_heads, each, dtype=torch.uint8, device=device), head_dim, page_size)
+
+
+class KVBatch:
+    """The sequences of a call: int32 CUDA tensors lengths [seqs], page_table [seqs, columns] and, where sequences
+    have other than one new token each, token_start [seqs + 1]."""
+
+    def __init__(self, lengths, page_table, token_start=None):
+        i32 = _torch().int32
+        seqs = lengths.shape[0]
+        if lengths.dtype is not i32 or page_table.dtype is not i32 or lengths.dim() != 1 or page_table.dim() != 2 or \
+                page_table.shape[0] != seqs or (seqs > 1 and lengths.stride(0) != 1) or \
+                (page_table.shape[1] > 1 and page_table.stride(1) != 1) or not lengths.is_cuda or \
+                page_table.device != lengths.device:
+            _bad("KVBatch", "lengths [seqs] and page_table [seqs, columns] are int32 CUDA tensors")
+        # (the row stride doubles as the number of columns that the kernels may read)
+        if seqs > 1 and page_table.stride(0) != page_table.shape[1]:
+            _bad("KVBatch", "page_table is contiguous")
+        if token_start is not None and (token_start.dtype is not i32 or token_start.shape != (seqs + 1,) or
+                                        token_start.stride(0) != 1 or token_start.device != lengths.device):
+            _bad("KVBatch", "token_start [seqs + 1] is an int32 CUDA tensor")
+        self.lengths, self.page_table, self.token_start, self.seqs = lengths, page_table, token_start, seqs
+        self.args = KVBatchArgs(lengths.data_ptr(), token_start.data_ptr() if token_start is not None else None,
+                                page_table.data_ptr(), page_table.shape[1], seqs, 0)
+
+
+class KVContext:
+    """Owner of one ``symar_kv_t``: what the cache operators of one stream share."""
+
+    def __init__(self, device_mem: int | None = None, device_bytes: int = 0, keepalive=None):
+        self._lib = load()
+        self._h = c_void_p()
+        self._keepalive = keepalive
+        if device_mem is None:
+            _ck(self._lib.symar_kv_create(byref(self._h)), "symar_kv_create")
+        else:
+            _ck(self._lib.symar_kv_create_on(byref(self._h), device_mem, device_bytes), "symar_kv_create_on")
+
+    @classmethod
+    def on_torch(cls, device="cuda:0") -> "KVContext":
+        """Context in a torch uint8 tensor."""
+        torch = _torch()
+        n = int(load().symar_kv_required_bytes())
+        buf = torch.empty(n + 256, dtype=torch.uint8, device=device)
+        with torch.cuda.device(buf.device):
+            return cls((buf.data_ptr() + 255) // 256 * 256, n, keepalive=buf)
+
+    def destroy(self) -> None:
+        if self._h:
+            self._lib.symar_kv_destroy(self._h)
+            self._h = c_void_p()
+            self._keepalive = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def reset(self, stream: int = 0) -> None:
+        _ck(self._lib.symar_kv_reset(self._h, stream), "symar_kv_reset")
+
+    def status(self):
+        code, seq, position = c_int(), c_int(), c_int()
+        _ck(self._lib.symar_kv_status(self._h, byref(code), byref(seq), byref(position)), "symar_kv_status")
+        return code.value, seq.value, position.value
+
+    @staticmethod
+    def _rows(where, name, t, tokens, heads, dim, like):
+        if t.shape != (tokens, heads, dim) or t.stride(2) != 1 or t.dtype is not like.dtype or t.device != like.device:
+            _bad(where, f"{name} is [{tokens}, {heads}, {dim}] {like.dtype} on {like.device} with contiguous channels, not "
+                        f"{tuple(t.shape)} {t.dtype} on {t.device}")
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    def append(self, cache: PagedKV, batch: KVBatch, k, v, *, q=None, q_out=None, rotations=None, interleaved: bool = False,
+               stream=None):
+        """Rotate q and k, store k and v (``symar_kv_append``); returns the rotated q (``q_out``, new unless given)."""
+        where = "symar_kv_append"
+        dim, tokens = cache.head_dim, k.shape[0]
+        kr = self._rows(where, "k", k, tokens, cache.kv_heads, dim, k)
+        vr = self._rows(where, "v", v, tokens, cache.kv_heads, dim, k)
+        qr = qo = (None, 0, 0)
+        q_heads = 0
+        if q is not None:
+            q_heads = q.shape[1] if q.dim() == 3 else -1
+            qr = self._rows(where, "q", q, tokens, q_heads, dim, k)
+            if q_out is None:
+                q_out = _torch().empty(tokens, q_heads, dim, dtype=q.dtype, device=q.device)
+            qo = self._rows(where, "q_out", q_out, tokens, q_heads, dim, k)
+        rows = rot = 0
+        if rotations is not None:
+            if rotations.dim() != 3 or rotations.shape[2] != 2 or rotations.dtype is not _torch().float32 or \
+                    not rotations.is_contiguous() or rotations.device != k.device:
+                _bad(where, "rotations are a contiguous float32 tensor [positions, rot_dim / 2, 2]")
+            rows, rot = rotations.shape[0], 2 * rotations.shape[1]
+        args = KVAppendArgs(*qr, *qo, *kr, *vr, rotations.data_ptr() if rotations is not None else None, rows, rot,
+                            1 if interleaved else 0, q_heads, _dtype_code(k, where))
+        batch.args.tokens = tokens
+        _call(self._lib.symar_kv_append, where, k, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+        return q_out
+
+    def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
+        """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
+        torch = _torch()
+        kv = torch.empty(2, tokens, cache.kv_heads, cache.head_dim, dtype=dtype or torch.bfloat16, device=cache.pages.device)
+        k, v = kv[0], kv[1]
+        ld, head = k.stride(0), k.stride(1)
+        args = KVReadArgs(k.data_ptr(), ld, head, v.data_ptr(), ld, head, _dtype_code(k, "symar_kv_read"))
+        batch.args.tokens = tokens
+        _call(self._lib.symar_kv_read, "symar_kv_read", k, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+        return k, v
+
+    def attention(self, cache: PagedKV, batch: KVBatch, q, *, out=None, scale: float = 0.0, window: int = 0, stream=None):
+        """Attention of the batch's new tokens over the cache (``symar_kv_attention``)."""
+        where = "symar_kv_attention"
+        if q.dim() != 3:
+            _bad(where, "q is [tokens, q_heads, head_dim]")
+        tokens, heads = q.shape[0], q.shape[1]
+        if out is None:
+            out = _torch().empty(tokens, heads, cache.head_dim, dtype=q.dtype, device=q.device)
+        args = KVAttentionArgs(*self._rows(where, "q", q, tokens, heads, cache.head_dim, q),
+                               *self._rows(where, "out", out, tokens, heads, cache.head_dim, q), scale, heads, window,
+                               _dtype_code(q, where))
+        batch.args.tokens = tokens
+        _call(self._lib.symar_kv_attention, where, q, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+        return out
 
 
 # -- probes --
