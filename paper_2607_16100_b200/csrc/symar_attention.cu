@@ -6,7 +6,10 @@
 namespace symar {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWarps   = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages  = 5;            // copies in flight per warp: four chunks ahead of the one in use
+constexpr int kMinChunks = 4 * kWarps; // a block's share of the work is at least this many chunks of 16 tokens
 
 struct AttnArgs {
     KvView  c;
@@ -15,63 +18,519 @@ struct AttnArgs {
     __nv_bfloat16 *out;
     int64_t q_ld, q_head, out_ld, out_head;
     float   scale_log2;         // scale * log2(e): softmax in powers of two
-    int     q_heads, window;
+    int     q_heads, share, window, q_vec, out_vec;
     int    *status;
+    unsigned *counters;
+    float  *partials;
 };
 
-// One warp per (token, query head): the running maximum, sum and output of a softmax, one key at a time.
-template <int D>
-__global__ void __launch_bounds__(kThreads) attention_kernel(const AttnArgs a)
+// ---- instructions -----------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on)
 {
-    constexpr int E = D / 32;                       // channels of a lane: c = lane * E ..
-    const int lane = (int)threadIdx.x & 31;
-    const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + (int)threadIdx.x / 32;
-    if (item >= (int64_t)a.b.tokens * a.q_heads) return;
-    const int token = (int)(item / a.q_heads), head = (int)(item - (int64_t)token * a.q_heads);
-    const int kvh = head / (a.q_heads / a.c.kv_heads);
-    int seq = token, pos;
+    const int n = on ? 16 : 0;         // 0: the 16 bytes become zeros and nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void matrices(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void matrices_t(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+// c[16][8] += a[16][16] b[16][8]
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+// Nibbles 0 and 4 of w, less the zero points of which `z` holds 128 + z twice, as two exact bf16: a nibble n under the
+// exponent of 128 is 128 + n, and the difference of two such numbers is exact.
+__device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t z)
+{
+    uint32_t v = (w & 0x000f000fu) | 0x43004300u;
+    __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), *reinterpret_cast<__nv_bfloat162 *>(&z));
+    return *reinterpret_cast<uint32_t *>(&d);
+}
+// 128 + z of two words' zero points
+__device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1) { return (__byte_perm(w0, w1, 0x5410) & 0x000f000fu) | 0x43004300u; }
+
+// ---- the sequences as work ----------------------------------------------------------------
+// An item is `rows` query rows (a token and a head of the key/value head's share, tokens first) of one sequence and one
+// key/value head; its work is the chunks of 16 cached tokens that any of its rows sees, one at least.
+struct Seq {
+    int start, fresh, len;       // first row of q, new tokens, all tokens
+};
+__device__ __forceinline__ Seq sequence(const AttnArgs &a, int b)
+{
+    Seq s;
+    s.len = a.b.lengths[b];
     if (a.b.token_start) {
-        int lo = 0, hi = a.b.seqs;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (a.b.token_start[mid + 1] > token) hi = mid;
-            else lo = mid + 1;
-        }
-        seq = lo;
-        if (seq >= a.b.seqs) return;
-        pos = a.b.lengths[seq] - (a.b.token_start[seq + 1] - token);
+        s.start = max(a.b.token_start[b], 0);
+        s.fresh = max(min(a.b.token_start[b + 1], a.b.tokens) - s.start, 0);
     } else {
-        pos = a.b.lengths[seq] - 1;
+        s.start = b;
+        s.fresh = 1;
     }
-    float q[E], o[E] = {};
-    for (int i = 0; i < E; ++i)
-        q[i] = __bfloat162float(a.q[(int64_t)token * a.q_ld + (int64_t)head * a.q_head + lane * E + i]);
-    float m = -INFINITY, l = 0.0f;
-    const int ps = 1 << a.c.page_shift, grp = lane * E / 64;
-    for (int j = a.window > 0 ? max(0, pos - a.window + 1) : 0; j <= pos; ++j) {
-        const int page = kv_page_of(a.c, a.b, a.status, seq, j);
-        if (page < 0) continue;
-        const unsigned char *base = a.c.pages + page * a.c.page_bytes + kvh * a.c.head_bytes;
-        const int row = j & (ps - 1);
-        const uint32_t *words = reinterpret_cast<const uint32_t *>(base + ps * D);
-        const uint32_t kw = words[row * (D / 64) + grp], vw = words[(ps + row) * (D / 64) + grp];
-        float s = 0.0f, v[E];
-        for (int i = 0; i < E; ++i) {
-            const int c = lane * E + i;
-            const int kn = base[row * (D / 2) + c / 2] >> (4 * (c & 1)) & 15, vn = base[(ps + row) * (D / 2) + c / 2] >> (4 * (c & 1)) & 15;
-            s    = fmaf(q[i], kv_scale(kw) * (float)(kn - kv_zero(kw)), s);
-            v[i] = kv_scale(vw) * (float)(vn - kv_zero(vw));
+    return s;
+}
+struct Item {
+    int lo, chunks;              // first token (a multiple of 16), chunks of 16 tokens
+};
+template <int R>
+__device__ __forceinline__ Item item_of(const AttnArgs &a, const Seq &s, int block)
+{
+    const int first = block * R / a.share, last = min((block * R + R - 1) / a.share, s.fresh - 1);
+    const int64_t most = a.b.table_ld << a.c.page_shift;           // tokens that the table has room for
+    int hi = s.len - s.fresh + last + 1;
+    if (hi > most) hi = (int)most;
+    int lo = a.window > 0 ? max(s.len - s.fresh + first + 1 - a.window, 0) : 0;
+    lo &= ~15;
+    return Item{lo, max((hi - lo + 15) >> 4, 1)};
+}
+template <int R>
+__device__ __forceinline__ int64_t chunks_of(const AttnArgs &a, const Seq &s)
+{
+    const int blocks = (s.fresh * a.share + R - 1) / R;
+    int64_t n = 0;
+    for (int i = 0; i < blocks; ++i) n += item_of<R>(a, s, i).chunks;
+    return n * a.c.kv_heads;
+}
+
+// One softmax over all work of an item, wherever it was done: unnormalised output relative to 2^m, and its sum.
+constexpr float kNothing = -3.402823466e38f;
+
+// S^T = K Q^T and O^T = V^T P^T: the cache's tokens (then its channels) are the sixteen rows of the matrix
+// instruction and eight query rows its columns, so that the eight heads of a share fill it with one token.  A chunk's 16
+// tokens are one warp's own: it copies them to its shared memory four chunks ahead, turns codes into exact bf16
+// whole numbers (n - z) in registers, multiplies, and keeps its own running maximum and sum; warps meet once per
+// piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability before
+// it is rounded to bf16 (V), the one rounding that binary32 arithmetic would not have.
+// The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
+template <int D, int NB>
+__global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attention_kernel(const AttnArgs a)
+{
+    constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2, kUnits = D / 32;
+    constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = 2 * (kCodes + kWords);
+    constexpr int kWarpBytes = kStages * kStage > R * D * 4 ? kStages * kStage : R * D * 4;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int64_t warp_sum[kWarps];
+    __shared__ float   warp_m[kWarps][R], warp_l[kWarps][R];
+    __shared__ int     page_ok[kWarps][kStages];
+    __shared__ int64_t at_flat;
+    __shared__ int     at_seq, is_last;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    unsigned char *mine = smem + warp * kWarpBytes;
+    const uint32_t mine_addr = smem_addr(mine);
+
+    // ---- this block's share: chunks [begin, end) of all items in order ----
+    const int each = (a.b.seqs + kThreads - 1) / kThreads;
+    const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
+    int64_t own = 0;
+    for (int b = s0; b < s1; ++b) own += chunks_of<R>(a, sequence(a, b));
+    int64_t incl = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) incl += total;
+        total += warp_sum[w];
+    }
+    const int64_t per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinChunks);
+    const int64_t begin = per * blockIdx.x, end = min(begin + per, total);
+    if (begin >= total) return;
+    if (begin >= incl - own && begin < incl) {
+        int64_t flat = incl - own;
+        for (int b = s0; b < s1; ++b) {
+            const int64_t n = chunks_of<R>(a, sequence(a, b));
+            if (begin < flat + n) {
+                at_seq  = b;
+                at_flat = flat;
+                break;
+            }
+            flat += n;
         }
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        s *= a.scale_log2;
-        const float top = fmaxf(m, s), keep = m == -INFINITY ? 0.0f : exp2f(m - top), p = exp2f(s - top);
-        l = fmaf(l, keep, p);
-        for (int i = 0; i < E; ++i) o[i] = fmaf(o[i], keep, p * v[i]);
-        m = top;
     }
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
-    for (int i = 0; i < E; ++i)
-        a.out[(int64_t)token * a.out_ld + (int64_t)head * a.out_head + lane * E + i] = __float2bfloat16_rn(o[i] * inv);
+    __syncthreads();
+    int seq = at_seq;
+    int64_t item_at = at_flat;                       // flat index of the current item's first chunk
+    Seq  s   = sequence(a, seq);
+    int  block = 0, head = 0;
+    Item item = item_of<R>(a, s, 0);
+    while (item_at + (int64_t)item.chunks * a.c.kv_heads <= begin) {
+        item_at += (int64_t)item.chunks * a.c.kv_heads;
+        item = item_of<R>(a, s, ++block);
+    }
+    head = (int)((begin - item_at) / item.chunks);
+    item_at += (int64_t)head * item.chunks;
+
+    const int ps = 1 << a.c.page_shift;
+    int64_t flat = begin;
+    while (flat < end) {
+        const int c_begin = (int)(flat - item_at), c_end = (int)min((int64_t)item.chunks, end - item_at);
+        if (tid == 0 && s.len > (a.b.table_ld << a.c.page_shift)) kv_record(a.status, seq, (int)(a.b.table_ld << a.c.page_shift));
+        // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
+        uint32_t qf[NB][NG * 4][2];
+        int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
+        const int rows = s.fresh * a.share;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int row = block * R + nb * 8 + g;
+            const bool on = row < rows;
+            const int tok = on ? row / a.share : 0, hh = on ? row - tok * a.share : 0;
+            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const __nv_bfloat16 *p = src + gr * 64 + half * 32 + t * 8;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (on && a.q_vec) {
+                        v = *reinterpret_cast<const uint4 *>(p);
+                    } else if (on) {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                                       h[6] | (uint32_t)h[7] << 16);
+                    }
+                    qf[nb][gr * 4 + 0][half] = __byte_perm(v.x, v.z, 0x5410);       // channels i and i + 4 of eight
+                    qf[nb][gr * 4 + 1][half] = __byte_perm(v.x, v.z, 0x7632);
+                    qf[nb][gr * 4 + 2][half] = __byte_perm(v.y, v.w, 0x5410);
+                    qf[nb][gr * 4 + 3][half] = __byte_perm(v.y, v.w, 0x7632);
+                }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = block * R + nb * 8 + 2 * t + j;
+                hi[nb][j] = 0x7fffffff;                                             // a row of padding masks nothing
+                lo[nb][j] = 0;
+                if (r < rows) {
+                    hi[nb][j] = s.len - s.fresh + r / a.share + 1;
+                    lo[nb][j] = a.window > 0 ? max(hi[nb][j] - a.window, 0) : 0;
+                }
+            }
+        }
+        {
+            const int first = block * R / a.share, last = min((block * R + R - 1) / a.share, s.fresh - 1);
+            least_hi = s.len - s.fresh + first + 1;
+            most_lo  = a.window > 0 ? s.len - s.fresh + last + 1 - a.window : 0;
+        }
+
+        float o[NB][NG * 4][4], m[NB][2], l[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int i = 0; i < NG * 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[nb][i][j] = 0.0f;
+            m[nb][0] = m[nb][1] = kNothing;
+            l[nb][0] = l[nb][1] = 0.0f;
+        }
+
+        // ---- this warp's chunks: c_begin + warp, + kWarps, ... ----
+        const int n = c_end - c_begin > warp ? (c_end - c_begin - warp + kWarps - 1) / kWarps : 0;
+        int pages = -1;                                       // lane i: the page of the warp's chunk (k & ~31) + i
+        auto token_of = [&](int k) { return item.lo + (c_begin + warp + k * kWarps) * 16; };
+        auto fetch = [&](int k) {
+            if (k < n) {
+                if ((k & 31) == 0) {
+                    const int tok = token_of(k + lane);
+                    pages = k + lane < n && tok < s.len ? kv_page_of(a.c, a.b, a.status, seq, tok) : -1;
+                }
+                const int page = __shfl_sync(0xffffffffu, pages, k & 31);
+                const int st = k % kStages, slot = token_of(k) & (ps - 1);
+                const bool on = page >= 0;
+                const unsigned char *base = a.c.pages + (on ? page : 0) * a.c.page_bytes + head * a.c.head_bytes;
+                const uint32_t dst = mine_addr + st * kStage;
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    const unsigned char *src = base + (side * ps + slot) * kRow;
+#pragma unroll
+                    for (int u0 = 0; u0 < 16 * kUnits; u0 += 32) {
+                        const int u = u0 + lane, tok = u / kUnits, c = u % kUnits;
+                        const int turn = D == 64 ? tok >> 2 & 1 : (D == 128 ? tok >> 1 & 3 : tok & 7);
+                        copy16(dst + side * kCodes + tok * kRow + ((c ^ turn) << 4), src + u * 16, on);
+                    }
+                }
+                if (lane < 8 * NG) {
+                    const int side = lane / (4 * NG), u = lane % (4 * NG);
+                    copy16(dst + 2 * kCodes + side * kWords + u * 16, base + ps * D + (side * ps + slot) * NG * 4 + u * 16, on);
+                }
+                if (lane == 0) page_ok[warp][st] = on;
+            }
+            copies_commit();
+        };
+#pragma unroll
+        for (int k = 0; k < kStages - 1; ++k) fetch(k);
+        for (int k = 0; k < n; ++k) {
+            copies_wait<kStages - 2>();
+            __syncwarp();
+            fetch(k + kStages - 1);
+            const int st = k % kStages, tok0 = token_of(k);
+            const uint32_t base = mine_addr + st * kStage;
+            const unsigned char *stage = mine + st * kStage;
+            // lane i names row i % 8 of matrix i / 8: tokens 0-7 and 8-15, first and second 32 channels of the group
+            const int mt = (lane >> 4) * 8 + (lane & 7), mc = lane >> 3 & 1;
+            const int turn = D == 64 ? mt >> 2 & 1 : (D == 128 ? mt >> 1 & 3 : mt & 7);
+            const uint32_t *kw = reinterpret_cast<const uint32_t *>(stage + 2 * kCodes), *vw = kw + 16 * NG;
+
+            float sc[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[nb][j] = 0.0f;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                uint32_t r[4];
+                matrices(r, base + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
+                const uint32_t w0 = kw[g * NG + gr], w1 = kw[(g + 8) * NG + gr];
+                const uint32_t z0 = zeros_of(w0, w0), z1 = zeros_of(w1, w1);
+                float acc[NB][4];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[nb][j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = nibbles(r[0] >> 4 * i, z0), a1 = nibbles(r[2] >> 4 * i, z1);
+                    const uint32_t a2 = nibbles(r[1] >> 4 * i, z0), a3 = nibbles(r[3] >> 4 * i, z1);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma(acc[nb], a0, a1, a2, a3, qf[nb][gr * 4 + i][0], qf[nb][gr * 4 + i][1]);
+                }
+                const float f0 = kv_scale(w0) * a.scale_log2, f1 = kv_scale(w1) * a.scale_log2;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    sc[nb][0] = __fmaf_rn(acc[nb][0], f0, sc[nb][0]);
+                    sc[nb][1] = __fmaf_rn(acc[nb][1], f0, sc[nb][1]);
+                    sc[nb][2] = __fmaf_rn(acc[nb][2], f1, sc[nb][2]);
+                    sc[nb][3] = __fmaf_rn(acc[nb][3], f1, sc[nb][3]);
+                }
+            }
+            // rows of the fragment: tokens tok0 + g (0, 1) and tok0 + g + 8 (2, 3); columns 2t and 2t + 1
+            const bool whole = tok0 + 16 <= least_hi && tok0 >= most_lo && page_ok[warp][st];
+            if (!whole) {
+                const bool some = page_ok[warp][st];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int tok = tok0 + g + (j >> 1) * 8;
+                        if (!some || tok >= hi[nb][j & 1] || tok < lo[nb][j & 1] || tok >= s.len) sc[nb][j] = -INFINITY;
+                    }
+            }
+            bool rise = false;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) rise |= fmaxf(sc[nb][j], sc[nb][j + 2]) > m[nb][j] + 8.0f;
+            if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float top = fmaxf(sc[nb][j], sc[nb][j + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        top = fmaxf(top, m[nb][j]);
+                        const float keep = power2(m[nb][j] - top);
+                        m[nb][j] = top;
+                        l[nb][j] *= keep;
+#pragma unroll
+                        for (int i = 0; i < NG * 4; ++i) {
+                            o[nb][i][j] *= keep;
+                            o[nb][i][j + 2] *= keep;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[nb][j] = power2(sc[nb][j] - m[nb][j & 1]);
+                l[nb][0] += sc[nb][0] + sc[nb][2];
+                l[nb][1] += sc[nb][1] + sc[nb][3];
+            }
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                uint32_t r[4], pf[NB][2];
+                matrices_t(r, base + kCodes + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
+                // beyond the sequence's end a page holds anything: no scale from there may meet a probability of 0
+                float f0 = kv_scale(vw[g * NG + gr]), f1 = kv_scale(vw[(g + 8) * NG + gr]);
+                if (!whole) {
+                    f0 = tok0 + g < s.len ? f0 : 0.0f;
+                    f1 = tok0 + g + 8 < s.len ? f1 : 0.0f;
+                }
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    pf[nb][0] = transposed(pack_bf16(sc[nb][0] * f0, sc[nb][1] * f0));
+                    pf[nb][1] = transposed(pack_bf16(sc[nb][2] * f1, sc[nb][3] * f1));
+                }
+                const uint32_t z0 = zeros_of(vw[2 * t * NG + gr], vw[(2 * t + 1) * NG + gr]);
+                const uint32_t z1 = zeros_of(vw[(2 * t + 8) * NG + gr], vw[(2 * t + 9) * NG + gr]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = nibbles(r[0] >> 4 * i, z0), a1 = nibbles(r[1] >> 4 * i, z0);
+                    const uint32_t a2 = nibbles(r[2] >> 4 * i, z1), a3 = nibbles(r[3] >> 4 * i, z1);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
+                }
+            }
+        }
+        copies_wait<0>();
+
+        // ---- the warps' results become one ----
+        // fragment i of a group: channels 4 g + i (0, 1) and 32 + 4 g + i (2, 3) of it
+        float *wo = reinterpret_cast<float *>(mine);
+        __syncwarp();
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float sum = l[nb][j];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                const int row = nb * 8 + 2 * t + j;
+                if (g == 0) {
+                    warp_m[warp][row] = m[nb][j];
+                    warp_l[warp][row] = sum;
+                }
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        *reinterpret_cast<float4 *>(wo + row * D + gr * 64 + half * 32 + 4 * g) =
+                            make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half],
+                                        o[nb][gr * 4 + 2][j + 2 * half], o[nb][gr * 4 + 3][j + 2 * half]);
+            }
+        __syncthreads();
+        const bool all = c_begin == 0 && c_end == item.chunks;
+        float *slot = a.partials + (size_t)(2 * blockIdx.x + (c_begin == 0 ? 1 : 0)) * (R * (D + 2));
+        auto store = [&](int row, int d, float4 v, float sum) {
+            const int r = block * R + row;
+            if (r >= rows) return;
+            const int tok = r / a.share, hh = r - tok * a.share;
+            const float f = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+            __nv_bfloat16 *p = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head + d;
+            const uint32_t x = pack_bf16(v.x * f, v.y * f), y = pack_bf16(v.z * f, v.w * f);
+            if (a.out_vec) {
+                *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
+            } else {
+                uint16_t *h = reinterpret_cast<uint16_t *>(p);
+                h[0] = (uint16_t)x; h[1] = (uint16_t)(x >> 16); h[2] = (uint16_t)y; h[3] = (uint16_t)(y >> 16);
+            }
+        };
+        for (int i = tid; i < R * D / 4; i += kThreads) {
+            const int row = i / (D / 4), d = i % (D / 4) * 4;
+            float top = kNothing, sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, warp_m[w][row]);
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = power2(warp_m[w][row] - top);
+                const float4 x = *reinterpret_cast<const float4 *>(smem + w * kWarpBytes + (row * D + d) * 4);
+                sum = __fmaf_rn(warp_l[w][row], f, sum);
+                v.x = __fmaf_rn(x.x, f, v.x); v.y = __fmaf_rn(x.y, f, v.y);
+                v.z = __fmaf_rn(x.z, f, v.z); v.w = __fmaf_rn(x.w, f, v.w);
+            }
+            if (all) {
+                store(row, d, v, sum);
+            } else {
+                *reinterpret_cast<float4 *>(slot + 2 * R + row * D + d) = v;
+                if (d == 0) {
+                    slot[row]     = top;
+                    slot[R + row] = sum;
+                }
+            }
+        }
+        if (!all) {
+            // ---- an item that several blocks share: the last to come joins their results, in the blocks' order ----
+            const int64_t first = item_at / per, last = (item_at + item.chunks - 1) / per;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const unsigned before = atomicAdd(&a.counters[first], 1u);
+                is_last = before == (unsigned)(last - first);
+                if (is_last) a.counters[first] = 0;
+                __threadfence();
+            }
+            __syncthreads();
+            if (is_last) {
+                for (int i = tid; i < R * D / 4; i += kThreads) {
+                    const int row = i / (D / 4), d = i % (D / 4) * 4;
+                    float top = kNothing, sum = 0.0f;
+                    for (int64_t x = first; x <= last; ++x)
+                        top = fmaxf(top, __ldcg(a.partials + (size_t)(2 * x + (x == first ? 1 : 0)) * (R * (D + 2)) + row));
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    for (int64_t x = first; x <= last; ++x) {
+                        const float *p = a.partials + (size_t)(2 * x + (x == first ? 1 : 0)) * (R * (D + 2));
+                        const float f = power2(__ldcg(p + row) - top);
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + 2 * R + row * D + d));
+                        sum = __fmaf_rn(__ldcg(p + R + row), f, sum);
+                        v.x = __fmaf_rn(y.x, f, v.x); v.y = __fmaf_rn(y.y, f, v.y);
+                        v.z = __fmaf_rn(y.z, f, v.z); v.w = __fmaf_rn(y.w, f, v.w);
+                    }
+                    store(row, d, v, sum);
+                }
+            }
+        }
+        __syncthreads();                                        // the shared memory is free for the next piece
+
+        // ---- next ----
+        flat = item_at + c_end;
+        if (c_end == item.chunks && flat < end) {
+            item_at = flat;
+            if (++head == a.c.kv_heads) {
+                head = 0;
+                if (++block >= (rows + R - 1) / R) {
+                    block = 0;
+                    do s = sequence(a, ++seq);
+                    while (s.fresh == 0);
+                }
+                item = item_of<R>(a, s, block);
+            }
+        }
+    }
+}
+
+template <int D, int NB>
+cudaError_t launch(const AttnArgs &a, int num_sms, cudaStream_t stream)
+{
+    constexpr int R = 8 * NB, kStage = 16 * D + 16 * (D / 64) * 8;
+    constexpr int kWarpBytes = kStages * kStage > R * D * 4 ? kStages * kStage : R * D * 4;
+    constexpr int kBytes = kWarps * kWarpBytes;
+    cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    const int blocks = num_sms * (NB == 1 && D <= 128 ? 2 : 1);
+    attention_kernel<D, NB><<<blocks < kAttnMaxBlocks ? blocks : kAttnMaxBlocks, kThreads, kBytes, stream>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -102,12 +561,18 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     a.q_heads    = args->q_heads;
     a.window     = args->window;
     a.status     = kv->status;
-    const int64_t items = (int64_t)a.b.tokens * a.q_heads, blocks = (items + kThreads / 32 - 1) / (kThreads / 32);
-    if (blocks > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (a.c.dim == 64) attention_kernel<64><<<(unsigned)blocks, kThreads, 0, s>>>(a);
-    else if (a.c.dim == 128) attention_kernel<128><<<(unsigned)blocks, kThreads, 0, s>>>(a);
-    else attention_kernel<256><<<(unsigned)blocks, kThreads, 0, s>>>(a);
-    cudaError_t e = cudaGetLastError();
+    a.share      = args->q_heads / cache->kv_heads;
+    a.q_vec      = (uintptr_t)args->q % 16 == 0 && args->q_ld % 8 == 0 && args->q_head % 8 == 0;
+    a.out_vec    = (uintptr_t)args->out % 8 == 0 && args->out_ld % 4 == 0 && args->out_head % 4 == 0;
+    a.counters   = kv->counters;
+    a.partials   = kv->partials;
+    if ((int64_t)a.b.tokens * a.share > 0x7fff0000) return SYMAR_ERR_UNSUPPORTED;
+    // eight rows where no sequence is likely to have more: a row block of sixteen halves the work per cached token
+    const bool wide = (int64_t)a.b.tokens * a.share > 8ll * a.b.seqs;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    if (a.c.dim == 64) e = wide ? launch<64, 2>(a, kv->num_sms, st) : launch<64, 1>(a, kv->num_sms, st);
+    else if (a.c.dim == 128) e = wide ? launch<128, 2>(a, kv->num_sms, st) : launch<128, 1>(a, kv->num_sms, st);
+    else e = wide ? launch<256, 2>(a, kv->num_sms, st) : launch<256, 1>(a, kv->num_sms, st);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_attention");
 }

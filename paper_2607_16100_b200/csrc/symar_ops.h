@@ -21,8 +21,8 @@ struct symar_kv {
 namespace symar {
 
 // ---- sizes of the attention grid that the context has room for ----
-constexpr int kAttnMaxBlocks = 1024;      // blocks of the largest attention grid
-constexpr int kAttnMaxRows   = 32;        // query rows of a block
+constexpr int kAttnMaxBlocks = 512;      // blocks of the largest attention grid
+constexpr int kAttnMaxRows   = 16;        // query rows of a block
 constexpr int kAttnMaxDim    = 256;
 
 constexpr size_t kKvCtrOff  = 256;
