@@ -453,9 +453,11 @@ typedef enum {
  * the tensor cores, whose additions truncate, are added up in IEEE binary32 every 128 products.
  * root: the one group that adds bias and residual; -1 = every group.  (Of P partial products that an AllReduce
  * will add, one rank carries the bias and the residual.)
- * group strides of 0 share an operand; an out_group of 0 is an error where groups > 1.  m, n or k of 0 is allowed
- * (k = 0: the product is 0).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
- * are read by the copy engine, others element by element.                                       */
+ * group strides of 0 share an operand; an out_group of 0 is an error where groups > 1, as is an out_ld below n.  m, n
+ * or k of 0 is allowed (k = 0: the product is 0).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
+ * are read by the copy engine, others by the block's threads.
+ * status: optional device word (may be NULL), cleared on the stream before the launch and set to SYMAR_ERR_TIMEOUT if a
+ * wait inside the kernel (for its own copies and products, four seconds at most) gave up; `out` is then incomplete.   */
 typedef struct {
     const void *x;        int64_t x_ld, x_group;
     const void *w;        int64_t w_ld, w_group;
@@ -466,6 +468,7 @@ typedef struct {
     int32_t     out_dtype;        /* symar_dtype_t */
     int32_t     act;              /* symar_act_t   */
     int32_t     root;
+    uint32_t   *status;
 } symar_linear_t;
 int symar_linear(const symar_linear_t *args, void *cuda_stream);
 

@@ -1,4 +1,15 @@
-// out_g = act(x_g w_g^T + bias_g) + residual_g, one matrix per rank (formulas in include/symar.h).
+// out_g = act(x_g w_g^T + bias_g) + residual_g, one matrix per rank (formulas in include/symar.h), on the fifth
+// generation's tensor cores.
+//
+// The weights are the 128 rows of every matrix instruction and the tokens its columns, 16 to 256 of them: with one
+// token or a few, as in a decode step, every instruction still uses all 128 lanes and the kernel is a stream of the
+// weights; with many it is an ordinary product of 128 x 256 tiles.  A block is one producer (the copy engine
+// fills a ring of 64-wide slices of both operands), one thread that issues the products, and four warps that take
+// finished accumulators out of tensor memory, where the next tile is already being summed in the other half.
+#include <cuda.h>
+
+#include <type_traits>
+
 #include "symar_ops.h"
 
 namespace symar {
@@ -10,7 +21,107 @@ struct LinearArgs {
     void       *out;
     int64_t x_ld, x_group, w_ld, w_group, bias_group, residual_ld, residual_group, out_ld, out_group;
     int     m, n, k, act, root;
+    int     n_tiles, m_tiles, tiles;       // of 128 channels, of NT tokens, of all groups
+    int     split;                         // blocks of a cluster that share a tile's k
+    unsigned *status;
 };
+
+constexpr int kRows = 128, kSlice = 64;    // channels of a tile; k of a stage: 128 bytes, one swizzled row
+constexpr int kMaxSplit = 8;
+constexpr uint64_t kWaitNs = 4000000000ull;
+
+// ---- instructions -----------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ uint64_t now_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// A warp's wait; false for all its lanes once it has lasted four seconds or another role has given up.
+__device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    const uint64_t t0 = now_ns();
+    for (;;) {
+        for (int i = 0; i < 256; ++i)
+            if (bar_try(bar, parity)) return true;
+        if (*failed || now_ns() - t0 > kWaitNs) {
+            *failed = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    bool ok = false;
+    for (int i = 0; i < 16 && !ok; ++i) ok = bar_try(bar, parity);
+    if (!ok) ok = bar_wait_long(bar, parity, failed);
+    return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// shared-memory operand: rows of 128 bytes, swizzled in blocks of eight
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t how, uint32_t add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(acc),
+                 "l"(a), "l"(b), "r"(how), "r"(add) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// sixteen columns of this warp's 32 lanes; the wait is the caller's
+__device__ __forceinline__ void acc_load16(uint32_t addr, float *v)
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float peer_load(uint32_t addr, int rank)
+{
+    uint32_t there;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
 
 __device__ __forceinline__ float activate(float y, int act)
 {
@@ -27,39 +138,381 @@ __device__ __forceinline__ float as_f32(__nv_bfloat16 v) { return __bfloat162flo
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
-constexpr int kTile = 64, kStep = 16;
-
-template <typename O>
-__global__ void __launch_bounds__(256) linear_kernel(const LinearArgs a)
+// Eight elements of a row from element k0 on, zeros beyond its end, where rows lie on no 16-byte boundary: the two
+// aligned vectors around them, shifted into place, unless one of those reaches out of the row.
+__device__ __forceinline__ uint4 row_chunk(const __nv_bfloat16 *row, int k0, int k)
 {
-    __shared__ float xs[kStep][kTile + 1], ws[kStep][kTile + 1];
-    const int g = blockIdx.z, m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-    const __nv_bfloat16 *x = a.x + g * a.x_group, *w = a.w + g * a.w_group;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < a.k; k0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-            const int r = i / kStep, k = k0 + i % kStep;
-            xs[i % kStep][r] = m0 + r < a.m && k < a.k ? __bfloat162float(x[(int64_t)(m0 + r) * a.x_ld + k]) : 0.0f;
-            ws[i % kStep][r] = n0 + r < a.n && k < a.k ? __bfloat162float(w[(int64_t)(n0 + r) * a.w_ld + k]) : 0.0f;
+    if (k0 >= k) return make_uint4(0, 0, 0, 0);
+    const uintptr_t p = (uintptr_t)(row + k0), base = p & ~(uintptr_t)15;
+    const int shift = (int)(p - base);
+    if (shift == 0 && k0 + 8 <= k) return __ldg(reinterpret_cast<const uint4 *>(p));
+    if (base >= (uintptr_t)row && base + 32 <= (uintptr_t)(row + k)) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(base)), v = __ldg(reinterpret_cast<const uint4 *>(base) + 1);
+        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        if (shift & 8) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
         }
-        __syncthreads();
-        for (int k = 0; k < kStep; ++k)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[k][ty + 16 * i], ws[k][tx + 16 * j], acc[i][j]);
+        if (shift & 4) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+        }
+        if (shift & 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    const uint16_t *h = reinterpret_cast<const uint16_t *>(row + k0);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (k0 + i < k) w[i >> 1] |= (uint32_t)h[i] << ((i & 1) * 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int NT, bool kWide, bool kTma>
+struct Shape {
+    static constexpr int kThreads = kTma ? 256 : 512;             // without the copy engine eight more warps load
+    static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
+    static constexpr int kStages = NT >= 256 ? 4 : (NT == 128 ? 6 : (NT == 64 ? 8 : 10));
+    static constexpr int kBytes = kStages * kStage + 1024;        // (the ring starts on a 1 KiB boundary)
+    static constexpr int kCols  = 2 * NT < 32 ? 32 : 2 * NT;      // two accumulators
+};
+constexpr int kChunk = 2;          // slices that a float32 result sums in the tensor cores at a time
+
+// kWide: float32 results (and the sums of 128 products added up in registers)
+template <int NT, bool kWide, bool kTma>
+__global__ void __launch_bounds__(Shape<NT, kWide, kTma>::kThreads, 1)
+linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const LinearArgs a)
+{
+    using S = Shape<NT, kWide, kTma>;
+    using O = typename std::conditional<kWide, float, __nv_bfloat16>::type;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed;
+    unsigned char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    const uint32_t ring_addr = smem_addr(ring);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(full + 8 * i, kTma ? 1 : 256);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(acc_full + 8 * i, 1);
+            bar_init(acc_empty + 8 * i, 128);
+        }
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_at;
+
+    // This block's slices of every one of its tiles: all of k, or its part where a cluster shares the tile.
+    const int slices = (a.k + kSlice - 1) / kSlice, rank = a.split > 1 ? (int)blockIdx.x % a.split : 0;
+    const int k_lo = (int)((int64_t)slices * rank / a.split), k_hi = (int)((int64_t)slices * (rank + 1) / a.split);
+    const int first = (int)blockIdx.x / a.split, step = (int)gridDim.x / a.split;
+    // up to sixteen tiles of tokens run through a column of weights before the next: at one time few weights and all
+    // of their tokens are read, from L2 after the first
+    auto place = [&](int tile, int &g, int &m0, int &n0) {
+        const int per = a.n_tiles * a.m_tiles;
+        g = tile / per;
+        int i = tile - g * per;
+        const int band = 16 * a.n_tiles, b = i / band, wide = min(16, a.m_tiles - 16 * b);
+        i -= b * band;
+        m0 = (16 * b + i % wide) * NT;
+        n0 = i / wide * kRows;
+    };
+
+    if (kTma ? warp == 0 : warp >= 8) {
+        // ---- producer ----
+        int st = 0, round = 0;
+        for (int tile = first; tile < a.tiles; tile += step) {
+            int g, m0, n0;
+            place(tile, g, m0, n0);
+            for (int ks = k_lo; ks < k_hi; ++ks) {
+                if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                const uint32_t at = ring_addr + st * S::kStage;
+                if (kTma) {
+                    if (lane == 0) {
+                        bar_expect(full + 8 * st, S::kStage);
+                        tma_load(at, &wmap, ks * kSlice, n0, a.w_group ? g : 0, full + 8 * st);
+                        tma_load(at + S::kA, &xmap, ks * kSlice, m0, a.x_group ? g : 0, full + 8 * st);
+                    }
+                    __syncwarp();
+                } else {
+                    const __nv_bfloat16 *w = a.w + g * a.w_group, *x = a.x + g * a.x_group;
+                    unsigned char *dst = ring + st * S::kStage;
+#pragma unroll 4
+                    for (int i = tid - 256; i < (kRows + NT) * 8; i += 256) {
+                        const int r = i >> 3, c = i & 7;
+                        const bool is_w = r < kRows;
+                        const int row = is_w ? n0 + r : m0 + r - kRows;
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (row < (is_w ? a.n : a.m))
+                            v = row_chunk((is_w ? w + row * a.w_ld : x + row * a.x_ld), ks * kSlice + c * 8, a.k);
+                        *reinterpret_cast<uint4 *>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = v;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    bar_arrive(full + 8 * st);
+                }
+                if (++st == S::kStages) st = 0, ++round;
+            }
+        }
+    } else if (warp == 1) {
+        // ---- products ----
+        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
+        int st = 0, round = 0;
+        uint32_t turn = 0;                              // accumulators filled so far
+        for (int tile = first; tile < a.tiles; tile += step) {
+            for (int ks = k_lo; ks < k_hi;) {
+                const int to = kWide ? min(ks + kChunk, k_hi) : k_hi;
+                const uint32_t buf = turn & 1, acc = tmem + buf * NT;
+                if (turn >= 2 && !bar_wait(acc_empty + 8 * buf, ((turn >> 1) - 1) & 1, &failed)) goto done;
+                tc_after();
+                for (int from = ks; ks < to; ++ks) {
+                    if (!bar_wait(full + 8 * st, round & 1, &failed)) goto done;
+                    tc_after();
+                    if (lane == 0) {
+                        const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
+#pragma unroll
+                        for (int i = 0; i < kSlice / 16; ++i) product(acc, w + 2 * i, x + 2 * i, kHow, ks > from || i > 0);
+                        commit(empty + 8 * st);
+                        if (ks + 1 == to) commit(acc_full + 8 * buf);
+                    }
+                    __syncwarp();
+                    if (++st == S::kStages) st = 0, ++round;
+                }
+                ++turn;
+            }
+        }
+    } else if (warp >= 4 && warp < 8) {
+        // ---- results: this thread is one channel of the tile, its registers are tokens ----
+        const int quarter = warp - 4, ch = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        const bool parts = k_hi > k_lo;
+        uint32_t turn = 0;
+        for (int tile = first; tile < a.tiles; tile += step) {
+            int g, m0, n0;
+            place(tile, g, m0, n0);
+            const int n = n0 + ch, tokens = min(NT, a.m - m0);
+            const bool mine = a.root < 0 || a.root == g, on = n < a.n;
+            const float bias = mine && a.bias && on ? __bfloat162float(a.bias[g * a.bias_group + n]) : 0.0f;
+            const O *res = mine && a.residual ? static_cast<const O *>(a.residual) + g * a.residual_group + (int64_t)m0 * a.residual_ld + n : nullptr;
+            O *out = static_cast<O *>(a.out) + g * a.out_group + (int64_t)m0 * a.out_ld + n;
+            auto finish16 = [&](const float *v, int c0) {
+                if (!on) return;
+                float r[16];
+                if (res) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = c0 + i < tokens ? as_f32(res[(int64_t)(c0 + i) * a.residual_ld]) : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (c0 + i >= tokens) break;
+                    float y = activate(v[i] + bias, a.act);
+                    if (res) y += r[i];
+                    put(out + (int64_t)(c0 + i) * a.out_ld, y);
+                }
+            };
+            float sum[kWide ? NT : 16];
+            if (kWide) {
+#pragma unroll
+                for (int i = 0; i < (kWide ? NT : 16); ++i) sum[i] = 0.0f;
+                for (int ks = k_lo; ks < k_hi; ks += kChunk, ++turn) {
+                    const uint32_t buf = turn & 1;
+                    if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    tc_after();
+#pragma unroll
+                    for (int c0 = 0; c0 < NT; c0 += 16) {
+                        float v[16];
+                        acc_load16(tmem + lanes + buf * NT + c0, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[kWide ? c0 + i : i] += v[i];
+                    }
+                    tc_before();
+                    bar_arrive(acc_empty + 8 * buf);
+                }
+            }
+            const uint32_t buf = turn & 1;
+            if (!kWide && parts) {
+                if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                tc_after();
+            }
+            float *part = reinterpret_cast<float *>(ring);            // [token][channel], the ring is not in use any more
+#pragma unroll
+            for (int c0 = 0; c0 < NT; c0 += 16) {
+                if (c0 >= tokens) break;
+                float v[16];
+                if (kWide) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = sum[kWide ? c0 + i : i];
+                } else if (parts) {
+                    acc_load16(tmem + lanes + buf * NT + c0, v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                }
+                if (a.split > 1) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) part[(c0 + i) * kRows + ch] = v[i];
+                } else {
+                    finish16(v, c0);
+                }
+            }
+            if (!kWide && parts) {
+                tc_before();
+                bar_arrive(acc_empty + 8 * buf);
+                ++turn;
+            }
+        }
+    }
+done:
+    __syncwarp();
+    if (a.split > 1) {
+        // ---- the cluster's parts of the tile: block r sums tokens r, r + split, ... over the blocks in order ----
+        cluster_sync();
+        int g, m0, n0;
+        place(first, g, m0, n0);
+        const int n = n0 + (tid & 127), tokens = min(NT, a.m - m0);
+        if (n < a.n) {
+            const bool mine = a.root < 0 || a.root == g;
+            const float bias = mine && a.bias ? __bfloat162float(a.bias[g * a.bias_group + n]) : 0.0f;
+            for (int t = rank + a.split * (tid >> 7); t < tokens; t += a.split * (S::kThreads / 128)) {
+                const uint32_t at = ring_addr + (t * kRows + (tid & 127)) * 4;
+                float v[kMaxSplit], y = 0.0f;
+#pragma unroll
+                for (int r = 0; r < kMaxSplit; ++r) v[r] = r < a.split ? peer_load(at, r) : 0.0f;
+#pragma unroll
+                for (int r = 0; r < kMaxSplit; ++r) y += v[r];
+                y = activate(y + bias, a.act);
+                if (mine && a.residual)
+                    y += as_f32(static_cast<const O *>(a.residual)[g * a.residual_group + (int64_t)(m0 + t) * a.residual_ld + n]);
+                put(static_cast<O *>(a.out) + g * a.out_group + (int64_t)(m0 + t) * a.out_ld + n, y);
+            }
+        }
+        cluster_sync();                                   // no block leaves while its part may be read
+    }
+    tc_before();
+    __syncthreads();
+    if (failed) {
+        // copies and products may still be in flight: give them time to end before the memory is let go
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (tid == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_TIMEOUT);
         __syncthreads();
     }
-    const bool mine = a.root < 0 || a.root == g;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m >= a.m || n >= a.n) continue;
-            float y = acc[i][j];
-            if (mine && a.bias) y += __bfloat162float(a.bias[g * a.bias_group + n]);
-            y = activate(y, a.act);
-            if (mine && a.residual) y += as_f32(static_cast<const O *>(a.residual)[g * a.residual_group + m * a.residual_ld + n]);
-            put(static_cast<O *>(a.out) + g * a.out_group + m * a.out_ld + n, y);
-        }
+    tc_after();
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kCols) : "memory");
+}
+
+// ---- host ---------------------------------------------------------------------------------
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+EncodeFn encoder()
+{
+    static EncodeFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
+}
+
+// Rows that the copy engine can read: on 16-byte boundaries, rows that do not overlap.
+bool engine_rows(const void *p, int64_t ld, int64_t group, int rows, int groups, int k)
+{
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && group % 8 == 0 && group >= 0 && (rows == 1 || ld >= k) && ld < (1ll << 38) &&
+           group < (1ll << 38) && k > 0 && (groups == 1 || group == 0 || group >= 8);
+}
+bool encode(CUtensorMap *map, const void *p, int64_t ld, int64_t group, int rows, int groups, int k, int box)
+{
+    const bool shared = group == 0 || groups == 1;
+    if (ld < 8) ld = (k + 7) / 8 * 8;                    // one row: the stride is never used
+    const cuuint64_t dims[3]    = {(cuuint64_t)k, (cuuint64_t)rows, (cuuint64_t)(shared ? 1 : groups)};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(shared ? ld : group) * 2};
+    const cuuint32_t boxes[3] = {kSlice, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, boxes, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Device {
+    int sms = 0;
+};
+int device_info(Device *d)
+{
+    static Device known[64];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
+    if (dev >= 0 && dev < 64 && known[dev].sms > 0) {
+        *d = known[dev];
+        return SYMAR_OK;
+    }
+    e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
+    if (dev >= 0 && dev < 64) known[dev] = *d;
+    return SYMAR_OK;
+}
+
+template <int NT, bool kWide, bool kTma>
+int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int groups, int sms, cudaStream_t stream)
+{
+    using S = Shape<NT, kWide, kTma>;
+    auto fn = linear_kernel<NT, kWide, kTma>;
+    a.n_tiles = (a.n + kRows - 1) / kRows;
+    a.m_tiles = (a.m + NT - 1) / NT;
+    const int64_t tiles = (int64_t)a.n_tiles * a.m_tiles * groups;
+    if (tiles > 0x3fffffff) return SYMAR_ERR_UNSUPPORTED;
+    a.tiles = (int)tiles;
+    const int slices = (a.k + kSlice - 1) / kSlice;
+    a.split = 1;
+    while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && slices >= a.split * 4 && NT * kRows * 4 <= S::kStages * S::kStage) a.split *= 2;
+    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    if (e != cudaSuccess) return cuda_fail(e, "symar_linear");
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim  = dim3((unsigned)(a.split > 1 ? tiles * a.split : (tiles < sms ? tiles : sms)));
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kBytes;
+    cfg.stream   = stream;
+    cfg.attrs    = attr;
+    if (a.split > 1) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)a.split;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+    }
+    e = cudaLaunchKernelEx(&cfg, fn, wmap, xmap, a);
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_linear");
+}
+
+template <int NT>
+int launch_as(const LinearArgs &a, int groups, int sms, bool wide, bool engine, cudaStream_t s)
+{
+    constexpr bool kBoth = NT <= 128;      // float32 results: the sums of a wider tile do not fit a thread's registers
+    CUtensorMap wmap{}, xmap{};
+    engine = engine && encoder() && encode(&wmap, a.w, a.w_ld, a.w_group, a.n, groups, a.k, kRows) &&
+             encode(&xmap, a.x, a.x_ld, a.x_group, a.m, groups, a.k, NT);
+    if (wide && kBoth) {
+        if (engine) return launch<NT, kBoth, true>(a, wmap, xmap, groups, sms, s);
+        return launch<(NT > 64 ? 64 : NT), kBoth, false>(a, wmap, xmap, groups, sms, s);   // (nor do 128 with twice the threads)
+    }
+    return engine ? launch<NT, false, true>(a, wmap, xmap, groups, sms, s) : launch<NT, false, false>(a, wmap, xmap, groups, sms, s);
 }
 
 }  // namespace
@@ -74,20 +527,40 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     if (p.groups < 0 || p.m < 0 || p.n < 0 || p.k < 0 || p.act < SYMAR_ACT_NONE || p.act > SYMAR_ACT_SILU) return SYMAR_ERR_INVAL;
     if (p.out_dtype != SYMAR_F32 && p.out_dtype != SYMAR_BF16) return SYMAR_ERR_INVAL;
     if (p.root < -1 || (p.root >= p.groups && p.groups > 0)) return SYMAR_ERR_INVAL;
-    if (p.groups > 65535) return SYMAR_ERR_UNSUPPORTED;
     if (p.groups == 0 || p.m == 0 || p.n == 0) return SYMAR_OK;
-    const uintptr_t wide = p.out_dtype == SYMAR_F32 ? 4 : 2;
-    if (!p.out || (p.k > 0 && (!p.x || !p.w))) return SYMAR_ERR_INVAL;
-    if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || ((uintptr_t)p.out | (uintptr_t)p.residual) % wide) return SYMAR_ERR_INVAL;
+    const uintptr_t width = p.out_dtype == SYMAR_F32 ? 4 : 2;
+    if (!p.out || (p.k > 0 && (!p.x || !p.w)) || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
+    if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || ((uintptr_t)p.out | (uintptr_t)p.residual) % width) return SYMAR_ERR_INVAL;
     if ((p.groups > 1 && p.out_group == 0) || (p.m > 1 && p.out_ld < p.n)) return SYMAR_ERR_INVAL;
-    LinearArgs a{(const __nv_bfloat16 *)p.x, (const __nv_bfloat16 *)p.w, (const __nv_bfloat16 *)p.bias, p.residual, p.out,
-                 p.x_ld, p.x_group, p.w_ld, p.w_group, p.bias_group, p.residual_ld, p.residual_group, p.out_ld, p.out_group,
-                 p.m, p.n, p.k, p.act, p.root};
-    const int mt = (p.m + kTile - 1) / kTile, nt = (p.n + kTile - 1) / kTile;
-    if (mt > 65535) return SYMAR_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)nt, (unsigned)mt, (unsigned)p.groups);
-    if (p.out_dtype == SYMAR_F32) linear_kernel<float><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-    else linear_kernel<__nv_bfloat16><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-    cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_linear");
+    Device d;
+    const int rc = device_info(&d);
+    if (rc != SYMAR_OK) return rc;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (p.status) {
+        cudaError_t e = cudaMemsetAsync(p.status, 0, sizeof(unsigned), s);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
+    }
+    LinearArgs a{};
+    a.x = (const __nv_bfloat16 *)p.x;  a.x_ld = p.x_ld;  a.x_group = p.groups > 1 ? p.x_group : 0;
+    a.w = (const __nv_bfloat16 *)p.w;  a.w_ld = p.w_ld;  a.w_group = p.groups > 1 ? p.w_group : 0;
+    a.bias = (const __nv_bfloat16 *)p.bias;  a.bias_group = p.bias_group;
+    a.residual = p.residual;  a.residual_ld = p.residual_ld;  a.residual_group = p.residual_group;
+    a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
+    a.m = p.m;  a.n = p.n;  a.k = p.k;  a.act = p.act;  a.root = p.root;  a.status = p.status;
+    const bool engine = engine_rows(p.x, p.x_ld, a.x_group, p.m, p.groups, p.k) && engine_rows(p.w, p.w_ld, a.w_group, p.n, p.groups, p.k);
+    const bool wide = p.out_dtype == SYMAR_F32;
+    // Tokens of a tile: as few columns as hold them all; for many tokens the widest tile that still gives every
+    // multiprocessor one.
+    const int64_t columns = (int64_t)((p.n + kRows - 1) / kRows) * p.groups;
+    int nt = 16;
+    while (nt < 256 && nt < p.m) nt *= 2;
+    while (nt > 64 && columns * ((p.m + nt - 1) / nt) < d.sms) nt /= 2;
+    if (wide && nt > 128) nt = 128;
+    switch (nt) {
+        case 16: return launch_as<16>(a, p.groups, d.sms, wide, engine, s);
+        case 32: return launch_as<32>(a, p.groups, d.sms, wide, engine, s);
+        case 64: return launch_as<64>(a, p.groups, d.sms, wide, engine, s);
+        case 128: return launch_as<128>(a, p.groups, d.sms, wide, engine, s);
+    }
+    return launch_as<256>(a, p.groups, d.sms, false, engine, s);
 }

@@ -395,7 +395,7 @@ class LinearArgs(ctypes.Structure):
         ("residual", c_void_p), ("residual_ld", c_int64), ("residual_group", c_int64),
         ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
         ("groups", c_int32), ("m", c_int32), ("n", c_int32), ("k", c_int32),
-        ("out_dtype", c_int32), ("act", c_int32), ("root", c_int32),
+        ("out_dtype", c_int32), ("act", c_int32), ("root", c_int32), ("status", c_void_p),
     ]
 
 
