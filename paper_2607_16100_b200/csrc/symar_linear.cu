@@ -23,6 +23,7 @@ struct LinearArgs {
     int     m, n, k, act, root;
     int     n_tiles, m_tiles, tiles;       // of 128 channels, of NT tokens, of all groups
     int     split;                         // blocks of a cluster that share a tile's k
+    int     vec_out, vec_res;              // four results at a time: rows on boundaries of four elements
     unsigned *status;
 };
 
@@ -114,29 +115,99 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float peer_load(uint32_t addr, int rank)
+__device__ __forceinline__ float4 peer_load4(uint32_t addr, int rank)
 {
     uint32_t there;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
     return v;
 }
+__device__ __forceinline__ void results_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-__device__ __forceinline__ float activate(float y, int act)
+// y / 2 (1 + tanh u) = y / (1 + exp(-2u)); the quotient's two units in the last place are far below the result's rounding
+__device__ __forceinline__ float gate(float y, float two_u) { return __fdividef(y, 1.0f + expf(-two_u)); }
+__device__ __forceinline__ void activate4(float (&y)[4], int act)
 {
-    switch (act) {
-        case SYMAR_ACT_RELU: return y < 0.0f ? 0.0f : y;
-        case SYMAR_ACT_GELU: return 0.5f * y * (1.0f + erff(y * 0.70710678118654752f));
-        case SYMAR_ACT_GELU_TANH: return 0.5f * y * (1.0f + tanhf(0.79788456080286536f * (y + 0.044715f * y * y * y)));
-        case SYMAR_ACT_SILU: return y / (1.0f + expf(-y));
+    if (act == SYMAR_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.0f ? 0.0f : y[i];
+    } else if (act == SYMAR_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = 0.5f * y[i] * (1.0f + erff(y[i] * 0.70710678118654752f));
+    } else if (act == SYMAR_ACT_GELU_TANH) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = gate(y[i], 1.5957691216057308f * (y[i] + 0.044715f * y[i] * y[i] * y[i]));
+    } else if (act == SYMAR_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = gate(y[i], y[i]);
     }
-    return y;
 }
 __device__ __forceinline__ float as_f32(float v) { return v; }
 __device__ __forceinline__ float as_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void load4(const float *p, float (&r)[4])
+{
+    const float4 v = *reinterpret_cast<const float4 *>(p);
+    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&r)[4])
+{
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    r[0] = __uint_as_float(v.x << 16); r[1] = __uint_as_float(v.x & 0xffff0000u);
+    r[2] = __uint_as_float(v.y << 16); r[3] = __uint_as_float(v.y & 0xffff0000u);
+}
+__device__ __forceinline__ void put4(float *p, const float (&r)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(r[0], r[1], r[2], r[3]); }
+__device__ __forceinline__ void put4(__nv_bfloat16 *p, const float (&r)[4])
+{
+    __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
+}
+
+// What follows the sums: four neighbouring channels of one token, from `n` on (fewer at the row's end).
+struct Channels {
+    float bias[4];
+    int   n, count, add;             // add: this group takes bias and residual
+};
+__device__ __forceinline__ Channels channels_of(const LinearArgs &a, int g, int n)
+{
+    Channels c;
+    c.n     = n;
+    c.count = max(0, min(4, a.n - n));
+    c.add   = a.root < 0 || a.root == g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c.bias[i] = c.add && a.bias && i < c.count ? __bfloat162float(a.bias[g * a.bias_group + n + i]) : 0.0f;
+    return c;
+}
+template <typename O>
+__device__ __forceinline__ void finish4(const LinearArgs &a, const Channels &c, int g, int token, float4 sum)
+{
+    if (c.count == 0) return;
+    float y[4] = {sum.x + c.bias[0], sum.y + c.bias[1], sum.z + c.bias[2], sum.w + c.bias[3]};
+    activate4(y, a.act);
+    if (c.add && a.residual) {
+        const O *p = static_cast<const O *>(a.residual) + g * a.residual_group + token * a.residual_ld + c.n;
+        float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.vec_res && c.count == 4) {
+            load4(p, r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < c.count) r[i] = as_f32(p[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += r[i];
+    }
+    O *p = static_cast<O *>(a.out) + g * a.out_group + token * a.out_ld + c.n;
+    if (a.vec_out && c.count == 4) {
+        put4(p, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < c.count) put(p + i, y[i]);
+    }
+}
 
 // Eight elements of a row from element k0 on, zeros beyond its end, where rows lie on no 16-byte boundary: the two
 // aligned vectors around them, shifted into place, unless one of those reaches out of the row.
@@ -175,8 +246,11 @@ template <int NT, bool kWide, bool kTma>
 struct Shape {
     static constexpr int kThreads = kTma ? 256 : 512;             // without the copy engine eight more warps load
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
-    static constexpr int kStages = NT >= 256 ? 4 : (NT == 128 ? 6 : (NT == 64 ? 8 : 10));
-    static constexpr int kBytes = kStages * kStage + 1024;        // (the ring starts on a 1 KiB boundary)
+    // float32 results leave the registers all at once, bf16 results 32 tokens at a time in two buffers
+    static constexpr int kStep  = NT < 32 ? NT : 32;
+    static constexpr int kHold  = (kWide ? NT : 2 * kStep) * kRows * 4;
+    static constexpr int kStages = (216 * 1024 - kHold) / kStage < 10 ? (216 * 1024 - kHold) / kStage : 10;
+    static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
     static constexpr int kCols  = 2 * NT < 32 ? 32 : 2 * NT;      // two accumulators
 };
 constexpr int kChunk = 2;          // slices that a float32 result sums in the tensor cores at a time
@@ -193,6 +267,7 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     unsigned char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    float *hold = reinterpret_cast<float *>(ring + S::kStages * S::kStage);
     const uint32_t ring_addr = smem_addr(ring);
     const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -297,38 +372,21 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
             }
         }
     } else if (warp >= 4 && warp < 8) {
-        // ---- results: this thread is one channel of the tile, its registers are tokens ----
+        // ---- results: out of tensor memory a thread holds one channel of many tokens; by way of shared memory it gets four
+        // channels of one token, which are neighbours in `out` (and the code of an activation is there once)
         const int quarter = warp - 4, ch = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool parts = k_hi > k_lo;
+        float *part = reinterpret_cast<float *>(ring);               // [token][channel] of a shared tile: the ring is not in use any more
         uint32_t turn = 0;
         for (int tile = first; tile < a.tiles; tile += step) {
             int g, m0, n0;
             place(tile, g, m0, n0);
-            const int n = n0 + ch, tokens = min(NT, a.m - m0);
-            const bool mine = a.root < 0 || a.root == g, on = n < a.n;
-            const float bias = mine && a.bias && on ? __bfloat162float(a.bias[g * a.bias_group + n]) : 0.0f;
-            const O *res = mine && a.residual ? static_cast<const O *>(a.residual) + g * a.residual_group + (int64_t)m0 * a.residual_ld + n : nullptr;
-            O *out = static_cast<O *>(a.out) + g * a.out_group + (int64_t)m0 * a.out_ld + n;
-            auto finish16 = [&](const float *v, int c0) {
-                if (!on) return;
-                float r[16];
-                if (res) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) r[i] = c0 + i < tokens ? as_f32(res[(int64_t)(c0 + i) * a.residual_ld]) : 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (c0 + i >= tokens) break;
-                    float y = activate(v[i] + bias, a.act);
-                    if (res) y += r[i];
-                    put(out + (int64_t)(c0 + i) * a.out_ld, y);
-                }
-            };
-            float sum[kWide ? NT : 16];
+            const int tokens = min(NT, a.m - m0);
             if (kWide) {
+                float sum[kWide ? NT : 1];
 #pragma unroll
-                for (int i = 0; i < (kWide ? NT : 16); ++i) sum[i] = 0.0f;
+                for (int i = 0; i < (kWide ? NT : 1); ++i) sum[i] = 0.0f;
                 for (int ks = k_lo; ks < k_hi; ks += kChunk, ++turn) {
                     const uint32_t buf = turn & 1;
                     if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
@@ -338,42 +396,54 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                         float v[16];
                         acc_load16(tmem + lanes + buf * NT + c0, v);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) sum[kWide ? c0 + i : i] += v[i];
+                        for (int i = 0; i < 16; ++i) sum[kWide ? c0 + i : 0] += v[i];
                     }
                     tc_before();
                     bar_arrive(acc_empty + 8 * buf);
                 }
-            }
-            const uint32_t buf = turn & 1;
-            if (!kWide && parts) {
-                if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
-                tc_after();
-            }
-            float *part = reinterpret_cast<float *>(ring);            // [token][channel], the ring is not in use any more
+                float *to = a.split > 1 ? part : hold;
 #pragma unroll
-            for (int c0 = 0; c0 < NT; c0 += 16) {
-                if (c0 >= tokens) break;
-                float v[16];
-                if (kWide) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = sum[kWide ? c0 + i : i];
-                } else if (parts) {
-                    acc_load16(tmem + lanes + buf * NT + c0, v);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                for (int i = 0; i < (kWide ? NT : 1); ++i) to[i * kRows + ch] = sum[i];
+                if (a.split == 1) {
+                    results_sync();
+                    const Channels c = channels_of(a, g, n0 + 4 * lane);
+                    for (int t = quarter; t < tokens; t += 4)
+                        finish4<O>(a, c, g, m0 + t, *reinterpret_cast<const float4 *>(hold + t * kRows + 4 * lane));
+                    results_sync();
                 }
-                if (a.split > 1) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) part[(c0 + i) * kRows + ch] = v[i];
-                } else {
-                    finish16(v, c0);
+            } else {
+                const uint32_t buf = turn & 1;
+                if (parts) {
+                    if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    tc_after();
                 }
-            }
-            if (!kWide && parts) {
-                tc_before();
-                bar_arrive(acc_empty + 8 * buf);
-                ++turn;
+                const Channels c = channels_of(a, g, n0 + 4 * lane);
+#pragma unroll 1
+                for (int c0 = 0; c0 < tokens; c0 += S::kStep) {
+                    float *to = a.split > 1 ? part + c0 * kRows : hold + ((c0 / S::kStep) & 1) * S::kStep * kRows;
+                    float v[S::kStep];
+#pragma unroll
+                    for (int i = 0; i < S::kStep; ++i) v[i] = 0.0f;
+                    if (parts) {
+#pragma unroll
+                        for (int i = 0; i < S::kStep; i += 16) acc_load16(tmem + lanes + buf * NT + c0 + i, v + i);
+                    }
+                    if (c0 + S::kStep >= tokens && parts) {          // the accumulator is free for the tile after the next
+                        tc_before();
+                        bar_arrive(acc_empty + 8 * buf);
+                    }
+#pragma unroll
+                    for (int i = 0; i < S::kStep; ++i) to[i * kRows + ch] = v[i];
+                    if (a.split == 1) {
+                        results_sync();      // one barrier a step: the other buffer was read before its last writer came here
+                        const int count = min(S::kStep, tokens - c0);
+                        for (int t = quarter; t < count; t += 4)
+                            finish4<O>(a, c, g, m0 + c0 + t, *reinterpret_cast<const float4 *>(to + t * kRows + 4 * lane));
+                    }
+                }
+                // a next tile's first step may be this tile's last buffer
+                if (a.split == 1) results_sync();
+                if (parts) ++turn;
             }
         }
     }
@@ -384,22 +454,18 @@ done:
         cluster_sync();
         int g, m0, n0;
         place(first, g, m0, n0);
-        const int n = n0 + (tid & 127), tokens = min(NT, a.m - m0);
-        if (n < a.n) {
-            const bool mine = a.root < 0 || a.root == g;
-            const float bias = mine && a.bias ? __bfloat162float(a.bias[g * a.bias_group + n]) : 0.0f;
-            for (int t = rank + a.split * (tid >> 7); t < tokens; t += a.split * (S::kThreads / 128)) {
-                const uint32_t at = ring_addr + (t * kRows + (tid & 127)) * 4;
-                float v[kMaxSplit], y = 0.0f;
+        const int tokens = min(NT, a.m - m0);
+        const Channels c = channels_of(a, g, n0 + 4 * lane);
+        for (int t = rank + a.split * warp; t < tokens; t += a.split * (S::kThreads / 32)) {
+            const uint32_t at = ring_addr + (t * kRows + 4 * lane) * 4;
+            float4 v[kMaxSplit], y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                for (int r = 0; r < kMaxSplit; ++r) v[r] = r < a.split ? peer_load(at, r) : 0.0f;
+            for (int r = 0; r < kMaxSplit; ++r) v[r] = r < a.split ? peer_load4(at, r) : y;
 #pragma unroll
-                for (int r = 0; r < kMaxSplit; ++r) y += v[r];
-                y = activate(y + bias, a.act);
-                if (mine && a.residual)
-                    y += as_f32(static_cast<const O *>(a.residual)[g * a.residual_group + (int64_t)(m0 + t) * a.residual_ld + n]);
-                put(static_cast<O *>(a.out) + g * a.out_group + (int64_t)(m0 + t) * a.out_ld + n, y);
+            for (int r = 0; r < kMaxSplit; ++r) {
+                y.x += v[r].x; y.y += v[r].y; y.z += v[r].z; y.w += v[r].w;
             }
+            finish4<O>(a, c, g, m0 + t, y);
         }
         cluster_sync();                                   // no block leaves while its part may be read
     }
@@ -546,6 +612,8 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     a.bias = (const __nv_bfloat16 *)p.bias;  a.bias_group = p.bias_group;
     a.residual = p.residual;  a.residual_ld = p.residual_ld;  a.residual_group = p.residual_group;
     a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
+    a.vec_out = ((uintptr_t)p.out % (4 * width) == 0) && p.out_ld % 4 == 0 && p.out_group % 4 == 0;
+    a.vec_res = ((uintptr_t)p.residual % (4 * width) == 0) && p.residual_ld % 4 == 0 && p.residual_group % 4 == 0;
     a.m = p.m;  a.n = p.n;  a.k = p.k;  a.act = p.act;  a.root = p.root;  a.status = p.status;
     const bool engine = engine_rows(p.x, p.x_ld, a.x_group, p.m, p.groups, p.k) && engine_rows(p.w, p.w_ld, a.w_group, p.n, p.groups, p.k);
     const bool wide = p.out_dtype == SYMAR_F32;
