@@ -58,7 +58,7 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
-// A warp's wait; false for all its lanes once it has lasted four seconds or another role has given up.
+// A thread's wait; false once it has lasted four seconds or another role has given up.
 __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed)
 {
     const uint64_t t0 = now_ns();
@@ -74,9 +74,24 @@ __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volati
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed)
 {
     bool ok = false;
-    for (int i = 0; i < 16 && !ok; ++i) ok = bar_try(bar, parity);
+#pragma unroll 1
+    for (int i = 0; i < 64 && !ok; ++i) ok = bar_try(bar, parity);
     if (!ok) ok = bar_wait_long(bar, parity, failed);
-    return __all_sync(0xffffffffu, ok);
+    return ok;
+}
+// The same for a whole warp: all its lanes go on, or none.  One lane polls.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    int ok = 0;
+    if ((threadIdx.x & 31) == 0) ok = bar_wait(bar, parity, failed);
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+// one lane of a converged warp
+__device__ __forceinline__ bool elected()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
@@ -123,7 +138,7 @@ __device__ __forceinline__ float4 peer_load4(uint32_t addr, int rank)
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
     return v;
 }
-__device__ __forceinline__ void results_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void results_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // y / 2 (1 + tanh u) = y / (1 + exp(-2u)); the quotient's two units in the last place are far below the result's rounding
 __device__ __forceinline__ float gate(float y, float two_u) { return __fdividef(y, 1.0f + expf(-two_u)); }
@@ -166,6 +181,9 @@ __device__ __forceinline__ void put4(__nv_bfloat16 *p, const float (&r)[4])
 }
 
 // What follows the sums: four neighbouring channels of one token, from `n` on (fewer at the row's end).
+template <typename O> struct Four;
+template <> struct Four<float> { float4 v; };
+template <> struct Four<__nv_bfloat16> { uint2 v; };
 struct Channels {
     float bias[4];
     int   n, count, add;             // add: this group takes bias and residual
@@ -181,21 +199,36 @@ __device__ __forceinline__ Channels channels_of(const LinearArgs &a, int g, int 
     return c;
 }
 template <typename O>
-__device__ __forceinline__ void finish4(const LinearArgs &a, const Channels &c, int g, int token, float4 sum)
+__device__ __forceinline__ Four<O> residual4(const LinearArgs &a, const Channels &c, int g, int token)
 {
-    if (c.count == 0) return;
+    Four<O> r{};
+    if (c.add && a.residual && c.count > 0) {
+        const O *p = static_cast<const O *>(a.residual) + g * a.residual_group + token * a.residual_ld + c.n;
+        if (a.vec_res && c.count == 4) {
+            r = *reinterpret_cast<const Four<O> *>(p);
+        } else {
+            O h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = i < c.count ? p[i] : O(0.0f);
+            r = *reinterpret_cast<const Four<O> *>(h);
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ void before_residual(const LinearArgs &a, const Channels &c, float4 &sum)
+{
     float y[4] = {sum.x + c.bias[0], sum.y + c.bias[1], sum.z + c.bias[2], sum.w + c.bias[3]};
     activate4(y, a.act);
+    sum = make_float4(y[0], y[1], y[2], y[3]);
+}
+template <typename O>
+__device__ __forceinline__ void store4(const LinearArgs &a, const Channels &c, int g, int token, float4 v, const Four<O> &res)
+{
+    if (c.count == 0) return;
+    float y[4] = {v.x, v.y, v.z, v.w};
     if (c.add && a.residual) {
-        const O *p = static_cast<const O *>(a.residual) + g * a.residual_group + token * a.residual_ld + c.n;
-        float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (a.vec_res && c.count == 4) {
-            load4(p, r);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < c.count) r[i] = as_f32(p[i]);
-        }
+        float r[4];
+        load4(reinterpret_cast<const O *>(&res), r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] += r[i];
     }
@@ -208,48 +241,98 @@ __device__ __forceinline__ void finish4(const LinearArgs &a, const Channels &c, 
             if (i < c.count) put(p + i, y[i]);
     }
 }
+// `count` (at most 8 N) tokens from `token` on whose sums lie in shared memory, one in eight of them this warp's: bias and activation
+// in a loop that is there once, then residuals, which were asked for before, and stores.
+template <typename O, int N>
+__device__ __forceinline__ void residuals_of(const LinearArgs &a, const Channels &c, int g, int token, int count, int w, Four<O> (&res)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (w + 8 * i < count) res[i] = residual4<O>(a, c, g, token + w + 8 * i);
+}
+template <typename O, int N>
+__device__ __forceinline__ void finish(const LinearArgs &a, const Channels &c, int g, int token, int count, int w, float *sums, const Four<O> (&res)[N])
+{
+    float4 *mine = reinterpret_cast<float4 *>(sums);          // this lane's four channels of the first token
+    if (a.act != SYMAR_ACT_NONE) {
+#pragma unroll 2
+        for (int t = w; t < count; t += 8) before_residual(a, c, mine[t * (kRows / 4)]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int t = w + 8 * i;
+        if (t < count) {
+            float4 v = mine[t * (kRows / 4)];
+            if (a.act == SYMAR_ACT_NONE) v = make_float4(v.x + c.bias[0], v.y + c.bias[1], v.z + c.bias[2], v.w + c.bias[3]);
+            store4<O>(a, c, g, token + t, v, res[i]);
+        }
+    }
+}
 
 // Eight elements of a row from element k0 on, zeros beyond its end, where rows lie on no 16-byte boundary: the two
 // aligned vectors around them, shifted into place, unless one of those reaches out of the row.
-__device__ __forceinline__ uint4 row_chunk(const __nv_bfloat16 *row, int k0, int k)
+__device__ __forceinline__ uint4 shifted(const uint4 &u, const uint4 &v, int shift)
 {
-    if (k0 >= k) return make_uint4(0, 0, 0, 0);
-    const uintptr_t p = (uintptr_t)(row + k0), base = p & ~(uintptr_t)15;
-    const int shift = (int)(p - base);
-    if (shift == 0 && k0 + 8 <= k) return __ldg(reinterpret_cast<const uint4 *>(p));
-    if (base >= (uintptr_t)row && base + 32 <= (uintptr_t)(row + k)) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(base)), v = __ldg(reinterpret_cast<const uint4 *>(base) + 1);
-        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-        if (shift & 8) {
+    uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        }
-        if (shift & 4) {
+    for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
 #pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-        }
-        if (shift & 2) {
+    for (int i = 0; i < 5; ++i) w[i] = shift & 4 ? w[i + 1] : w[i];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    const uint16_t *h = reinterpret_cast<const uint16_t *>(row + k0);
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (shift & 2) * 8);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __noinline__ uint4 edge_chunk(const __nv_bfloat16 *row, int k0, int k)
+{
+    const uint16_t *h = reinterpret_cast<const uint16_t *>(row);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (k0 + i < k) w[i >> 1] |= (uint32_t)h[i] << ((i & 1) * 16);
+        if (k0 + i < k) w[i >> 1] |= (uint32_t)h[k0 + i] << ((i & 1) * 16);
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Rows first, first + 4, ... of a stage (of `rows`, the operand's rows from row0 on), chunk c of each: eight rows' loads
+// at a time before the first is used.
+__device__ __forceinline__ void load_rows(unsigned char *dst, const __nv_bfloat16 *p, int64_t ld, int row0, int left, int rows, int first, int c,
+                                          int k0, int k)
+{
+#pragma unroll 1
+    for (int r0 = first; r0 < rows; r0 += 32) {
+        uint4 u[8], v[8];
+        int how[8];                                     // byte shift; -1: by elements; -2: zeros
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = r0 + 4 * j;
+            const __nv_bfloat16 *row = p + (int64_t)(row0 + r) * ld;
+            const uintptr_t base = (uintptr_t)(row + k0) & ~(uintptr_t)15;
+            how[j] = r < left && r < rows && k0 < k ? (int)((uintptr_t)(row + k0) - base) : -2;
+            if (how[j] >= 0 && (base < (uintptr_t)row || base + 32 > (uintptr_t)(row + k))) how[j] = -1;
+            u[j] = v[j] = make_uint4(0, 0, 0, 0);
+            if (how[j] >= 0) {
+                u[j] = __ldg(reinterpret_cast<const uint4 *>(base));
+                v[j] = __ldg(reinterpret_cast<const uint4 *>(base) + 1);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = r0 + 4 * j;
+            if (r >= rows) break;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (how[j] >= 0) x = shifted(u[j], v[j], how[j]);
+            else if (how[j] == -1) x = edge_chunk(p + (int64_t)(row0 + r) * ld, k0, k);
+            *reinterpret_cast<uint4 *>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = x;
+        }
+    }
 }
 
 template <int NT, bool kWide, bool kTma>
 struct Shape {
-    static constexpr int kThreads = kTma ? 256 : 512;             // without the copy engine eight more warps load
+    static constexpr int kThreads = kTma ? 384 : 640;             // without the copy engine eight more warps load
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
     // float32 results leave the registers all at once, bf16 results 32 tokens at a time in two buffers
     static constexpr int kStep  = NT < 32 ? NT : 32;
     static constexpr int kHold  = (kWide ? NT : 2 * kStep) * kRows * 4;
-    static constexpr int kStages = (216 * 1024 - kHold) / kStage < 10 ? (216 * 1024 - kHold) / kStage : 10;
+    static constexpr int kStages = (224 * 1024 - kHold) / kStage < 10 ? (224 * 1024 - kHold) / kStage : 10;
     static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
     static constexpr int kCols  = 2 * NT < 32 ? 32 : 2 * NT;      // two accumulators
 };
@@ -274,12 +357,12 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
 
     if (tid == 0) {
         for (int i = 0; i < S::kStages; ++i) {
-            bar_init(full + 8 * i, kTma ? 1 : 256);
+            bar_init(full + 8 * i, kTma ? 1 : 32);
             bar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(acc_full + 8 * i, 1);
-            bar_init(acc_empty + 8 * i, 128);
+            bar_init(acc_empty + 8 * i, 256);
         }
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -309,43 +392,34 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
         n0 = i / wide * kRows;
     };
 
-    if (kTma ? warp == 0 : warp >= 8) {
-        // ---- producer ----
-        int st = 0, round = 0;
+    if (kTma ? warp == 0 && elected() : warp >= 12) {
+        // ---- producer: one thread, or eight warps, a stage each in turn, where rows lie on no boundary that the copy engine takes ----
+        int st = 0, round = 0, turn = 0;
         for (int tile = first; tile < a.tiles; tile += step) {
             int g, m0, n0;
             place(tile, g, m0, n0);
-            for (int ks = k_lo; ks < k_hi; ++ks) {
-                if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
-                const uint32_t at = ring_addr + st * S::kStage;
+            for (int ks = k_lo; ks < k_hi; ++ks, ++turn) {
                 if (kTma) {
-                    if (lane == 0) {
-                        bar_expect(full + 8 * st, S::kStage);
-                        tma_load(at, &wmap, ks * kSlice, n0, a.w_group ? g : 0, full + 8 * st);
-                        tma_load(at + S::kA, &xmap, ks * kSlice, m0, a.x_group ? g : 0, full + 8 * st);
-                    }
-                    __syncwarp();
-                } else {
+                    if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                    const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
+                    bar_expect(bar, S::kStage);
+                    tma_load(at, &wmap, ks * kSlice, n0, a.w_group ? g : 0, bar);
+                    tma_load(at + S::kA, &xmap, ks * kSlice, m0, a.x_group ? g : 0, bar);
+                } else if ((turn & 7) == warp - 12) {
+                    if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                     const __nv_bfloat16 *w = a.w + g * a.w_group, *x = a.x + g * a.x_group;
                     unsigned char *dst = ring + st * S::kStage;
-#pragma unroll 4
-                    for (int i = tid - 256; i < (kRows + NT) * 8; i += 256) {
-                        const int r = i >> 3, c = i & 7;
-                        const bool is_w = r < kRows;
-                        const int row = is_w ? n0 + r : m0 + r - kRows;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (row < (is_w ? a.n : a.m))
-                            v = row_chunk((is_w ? w + row * a.w_ld : x + row * a.x_ld), ks * kSlice + c * 8, a.k);
-                        *reinterpret_cast<uint4 *>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = v;
-                    }
+                    const int c = lane & 7, k0 = ks * kSlice + c * 8;
+                    load_rows(dst, w, a.w_ld, n0, a.n - n0, kRows, lane >> 3, c, k0, a.k);
+                    load_rows(dst + S::kA, x, a.x_ld, m0, a.m - m0, NT, lane >> 3, c, k0, a.k);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     bar_arrive(full + 8 * st);
                 }
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
-    } else if (warp == 1) {
-        // ---- products ----
+    } else if (warp == 1 && elected()) {
+        // ---- products: one thread ----
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
         int st = 0, round = 0;
         uint32_t turn = 0;                              // accumulators filled so far
@@ -355,26 +429,24 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                 const uint32_t buf = turn & 1, acc = tmem + buf * NT;
                 if (turn >= 2 && !bar_wait(acc_empty + 8 * buf, ((turn >> 1) - 1) & 1, &failed)) goto done;
                 tc_after();
-                for (int from = ks; ks < to; ++ks) {
+                for (uint32_t add = 0; ks < to; ++ks, add = 1) {
                     if (!bar_wait(full + 8 * st, round & 1, &failed)) goto done;
                     tc_after();
-                    if (lane == 0) {
-                        const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
+                    const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
+                    product(acc, w, x, kHow, add);
 #pragma unroll
-                        for (int i = 0; i < kSlice / 16; ++i) product(acc, w + 2 * i, x + 2 * i, kHow, ks > from || i > 0);
-                        commit(empty + 8 * st);
-                        if (ks + 1 == to) commit(acc_full + 8 * buf);
-                    }
-                    __syncwarp();
+                    for (int i = 1; i < kSlice / 16; ++i) product(acc, w + 2 * i, x + 2 * i, kHow, 1);
+                    commit(empty + 8 * st);
                     if (++st == S::kStages) st = 0, ++round;
                 }
+                commit(acc_full + 8 * buf);
                 ++turn;
             }
         }
-    } else if (warp >= 4 && warp < 8) {
+    } else if (warp >= 4 && warp < 12) {
         // ---- results: out of tensor memory a thread holds one channel of many tokens; by way of shared memory it gets four
         // channels of one token, which are neighbours in `out` (and the code of an activation is there once)
-        const int quarter = warp - 4, ch = quarter * 32 + lane;
+        const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;   // a quarter's channels: two warps, half of the tokens each
         const uint32_t lanes = (uint32_t)quarter << 21;
         const bool parts = k_hi > k_lo;
         float *part = reinterpret_cast<float *>(ring);               // [token][channel] of a shared tile: the ring is not in use any more
@@ -384,17 +456,19 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
             place(tile, g, m0, n0);
             const int tokens = min(NT, a.m - m0);
             if (kWide) {
-                float sum[kWide ? NT : 1];
+                constexpr int kOwn = kWide ? (NT < 32 ? 16 : NT / 2) : 1;     // (of 16 tokens one half of the warps holds all)
+                const int col = NT < 32 ? 0 : side * kOwn;
+                float sum[kOwn];
 #pragma unroll
-                for (int i = 0; i < (kWide ? NT : 1); ++i) sum[i] = 0.0f;
+                for (int i = 0; i < kOwn; ++i) sum[i] = 0.0f;
                 for (int ks = k_lo; ks < k_hi; ks += kChunk, ++turn) {
                     const uint32_t buf = turn & 1;
-                    if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    if (!warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
                     tc_after();
 #pragma unroll
-                    for (int c0 = 0; c0 < NT; c0 += 16) {
+                    for (int c0 = 0; c0 < kOwn; c0 += 16) {
                         float v[16];
-                        acc_load16(tmem + lanes + buf * NT + c0, v);
+                        acc_load16(tmem + lanes + buf * NT + col + c0, v);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum[kWide ? c0 + i : 0] += v[i];
                     }
@@ -402,43 +476,52 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                     bar_arrive(acc_empty + 8 * buf);
                 }
                 float *to = a.split > 1 ? part : hold;
+                if (NT >= 32 || side == 0) {
 #pragma unroll
-                for (int i = 0; i < (kWide ? NT : 1); ++i) to[i * kRows + ch] = sum[i];
+                    for (int i = 0; i < kOwn; ++i) to[(col + i) * kRows + ch] = sum[i];
+                }
                 if (a.split == 1) {
                     results_sync();
                     const Channels c = channels_of(a, g, n0 + 4 * lane);
-                    for (int t = quarter; t < tokens; t += 4)
-                        finish4<O>(a, c, g, m0 + t, *reinterpret_cast<const float4 *>(hold + t * kRows + 4 * lane));
+                    Four<O> res[4];
+#pragma unroll 1
+                    for (int t0 = 0; t0 < tokens; t0 += 32) {
+                        const int count = min(32, tokens - t0);
+                        residuals_of<O>(a, c, g, m0 + t0, count, ew, res);
+                        finish<O>(a, c, g, m0 + t0, count, ew, hold + t0 * kRows + 4 * lane, res);
+                    }
                     results_sync();
                 }
             } else {
                 const uint32_t buf = turn & 1;
+                const Channels c = channels_of(a, g, n0 + 4 * lane);
+                Four<O> res[S::kStep / 8];
+                if (a.split == 1) residuals_of<O>(a, c, g, m0, min(S::kStep, tokens), ew, res);
                 if (parts) {
-                    if (!bar_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    if (!warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
                     tc_after();
                 }
-                const Channels c = channels_of(a, g, n0 + 4 * lane);
 #pragma unroll 1
                 for (int c0 = 0; c0 < tokens; c0 += S::kStep) {
                     float *to = a.split > 1 ? part + c0 * kRows : hold + ((c0 / S::kStep) & 1) * S::kStep * kRows;
-                    float v[S::kStep];
+                    const int col = S::kStep < 32 ? 0 : side * 16;              // a half of the warps takes sixteen of the tokens
+                    float v[16];
 #pragma unroll
-                    for (int i = 0; i < S::kStep; ++i) v[i] = 0.0f;
-                    if (parts) {
-#pragma unroll
-                        for (int i = 0; i < S::kStep; i += 16) acc_load16(tmem + lanes + buf * NT + c0 + i, v + i);
-                    }
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                    if (parts) acc_load16(tmem + lanes + buf * NT + c0 + col, v);
                     if (c0 + S::kStep >= tokens && parts) {          // the accumulator is free for the tile after the next
                         tc_before();
                         bar_arrive(acc_empty + 8 * buf);
                     }
+                    if (S::kStep == 32 || side == 0) {
 #pragma unroll
-                    for (int i = 0; i < S::kStep; ++i) to[i * kRows + ch] = v[i];
+                        for (int i = 0; i < 16; ++i) to[(col + i) * kRows + ch] = v[i];
+                    }
                     if (a.split == 1) {
                         results_sync();      // one barrier a step: the other buffer was read before its last writer came here
                         const int count = min(S::kStep, tokens - c0);
-                        for (int t = quarter; t < count; t += 4)
-                            finish4<O>(a, c, g, m0 + c0 + t, *reinterpret_cast<const float4 *>(to + t * kRows + 4 * lane));
+                        finish<O>(a, c, g, m0 + c0, count, ew, to + 4 * lane, res);
+                        residuals_of<O>(a, c, g, m0 + c0 + S::kStep, min(S::kStep, tokens - c0 - S::kStep), ew, res);
                     }
                 }
                 // a next tile's first step may be this tile's last buffer
@@ -456,7 +539,9 @@ done:
         place(first, g, m0, n0);
         const int tokens = min(NT, a.m - m0);
         const Channels c = channels_of(a, g, n0 + 4 * lane);
+#pragma unroll 2
         for (int t = rank + a.split * warp; t < tokens; t += a.split * (S::kThreads / 32)) {
+            const Four<O> res = residual4<O>(a, c, g, m0 + t);
             const uint32_t at = ring_addr + (t * kRows + 4 * lane) * 4;
             float4 v[kMaxSplit], y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
@@ -465,7 +550,8 @@ done:
             for (int r = 0; r < kMaxSplit; ++r) {
                 y.x += v[r].x; y.y += v[r].y; y.z += v[r].z; y.w += v[r].w;
             }
-            finish4<O>(a, c, g, m0 + t, y);
+            before_residual(a, c, y);
+            store4<O>(a, c, g, m0 + t, y, res);
         }
         cluster_sync();                                   // no block leaves while its part may be read
     }
@@ -617,13 +703,10 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     a.m = p.m;  a.n = p.n;  a.k = p.k;  a.act = p.act;  a.root = p.root;  a.status = p.status;
     const bool engine = engine_rows(p.x, p.x_ld, a.x_group, p.m, p.groups, p.k) && engine_rows(p.w, p.w_ld, a.w_group, p.n, p.groups, p.k);
     const bool wide = p.out_dtype == SYMAR_F32;
-    // Tokens of a tile: as few columns as hold them all; for many tokens the widest tile that still gives every
-    // multiprocessor one.
-    const int64_t columns = (int64_t)((p.n + kRows - 1) / kRows) * p.groups;
+    // Tokens of a tile: as few columns as hold them all, 256 at most (128 for float32 results, whose sums are registers).
+    // Fewer would read the weights again; where tiles are few, clusters share their k instead.
     int nt = 16;
-    while (nt < 256 && nt < p.m) nt *= 2;
-    while (nt > 64 && columns * ((p.m + nt - 1) / nt) < d.sms) nt /= 2;
-    if (wide && nt > 128) nt = 128;
+    while (nt < (wide ? 128 : 256) && nt < p.m) nt *= 2;
     switch (nt) {
         case 16: return launch_as<16>(a, p.groups, d.sms, wide, engine, s);
         case 32: return launch_as<32>(a, p.groups, d.sms, wide, engine, s);
