@@ -269,11 +269,39 @@ __device__ __forceinline__ void finish(const LinearArgs &a, const Channels &c, i
     }
 }
 
-// Eight elements of a row from element k0 on, zeros beyond its end, where rows lie on no 16-byte boundary: the two
-// aligned vectors around them, shifted into place, unless one of those reaches out of the row.
-__device__ __forceinline__ uint4 shifted(const uint4 &u, const uint4 &v, int shift)
+// ---- rows on no 16-byte boundary ----
+// Eight neighbouring lanes hold the eight aligned 16-byte pieces that a slice of a row begins in; the slice's own eight
+// pieces start `shift` bytes into them.  A lane takes the missing end of its piece from its neighbour, the eighth from the
+// first lane's piece of the next slice, which is on its way by then; so every piece is loaded once.
+struct Span {
+    const char *lo, *hi;         // the operand's bytes: nothing outside is read
+};
+__device__ __noinline__ uint4 edge_piece(const char *at, Span s)
 {
-    uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (at + 2 * i >= s.lo && at + 2 * i + 2 <= s.hi) w[i >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t *>(at + 2 * i) << ((i & 1) * 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 piece(const char *row, int64_t byte, bool on, Span s)
+{
+    const char *at = reinterpret_cast<const char *>((uintptr_t)row & ~(uintptr_t)15) + byte;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (on && at < s.hi) {
+        if (at >= s.lo && at + 16 <= s.hi) v = __ldg(reinterpret_cast<const uint4 *>(at));
+        else v = edge_piece(at, s);
+    }
+    return v;
+}
+__device__ __forceinline__ uint4 joined(const uint4 &u, const uint4 &next, int shift, int c, int lane)
+{
+    const int from = c < 7 ? lane + 1 : lane - 7;
+    uint32_t w[8] = {u.x, u.y, u.z, u.w, 0, 0, 0, 0};
+    w[4] = __shfl_sync(0xffffffffu, c == 0 ? next.x : u.x, from);
+    w[5] = __shfl_sync(0xffffffffu, c == 0 ? next.y : u.y, from);
+    w[6] = __shfl_sync(0xffffffffu, c == 0 ? next.z : u.z, from);
+    w[7] = __shfl_sync(0xffffffffu, c == 0 ? next.w : u.w, from);
 #pragma unroll
     for (int i = 0; i < 6; ++i) w[i] = shift & 8 ? w[i + 2] : w[i];
 #pragma unroll
@@ -282,47 +310,13 @@ __device__ __forceinline__ uint4 shifted(const uint4 &u, const uint4 &v, int shi
     for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (shift & 2) * 8);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __noinline__ uint4 edge_chunk(const __nv_bfloat16 *row, int k0, int k)
+// zeros from element `count` on
+__device__ __forceinline__ uint4 cut(uint4 v, int count)
 {
-    const uint16_t *h = reinterpret_cast<const uint16_t *>(row);
-    uint32_t w[4] = {0, 0, 0, 0};
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (k0 + i < k) w[i >> 1] |= (uint32_t)h[k0 + i] << ((i & 1) * 16);
+    for (int i = 0; i < 4; ++i) w[i] = count >= 2 * i + 2 ? w[i] : (count == 2 * i + 1 ? w[i] & 0xffffu : 0u);
     return make_uint4(w[0], w[1], w[2], w[3]);
-}
-// Rows first, first + 4, ... of a stage (of `rows`, the operand's rows from row0 on), chunk c of each: eight rows' loads
-// at a time before the first is used.
-__device__ __forceinline__ void load_rows(unsigned char *dst, const __nv_bfloat16 *p, int64_t ld, int row0, int left, int rows, int first, int c,
-                                          int k0, int k)
-{
-#pragma unroll 1
-    for (int r0 = first; r0 < rows; r0 += 32) {
-        uint4 u[8], v[8];
-        int how[8];                                     // byte shift; -1: by elements; -2: zeros
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = r0 + 4 * j;
-            const __nv_bfloat16 *row = p + (int64_t)(row0 + r) * ld;
-            const uintptr_t base = (uintptr_t)(row + k0) & ~(uintptr_t)15;
-            how[j] = r < left && r < rows && k0 < k ? (int)((uintptr_t)(row + k0) - base) : -2;
-            if (how[j] >= 0 && (base < (uintptr_t)row || base + 32 > (uintptr_t)(row + k))) how[j] = -1;
-            u[j] = v[j] = make_uint4(0, 0, 0, 0);
-            if (how[j] >= 0) {
-                u[j] = __ldg(reinterpret_cast<const uint4 *>(base));
-                v[j] = __ldg(reinterpret_cast<const uint4 *>(base) + 1);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = r0 + 4 * j;
-            if (r >= rows) break;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (how[j] >= 0) x = shifted(u[j], v[j], how[j]);
-            else if (how[j] == -1) x = edge_chunk(p + (int64_t)(row0 + r) * ld, k0, k);
-            *reinterpret_cast<uint4 *>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = x;
-        }
-    }
 }
 
 template <int NT, bool kWide, bool kTma>
@@ -357,7 +351,7 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
 
     if (tid == 0) {
         for (int i = 0; i < S::kStages; ++i) {
-            bar_init(full + 8 * i, kTma ? 1 : 32);
+            bar_init(full + 8 * i, kTma ? 1 : 256);
             bar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -392,29 +386,56 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
         n0 = i / wide * kRows;
     };
 
-    if (kTma ? warp == 0 && elected() : warp >= 12) {
-        // ---- producer: one thread, or eight warps, a stage each in turn, where rows lie on no boundary that the copy engine takes ----
-        int st = 0, round = 0, turn = 0;
+    if (kTma && warp == 0 && elected()) {
+        // ---- producer: one thread ----
+        int st = 0, round = 0;
         for (int tile = first; tile < a.tiles; tile += step) {
             int g, m0, n0;
             place(tile, g, m0, n0);
-            for (int ks = k_lo; ks < k_hi; ++ks, ++turn) {
-                if (kTma) {
-                    if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
-                    const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
-                    bar_expect(bar, S::kStage);
-                    tma_load(at, &wmap, ks * kSlice, n0, a.w_group ? g : 0, bar);
-                    tma_load(at + S::kA, &xmap, ks * kSlice, m0, a.x_group ? g : 0, bar);
-                } else if ((turn & 7) == warp - 12) {
-                    if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
-                    const __nv_bfloat16 *w = a.w + g * a.w_group, *x = a.x + g * a.x_group;
-                    unsigned char *dst = ring + st * S::kStage;
-                    const int c = lane & 7, k0 = ks * kSlice + c * 8;
-                    load_rows(dst, w, a.w_ld, n0, a.n - n0, kRows, lane >> 3, c, k0, a.k);
-                    load_rows(dst + S::kA, x, a.x_ld, m0, a.m - m0, NT, lane >> 3, c, k0, a.k);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    bar_arrive(full + 8 * st);
+            for (int ks = k_lo; ks < k_hi; ++ks) {
+                if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
+                bar_expect(bar, S::kStage);
+                tma_load(at, &wmap, ks * kSlice, n0, a.w_group ? g : 0, bar);
+                tma_load(at + S::kA, &xmap, ks * kSlice, m0, a.x_group ? g : 0, bar);
+                if (++st == S::kStages) st = 0, ++round;
+            }
+        }
+    } else if (!kTma && warp >= 12) {
+        // ---- producer: eight warps; a thread has one piece of every thirty-second row ----
+        constexpr int kOf = kTma ? 1 : 4 + (NT + 31) / 32;
+        int st = 0, round = 0;
+        const int c = tid & 7, r = (tid - 384) >> 3;
+        for (int tile = first; tile < a.tiles && k_lo < k_hi; tile += step) {
+            int g, m0, n0;
+            place(tile, g, m0, n0);
+            const char *w = reinterpret_cast<const char *>(a.w + g * a.w_group), *x = reinterpret_cast<const char *>(a.x + g * a.x_group);
+            const Span ws{w, w + ((int64_t)(a.n - 1) * a.w_ld + a.k) * 2}, xs{x, x + ((int64_t)(a.m - 1) * a.x_ld + a.k) * 2};
+            const char *w_row = w + (int64_t)(n0 + r) * a.w_ld * 2, *x_row = x + (int64_t)(m0 + r) * a.x_ld * 2;
+            auto row_of = [&](int j) { return j < 4 ? w_row + j * 64 * a.w_ld : x_row + (j - 4) * 64 * a.x_ld; };
+            auto on = [&](int j) { return j < 4 ? n0 + r + 32 * j < a.n : m0 + r + 32 * (j - 4) < a.m && r + 32 * (j - 4) < NT; };
+            uint4 u[kOf], next[kOf];
+#pragma unroll
+            for (int j = 0; j < kOf; ++j) u[j] = piece(row_of(j), (int64_t)k_lo * 128 + c * 16, on(j), j < 4 ? ws : xs);
+            for (int ks = k_lo; ks < k_hi; ++ks) {
+                // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece)
+                const bool more = ks + 1 < k_hi || c == 0;
+#pragma unroll
+                for (int j = 0; j < kOf; ++j) next[j] = piece(row_of(j), (int64_t)(ks + 1) * 128 + c * 16, more && on(j), j < 4 ? ws : xs);
+                if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                unsigned char *dst = ring + st * S::kStage;
+                const int left = a.k - ks * kSlice - c * 8;
+#pragma unroll
+                for (int j = 0; j < kOf; ++j) {
+                    uint4 v = joined(u[j], next[j], (int)((uintptr_t)row_of(j) & 15), c, lane);
+                    if (left < 8) v = cut(v, left);
+                    if (!on(j)) v = make_uint4(0, 0, 0, 0);
+                    const int at = j < 4 ? r + 32 * j : r + 32 * (j - 4);
+                    if (j < 4 || at < NT) *reinterpret_cast<uint4 *>(dst + (j < 4 ? 0 : S::kA) + at * 128 + ((c ^ (at & 7)) << 4)) = v;
+                    u[j] = next[j];
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                bar_arrive(full + 8 * st);
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
@@ -656,15 +677,13 @@ int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int g
 template <int NT>
 int launch_as(const LinearArgs &a, int groups, int sms, bool wide, bool engine, cudaStream_t s)
 {
-    constexpr bool kBoth = NT <= 128;      // float32 results: the sums of a wider tile do not fit a thread's registers
+    constexpr bool kBoth = NT <= 128;              // float32 results: the sums of a wider tile do not fit a thread's registers
+    constexpr int  kByHand = NT > 64 ? 64 : NT;    // nor do the pieces of its rows where the block's threads load them
     CUtensorMap wmap{}, xmap{};
     engine = engine && encoder() && encode(&wmap, a.w, a.w_ld, a.w_group, a.n, groups, a.k, kRows) &&
              encode(&xmap, a.x, a.x_ld, a.x_group, a.m, groups, a.k, NT);
-    if (wide && kBoth) {
-        if (engine) return launch<NT, kBoth, true>(a, wmap, xmap, groups, sms, s);
-        return launch<(NT > 64 ? 64 : NT), kBoth, false>(a, wmap, xmap, groups, sms, s);   // (nor do 128 with twice the threads)
-    }
-    return engine ? launch<NT, false, true>(a, wmap, xmap, groups, sms, s) : launch<NT, false, false>(a, wmap, xmap, groups, sms, s);
+    if (wide && kBoth) return engine ? launch<NT, kBoth, true>(a, wmap, xmap, groups, sms, s) : launch<kByHand, kBoth, false>(a, wmap, xmap, groups, sms, s);
+    return engine ? launch<NT, false, true>(a, wmap, xmap, groups, sms, s) : launch<kByHand, false, false>(a, wmap, xmap, groups, sms, s);
 }
 
 }  // namespace
@@ -684,6 +703,9 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     if (!p.out || (p.k > 0 && (!p.x || !p.w)) || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
     if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || ((uintptr_t)p.out | (uintptr_t)p.residual) % width) return SYMAR_ERR_INVAL;
     if ((p.groups > 1 && p.out_group == 0) || (p.m > 1 && p.out_ld < p.n)) return SYMAR_ERR_INVAL;
+    if (p.x_ld < 0 || p.x_group < 0 || p.w_ld < 0 || p.w_group < 0 || p.bias_group < 0 || p.residual_ld < 0 || p.residual_group < 0 ||
+        p.out_ld < 0 || p.out_group < 0)
+        return SYMAR_ERR_INVAL;
     Device d;
     const int rc = device_info(&d);
     if (rc != SYMAR_OK) return rc;

@@ -26,7 +26,8 @@ def linear_args(**change):
 @pytest.mark.parametrize("change", [
     dict(x=None), dict(w=None), dict(out=None), dict(m=-1), dict(n=-1), dict(k=-1), dict(groups=-1), dict(act=5), dict(act=-1),
     dict(out_dtype=2), dict(root=1), dict(root=-2), dict(x=SOME + 1), dict(w=SOME + 1), dict(bias=SOME + 1), dict(out=SOME + 1),
-    dict(out=SOME + 2, out_dtype=symar.F32), dict(residual=SOME + 1), dict(groups=2, out_group=0), dict(out_ld=31),
+    dict(out=SOME + 2, out_dtype=symar.F32), dict(residual=SOME + 1), dict(groups=2, out_group=0), dict(out_ld=31), dict(x_ld=-64), dict(w_ld=-64),
+    dict(x_group=-1), dict(w_group=-1), dict(bias_group=-1), dict(residual_ld=-1), dict(residual_group=-1), dict(out_group=-1),
 ], ids=lambda c: ",".join(f"{k}={v}" for k, v in c.items()))
 def test_linear_refuses(lib, change):
     assert lib.symar_linear(linear_args(**change), None) == symar.ERR_INVAL
