@@ -284,15 +284,37 @@ __device__ __noinline__ uint4 edge_piece(const char *at, Span s)
         if (at + 2 * i >= s.lo && at + 2 * i + 2 <= s.hi) w[i >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t *>(at + 2 * i) << ((i & 1) * 16);
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint4 piece(const char *row, int64_t byte, bool on, Span s)
+// (predicated, not a branch: the loads of all rows go out one after the other)
+__device__ __forceinline__ uint4 load_if(const char *at, bool on)
 {
-    const char *at = reinterpret_cast<const char *>((uintptr_t)row & ~(uintptr_t)15) + byte;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (on && at < s.hi) {
-        if (at >= s.lo && at + 16 <= s.hi) v = __ldg(reinterpret_cast<const uint4 *>(at));
-        else v = edge_piece(at, s);
-    }
+    uint4 v;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+                 "@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(at), "r"((int)on));
     return v;
+}
+// One piece of each of N rows (of the first `split` of operand s0, the others of s1) where the row exists (bit 4 of how) and, for
+// what bit 5 does not vouch for, the piece lies in the operand; pieces that lie in it in part are put together element by element.
+template <int N>
+__device__ __forceinline__ void pieces(uint4 (&v)[N], const char *const (&at)[N], const int (&how)[N], int64_t byte, bool on, int split, Span s0, Span s1)
+{
+    bool rest = false;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const Span &s = j < split ? s0 : s1;
+        const char *p = at[j] + byte;
+        const bool want = on && (how[j] & 16), safe = (how[j] & 32) || (p >= s.lo && p + 16 <= s.hi);
+        v[j] = load_if(p, want && safe);
+        rest |= want && !safe;
+    }
+    if (rest) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const Span &s = j < split ? s0 : s1;
+            const char *p = at[j] + byte;
+            if (on && (how[j] & 16) && !((how[j] & 32) || (p >= s.lo && p + 16 <= s.hi))) v[j] = edge_piece(p, s);
+        }
+    }
 }
 __device__ __forceinline__ uint4 joined(const uint4 &u, const uint4 &next, int shift, int c, int lane)
 {
@@ -412,26 +434,35 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
             const char *w = reinterpret_cast<const char *>(a.w + g * a.w_group), *x = reinterpret_cast<const char *>(a.x + g * a.x_group);
             const Span ws{w, w + ((int64_t)(a.n - 1) * a.w_ld + a.k) * 2}, xs{x, x + ((int64_t)(a.m - 1) * a.x_ld + a.k) * 2};
             const char *w_row = w + (int64_t)(n0 + r) * a.w_ld * 2, *x_row = x + (int64_t)(m0 + r) * a.x_ld * 2;
-            auto row_of = [&](int j) { return j < 4 ? w_row + j * 64 * a.w_ld : x_row + (j - 4) * 64 * a.x_ld; };
-            auto on = [&](int j) { return j < 4 ? n0 + r + 32 * j < a.n : m0 + r + 32 * (j - 4) < a.m && r + 32 * (j - 4) < NT; };
+            const char *at[kOf];                       // the aligned piece that the row begins in
+            int how[kOf];                              // byte shift of the row, + 16 where it exists, + 32 where it is inner
+#pragma unroll
+            for (int j = 0; j < kOf; ++j) {
+                const char *row = j < 4 ? w_row + j * 64 * a.w_ld : x_row + (j - 4) * 64 * a.x_ld;
+                const int i = j < 4 ? n0 + r + 32 * j : m0 + r + 32 * (j - 4), rows = j < 4 ? a.n : a.m;
+                at[j]  = reinterpret_cast<const char *>((uintptr_t)row & ~(uintptr_t)15);
+                how[j] = (int)((uintptr_t)row & 15) | (i < rows && (j < 4 || r + 32 * (j - 4) < NT) ? 16 : 0) |
+                         (row >= (j < 4 ? ws : xs).lo + 16 && row + 2 * a.k + 32 <= (j < 4 ? ws : xs).hi ? 32 : 0);
+            }
             uint4 u[kOf], next[kOf];
-#pragma unroll
-            for (int j = 0; j < kOf; ++j) u[j] = piece(row_of(j), (int64_t)k_lo * 128 + c * 16, on(j), j < 4 ? ws : xs);
+            int64_t byte = (int64_t)k_lo * 128 + c * 16;
+            pieces<kOf>(u, at, how, byte, true, 4, ws, xs);
+#pragma unroll 2            // (the pieces on their way change places with those in hand without a copy, which would wait for them)
             for (int ks = k_lo; ks < k_hi; ++ks) {
-                // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece)
-                const bool more = ks + 1 < k_hi || c == 0;
-#pragma unroll
-                for (int j = 0; j < kOf; ++j) next[j] = piece(row_of(j), (int64_t)(ks + 1) * 128 + c * 16, more && on(j), j < 4 ? ws : xs);
+                // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece, which
+                // begins in the row)
+                byte += 128;
+                const int left = a.k - ks * kSlice - c * 8;
+                const bool more = left - kSlice + 8 > 0;
+                pieces<kOf>(next, at, how, byte, more, 4, ws, xs);
                 if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 unsigned char *dst = ring + st * S::kStage;
-                const int left = a.k - ks * kSlice - c * 8;
 #pragma unroll
                 for (int j = 0; j < kOf; ++j) {
-                    uint4 v = joined(u[j], next[j], (int)((uintptr_t)row_of(j) & 15), c, lane);
+                    uint4 v = joined(u[j], next[j], how[j], c, lane);
                     if (left < 8) v = cut(v, left);
-                    if (!on(j)) v = make_uint4(0, 0, 0, 0);
-                    const int at = j < 4 ? r + 32 * j : r + 32 * (j - 4);
-                    if (j < 4 || at < NT) *reinterpret_cast<uint4 *>(dst + (j < 4 ? 0 : S::kA) + at * 128 + ((c ^ (at & 7)) << 4)) = v;
+                    const int to = j < 4 ? r + 32 * j : r + 32 * (j - 4);
+                    if (j < 4 || to < NT) *reinterpret_cast<uint4 *>(dst + (j < 4 ? 0 : S::kA) + to * 128 + ((c ^ (to & 7)) << 4)) = v;
                     u[j] = next[j];
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -678,7 +709,7 @@ template <int NT>
 int launch_as(const LinearArgs &a, int groups, int sms, bool wide, bool engine, cudaStream_t s)
 {
     constexpr bool kBoth = NT <= 128;              // float32 results: the sums of a wider tile do not fit a thread's registers
-    constexpr int  kByHand = NT > 64 ? 64 : NT;    // nor do the pieces of its rows where the block's threads load them
+    constexpr int  kByHand = NT > 128 ? 128 : NT;    // nor do the pieces of its rows where the block's threads load them
     CUtensorMap wmap{}, xmap{};
     engine = engine && encoder() && encode(&wmap, a.w, a.w_ld, a.w_group, a.n, groups, a.k, kRows) &&
              encode(&xmap, a.x, a.x_ld, a.x_group, a.m, groups, a.k, NT);
