@@ -74,6 +74,24 @@ __device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t z)
     __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), *reinterpret_cast<__nv_bfloat162 *>(&z));
     return *reinterpret_cast<uint32_t *>(&d);
 }
+// n + 128 under the exponent of 128, zero points left in
+__device__ __forceinline__ uint32_t raw_nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }
+// a token's words
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t *p)
+{
+    if (N == 1) {
+        w[0] = p[0];
+    } else if (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        w[0] = v.x; w[N - 1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(p + i);
+            w[i] = v.x; w[(i + 1) % N] = v.y; w[(i + 2) % N] = v.z; w[(i + 3) % N] = v.w;
+        }
+    }
+}
 // 128 + z of two words' zero points
 __device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1) { return (__byte_perm(w0, w1, 0x5410) & 0x000f000fu) | 0x43004300u; }
 
@@ -134,11 +152,11 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
 {
     constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2, kUnits = D / 32;
     constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = 2 * (kCodes + kWords);
-    constexpr int kWarpBytes = kStages * kStage > R * D * 4 ? kStages * kStage : R * D * 4;
+    constexpr int kOut = D + 4;      // floats from row to row of a warp's result: rows start in different banks
+    constexpr int kWarpBytes = kStages * kStage > R * kOut * 4 ? kStages * kStage : R * kOut * 4;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int64_t warp_sum[kWarps];
     __shared__ float   warp_m[kWarps][R], warp_l[kWarps][R];
-    __shared__ int     page_ok[kWarps][kStages];
     __shared__ int64_t at_flat;
     __shared__ int     at_seq, is_last;
 
@@ -199,6 +217,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
         if (tid == 0 && s.len > (a.b.table_ld << a.c.page_shift)) kv_record(a.status, seq, (int)(a.b.table_ld << a.c.page_shift));
         // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
         uint32_t qf[NB][NG * 4][2];
+        float qs[NB][NG][2];                    // the sum of a group's channels in this thread's two columns
         int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
         const int rows = s.fresh * a.share;
 #pragma unroll
@@ -225,6 +244,19 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                     qf[nb][gr * 4 + 2][half] = __byte_perm(v.y, v.w, 0x5410);
                     qf[nb][gr * 4 + 3][half] = __byte_perm(v.y, v.w, 0x7632);
                 }
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t v = qf[nb][gr * 4 + i / 2][i & 1];
+                    sum += __uint_as_float(v << 16) + __uint_as_float(v & 0xffff0000u);
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                qs[nb][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+                qs[nb][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = block * R + nb * 8 + 2 * t + j;
@@ -256,61 +288,68 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
         // ---- this warp's chunks: c_begin + warp, + kWarps, ... ----
         const int n = c_end - c_begin > warp ? (c_end - c_begin - warp + kWarps - 1) / kWarps : 0;
         int pages = -1;                                       // lane i: the page of the warp's chunk (k & ~31) + i
-        auto token_of = [&](int k) { return item.lo + (c_begin + warp + k * kWarps) * 16; };
+        uint32_t seen = 0;                                    // bit i: the chunk fetched i fetches ago has a page
+        const int first_tok = item.lo + (c_begin + warp) * 16;
+        const unsigned char *head_base = a.c.pages + head * a.c.head_bytes + lane * 16;
+        const int side_bytes = ps * kRow;
+        const int word_side = lane / (4 * NG);                // lanes below 8 NG copy words: 4 NG pieces of each side
+        const int word_src = 2 * side_bytes + word_side * (ps * NG * 4 - 4 * NG * 16);
+        int f_tok = first_tok, f_at = 0;                      // next fetch: its first token, its stage's offset
         auto fetch = [&](int k) {
             if (k < n) {
                 if ((k & 31) == 0) {
-                    const int tok = token_of(k + lane);
+                    const int tok = f_tok + lane * (16 * kWarps);
                     pages = k + lane < n && tok < s.len ? kv_page_of(a.c, a.b, a.status, seq, tok) : -1;
                 }
-                const int page = __shfl_sync(0xffffffffu, pages, k & 31);
-                const int st = k % kStages, slot = token_of(k) & (ps - 1);
+                const int page = __shfl_sync(0xffffffffu, pages, k & 31), slot = f_tok & (ps - 1);
                 const bool on = page >= 0;
-                const unsigned char *base = a.c.pages + (on ? page : 0) * a.c.page_bytes + head * a.c.head_bytes;
-                const uint32_t dst = mine_addr + st * kStage;
+                const unsigned char *base = head_base + (int64_t)(on ? page : 0) * a.c.page_bytes;
+                const unsigned char *src = base + slot * kRow;
+                const uint32_t dst = mine_addr + f_at;
 #pragma unroll
-                for (int side = 0; side < 2; ++side) {
-                    const unsigned char *src = base + (side * ps + slot) * kRow;
-#pragma unroll
-                    for (int u0 = 0; u0 < 16 * kUnits; u0 += 32) {
-                        const int u = u0 + lane, tok = u / kUnits, c = u % kUnits;
-                        const int turn = D == 64 ? tok >> 2 & 1 : (D == 128 ? tok >> 1 & 3 : tok & 7);
-                        copy16(dst + side * kCodes + tok * kRow + ((c ^ turn) << 4), src + u * 16, on);
-                    }
+                for (int u0 = 0; u0 < 16 * kUnits; u0 += 32) {
+                    const int tok = (u0 + lane) / kUnits, c = lane % kUnits;
+                    const int turn = D == 64 ? tok >> 2 & 1 : (D == 128 ? tok >> 1 & 3 : tok & 7);
+                    const uint32_t to = dst + tok * kRow + ((c ^ turn) << 4);
+                    copy16(to, src + u0 * 16, on);
+                    copy16(to + kCodes, src + side_bytes + u0 * 16, on);
                 }
-                if (lane < 8 * NG) {
-                    const int side = lane / (4 * NG), u = lane % (4 * NG);
-                    copy16(dst + 2 * kCodes + side * kWords + u * 16, base + ps * D + (side * ps + slot) * NG * 4 + u * 16, on);
-                }
-                if (lane == 0) page_ok[warp][st] = on;
+                if (lane < 8 * NG) copy16(dst + 2 * kCodes + lane * 16, base + word_src + slot * (NG * 4), on);
+                seen = seen << 1 | (uint32_t)on;
+                f_tok += 16 * kWarps;
+                f_at = f_at == (kStages - 1) * kStage ? 0 : f_at + kStage;
             }
             copies_commit();
         };
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k) fetch(k);
-        for (int k = 0; k < n; ++k) {
+        int tok0 = first_tok, at = 0;
+        for (int k = 0; k < n; ++k, tok0 += 16 * kWarps, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
             copies_wait<kStages - 2>();
             __syncwarp();
+            const int ahead = min(kStages - 1, n - 1 - k);            // chunks fetched after this one
             fetch(k + kStages - 1);
-            const int st = k % kStages, tok0 = token_of(k);
-            const uint32_t base = mine_addr + st * kStage;
-            const unsigned char *stage = mine + st * kStage;
+            const bool paged = seen >> ahead & 1;
+            const uint32_t base = mine_addr + at;
+            const unsigned char *stage = mine + at;
             // lane i names row i % 8 of matrix i / 8: tokens 0-7 and 8-15, first and second 32 channels of the group
             const int mt = (lane >> 4) * 8 + (lane & 7), mc = lane >> 3 & 1;
             const int turn = D == 64 ? mt >> 2 & 1 : (D == 128 ? mt >> 1 & 3 : mt & 7);
             const uint32_t *kw = reinterpret_cast<const uint32_t *>(stage + 2 * kCodes), *vw = kw + 16 * NG;
 
+            // score = s (acc - (128 + z) sum of q): the zero points are taken off the sums, not off every code
             float sc[NB][4];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sc[nb][j] = 0.0f;
+            uint32_t w0[NG], w1[NG];
+            load_words<NG>(w0, kw + g * NG);
+            load_words<NG>(w1, kw + (g + 8) * NG);
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 uint32_t r[4];
                 matrices(r, base + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
-                const uint32_t w0 = kw[g * NG + gr], w1 = kw[(g + 8) * NG + gr];
-                const uint32_t z0 = zeros_of(w0, w0), z1 = zeros_of(w1, w1);
                 float acc[NB][4];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
@@ -318,30 +357,31 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                     for (int j = 0; j < 4; ++j) acc[nb][j] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = nibbles(r[0] >> 4 * i, z0), a1 = nibbles(r[2] >> 4 * i, z1);
-                    const uint32_t a2 = nibbles(r[1] >> 4 * i, z0), a3 = nibbles(r[3] >> 4 * i, z1);
+                    const uint32_t a0 = raw_nibbles(r[0] >> 4 * i), a1 = raw_nibbles(r[2] >> 4 * i);
+                    const uint32_t a2 = raw_nibbles(r[1] >> 4 * i), a3 = raw_nibbles(r[3] >> 4 * i);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma(acc[nb], a0, a1, a2, a3, qf[nb][gr * 4 + i][0], qf[nb][gr * 4 + i][1]);
                 }
-                const float f0 = kv_scale(w0) * a.scale_log2, f1 = kv_scale(w1) * a.scale_log2;
+                const float f0 = kv_scale(w0[gr]) * a.scale_log2, f1 = kv_scale(w1[gr]) * a.scale_log2;
+                const float h0 = -f0 * __uint_as_float((w0[gr] & 15u) * 65536u + 0x43000000u);      // 128 + z
+                const float h1 = -f1 * __uint_as_float((w1[gr] & 15u) * 65536u + 0x43000000u);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    sc[nb][0] = __fmaf_rn(acc[nb][0], f0, sc[nb][0]);
-                    sc[nb][1] = __fmaf_rn(acc[nb][1], f0, sc[nb][1]);
-                    sc[nb][2] = __fmaf_rn(acc[nb][2], f1, sc[nb][2]);
-                    sc[nb][3] = __fmaf_rn(acc[nb][3], f1, sc[nb][3]);
+                    sc[nb][0] = __fmaf_rn(qs[nb][gr][0], h0, __fmaf_rn(acc[nb][0], f0, sc[nb][0]));
+                    sc[nb][1] = __fmaf_rn(qs[nb][gr][1], h0, __fmaf_rn(acc[nb][1], f0, sc[nb][1]));
+                    sc[nb][2] = __fmaf_rn(qs[nb][gr][0], h1, __fmaf_rn(acc[nb][2], f1, sc[nb][2]));
+                    sc[nb][3] = __fmaf_rn(qs[nb][gr][1], h1, __fmaf_rn(acc[nb][3], f1, sc[nb][3]));
                 }
             }
             // rows of the fragment: tokens tok0 + g (0, 1) and tok0 + g + 8 (2, 3); columns 2t and 2t + 1
-            const bool whole = tok0 + 16 <= least_hi && tok0 >= most_lo && page_ok[warp][st];
+            const bool whole = tok0 + 16 <= least_hi && tok0 >= most_lo && paged;
             if (!whole) {
-                const bool some = page_ok[warp][st];
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int tok = tok0 + g + (j >> 1) * 8;
-                        if (!some || tok >= hi[nb][j & 1] || tok < lo[nb][j & 1] || tok >= s.len) sc[nb][j] = -INFINITY;
+                        if (!paged || tok >= hi[nb][j & 1] || tok < lo[nb][j & 1] || tok >= s.len) sc[nb][j] = -INFINITY;
                     }
             }
             bool rise = false;
@@ -376,23 +416,30 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                 l[nb][0] += sc[nb][0] + sc[nb][2];
                 l[nb][1] += sc[nb][1] + sc[nb][3];
             }
+            uint32_t z2[4][NG];                              // words of the tokens 2t, 2t + 1, 2t + 8, 2t + 9
+            load_words<NG>(w0, vw + g * NG);
+            load_words<NG>(w1, vw + (g + 8) * NG);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) load_words<NG>(z2[j], vw + (2 * t + (j >> 1) * 8 + (j & 1)) * NG);
+            if (!whole) {
+                // beyond the sequence's end a page holds anything: no scale from there may meet a probability of 0
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    w0[gr] = tok0 + g < s.len ? w0[gr] : 0u;
+                    w1[gr] = tok0 + g + 8 < s.len ? w1[gr] : 0u;
+                }
+            }
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 uint32_t r[4], pf[NB][2];
                 matrices_t(r, base + kCodes + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
-                // beyond the sequence's end a page holds anything: no scale from there may meet a probability of 0
-                float f0 = kv_scale(vw[g * NG + gr]), f1 = kv_scale(vw[(g + 8) * NG + gr]);
-                if (!whole) {
-                    f0 = tok0 + g < s.len ? f0 : 0.0f;
-                    f1 = tok0 + g + 8 < s.len ? f1 : 0.0f;
-                }
+                const float f0 = kv_scale(w0[gr]), f1 = kv_scale(w1[gr]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     pf[nb][0] = transposed(pack_bf16(sc[nb][0] * f0, sc[nb][1] * f0));
                     pf[nb][1] = transposed(pack_bf16(sc[nb][2] * f1, sc[nb][3] * f1));
                 }
-                const uint32_t z0 = zeros_of(vw[2 * t * NG + gr], vw[(2 * t + 1) * NG + gr]);
-                const uint32_t z1 = zeros_of(vw[(2 * t + 8) * NG + gr], vw[(2 * t + 9) * NG + gr]);
+                const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr]), z1 = zeros_of(z2[2][gr], z2[3][gr]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t a0 = nibbles(r[0] >> 4 * i, z0), a1 = nibbles(r[1] >> 4 * i, z0);
@@ -425,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                 for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
-                        *reinterpret_cast<float4 *>(wo + row * D + gr * 64 + half * 32 + 4 * g) =
+                        *reinterpret_cast<float4 *>(wo + row * kOut + gr * 64 + half * 32 + 4 * g) =
                             make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half],
                                         o[nb][gr * 4 + 2][j + 2 * half], o[nb][gr * 4 + 3][j + 2 * half]);
             }
@@ -455,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const float f = power2(warp_m[w][row] - top);
-                const float4 x = *reinterpret_cast<const float4 *>(smem + w * kWarpBytes + (row * D + d) * 4);
+                const float4 x = *reinterpret_cast<const float4 *>(smem + w * kWarpBytes + (row * kOut + d) * 4);
                 sum = __fmaf_rn(warp_l[w][row], f, sum);
                 v.x = __fmaf_rn(x.x, f, v.x); v.y = __fmaf_rn(x.y, f, v.y);
                 v.z = __fmaf_rn(x.z, f, v.z); v.w = __fmaf_rn(x.w, f, v.w);
@@ -483,21 +530,42 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
             }
             __syncthreads();
             if (is_last) {
+                // weights first, a warp per row, then every thread its part of the output, many loads at a time
+                const int parts = (int)(last - first) + 1;
+                float *weight = reinterpret_cast<float *>(smem);          // [part][R]
+                auto part = [&](int x) { return a.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * (R * (D + 2)); };
+                for (int row = warp; row < R; row += kWarps) {
+                    float top = kNothing, sum = 0.0f;
+                    for (int x = lane; x < parts; x += 32) top = fmaxf(top, __ldcg(part(x) + row));
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    for (int x = lane; x < parts; x += 32) {
+                        const float f = power2(__ldcg(part(x) + row) - top);
+                        weight[x * R + row] = f;
+                        sum = __fmaf_rn(__ldcg(part(x) + R + row), f, sum);
+                    }
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    if (lane == 0) warp_l[0][row] = sum;
+                }
+                __syncthreads();
                 for (int i = tid; i < R * D / 4; i += kThreads) {
                     const int row = i / (D / 4), d = i % (D / 4) * 4;
-                    float top = kNothing, sum = 0.0f;
-                    for (int64_t x = first; x <= last; ++x)
-                        top = fmaxf(top, __ldcg(a.partials + (size_t)(2 * x + (x == first ? 1 : 0)) * (R * (D + 2)) + row));
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int64_t x = first; x <= last; ++x) {
-                        const float *p = a.partials + (size_t)(2 * x + (x == first ? 1 : 0)) * (R * (D + 2));
-                        const float f = power2(__ldcg(p + row) - top);
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + 2 * R + row * D + d));
-                        sum = __fmaf_rn(__ldcg(p + R + row), f, sum);
-                        v.x = __fmaf_rn(y.x, f, v.x); v.y = __fmaf_rn(y.y, f, v.y);
-                        v.z = __fmaf_rn(y.z, f, v.z); v.w = __fmaf_rn(y.w, f, v.w);
+                    for (int x0 = 0; x0 < parts; x0 += 8) {
+                        float4 y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (x0 + j < parts) y[j] = __ldcg(reinterpret_cast<const float4 *>(part(x0 + j) + 2 * R + row * D + d));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (x0 + j < parts) {
+                                const float f = weight[(x0 + j) * R + row];
+                                v.x = __fmaf_rn(y[j].x, f, v.x); v.y = __fmaf_rn(y[j].y, f, v.y);
+                                v.z = __fmaf_rn(y[j].z, f, v.z); v.w = __fmaf_rn(y[j].w, f, v.w);
+                            }
                     }
-                    store(row, d, v, sum);
+                    store(row, d, v, warp_l[0][row]);
                 }
             }
         }
@@ -524,7 +592,7 @@ template <int D, int NB>
 cudaError_t launch(const AttnArgs &a, int num_sms, cudaStream_t stream)
 {
     constexpr int R = 8 * NB, kStage = 16 * D + 16 * (D / 64) * 8;
-    constexpr int kWarpBytes = kStages * kStage > R * D * 4 ? kStages * kStage : R * D * 4;
+    constexpr int kWarpBytes = kStages * kStage > R * (D + 4) * 4 ? kStages * kStage : R * (D + 4) * 4;
     constexpr int kBytes = kWarps * kWarpBytes;
     cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != cudaSuccess) return e;
