@@ -19,6 +19,7 @@ struct AttnArgs {
     int64_t q_ld, q_head, out_ld, out_head;
     float   scale_log2;         // scale * log2(e): softmax in powers of two
     int     q_heads, share, window, q_vec, out_vec;
+    uint32_t magic, one;        // bf16 128 and 1, twice each (see nibbles)
     int    *status;
     unsigned *counters;
     float  *partials;
@@ -66,16 +67,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t *>(&h);
 }
-// Nibbles 0 and 4 of w, less the zero points of which `z` holds 128 + z twice, as two exact bf16: a nibble n under the
-// exponent of 128 is 128 + n, and the difference of two such numbers is exact.
-__device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t z)
+// Nibbles 0 and 4 of w as bf16: a nibble n under the exponent of 128 is 128 + n.  `magic` is that exponent twice, in a register that
+// the compiler does not know to be a constant: with two constants it takes two instructions for what is one.
+__device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t magic)
 {
-    uint32_t v = (w & 0x000f000fu) | 0x43004300u;
-    __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), *reinterpret_cast<__nv_bfloat162 *>(&z));
-    return *reinterpret_cast<uint32_t *>(&d);
+    uint32_t v;
+    asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(v) : "r"(w), "r"(magic));       // (w & mask) | magic
+    return v;
 }
-// n + 128 under the exponent of 128, zero points left in
-__device__ __forceinline__ uint32_t raw_nibbles(uint32_t w) { return (w & 0x000f000fu) | 0x43004300u; }
+// n - z, exact: `less` holds -(128 + z) twice
+__device__ __forceinline__ uint32_t minus(uint32_t v, uint32_t less, uint32_t one)
+{
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(one), "r"(less));
+    return d;
+}
 // a token's words
 template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t *p)
 {
@@ -92,8 +98,8 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
         }
     }
 }
-// 128 + z of two words' zero points
-__device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1) { return (__byte_perm(w0, w1, 0x5410) & 0x000f000fu) | 0x43004300u; }
+// -(128 + z) of two words' zero points
+__device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1, uint32_t magic) { return nibbles(__byte_perm(w0, w1, 0x5410), magic) ^ 0x80008000u; }
 
 // ---- the sequences as work ----------------------------------------------------------------
 // An item is `rows` query rows (a token and a head of the key/value head's share, tokens first) of one sequence and one
@@ -162,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     unsigned char *mine = smem + warp * kWarpBytes;
-    const uint32_t mine_addr = smem_addr(mine);
+    const uint32_t mine_addr = smem_addr(mine), magic = a.magic, one = a.one;
 
     // ---- this block's share: chunks [begin, end) of all items in order ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
@@ -357,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                     for (int j = 0; j < 4; ++j) acc[nb][j] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = raw_nibbles(r[0] >> 4 * i), a1 = raw_nibbles(r[2] >> 4 * i);
-                    const uint32_t a2 = raw_nibbles(r[1] >> 4 * i), a3 = raw_nibbles(r[3] >> 4 * i);
+                    const uint32_t a0 = nibbles(r[0] >> 4 * i, magic), a1 = nibbles(r[2] >> 4 * i, magic);
+                    const uint32_t a2 = nibbles(r[1] >> 4 * i, magic), a3 = nibbles(r[3] >> 4 * i, magic);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma(acc[nb], a0, a1, a2, a3, qf[nb][gr * 4 + i][0], qf[nb][gr * 4 + i][1]);
                 }
@@ -439,11 +445,11 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                     pf[nb][0] = transposed(pack_bf16(sc[nb][0] * f0, sc[nb][1] * f0));
                     pf[nb][1] = transposed(pack_bf16(sc[nb][2] * f1, sc[nb][3] * f1));
                 }
-                const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr]), z1 = zeros_of(z2[2][gr], z2[3][gr]);
+                const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr], magic), z1 = zeros_of(z2[2][gr], z2[3][gr], magic);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = nibbles(r[0] >> 4 * i, z0), a1 = nibbles(r[1] >> 4 * i, z0);
-                    const uint32_t a2 = nibbles(r[2] >> 4 * i, z1), a3 = nibbles(r[3] >> 4 * i, z1);
+                    const uint32_t a0 = minus(nibbles(r[0] >> 4 * i, magic), z0, one), a1 = minus(nibbles(r[1] >> 4 * i, magic), z0, one);
+                    const uint32_t a2 = minus(nibbles(r[2] >> 4 * i, magic), z1, one), a3 = minus(nibbles(r[3] >> 4 * i, magic), z1, one);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
                 }
@@ -632,6 +638,8 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     a.share      = args->q_heads / cache->kv_heads;
     a.q_vec      = (uintptr_t)args->q % 16 == 0 && args->q_ld % 8 == 0 && args->q_head % 8 == 0;
     a.out_vec    = (uintptr_t)args->out % 8 == 0 && args->out_ld % 4 == 0 && args->out_head % 4 == 0;
+    a.magic      = 0x43004300u;
+    a.one        = 0x3f803f80u;
     a.counters   = kv->counters;
     a.partials   = kv->partials;
     if ((int64_t)a.b.tokens * a.share > 0x7fff0000) return SYMAR_ERR_UNSUPPORTED;
