@@ -6,10 +6,9 @@
 namespace symar {
 namespace {
 
-constexpr int kWarps   = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kStages  = 5;            // copies in flight per warp: four chunks ahead of the one in use
-constexpr int kMinChunks = 4 * kWarps; // a block's share of the work is at least this many chunks of 16 tokens
+constexpr int kStages   = 4;           // copies in flight per warp: three chunks ahead of the one in use
+constexpr int kMinChunks = 4;          // a warp's share of the work is at least this many chunks of 16 tokens
+constexpr int kItemCost  = 3;          // what an item costs a warp besides its chunks, in chunks
 
 struct AttnArgs {
     KvView  c;
@@ -135,12 +134,28 @@ __device__ __forceinline__ Item item_of(const AttnArgs &a, const Seq &s, int blo
     return Item{lo, max((hi - lo + 15) >> 4, 1)};
 }
 template <int R>
-__device__ __forceinline__ int64_t chunks_of(const AttnArgs &a, const Seq &s)
+__device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 {
     const int blocks = (s.fresh * a.share + R - 1) / R;
     int64_t n = 0;
-    for (int i = 0; i < blocks; ++i) n += item_of<R>(a, s, i).chunks;
+    for (int i = 0; i < blocks; ++i) n += item_of<R>(a, s, i).chunks + kItemCost;
     return n * a.c.kv_heads;
+}
+
+// Four channels of a row's output, divided by the row's sum (0 where nothing was seen).
+__device__ __forceinline__ void store4(const AttnArgs &a, const Seq &s, int rows, int r, int head, int d, float4 v, float sum)
+{
+    if (r >= rows) return;
+    const int tok = r / a.share, hh = r - tok * a.share;
+    const float f = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+    __nv_bfloat16 *p = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head + d;
+    const uint32_t x = pack_bf16(v.x * f, v.y * f), y = pack_bf16(v.z * f, v.w * f);
+    if (a.out_vec) {
+        *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
+    } else {
+        uint16_t *h = reinterpret_cast<uint16_t *>(p);
+        h[0] = (uint16_t)x; h[1] = (uint16_t)(x >> 16); h[2] = (uint16_t)y; h[3] = (uint16_t)(y >> 16);
+    }
 }
 
 // One softmax over all work of an item, wherever it was done: unnormalised output relative to 2^m, and its sum.
@@ -154,27 +169,45 @@ constexpr float kNothing = -3.402823466e38f;
 // it is rounded to bf16 (V), the one rounding that binary32 arithmetic would not have.
 // The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
 template <int D, int NB>
-__global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attention_kernel(const AttnArgs a)
+struct Shape {
+    static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;
+    static constexpr int kWarps  = D == 256 && NB == 2 ? 4 : 8;
+    static constexpr int kBlocks = NB == 1 && D <= 128 ? 2 : 1;          // per multiprocessor
+    static constexpr int kOut    = D + 4;                                // floats from row to row of a partial result: rows start in different banks
+    static constexpr int kPart   = (R * kOut + 2 * R) * 4;               // output, maxima, sums
+    static constexpr int kStage  = 2 * 16 * (kRow + NG * 4);
+    static constexpr int kRing   = kStages * kStage > kPart ? kStages * kStage : kPart;
+    static constexpr int kBytes  = kWarps * (kRing + kPart);
+};
+// A piece of an item that does not make it whole: chunks [begin, end) of `chunks`.
+struct Piece {
+    int64_t at;                  // the item's place in the order of all work
+    int     seq, block, head, begin, end, chunks;
+};
+
+template <int D, int NB>
+__global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBlocks) attention_kernel(const AttnArgs a)
 {
-    constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2, kUnits = D / 32;
-    constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = 2 * (kCodes + kWords);
-    constexpr int kOut = D + 4;      // floats from row to row of a warp's result: rows start in different banks
-    constexpr int kWarpBytes = kStages * kStage > R * kOut * 4 ? kStages * kStage : R * kOut * 4;
+    using S = Shape<D, NB>;
+    constexpr int R = S::R, NG = S::NG, kRow = S::kRow, kUnits = D / 32, kWarps = S::kWarps, kThreads = 32 * kWarps;
+    constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = S::kStage, kOut = S::kOut;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int64_t warp_sum[kWarps];
-    __shared__ float   warp_m[kWarps][R], warp_l[kWarps][R];
-    __shared__ int64_t at_flat;
-    __shared__ int     at_seq, is_last;
+    __shared__ int64_t warp_sum[kWarps], at_flat[kWarps];
+    __shared__ int     at_seq[kWarps], is_last;
+    __shared__ Piece   piece[2 * kWarps];        // of each warp: the end of an item that began before, the beginning of one that goes on
+    __shared__ float   row_sum[R];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    unsigned char *mine = smem + warp * kWarpBytes;
+    // this warp's ring; its unfinished first piece has a place of its own, its unfinished last piece that of the ring
+    unsigned char *mine = smem + warp * S::kRing;
+    auto result_of = [&](int i) { return reinterpret_cast<float *>(i & 1 ? smem + (i >> 1) * S::kRing : smem + kWarps * S::kRing + (i >> 1) * S::kPart); };
     const uint32_t mine_addr = smem_addr(mine), magic = a.magic, one = a.one;
 
-    // ---- this block's share: chunks [begin, end) of all items in order ----
+    // ---- shares: places [begin, end) of all items in order, kItemCost places and one per chunk each ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
     int64_t own = 0;
-    for (int b = s0; b < s1; ++b) own += chunks_of<R>(a, sequence(a, b));
+    for (int b = s0; b < s1; ++b) own += places_of<R>(a, sequence(a, b));
     int64_t incl = own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -182,50 +215,58 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
         if (lane >= d) incl += o;
     }
     if (lane == 31) warp_sum[warp] = incl;
+    if (tid < 2 * kWarps) piece[tid].chunks = 0;
     __syncthreads();
     int64_t total = 0;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w == warp) incl += total;
         total += warp_sum[w];
     }
-    const int64_t per = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinChunks);
-    const int64_t begin = per * blockIdx.x, end = min(begin + per, total);
-    if (begin >= total) return;
-    if (begin >= incl - own && begin < incl) {
-        int64_t flat = incl - own;
-        for (int b = s0; b < s1; ++b) {
-            const int64_t n = chunks_of<R>(a, sequence(a, b));
-            if (begin < flat + n) {
-                at_seq  = b;
-                at_flat = flat;
-                break;
+    const int64_t per_warp = max((total + (int64_t)gridDim.x * kWarps - 1) / ((int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
+    const int64_t per = per_warp * kWarps, block_begin = per * blockIdx.x;
+    if (block_begin >= total) return;
+    for (int w = 0; w < kWarps; ++w) {
+        const int64_t begin = block_begin + w * per_warp;
+        if (begin >= incl - own && begin < incl) {
+            int64_t flat = incl - own;
+            for (int b = s0; b < s1; ++b) {
+                const int64_t n = places_of<R>(a, sequence(a, b));
+                if (begin < flat + n) {
+                    at_seq[w]  = b;
+                    at_flat[w] = flat;
+                    break;
+                }
+                flat += n;
             }
-            flat += n;
         }
     }
     __syncthreads();
-    int seq = at_seq;
-    int64_t item_at = at_flat;                       // flat index of the current item's first chunk
-    Seq  s   = sequence(a, seq);
-    int  block = 0, head = 0;
+    const int64_t begin = block_begin + warp * per_warp, end = min(begin + per_warp, total);
+    const int ps = 1 << a.c.page_shift;
+
+    if (begin < end) {
+    int seq = at_seq[warp], block = 0, head = 0;
+    int64_t item_at = at_flat[warp];                 // place of the current item
+    Seq  s    = sequence(a, seq);
     Item item = item_of<R>(a, s, 0);
-    while (item_at + (int64_t)item.chunks * a.c.kv_heads <= begin) {
-        item_at += (int64_t)item.chunks * a.c.kv_heads;
+    while (item_at + (int64_t)(item.chunks + kItemCost) * a.c.kv_heads <= begin) {
+        item_at += (int64_t)(item.chunks + kItemCost) * a.c.kv_heads;
         item = item_of<R>(a, s, ++block);
     }
-    head = (int)((begin - item_at) / item.chunks);
-    item_at += (int64_t)head * item.chunks;
+    head = (int)((begin - item_at) / (item.chunks + kItemCost));
+    item_at += (int64_t)head * (item.chunks + kItemCost);
 
-    const int ps = 1 << a.c.page_shift;
-    int64_t flat = begin;
-    while (flat < end) {
-        const int c_begin = (int)(flat - item_at), c_end = (int)min((int64_t)item.chunks, end - item_at);
-        if (tid == 0 && s.len > (a.b.table_ld << a.c.page_shift)) kv_record(a.status, seq, (int)(a.b.table_ld << a.c.page_shift));
+    for (;;) {
+        // (an item's own places come before those of its chunks)
+        const int c_begin = (int)max(begin - item_at - kItemCost, (int64_t)0), c_end = (int)min((int64_t)item.chunks, end - item_at - kItemCost);
+        const int rows = s.fresh * a.share;
+        if (c_begin < c_end) {
+        if (lane == 0 && s.len > (a.b.table_ld << a.c.page_shift)) kv_record(a.status, seq, (int)(a.b.table_ld << a.c.page_shift));
         // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
         uint32_t qf[NB][NG * 4][2];
         float qs[NB][NG][2];                    // the sum of a group's channels in this thread's two columns
         int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
-        const int rows = s.fresh * a.share;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int row = block * R + nb * 8 + g;
@@ -291,11 +332,11 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
             l[nb][0] = l[nb][1] = 0.0f;
         }
 
-        // ---- this warp's chunks: c_begin + warp, + kWarps, ... ----
-        const int n = c_end - c_begin > warp ? (c_end - c_begin - warp + kWarps - 1) / kWarps : 0;
-        int pages = -1;                                       // lane i: the page of the warp's chunk (k & ~31) + i
+        // ---- the chunks ----
+        const int n = c_end - c_begin;
+        int pages = -1;                                       // lane i: the page of chunk (k & ~31) + i
         uint32_t seen = 0;                                    // bit i: the chunk fetched i fetches ago has a page
-        const int first_tok = item.lo + (c_begin + warp) * 16;
+        const int first_tok = item.lo + c_begin * 16;
         const unsigned char *head_base = a.c.pages + head * a.c.head_bytes + lane * 16;
         const int side_bytes = ps * kRow;
         const int word_side = lane / (4 * NG);                // lanes below 8 NG copy words: 4 NG pieces of each side
@@ -304,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
         auto fetch = [&](int k) {
             if (k < n) {
                 if ((k & 31) == 0) {
-                    const int tok = f_tok + lane * (16 * kWarps);
+                    const int tok = f_tok + lane * 16;
                     pages = k + lane < n && tok < s.len ? kv_page_of(a.c, a.b, a.status, seq, tok) : -1;
                 }
                 const int page = __shfl_sync(0xffffffffu, pages, k & 31), slot = f_tok & (ps - 1);
@@ -322,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                 }
                 if (lane < 8 * NG) copy16(dst + 2 * kCodes + lane * 16, base + word_src + slot * (NG * 4), on);
                 seen = seen << 1 | (uint32_t)on;
-                f_tok += 16 * kWarps;
+                f_tok += 16;
                 f_at = f_at == (kStages - 1) * kStage ? 0 : f_at + kStage;
             }
             copies_commit();
@@ -330,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k) fetch(k);
         int tok0 = first_tok, at = 0;
-        for (int k = 0; k < n; ++k, tok0 += 16 * kWarps, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
+        for (int k = 0; k < n; ++k, tok0 += 16, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
             copies_wait<kStages - 2>();
             __syncwarp();
             const int ahead = min(kStages - 1, n - 1 - k);            // chunks fetched after this one
@@ -457,64 +498,91 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
         }
         copies_wait<0>();
 
-        // ---- the warps' results become one ----
-        // fragment i of a group: channels 4 g + i (0, 1) and 32 + 4 g + i (2, 3) of it
-        float *wo = reinterpret_cast<float *>(mine);
         __syncwarp();
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float sum = l[nb][j];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                l[nb][j] += __shfl_xor_sync(0xffffffffu, l[nb][j], 4);
+                l[nb][j] += __shfl_xor_sync(0xffffffffu, l[nb][j], 8);
+                l[nb][j] += __shfl_xor_sync(0xffffffffu, l[nb][j], 16);
+            }
+        const bool all = c_begin == 0 && c_end == item.chunks;
+        const int which = 2 * warp + (c_begin == 0 ? 1 : 0);
+        float *to = result_of(which);
+        if (!all && lane == 0) piece[which] = Piece{item_at, seq, block, head, c_begin, c_end, item.chunks};
+        // fragment i of a group: channels 4 g + i (0, 1) and 32 + 4 g + i (2, 3) of it
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
                 const int row = nb * 8 + 2 * t + j;
-                if (g == 0) {
-                    warp_m[warp][row] = m[nb][j];
-                    warp_l[warp][row] = sum;
+                if (!all && g == 0) {
+                    to[R * kOut + row]     = m[nb][j];
+                    to[R * kOut + R + row] = l[nb][j];
                 }
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        *reinterpret_cast<float4 *>(wo + row * kOut + gr * 64 + half * 32 + 4 * g) =
-                            make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half],
-                                        o[nb][gr * 4 + 2][j + 2 * half], o[nb][gr * 4 + 3][j + 2 * half]);
+                    for (int half = 0; half < 2; ++half) {
+                        const float4 v = make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half],
+                                                     o[nb][gr * 4 + 2][j + 2 * half], o[nb][gr * 4 + 3][j + 2 * half]);
+                        const int d = gr * 64 + half * 32 + 4 * g;
+                        if (all) store4(a, s, rows, block * R + row, head, d, v, l[nb][j]);
+                        else *reinterpret_cast<float4 *>(to + row * kOut + d) = v;
+                    }
             }
-        __syncthreads();
-        const bool all = c_begin == 0 && c_end == item.chunks;
-        float *slot = a.partials + (size_t)(2 * blockIdx.x + (c_begin == 0 ? 1 : 0)) * (R * (D + 2));
-        auto store = [&](int row, int d, float4 v, float sum) {
-            const int r = block * R + row;
-            if (r >= rows) return;
-            const int tok = r / a.share, hh = r - tok * a.share;
-            const float f = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-            __nv_bfloat16 *p = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head + d;
-            const uint32_t x = pack_bf16(v.x * f, v.y * f), y = pack_bf16(v.z * f, v.w * f);
-            if (a.out_vec) {
-                *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
-            } else {
-                uint16_t *h = reinterpret_cast<uint16_t *>(p);
-                h[0] = (uint16_t)x; h[1] = (uint16_t)(x >> 16); h[2] = (uint16_t)y; h[3] = (uint16_t)(y >> 16);
+        __syncwarp();
+        }
+        // ---- next ----
+        item_at += kItemCost + item.chunks;
+        if (item_at >= end) break;
+        if (++head == a.c.kv_heads) {
+            head = 0;
+            if (++block >= (rows + R - 1) / R) {
+                block = 0;
+                do s = sequence(a, ++seq);
+                while (s.fresh == 0);
             }
-        };
-        for (int i = tid; i < R * D / 4; i += kThreads) {
-            const int row = i / (D / 4), d = i % (D / 4) * 4;
+            item = item_of<R>(a, s, block);
+        }
+    }
+    }
+
+    // ---- pieces become items ----
+    Piece shared_item[2];                        // items that this block shares with others: at most its first and its last
+    int   shared_items = 0;
+    __syncthreads();
+    for (int i = 0; i < 2 * kWarps;) {
+        if (piece[i].chunks == 0) {
+            ++i;
+            continue;
+        }
+        const Piece p = piece[i];
+        int to = i, parts = 0, c_end = p.end;              // the item's pieces: i .. to, those that are
+        for (; to < 2 * kWarps && (piece[to].chunks == 0 || piece[to].at == p.at); ++to)
+            if (piece[to].chunks) ++parts, c_end = piece[to].end;
+        const bool all = p.begin == 0 && c_end == p.chunks;
+        const Seq s = sequence(a, p.seq);
+        const int rows = s.fresh * a.share;
+        float *slot = a.partials + (size_t)(2 * blockIdx.x + (p.begin == 0 ? 1 : 0)) * (R * (D + 2));
+        for (int e = tid; e < R * D / 4; e += kThreads) {
+            const int row = e / (D / 4), d = e % (D / 4) * 4;
             float top = kNothing, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, warp_m[w][row]);
+            for (int x = i; x < to; ++x)
+                if (piece[x].chunks) top = fmaxf(top, result_of(x)[R * kOut + row]);
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float f = power2(warp_m[w][row] - top);
-                const float4 x = *reinterpret_cast<const float4 *>(smem + w * kWarpBytes + (row * kOut + d) * 4);
-                sum = __fmaf_rn(warp_l[w][row], f, sum);
-                v.x = __fmaf_rn(x.x, f, v.x); v.y = __fmaf_rn(x.y, f, v.y);
-                v.z = __fmaf_rn(x.z, f, v.z); v.w = __fmaf_rn(x.w, f, v.w);
+            for (int x = i; x < to; ++x) {
+                if (!piece[x].chunks) continue;
+                const float *r = result_of(x);
+                const float f = power2(r[R * kOut + row] - top);
+                const float4 y = *reinterpret_cast<const float4 *>(r + row * kOut + d);
+                sum = __fmaf_rn(r[R * kOut + R + row], f, sum);
+                v.x = __fmaf_rn(y.x, f, v.x); v.y = __fmaf_rn(y.y, f, v.y);
+                v.z = __fmaf_rn(y.z, f, v.z); v.w = __fmaf_rn(y.w, f, v.w);
             }
             if (all) {
-                store(row, d, v, sum);
+                store4(a, s, rows, p.block * R + row, p.head, d, v, sum);
             } else {
                 *reinterpret_cast<float4 *>(slot + 2 * R + row * D + d) = v;
                 if (d == 0) {
@@ -523,87 +591,80 @@ __global__ void __launch_bounds__(kThreads, NB == 1 && D <= 128 ? 2 : 1) attenti
                 }
             }
         }
+        i = to;
         if (!all) {
-            // ---- an item that several blocks share: the last to come joins their results, in the blocks' order ----
-            const int64_t first = item_at / per, last = (item_at + item.chunks - 1) / per;
+            if (p.begin == 0) shared_item[1] = p, shared_items |= 2;
+            else shared_item[0] = p, shared_items |= 1;
+        }
+    }
+    // ---- an item that several blocks share: the last to come joins their results, in the blocks' order ----
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (!(shared_items >> i & 1)) continue;
+        const Piece &p = shared_item[i];
+        const Seq s = sequence(a, p.seq);
+        const int rows = s.fresh * a.share;
+        const int64_t first = (p.at + kItemCost) / per, last = (p.at + kItemCost + p.chunks - 1) / per;
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            const unsigned before = atomicAdd(&a.counters[first], 1u);
+            is_last = before == (unsigned)(last - first);
+            if (is_last) a.counters[first] = 0;
             __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const unsigned before = atomicAdd(&a.counters[first], 1u);
-                is_last = before == (unsigned)(last - first);
-                if (is_last) a.counters[first] = 0;
-                __threadfence();
+        }
+        __syncthreads();
+        if (is_last) {
+            // weights first, a warp per row, then every thread its part of the output, many loads at a time
+            const int joined = (int)(last - first) + 1;
+            float *weight = reinterpret_cast<float *>(smem);          // [part][R]; the pieces' results are not needed any more
+            auto part = [&](int x) { return a.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * (R * (D + 2)); };
+            for (int row = warp; row < R; row += kWarps) {
+                float top = kNothing, sum = 0.0f;
+                for (int x = lane; x < joined; x += 32) top = fmaxf(top, __ldcg(part(x) + row));
+#pragma unroll
+                for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                for (int x = lane; x < joined; x += 32) {
+                    const float f = power2(__ldcg(part(x) + row) - top);
+                    weight[x * R + row] = f;
+                    sum = __fmaf_rn(__ldcg(part(x) + R + row), f, sum);
+                }
+#pragma unroll
+                for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if (lane == 0) row_sum[row] = sum;
             }
             __syncthreads();
-            if (is_last) {
-                // weights first, a warp per row, then every thread its part of the output, many loads at a time
-                const int parts = (int)(last - first) + 1;
-                float *weight = reinterpret_cast<float *>(smem);          // [part][R]
-                auto part = [&](int x) { return a.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * (R * (D + 2)); };
-                for (int row = warp; row < R; row += kWarps) {
-                    float top = kNothing, sum = 0.0f;
-                    for (int x = lane; x < parts; x += 32) top = fmaxf(top, __ldcg(part(x) + row));
+            for (int e = tid; e < R * D / 4; e += kThreads) {
+                const int row = e / (D / 4), d = e % (D / 4) * 4;
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                for (int x0 = 0; x0 < joined; x0 += 8) {
+                    float4 y[8];
 #pragma unroll
-                    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    for (int x = lane; x < parts; x += 32) {
-                        const float f = power2(__ldcg(part(x) + row) - top);
-                        weight[x * R + row] = f;
-                        sum = __fmaf_rn(__ldcg(part(x) + R + row), f, sum);
-                    }
+                    for (int j = 0; j < 8; ++j)
+                        if (x0 + j < joined) y[j] = __ldcg(reinterpret_cast<const float4 *>(part(x0 + j) + 2 * R + row * D + d));
 #pragma unroll
-                    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    if (lane == 0) warp_l[0][row] = sum;
+                    for (int j = 0; j < 8; ++j)
+                        if (x0 + j < joined) {
+                            const float f = weight[(x0 + j) * R + row];
+                            v.x = __fmaf_rn(y[j].x, f, v.x); v.y = __fmaf_rn(y[j].y, f, v.y);
+                            v.z = __fmaf_rn(y[j].z, f, v.z); v.w = __fmaf_rn(y[j].w, f, v.w);
+                        }
                 }
-                __syncthreads();
-                for (int i = tid; i < R * D / 4; i += kThreads) {
-                    const int row = i / (D / 4), d = i % (D / 4) * 4;
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int x0 = 0; x0 < parts; x0 += 8) {
-                        float4 y[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (x0 + j < parts) y[j] = __ldcg(reinterpret_cast<const float4 *>(part(x0 + j) + 2 * R + row * D + d));
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (x0 + j < parts) {
-                                const float f = weight[(x0 + j) * R + row];
-                                v.x = __fmaf_rn(y[j].x, f, v.x); v.y = __fmaf_rn(y[j].y, f, v.y);
-                                v.z = __fmaf_rn(y[j].z, f, v.z); v.w = __fmaf_rn(y[j].w, f, v.w);
-                            }
-                    }
-                    store(row, d, v, warp_l[0][row]);
-                }
+                store4(a, s, rows, p.block * R + row, p.head, d, v, row_sum[row]);
             }
         }
-        __syncthreads();                                        // the shared memory is free for the next piece
-
-        // ---- next ----
-        flat = item_at + c_end;
-        if (c_end == item.chunks && flat < end) {
-            item_at = flat;
-            if (++head == a.c.kv_heads) {
-                head = 0;
-                if (++block >= (rows + R - 1) / R) {
-                    block = 0;
-                    do s = sequence(a, ++seq);
-                    while (s.fresh == 0);
-                }
-                item = item_of<R>(a, s, block);
-            }
-        }
+        __syncthreads();
     }
 }
 
 template <int D, int NB>
 cudaError_t launch(const AttnArgs &a, int num_sms, cudaStream_t stream)
 {
-    constexpr int R = 8 * NB, kStage = 16 * D + 16 * (D / 64) * 8;
-    constexpr int kWarpBytes = kStages * kStage > R * (D + 4) * 4 ? kStages * kStage : R * (D + 4) * 4;
-    constexpr int kBytes = kWarps * kWarpBytes;
-    cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    using S = Shape<D, NB>;
+    cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
     if (e != cudaSuccess) return e;
-    const int blocks = num_sms * (NB == 1 && D <= 128 ? 2 : 1);
-    attention_kernel<D, NB><<<blocks < kAttnMaxBlocks ? blocks : kAttnMaxBlocks, kThreads, kBytes, stream>>>(a);
+    const int blocks = num_sms * S::kBlocks;
+    attention_kernel<D, NB><<<blocks < kAttnMaxBlocks ? blocks : kAttnMaxBlocks, 32 * S::kWarps, S::kBytes, stream>>>(a);
     return cudaGetLastError();
 }
 
