@@ -100,6 +100,11 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // -(128 + z) of two words' zero points
 __device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1, uint32_t magic) { return nibbles(__byte_perm(w0, w1, 0x5410), magic) ^ 0x80008000u; }
 
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)         // of what is hardly ever above 32 bits
+{
+    return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // ---- the sequences as work ----------------------------------------------------------------
 // An item is `rows` query rows (a token and a head of the key/value head's share, tokens first) of one sequence and one
 // key/value head; its work is the chunks of 16 cached tokens that any of its rows sees, one at least.
@@ -182,7 +187,8 @@ struct Shape {
 // A piece of an item that does not make it whole: chunks [begin, end) of `chunks`.
 struct Piece {
     int64_t at;                  // the item's place in the order of all work
-    int     seq, block, head, begin, end, chunks;
+    int     block, head, begin, end, chunks;
+    Seq     s;
 };
 
 template <int D, int NB>
@@ -223,7 +229,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         if (w == warp) incl += total;
         total += warp_sum[w];
     }
-    const int64_t per_warp = max((total + (int64_t)gridDim.x * kWarps - 1) / ((int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
+    const int64_t per_warp = max(quotient(total + (int64_t)gridDim.x * kWarps - 1, (int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
     const int64_t per = per_warp * kWarps, block_begin = per * blockIdx.x;
     if (block_begin >= total) return;
     for (int w = 0; w < kWarps; ++w) {
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         item_at += (int64_t)(item.chunks + kItemCost) * a.c.kv_heads;
         item = item_of<R>(a, s, ++block);
     }
-    head = (int)((begin - item_at) / (item.chunks + kItemCost));
+    head = (int)quotient(begin - item_at, item.chunks + kItemCost);
     item_at += (int64_t)head * (item.chunks + kItemCost);
 
     for (;;) {
@@ -510,7 +516,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         const bool all = c_begin == 0 && c_end == item.chunks;
         const int which = 2 * warp + (c_begin == 0 ? 1 : 0);
         float *to = result_of(which);
-        if (!all && lane == 0) piece[which] = Piece{item_at, seq, block, head, c_begin, c_end, item.chunks};
+        if (!all && lane == 0) piece[which] = Piece{item_at, block, head, c_begin, c_end, item.chunks, s};
         // fragment i of a group: channels 4 g + i (0, 1) and 32 + 4 g + i (2, 3) of it
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -549,52 +555,70 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     }
     }
 
-    // ---- pieces become items ----
-    Piece shared_item[2];                        // items that this block shares with others: at most its first and its last
-    int   shared_items = 0;
+    // ---- pieces become items: a warp takes a row of an item at a time ----
     __syncthreads();
-    for (int i = 0; i < 2 * kWarps;) {
-        if (piece[i].chunks == 0) {
-            ++i;
-            continue;
-        }
-        const Piece p = piece[i];
-        int to = i, parts = 0, c_end = p.end;              // the item's pieces: i .. to, those that are
-        for (; to < 2 * kWarps && (piece[to].chunks == 0 || piece[to].at == p.at); ++to)
-            if (piece[to].chunks) ++parts, c_end = piece[to].end;
-        const bool all = p.begin == 0 && c_end == p.chunks;
-        const Seq s = sequence(a, p.seq);
-        const int rows = s.fresh * a.share;
+    static_assert(2 * kWarps <= 32, "a lane per piece");
+    const int64_t my_at = lane < 2 * kWarps ? piece[lane].at : 0;
+    const uint32_t there = __ballot_sync(0xffffffffu, lane < 2 * kWarps && piece[lane].chunks > 0);
+    const uint32_t below = there & ((1u << lane) - 1u);
+    const int64_t before_at = __shfl_sync(0xffffffffu, my_at, below ? 31 - __clz(below) : lane);
+    const uint32_t firsts = __ballot_sync(0xffffffffu, (there >> lane & 1u) && (below == 0 || before_at != my_at));
+    const int items = __popc(firsts);
+    uint32_t rest = firsts;
+    for (int j = 0; j < lane && rest; ++j) rest &= rest - 1;
+    const int nth = rest ? __ffs(rest) - 1 : 32;              // lane i: the first piece of the i-th item
+    auto item_pieces = [&](int i, uint32_t &mask) {           // first piece of the i-th item; all of its pieces
+        const int from = __shfl_sync(0xffffffffu, nth, i), to = __shfl_sync(0xffffffffu, nth, i + 1);
+        mask = there & ~((1u << from) - 1u) & (to < 32 ? (1u << to) - 1u : 0xffffffffu);
+        return from;
+    };
+    for (int u = warp; u < items * R; u += kWarps) {
+        const int i = u / R, row = u - i * R;
+        uint32_t mask;
+        const Piece &p = piece[item_pieces(i, mask)];
+        const bool all = p.begin == 0 && piece[31 - __clz(mask)].end == p.chunks;
         float *slot = a.partials + (size_t)(2 * blockIdx.x + (p.begin == 0 ? 1 : 0)) * (R * (D + 2));
-        for (int e = tid; e < R * D / 4; e += kThreads) {
-            const int row = e / (D / 4), d = e % (D / 4) * 4;
-            float top = kNothing, sum = 0.0f;
-            for (int x = i; x < to; ++x)
-                if (piece[x].chunks) top = fmaxf(top, result_of(x)[R * kOut + row]);
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int x = i; x < to; ++x) {
-                if (!piece[x].chunks) continue;
-                const float *r = result_of(x);
-                const float f = power2(r[R * kOut + row] - top);
-                const float4 y = *reinterpret_cast<const float4 *>(r + row * kOut + d);
-                sum = __fmaf_rn(r[R * kOut + R + row], f, sum);
-                v.x = __fmaf_rn(y.x, f, v.x); v.y = __fmaf_rn(y.y, f, v.y);
-                v.z = __fmaf_rn(y.z, f, v.z); v.w = __fmaf_rn(y.w, f, v.w);
-            }
-            if (all) {
-                store4(a, s, rows, p.block * R + row, p.head, d, v, sum);
-            } else {
-                *reinterpret_cast<float4 *>(slot + 2 * R + row * D + d) = v;
-                if (d == 0) {
-                    slot[row]     = top;
-                    slot[R + row] = sum;
+        float top = kNothing, sum = 0.0f;
+        for (uint32_t x = mask; x; x &= x - 1) top = fmaxf(top, result_of(__ffs(x) - 1)[R * kOut + row]);
+        float4 v[(D + 127) / 128];
+#pragma unroll
+        for (int j = 0; j < (D + 127) / 128; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (uint32_t x = mask; x; x &= x - 1) {
+            const float *r = result_of(__ffs(x) - 1);
+            const float f = power2(r[R * kOut + row] - top);
+            sum = __fmaf_rn(r[R * kOut + R + row], f, sum);
+#pragma unroll
+            for (int j = 0; j < (D + 127) / 128; ++j) {
+                if (D >= 128 || lane < D / 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(r + row * kOut + j * 128 + lane * 4);
+                    v[j].x = __fmaf_rn(y.x, f, v[j].x); v[j].y = __fmaf_rn(y.y, f, v[j].y);
+                    v[j].z = __fmaf_rn(y.z, f, v[j].z); v[j].w = __fmaf_rn(y.w, f, v[j].w);
                 }
             }
         }
-        i = to;
-        if (!all) {
-            if (p.begin == 0) shared_item[1] = p, shared_items |= 2;
-            else shared_item[0] = p, shared_items |= 1;
+#pragma unroll
+        for (int j = 0; j < (D + 127) / 128; ++j) {
+            if (D >= 128 || lane < D / 4) {
+                if (all) store4(a, p.s, p.s.fresh * a.share, p.block * R + row, p.head, j * 128 + lane * 4, v[j], sum);
+                else *reinterpret_cast<float4 *>(slot + 2 * R + row * D + j * 128 + lane * 4) = v[j];
+            }
+        }
+        if (!all && lane == 0) {
+            slot[row]     = top;
+            slot[R + row] = sum;
+        }
+    }
+    // items that this block shares with others: at most its first and its last
+    Piece shared_item[2];
+    int   shared_items = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if (e < items) {
+            uint32_t mask;
+            const Piece p = piece[item_pieces(e ? items - 1 : 0, mask)];
+            const bool all = p.begin == 0 && piece[31 - __clz(mask)].end == p.chunks;
+            if (!all && (p.begin == 0) == (e == 1)) shared_item[e] = p, shared_items |= 1 << e;
+            if (!all && e == 0 && items == 1 && p.begin == 0) shared_item[1] = p, shared_items |= 2;
         }
     }
     // ---- an item that several blocks share: the last to come joins their results, in the blocks' order ----
@@ -602,9 +626,9 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     for (int i = 0; i < 2; ++i) {
         if (!(shared_items >> i & 1)) continue;
         const Piece &p = shared_item[i];
-        const Seq s = sequence(a, p.seq);
+        const Seq &s = p.s;
         const int rows = s.fresh * a.share;
-        const int64_t first = (p.at + kItemCost) / per, last = (p.at + kItemCost + p.chunks - 1) / per;
+        const int64_t first = quotient(p.at + kItemCost, per), last = quotient(p.at + kItemCost + p.chunks - 1, per);
         __threadfence();
         __syncthreads();
         if (tid == 0) {
