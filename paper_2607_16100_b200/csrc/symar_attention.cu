@@ -19,6 +19,7 @@ struct AttnArgs {
     float   scale_log2;         // scale * log2(e): softmax in powers of two
     int     q_heads, share, window, q_vec, out_vec;
     uint32_t magic, one;        // bf16 128 and 1, twice each (see nibbles)
+    uint32_t share_mul, share_shift;
     int    *status;
     unsigned *counters;
     float  *partials;
@@ -105,6 +106,9 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)         // of 
     return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
 
+// n / share for 0 <= n < 2^31, by the reciprocal that the host rounded up
+__device__ __forceinline__ int by_share(const AttnArgs &a, int n) { return (int)((uint64_t)(uint32_t)n * a.share_mul >> a.share_shift); }
+
 // ---- the sequences as work ----------------------------------------------------------------
 // An item is `rows` query rows (a token and a head of the key/value head's share, tokens first) of one sequence and one
 // key/value head; its work is the chunks of 16 cached tokens that any of its rows sees, one at least.
@@ -130,7 +134,7 @@ struct Item {
 template <int R>
 __device__ __forceinline__ Item item_of(const AttnArgs &a, const Seq &s, int block)
 {
-    const int first = block * R / a.share, last = min((block * R + R - 1) / a.share, s.fresh - 1);
+    const int first = by_share(a, block * R), last = min(by_share(a, block * R + R - 1), s.fresh - 1);
     const int64_t most = a.b.table_ld << a.c.page_shift;           // tokens that the table has room for
     int hi = s.len - s.fresh + last + 1;
     if (hi > most) hi = (int)most;
@@ -151,7 +155,7 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 __device__ __forceinline__ void store4(const AttnArgs &a, const Seq &s, int rows, int r, int head, int d, float4 v, float sum)
 {
     if (r >= rows) return;
-    const int tok = r / a.share, hh = r - tok * a.share;
+    const int tok = by_share(a, r), hh = r - tok * a.share;
     const float f = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
     __nv_bfloat16 *p = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head + d;
     const uint32_t x = pack_bf16(v.x * f, v.y * f), y = pack_bf16(v.z * f, v.w * f);
@@ -198,8 +202,8 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     constexpr int R = S::R, NG = S::NG, kRow = S::kRow, kUnits = D / 32, kWarps = S::kWarps, kThreads = 32 * kWarps;
     constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = S::kStage, kOut = S::kOut;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int64_t warp_sum[kWarps], at_flat[kWarps];
-    __shared__ int     at_seq[kWarps], is_last;
+    __shared__ int64_t warp_sum[kWarps], before[kThreads];
+    __shared__ int     is_last[2];
     __shared__ Piece   piece[2 * kWarps];        // of each warp: the end of an item that began before, the beginning of one that goes on
     __shared__ float   row_sum[R];
 
@@ -232,29 +236,22 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     const int64_t per_warp = max(quotient(total + (int64_t)gridDim.x * kWarps - 1, (int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
     const int64_t per = per_warp * kWarps, block_begin = per * blockIdx.x;
     if (block_begin >= total) return;
-    for (int w = 0; w < kWarps; ++w) {
-        const int64_t begin = block_begin + w * per_warp;
-        if (begin >= incl - own && begin < incl) {
-            int64_t flat = incl - own;
-            for (int b = s0; b < s1; ++b) {
-                const int64_t n = places_of<R>(a, sequence(a, b));
-                if (begin < flat + n) {
-                    at_seq[w]  = b;
-                    at_flat[w] = flat;
-                    break;
-                }
-                flat += n;
-            }
-        }
-    }
+    before[tid] = incl - own;
     __syncthreads();
     const int64_t begin = block_begin + warp * per_warp, end = min(begin + per_warp, total);
     const int ps = 1 << a.c.page_shift;
 
     if (begin < end) {
-    int seq = at_seq[warp], block = 0, head = 0;
-    int64_t item_at = at_flat[warp];                 // place of the current item
+    // the last thread whose sequences begin no later than this warp's share, then the sequence among them
+    int owner = -1;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) owner += __popc(__ballot_sync(0xffffffffu, before[i * 32 + lane] <= begin));
+    int seq = owner * each, block = 0, head = 0;
+    int64_t item_at = before[owner];                 // place of the current item
     Seq  s    = sequence(a, seq);
+    if (each > 1) {
+        for (int64_t n; item_at + (n = places_of<R>(a, s)) <= begin; item_at += n) s = sequence(a, ++seq);
+    }
     Item item = item_of<R>(a, s, 0);
     while (item_at + (int64_t)(item.chunks + kItemCost) * a.c.kv_heads <= begin) {
         item_at += (int64_t)(item.chunks + kItemCost) * a.c.kv_heads;
@@ -269,64 +266,6 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         const int rows = s.fresh * a.share;
         if (c_begin < c_end) {
         if (lane == 0 && s.len > (a.b.table_ld << a.c.page_shift)) kv_record(a.status, seq, (int)(a.b.table_ld << a.c.page_shift));
-        // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
-        uint32_t qf[NB][NG * 4][2];
-        float qs[NB][NG][2];                    // the sum of a group's channels in this thread's two columns
-        int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int row = block * R + nb * 8 + g;
-            const bool on = row < rows;
-            const int tok = on ? row / a.share : 0, hh = on ? row - tok * a.share : 0;
-            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const __nv_bfloat16 *p = src + gr * 64 + half * 32 + t * 8;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (on && a.q_vec) {
-                        v = *reinterpret_cast<const uint4 *>(p);
-                    } else if (on) {
-                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                                       h[6] | (uint32_t)h[7] << 16);
-                    }
-                    qf[nb][gr * 4 + 0][half] = __byte_perm(v.x, v.z, 0x5410);       // channels i and i + 4 of eight
-                    qf[nb][gr * 4 + 1][half] = __byte_perm(v.x, v.z, 0x7632);
-                    qf[nb][gr * 4 + 2][half] = __byte_perm(v.y, v.w, 0x5410);
-                    qf[nb][gr * 4 + 3][half] = __byte_perm(v.y, v.w, 0x7632);
-                }
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t v = qf[nb][gr * 4 + i / 2][i & 1];
-                    sum += __uint_as_float(v << 16) + __uint_as_float(v & 0xffff0000u);
-                }
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                qs[nb][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
-                qs[nb][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int r = block * R + nb * 8 + 2 * t + j;
-                hi[nb][j] = 0x7fffffff;                                             // a row of padding masks nothing
-                lo[nb][j] = 0;
-                if (r < rows) {
-                    hi[nb][j] = s.len - s.fresh + r / a.share + 1;
-                    lo[nb][j] = a.window > 0 ? max(hi[nb][j] - a.window, 0) : 0;
-                }
-            }
-        }
-        {
-            const int first = block * R / a.share, last = min((block * R + R - 1) / a.share, s.fresh - 1);
-            least_hi = s.len - s.fresh + first + 1;
-            most_lo  = a.window > 0 ? s.len - s.fresh + last + 1 - a.window : 0;
-        }
-
         float o[NB][NG * 4][4], m[NB][2], l[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -376,6 +315,64 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         };
 #pragma unroll
         for (int k = 0; k < kStages - 1; ++k) fetch(k);
+        // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
+        uint32_t qf[NB][NG * 4][2];
+        float qs[NB][NG][2];                    // the sum of a group's channels in this thread's two columns
+        int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int row = block * R + nb * 8 + g;
+            const bool on = row < rows;
+            const int tok = on ? by_share(a, row) : 0, hh = on ? row - tok * a.share : 0;
+            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const __nv_bfloat16 *p = src + gr * 64 + half * 32 + t * 8;
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (on && a.q_vec) {
+                        v = *reinterpret_cast<const uint4 *>(p);
+                    } else if (on) {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+                                       h[6] | (uint32_t)h[7] << 16);
+                    }
+                    qf[nb][gr * 4 + 0][half] = __byte_perm(v.x, v.z, 0x5410);       // channels i and i + 4 of eight
+                    qf[nb][gr * 4 + 1][half] = __byte_perm(v.x, v.z, 0x7632);
+                    qf[nb][gr * 4 + 2][half] = __byte_perm(v.y, v.w, 0x5410);
+                    qf[nb][gr * 4 + 3][half] = __byte_perm(v.y, v.w, 0x7632);
+                }
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t v = qf[nb][gr * 4 + i / 2][i & 1];
+                    sum += __uint_as_float(v << 16) + __uint_as_float(v & 0xffff0000u);
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                qs[nb][gr][0] = __shfl_sync(0xffffffffu, sum, 8 * t);
+                qs[nb][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = block * R + nb * 8 + 2 * t + j;
+                hi[nb][j] = 0x7fffffff;                                             // a row of padding masks nothing
+                lo[nb][j] = 0;
+                if (r < rows) {
+                    hi[nb][j] = s.len - s.fresh + by_share(a, r) + 1;
+                    lo[nb][j] = a.window > 0 ? max(hi[nb][j] - a.window, 0) : 0;
+                }
+            }
+        }
+        {
+            const int first = by_share(a, block * R), last = min(by_share(a, block * R + R - 1), s.fresh - 1);
+            least_hi = s.len - s.fresh + first + 1;
+            most_lo  = a.window > 0 ? s.len - s.fresh + last + 1 - a.window : 0;
+        }
+
         int tok0 = first_tok, at = 0;
         for (int k = 0; k < n; ++k, tok0 += 16, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
             copies_wait<kStages - 2>();
@@ -564,6 +561,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     const int64_t before_at = __shfl_sync(0xffffffffu, my_at, below ? 31 - __clz(below) : lane);
     const uint32_t firsts = __ballot_sync(0xffffffffu, (there >> lane & 1u) && (below == 0 || before_at != my_at));
     const int items = __popc(firsts);
+    if (items == 0) return;
     uint32_t rest = firsts;
     for (int j = 0; j < lane && rest; ++j) rest &= rest - 1;
     const int nth = rest ? __ffs(rest) - 1 : 32;              // lane i: the first piece of the i-th item
@@ -578,15 +576,25 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         const Piece &p = piece[item_pieces(i, mask)];
         const bool all = p.begin == 0 && piece[31 - __clz(mask)].end == p.chunks;
         float *slot = a.partials + (size_t)(2 * blockIdx.x + (p.begin == 0 ? 1 : 0)) * (R * (D + 2));
-        float top = kNothing, sum = 0.0f;
-        for (uint32_t x = mask; x; x &= x - 1) top = fmaxf(top, result_of(__ffs(x) - 1)[R * kOut + row]);
+        const float *r0 = result_of(min(lane, 2 * kWarps - 1));            // lane i: the i-th piece's maximum and sum
+        const float m0 = mask >> lane & 1u ? r0[R * kOut + row] : kNothing;
+        float top = m0;
+#pragma unroll
+        for (int d = 1; d < 2 * kWarps; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        top = __shfl_sync(0xffffffffu, top, 0);
+        const float f0 = mask >> lane & 1u ? power2(m0 - top) : 0.0f;
+        float sum = mask >> lane & 1u ? r0[R * kOut + R + row] * f0 : 0.0f;
+#pragma unroll
+        for (int d = 1; d < 2 * kWarps; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        sum = __shfl_sync(0xffffffffu, sum, 0);
         float4 v[(D + 127) / 128];
 #pragma unroll
         for (int j = 0; j < (D + 127) / 128; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (uint32_t x = mask; x; x &= x - 1) {
-            const float *r = result_of(__ffs(x) - 1);
-            const float f = power2(r[R * kOut + row] - top);
-            sum = __fmaf_rn(r[R * kOut + R + row], f, sum);
+#pragma unroll 4
+        for (int x = 0; x < 2 * kWarps; ++x) {
+            if (!(mask >> x & 1u)) continue;
+            const float *r = result_of(x);
+            const float f = __shfl_sync(0xffffffffu, f0, x);
 #pragma unroll
             for (int j = 0; j < (D + 127) / 128; ++j) {
                 if (D >= 128 || lane < D / 4) {
@@ -608,37 +616,35 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
             slot[R + row] = sum;
         }
     }
-    // items that this block shares with others: at most its first and its last
-    Piece shared_item[2];
-    int   shared_items = 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (e < items) {
-            uint32_t mask;
-            const Piece p = piece[item_pieces(e ? items - 1 : 0, mask)];
-            const bool all = p.begin == 0 && piece[31 - __clz(mask)].end == p.chunks;
-            if (!all && (p.begin == 0) == (e == 1)) shared_item[e] = p, shared_items |= 1 << e;
-            if (!all && e == 0 && items == 1 && p.begin == 0) shared_item[1] = p, shared_items |= 2;
-        }
-    }
-    // ---- an item that several blocks share: the last to come joins their results, in the blocks' order ----
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (!(shared_items >> i & 1)) continue;
-        const Piece &p = shared_item[i];
-        const Seq &s = p.s;
-        const int rows = s.fresh * a.share;
-        const int64_t first = quotient(p.at + kItemCost, per), last = quotient(p.at + kItemCost + p.chunks - 1, per);
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            const unsigned before = atomicAdd(&a.counters[first], 1u);
-            is_last = before == (unsigned)(last - first);
-            if (is_last) a.counters[first] = 0;
+    // ---- items that this block shares with others, at most its first and its last: the last block to come joins their
+    // results, in the blocks' order ----
+    uint32_t mask0, mask1;
+    const int at0 = item_pieces(0, mask0), at1 = item_pieces(items - 1, mask1);
+    const bool goes_on = piece[31 - __clz(mask1)].end < piece[at1].chunks, came = piece[at0].begin > 0;
+    if (!goes_on && !came) return;
+    __syncthreads();
+    if (tid < 2) {
+        // (one thread's fence is enough: the barrier orders what the others wrote before it)
+        is_last[tid] = 0;
+        if (tid == 0 ? came : goes_on && (items > 1 || !came)) {
+            const Piece &p = piece[tid ? at1 : at0];
+            const int64_t first = quotient(p.at + kItemCost, per), last = quotient(p.at + kItemCost + p.chunks - 1, per);
+            __threadfence();
+            const unsigned arrived = atomicAdd(&a.counters[first], 1u);
+            if (arrived == (unsigned)(last - first)) {
+                a.counters[first] = 0;
+                is_last[tid] = 1;
+            }
             __threadfence();
         }
-        __syncthreads();
-        if (is_last) {
+    }
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        if (is_last[i]) {
+            const Piece &p = piece[i ? at1 : at0];
+            const Seq &s = p.s;
+            const int rows = s.fresh * a.share;
+            const int64_t first = quotient(p.at + kItemCost, per), last = quotient(p.at + kItemCost + p.chunks - 1, per);
             // weights first, a warp per row, then every thread its part of the output, many loads at a time
             const int joined = (int)(last - first) + 1;
             float *weight = reinterpret_cast<float *>(smem);          // [part][R]; the pieces' results are not needed any more
@@ -676,8 +682,8 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
                 }
                 store4(a, s, rows, p.block * R + row, p.head, d, v, row_sum[row]);
             }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -724,6 +730,10 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     a.q_vec      = (uintptr_t)args->q % 16 == 0 && args->q_ld % 8 == 0 && args->q_head % 8 == 0;
     a.out_vec    = (uintptr_t)args->out % 8 == 0 && args->out_ld % 4 == 0 && args->out_head % 4 == 0;
     a.magic      = 0x43004300u;
+    int bits = 0;
+    while ((1 << bits) < a.share) ++bits;
+    a.share_shift = 31 + bits;
+    a.share_mul   = (uint32_t)((((uint64_t)1 << a.share_shift) + a.share - 1) / a.share);
     a.one        = 0x3f803f80u;
     a.counters   = kv->counters;
     a.partials   = kv->partials;
