@@ -7,7 +7,7 @@ namespace symar {
 namespace {
 
 constexpr int kStages   = 4;           // copies in flight per warp: three chunks ahead of the one in use
-constexpr int kMinChunks = 4;          // a warp's share of the work is at least this many chunks of 16 tokens
+constexpr int kMinChunks = 1;          // a warp's share of the work is at least this many chunks of 16 tokens
 constexpr int kItemCost  = 3;          // what an item costs a warp besides its chunks, in chunks
 
 struct AttnArgs {
@@ -101,7 +101,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
 // -(128 + z) of two words' zero points
 __device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1, uint32_t magic) { return nibbles(__byte_perm(w0, w1, 0x5410), magic) ^ 0x80008000u; }
 
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)         // of what is hardly ever above 32 bits
+__device__ __noinline__ int64_t quotient(int64_t a, int64_t b)         // of what is hardly ever above 32 bits
 {
     return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
 }
@@ -147,6 +147,7 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 {
     const int blocks = (s.fresh * a.share + R - 1) / R;
     int64_t n = 0;
+#pragma unroll 1
     for (int i = 0; i < blocks; ++i) n += item_of<R>(a, s, i).chunks + kItemCost;
     return n * a.c.kv_heads;
 }
@@ -180,8 +181,9 @@ constexpr float kNothing = -3.402823466e38f;
 template <int D, int NB>
 struct Shape {
     static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;
-    static constexpr int kWarps  = D == 256 && NB == 2 ? 4 : 8;
-    static constexpr int kBlocks = NB == 1 && D <= 128 ? 2 : 1;          // per multiprocessor
+    // one block per multiprocessor, of as many warps as its registers let it have: blocks that share one have an older and a
+    // younger, which starves while the older runs (measured: 34 and 47 us for equal shares)
+    static constexpr int kWarps = NB == 1 && D <= 128 ? 16 : (D == 256 && NB == 2 ? 4 : 8);
     static constexpr int kOut    = D + 4;                                // floats from row to row of a partial result: rows start in different banks
     static constexpr int kPart   = (R * kOut + 2 * R) * 4;               // output, maxima, sums
     static constexpr int kStage  = 2 * 16 * (kRow + NG * 4);
@@ -196,11 +198,11 @@ struct Piece {
 };
 
 template <int D, int NB>
-__global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBlocks) attention_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel(const AttnArgs a)
 {
     using S = Shape<D, NB>;
     constexpr int R = S::R, NG = S::NG, kRow = S::kRow, kUnits = D / 32, kWarps = S::kWarps, kThreads = 32 * kWarps;
-    constexpr int kCodes = 16 * kRow, kWords = 16 * NG * 4, kStage = S::kStage, kOut = S::kOut;
+    constexpr int kCodes = 16 * kRow, kStage = S::kStage, kOut = S::kOut;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int64_t warp_sum[kWarps], before[kThreads];
     __shared__ int     is_last[2];
@@ -217,6 +219,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
     int64_t own = 0;
+#pragma unroll 1
     for (int b = s0; b < s1; ++b) own += places_of<R>(a, sequence(a, b));
     int64_t incl = own;
 #pragma unroll
@@ -234,11 +237,13 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         total += warp_sum[w];
     }
     const int64_t per_warp = max(quotient(total + (int64_t)gridDim.x * kWarps - 1, (int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
-    const int64_t per = per_warp * kWarps, block_begin = per * blockIdx.x;
+    // (little work goes to many multiprocessors, four warps each at least, rather than to all warps of a few)
+    const int used = (int)min((int64_t)kWarps, max(quotient(total + per_warp * gridDim.x - 1, per_warp * gridDim.x), (int64_t)4));
+    const int64_t per = per_warp * used, block_begin = per * blockIdx.x;
     if (block_begin >= total) return;
     before[tid] = incl - own;
     __syncthreads();
-    const int64_t begin = block_begin + warp * per_warp, end = min(begin + per_warp, total);
+    const int64_t begin = block_begin + warp * per_warp, end = warp < used ? min(begin + per_warp, total) : begin;
     const int ps = 1 << a.c.page_shift;
 
     if (begin < end) {
@@ -250,9 +255,11 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     int64_t item_at = before[owner];                 // place of the current item
     Seq  s    = sequence(a, seq);
     if (each > 1) {
+#pragma unroll 1
         for (int64_t n; item_at + (n = places_of<R>(a, s)) <= begin; item_at += n) s = sequence(a, ++seq);
     }
     Item item = item_of<R>(a, s, 0);
+#pragma unroll 1
     while (item_at + (int64_t)(item.chunks + kItemCost) * a.c.kv_heads <= begin) {
         item_at += (int64_t)(item.chunks + kItemCost) * a.c.kv_heads;
         item = item_of<R>(a, s, ++block);
@@ -287,6 +294,22 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         const int word_side = lane / (4 * NG);                // lanes below 8 NG copy words: 4 NG pieces of each side
         const int word_src = 2 * side_bytes + word_side * (ps * NG * 4 - 4 * NG * 16);
         int f_tok = first_tok, f_at = 0;                      // next fetch: its first token, its stage's offset
+        uint4 q_in[R * D / 256];                              // the queries: asked for before the pages are waited for
+#pragma unroll
+        for (int i = 0; i < R * D / 256; ++i) {
+            const int row = block * R + (i * 32 + lane) / (D / 8), d = (i * 32 + lane) % (D / 8) * 8;
+            q_in[i] = make_uint4(0, 0, 0, 0);
+            if (row < rows) {
+                const int tok = by_share(a, row), hh = row - tok * a.share;
+                const __nv_bfloat16 *p = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head + d;
+                if (a.q_vec) {
+                    q_in[i] = *reinterpret_cast<const uint4 *>(p);
+                } else {
+                    const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+                    q_in[i] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                }
+            }
+        }
         auto fetch = [&](int k) {
             if (k < n) {
                 if ((k & 31) == 0) {
@@ -313,31 +336,26 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
             }
             copies_commit();
         };
-#pragma unroll
-        for (int k = 0; k < kStages - 1; ++k) fetch(k);
-        // ---- query rows: fragments of Q^T, and what each of this thread's two columns sees ----
+#pragma unroll 1
+        for (int k = 0; k < kStages - NB; ++k) fetch(k);
+        // ---- query rows, by way of the ring's stages that are still free: fragments of Q^T, and what each of this thread's two
+        // columns sees ----
+        static_assert(NB * kStage >= R * D * 2, "the queries fit the last NB stages");
         uint32_t qf[NB][NG * 4][2];
         float qs[NB][NG][2];                    // the sum of a group's channels in this thread's two columns
-        int hi[NB][2], lo[NB][2], least_hi = 0x7fffffff, most_lo = 0;
+        int hi[NB][2], lo[NB][2];
+        uint4 *q_at = reinterpret_cast<uint4 *>(mine + (kStages - NB) * kStage);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < R * D / 256; ++i) q_at[i * 32 + lane] = q_in[i];
+        __syncwarp();
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const int row = block * R + nb * 8 + g;
-            const bool on = row < rows;
-            const int tok = on ? by_share(a, row) : 0, hh = on ? row - tok * a.share : 0;
-            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const __nv_bfloat16 *p = src + gr * 64 + half * 32 + t * 8;
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (on && a.q_vec) {
-                        v = *reinterpret_cast<const uint4 *>(p);
-                    } else if (on) {
-                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-                        v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
-                                       h[6] | (uint32_t)h[7] << 16);
-                    }
+                    const uint4 v = q_at[(nb * 8 + g) * (D / 8) + gr * 8 + half * 4 + t];
                     qf[nb][gr * 4 + 0][half] = __byte_perm(v.x, v.z, 0x5410);       // channels i and i + 4 of eight
                     qf[nb][gr * 4 + 1][half] = __byte_perm(v.x, v.z, 0x7632);
                     qf[nb][gr * 4 + 2][half] = __byte_perm(v.y, v.w, 0x5410);
@@ -367,13 +385,13 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
                 }
             }
         }
-        {
-            const int first = by_share(a, block * R), last = min(by_share(a, block * R + R - 1), s.fresh - 1);
-            least_hi = s.len - s.fresh + first + 1;
-            most_lo  = a.window > 0 ? s.len - s.fresh + last + 1 - a.window : 0;
-        }
-
+        const int least_hi = s.len - s.fresh + by_share(a, block * R) + 1;
+        const int most_lo  = a.window > 0 ? s.len - s.fresh + min(by_share(a, block * R + R - 1), s.fresh - 1) + 1 - a.window : 0;
+        __syncwarp();                           // (q has been read: the stages are free)
+#pragma unroll
+        for (int k = kStages - NB; k < kStages - 1; ++k) fetch(k);
         int tok0 = first_tok, at = 0;
+#pragma unroll 1
         for (int k = 0; k < n; ++k, tok0 += 16, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
             copies_wait<kStages - 2>();
             __syncwarp();
@@ -520,22 +538,27 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int row = nb * 8 + 2 * t + j;
-                if (!all && g == 0) {
+                if (g == 0) {
                     to[R * kOut + row]     = m[nb][j];
                     to[R * kOut + R + row] = l[nb][j];
                 }
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const float4 v = make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half],
-                                                     o[nb][gr * 4 + 2][j + 2 * half], o[nb][gr * 4 + 3][j + 2 * half]);
-                        const int d = gr * 64 + half * 32 + 4 * g;
-                        if (all) store4(a, s, rows, block * R + row, head, d, v, l[nb][j]);
-                        else *reinterpret_cast<float4 *>(to + row * kOut + d) = v;
-                    }
+                    for (int half = 0; half < 2; ++half)
+                        *reinterpret_cast<float4 *>(to + row * kOut + gr * 64 + half * 32 + 4 * g) =
+                            make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half], o[nb][gr * 4 + 2][j + 2 * half],
+                                        o[nb][gr * 4 + 3][j + 2 * half]);
             }
         __syncwarp();
+        if (all) {
+#pragma unroll 1
+            for (int e = lane; e < R * D / 4; e += 32) {
+                const int row = e / (D / 4), d = e % (D / 4) * 4;
+                store4(a, s, rows, block * R + row, head, d, *reinterpret_cast<const float4 *>(to + row * kOut + d), to[R * kOut + R + row]);
+            }
+            __syncwarp();
+        }
         }
         // ---- next ----
         item_at += kItemCost + item.chunks;
@@ -544,6 +567,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
             head = 0;
             if (++block >= (rows + R - 1) / R) {
                 block = 0;
+#pragma unroll 1
                 do s = sequence(a, ++seq);
                 while (s.fresh == 0);
             }
@@ -563,6 +587,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
     const int items = __popc(firsts);
     if (items == 0) return;
     uint32_t rest = firsts;
+#pragma unroll 1
     for (int j = 0; j < lane && rest; ++j) rest &= rest - 1;
     const int nth = rest ? __ffs(rest) - 1 : 32;              // lane i: the first piece of the i-th item
     auto item_pieces = [&](int i, uint32_t &mask) {           // first piece of the i-th item; all of its pieces
@@ -570,6 +595,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         mask = there & ~((1u << from) - 1u) & (to < 32 ? (1u << to) - 1u : 0xffffffffu);
         return from;
     };
+#pragma unroll 1
     for (int u = warp; u < items * R; u += kWarps) {
         const int i = u / R, row = u - i * R;
         uint32_t mask;
@@ -590,19 +616,28 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         float4 v[(D + 127) / 128];
 #pragma unroll
         for (int j = 0; j < (D + 127) / 128; ++j) v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int x = 0; x < 2 * kWarps; ++x) {
-            if (!(mask >> x & 1u)) continue;
-            const float *r = result_of(x);
-            const float f = __shfl_sync(0xffffffffu, f0, x);
+#pragma unroll 1
+        for (uint32_t x = mask; x;) {                                     // four pieces at a time
+            float f[4];
+            float4 y[4][(D + 127) / 128];
 #pragma unroll
-            for (int j = 0; j < (D + 127) / 128; ++j) {
-                if (D >= 128 || lane < D / 4) {
-                    const float4 y = *reinterpret_cast<const float4 *>(r + row * kOut + j * 128 + lane * 4);
-                    v[j].x = __fmaf_rn(y.x, f, v[j].x); v[j].y = __fmaf_rn(y.y, f, v[j].y);
-                    v[j].z = __fmaf_rn(y.z, f, v[j].z); v[j].w = __fmaf_rn(y.w, f, v[j].w);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const int at = x ? __ffs(x) - 1 : 0;
+                const float w = __shfl_sync(0xffffffffu, f0, at);
+                f[i] = x ? w : 0.0f;
+#pragma unroll
+                for (int j = 0; j < (D + 127) / 128; ++j)
+                    if (x && (D >= 128 || lane < D / 4)) y[i][j] = *reinterpret_cast<const float4 *>(result_of(at) + row * kOut + j * 128 + lane * 4);
+                    else y[i][j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                x &= x - 1;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < (D + 127) / 128; ++j) {
+                    v[j].x = __fmaf_rn(y[i][j].x, f[i], v[j].x); v[j].y = __fmaf_rn(y[i][j].y, f[i], v[j].y);
+                    v[j].z = __fmaf_rn(y[i][j].z, f[i], v[j].z); v[j].w = __fmaf_rn(y[i][j].w, f[i], v[j].w);
+                }
         }
 #pragma unroll
         for (int j = 0; j < (D + 127) / 128; ++j) {
@@ -639,6 +674,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
         }
     }
     __syncthreads();
+#pragma unroll 1
     for (int i = 0; i < 2; ++i) {
         if (is_last[i]) {
             const Piece &p = piece[i ? at1 : at0];
@@ -649,11 +685,14 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
             const int joined = (int)(last - first) + 1;
             float *weight = reinterpret_cast<float *>(smem);          // [part][R]; the pieces' results are not needed any more
             auto part = [&](int x) { return a.partials + (size_t)(2 * (first + x) + (x == 0 ? 1 : 0)) * (R * (D + 2)); };
+#pragma unroll 1
             for (int row = warp; row < R; row += kWarps) {
                 float top = kNothing, sum = 0.0f;
+#pragma unroll 1
                 for (int x = lane; x < joined; x += 32) top = fmaxf(top, __ldcg(part(x) + row));
 #pragma unroll
                 for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+#pragma unroll 1
                 for (int x = lane; x < joined; x += 32) {
                     const float f = power2(__ldcg(part(x) + row) - top);
                     weight[x * R + row] = f;
@@ -664,9 +703,11 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, Shape<D, NB>::kBloc
                 if (lane == 0) row_sum[row] = sum;
             }
             __syncthreads();
+#pragma unroll 1
             for (int e = tid; e < R * D / 4; e += kThreads) {
                 const int row = e / (D / 4), d = e % (D / 4) * 4;
                 float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
                 for (int x0 = 0; x0 < joined; x0 += 8) {
                     float4 y[8];
 #pragma unroll
@@ -693,8 +734,7 @@ cudaError_t launch(const AttnArgs &a, int num_sms, cudaStream_t stream)
     using S = Shape<D, NB>;
     cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
     if (e != cudaSuccess) return e;
-    const int blocks = num_sms * S::kBlocks;
-    attention_kernel<D, NB><<<blocks < kAttnMaxBlocks ? blocks : kAttnMaxBlocks, 32 * S::kWarps, S::kBytes, stream>>>(a);
+    attention_kernel<D, NB><<<num_sms < kAttnMaxBlocks ? num_sms : kAttnMaxBlocks, 32 * S::kWarps, S::kBytes, stream>>>(a);
     return cudaGetLastError();
 }
 

@@ -21,7 +21,7 @@ struct symar_kv {
 namespace symar {
 
 // ---- sizes of the attention grid that the context has room for ----
-constexpr int kAttnMaxBlocks = 512;      // blocks of the largest attention grid
+constexpr int kAttnMaxBlocks = 256;      // blocks of the largest attention grid
 constexpr int kAttnMaxRows   = 16;        // query rows of a block
 constexpr int kAttnMaxDim    = 256;
 
@@ -49,7 +49,7 @@ __device__ __forceinline__ float kv_scale(uint32_t w) { return __uint_as_float(w
 __device__ __forceinline__ int kv_zero(uint32_t w) { return (int)(w & 15u); }
 
 // First offence of a call is kept: code last, so that a reader that sees it sees where.
-__device__ __forceinline__ void kv_record(int *status, int seq, int position)
+static __device__ __noinline__ void kv_record(int *status, int seq, int position)
 {
     if (atomicCAS(status + 3, 0, 1) == 0) {
         status[1] = seq;
