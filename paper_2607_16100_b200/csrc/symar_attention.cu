@@ -17,8 +17,8 @@ struct AttnArgs {
     __nv_bfloat16 *out;
     int64_t q_ld, q_head, out_ld, out_head;
     float   scale_log2;         // scale * log2(e): softmax in powers of two
+    float   scale_code;         // the same times 2^69: what a product with codes lacks
     int     q_heads, share, window, q_vec, out_vec;
-    uint32_t magic, one;        // bf16 128 and 1, twice each (see nibbles)
     uint32_t share_mul, share_shift;
     int    *status;
     unsigned *counters;
@@ -67,21 +67,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t *>(&h);
 }
-// Nibbles 0 and 4 of w as bf16: a nibble n under the exponent of 128 is 128 + n.  `magic` is that exponent twice, in a register that
-// the compiler does not know to be a constant: with two constants it takes two instructions for what is one.
-__device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t magic)
-{
-    uint32_t v;
-    asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(v) : "r"(w), "r"(magic));       // (w & mask) | magic
-    return v;
-}
-// n - z, exact: `less` holds -(128 + z) twice
-__device__ __forceinline__ uint32_t minus(uint32_t v, uint32_t less, uint32_t one)
+// A code n in bits 0-3 or 4-7 of a bf16 whose other bits are 0 is the number n 2^-133 or n 2^-129: the smallest numbers are evenly
+// spaced.  So one AND makes two of them of a word (channels i and i + 4 of eight, 4 bits apart in i), and both the matrix instruction and
+// fused multiply-add take them exactly (tested for every n and z).  The keys go into the product like that, against queries times
+// 2^64 (2^60 for the second kind); the values are brought to (n - z) / 64 and (n - z) / 4 first, whose factors the result loses at the end.
+__device__ __forceinline__ uint32_t codes(uint32_t w, int i) { return (i & 2 ? w >> 8 : w) & (i & 1 ? 0x00f000f0u : 0x000f000fu); }
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c)
 {
     uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(one), "r"(less));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+constexpr uint32_t kTwo127 = 0x7f007f00u, kMinusTwo127 = 0xff00ff00u, kTwo64 = 0x5f805f80u, kTwo60 = 0x5d805d80u, kSixteen = 0x41804180u;
 // a token's words
 template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t *p)
 {
@@ -98,8 +101,8 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
         }
     }
 }
-// -(128 + z) of two words' zero points
-__device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1, uint32_t magic) { return nibbles(__byte_perm(w0, w1, 0x5410), magic) ^ 0x80008000u; }
+// -z / 64 of two words' zero points
+__device__ __forceinline__ uint32_t zeros_of(uint32_t w0, uint32_t w1) { return mul2(__byte_perm(w0, w1, 0x5410) & 0x000f000fu, kMinusTwo127); }
 
 __device__ __noinline__ int64_t quotient(int64_t a, int64_t b)         // of what is hardly ever above 32 bits
 {
@@ -213,7 +216,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     // this warp's ring; its unfinished first piece has a place of its own, its unfinished last piece that of the ring
     unsigned char *mine = smem + warp * S::kRing;
     auto result_of = [&](int i) { return reinterpret_cast<float *>(i & 1 ? smem + (i >> 1) * S::kRing : smem + kWarps * S::kRing + (i >> 1) * S::kPart); };
-    const uint32_t mine_addr = smem_addr(mine), magic = a.magic, one = a.one;
+    const uint32_t mine_addr = smem_addr(mine);
 
     // ---- shares: places [begin, end) of all items in order, kItemCost places and one per chunk each ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
@@ -287,7 +290,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
         // ---- the chunks ----
         const int n = c_end - c_begin;
         int pages = -1;                                       // lane i: the page of chunk (k & ~31) + i
-        uint32_t seen = 0;                                    // bit i: the chunk fetched i fetches ago has a page
+        bool torn = false;                                    // a chunk without a page was met: every chunk is looked at again
         const int first_tok = item.lo + c_begin * 16;
         const unsigned char *head_base = a.c.pages + head * a.c.head_bytes + lane * 16;
         const int side_bytes = ps * kRow;
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                     copy16(to + kCodes, src + side_bytes + u0 * 16, on);
                 }
                 if (lane < 8 * NG) copy16(dst + 2 * kCodes + lane * 16, base + word_src + slot * (NG * 4), on);
-                seen = seen << 1 | (uint32_t)on;
+                torn |= !on;
                 f_tok += 16;
                 f_at = f_at == (kStages - 1) * kStage ? 0 : f_at + kStage;
             }
@@ -375,6 +378,10 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                 qs[nb][gr][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
             }
 #pragma unroll
+            for (int i = 0; i < NG * 4; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) qf[nb][i][half] = mul2(qf[nb][i][half], i & 1 ? kTwo60 : kTwo64);
+#pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = block * R + nb * 8 + 2 * t + j;
                 hi[nb][j] = 0x7fffffff;                                             // a row of padding masks nothing
@@ -395,9 +402,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
         for (int k = 0; k < n; ++k, tok0 += 16, at = at == (kStages - 1) * kStage ? 0 : at + kStage) {
             copies_wait<kStages - 2>();
             __syncwarp();
-            const int ahead = min(kStages - 1, n - 1 - k);            // chunks fetched after this one
             fetch(k + kStages - 1);
-            const bool paged = seen >> ahead & 1;
             const uint32_t base = mine_addr + at;
             const unsigned char *stage = mine + at;
             // lane i names row i % 8 of matrix i / 8: tokens 0-7 and 8-15, first and second 32 channels of the group
@@ -405,7 +410,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
             const int turn = D == 64 ? mt >> 2 & 1 : (D == 128 ? mt >> 1 & 3 : mt & 7);
             const uint32_t *kw = reinterpret_cast<const uint32_t *>(stage + 2 * kCodes), *vw = kw + 16 * NG;
 
-            // score = s (acc - (128 + z) sum of q): the zero points are taken off the sums, not off every code
+            // score = s (sum of q n - z sum of q): the zero points are taken off the sums, not off every code
             float sc[NB][4];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -425,14 +430,13 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                     for (int j = 0; j < 4; ++j) acc[nb][j] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = nibbles(r[0] >> 4 * i, magic), a1 = nibbles(r[2] >> 4 * i, magic);
-                    const uint32_t a2 = nibbles(r[1] >> 4 * i, magic), a3 = nibbles(r[3] >> 4 * i, magic);
+                    const uint32_t a0 = codes(r[0], i), a1 = codes(r[2], i), a2 = codes(r[1], i), a3 = codes(r[3], i);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma(acc[nb], a0, a1, a2, a3, qf[nb][gr * 4 + i][0], qf[nb][gr * 4 + i][1]);
                 }
-                const float f0 = kv_scale(w0[gr]) * a.scale_log2, f1 = kv_scale(w1[gr]) * a.scale_log2;
-                const float h0 = -f0 * __uint_as_float((w0[gr] & 15u) * 65536u + 0x43000000u);      // 128 + z
-                const float h1 = -f1 * __uint_as_float((w1[gr] & 15u) * 65536u + 0x43000000u);
+                // (a word as a number is the scale but for the zero point's bits, less than 2^-19 of it)
+                const float s0 = __uint_as_float(w0[gr]), s1 = __uint_as_float(w1[gr]), f0 = s0 * a.scale_code, f1 = s1 * a.scale_code;
+                const float h0 = -(s0 * a.scale_log2) * (float)(w0[gr] & 15u), h1 = -(s1 * a.scale_log2) * (float)(w1[gr] & 15u);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     sc[nb][0] = __fmaf_rn(qs[nb][gr][0], h0, __fmaf_rn(acc[nb][0], f0, sc[nb][0]));
@@ -442,8 +446,9 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                 }
             }
             // rows of the fragment: tokens tok0 + g (0, 1) and tok0 + g + 8 (2, 3); columns 2t and 2t + 1
-            const bool whole = tok0 + 16 <= least_hi && tok0 >= most_lo && paged;
+            const bool whole = tok0 + 16 <= least_hi && tok0 >= most_lo && !torn;
             if (!whole) {
+                const bool paged = !torn || (tok0 < s.len && kv_page_of(a.c, a.b, a.status, seq, tok0) >= 0);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -501,17 +506,18 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
             for (int gr = 0; gr < NG; ++gr) {
                 uint32_t r[4], pf[NB][2];
                 matrices_t(r, base + kCodes + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
-                const float f0 = kv_scale(w0[gr]), f1 = kv_scale(w1[gr]);
+                const float f0 = __uint_as_float(w0[gr]), f1 = __uint_as_float(w1[gr]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     pf[nb][0] = transposed(pack_bf16(sc[nb][0] * f0, sc[nb][1] * f0));
                     pf[nb][1] = transposed(pack_bf16(sc[nb][2] * f1, sc[nb][3] * f1));
                 }
-                const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr], magic), z1 = zeros_of(z2[2][gr], z2[3][gr], magic);
+                const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr]), z1 = zeros_of(z2[2][gr], z2[3][gr]);
+                const uint32_t y0 = mul2(z0, kSixteen), y1 = mul2(z1, kSixteen);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = minus(nibbles(r[0] >> 4 * i, magic), z0, one), a1 = minus(nibbles(r[1] >> 4 * i, magic), z0, one);
-                    const uint32_t a2 = minus(nibbles(r[2] >> 4 * i, magic), z1, one), a3 = minus(nibbles(r[3] >> 4 * i, magic), z1, one);
+                    const uint32_t a0 = fma2(codes(r[0], i), kTwo127, i & 1 ? y0 : z0), a1 = fma2(codes(r[1], i), kTwo127, i & 1 ? y0 : z0);
+                    const uint32_t a2 = fma2(codes(r[2], i), kTwo127, i & 1 ? y1 : z1), a3 = fma2(codes(r[3], i), kTwo127, i & 1 ? y1 : z1);
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
                 }
@@ -547,8 +553,8 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
                         *reinterpret_cast<float4 *>(to + row * kOut + gr * 64 + half * 32 + 4 * g) =
-                            make_float4(o[nb][gr * 4 + 0][j + 2 * half], o[nb][gr * 4 + 1][j + 2 * half], o[nb][gr * 4 + 2][j + 2 * half],
-                                        o[nb][gr * 4 + 3][j + 2 * half]);
+                            make_float4(64.0f * o[nb][gr * 4 + 0][j + 2 * half], 4.0f * o[nb][gr * 4 + 1][j + 2 * half],
+                                        64.0f * o[nb][gr * 4 + 2][j + 2 * half], 4.0f * o[nb][gr * 4 + 3][j + 2 * half]);
             }
         __syncwarp();
         if (all) {
@@ -763,18 +769,17 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     a.out_head   = args->out_head;
     const double scale = args->scale == 0.0f ? 1.0 / std::sqrt((double)cache->head_dim) : (double)args->scale;
     a.scale_log2 = (float)(scale * 1.4426950408889634);
+    a.scale_code = std::ldexp(a.scale_log2, 69);
     a.q_heads    = args->q_heads;
     a.window     = args->window;
     a.status     = kv->status;
     a.share      = args->q_heads / cache->kv_heads;
     a.q_vec      = (uintptr_t)args->q % 16 == 0 && args->q_ld % 8 == 0 && args->q_head % 8 == 0;
     a.out_vec    = (uintptr_t)args->out % 8 == 0 && args->out_ld % 4 == 0 && args->out_head % 4 == 0;
-    a.magic      = 0x43004300u;
     int bits = 0;
     while ((1 << bits) < a.share) ++bits;
     a.share_shift = 31 + bits;
     a.share_mul   = (uint32_t)((((uint64_t)1 << a.share_shift) + a.share - 1) / a.share);
-    a.one        = 0x3f803f80u;
     a.counters   = kv->counters;
     a.partials   = kv->partials;
     if ((int64_t)a.b.tokens * a.share > 0x7fff0000) return SYMAR_ERR_UNSUPPORTED;
