@@ -735,10 +735,11 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
 }
 
 template <int D, int NB>
-cudaError_t launch(const AttnArgs &a, int num_sms, cudaStream_t stream)
+cudaError_t launch(const AttnArgs &a, int num_sms, int device, cudaStream_t stream)
 {
     using S = Shape<D, NB>;
-    cudaError_t e = cudaFuncSetAttribute(attention_kernel<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared((const void *)attention_kernel<D, NB>, S::kBytes, device, allowed);
     if (e != cudaSuccess) return e;
     attention_kernel<D, NB><<<num_sms < kAttnMaxBlocks ? num_sms : kAttnMaxBlocks, 32 * S::kWarps, S::kBytes, stream>>>(a);
     return cudaGetLastError();
@@ -787,8 +788,8 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     const bool wide = (int64_t)a.b.tokens * a.share > 8ll * a.b.seqs;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (a.c.dim == 64) e = wide ? launch<64, 2>(a, kv->num_sms, st) : launch<64, 1>(a, kv->num_sms, st);
-    else if (a.c.dim == 128) e = wide ? launch<128, 2>(a, kv->num_sms, st) : launch<128, 1>(a, kv->num_sms, st);
-    else e = wide ? launch<256, 2>(a, kv->num_sms, st) : launch<256, 1>(a, kv->num_sms, st);
+    if (a.c.dim == 64) e = wide ? launch<64, 2>(a, kv->num_sms, kv->device, st) : launch<64, 1>(a, kv->num_sms, kv->device, st);
+    else if (a.c.dim == 128) e = wide ? launch<128, 2>(a, kv->num_sms, kv->device, st) : launch<128, 1>(a, kv->num_sms, kv->device, st);
+    else e = wide ? launch<256, 2>(a, kv->num_sms, kv->device, st) : launch<256, 1>(a, kv->num_sms, kv->device, st);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_attention");
 }

@@ -655,7 +655,7 @@ bool encode(CUtensorMap *map, const void *p, int64_t ld, int64_t group, int rows
 }
 
 struct Device {
-    int sms = 0;
+    int sms = 0, id = -1;
 };
 int device_info(Device *d)
 {
@@ -667,14 +667,15 @@ int device_info(Device *d)
         *d = known[dev];
         return SYMAR_OK;
     }
-    e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev);
+    d->id = dev;
+    e     = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
     if (dev >= 0 && dev < 64) known[dev] = *d;
     return SYMAR_OK;
 }
 
 template <int NT, bool kWide, bool kTma>
-int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int groups, int sms, cudaStream_t stream)
+int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int groups, const Device &d, cudaStream_t stream)
 {
     using S = Shape<NT, kWide, kTma>;
     auto fn = linear_kernel<NT, kWide, kTma>;
@@ -685,12 +686,13 @@ int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int g
     a.tiles = (int)tiles;
     const int slices = (a.k + kSlice - 1) / kSlice;
     a.split = 1;
-    while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && slices >= a.split * 4 && NT * kRows * 4 <= S::kStages * S::kStage) a.split *= 2;
-    cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    while (a.split < kMaxSplit && tiles * a.split * 2 <= d.sms && slices >= a.split * 4 && NT * kRows * 4 <= S::kStages * S::kStage) a.split *= 2;
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_shared((const void *)fn, S::kBytes, d.id, allowed);
     if (e != cudaSuccess) return cuda_fail(e, "symar_linear");
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr[1];
-    cfg.gridDim  = dim3((unsigned)(a.split > 1 ? tiles * a.split : (tiles < sms ? tiles : sms)));
+    cfg.gridDim  = dim3((unsigned)(a.split > 1 ? tiles * a.split : (tiles < d.sms ? tiles : d.sms)));
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kBytes;
     cfg.stream   = stream;
@@ -706,15 +708,15 @@ int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int g
 }
 
 template <int NT>
-int launch_as(const LinearArgs &a, int groups, int sms, bool wide, bool engine, cudaStream_t s)
+int launch_as(const LinearArgs &a, int groups, const Device &d, bool wide, bool engine, cudaStream_t s)
 {
     constexpr bool kBoth = NT <= 128;              // float32 results: the sums of a wider tile do not fit a thread's registers
     constexpr int  kByHand = NT > 128 ? 128 : NT;    // nor do the pieces of its rows where the block's threads load them
     CUtensorMap wmap{}, xmap{};
     engine = engine && encoder() && encode(&wmap, a.w, a.w_ld, a.w_group, a.n, groups, a.k, kRows) &&
              encode(&xmap, a.x, a.x_ld, a.x_group, a.m, groups, a.k, NT);
-    if (wide && kBoth) return engine ? launch<NT, kBoth, true>(a, wmap, xmap, groups, sms, s) : launch<kByHand, kBoth, false>(a, wmap, xmap, groups, sms, s);
-    return engine ? launch<NT, false, true>(a, wmap, xmap, groups, sms, s) : launch<kByHand, false, false>(a, wmap, xmap, groups, sms, s);
+    if (wide && kBoth) return engine ? launch<NT, kBoth, true>(a, wmap, xmap, groups, d, s) : launch<kByHand, kBoth, false>(a, wmap, xmap, groups, d, s);
+    return engine ? launch<NT, false, true>(a, wmap, xmap, groups, d, s) : launch<kByHand, false, false>(a, wmap, xmap, groups, d, s);
 }
 
 }  // namespace
@@ -761,10 +763,10 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     int nt = 16;
     while (nt < (wide ? 128 : 256) && nt < p.m) nt *= 2;
     switch (nt) {
-        case 16: return launch_as<16>(a, p.groups, d.sms, wide, engine, s);
-        case 32: return launch_as<32>(a, p.groups, d.sms, wide, engine, s);
-        case 64: return launch_as<64>(a, p.groups, d.sms, wide, engine, s);
-        case 128: return launch_as<128>(a, p.groups, d.sms, wide, engine, s);
+        case 16: return launch_as<16>(a, p.groups, d, wide, engine, s);
+        case 32: return launch_as<32>(a, p.groups, d, wide, engine, s);
+        case 64: return launch_as<64>(a, p.groups, d, wide, engine, s);
+        case 128: return launch_as<128>(a, p.groups, d, wide, engine, s);
     }
-    return launch_as<256>(a, p.groups, d.sms, false, engine, s);
+    return launch_as<256>(a, p.groups, d, false, engine, s);
 }

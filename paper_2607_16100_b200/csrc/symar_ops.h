@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "symar.h"
 #include "symar_internal.h"
 
@@ -69,6 +71,16 @@ __device__ __forceinline__ int kv_page_of(const KvView &c, const KvBatch &b, int
     return -1;
 }
 #endif
+
+// Dynamic shared memory of a kernel, allowed once per device (`done`: a bit per device, one word per kernel).
+inline cudaError_t allow_shared(const void *fn, int bytes, int device, std::atomic<uint64_t> &done)
+{
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Argument checks shared by the calls on a cache; fills the views.
 int kv_check(const symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch, KvView *c, KvBatch *b);

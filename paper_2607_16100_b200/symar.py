@@ -436,13 +436,22 @@ class KVAttentionArgs(ctypes.Structure):
                 ("scale", c_float), ("q_heads", c_int32), ("window", c_int32), ("dtype", c_int32)]
 
 
+_T = None               # torch, once a call needed it
+_raw_stream = None      # device index -> handle of torch's current stream
+
+
 def _torch():
-    import torch
-    return torch
+    global _T, _raw_stream
+    if _T is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _T = torch
+    return _T
 
 
 def _dtype_code(t, where: str) -> int:
-    torch = _torch()
+    torch = _T or _torch()
     if t.dtype is torch.bfloat16:
         return BF16
     if t.dtype is torch.float32:
@@ -454,22 +463,18 @@ def _bad(where: str, what: str):
     raise SymarError(ERR_INVAL, f"{where}: {what}")
 
 
-def _on_device(t, stream):
-    """(context manager that makes t's device current or None, stream handle)."""
-    torch = _torch()
-    index = t.device.index
+def _call(fn, where, index: int, stream, *args) -> None:
+    """fn(*args, stream) with CUDA device ``index`` current; stream None = torch's current one."""
+    torch = _T or _torch()
     if stream is None:
-        stream = torch.cuda.current_stream(index).cuda_stream
-    return (None if index == torch.cuda.current_device() else torch.cuda.device(index)), stream
-
-
-def _call(fn, where, t, stream, *args) -> None:
-    guard, stream = _on_device(t, stream)
-    if guard is None:
-        _ck(fn(*args, stream), where)
+        stream = _raw_stream(index)
+    if index == torch.cuda.current_device():
+        rc = fn(*args, stream)
     else:
-        with guard:
-            _ck(fn(*args, stream), where)
+        with torch.cuda.device(index):
+            rc = fn(*args, stream)
+    if rc != OK:
+        raise SymarError(rc, where)
 
 
 def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, stream=None):
@@ -479,43 +484,50 @@ def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root:
     result [m, n] or [groups, m, n] of ``out_dtype`` (bfloat16 unless said or given by ``out``).  Operands of two
     dimensions (or expanded ones) are shared by all groups.  ``root``: the one group that adds bias and residual,
     -1 = every group."""
-    torch = _torch()
+    torch = _T or _torch()
     where = "symar_linear"
     bf16 = torch.bfloat16
     if x.dtype is not bf16 or w.dtype is not bf16 or (bias is not None and bias.dtype is not bf16):
         raise SymarError(ERR_UNSUPPORTED, f"{where}: operands are bfloat16")
-    if not x.is_cuda or x.dim() not in (2, 3) or w.dim() not in (2, 3) or act not in ACTS:
+    index = x.get_device()
+    xsh, wsh, xs, ws = x.shape, w.shape, x.stride(), w.stride()
+    xd, wd = len(xsh), len(wsh)
+    act_code = ACTS.get(act)
+    if index < 0 or xd not in (2, 3) or wd not in (2, 3) or act_code is None:
         _bad(where, "x, w are CUDA tensors of two or three dimensions, act is one of " + ", ".join(ACTS))
-    grouped = x.dim() == 3 or w.dim() == 3
-    groups = x.shape[0] if x.dim() == 3 else (w.shape[0] if grouped else 1)
-    (m, k), n = x.shape[-2:], w.shape[-2]
-    shape = (groups, m, n) if grouped else (m, n)
+    m, k, n = xsh[-2], xsh[-1], wsh[-2]
+    if xd == 3 or wd == 3:
+        groups = xsh[0] if xd == 3 else wsh[0]
+        shape = (groups, m, n)
+    else:
+        groups, shape = 1, (m, n)
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype or bf16, device=x.device)
-    elif out_dtype is not None and out.dtype is not out_dtype:
-        _bad(where, "out is not of out_dtype")
-    xs, ws, os = x.stride(), w.stride(), out.stride()
-    if w.shape[-1] != k or (w.dim() == 3 and w.shape[0] != groups) or out.shape != shape:
-        _bad(where, f"shapes of x {tuple(x.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)}")
-    if (k > 1 and (xs[-1] != 1 or ws[-1] != 1)) or (n > 1 and os[-1] != 1):
+        out = x.new_empty(shape, dtype=out_dtype or bf16)
+        os = out.stride()
+    else:
+        os = out.stride()
+        if (out_dtype is not None and out.dtype is not out_dtype) or out.shape != shape or (n > 1 and os[-1] != 1) or \
+                out.get_device() != index:
+            _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+    if wsh[-1] != k or (wd == 3 and wsh[0] != groups) or w.get_device() != index:
+        _bad(where, f"shapes of x {tuple(xsh)} and w {tuple(wsh)}, or not on one device")
+    if k > 1 and (xs[-1] != 1 or ws[-1] != 1):
         _bad(where, "the innermost axis is contiguous")
     bp = bg = rp = rl = rg = 0
     if bias is not None:
-        if bias.shape not in ((n,), (groups, n)) or (n > 1 and bias.stride(-1) != 1) or bias.device != x.device:
+        if bias.shape not in ((n,), (groups, n)) or (n > 1 and bias.stride(-1) != 1) or bias.get_device() != index:
             _bad(where, f"bias of shape {tuple(bias.shape)}")
         bp, bg = bias.data_ptr(), bias.stride(0) if bias.dim() == 2 else 0
     if residual is not None:
-        if residual.shape not in (shape, (m, n)) or residual.dtype is not out.dtype or (n > 1 and residual.stride(-1) != 1) or \
-                residual.device != x.device:
-            _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rs = residual.stride()
+        if residual.shape not in (shape, (m, n)) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or \
+                residual.get_device() != index:
+            _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
-    if w.device != x.device or out.device != x.device:
-        _bad(where, "all tensors are on one device")
-    args = LinearArgs(x.data_ptr(), xs[-2], xs[0] if len(xs) == 3 else 0, w.data_ptr(), ws[-2],
-                      ws[0] if len(ws) == 3 else 0, bp, bg, rp, rl, rg, out.data_ptr(), os[-2],
-                      os[0] if len(os) == 3 else 0, groups, m, n, k, _dtype_code(out, where), ACTS[act], root)
-    _call(load().symar_linear, where, x, stream, byref(args))
+    args = LinearArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[0] if wd == 3 else 0, bp, bg, rp, rl,
+                      rg, out.data_ptr(), os[-2], os[0] if len(os) == 3 else 0, groups, m, n, k,
+                      BF16 if out.dtype is bf16 else _dtype_code(out, where), act_code, root)
+    _call((_lib or load()).symar_linear, where, index, stream, byref(args))
     return out
 
 
@@ -528,7 +540,7 @@ def rope_table(rows: int, rot_dim: int, *, base: float = 10000.0, kind: str = "p
         _bad("symar_rope_table", f"rows {rows}, kind {kind!r}")
     table = torch.empty(rows, rot_dim // 2, 2, dtype=torch.float32, device=device)
     how = RopeScaling(base, factor, original, low, high, magnitude, ROPE_KINDS[kind], rot_dim)
-    _call(load().symar_rope_table, "symar_rope_table", table, stream, table.data_ptr(), rows, byref(how))
+    _call(load().symar_rope_table, "symar_rope_table", table.get_device(), stream, table.data_ptr(), rows, byref(how))
     return table
 
 
@@ -536,15 +548,17 @@ class PagedKV:
     """A pool of 4-bit key/value pages in a torch uint8 tensor [pages, kv_heads, bytes of one head's page]."""
 
     def __init__(self, pages, head_dim: int, page_size: int):
-        torch = _torch()
-        each = int(load().symar_kv_page_bytes(1, head_dim, page_size))
-        if not each:
+        torch = _T or _torch()
+        shape = pages.shape
+        each = page_size * head_dim + 8 * page_size * (head_dim // KV_GROUP)
+        if head_dim not in (64, 128, 256) or page_size not in (16, 32, 64, 128, 256):
             raise SymarError(ERR_UNSUPPORTED, f"PagedKV: head_dim {head_dim}, page_size {page_size}")
-        if pages.dtype is not torch.uint8 or pages.dim() != 3 or pages.shape[2] != each or not pages.is_contiguous() or \
+        if pages.dtype is not torch.uint8 or len(shape) != 3 or shape[2] != each or not pages.is_contiguous() or \
                 not pages.is_cuda:
             _bad("PagedKV", f"pages are a contiguous CUDA uint8 tensor [pages, kv_heads, {each}]")
-        self.pages, self.head_dim, self.page_size, self.kv_heads = pages, head_dim, page_size, pages.shape[1]
-        self.args = KVCacheArgs(pages.data_ptr(), pages.shape[0], pages.shape[1], head_dim, page_size)
+        self.pages, self.head_dim, self.page_size, self.kv_heads = pages, head_dim, page_size, shape[1]
+        self.args = KVCacheArgs(pages.data_ptr(), shape[0], shape[1], head_dim, page_size)
+        self.ref = byref(self.args)
 
     @classmethod
     def zeros(cls, pages: int, kv_heads: int, head_dim: int, page_size: int, device="cuda") -> "PagedKV":
@@ -558,28 +572,30 @@ class KVBatch:
     have other than one new token each, token_start [seqs + 1]."""
 
     def __init__(self, lengths, page_table, token_start=None):
-        i32 = _torch().int32
-        seqs = lengths.shape[0]
-        if lengths.dtype is not i32 or page_table.dtype is not i32 or lengths.dim() != 1 or page_table.dim() != 2 or \
-                page_table.shape[0] != seqs or (seqs > 1 and lengths.stride(0) != 1) or \
-                (page_table.shape[1] > 1 and page_table.stride(1) != 1) or not lengths.is_cuda or \
-                page_table.device != lengths.device:
-            _bad("KVBatch", "lengths [seqs] and page_table [seqs, columns] are int32 CUDA tensors")
+        i32 = (_T or _torch()).int32
+        ls, ps = lengths.shape, page_table.shape
+        index = lengths.get_device()
         # (the row stride doubles as the number of columns that the kernels may read)
-        if seqs > 1 and page_table.stride(0) != page_table.shape[1]:
-            _bad("KVBatch", "page_table is contiguous")
-        if token_start is not None and (token_start.dtype is not i32 or token_start.shape != (seqs + 1,) or
-                                        token_start.stride(0) != 1 or token_start.device != lengths.device):
-            _bad("KVBatch", "token_start [seqs + 1] is an int32 CUDA tensor")
-        self.lengths, self.page_table, self.token_start, self.seqs = lengths, page_table, token_start, seqs
-        self.args = KVBatchArgs(lengths.data_ptr(), token_start.data_ptr() if token_start is not None else None,
-                                page_table.data_ptr(), page_table.shape[1], seqs, 0)
+        if lengths.dtype is not i32 or page_table.dtype is not i32 or len(ls) != 1 or len(ps) != 2 or ps[0] != ls[0] or \
+                not lengths.is_contiguous() or not page_table.is_contiguous() or index < 0 or page_table.get_device() != index:
+            _bad("KVBatch", "lengths [seqs] and page_table [seqs, columns] are contiguous int32 CUDA tensors")
+        seqs = ls[0]
+        start = None
+        if token_start is not None:
+            if token_start.dtype is not i32 or token_start.shape != (seqs + 1,) or not token_start.is_contiguous() or \
+                    token_start.get_device() != index:
+                _bad("KVBatch", "token_start [seqs + 1] is a contiguous int32 CUDA tensor")
+            start = token_start.data_ptr()
+        self.lengths, self.page_table, self.token_start, self.seqs, self.index = lengths, page_table, token_start, seqs, index
+        self.args = KVBatchArgs(lengths.data_ptr(), start, page_table.data_ptr(), ps[1], seqs, 0)
+        self.ref = byref(self.args)
 
 
 class KVContext:
     """Owner of one ``symar_kv_t``: what the cache operators of one stream share."""
 
     def __init__(self, device_mem: int | None = None, device_bytes: int = 0, keepalive=None):
+        _torch()
         self._lib = load()
         self._h = c_void_p()
         self._keepalive = keepalive
@@ -618,63 +634,65 @@ class KVContext:
         return code.value, seq.value, position.value
 
     @staticmethod
-    def _rows(where, name, t, tokens, heads, dim, like):
-        if t.shape != (tokens, heads, dim) or t.stride(2) != 1 or t.dtype is not like.dtype or t.device != like.device:
-            _bad(where, f"{name} is [{tokens}, {heads}, {dim}] {like.dtype} on {like.device} with contiguous channels, not "
+    def _rows(where, name, t, shape, dtype, index):
+        st = t.stride()
+        if t.shape != shape or st[2] != 1 or t.dtype is not dtype or t.get_device() != index:
+            _bad(where, f"{name} is {list(shape)} {dtype} on the batch's device with contiguous channels, not "
                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
-        return t.data_ptr(), t.stride(0), t.stride(1)
+        return t.data_ptr(), st[0], st[1]
 
     def append(self, cache: PagedKV, batch: KVBatch, k, v, *, q=None, q_out=None, rotations=None, interleaved: bool = False,
                stream=None):
         """Rotate q and k, store k and v (``symar_kv_append``); returns the rotated q (``q_out``, new unless given)."""
         where = "symar_kv_append"
-        dim, tokens = cache.head_dim, k.shape[0]
-        kr = self._rows(where, "k", k, tokens, cache.kv_heads, dim, k)
-        vr = self._rows(where, "v", v, tokens, cache.kv_heads, dim, k)
-        qr = qo = (None, 0, 0)
-        q_heads = 0
+        dtype, index, dim, tokens = k.dtype, batch.index, cache.head_dim, k.shape[0]
+        shape = (tokens, cache.kv_heads, dim)
+        kp, kl, kh = self._rows(where, "k", k, shape, dtype, index)
+        vp, vl, vh = self._rows(where, "v", v, shape, dtype, index)
+        qp = ql = qh = op = ol = oh = q_heads = rp = rows = rot = 0
         if q is not None:
-            q_heads = q.shape[1] if q.dim() == 3 else -1
-            qr = self._rows(where, "q", q, tokens, q_heads, dim, k)
+            if q.dim() != 3:
+                _bad(where, "q is [tokens, q_heads, head_dim]")
+            q_heads = q.shape[1]
+            shape = (tokens, q_heads, dim)
+            qp, ql, qh = self._rows(where, "q", q, shape, dtype, index)
             if q_out is None:
-                q_out = _torch().empty(tokens, q_heads, dim, dtype=q.dtype, device=q.device)
-            qo = self._rows(where, "q_out", q_out, tokens, q_heads, dim, k)
-        rows = rot = 0
+                q_out = q.new_empty(shape)
+            op, ol, oh = self._rows(where, "q_out", q_out, shape, dtype, index)
         if rotations is not None:
-            if rotations.dim() != 3 or rotations.shape[2] != 2 or rotations.dtype is not _torch().float32 or \
-                    not rotations.is_contiguous() or rotations.device != k.device:
+            rs = rotations.shape
+            if len(rs) != 3 or rs[2] != 2 or rotations.dtype is not (_T or _torch()).float32 or \
+                    not rotations.is_contiguous() or rotations.get_device() != index:
                 _bad(where, "rotations are a contiguous float32 tensor [positions, rot_dim / 2, 2]")
-            rows, rot = rotations.shape[0], 2 * rotations.shape[1]
-        args = KVAppendArgs(*qr, *qo, *kr, *vr, rotations.data_ptr() if rotations is not None else None, rows, rot,
-                            1 if interleaved else 0, q_heads, _dtype_code(k, where))
+            rp, rows, rot = rotations.data_ptr(), rs[0], 2 * rs[1]
+        args = KVAppendArgs(qp, ql, qh, op, ol, oh, kp, kl, kh, vp, vl, vh, rp, rows, rot, 1 if interleaved else 0, q_heads,
+                            _dtype_code(k, where))
         batch.args.tokens = tokens
-        _call(self._lib.symar_kv_append, where, k, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+        _call(self._lib.symar_kv_append, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
         return q_out
 
     def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
         """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
-        torch = _torch()
-        kv = torch.empty(2, tokens, cache.kv_heads, cache.head_dim, dtype=dtype or torch.bfloat16, device=cache.pages.device)
-        k, v = kv[0], kv[1]
-        ld, head = k.stride(0), k.stride(1)
-        args = KVReadArgs(k.data_ptr(), ld, head, v.data_ptr(), ld, head, _dtype_code(k, "symar_kv_read"))
+        heads, dim = cache.kv_heads, cache.head_dim
+        k, v = cache.pages.new_empty((2, tokens, heads, dim), dtype=dtype or (_T or _torch()).bfloat16).unbind(0)
+        args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(k, "symar_kv_read"))
         batch.args.tokens = tokens
-        _call(self._lib.symar_kv_read, "symar_kv_read", k, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+        _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.ref, byref(args))
         return k, v
 
     def attention(self, cache: PagedKV, batch: KVBatch, q, *, out=None, scale: float = 0.0, window: int = 0, stream=None):
         """Attention of the batch's new tokens over the cache (``symar_kv_attention``)."""
         where = "symar_kv_attention"
-        if q.dim() != 3:
+        shape, dtype, index = q.shape, q.dtype, batch.index
+        if len(shape) != 3 or shape[2] != cache.head_dim:
             _bad(where, "q is [tokens, q_heads, head_dim]")
-        tokens, heads = q.shape[0], q.shape[1]
         if out is None:
-            out = _torch().empty(tokens, heads, cache.head_dim, dtype=q.dtype, device=q.device)
-        args = KVAttentionArgs(*self._rows(where, "q", q, tokens, heads, cache.head_dim, q),
-                               *self._rows(where, "out", out, tokens, heads, cache.head_dim, q), scale, heads, window,
-                               _dtype_code(q, where))
-        batch.args.tokens = tokens
-        _call(self._lib.symar_kv_attention, where, q, stream, self._h, byref(cache.args), byref(batch.args), byref(args))
+            out = q.new_empty(shape)
+        qp, ql, qh = self._rows(where, "q", q, shape, dtype, index)
+        op, ol, oh = self._rows(where, "out", out, shape, dtype, index)
+        args = KVAttentionArgs(qp, ql, qh, op, ol, oh, scale, shape[1], window, _dtype_code(q, where))
+        batch.args.tokens = shape[0]
+        _call(self._lib.symar_kv_attention, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
         return out
 
 
