@@ -475,7 +475,7 @@ int symar_linear(const symar_linear_t *args, void *cuda_stream);
 /* The paged 4-bit cache.  `pages` holds num_pages pages of
  *     [kv_heads][ K codes [page_size][D/2] u8 | V codes [page_size][D/2] u8 |
  *                 K words [page_size][D/64] u32 | V words [page_size][D/64] u32 ]
- * 16-byte aligned; D = head_dim is 64, 128 or 256, page_size 16, 32, 64, 128 or 256 tokens.  Channel c of a token is
+ * 16-byte aligned; D = head_dim is 64, 128 or 256, page_size 16, 32, 64, 128 or 256 tokens, at most 4096 heads.  Channel c of a token is
  * nibble c, low nibble first.  Each 64 channels share a word: a binary32 scale s >= 0 whose four lowest bits hold the
  * zero point z; code n stands for s (n - z).  A group x is stored with lo = min(0, x), hi = max(0, x),
  * s = hi/15 - lo/15 (each product rounded, 1/15 being the binary32 nearest to it; the difference's four lowest bits

@@ -758,7 +758,8 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     if (rc != SYMAR_OK) return rc;
     if (!args || (args->dtype != SYMAR_F32 && args->dtype != SYMAR_BF16)) return SYMAR_ERR_INVAL;
     if (args->dtype != SYMAR_BF16) return SYMAR_ERR_UNSUPPORTED;
-    if (args->q_heads < 1 || args->q_heads % cache->kv_heads || args->q_heads > 65536 || args->window < 0) return SYMAR_ERR_INVAL;
+    if (args->q_heads > 4096) return SYMAR_ERR_UNSUPPORTED;
+    if (args->q_heads < 1 || args->q_heads % cache->kv_heads || args->window < 0) return SYMAR_ERR_INVAL;
     if (!(args->scale >= 0.0f) || std::isinf(args->scale)) return SYMAR_ERR_INVAL;
     if (batch->tokens == 0) return SYMAR_OK;
     if (!args->q || !args->out || ((uintptr_t)args->q | (uintptr_t)args->out) % 2) return SYMAR_ERR_INVAL;

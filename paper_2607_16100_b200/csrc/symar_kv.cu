@@ -108,6 +108,10 @@ struct AppendArgs {
     int     rot, interleaved, q_heads;
     int    *status;
     int     tokens_per_block;
+    int     run;                 // query heads that a thread turns by the rotations it has loaded
+    int     groups;              // of `run` query heads
+    int     kv_blocks;           // blocks of the first kind (see append_kernel)
+    uint32_t by_groups, by_heads;      // reciprocals: 2^32 / groups, 2^32 / (2 kv_heads), rounded up
 };
 
 // One unit is one head of one token: dim/8 lanes of a warp, eight channels each.  The partner channels of the
@@ -153,6 +157,9 @@ __device__ __forceinline__ void rotate8(float (&x)[8], const T *row, bool vec, i
     }
 }
 
+// x rounded to a whole number, for |x| < 2^22: what lies below 1 in a sum with 1.5 * 2^23 is rounded away, ties to even
+__device__ __forceinline__ float whole(float x) { return __fsub_rn(__fadd_rn(x, 12582912.0f), 12582912.0f); }
+
 // Codes and word of a group of 64 channels held by eight neighbouring lanes.  Returns this lane's eight codes.
 __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &word)
 {
@@ -161,7 +168,7 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &wor
     for (int i = 0; i < 8; ++i) {
         lo  = fminf(lo, x[i]);
         hi  = fmaxf(hi, x[i]);
-        odd = __fadd_rn(odd, __fmul_rn(x[i], 0.0f));
+        odd = __fmaf_rn(x[i], 0.0f, odd);
     }
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) {
@@ -181,18 +188,85 @@ __device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t &wor
         return 0u;
     }
     const float inv = __fdiv_rn(1.0f, s);
-    const float z   = rintf(__fmul_rn(-lo, inv));
+    const float z   = whole(__fmul_rn(-lo, inv));
     word            = bits | (uint32_t)z;
-    uint32_t codes  = 0;
+    float half[2];                                     // four codes each: n0 + 16 n1 + 256 n2 + 4096 n3, exact
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float n = fminf(fmaxf(__fadd_rn(rintf(__fmul_rn(x[i], inv)), z), 0.0f), 15.0f);
-        codes |= (uint32_t)n << (4 * i);
+    for (int j = 0; j < 2; ++j) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+            sum = __fmaf_rn(sum, 16.0f, fminf(fmaxf(__fadd_rn(whole(__fmul_rn(x[4 * j + i], inv)), z), 0.0f), 15.0f));
+        half[j] = __fadd_rn(sum, 8388608.0f);
     }
-    return codes;
+    return __byte_perm(__float_as_uint(half[0]), __float_as_uint(half[1]), 0x5410);
 }
 
+// n / d for n < 2^31 / d, by the reciprocal that the host rounded up
+__device__ __forceinline__ int over(int n, uint32_t reciprocal) { return reciprocal ? (int)__umulhi((uint32_t)n, reciprocal) : n; }
+
+// (a, b) turned by eight angles
+__device__ __forceinline__ void turn8(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = a[i], y = b[i];
+        a[i] = __fsub_rn(__fmul_rn(x, c[i]), __fmul_rn(y, s[i]));
+        b[i] = __fadd_rn(__fmul_rn(y, c[i]), __fmul_rn(x, s[i]));
+    }
+}
+
+// Queries of a block's tokens.  A thread has sixteen channels of `run` heads of one token: in the half layout eight and the eight
+// that they are turned with, so that nothing is read twice and the eight rotations are loaded once for all its heads; in the interleaved
+// layout sixteen neighbours.  Channels that are not turned go along in pairs of eights.
 template <typename T>
+__device__ __forceinline__ void queries(const AppendArgs &a, const Place *at, int first, int mine)
+{
+    const int lanes = a.c.dim / 16, shift = 31 - __clz(lanes), half = a.rot >> 4;      // half: threads of a head that turn something
+    const int total = mine * a.groups * lanes;
+    for (int u = (int)((blockIdx.y - (unsigned)a.kv_blocks) * kThreads + threadIdx.x); u < total; u += (int)(gridDim.y - (unsigned)a.kv_blocks) * kThreads) {
+        const int j = u & (lanes - 1), tg = u >> shift, t = over(tg, a.by_groups), group = tg - t * a.groups;
+        const Place p = at[t];
+        const bool turn = a.table && p.pos >= 0 && p.pos < a.table_rows && j < half;
+        const int c0 = a.interleaved ? 16 * j : (j < half ? 8 * j : a.rot + 16 * (j - half));
+        const int c1 = a.interleaved || j >= half ? c0 + 8 : c0 + (a.rot >> 1);
+        float cs[8], sn[8];
+        if (turn) {
+            const float4 *w = reinterpret_cast<const float4 *>(a.table + (int64_t)p.pos * (a.rot >> 1) + 8 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 v = __ldg(w + i);
+                cs[2 * i] = v.x; sn[2 * i] = v.y; cs[2 * i + 1] = v.z; sn[2 * i + 1] = v.w;
+            }
+        }
+        if (a.table && p.pos >= a.table_rows && j == 0 && group == 0) kv_record(a.status, p.seq, p.pos);
+        const T *src = reinterpret_cast<const T *>(a.q.p) + (int64_t)(first + t) * a.q.ld + (int64_t)(group * a.run) * a.q.head;
+        T *dst       = reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + t) * a.qo.ld + (int64_t)(group * a.run) * a.qo.head;
+        const int heads = min(a.run, a.q_heads - group * a.run);
+#pragma unroll 2
+        for (int h = 0; h < heads; ++h, src += a.q.head, dst += a.qo.head) {
+            float x[8], y[8];
+            load8(src + c0, a.q.vec, x);
+            load8(src + c1, a.q.vec, y);
+            if (turn && !a.interleaved) {
+                turn8(x, y, cs, sn);
+            } else if (turn) {
+                float e[8], o[8];                      // the pairs' first and second channels
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = x[2 * i], o[i] = x[2 * i + 1], e[i + 4] = y[2 * i], o[i + 4] = y[2 * i + 1];
+                turn8(e, o, cs, sn);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[2 * i] = e[i], x[2 * i + 1] = o[i], y[2 * i] = e[i + 4], y[2 * i + 1] = o[i + 4];
+            }
+            store8(dst + c0, a.qo.vec, x);
+            store8(dst + c1, a.qo.vec, y);
+        }
+    }
+}
+
+// Blocks with the first kv_blocks indexes in y store keys and values, the others turn queries.  (Where the queries' pairs do not come in
+// eights, kPaired is false and every block does both, a head of a token like another.)
+template <typename T, bool kPaired>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
 {
     __shared__ Place at[kMaxTokens];
@@ -200,18 +274,22 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
     const int mine  = min(a.tokens_per_block, a.b.tokens - first);
     if ((int)threadIdx.x < mine) at[threadIdx.x] = place_of(a.c, a.b, a.status, first + threadIdx.x);
     __syncthreads();
+    if (kPaired && (int)blockIdx.y >= a.kv_blocks) {
+        queries<T>(a, at, first, mine);
+        return;
+    }
 
-    const int lanes = a.c.dim / 8, per_pass = kThreads / lanes;
-    const int heads = a.q_heads + 2 * a.c.kv_heads, units = mine * heads;
+    const int lanes = a.c.dim / 8, shift = 31 - __clz(lanes), per_pass = kThreads / lanes;
+    const int q_heads = kPaired ? 0 : a.q_heads, heads = q_heads + 2 * a.c.kv_heads, units = mine * heads;
     const int lane  = (int)threadIdx.x & (lanes - 1), c0 = lane * 8;
     // every warp makes the same number of trips: the shuffles and the barrier below take whole warps
-    for (int u0 = (int)blockIdx.y * per_pass; u0 < units; u0 += (int)gridDim.y * per_pass) {
-        const int  u   = u0 + (int)threadIdx.x / lanes;
+    for (int u0 = (int)blockIdx.y * per_pass; u0 < units; u0 += (kPaired ? a.kv_blocks : (int)gridDim.y) * per_pass) {
+        const int  u   = u0 + ((int)threadIdx.x >> shift);
         const bool on  = u < units;
-        const int  t   = on ? u / heads : 0, h = on ? u - t * heads : 0;
+        const int  t   = on ? over(u, a.by_heads) : 0, h = on ? u - t * heads : 0;
         const Place p  = at[t];
-        const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.c.kv_heads;
-        const int  hh   = is_q ? h : (is_k ? h - a.q_heads : h - a.q_heads - a.c.kv_heads);
+        const bool is_q = h < q_heads, is_k = !is_q && h < q_heads + a.c.kv_heads;
+        const int  hh   = is_q ? h : (is_k ? h - q_heads : h - q_heads - a.c.kv_heads);
         const Rows &r   = is_q ? a.q : (is_k ? a.k : a.v);
         const T *row    = reinterpret_cast<const T *>(r.p) + (int64_t)(first + t) * r.ld + (int64_t)hh * r.head;
         float x[8] = {};
@@ -243,6 +321,7 @@ struct ReadArgs {
     Rows    k, v;
     int    *status;
     int     tokens_per_block;
+    uint32_t by_heads;
 };
 
 template <typename T>
@@ -254,11 +333,11 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
     if ((int)threadIdx.x < mine) at[threadIdx.x] = place_of(a.c, a.b, a.status, first + threadIdx.x);
     __syncthreads();
 
-    const int lanes = a.c.dim / 8, per_pass = kThreads / lanes;
+    const int lanes = a.c.dim / 8, shift = 31 - __clz(lanes), per_pass = kThreads / lanes;
     const int heads = 2 * a.c.kv_heads, units = mine * heads, ps = 1 << a.c.page_shift;
     const int lane  = (int)threadIdx.x & (lanes - 1);
-    for (int u = (int)blockIdx.y * per_pass + (int)threadIdx.x / lanes; u < units; u += (int)gridDim.y * per_pass) {
-        const int  t = u / heads, h = u - t * heads;
+    for (int u = (int)blockIdx.y * per_pass + ((int)threadIdx.x >> shift); u < units; u += (int)gridDim.y * per_pass) {
+        const int  t = over(u, a.by_heads), h = u - t * heads;
         const bool is_k = h < a.c.kv_heads;
         const int  hh   = is_k ? h : h - a.c.kv_heads;
         const Rows &r   = is_k ? a.k : a.v;
@@ -315,6 +394,9 @@ bool make_rows(Rows *r, const void *p, int64_t ld, int64_t head, int dtype)
     r->vec  = (uintptr_t)p % 16 == 0 && ld % vec == 0 && head % vec == 0;
     return true;
 }
+
+// 2^32 / d rounded up (0 stands for 1): n * that / 2^32 is n / d while n d < 2^32
+uint32_t reciprocal(int d) { return d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
 
 // Blocks of append and read: few tokens take one head per thread group, many take up to eight tokens per block.
 dim3 token_grid(int tokens, int heads, int lanes, int num_sms, int *tokens_per_block)
@@ -478,7 +560,8 @@ int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_k
     const int rc = kv_check(kv, cache, batch, &a.c, &a.b);
     if (rc != SYMAR_OK) return rc;
     if (!args || (args->dtype != SYMAR_F32 && args->dtype != SYMAR_BF16)) return SYMAR_ERR_INVAL;
-    if (args->q_heads < 0 || args->q_heads > 65536 || (args->interleaved != 0 && args->interleaved != 1)) return SYMAR_ERR_INVAL;
+    if (args->q_heads > 4096) return SYMAR_ERR_UNSUPPORTED;
+    if (args->q_heads < 0 || (args->interleaved != 0 && args->interleaved != 1)) return SYMAR_ERR_INVAL;
     if (args->rotations && (args->rot_dim < 2 || args->rot_dim % 2 || args->rot_dim > cache->head_dim || args->rotation_rows < 0 ||
                             (uintptr_t)args->rotations % 8))
         return SYMAR_ERR_INVAL;
@@ -495,9 +578,32 @@ int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_k
     a.rot         = args->rotations ? args->rot_dim : 0;
     a.interleaved = args->interleaved;
     a.status      = kv->status;
-    const dim3 grid = token_grid(batch->tokens, a.q_heads + 2 * a.c.kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
-    if (args->dtype == SYMAR_F32) append_kernel<float><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
-    else append_kernel<__nv_bfloat16><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    // queries by pairs of eights where their rotated part and its halves come in eights and the table's rows on 16 bytes
+    const bool paired = a.q_heads > 0 && a.rot % 16 == 0 && (uintptr_t)a.table % 16 == 0;
+    const int kv_heads = (paired || a.q_heads == 0 ? 0 : a.q_heads) + 2 * a.c.kv_heads;
+    dim3 grid = token_grid(batch->tokens, kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
+    a.by_heads  = reciprocal(kv_heads);
+    a.kv_blocks = (int)grid.y;
+    a.run = a.groups = 1;
+    a.by_groups = 0;
+    if (paired) {
+        // a run of heads per thread once there are more than a few waves of threads without it
+        const int64_t threads = (int64_t)batch->tokens * a.q_heads * (a.c.dim / 16);
+        a.run = 1;
+        while (a.run < 8 && a.run < a.q_heads && threads / (2 * a.run) >= 4096ll * kv->num_sms) a.run *= 2;
+        a.groups    = (a.q_heads + a.run - 1) / a.run;
+        a.by_groups = reciprocal(a.groups);
+        const int64_t per_block = (int64_t)a.tokens_per_block * a.groups * (a.c.dim / 16);
+        grid.y += (unsigned)((per_block + kThreads - 1) / kThreads);
+    }
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (args->dtype == SYMAR_F32) {
+        if (paired) append_kernel<float, true><<<grid, kThreads, 0, s>>>(a);
+        else append_kernel<float, false><<<grid, kThreads, 0, s>>>(a);
+    } else {
+        if (paired) append_kernel<__nv_bfloat16, true><<<grid, kThreads, 0, s>>>(a);
+        else append_kernel<__nv_bfloat16, false><<<grid, kThreads, 0, s>>>(a);
+    }
     cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_append");
 }
@@ -514,6 +620,7 @@ int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_
         !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype))
         return SYMAR_ERR_INVAL;
     a.status = kv->status;
+    a.by_heads = reciprocal(2 * a.c.kv_heads);
     const dim3 grid = token_grid(batch->tokens, 2 * a.c.kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
     if (args->dtype == SYMAR_F32) read_kernel<float><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
     else read_kernel<__nv_bfloat16><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
