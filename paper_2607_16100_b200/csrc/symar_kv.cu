@@ -10,38 +10,47 @@ namespace symar {
 namespace {
 
 constexpr int kThreads   = 256;
-constexpr int kMaxTokens = 8;       // tokens that one block of append or read takes
+constexpr int kMaxTokens = 16;      // tokens that one block of append or read takes
 
 // ---- eight channels of a row, in binary32 ------------------------------------------
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
-__device__ __forceinline__ void load8(const float *p, bool vec, float (&x)[8])
-{
-    if (vec) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = p[i];
+template <typename T> struct Eight;                 // eight channels as they lie in memory
+template <> struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p, bool vec)
+    {
+        if (vec) a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+        else a = make_float4(p[0], p[1], p[2], p[3]), b = make_float4(p[4], p[5], p[6], p[7]);
     }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, bool vec, float (&x)[8])
-{
-    if (vec) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+};
+template <> struct Eight<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool vec)
+    {
+        if (vec) {
+            a = *reinterpret_cast<const uint4 *>(p);
+        } else {
+            const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+            a = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i]     = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __bfloat162float(p[i]);
     }
-}
+};
 __device__ __forceinline__ void store8(float *p, bool vec, const float (&x)[8])
 {
     if (vec) {
@@ -114,12 +123,13 @@ struct AppendArgs {
     uint32_t by_groups, by_heads;      // reciprocals: 2^32 / groups, 2^32 / (2 kv_heads), rounded up
 };
 
-// One unit is one head of one token: dim/8 lanes of a warp, eight channels each.  The partner channels of the
-// half layout are read again from global memory (they are in L1: another lane of the same warp reads them too),
-// before any lane of the warp writes, so that q may be rotated in place.
+// One unit is one head of one token: dim/8 lanes of a warp, eight channels each.  The channels that those of the half layout are
+// turned with are read beside them (another lane of the warp reads them too), before any lane of the warp writes, so that q may be
+// rotated in place.
+__device__ __forceinline__ bool whole_chunk_pairs(int rot) { return (rot & 15) == 0; }
+__device__ __forceinline__ int pair_of(int c0, int rot) { return c0 < (rot >> 1) ? c0 + (rot >> 1) : c0 - (rot >> 1); }
 template <typename T>
-__device__ __forceinline__ void rotate8(float (&x)[8], const T *row, bool vec, int c0, int rot, bool interleaved,
-                                        const float2 *cs)
+__device__ __forceinline__ void rotate8(float (&x)[8], const Eight<T> &pair, const T *row, int c0, int rot, bool interleaved, const float2 *cs)
 {
     if (c0 >= rot) return;
     if (interleaved) {
@@ -127,7 +137,7 @@ __device__ __forceinline__ void rotate8(float (&x)[8], const T *row, bool vec, i
         for (int i = 0; i < 4; ++i) {
             const int ch = c0 + 2 * i;
             if (ch < rot) {
-                const float2 t = cs[ch >> 1];
+                const float2 t = __ldg(cs + (ch >> 1));
                 const float a = x[2 * i], b = x[2 * i + 1];
                 x[2 * i]     = __fsub_rn(__fmul_rn(a, t.x), __fmul_rn(b, t.y));
                 x[2 * i + 1] = __fadd_rn(__fmul_rn(b, t.x), __fmul_rn(a, t.y));
@@ -137,20 +147,36 @@ __device__ __forceinline__ void rotate8(float (&x)[8], const T *row, bool vec, i
     }
     const int h = rot >> 1;
     float y[8];
-    if ((h & 7) == 0) {                                // the whole chunk lies in one half
-        load8(row + (c0 < h ? c0 + h : c0 - h), vec, y);
-    } else {
+    if (whole_chunk_pairs(rot)) {                      // the chunk lies in one half
+        pair.get(y);
+        const float4 *w = reinterpret_cast<const float4 *>(cs + (c0 < h ? c0 : c0 - h));
+        const bool low = c0 < h;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int ch = c0 + i;
-            y[i] = ch < rot ? to_f32(row[ch < h ? ch + h : ch - h]) : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            float4 t;
+            if (((uintptr_t)cs & 15) == 0) {
+                t = __ldg(w + i);
+            } else {
+                const float2 u = __ldg(reinterpret_cast<const float2 *>(w + i)), v = __ldg(reinterpret_cast<const float2 *>(w + i) + 1);
+                t = make_float4(u.x, u.y, v.x, v.y);
+            }
+            const float a0 = __fmul_rn(x[2 * i], t.x), b0 = __fmul_rn(y[2 * i], t.y);
+            const float a1 = __fmul_rn(x[2 * i + 1], t.z), b1 = __fmul_rn(y[2 * i + 1], t.w);
+            x[2 * i]     = low ? __fsub_rn(a0, b0) : __fadd_rn(a0, b0);
+            x[2 * i + 1] = low ? __fsub_rn(a1, b1) : __fadd_rn(a1, b1);
         }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int ch = c0 + i;
+        y[i] = ch < rot ? to_f32(row[ch < h ? ch + h : ch - h]) : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int ch = c0 + i;
         if (ch < rot) {
-            const float2 t = cs[ch < h ? ch : ch - h];
+            const float2 t = __ldg(cs + (ch < h ? ch : ch - h));
             const float a = __fmul_rn(x[i], t.x), b = __fmul_rn(y[i], t.y);
             x[i] = ch < h ? __fsub_rn(a, b) : __fadd_rn(a, b);
         }
@@ -243,31 +269,40 @@ __device__ __forceinline__ void queries(const AppendArgs &a, const Place *at, in
         const T *src = reinterpret_cast<const T *>(a.q.p) + (int64_t)(first + t) * a.q.ld + (int64_t)(group * a.run) * a.q.head;
         T *dst       = reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + t) * a.qo.ld + (int64_t)(group * a.run) * a.qo.head;
         const int heads = min(a.run, a.q_heads - group * a.run);
-#pragma unroll 2
-        for (int h = 0; h < heads; ++h, src += a.q.head, dst += a.qo.head) {
-            float x[8], y[8];
-            load8(src + c0, a.q.vec, x);
-            load8(src + c1, a.q.vec, y);
-            if (turn && !a.interleaved) {
-                turn8(x, y, cs, sn);
-            } else if (turn) {
-                float e[8], o[8];                      // the pairs' first and second channels
+        constexpr int kAhead = sizeof(T) == 2 ? 2 : 1;             // heads whose loads are on their way at a time
+        for (int h0 = 0; h0 < heads; h0 += kAhead, src += kAhead * a.q.head, dst += kAhead * a.qo.head) {
+            Eight<T> u[kAhead], v[kAhead];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = x[2 * i], o[i] = x[2 * i + 1], e[i + 4] = y[2 * i], o[i + 4] = y[2 * i + 1];
-                turn8(e, o, cs, sn);
+            for (int i = 0; i < kAhead; ++i)
+                if (h0 + i < heads) u[i].load(src + i * a.q.head + c0, a.q.vec), v[i].load(src + i * a.q.head + c1, a.q.vec);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[2 * i] = e[i], x[2 * i + 1] = o[i], y[2 * i] = e[i + 4], y[2 * i + 1] = o[i + 4];
+            for (int i = 0; i < kAhead; ++i) {
+                if (h0 + i >= heads) break;
+                float x[8], y[8];
+                u[i].get(x);
+                v[i].get(y);
+                if (turn && !a.interleaved) {
+                    turn8(x, y, cs, sn);
+                } else if (turn) {
+                    float e[8], o[8];                  // the pairs' first and second channels
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) e[l] = x[2 * l], o[l] = x[2 * l + 1], e[l + 4] = y[2 * l], o[l + 4] = y[2 * l + 1];
+                    turn8(e, o, cs, sn);
+#pragma unroll
+                    for (int l = 0; l < 4; ++l) x[2 * l] = e[l], x[2 * l + 1] = o[l], y[2 * l] = e[l + 4], y[2 * l + 1] = o[l + 4];
+                }
+                store8(dst + i * a.qo.head + c0, a.qo.vec, x);
+                store8(dst + i * a.qo.head + c1, a.qo.vec, y);
             }
-            store8(dst + c0, a.qo.vec, x);
-            store8(dst + c1, a.qo.vec, y);
         }
     }
 }
 
 // Blocks with the first kv_blocks indexes in y store keys and values, the others turn queries.  (Where the queries' pairs do not come in
 // eights, kPaired is false and every block does both, a head of a token like another.)
+// (four blocks per multiprocessor: measured against three and five, with one, two or four heads' loads ahead)
 template <typename T, bool kPaired>
-__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(kThreads, 4) append_kernel(const AppendArgs a)
 {
     __shared__ Place at[kMaxTokens];
     const int first = (int)blockIdx.x * a.tokens_per_block;
@@ -282,36 +317,51 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
     const int lanes = a.c.dim / 8, shift = 31 - __clz(lanes), per_pass = kThreads / lanes;
     const int q_heads = kPaired ? 0 : a.q_heads, heads = q_heads + 2 * a.c.kv_heads, units = mine * heads;
     const int lane  = (int)threadIdx.x & (lanes - 1), c0 = lane * 8;
+    struct Unit {
+        Eight<T> x, pair;
+        const T *row;
+        int t, h;                                      // t < 0: none
+    };
+    auto fetch = [&](int u) {
+        Unit f;
+        f.t = u < units ? over(u, a.by_heads) : -1;
+        if (f.t >= 0) {
+            f.h = u - f.t * heads;
+            const bool is_q = f.h < q_heads, is_k = !is_q && f.h < q_heads + a.c.kv_heads;
+            const Rows &r   = is_q ? a.q : (is_k ? a.k : a.v);
+            f.row = reinterpret_cast<const T *>(r.p) + (int64_t)(first + f.t) * r.ld + (int64_t)(is_q ? f.h : f.h - q_heads - (is_k ? 0 : a.c.kv_heads)) * r.head;
+            f.x.load(f.row + c0, r.vec);
+            if ((is_q || is_k) && !a.interleaved && c0 < a.rot && whole_chunk_pairs(a.rot)) f.pair.load(f.row + pair_of(c0, a.rot), r.vec);
+        }
+        return f;
+    };
     // every warp makes the same number of trips: the shuffles and the barrier below take whole warps
-    for (int u0 = (int)blockIdx.y * per_pass; u0 < units; u0 += (kPaired ? a.kv_blocks : (int)gridDim.y) * per_pass) {
-        const int  u   = u0 + ((int)threadIdx.x >> shift);
-        const bool on  = u < units;
-        const int  t   = on ? over(u, a.by_heads) : 0, h = on ? u - t * heads : 0;
-        const Place p  = at[t];
-        const bool is_q = h < q_heads, is_k = !is_q && h < q_heads + a.c.kv_heads;
-        const int  hh   = is_q ? h : (is_k ? h - q_heads : h - q_heads - a.c.kv_heads);
-        const Rows &r   = is_q ? a.q : (is_k ? a.k : a.v);
-        const T *row    = reinterpret_cast<const T *>(r.p) + (int64_t)(first + t) * r.ld + (int64_t)hh * r.head;
+    const int step = (kPaired ? a.kv_blocks : (int)gridDim.y) * per_pass, mine_at = (int)threadIdx.x >> shift;
+    Unit next = fetch((int)blockIdx.y * per_pass + mine_at);
+    for (int u0 = (int)blockIdx.y * per_pass; u0 < units; u0 += step) {
+        const Unit f = next;
+        if (kPaired) next = fetch(u0 + step + mine_at);        // (q rotated in place: nothing of it is read ahead of a write)
+        const bool on  = f.t >= 0, is_q = on && f.h < q_heads, is_k = on && !is_q && f.h < q_heads + a.c.kv_heads;
+        const Place p  = at[on ? f.t : 0];
         float x[8] = {};
         if (on) {
-            load8(row + c0, r.vec, x);
+            f.x.get(x);
             if ((is_q || is_k) && a.table && p.pos >= 0) {
-                if (p.pos < a.table_rows) rotate8(x, row, r.vec, c0, a.rot, a.interleaved, a.table + (int64_t)p.pos * (a.rot >> 1));
+                if (p.pos < a.table_rows) rotate8(x, f.pair, f.row, c0, a.rot, a.interleaved, a.table + (int64_t)p.pos * (a.rot >> 1));
                 else if (lane == 0) kv_record(a.status, p.seq, p.pos);
             }
         }
         __syncwarp();
-        if (is_q && on)
-            store8(reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + t) * a.qo.ld + (int64_t)hh * a.qo.head + c0, a.qo.vec, x);
+        if (is_q) store8(reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + f.t) * a.qo.ld + (int64_t)f.h * a.qo.head + c0, a.qo.vec, x);
         uint32_t word;
         const uint32_t codes = quantise8(x, word);
         if (on && !is_q && p.page >= 0 && !(a.table && p.pos >= a.table_rows)) {
-            const int slot = p.pos & ((1 << a.c.page_shift) - 1), ps = 1 << a.c.page_shift;
+            const int hh = f.h - q_heads - (is_k ? 0 : a.c.kv_heads), ps = 1 << a.c.page_shift, row = (is_k ? 0 : ps) + (p.pos & (ps - 1));
             unsigned char *base = a.c.pages + p.page * a.c.page_bytes + hh * a.c.head_bytes;
-            *reinterpret_cast<uint32_t *>(base + ((is_k ? 0 : ps) + slot) * (a.c.dim / 2) + lane * 4) = codes;
-            if ((lane & 7) == 0)
-                reinterpret_cast<uint32_t *>(base + ps * a.c.dim)[((is_k ? 0 : ps) + slot) * a.c.groups + (lane >> 3)] = word;
+            *reinterpret_cast<uint32_t *>(base + row * (a.c.dim / 2) + lane * 4) = codes;
+            if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(base + ps * a.c.dim)[row * a.c.groups + (lane >> 3)] = word;
         }
+        if (!kPaired) next = fetch(u0 + step + mine_at);
     }
 }
 
@@ -398,17 +448,15 @@ bool make_rows(Rows *r, const void *p, int64_t ld, int64_t head, int dtype)
 // 2^32 / d rounded up (0 stands for 1): n * that / 2^32 is n / d while n d < 2^32
 uint32_t reciprocal(int d) { return d <= 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
 
-// Blocks of append and read: few tokens take one head per thread group, many take up to eight tokens per block.
+// Blocks of append and read.  Finding a block's tokens takes two or three trips to memory, so a block takes as many tokens as still leave
+// every multiprocessor eight blocks (sixteen at most), and a thread about four units of them where there are many.
 dim3 token_grid(int tokens, int heads, int lanes, int num_sms, int *tokens_per_block)
 {
-    const int per_pass = kThreads / lanes;
-    const int64_t passes = ((int64_t)tokens * heads + per_pass - 1) / per_pass;
     int tpb = 1;
-    while (tpb < kMaxTokens && passes / tpb > 16ll * num_sms) tpb *= 2;
+    while (tpb < kMaxTokens && tokens / (2 * tpb) >= 8 * num_sms) tpb *= 2;
     *tokens_per_block = tpb;
-    const int units = tpb * heads;
-    const int split = passes > 64ll * num_sms ? 1 : (units + per_pass - 1) / per_pass;
-    return dim3((unsigned)((tokens + tpb - 1) / tpb), (unsigned)split, 1);
+    const int per_pass = kThreads / lanes, passes = (tpb * heads + per_pass - 1) / per_pass, deep = tpb >= 4 ? 4 : 1;
+    return dim3((unsigned)((tokens + tpb - 1) / tpb), (unsigned)((passes + deep - 1) / deep), 1);
 }
 
 }  // namespace
