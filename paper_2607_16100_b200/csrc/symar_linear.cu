@@ -6,11 +6,10 @@
 // weights; with many it is an ordinary product of 128 x 256 tiles.  A block is one producer (the copy engine
 // fills a ring of 64-wide slices of both operands), one thread that issues the products, and four warps that take
 // finished accumulators out of tensor memory, where the next tile is already being summed in the other half.
-#include <cuda.h>
-
 #include <type_traits>
 
 #include "symar_ops.h"
+#include "symar_tc.cuh"
 
 namespace symar {
 namespace {
@@ -29,103 +28,7 @@ struct LinearArgs {
 
 constexpr int kRows = 128, kSlice = 64;    // channels of a tile; k of a stage: 128 bytes, one swizzled row
 constexpr int kMaxSplit = 8;
-constexpr uint64_t kWaitNs = 4000000000ull;
 
-// ---- instructions -----------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-__device__ __forceinline__ uint64_t now_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-// A thread's wait; false once it has lasted four seconds or another role has given up.
-__device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed)
-{
-    const uint64_t t0 = now_ns();
-    for (;;) {
-        for (int i = 0; i < 256; ++i)
-            if (bar_try(bar, parity)) return true;
-        if (*failed || now_ns() - t0 > kWaitNs) {
-            *failed = 1;
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed)
-{
-    bool ok = false;
-#pragma unroll 1
-    for (int i = 0; i < 64 && !ok; ++i) ok = bar_try(bar, parity);
-    if (!ok) ok = bar_wait_long(bar, parity, failed);
-    return ok;
-}
-// The same for a whole warp: all its lanes go on, or none.  One lane polls.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *failed)
-{
-    int ok = 0;
-    if ((threadIdx.x & 31) == 0) ok = bar_wait(bar, parity, failed);
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
-}
-// one lane of a converged warp
-__device__ __forceinline__ bool elected()
-{
-    uint32_t one;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
-    return one != 0;
-}
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
-// shared-memory operand: rows of 128 bytes, swizzled in blocks of eight
-__device__ __forceinline__ uint64_t operand(uint32_t addr)
-{
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t how, uint32_t add)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(acc),
-                 "l"(a), "l"(b), "r"(how), "r"(add) : "memory");
-}
-__device__ __forceinline__ void commit(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// sixteen columns of this warp's 32 lanes; the wait is the caller's
-__device__ __forceinline__ void acc_load16(uint32_t addr, float *v)
-{
-    uint32_t r[16];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -158,8 +61,6 @@ __device__ __forceinline__ void activate4(float (&y)[4], int act)
         for (int i = 0; i < 4; ++i) y[i] = gate(y[i], y[i]);
     }
 }
-__device__ __forceinline__ float as_f32(float v) { return v; }
-__device__ __forceinline__ float as_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void load4(const float *p, float (&r)[4])
@@ -515,7 +416,7 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                 for (int i = 0; i < kOwn; ++i) sum[i] = 0.0f;
                 for (int ks = k_lo; ks < k_hi; ks += kChunk, ++turn) {
                     const uint32_t buf = turn & 1;
-                    if (!warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    (void)warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
                     tc_after();
 #pragma unroll
                     for (int c0 = 0; c0 < kOwn; c0 += 16) {
@@ -550,7 +451,7 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                 Four<O> res[S::kStep / 8];
                 if (a.split == 1) residuals_of<O>(a, c, g, m0, min(S::kStep, tokens), ew, res);
                 if (parts) {
-                    if (!warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed)) goto done;
+                    (void)warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
                     tc_after();
                 }
 #pragma unroll 1

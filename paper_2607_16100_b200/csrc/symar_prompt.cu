@@ -1,0 +1,472 @@
+// Attention of many query rows (prompts, pieces of prompts) over the paged 4-bit cache, on the fifth generation's tensor cores.
+//
+// A block has 128 query rows (tokens and the heads of one key/value head's share) and walks over the cached tokens 64 at a time.  Eight
+// warps bring the codes in and write them out again as what a tensor-core operand is: whole numbers n - z in bf16, exact, keys as rows of
+// channels, values transposed.  The scales stay apart, so that nothing is rounded that the definition does not round but the probabilities:
+// every group of 64 channels has a product of its own, S_g = Q_g N_g^T, whose columns the softmax multiplies by the keys' scales and adds;
+// and a set of probabilities of its own, P_g = P s_g, for O_g = P_g N_g.  Two groups of four warps take the tiles in turn, each with its
+// scores, its running maximum and sum and its output, a thread to a row, so that one group's exponentials run beside the other's products;
+// the two halves are joined at the end.  A channel's place in an operand is the one that its code comes out of the register at: the
+// queries are permuted alike, the output back.
+// Bound: 16 exponentials a cycle and 4096 products a cycle meet at 512 cycles per tile and multiprocessor for D = 128; the softmax's
+// other instructions take about 700.
+#include "symar_attention.cuh"
+
+namespace symar {
+namespace {
+
+constexpr int kRows = 128, kKeys = 64, kStages = 3, kRaw = 3;
+constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
+constexpr int kThreads = 32 * (8 + kWorkers + 1);      // two softmax groups of four warps, the workers, one warp for the products
+
+template <int D>
+struct Shape {
+    static constexpr int NG = D / 64, kRow = D / 2;
+    static constexpr int kSlabQ = kRows * 128, kSlabK = kKeys * 128;      // 64 channels (or keys) of every row: 128 bytes, swizzled
+    static constexpr int kStage = 2 * NG * kSlabK;
+    static constexpr int kScales = 2 * NG * kKeys * 4;
+    static constexpr int kRawChunk = 16 * (kRow + NG * 4);
+    static constexpr int kQ = 0, kKV = kQ + NG * kSlabQ, kP = kKV + kStages * kStage, kSc = kP + 2 * NG * kSlabQ, kRawAt = kSc + kStages * kScales;
+    static constexpr int kBytes = kRawAt + kWorkers * kRaw * kRawChunk + 1024;
+};
+
+__device__ __forceinline__ void matrices_out(uint32_t addr, const uint32_t (&r)[4])
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void acc_store16(uint32_t addr, const float *v)
+{
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void acc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void to_engine() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
+{
+    using S = Shape<D>;
+    constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 6];
+    __shared__ int64_t warp_sum[kThreads / 32];
+    __shared__ float   row_m[2][kRows], row_l[2][kRows];
+    __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed, at_seq, at_item;
+    unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    const uint32_t base = smem_addr(smem);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // ---- this block's item ----
+    const int each = (a.b.seqs + kThreads - 1) / kThreads;
+    const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
+    auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kRows - 1) / kRows) * a.c.kv_heads; };
+    int64_t own = 0;
+#pragma unroll 1
+    for (int b = s0; b < s1; ++b) own += items_of(sequence(a, b));
+    int64_t incl = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+    }
+    if (lane == 31) warp_sum[warp] = incl;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(full + 8 * i, kWorkers);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(s_full + 8 * i, 1);
+            bar_init(p_full + 8 * i, 4);
+            bar_init(o_done + 8 * i, 1);
+        }
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll 1
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w == warp) incl += total;
+        total += warp_sum[w];
+    }
+    if ((int64_t)blockIdx.x >= total) return;
+    if ((int64_t)blockIdx.x >= incl - own && (int64_t)blockIdx.x < incl) {
+        int64_t flat = incl - own;
+#pragma unroll 1
+        for (int b = s0; b < s1; ++b) {
+            const int64_t n = items_of(sequence(a, b));
+            if ((int64_t)blockIdx.x < flat + n) {
+                at_seq  = b;
+                at_item = (int)((int64_t)blockIdx.x - flat);
+                break;
+            }
+            flat += n;
+        }
+    }
+    if (warp == 16) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_at)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_at;
+    const int  seq = at_seq;
+    const Seq  s   = sequence(a, seq);
+    const int  rows = s.fresh * a.share, blocks = (rows + kRows - 1) / kRows;
+    const int  block = blocks - 1 - at_item / a.c.kv_heads, head = at_item % a.c.kv_heads;      // (the longest first)
+    const int64_t most = a.b.table_ld << a.c.page_shift;
+    const int  first_tok = by_share(a, block * kRows), last_tok = min(by_share(a, block * kRows + kRows - 1), s.fresh - 1);
+    const int  end = (int)min((int64_t)(s.len - s.fresh + last_tok + 1), most);
+    const int  lo  = a.window > 0 ? max(s.len - s.fresh + first_tok + 1 - a.window, 0) & ~15 : 0;
+    const int  n   = end > lo ? (end - lo + kKeys - 1) / kKeys : 0;
+    if (tid == 0 && s.len > most) kv_record(a.status, seq, (int)most);
+
+    // ---- the queries: a row per thread, group (or half of the one group) w per four warps; times 64 or 4, which the codes lack ----
+    if (warp < 8) {
+        const int r = tid & (kRows - 1), w = warp >> 2, row = block * kRows + r;
+        const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
+        const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
+#pragma unroll
+        for (int cc = 0; cc < (NG == 2 ? 2 : 1); ++cc) {
+            const int gr = NG == 2 ? w : 0, c = NG == 2 ? cc : w;
+            uint4 v[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const __nv_bfloat16 *p = src + gr * 64 + c * 32 + t * 8;
+                v[t] = make_uint4(0, 0, 0, 0);
+                if (row < rows) {
+                    if (a.q_vec) {
+                        v[t] = *reinterpret_cast<const uint4 *>(p);
+                    } else {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+                        v[t] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {              // sixteen bytes: channels 8 t + i and 8 t + i + 4
+                uint32_t x[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    x[t] = mul2(__byte_perm(i < 2 ? v[t].x : v[t].y, i < 2 ? v[t].z : v[t].w, i & 1 ? 0x7632 : 0x5410), i & 1 ? 0x40804080u : 0x42804280u);
+                *reinterpret_cast<uint4 *>(smem + S::kQ + gr * S::kSlabQ + r * 128 + (((4 * c + i) ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+        }
+        to_engine();
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+
+    if (warp >= 8 && warp < 16) {
+        // ---- codes to operands ----
+        const int dw = warp - 8, c = dw & 3, side = dw >> 2, ps = 1 << a.c.page_shift, g = lane >> 2, t = lane & 3;
+        unsigned char *raw = smem + S::kRawAt + dw * kRaw * S::kRawChunk;
+        const uint32_t raw_addr = smem_addr(raw);
+        int pages = -1;
+        uint32_t have = 0;                              // bit i: the chunk fetched i fetches ago has a page
+        auto fetch = [&](int j) {
+            if (j < n) {
+                if ((j & 31) == 0) {
+                    const int tok = lo + (j + lane) * kKeys + c * 16;
+                    pages = j + lane < n && tok < end ? kv_page_of(a.c, a.b, a.status, seq, tok) : -1;
+                }
+                const int page = __shfl_sync(0xffffffffu, pages, j & 31), slot = (lo + j * kKeys + c * 16) & (ps - 1);
+                const bool on = page >= 0;
+                const unsigned char *head_at = a.c.pages + (int64_t)(on ? page : 0) * a.c.page_bytes + (int64_t)head * a.c.head_bytes;
+                const unsigned char *src = head_at + (side * ps + slot) * kRow + lane * 16;
+                const uint32_t dst = raw_addr + (j % kRaw) * S::kRawChunk;
+#pragma unroll
+                for (int u0 = 0; u0 < 16 * kUnits; u0 += 32) {
+                    const int tok = (u0 + lane) / kUnits, u = lane % kUnits, turn = D == 64 ? tok >> 2 & 1 : tok >> 1 & 3;
+                    copy16(dst + tok * kRow + ((u ^ turn) << 4), src + u0 * 16, on);
+                }
+                if (lane < 4 * NG) copy16(dst + 16 * kRow + lane * 16, head_at + ps * D + (side * ps + slot) * NG * 4 + lane * 16, on);
+                have = have << 1 | (uint32_t)on;
+            }
+            copies_commit();
+        };
+#pragma unroll 1
+        for (int j = 0; j < kRaw - 1; ++j) fetch(j);
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+            copies_wait<kRaw - 2>();
+            __syncwarp();
+            fetch(j + kRaw - 1);
+            const bool on = have >> min(kRaw - 1, n - 1 - j) & 1;
+            const int st = j % kStages, tok0 = lo + j * kKeys + c * 16;
+            if (j >= kStages && !warp_wait(empty + 8 * st, (j / kStages - 1) & 1, &failed)) goto done;
+            const uint32_t from = raw_addr + (j % kRaw) * S::kRawChunk;
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(raw + (j % kRaw) * S::kRawChunk + 16 * kRow);
+            const uint32_t to = base + S::kKV + st * S::kStage + side * NG * S::kSlabK;
+            const int mt = (lane >> 4) * 8 + (lane & 7), mc = lane >> 3 & 1, turn = D == 64 ? mt >> 2 & 1 : mt >> 1 & 3;
+            if (lane < 16) {
+                // beyond the sequence's end a page holds anything: values from there count for nothing
+                float *scales = reinterpret_cast<float *>(smem + S::kSc + st * S::kScales) + side * NG * kKeys + c * 16 + lane;
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    const float f = __uint_as_float(words[lane * NG + gr]);
+                    scales[gr * kKeys] = side ? (tok0 + lane < s.len ? f : 0.0f) : f * a.scale_log2;
+                }
+            }
+            if (side == 0 && lane == 0) bad[st][c] = !on && tok0 < end;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                uint32_t r[4], z0, z1, y0, y1;
+                if (side == 0) {
+                    matrices(r, from + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
+                    const uint32_t w0 = words[g * NG + gr], w1 = words[(g + 8) * NG + gr];
+                    z0 = zeros_of(w0, w0), z1 = zeros_of(w1, w1);
+                } else {
+                    matrices_t(r, from + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
+                    z0 = zeros_of(words[2 * t * NG + gr], words[(2 * t + 1) * NG + gr]);
+                    z1 = zeros_of(words[(2 * t + 8) * NG + gr], words[(2 * t + 9) * NG + gr]);
+                }
+                y0 = mul2(z0, kSixteen), y1 = mul2(z1, kSixteen);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t v[4] = {fma2(codes(r[0], i), kTwo127, i & 1 ? y0 : z0), fma2(codes(r[1], i), kTwo127, i & 1 ? y0 : z0),
+                                           fma2(codes(r[2], i), kTwo127, i & 1 ? y1 : z1), fma2(codes(r[3], i), kTwo127, i & 1 ? y1 : z1)};
+                    // four 8 x 8 matrices: keys' rows are tokens, their sixteen bytes channels; values' rows are channels 32 c + 4 g + i (at row
+                    // 32 c + 8 i + g), their sixteen bytes eight tokens
+                    const int row = side == 0 ? c * 16 + mt : mc * 32 + i * 8 + (lane & 7);
+                    const int piece = side == 0 ? 4 * mc + i : c * 2 + (lane >> 4);
+                    matrices_out(to + gr * S::kSlabK + row * 128 + ((piece ^ (row & 7)) << 4), v);
+                }
+            }
+            to_engine();
+            __syncwarp();
+            if (lane == 0) bar_arrive(full + 8 * st);
+        }
+        copies_wait<0>();
+    } else if (warp == 16 && elected()) {
+        // ---- products ----
+        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
+        auto scores = [&](int i) {
+            const int st = i % kStages;
+            if (!bar_wait(full + 8 * st, (i / kStages) & 1, &failed)) return false;
+            tc_after();
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const uint64_t q = operand(base + S::kQ + gr * S::kSlabQ), k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) product(tmem + (i & 1) * 128 + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
+            }
+            commit(s_full + 8 * (i & 1));
+            return true;
+        };
+        for (int i = 0; i < 2 && i < n; ++i)
+            if (!scores(i)) goto done;
+        for (int i = 0; i < n; ++i) {
+            const int st = i % kStages, w = i & 1;
+            if (!bar_wait(p_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
+            tc_after();
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const uint64_t p = operand(base + S::kP + (w * NG + gr) * S::kSlabQ), v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) product(tmem + 256 + w * 128 + gr * 64, p + 2 * x, v + 2 * x, kHow, i >= 2 || x > 0);
+            }
+            commit(o_done + 8 * w);
+            commit(empty + 8 * st);
+            if (i + 2 < n && !scores(i + 2)) goto done;
+        }
+    } else if (warp < 8) {
+        // ---- softmax: a row per thread ----
+        const int w = warp >> 2, r = tid & (kRows - 1), row = block * kRows + r;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        int hi = 0x7fffffff, low = 0;                   // a row of padding masks nothing
+        if (row < rows) {
+            hi  = s.len - s.fresh + by_share(a, row) + 1;
+            low = a.window > 0 ? max(hi - a.window, 0) : 0;
+        }
+        const int least_hi = s.len - s.fresh + first_tok + 1, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
+        unsigned char *p_at = smem + S::kP + w * NG * S::kSlabQ + r * 128;
+        float m = kNothing, l = 0.0f;
+#pragma unroll 1
+        for (int i = w; i < n; i += 2) {
+            const int st = i % kStages, tok0 = lo + i * kKeys;
+            const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales), *vs = ks + NG * kKeys;
+            if (!warp_wait(s_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
+            tc_after();
+            float sc[kKeys];
+#pragma unroll
+            for (int c0 = 0; c0 < kKeys; c0 += 16) {
+                acc_load16(tmem + lanes + w * 128 + c0, sc + c0);
+#pragma unroll
+                for (int x = 0; x < 16; x += 4) {
+                    const float4 k = *reinterpret_cast<const float4 *>(ks + c0 + x);
+                    sc[c0 + x] *= k.x; sc[c0 + x + 1] *= k.y; sc[c0 + x + 2] *= k.z; sc[c0 + x + 3] *= k.w;
+                }
+                if (NG == 2) {
+                    float more[16];
+                    acc_load16(tmem + lanes + w * 128 + 64 + c0, more);
+#pragma unroll
+                    for (int x = 0; x < 16; x += 4) {
+                        const float4 k = *reinterpret_cast<const float4 *>(ks + kKeys + c0 + x);
+                        sc[c0 + x]     = __fmaf_rn(more[x], k.x, sc[c0 + x]);
+                        sc[c0 + x + 1] = __fmaf_rn(more[x + 1], k.y, sc[c0 + x + 1]);
+                        sc[c0 + x + 2] = __fmaf_rn(more[x + 2], k.z, sc[c0 + x + 2]);
+                        sc[c0 + x + 3] = __fmaf_rn(more[x + 3], k.w, sc[c0 + x + 3]);
+                    }
+                }
+            }
+            const uint32_t gone = *reinterpret_cast<const uint32_t *>(bad[st]);
+            if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
+#pragma unroll
+                for (int x = 0; x < kKeys; ++x)
+                    if (tok0 + x >= hi || tok0 + x < low || tok0 + x >= end || (gone >> 8 * (x >> 4) & 1u)) sc[x] = -INFINITY;
+            }
+            float top = sc[0];
+#pragma unroll
+            for (int x = 1; x < kKeys; ++x) top = fmaxf(top, sc[x]);
+            // the last product with this group's probabilities is over: they may be overwritten, and its output rescaled
+            if (i >= 2 && !warp_wait(o_done + 8 * w, ((i >> 1) - 1) & 1, &failed)) goto done;
+            // (the maximum in use may lie up to 2^8 below the true one)
+            if (__any_sync(0xffffffffu, top > m + 8.0f)) {
+                const float now = fmaxf(top, m), keep = power2(m - now);
+                m = now;
+                l *= keep;
+                if (i >= 2) {
+                    tc_after();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < NG * 64; c0 += 16) {
+                        float v[16];
+                        acc_load16(tmem + lanes + 256 + w * 128 + c0, v);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) v[x] *= keep;
+                        acc_store16(tmem + lanes + 256 + w * 128 + c0, v);
+                    }
+                    acc_stored();
+                }
+            }
+            float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x0 = 0; x0 < kKeys; x0 += 8) {
+#pragma unroll
+                for (int x = x0; x < x0 + 8; ++x) {
+                    sc[x] = power2(sc[x] - m);
+                    sums[x & 3] += sc[x];
+                }
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    const float4 u = *reinterpret_cast<const float4 *>(vs + gr * kKeys + x0), v = *reinterpret_cast<const float4 *>(vs + gr * kKeys + x0 + 4);
+                    *reinterpret_cast<uint4 *>(p_at + gr * S::kSlabQ + (((x0 >> 3) ^ (r & 7)) << 4)) =
+                        make_uint4(pack_bf16(sc[x0] * u.x, sc[x0 + 1] * u.y), pack_bf16(sc[x0 + 2] * u.z, sc[x0 + 3] * u.w),
+                                   pack_bf16(sc[x0 + 4] * v.x, sc[x0 + 5] * v.y), pack_bf16(sc[x0 + 6] * v.z, sc[x0 + 7] * v.w));
+                }
+            }
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            to_engine();
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(p_full + 8 * w);
+        }
+        row_m[w][r] = m;
+        row_l[w][r] = l;
+        // this group's last product (the other's is waited for by the other, and the block's barrier below by both)
+        const int count = (n + 1 - w) / 2;
+        if (count > 0 && !warp_wait(o_done + 8 * w, (count - 1) & 1, &failed)) goto done;
+    }
+done:
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (failed) {
+        // copies and products may still be in flight: give them time to end before the memory is let go
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (tid == 0 && atomicCAS(a.status + 3, 0, 1) == 0) atomicExch(a.status, SYMAR_ERR_TIMEOUT);
+    } else if (warp < 8) {
+        // ---- the two groups' outputs joined: group w of the channels (or half of the one group) per four warps ----
+        const int w = warp >> 2, r = tid & (kRows - 1), row = block * kRows + r;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        const float m0 = row_m[0][r], m1 = row_m[1][r], top = fmaxf(m0, m1), f0 = power2(m0 - top), f1 = power2(m1 - top);
+        const float sum = n > 0 ? __fmaf_rn(row_l[1][r], f1, row_l[0][r] * f0) : 0.0f;
+        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+        const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
+        __nv_bfloat16 *out = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head;
+#pragma unroll 1
+        for (int cc = 0; cc < (NG == 2 ? 2 : 1); ++cc) {
+            const int at = (NG == 2 ? w * 64 : 0) + (NG == 2 ? cc : w) * 32;
+            float v[32];
+#pragma unroll
+            for (int x = 0; x < 32; ++x) v[x] = 0.0f;
+#pragma unroll
+            for (int c0 = 0; c0 < 32; c0 += 16) {
+                float u[16];
+                if (n > 0) {
+                    acc_load16(tmem + lanes + 256 + at + c0, u);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) v[c0 + x] = u[x] * f0;
+                }
+                if (n > 1) {
+                    acc_load16(tmem + lanes + 256 + 128 + at + c0, u);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) v[c0 + x] = __fmaf_rn(u[x], f1, v[c0 + x]);
+                }
+            }
+            if (row < rows) {
+                // column 8 i + g is channel 4 g + i
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const uint32_t x = pack_bf16(64.0f * v[g] * inv, 4.0f * v[8 + g] * inv), y = pack_bf16(64.0f * v[16 + g] * inv, 4.0f * v[24 + g] * inv);
+                    __nv_bfloat16 *p = out + at + 4 * g;
+                    if (a.out_vec) {
+                        *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
+                    } else {
+                        uint16_t *h = reinterpret_cast<uint16_t *>(p);
+                        h[0] = (uint16_t)x; h[1] = (uint16_t)(x >> 16); h[2] = (uint16_t)y; h[3] = (uint16_t)(y >> 16);
+                    }
+                }
+            }
+        }
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// items that the call has at most: a block each (blocks beyond the last item leave at once)
+int64_t items_at_most(const AttnArgs &a)
+{
+    return ((int64_t)a.b.tokens * a.share / kRows + (a.b.seqs < a.b.tokens ? a.b.seqs : a.b.tokens)) * a.c.kv_heads;
+}
+
+}  // namespace
+
+bool prompt_attention_takes(const AttnArgs &a, int num_sms)
+{
+    if (a.c.dim > 128 || items_at_most(a) > 0x3fffffff) return false;
+    const int64_t rows = (int64_t)a.b.tokens * a.share;                // of one key/value head
+    return rows >= 64ll * a.b.seqs && rows / kRows * a.c.kv_heads >= num_sms / 2;
+}
+
+cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream)
+{
+    const unsigned blocks = (unsigned)items_at_most(a);
+    static std::atomic<uint64_t> allowed64{0}, allowed128{0};
+    if (a.c.dim == 64) {
+        const cudaError_t e = allow_shared((const void *)prompt_kernel<64>, Shape<64>::kBytes, device, allowed64);
+        if (e != cudaSuccess) return e;
+        prompt_kernel<64><<<blocks, kThreads, Shape<64>::kBytes, stream>>>(a);
+    } else {
+        const cudaError_t e = allow_shared((const void *)prompt_kernel<128>, Shape<128>::kBytes, device, allowed128);
+        if (e != cudaSuccess) return e;
+        prompt_kernel<128><<<blocks, kThreads, Shape<128>::kBytes, stream>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace symar

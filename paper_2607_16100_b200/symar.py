@@ -674,7 +674,8 @@ class KVContext:
     def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
         """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
         heads, dim = cache.kv_heads, cache.head_dim
-        k, v = cache.pages.new_empty((2, tokens, heads, dim), dtype=dtype or (_T or _torch()).bfloat16).unbind(0)
+        dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
+        k, v = cache.pages.new_empty(shape, dtype=dtype), cache.pages.new_empty(shape, dtype=dtype)
         args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(k, "symar_kv_read"))
         batch.args.tokens = tokens
         _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.ref, byref(args))
