@@ -44,6 +44,52 @@ __device__ __forceinline__ void acc_store16(uint32_t addr, const float *v)
                  "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
+// sixteen columns, waited for later (acc_loaded)
+__device__ __forceinline__ void acc_ask16(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
+template <int N> __device__ __forceinline__ void acc_loaded(uint32_t (&r)[N])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));         // not used before the wait
+}
+// two binary32 numbers at a time
+__device__ __forceinline__ uint64_t two(float a, float b)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void apart(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint32_t pack_two(uint64_t v)
+{
+    float a, b;
+    apart(v, a, b);
+    return pack_bf16(a, b);
+}
 __device__ __forceinline__ void acc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void to_engine() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -53,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     using S = Shape<D>;
     constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 6];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 8];
     __shared__ int64_t warp_sum[kThreads / 32];
     __shared__ float   row_m[2][kRows], row_l[2][kRows];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
@@ -61,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- this block's item ----
@@ -87,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_init(s_full + 8 * i, 1);
             bar_init(p_full + 8 * i, 4);
             bar_init(o_done + 8 * i, 1);
+            bar_init(s_read + 8 * i, 4);
         }
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -268,7 +315,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         for (int i = 0; i < 2 && i < n; ++i)
             if (!scores(i)) goto done;
         for (int i = 0; i < n; ++i) {
+            // (the next scores of a group while it takes its exponentials)
             const int st = i % kStages, w = i & 1;
+            if (i + 2 < n) {
+                if (!bar_wait(s_read + 8 * w, (i >> 1) & 1, &failed) || !scores(i + 2)) goto done;
+            }
             if (!bar_wait(p_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
             tc_after();
 #pragma unroll
@@ -279,7 +330,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             }
             commit(o_done + 8 * w);
             commit(empty + 8 * st);
-            if (i + 2 < n && !scores(i + 2)) goto done;
         }
     } else if (warp < 8) {
         // ---- softmax: a row per thread ----
@@ -299,37 +349,50 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales), *vs = ks + NG * kKeys;
             if (!warp_wait(s_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
             tc_after();
-            float sc[kKeys];
+            uint64_t sc[kKeys / 2];                     // two neighbouring columns each
 #pragma unroll
             for (int c0 = 0; c0 < kKeys; c0 += 16) {
-                acc_load16(tmem + lanes + w * 128 + c0, sc + c0);
+                uint32_t x[16 * NG];
+                acc_ask16(tmem + lanes + w * 128 + c0, *reinterpret_cast<uint32_t(*)[16]>(x));
+                if (NG == 2) acc_ask16(tmem + lanes + w * 128 + 64 + c0, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * (NG - 1)));
+                acc_loaded(x);
 #pragma unroll
-                for (int x = 0; x < 16; x += 4) {
-                    const float4 k = *reinterpret_cast<const float4 *>(ks + c0 + x);
-                    sc[c0 + x] *= k.x; sc[c0 + x + 1] *= k.y; sc[c0 + x + 2] *= k.z; sc[c0 + x + 3] *= k.w;
-                }
-                if (NG == 2) {
-                    float more[16];
-                    acc_load16(tmem + lanes + w * 128 + 64 + c0, more);
-#pragma unroll
-                    for (int x = 0; x < 16; x += 4) {
-                        const float4 k = *reinterpret_cast<const float4 *>(ks + kKeys + c0 + x);
-                        sc[c0 + x]     = __fmaf_rn(more[x], k.x, sc[c0 + x]);
-                        sc[c0 + x + 1] = __fmaf_rn(more[x + 1], k.y, sc[c0 + x + 1]);
-                        sc[c0 + x + 2] = __fmaf_rn(more[x + 2], k.z, sc[c0 + x + 2]);
-                        sc[c0 + x + 3] = __fmaf_rn(more[x + 3], k.w, sc[c0 + x + 3]);
+                for (int y = 0; y < 16; y += 4) {
+                    const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(ks + c0 + y);
+                    uint64_t u = mul_two(two(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), k.x);
+                    uint64_t v = mul_two(two(__uint_as_float(x[y + 2]), __uint_as_float(x[y + 3])), k.y);
+                    if (NG == 2) {
+                        const ulonglong2 k1 = *reinterpret_cast<const ulonglong2 *>(ks + kKeys + c0 + y);
+                        u = fma_two(two(__uint_as_float(x[16 * (NG - 1) + y]), __uint_as_float(x[16 * (NG - 1) + y + 1])), k1.x, u);
+                        v = fma_two(two(__uint_as_float(x[16 * (NG - 1) + y + 2]), __uint_as_float(x[16 * (NG - 1) + y + 3])), k1.y, v);
                     }
+                    sc[(c0 + y) / 2] = u, sc[(c0 + y) / 2 + 1] = v;
                 }
             }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(s_read + 8 * w);
             const uint32_t gone = *reinterpret_cast<const uint32_t *>(bad[st]);
             if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
-                for (int x = 0; x < kKeys; ++x)
-                    if (tok0 + x >= hi || tok0 + x < low || tok0 + x >= end || (gone >> 8 * (x >> 4) & 1u)) sc[x] = -INFINITY;
+                for (int x = 0; x < kKeys; x += 2) {
+                    float u, v;
+                    apart(sc[x / 2], u, v);
+                    const bool lost = gone >> 8 * (x >> 4) & 1u;
+                    if (tok0 + x >= hi || tok0 + x < low || tok0 + x >= end || lost) u = -INFINITY;
+                    if (tok0 + x + 1 >= hi || tok0 + x + 1 < low || tok0 + x + 1 >= end || lost) v = -INFINITY;
+                    sc[x / 2] = two(u, v);
+                }
             }
-            float top = sc[0];
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int x = 1; x < kKeys; ++x) top = fmaxf(top, sc[x]);
+            for (int x = 0; x < kKeys / 2; ++x) {
+                float u, v;
+                apart(sc[x], u, v);
+                tops[2 * (x & 1)]     = fmaxf(tops[2 * (x & 1)], u);
+                tops[2 * (x & 1) + 1] = fmaxf(tops[2 * (x & 1) + 1], v);
+            }
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
             // the last product with this group's probabilities is over: they may be overwritten, and its output rescaled
             if (i >= 2 && !warp_wait(o_done + 8 * w, ((i >> 1) - 1) & 1, &failed)) goto done;
             // (the maximum in use may lie up to 2^8 below the true one)
@@ -350,23 +413,30 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     acc_stored();
                 }
             }
-            float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            uint64_t sums[2] = {0, 0};
+            const uint64_t less = two(-m, -m);
 #pragma unroll
             for (int x0 = 0; x0 < kKeys; x0 += 8) {
+                uint64_t p[4];
 #pragma unroll
-                for (int x = x0; x < x0 + 8; ++x) {
-                    sc[x] = power2(sc[x] - m);
-                    sums[x & 3] += sc[x];
+                for (int x = 0; x < 4; ++x) {
+                    float u, v;
+                    apart(add_two(sc[x0 / 2 + x], less), u, v);
+                    p[x] = two(power2(u), power2(v));
+                    sums[x & 1] = add_two(sums[x & 1], p[x]);
                 }
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    const float4 u = *reinterpret_cast<const float4 *>(vs + gr * kKeys + x0), v = *reinterpret_cast<const float4 *>(vs + gr * kKeys + x0 + 4);
+                    const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(vs + gr * kKeys + x0), v = *reinterpret_cast<const ulonglong2 *>(vs + gr * kKeys + x0 + 4);
                     *reinterpret_cast<uint4 *>(p_at + gr * S::kSlabQ + (((x0 >> 3) ^ (r & 7)) << 4)) =
-                        make_uint4(pack_bf16(sc[x0] * u.x, sc[x0 + 1] * u.y), pack_bf16(sc[x0 + 2] * u.z, sc[x0 + 3] * u.w),
-                                   pack_bf16(sc[x0 + 4] * v.x, sc[x0 + 5] * v.y), pack_bf16(sc[x0 + 6] * v.z, sc[x0 + 7] * v.w));
+                        make_uint4(pack_two(mul_two(p[0], u.x)), pack_two(mul_two(p[1], u.y)), pack_two(mul_two(p[2], v.x)), pack_two(mul_two(p[3], v.y)));
                 }
             }
-            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            {
+                float u, v;
+                apart(add_two(sums[0], sums[1]), u, v);
+                l += u + v;
+            }
             to_engine();
             tc_before();
             __syncwarp();
