@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     using S = Shape<D>;
     constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 8];
+    __shared__ __align__(8) uint64_t bars[3 * kStages + 8];
     __shared__ int64_t warp_sum[kThreads / 32];
     __shared__ float   row_m[2][kRows], row_l[2][kRows];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, s_full = empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
+    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, s_full = v_empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- this block's item ----
@@ -126,8 +126,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     if (lane == 31) warp_sum[warp] = incl;
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
-            bar_init(full + 8 * i, kWorkers);
-            bar_init(empty + 8 * i, 1);
+            bar_init(k_full + 8 * i, kWorkers / 2);
+            bar_init(v_full + 8 * i, kWorkers / 2);
+            bar_init(v_empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
@@ -252,7 +253,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             fetch(j + kRaw - 1);
             const bool on = have >> min(kRaw - 1, n - 1 - j) & 1;
             const int st = j % kStages, tok0 = lo + j * kKeys + c * 16;
-            if (j >= kStages && !warp_wait(empty + 8 * st, (j / kStages - 1) & 1, &failed)) goto done;
+            // a stage's keys are free once the softmax has taken the scores (and the scales) of the tile before it there, its values
+            // once that tile's product with them is over
+            if (j >= kStages) {
+                const int old = j - kStages;
+                if (side == 0 ? !warp_wait(s_read + 8 * (old & 1), (old >> 1) & 1, &failed) : !warp_wait(v_empty + 8 * st, (j / kStages - 1) & 1, &failed))
+                    goto done;
+            }
             const uint32_t from = raw_addr + (j % kRaw) * S::kRawChunk;
             const uint32_t *words = reinterpret_cast<const uint32_t *>(raw + (j % kRaw) * S::kRawChunk + 16 * kRow);
             const uint32_t to = base + S::kKV + st * S::kStage + side * NG * S::kSlabK;
@@ -293,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             }
             to_engine();
             __syncwarp();
-            if (lane == 0) bar_arrive(full + 8 * st);
+            if (lane == 0) bar_arrive((side ? v_full : k_full) + 8 * st);
         }
         copies_wait<0>();
     } else if (warp == 16 && elected()) {
@@ -301,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
         auto scores = [&](int i) {
             const int st = i % kStages;
-            if (!bar_wait(full + 8 * st, (i / kStages) & 1, &failed)) return false;
+            if (!bar_wait(k_full + 8 * st, (i / kStages) & 1, &failed)) return false;
             tc_after();
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
@@ -320,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             if (i + 2 < n) {
                 if (!bar_wait(s_read + 8 * w, (i >> 1) & 1, &failed) || !scores(i + 2)) goto done;
             }
-            if (!bar_wait(p_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
+            if (!bar_wait(v_full + 8 * st, (i / kStages) & 1, &failed) || !bar_wait(p_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
             tc_after();
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                 for (int x = 0; x < 4; ++x) product(tmem + 256 + w * 128 + gr * 64, p + 2 * x, v + 2 * x, kHow, i >= 2 || x > 0);
             }
             commit(o_done + 8 * w);
-            commit(empty + 8 * st);
+            commit(v_empty + 8 * st);
         }
     } else if (warp < 8) {
         // ---- softmax: a row per thread ----
@@ -369,10 +376,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     sc[(c0 + y) / 2] = u, sc[(c0 + y) / 2 + 1] = v;
                 }
             }
+            const uint32_t gone = *reinterpret_cast<const volatile uint32_t *>(bad[st]);
             tc_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(s_read + 8 * w);
-            const uint32_t gone = *reinterpret_cast<const uint32_t *>(bad[st]);
+            if (lane == 0) bar_arrive(s_read + 8 * w);         // scores, scales and `bad` are in registers
             if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
                 for (int x = 0; x < kKeys; x += 2) {
