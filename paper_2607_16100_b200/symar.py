@@ -259,6 +259,22 @@ class SymHeap:
         start = self.base + rank * self.stride + offset - self._keepalive.data_ptr()
         return self._keepalive[start:start + nbytes]
 
+    def view(self, offset: int, shape, dtype):
+        """torch tensor [P, *shape] of every rank's user region from byte ``offset`` on (no copy)."""
+        size = dtype.itemsize
+        n = 1
+        for d in shape:
+            n *= d
+        self._bytes_view(0, offset, n * size)                   # range check
+        if offset % size:
+            raise SymarError(ERR_INVAL, "SymHeap.view: offset")
+        start = self.base + offset - self._keepalive.data_ptr()
+        flat = self._keepalive[start:start + (self.P - 1) * self.stride + n * size].view(dtype)
+        inner = [1] * len(shape)
+        for i in range(len(shape) - 2, -1, -1):
+            inner[i] = inner[i + 1] * shape[i + 1]
+        return flat.as_strided((self.P, *shape), (self.stride // size, *inner))
+
     def write_rank(self, rank: int, offset: int, array) -> None:
         """Copy a host numpy array into rank ``rank``'s user region at ``offset``."""
         import numpy as np
