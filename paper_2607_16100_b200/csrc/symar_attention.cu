@@ -99,8 +99,10 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
         total += warp_sum[w];
     }
     const int64_t per_warp = max(quotient(total + (int64_t)gridDim.x * kWarps - 1, (int64_t)gridDim.x * kWarps), (int64_t)(kMinChunks + kItemCost));
-    // (little work goes to many multiprocessors, four warps each at least, rather than to all warps of a few)
-    const int used = (int)min((int64_t)kWarps, max(quotient(total + per_warp * gridDim.x - 1, per_warp * gridDim.x), (int64_t)4));
+    // (little work goes to many multiprocessors, four warps each at least, rather than to all warps of a few; what one block can do by
+    // itself spares the joining of blocks)
+    const int used = total <= per_warp * kWarps ? kWarps
+                                                : (int)min((int64_t)kWarps, max(quotient(total + per_warp * gridDim.x - 1, per_warp * gridDim.x), (int64_t)4));
     const int64_t per = per_warp * used, block_begin = per * blockIdx.x;
     if (block_begin >= total) return;
     before[tid] = incl - own;

@@ -454,25 +454,27 @@ class KVAttentionArgs(ctypes.Structure):
 
 _T = None               # torch, once a call needed it
 _raw_stream = None      # device index -> handle of torch's current stream
+_device = None          # -> index of the current device
+_CODES = {}             # torch dtype -> symar_dtype_t
 
 
 def _torch():
-    global _T, _raw_stream
+    global _T, _raw_stream, _device
     if _T is None:
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _CODES.update({torch.float32: F32, torch.bfloat16: BF16})
         _T = torch
     return _T
 
 
-def _dtype_code(t, where: str) -> int:
-    torch = _T or _torch()
-    if t.dtype is torch.bfloat16:
-        return BF16
-    if t.dtype is torch.float32:
-        return F32
-    raise SymarError(ERR_UNSUPPORTED, f"{where}: dtype {t.dtype}")
+def _dtype_code(dtype, where: str) -> int:
+    code = _CODES.get(dtype)
+    if code is None:
+        raise SymarError(ERR_UNSUPPORTED, f"{where}: dtype {dtype}")
+    return code
 
 
 def _bad(where: str, what: str):
@@ -481,13 +483,12 @@ def _bad(where: str, what: str):
 
 def _call(fn, where, index: int, stream, *args) -> None:
     """fn(*args, stream) with CUDA device ``index`` current; stream None = torch's current one."""
-    torch = _T or _torch()
     if stream is None:
         stream = _raw_stream(index)
-    if index == torch.cuda.current_device():
+    if index == _device():
         rc = fn(*args, stream)
     else:
-        with torch.cuda.device(index):
+        with _T.cuda.device(index):
             rc = fn(*args, stream)
     if rc != OK:
         raise SymarError(rc, where)
@@ -542,7 +543,7 @@ def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root:
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
     args = LinearArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[0] if wd == 3 else 0, bp, bg, rp, rl,
                       rg, out.data_ptr(), os[-2], os[0] if len(os) == 3 else 0, groups, m, n, k,
-                      BF16 if out.dtype is bf16 else _dtype_code(out, where), act_code, root)
+                      _dtype_code(out.dtype, where), act_code, root)
     _call((_lib or load()).symar_linear, where, index, stream, byref(args))
     return out
 
@@ -650,39 +651,45 @@ class KVContext:
         return code.value, seq.value, position.value
 
     @staticmethod
-    def _rows(where, name, t, shape, dtype, index):
-        st = t.stride()
-        if t.shape != shape or st[2] != 1 or t.dtype is not dtype or t.get_device() != index:
-            _bad(where, f"{name} is {list(shape)} {dtype} on the batch's device with contiguous channels, not "
-                        f"{tuple(t.shape)} {t.dtype} on {t.device}")
-        return t.data_ptr(), st[0], st[1]
+    def _refuse(where, name, t, shape, dtype):
+        _bad(where, f"{name} is {list(shape)} {dtype} on the batch's device with contiguous channels, not {tuple(t.shape)} {t.dtype} on "
+                    f"{t.device}")
 
     def append(self, cache: PagedKV, batch: KVBatch, k, v, *, q=None, q_out=None, rotations=None, interleaved: bool = False,
                stream=None):
         """Rotate q and k, store k and v (``symar_kv_append``); returns the rotated q (``q_out``, new unless given)."""
         where = "symar_kv_append"
-        dtype, index, dim, tokens = k.dtype, batch.index, cache.head_dim, k.shape[0]
+        dtype, index, dim, ks, vs = k.dtype, batch.index, cache.head_dim, k.stride(), v.stride()
+        code = _dtype_code(dtype, where)
+        tokens = k.shape[0]
         shape = (tokens, cache.kv_heads, dim)
-        kp, kl, kh = self._rows(where, "k", k, shape, dtype, index)
-        vp, vl, vh = self._rows(where, "v", v, shape, dtype, index)
-        qp = ql = qh = op = ol = oh = q_heads = rp = rows = rot = 0
+        if k.shape != shape or ks[2] != 1 or k.get_device() != index:
+            self._refuse(where, "k", k, shape, dtype)
+        if v.shape != shape or vs[2] != 1 or v.dtype is not dtype or v.get_device() != index:
+            self._refuse(where, "v", v, shape, dtype)
+        qp = op = q_heads = rp = rows = rot = 0
+        qs = os = (0, 0)
         if q is not None:
-            if q.dim() != 3:
-                _bad(where, "q is [tokens, q_heads, head_dim]")
-            q_heads = q.shape[1]
-            shape = (tokens, q_heads, dim)
-            qp, ql, qh = self._rows(where, "q", q, shape, dtype, index)
+            qs, shape = q.stride(), q.shape
+            q_heads = shape[1]
+            if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or q.dtype is not dtype or q.get_device() != index:
+                self._refuse(where, "q", q, (tokens, q_heads, dim), dtype)
             if q_out is None:
                 q_out = q.new_empty(shape)
-            op, ol, oh = self._rows(where, "q_out", q_out, shape, dtype, index)
+                os = (q_heads * dim, dim)
+            else:
+                os = q_out.stride()
+                if q_out.shape != shape or os[2] != 1 or q_out.dtype is not dtype or q_out.get_device() != index:
+                    self._refuse(where, "q_out", q_out, shape, dtype)
+            qp, op = q.data_ptr(), q_out.data_ptr()
         if rotations is not None:
             rs = rotations.shape
-            if len(rs) != 3 or rs[2] != 2 or rotations.dtype is not (_T or _torch()).float32 or \
-                    not rotations.is_contiguous() or rotations.get_device() != index:
+            if len(rs) != 3 or rs[2] != 2 or rotations.dtype is not _T.float32 or not rotations.is_contiguous() or \
+                    rotations.get_device() != index:
                 _bad(where, "rotations are a contiguous float32 tensor [positions, rot_dim / 2, 2]")
             rp, rows, rot = rotations.data_ptr(), rs[0], 2 * rs[1]
-        args = KVAppendArgs(qp, ql, qh, op, ol, oh, kp, kl, kh, vp, vl, vh, rp, rows, rot, 1 if interleaved else 0, q_heads,
-                            _dtype_code(k, where))
+        args = KVAppendArgs(qp, qs[0], qs[1], op, os[0], os[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], rp, rows, rot,
+                            1 if interleaved else 0, q_heads, code)
         batch.args.tokens = tokens
         _call(self._lib.symar_kv_append, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
         return q_out
@@ -692,7 +699,7 @@ class KVContext:
         heads, dim = cache.kv_heads, cache.head_dim
         dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
         k, v = cache.pages.new_empty(shape, dtype=dtype), cache.pages.new_empty(shape, dtype=dtype)
-        args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(k, "symar_kv_read"))
+        args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(dtype, "symar_kv_read"))
         batch.args.tokens = tokens
         _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.ref, byref(args))
         return k, v
@@ -701,13 +708,15 @@ class KVContext:
         """Attention of the batch's new tokens over the cache (``symar_kv_attention``)."""
         where = "symar_kv_attention"
         shape, dtype, index = q.shape, q.dtype, batch.index
-        if len(shape) != 3 or shape[2] != cache.head_dim:
-            _bad(where, "q is [tokens, q_heads, head_dim]")
+        code, qs = _dtype_code(dtype, where), q.stride()
+        if len(shape) != 3 or shape[2] != cache.head_dim or qs[2] != 1 or q.get_device() != index:
+            _bad(where, f"q is [tokens, q_heads, {cache.head_dim}] on the batch's device with contiguous channels, not {tuple(shape)}")
         if out is None:
             out = q.new_empty(shape)
-        qp, ql, qh = self._rows(where, "q", q, shape, dtype, index)
-        op, ol, oh = self._rows(where, "out", out, shape, dtype, index)
-        args = KVAttentionArgs(qp, ql, qh, op, ol, oh, scale, shape[1], window, _dtype_code(q, where))
+        os = out.stride()
+        if out.shape != shape or os[2] != 1 or out.dtype is not dtype or out.get_device() != index:
+            self._refuse(where, "out", out, shape, dtype)
+        args = KVAttentionArgs(q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], scale, shape[1], window, code)
         batch.args.tokens = shape[0]
         _call(self._lib.symar_kv_attention, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
         return out
