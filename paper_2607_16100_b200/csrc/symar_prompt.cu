@@ -1,21 +1,22 @@
 // Attention of many query rows (prompts, pieces of prompts) over the paged 4-bit cache, on the fifth generation's tensor cores.
 //
-// A block has 128 query rows (tokens and the heads of one key/value head's share) and walks over the cached tokens 64 at a time.  Eight
+// A block has 256 query rows (tokens and the heads of one key/value head's share) and walks over the cached tokens 64 at a time.  Eight
 // warps bring the codes in and write them out again as what a tensor-core operand is: whole numbers n - z in bf16, exact, keys as rows of
 // channels, values transposed.  The scales stay apart, so that nothing is rounded that the definition does not round but the probabilities:
 // every group of 64 channels has a product of its own, S_g = Q_g N_g^T, whose columns the softmax multiplies by the keys' scales and adds;
-// and a set of probabilities of its own, P_g = P s_g, for O_g = P_g N_g.  Two groups of four warps take the tiles in turn, each with its
-// scores, its running maximum and sum and its output, a thread to a row, so that one group's exponentials run beside the other's products;
-// the two halves are joined at the end.  A channel's place in an operand is the one that its code comes out of the register at: the
-// queries are permuted alike, the output back.
-// Bound: 16 exponentials a cycle and 4096 products a cycle meet at 512 cycles per tile and multiprocessor for D = 128; the softmax's
-// other instructions take about 700.
+// and a set of probabilities of its own, P_g = P s_g, for O_g = P_g N_g.  Two groups of four warps have 128 of the rows each, a thread to a
+// row, with their scores, running maxima and sums and outputs; each takes its exponentials beside the other's products, and the next tile's
+// scores are there when a tile's probabilities are written.  A channel's place in an operand is the one that its code comes out of the
+// register at: the queries are permuted alike, the output back.
+// (Values scaled and probabilities in f16 would halve the products' and the softmax's traffic, but f16 has nothing below 2^-24: a row
+// whose likeliest token has a value of 0 loses what the others give it.)
+// Bound: 16 exponentials a cycle and 4096 products a cycle meet at 512 cycles per tile, group and multiprocessor for D = 128.
 #include "symar_attention.cuh"
 
 namespace symar {
 namespace {
 
-constexpr int kRows = 128, kKeys = 64, kStages = 3, kRaw = 3;
+constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kStages = 2, kRaw = 3;
 constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
 constexpr int kThreads = 32 * (8 + kWorkers + 1);      // two softmax groups of four warps, the workers, one warp for the products
 
@@ -26,7 +27,7 @@ struct Shape {
     static constexpr int kStage = 2 * NG * kSlabK;
     static constexpr int kScales = 2 * NG * kKeys * 4;
     static constexpr int kRawChunk = 16 * (kRow + NG * 4);
-    static constexpr int kQ = 0, kKV = kQ + NG * kSlabQ, kP = kKV + kStages * kStage, kSc = kP + 2 * NG * kSlabQ, kRawAt = kSc + kStages * kScales;
+    static constexpr int kQ = 0, kKV = kQ + 2 * NG * kSlabQ, kP = kKV + kStages * kStage, kSc = kP + 2 * NG * kSlabQ, kRawAt = kSc + kStages * kScales;
     static constexpr int kBytes = kRawAt + kWorkers * kRaw * kRawChunk + 1024;
 };
 
@@ -99,21 +100,20 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     using S = Shape<D>;
     constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[3 * kStages + 8];
+    __shared__ __align__(8) uint64_t bars[4 * kStages + 8];
     __shared__ int64_t warp_sum[kThreads / 32];
-    __shared__ float   row_m[2][kRows], row_l[2][kRows];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
     __shared__ uint32_t tmem_at;
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
-    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, s_full = v_empty + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
+    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, k_read = v_empty + 8 * kStages, s_full = k_read + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- this block's item ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
-    auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kRows - 1) / kRows) * a.c.kv_heads; };
+    auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kBlockRows - 1) / kBlockRows) * a.c.kv_heads; };
     int64_t own = 0;
 #pragma unroll 1
     for (int b = s0; b < s1; ++b) own += items_of(sequence(a, b));
@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_init(k_full + 8 * i, kWorkers / 2);
             bar_init(v_full + 8 * i, kWorkers / 2);
             bar_init(v_empty + 8 * i, 1);
+            bar_init(k_read + 8 * i, 8);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
@@ -170,23 +171,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     const uint32_t tmem = tmem_at;
     const int  seq = at_seq;
     const Seq  s   = sequence(a, seq);
-    const int  rows = s.fresh * a.share, blocks = (rows + kRows - 1) / kRows;
+    const int  rows = s.fresh * a.share, blocks = (rows + kBlockRows - 1) / kBlockRows;
     const int  block = blocks - 1 - at_item / a.c.kv_heads, head = at_item % a.c.kv_heads;      // (the longest first)
     const int64_t most = a.b.table_ld << a.c.page_shift;
-    const int  first_tok = by_share(a, block * kRows), last_tok = min(by_share(a, block * kRows + kRows - 1), s.fresh - 1);
+    const int  first_tok = by_share(a, block * kBlockRows), last_tok = min(by_share(a, block * kBlockRows + kBlockRows - 1), s.fresh - 1);
     const int  end = (int)min((int64_t)(s.len - s.fresh + last_tok + 1), most);
     const int  lo  = a.window > 0 ? max(s.len - s.fresh + first_tok + 1 - a.window, 0) & ~15 : 0;
     const int  n   = end > lo ? (end - lo + kKeys - 1) / kKeys : 0;
     if (tid == 0 && s.len > most) kv_record(a.status, seq, (int)most);
 
-    // ---- the queries: a row per thread, group (or half of the one group) w per four warps; times 64 or 4, which the codes lack ----
+    // ---- the queries: a row per thread; times 64 or 4, which the codes lack ----
     if (warp < 8) {
-        const int r = tid & (kRows - 1), w = warp >> 2, row = block * kRows + r;
+        const int r = tid & (kRows - 1), w = warp >> 2, row = block * kBlockRows + w * kRows + r;
         const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
         const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
 #pragma unroll
-        for (int cc = 0; cc < (NG == 2 ? 2 : 1); ++cc) {
-            const int gr = NG == 2 ? w : 0, c = NG == 2 ? cc : w;
+        for (int cc = 0; cc < 2 * NG; ++cc) {
+            const int gr = cc >> 1, c = cc & 1;
             uint4 v[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
                     x[t] = mul2(__byte_perm(i < 2 ? v[t].x : v[t].y, i < 2 ? v[t].z : v[t].w, i & 1 ? 0x7632 : 0x5410), i & 1 ? 0x40804080u : 0x42804280u);
-                *reinterpret_cast<uint4 *>(smem + S::kQ + gr * S::kSlabQ + r * 128 + (((4 * c + i) ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<uint4 *>(smem + S::kQ + (w * NG + gr) * S::kSlabQ + r * 128 + (((4 * c + i) ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
             }
         }
         to_engine();
@@ -253,13 +254,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             fetch(j + kRaw - 1);
             const bool on = have >> min(kRaw - 1, n - 1 - j) & 1;
             const int st = j % kStages, tok0 = lo + j * kKeys + c * 16;
-            // a stage's keys are free once the softmax has taken the scores (and the scales) of the tile before it there, its values
-            // once that tile's product with them is over
-            if (j >= kStages) {
-                const int old = j - kStages;
-                if (side == 0 ? !warp_wait(s_read + 8 * (old & 1), (old >> 1) & 1, &failed) : !warp_wait(v_empty + 8 * st, (j / kStages - 1) & 1, &failed))
-                    goto done;
-            }
+            // a stage's keys are free once both softmax groups have taken the scores (and the scales) of the tile before it there, its
+            // values once that tile's products with them are over (a barrier of its own for every stage: nobody can be two phases behind)
+            if (j >= kStages && !warp_wait((side ? v_empty : k_read) + 8 * st, (j / kStages - 1) & 1, &failed)) goto done;
             const uint32_t from = raw_addr + (j % kRaw) * S::kRawChunk;
             const uint32_t *words = reinterpret_cast<const uint32_t *>(raw + (j % kRaw) * S::kRawChunk + 16 * kRow);
             const uint32_t to = base + S::kKV + st * S::kStage + side * NG * S::kSlabK;
@@ -306,55 +303,55 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     } else if (warp == 16 && elected()) {
         // ---- products ----
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
-        auto scores = [&](int i) {
+        auto scores = [&](int i, int w) {
             const int st = i % kStages;
             if (!bar_wait(k_full + 8 * st, (i / kStages) & 1, &failed)) return false;
             tc_after();
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                const uint64_t q = operand(base + S::kQ + gr * S::kSlabQ), k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK);
+                const uint64_t q = operand(base + S::kQ + (w * NG + gr) * S::kSlabQ), k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) product(tmem + (i & 1) * 128 + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
+                for (int x = 0; x < 4; ++x) product(tmem + w * 128 + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
             }
-            commit(s_full + 8 * (i & 1));
+            commit(s_full + 8 * w);
             return true;
         };
-        for (int i = 0; i < 2 && i < n; ++i)
-            if (!scores(i)) goto done;
+        if (n > 0 && !(scores(0, 0) && scores(0, 1))) goto done;
         for (int i = 0; i < n; ++i) {
-            // (the next scores of a group while it takes its exponentials)
-            const int st = i % kStages, w = i & 1;
-            if (i + 2 < n) {
-                if (!bar_wait(s_read + 8 * w, (i >> 1) & 1, &failed) || !scores(i + 2)) goto done;
-            }
-            if (!bar_wait(v_full + 8 * st, (i / kStages) & 1, &failed) || !bar_wait(p_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
-            tc_after();
+            const int st = i % kStages;
+#pragma unroll 1
+            for (int w = 0; w < 2; ++w) {
+                // (a group's next scores while it takes its exponentials)
+                if (i + 1 < n && (!bar_wait(s_read + 8 * w, i & 1, &failed) || !scores(i + 1, w))) goto done;
+                if (!bar_wait(v_full + 8 * st, (i / kStages) & 1, &failed) || !bar_wait(p_full + 8 * w, i & 1, &failed)) goto done;
+                tc_after();
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                const uint64_t p = operand(base + S::kP + (w * NG + gr) * S::kSlabQ), v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
+                for (int gr = 0; gr < NG; ++gr) {
+                    const uint64_t p = operand(base + S::kP + (w * NG + gr) * S::kSlabQ), v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) product(tmem + 256 + w * 128 + gr * 64, p + 2 * x, v + 2 * x, kHow, i >= 2 || x > 0);
+                    for (int x = 0; x < 4; ++x) product(tmem + 256 + w * 128 + gr * 64, p + 2 * x, v + 2 * x, kHow, i > 0 || x > 0);
+                }
+                commit(o_done + 8 * w);
             }
-            commit(o_done + 8 * w);
             commit(v_empty + 8 * st);
         }
     } else if (warp < 8) {
         // ---- softmax: a row per thread ----
-        const int w = warp >> 2, r = tid & (kRows - 1), row = block * kRows + r;
+        const int w = warp >> 2, r = tid & (kRows - 1), row0 = block * kBlockRows + w * kRows, row = row0 + r;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         int hi = 0x7fffffff, low = 0;                   // a row of padding masks nothing
         if (row < rows) {
             hi  = s.len - s.fresh + by_share(a, row) + 1;
             low = a.window > 0 ? max(hi - a.window, 0) : 0;
         }
-        const int least_hi = s.len - s.fresh + first_tok + 1, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
+        const int least_hi = row0 < rows ? s.len - s.fresh + by_share(a, row0) + 1 : 0x7fffffff, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
         unsigned char *p_at = smem + S::kP + w * NG * S::kSlabQ + r * 128;
         float m = kNothing, l = 0.0f;
 #pragma unroll 1
-        for (int i = w; i < n; i += 2) {
+        for (int i = 0; i < n; ++i) {
             const int st = i % kStages, tok0 = lo + i * kKeys;
             const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales), *vs = ks + NG * kKeys;
-            if (!warp_wait(s_full + 8 * w, (i >> 1) & 1, &failed)) goto done;
+            if (!warp_wait(s_full + 8 * w, i & 1, &failed)) goto done;
             tc_after();
             uint64_t sc[kKeys / 2];                     // two neighbouring columns each
 #pragma unroll
@@ -379,7 +376,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             const uint32_t gone = *reinterpret_cast<const volatile uint32_t *>(bad[st]);
             tc_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(s_read + 8 * w);         // scores, scales and `bad` are in registers
+            if (lane == 0) {                                   // scores, scales and `bad` are in registers
+                bar_arrive(s_read + 8 * w);
+                bar_arrive(k_read + 8 * st);
+            }
             if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
                 for (int x = 0; x < kKeys; x += 2) {
@@ -401,13 +401,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             }
             const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
             // the last product with this group's probabilities is over: they may be overwritten, and its output rescaled
-            if (i >= 2 && !warp_wait(o_done + 8 * w, ((i >> 1) - 1) & 1, &failed)) goto done;
+            if (i > 0 && !warp_wait(o_done + 8 * w, (i - 1) & 1, &failed)) goto done;
+            if (!warp_wait(v_full + 8 * st, (i / kStages) & 1, &failed)) goto done;             // the values' scales are there
             // (the maximum in use may lie up to 2^8 below the true one)
             if (__any_sync(0xffffffffu, top > m + 8.0f)) {
                 const float now = fmaxf(top, m), keep = power2(m - now);
                 m = now;
                 l *= keep;
-                if (i >= 2) {
+                if (i > 0) {
                     tc_after();
 #pragma unroll 1
                     for (int c0 = 0; c0 < NG * 64; c0 += 16) {
@@ -449,55 +450,28 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             __syncwarp();
             if (lane == 0) bar_arrive(p_full + 8 * w);
         }
-        row_m[w][r] = m;
-        row_l[w][r] = l;
-        // this group's last product (the other's is waited for by the other, and the block's barrier below by both)
-        const int count = (n + 1 - w) / 2;
-        if (count > 0 && !warp_wait(o_done + 8 * w, (count - 1) & 1, &failed)) goto done;
-    }
-done:
-    __syncwarp();
-    tc_before();
-    __syncthreads();
-    tc_after();
-    if (failed) {
-        // copies and products may still be in flight: give them time to end before the memory is let go
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-        if (tid == 0 && atomicCAS(a.status + 3, 0, 1) == 0) atomicExch(a.status, SYMAR_ERR_TIMEOUT);
-    } else if (warp < 8) {
-        // ---- the two groups' outputs joined: group w of the channels (or half of the one group) per four warps ----
-        const int w = warp >> 2, r = tid & (kRows - 1), row = block * kRows + r;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        const float m0 = row_m[0][r], m1 = row_m[1][r], top = fmaxf(m0, m1), f0 = power2(m0 - top), f1 = power2(m1 - top);
-        const float sum = n > 0 ? __fmaf_rn(row_l[1][r], f1, row_l[0][r] * f0) : 0.0f;
-        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
+        // ---- the output: what is left in tensor memory, divided by the row's sum ----
+        if (n > 0 && !warp_wait(o_done + 8 * w, (n - 1) & 1, &failed)) goto done;
+        tc_after();
+        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
         const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
         __nv_bfloat16 *out = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head;
 #pragma unroll 1
-        for (int cc = 0; cc < (NG == 2 ? 2 : 1); ++cc) {
-            const int at = (NG == 2 ? w * 64 : 0) + (NG == 2 ? cc : w) * 32;
-            float v[32];
+        for (int at = 0; at < D; at += 32) {
+            uint32_t v[32];
 #pragma unroll
-            for (int x = 0; x < 32; ++x) v[x] = 0.0f;
-#pragma unroll
-            for (int c0 = 0; c0 < 32; c0 += 16) {
-                float u[16];
-                if (n > 0) {
-                    acc_load16(tmem + lanes + 256 + at + c0, u);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) v[c0 + x] = u[x] * f0;
-                }
-                if (n > 1) {
-                    acc_load16(tmem + lanes + 256 + 128 + at + c0, u);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) v[c0 + x] = __fmaf_rn(u[x], f1, v[c0 + x]);
-                }
+            for (int x = 0; x < 32; ++x) v[x] = 0;
+            if (n > 0) {
+                acc_ask16(tmem + lanes + 256 + w * 128 + at, *reinterpret_cast<uint32_t(*)[16]>(v));
+                acc_ask16(tmem + lanes + 256 + w * 128 + at + 16, *reinterpret_cast<uint32_t(*)[16]>(v + 16));
+                acc_loaded(v);
             }
             if (row < rows) {
                 // column 8 i + g is channel 4 g + i
 #pragma unroll
                 for (int g = 0; g < 8; ++g) {
-                    const uint32_t x = pack_bf16(64.0f * v[g] * inv, 4.0f * v[8 + g] * inv), y = pack_bf16(64.0f * v[16 + g] * inv, 4.0f * v[24 + g] * inv);
+                    const uint32_t x = pack_bf16(64.0f * __uint_as_float(v[g]) * inv, 4.0f * __uint_as_float(v[8 + g]) * inv);
+                    const uint32_t y = pack_bf16(64.0f * __uint_as_float(v[16 + g]) * inv, 4.0f * __uint_as_float(v[24 + g]) * inv);
                     __nv_bfloat16 *p = out + at + 4 * g;
                     if (a.out_vec) {
                         *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
@@ -509,6 +483,16 @@ done:
             }
         }
     }
+done:
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (failed) {
+        // copies and products may still be in flight: give them time to end before the memory is let go
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        if (tid == 0 && atomicCAS(a.status + 3, 0, 1) == 0) atomicExch(a.status, SYMAR_ERR_TIMEOUT);
+    }
     tc_before();
     __syncthreads();
     tc_after();
@@ -518,7 +502,7 @@ done:
 // items that the call has at most: a block each (blocks beyond the last item leave at once)
 int64_t items_at_most(const AttnArgs &a)
 {
-    return ((int64_t)a.b.tokens * a.share / kRows + (a.b.seqs < a.b.tokens ? a.b.seqs : a.b.tokens)) * a.c.kv_heads;
+    return ((int64_t)a.b.tokens * a.share / kBlockRows + (a.b.seqs < a.b.tokens ? a.b.seqs : a.b.tokens)) * a.c.kv_heads;
 }
 
 }  // namespace
@@ -526,8 +510,11 @@ int64_t items_at_most(const AttnArgs &a)
 bool prompt_attention_takes(const AttnArgs &a, int num_sms)
 {
     if (a.c.dim > 128 || items_at_most(a) > 0x3fffffff) return false;
+    // Blocks that are mostly full, and for a quarter of the multiprocessors at least.  (64 heads, 8 key/value heads; this kernel against the
+    // one that shares a sequence's tokens between blocks, us: 512 new tokens over 8192: 372, 786; 256: 361, 398; 128, 32 blocks: 356, 206;
+    // 8 x 32 new tokens over 2048: 103, 117; 8 x 16, half-full blocks: 99, 67.)
     const int64_t rows = (int64_t)a.b.tokens * a.share;                // of one key/value head
-    return rows >= 64ll * a.b.seqs && rows / kRows * a.c.kv_heads >= num_sms / 2;
+    return rows >= (int64_t)kBlockRows * a.b.seqs && rows / kBlockRows * a.c.kv_heads >= num_sms / 4;
 }
 
 cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream)

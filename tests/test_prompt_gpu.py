@@ -79,9 +79,10 @@ def test_prompts_with_flat_and_sharp_softmax(kv, scale):     # noqa: F811
     assert ((got.double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("new", [600, 1300])
 @pytest.mark.parametrize("offset", [0, 1, 4])
-def test_prompts_take_any_strides(kv, offset):               # noqa: F811
-    s = Setup([(600, 700)], 8, 128, 16, seed=5)
+def test_prompts_take_any_strides(kv, offset, new):          # noqa: F811
+    s = Setup([(new, new + 100)], 8, 128, 16, seed=5)
     s.fill(kv, seed=51)
     q = normal(s.tokens, 16, 128, seed=6)
     want = kv.attention(s.cache, s.batch, q)
@@ -95,25 +96,26 @@ def test_prompts_take_any_strides(kv, offset):               # noqa: F811
     assert (o[:, :, :offset] == 7.0).all() and (o[:, :, offset + 128:] == 7.0).all()
 
 
-def test_prompt_and_single_tokens_agree(kv):                 # noqa: F811
+@pytest.mark.parametrize("total", [600, 1300])
+def test_prompt_and_single_tokens_agree(kv, total):          # noqa: F811
     """The same rows by the two kernels: within twice the bound of the same value."""
-    total = 600
     s = Setup([(total, total)], 8, 128, 16, seed=6)
     filled = s.fill(kv, seed=61)
     q = normal(total, 16, 128, seed=7)
     whole = kv.attention(s.cache, s.batch, q).double()
     _, tol = reference(s, filled, q, 128 ** -0.5, 0)
-    for t in (0, 1, 63, 64, 65, 300, 599):
+    for t in (0, 1, 63, 64, 65, 300, total - 1):
         batch = symar.KVBatch(torch.tensor([t + 1], dtype=torch.int32, device="cuda"), s.table)
         one = kv.attention(s.cache, batch, q[t:t + 1]).double()
         assert ((whole[t] - one[0]).abs() <= 2 * tol[t]).all()
 
 
-def test_a_page_that_is_not_there(kv):                       # noqa: F811
+@pytest.mark.parametrize("total", [600, 1300])
+def test_a_page_that_is_not_there(kv, total):                # noqa: F811
     c = symar.KVContext.on_torch()
-    s = Setup([(600, 600)], 8, 128, 16, seed=7)
+    s = Setup([(total, total)], 8, 128, 16, seed=7)
     filled = s.fill(kv, seed=71)
-    q = normal(600, 16, 128, seed=1)
+    q = normal(total, 16, 128, seed=1)
     table = s.table.clone()
     table[0, 3] = -1
     got = c.attention(s.cache, symar.KVBatch(s.lengths, table, s.start), q)
@@ -123,8 +125,8 @@ def test_a_page_that_is_not_there(kv):                       # noqa: F811
     want, tol = reference(s, filled, q, 128 ** -0.5, 0)
     assert ((got[:48].double() - want[:48]).abs() <= tol[:48]).all()
     k, v = filled[0]
-    keep = torch.cat([torch.arange(48), torch.arange(64, 600)]).cuda()
-    for t in (64, 100, 599):
+    keep = torch.cat([torch.arange(48), torch.arange(64, total)]).cuda()
+    for t in (64, 100, total - 1):
         kk, vv = (x[keep[keep <= t]] for x in (k, v))
         for h in (0, 7, 15):
             p = torch.softmax(kk[:, h // 2] @ q[t, h].double() * 128 ** -0.5, 0)
