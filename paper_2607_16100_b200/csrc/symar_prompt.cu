@@ -16,9 +16,11 @@
 namespace symar {
 namespace {
 
-constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kStages = 2, kRaw = 3;
+constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kStages = 3, kRaw = 3;
 constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
-constexpr int kThreads = 32 * (8 + kWorkers + 1);      // two softmax groups of four warps, the workers, one warp for the products
+constexpr int kThreads = 32 * (8 + kWorkers + 4);      // two softmax groups of four warps, the workers, a warp for each group's products, two idle ones
+constexpr int kRegsSoftmax = 144, kRegsWorker = 72, kRegsRest = 48, kRegsLaunch = 96;
+static_assert(2 * kRegsSoftmax + 2 * kRegsWorker + kRegsRest <= 5 * kRegsLaunch, "the warpgroups' shares must not be above what a block is launched with");
 
 template <int D>
 struct Shape {
@@ -27,7 +29,7 @@ struct Shape {
     static constexpr int kStage = 2 * NG * kSlabK;
     static constexpr int kScales = 2 * NG * kKeys * 4;
     static constexpr int kRawChunk = 16 * (kRow + NG * 4);
-    static constexpr int kQ = 0, kKV = kQ + 2 * NG * kSlabQ, kP = kKV + kStages * kStage, kSc = kP + 2 * NG * kSlabQ, kRawAt = kSc + kStages * kScales;
+    static constexpr int kQ = 0, kKV = kQ + 2 * NG * kSlabQ, kSc = kKV + kStages * kStage, kRawAt = kSc + kStages * kScales;
     static constexpr int kBytes = kRawAt + kWorkers * kRaw * kRawChunk + 1024;
 };
 
@@ -45,6 +47,33 @@ __device__ __forceinline__ void acc_store16(uint32_t addr, const float *v)
                  "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
+// Sixteen lanes and 64 columns, as the result of a matrix instruction lies in a warp: a thread has columns 8 j + 2 t and the next one of
+// lanes lane / 4 (v[4 j], v[4 j + 1]) and lane / 4 + 8 (v[4 j + 2], v[4 j + 3]), t = lane % 4.  Waited for later (acc_loaded).
+__device__ __forceinline__ void acc_ask_rows(uint32_t addr, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
+                 "%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr));
+}
+// The same lanes, sixteen columns of pairs of bf16: a thread's pairs 4 j + t of lanes lane / 4 (v[2 j]) and lane / 4 + 8 (v[2 j + 1]).
+__device__ __forceinline__ void pairs_store(uint32_t addr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+// a product whose first operand is in tensor memory
+__device__ __forceinline__ void product_of(uint32_t acc, uint32_t a, uint64_t b, uint32_t how, uint32_t add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(acc),
+                 "r"(a), "l"(b), "r"(how), "r"(add) : "memory");
+}
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 // sixteen columns, waited for later (acc_loaded)
 __device__ __forceinline__ void acc_ask16(uint32_t addr, uint32_t (&r)[16])
 {
@@ -128,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         for (int i = 0; i < kStages; ++i) {
             bar_init(k_full + 8 * i, kWorkers / 2);
             bar_init(v_full + 8 * i, kWorkers / 2);
-            bar_init(v_empty + 8 * i, 1);
+            bar_init(v_empty + 8 * i, 2);
             bar_init(k_read + 8 * i, 8);
         }
         for (int i = 0; i < 2; ++i) {
@@ -218,6 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     tc_after();
 
     if (warp >= 8 && warp < 16) {
+        registers_down<kRegsWorker>();
         // ---- codes to operands ----
         const int dw = warp - 8, c = dw & 3, side = dw >> 2, ps = 1 << a.c.page_shift, g = lane >> 2, t = lane & 3;
         unsigned char *raw = smem + S::kRawAt + dw * kRaw * S::kRawChunk;
@@ -263,11 +293,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             const int mt = (lane >> 4) * 8 + (lane & 7), mc = lane >> 3 & 1, turn = D == 64 ? mt >> 2 & 1 : mt >> 1 & 3;
             if (lane < 16) {
                 // beyond the sequence's end a page holds anything: values from there count for nothing
-                float *scales = reinterpret_cast<float *>(smem + S::kSc + st * S::kScales) + side * NG * kKeys + c * 16 + lane;
+                float *scales = reinterpret_cast<float *>(smem + S::kSc + st * S::kScales) + side * NG * kKeys + (c * 8 + (lane >> 1)) * 2 * NG + (lane & 1);
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
                     const float f = __uint_as_float(words[lane * NG + gr]);
-                    scales[gr * kKeys] = side ? (tok0 + lane < s.len ? f : 0.0f) : f * a.scale_log2;
+                    scales[gr * 2] = side ? (tok0 + lane < s.len ? f : 0.0f) : f * a.scale_log2;
                 }
             }
             if (side == 0 && lane == 0) bad[st][c] = !on && tok0 < end;
@@ -297,163 +327,206 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             }
             to_engine();
             __syncwarp();
-            if (lane == 0) bar_arrive((side ? v_full : k_full) + 8 * st);
+            bar_arrive_if((side ? v_full : k_full) + 8 * st, lane == 0);
         }
         copies_wait<0>();
-    } else if (warp == 16 && elected()) {
-        // ---- products ----
-        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
-        auto scores = [&](int i, int w) {
-            const int st = i % kStages;
-            if (!bar_wait(k_full + 8 * st, (i / kStages) & 1, &failed)) return false;
-            tc_after();
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
+    } else if (warp >= 16) {
+        registers_down<kRegsRest>();
+        if (warp < 18 && elected()) {
+            // ---- a group's products.  Its probabilities take the place of the first 64 channels' scores: those of the next tile wait until the
+            // product with them is over, the second 64 channels' only until the softmax has read the scores. ----
+            constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
+            const int w = warp - 16;
+            const uint32_t sc_at = tmem + w * 128, out_at = tmem + 256 + w * 128;
+            auto scores = [&](int st, int gr) {
                 const uint64_t q = operand(base + S::kQ + (w * NG + gr) * S::kSlabQ), k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) product(tmem + w * 128 + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
+                for (int x = 0; x < 4; ++x) product(sc_at + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
+            };
+            if (n > 0) {
+                if (!bar_wait(k_full, 0, &failed) || !bar_wait(v_full, 0, &failed)) goto done;
+                tc_after();
+                if (NG == 2) scores(0, NG - 1);
+                scores(0, 0);
+                commit(s_full + 8 * w);
             }
-            commit(s_full + 8 * w);
-            return true;
-        };
-        if (n > 0 && !(scores(0, 0) && scores(0, 1))) goto done;
-        for (int i = 0; i < n; ++i) {
-            const int st = i % kStages;
 #pragma unroll 1
-            for (int w = 0; w < 2; ++w) {
-                // (a group's next scores while it takes its exponentials)
-                if (i + 1 < n && (!bar_wait(s_read + 8 * w, i & 1, &failed) || !scores(i + 1, w))) goto done;
-                if (!bar_wait(v_full + 8 * st, (i / kStages) & 1, &failed) || !bar_wait(p_full + 8 * w, i & 1, &failed)) goto done;
+            for (int i = 0; i < n; ++i) {
+                const int st = i % kStages, next = (i + 1) % kStages;
+                if (i + 1 < n) {
+                    // (the softmax takes the scales of the values without a wait of its own: scores are there when the values are, too)
+                    const uint32_t round = ((i + 1) / kStages) & 1;
+                    if (!bar_wait(k_full + 8 * next, round, &failed) || !bar_wait(v_full + 8 * next, round, &failed)) goto done;
+                    if (NG == 2) {
+                        if (!bar_wait(s_read + 8 * w, i & 1, &failed)) goto done;
+                        tc_after();
+                        scores(next, NG - 1);
+                    }
+                }
+                if (!bar_wait(p_full + 8 * w, i & 1, &failed)) goto done;
                 tc_after();
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    const uint64_t p = operand(base + S::kP + (w * NG + gr) * S::kSlabQ), v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
+                    const uint64_t v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) product(tmem + 256 + w * 128 + gr * 64, p + 2 * x, v + 2 * x, kHow, i > 0 || x > 0);
+                    for (int x = 0; x < 4; ++x) product_of(out_at + gr * 64, sc_at + gr * 32 + x * 8, v + 2 * x, kHow, i > 0 || x > 0);
                 }
                 commit(o_done + 8 * w);
+                commit(v_empty + 8 * st);
+                if (i + 1 < n) {
+                    if (!bar_wait(o_done + 8 * w, i & 1, &failed)) goto done;
+                    tc_after();
+                    scores(next, 0);
+                    commit(s_full + 8 * w);
+                }
             }
-            commit(v_empty + 8 * st);
         }
-    } else if (warp < 8) {
-        // ---- softmax: a row per thread ----
-        const int w = warp >> 2, r = tid & (kRows - 1), row0 = block * kBlockRows + w * kRows, row = row0 + r;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
-        int hi = 0x7fffffff, low = 0;                   // a row of padding masks nothing
-        if (row < rows) {
-            hi  = s.len - s.fresh + by_share(a, row) + 1;
-            low = a.window > 0 ? max(hi - a.window, 0) : 0;
-        }
+    } else {
+        // ---- softmax: a thread has four rows of its warp's 32 (8 q + lane / 4) and every eighth pair of columns, so that a scale that it
+        // loads serves four rows ----
+        registers_up<kRegsSoftmax>();
+        const int w = warp >> 2, row0 = block * kBlockRows + w * kRows, mine = row0 + (warp & 3) * 32 + (lane >> 2), t2 = (lane & 3) * 2;
+        const uint32_t sc_at = tmem + ((uint32_t)(warp & 3) << 21) + w * 128, out_at = sc_at + 256;
         const int least_hi = row0 < rows ? s.len - s.fresh + by_share(a, row0) + 1 : 0x7fffffff, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
-        unsigned char *p_at = smem + S::kP + w * NG * S::kSlabQ + r * 128;
-        float m = kNothing, l = 0.0f;
+        float m[4] = {kNothing, kNothing, kNothing, kNothing};
+        uint64_t l[4] = {0, 0, 0, 0};                   // of the thread's even and odd columns
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
             const int st = i % kStages, tok0 = lo + i * kKeys;
-            const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales), *vs = ks + NG * kKeys;
+            const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales) + t2 * NG, *vs = ks + NG * kKeys;
             if (!warp_wait(s_full + 8 * w, i & 1, &failed)) goto done;
             tc_after();
-            uint64_t sc[kKeys / 2];                     // two neighbouring columns each
+            uint64_t sc[4][8];                          // rows 8 q + lane / 4, columns 8 j + t2 and the next
 #pragma unroll
-            for (int c0 = 0; c0 < kKeys; c0 += 16) {
-                uint32_t x[16 * NG];
-                acc_ask16(tmem + lanes + w * 128 + c0, *reinterpret_cast<uint32_t(*)[16]>(x));
-                if (NG == 2) acc_ask16(tmem + lanes + w * 128 + 64 + c0, *reinterpret_cast<uint32_t(*)[16]>(x + 16 * (NG - 1)));
+            for (int h = 0; h < 2; ++h) {
+                uint32_t x[32 * NG];
+                acc_ask_rows(sc_at + ((uint32_t)h << 20), x);
+                if (NG == 2) acc_ask_rows(sc_at + ((uint32_t)h << 20) + 64, x + 32 * (NG - 1));
                 acc_loaded(x);
 #pragma unroll
-                for (int y = 0; y < 16; y += 4) {
-                    const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(ks + c0 + y);
-                    uint64_t u = mul_two(two(__uint_as_float(x[y]), __uint_as_float(x[y + 1])), k.x);
-                    uint64_t v = mul_two(two(__uint_as_float(x[y + 2]), __uint_as_float(x[y + 3])), k.y);
-                    if (NG == 2) {
-                        const ulonglong2 k1 = *reinterpret_cast<const ulonglong2 *>(ks + kKeys + c0 + y);
-                        u = fma_two(two(__uint_as_float(x[16 * (NG - 1) + y]), __uint_as_float(x[16 * (NG - 1) + y + 1])), k1.x, u);
-                        v = fma_two(two(__uint_as_float(x[16 * (NG - 1) + y + 2]), __uint_as_float(x[16 * (NG - 1) + y + 3])), k1.y, v);
+                for (int j = 0; j < 8; ++j) {
+                    ulonglong2 k;
+                    if (NG == 2) k = *reinterpret_cast<const ulonglong2 *>(ks + j * 8 * NG);
+                    else k.x = *reinterpret_cast<const uint64_t *>(ks + j * 8 * NG), k.y = 0;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        uint64_t v = mul_two(two(__uint_as_float(x[4 * j + 2 * b]), __uint_as_float(x[4 * j + 2 * b + 1])), k.x);
+                        if (NG == 2) v = fma_two(two(__uint_as_float(x[32 * (NG - 1) + 4 * j + 2 * b]), __uint_as_float(x[32 * (NG - 1) + 4 * j + 2 * b + 1])), k.y, v);
+                        sc[2 * h + b][j] = v;
                     }
-                    sc[(c0 + y) / 2] = u, sc[(c0 + y) / 2 + 1] = v;
                 }
             }
             const uint32_t gone = *reinterpret_cast<const volatile uint32_t *>(bad[st]);
             tc_before();
             __syncwarp();
-            if (lane == 0) {                                   // scores, scales and `bad` are in registers
-                bar_arrive(s_read + 8 * w);
-                bar_arrive(k_read + 8 * st);
-            }
+            bar_arrive_if(s_read + 8 * w, lane == 0);         // scores, scales and `bad` are in registers
+            bar_arrive_if(k_read + 8 * st, lane == 0);
             if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
-                for (int x = 0; x < kKeys; x += 2) {
-                    float u, v;
-                    apart(sc[x / 2], u, v);
-                    const bool lost = gone >> 8 * (x >> 4) & 1u;
-                    if (tok0 + x >= hi || tok0 + x < low || tok0 + x >= end || lost) u = -INFINITY;
-                    if (tok0 + x + 1 >= hi || tok0 + x + 1 < low || tok0 + x + 1 >= end || lost) v = -INFINITY;
-                    sc[x / 2] = two(u, v);
+                for (int q = 0; q < 4; ++q) {
+                    int hi = 0x7fffffff, low = 0;       // a row of padding masks nothing
+                    if (mine + 8 * q < rows) {
+                        hi  = s.len - s.fresh + by_share(a, mine + 8 * q) + 1;
+                        low = a.window > 0 ? max(hi - a.window, 0) : 0;
+                    }
+                    hi = min(hi, end);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float u, v;
+                        apart(sc[q][j], u, v);
+                        const int tok = tok0 + 8 * j + t2;
+                        const bool lost = gone >> 8 * (j >> 1) & 1u;
+                        if (tok >= hi || tok < low || lost) u = -INFINITY;
+                        if (tok + 1 >= hi || tok + 1 < low || lost) v = -INFINITY;
+                        sc[q][j] = two(u, v);
+                    }
                 }
             }
-            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float top[4];
+            bool  more = false;
 #pragma unroll
-            for (int x = 0; x < kKeys / 2; ++x) {
-                float u, v;
-                apart(sc[x], u, v);
-                tops[2 * (x & 1)]     = fmaxf(tops[2 * (x & 1)], u);
-                tops[2 * (x & 1) + 1] = fmaxf(tops[2 * (x & 1) + 1], v);
+            for (int q = 0; q < 4; ++q) {
+                top[q] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float u, v;
+                    apart(sc[q][j], u, v);
+                    top[q] = fmaxf(fmaxf(top[q], u), v);
+                }
+                more |= top[q] > m[q] + 8.0f;
             }
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-            // the last product with this group's probabilities is over: they may be overwritten, and its output rescaled
-            if (i > 0 && !warp_wait(o_done + 8 * w, (i - 1) & 1, &failed)) goto done;
-            if (!warp_wait(v_full + 8 * st, (i / kStages) & 1, &failed)) goto done;             // the values' scales are there
             // (the maximum in use may lie up to 2^8 below the true one)
-            if (__any_sync(0xffffffffu, top > m + 8.0f)) {
-                const float now = fmaxf(top, m), keep = power2(m - now);
-                m = now;
-                l *= keep;
+            if (__any_sync(0xffffffffu, more)) {
+                float keep[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 1));
+                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 2));
+                    const float now = fmaxf(top[q], m[q]);
+                    keep[q] = power2(m[q] - now);
+                    m[q] = now;
+                    l[q] = mul_two(l[q], two(keep[q], keep[q]));
+                }
+                // (the scores of this tile were asked for after the last product with this group's probabilities was over)
                 if (i > 0) {
-                    tc_after();
 #pragma unroll 1
                     for (int c0 = 0; c0 < NG * 64; c0 += 16) {
                         float v[16];
-                        acc_load16(tmem + lanes + 256 + w * 128 + c0, v);
+                        const float k0 = __shfl_sync(0xffffffffu, keep[0], (lane & 7) * 4), k1 = __shfl_sync(0xffffffffu, keep[1], (lane & 7) * 4);
+                        const float k2 = __shfl_sync(0xffffffffu, keep[2], (lane & 7) * 4), k3 = __shfl_sync(0xffffffffu, keep[3], (lane & 7) * 4);
+                        const float k = lane < 16 ? (lane < 8 ? k0 : k1) : (lane < 24 ? k2 : k3);
+                        acc_load16(out_at + c0, v);
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) v[x] *= keep;
-                        acc_store16(tmem + lanes + 256 + w * 128 + c0, v);
+                        for (int x = 0; x < 16; ++x) v[x] *= k;
+                        acc_store16(out_at + c0, v);
                     }
-                    acc_stored();
                 }
             }
-            uint64_t sums[2] = {0, 0};
-            const uint64_t less = two(-m, -m);
 #pragma unroll
-            for (int x0 = 0; x0 < kKeys; x0 += 8) {
-                uint64_t p[4];
+            for (int j0 = 0; j0 < 8; j0 += 4) {
+                uint32_t p[NG][2][8];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    float u, v;
-                    apart(add_two(sc[x0 / 2 + x], less), u, v);
-                    p[x] = two(power2(u), power2(v));
-                    sums[x & 1] = add_two(sums[x & 1], p[x]);
+                for (int j = 0; j < 4; ++j) {
+                    ulonglong2 f;
+                    if (NG == 2) f = *reinterpret_cast<const ulonglong2 *>(vs + (j0 + j) * 8 * NG);
+                    else f.x = *reinterpret_cast<const uint64_t *>(vs + (j0 + j) * 8 * NG), f.y = 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float u, v;
+                        apart(add_two(sc[q][j0 + j], two(-m[q], -m[q])), u, v);
+                        const uint64_t e = two(power2(u), power2(v));
+                        l[q] = add_two(l[q], e);
+                        p[0][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.x));
+                        if (NG == 2) p[NG - 1][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.y));
+                    }
                 }
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    const ulonglong2 u = *reinterpret_cast<const ulonglong2 *>(vs + gr * kKeys + x0), v = *reinterpret_cast<const ulonglong2 *>(vs + gr * kKeys + x0 + 4);
-                    *reinterpret_cast<uint4 *>(p_at + gr * S::kSlabQ + (((x0 >> 3) ^ (r & 7)) << 4)) =
-                        make_uint4(pack_two(mul_two(p[0], u.x)), pack_two(mul_two(p[1], u.y)), pack_two(mul_two(p[2], v.x)), pack_two(mul_two(p[3], v.y)));
+                    pairs_store(sc_at + gr * 32 + j0 * 4, p[gr][0]);
+                    pairs_store(sc_at + gr * 32 + j0 * 4 + (16u << 16), p[gr][1]);
                 }
             }
-            {
-                float u, v;
-                apart(add_two(sums[0], sums[1]), u, v);
-                l += u + v;
-            }
-            to_engine();
+            acc_stored();
             tc_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(p_full + 8 * w);
+            bar_arrive_if(p_full + 8 * w, lane == 0);
         }
-        // ---- the output: what is left in tensor memory, divided by the row's sum ----
+        // ---- the output: what is left in tensor memory, a row per thread, divided by the row's sum ----
         if (n > 0 && !warp_wait(o_done + 8 * w, (n - 1) & 1, &failed)) goto done;
         tc_after();
-        const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+        float sum = 0.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float u, v;
+            apart(l[q], u, v);
+            u += v;
+            u += __shfl_xor_sync(0xffffffffu, u, 1);
+            u += __shfl_xor_sync(0xffffffffu, u, 2);
+            u = __shfl_sync(0xffffffffu, u, (lane & 7) * 4);
+            if (lane >> 3 == q) sum = u;
+        }
+        const int row = row0 + (tid & (kRows - 1));
+        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
         const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
         __nv_bfloat16 *out = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head;
 #pragma unroll 1
@@ -462,8 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 #pragma unroll
             for (int x = 0; x < 32; ++x) v[x] = 0;
             if (n > 0) {
-                acc_ask16(tmem + lanes + 256 + w * 128 + at, *reinterpret_cast<uint32_t(*)[16]>(v));
-                acc_ask16(tmem + lanes + 256 + w * 128 + at + 16, *reinterpret_cast<uint32_t(*)[16]>(v + 16));
+                acc_ask16(out_at + at, *reinterpret_cast<uint32_t(*)[16]>(v));
+                acc_ask16(out_at + at + 16, *reinterpret_cast<uint32_t(*)[16]>(v + 16));
                 acc_loaded(v);
             }
             if (row < rows) {
@@ -517,20 +590,31 @@ bool prompt_attention_takes(const AttnArgs &a, int num_sms)
     return rows >= (int64_t)kBlockRows * a.b.seqs && rows / kBlockRows * a.c.kv_heads >= num_sms / 4;
 }
 
+namespace {
+template <int D>
+cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t stream)
+{
+    static std::atomic<uint64_t> allowed{0}, fits{0};
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (!(fits.load(std::memory_order_relaxed) & bit)) {
+        // the warpgroups share out what a block is launched with; with less than that they would wait for ever
+        cudaFuncAttributes at;
+        const cudaError_t e = cudaFuncGetAttributes(&at, (const void *)prompt_kernel<D>);
+        if (e != cudaSuccess) return e;
+        if (at.numRegs < kRegsLaunch) return cudaErrorLaunchOutOfResources;
+        fits.fetch_or(bit, std::memory_order_relaxed);
+    }
+    const cudaError_t e = allow_shared((const void *)prompt_kernel<D>, Shape<D>::kBytes, device, allowed);
+    if (e != cudaSuccess) return e;
+    prompt_kernel<D><<<blocks, kThreads, Shape<D>::kBytes, stream>>>(a);
+    return cudaGetLastError();
+}
+}  // namespace
+
 cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream)
 {
     const unsigned blocks = (unsigned)items_at_most(a);
-    static std::atomic<uint64_t> allowed64{0}, allowed128{0};
-    if (a.c.dim == 64) {
-        const cudaError_t e = allow_shared((const void *)prompt_kernel<64>, Shape<64>::kBytes, device, allowed64);
-        if (e != cudaSuccess) return e;
-        prompt_kernel<64><<<blocks, kThreads, Shape<64>::kBytes, stream>>>(a);
-    } else {
-        const cudaError_t e = allow_shared((const void *)prompt_kernel<128>, Shape<128>::kBytes, device, allowed128);
-        if (e != cudaSuccess) return e;
-        prompt_kernel<128><<<blocks, kThreads, Shape<128>::kBytes, stream>>>(a);
-    }
-    return cudaGetLastError();
+    return a.c.dim == 64 ? launch<64>(a, blocks, device, stream) : launch<128>(a, blocks, device, stream);
 }
 
 }  // namespace symar

@@ -18,6 +18,10 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void bar_arrive_if(uint32_t bar, bool on)      // (no branch)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((int)on) : "memory");
+}
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -36,7 +40,7 @@ __device__ __forceinline__ uint64_t now_ns()
     return t;
 }
 // A thread's wait; false once it has lasted four seconds or another role has given up.
-static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed)
+__device__ __forceinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int *failed)
 {
     const uint64_t t0 = now_ns();
     for (;;) {
@@ -56,12 +60,22 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     if (!ok) ok = bar_wait_long(bar, parity, failed);
     return ok;
 }
-// The same for a whole warp: all its lanes go on, or none.  One lane polls.
+// The same for a whole warp: all its lanes go on, or none.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *failed)
 {
-    int ok = 0;
-    if ((threadIdx.x & 31) == 0) ok = bar_wait(bar, parity, failed);
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    const uint64_t t0 = now_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 256; ++i)
+            if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *failed || now_ns() - t0 > kWaitNs)) {
+            *failed = 1;
+            return false;
+        }
+    }
 }
 // one lane of a converged warp
 __device__ __forceinline__ bool elected()
