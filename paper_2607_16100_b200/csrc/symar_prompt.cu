@@ -16,7 +16,7 @@
 namespace symar {
 namespace {
 
-constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kStages = 3, kRaw = 3;
+constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kSub = 32, kStages = 3, kRaw = 3;
 constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
 constexpr int kThreads = 32 * (8 + kWorkers + 4);      // two softmax groups of four warps, the workers, a warp for each group's products, two idle ones
 constexpr int kRegsSoftmax = 144, kRegsWorker = 72, kRegsRest = 48, kRegsLaunch = 96;
@@ -47,16 +47,13 @@ __device__ __forceinline__ void acc_store16(uint32_t addr, const float *v)
                  "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
-// Sixteen lanes and 64 columns, as the result of a matrix instruction lies in a warp: a thread has columns 8 j + 2 t and the next one of
+// Sixteen lanes and 32 columns, as the result of a matrix instruction lies in a warp: a thread has columns 8 j + 2 t and the next one of
 // lanes lane / 4 (v[4 j], v[4 j + 1]) and lane / 4 + 8 (v[4 j + 2], v[4 j + 3]), t = lane % 4.  Waited for later (acc_loaded).
 __device__ __forceinline__ void acc_ask_rows(uint32_t addr, uint32_t *r)
 {
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
-                 "%26,%27,%28,%29,%30,%31}, [%32];"
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr));
 }
 // The same lanes, sixteen columns of pairs of bf16: a thread's pairs 4 j + t of lanes lane / 4 (v[2 j]) and lane / 4 + 8 (v[2 j + 1]).
@@ -129,14 +126,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     using S = Shape<D>;
     constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[4 * kStages + 8];
+    __shared__ __align__(8) uint64_t bars[4 * kStages + 12];
     __shared__ int64_t warp_sum[kThreads / 32];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
     __shared__ uint32_t tmem_at;
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
-    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, k_read = v_empty + 8 * kStages, s_full = k_read + 8 * kStages, p_full = s_full + 16, o_done = p_full + 16, s_read = o_done + 16;
+    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, k_read = v_empty + 8 * kStages, s_full = k_read + 8 * kStages, p_full = s_full + 16, o_done = p_full + 32, s_read = o_done + 32;
+    // (p_full and o_done of a group: one for even, one for odd tiles.  A warp may be a tile ahead of the others' probabilities, and not every
+    // product's end is waited for.)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- this block's item ----
@@ -162,8 +161,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
-            bar_init(p_full + 8 * i, 4);
-            bar_init(o_done + 8 * i, 1);
+            bar_init(p_full + 16 * i, 4);
+            bar_init(p_full + 16 * i + 8, 4);
+            bar_init(o_done + 16 * i, 1);
+            bar_init(o_done + 16 * i + 8, 1);
             bar_init(s_read + 8 * i, 4);
         }
         failed = 0;
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     const int  first_tok = by_share(a, block * kBlockRows), last_tok = min(by_share(a, block * kBlockRows + kBlockRows - 1), s.fresh - 1);
     const int  end = (int)min((int64_t)(s.len - s.fresh + last_tok + 1), most);
     const int  lo  = a.window > 0 ? max(s.len - s.fresh + first_tok + 1 - a.window, 0) & ~15 : 0;
-    const int  n   = end > lo ? (end - lo + kKeys - 1) / kKeys : 0;
+    const int  subs = end > lo ? (end - lo + kSub - 1) / kSub : 0, n = (subs + 1) / 2;
     if (tid == 0 && s.len > most) kv_record(a.status, seq, (int)most);
 
     // ---- the queries: a row per thread; times 64 or 4, which the codes lack ----
@@ -333,52 +334,53 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     } else if (warp >= 16) {
         registers_down<kRegsRest>();
         if (warp < 18 && elected()) {
-            // ---- a group's products.  Its probabilities take the place of the first 64 channels' scores: those of the next tile wait until the
-            // product with them is over, the second 64 channels' only until the softmax has read the scores. ----
-            constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys / 8) << 17) | ((uint32_t)(kRows / 16) << 24);
+            // ---- a group's products, 32 keys at a time.  The next scores follow as soon as the softmax has read the ones before; there are two
+            // sets of probabilities.  (The softmax takes a set's place, and the scales of the values, without a wait of its own: when scores are
+            // there, the values are, and the products with the probabilities of two times before are over.) ----
+            constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
+            constexpr uint32_t kHowScores = kHow | ((uint32_t)(kSub / 8) << 17), kHowOut = kHow | (8u << 17);
             const int w = warp - 16;
-            const uint32_t sc_at = tmem + w * 128, out_at = tmem + 256 + w * 128;
-            auto scores = [&](int st, int gr) {
-                const uint64_t q = operand(base + S::kQ + (w * NG + gr) * S::kSlabQ), k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK);
+            const uint32_t sc_at = tmem + w * 256, out_at = sc_at + 128;
+            auto scores = [&](int i) {
+                const int st = (i >> 1) % kStages;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) product(sc_at + gr * 64, q + 2 * x, k + 2 * x, kHow, x > 0);
+                for (int gr = 0; gr < NG; ++gr) {
+                    const uint64_t q = operand(base + S::kQ + (w * NG + gr) * S::kSlabQ);
+                    const uint64_t k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK + (i & 1) * kSub * 128);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) product(sc_at + gr * kSub, q + 2 * x, k + 2 * x, kHowScores, x > 0);
+                }
+                commit(s_full + 8 * w);
             };
-            if (n > 0) {
+            if (subs > 0) {
                 if (!bar_wait(k_full, 0, &failed) || !bar_wait(v_full, 0, &failed)) goto done;
                 tc_after();
-                if (NG == 2) scores(0, NG - 1);
-                scores(0, 0);
-                commit(s_full + 8 * w);
+                scores(0);
             }
 #pragma unroll 1
-            for (int i = 0; i < n; ++i) {
-                const int st = i % kStages, next = (i + 1) % kStages;
-                if (i + 1 < n) {
-                    // (the softmax takes the scales of the values without a wait of its own: scores are there when the values are, too)
-                    const uint32_t round = ((i + 1) / kStages) & 1;
-                    if (!bar_wait(k_full + 8 * next, round, &failed) || !bar_wait(v_full + 8 * next, round, &failed)) goto done;
-                    if (NG == 2) {
-                        if (!bar_wait(s_read + 8 * w, i & 1, &failed)) goto done;
-                        tc_after();
-                        scores(next, NG - 1);
+            for (int i = 0; i < subs; ++i) {
+                const int st = (i >> 1) % kStages;
+                if (i + 1 < subs) {
+                    if (i & 1) {
+                        const int next = ((i + 1) >> 1) % kStages;
+                        const uint32_t round = (((i + 1) >> 1) / kStages) & 1;
+                        if (!bar_wait(k_full + 8 * next, round, &failed) || !bar_wait(v_full + 8 * next, round, &failed)) goto done;
                     }
+                    if (!bar_wait(s_read + 8 * w, i & 1, &failed)) goto done;
+                    tc_after();
+                    scores(i + 1);
                 }
-                if (!bar_wait(p_full + 8 * w, i & 1, &failed)) goto done;
+                if (!bar_wait(p_full + 16 * w + 8 * (i & 1), i >> 1 & 1, &failed)) goto done;
                 tc_after();
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    const uint64_t v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK);
+                    const uint64_t v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK) + 4 * (i & 1);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) product_of(out_at + gr * 64, sc_at + gr * 32 + x * 8, v + 2 * x, kHow, i > 0 || x > 0);
+                    for (int x = 0; x < 2; ++x)
+                        product_of(out_at + gr * 64, sc_at + 64 + (i & 1) * 32 + gr * 16 + x * 8, v + 2 * x, kHowOut, i > 0 || x > 0);
                 }
-                commit(o_done + 8 * w);
-                commit(v_empty + 8 * st);
-                if (i + 1 < n) {
-                    if (!bar_wait(o_done + 8 * w, i & 1, &failed)) goto done;
-                    tc_after();
-                    scores(next, 0);
-                    commit(s_full + 8 * w);
-                }
+                commit(o_done + 16 * w + 8 * (i & 1));
+                if ((i & 1) || i + 1 == subs) commit(v_empty + 8 * st);
             }
         }
     } else {
@@ -386,42 +388,46 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         // loads serves four rows ----
         registers_up<kRegsSoftmax>();
         const int w = warp >> 2, row0 = block * kBlockRows + w * kRows, mine = row0 + (warp & 3) * 32 + (lane >> 2), t2 = (lane & 3) * 2;
-        const uint32_t sc_at = tmem + ((uint32_t)(warp & 3) << 21) + w * 128, out_at = sc_at + 256;
+        const uint32_t sc_at = tmem + ((uint32_t)(warp & 3) << 21) + w * 256, out_at = sc_at + 128;
         const int least_hi = row0 < rows ? s.len - s.fresh + by_share(a, row0) + 1 : 0x7fffffff, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
         float m[4] = {kNothing, kNothing, kNothing, kNothing};
         uint64_t l[4] = {0, 0, 0, 0};                   // of the thread's even and odd columns
 #pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-            const int st = i % kStages, tok0 = lo + i * kKeys;
-            const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales) + t2 * NG, *vs = ks + NG * kKeys;
+        for (int i = 0; i < subs; ++i) {
+            const int st = (i >> 1) % kStages, tok0 = lo + i * kSub;
+            const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales) + ((i & 1) * kSub + t2) * NG, *vs = ks + NG * kKeys;
             if (!warp_wait(s_full + 8 * w, i & 1, &failed)) goto done;
             tc_after();
-            uint64_t sc[4][8];                          // rows 8 q + lane / 4, columns 8 j + t2 and the next
+            uint64_t sc[4][4];                          // rows 8 q + lane / 4, columns 8 j + t2 and the next
+            {
+                uint32_t x[2][16 * NG];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t x[32 * NG];
-                acc_ask_rows(sc_at + ((uint32_t)h << 20), x);
-                if (NG == 2) acc_ask_rows(sc_at + ((uint32_t)h << 20) + 64, x + 32 * (NG - 1));
-                acc_loaded(x);
+                for (int h = 0; h < 2; ++h) {
+                    acc_ask_rows(sc_at + ((uint32_t)h << 20), x[h]);
+                    if (NG == 2) acc_ask_rows(sc_at + ((uint32_t)h << 20) + kSub, x[h] + 16 * (NG - 1));
+                }
+                acc_loaded(x[0]);
+                acc_loaded(x[1]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 4; ++j) {
                     ulonglong2 k;
                     if (NG == 2) k = *reinterpret_cast<const ulonglong2 *>(ks + j * 8 * NG);
                     else k.x = *reinterpret_cast<const uint64_t *>(ks + j * 8 * NG), k.y = 0;
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        uint64_t v = mul_two(two(__uint_as_float(x[4 * j + 2 * b]), __uint_as_float(x[4 * j + 2 * b + 1])), k.x);
-                        if (NG == 2) v = fma_two(two(__uint_as_float(x[32 * (NG - 1) + 4 * j + 2 * b]), __uint_as_float(x[32 * (NG - 1) + 4 * j + 2 * b + 1])), k.y, v);
-                        sc[2 * h + b][j] = v;
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t *y = x[q >> 1] + 4 * j + 2 * (q & 1);
+                        uint64_t v = mul_two(two(__uint_as_float(y[0]), __uint_as_float(y[1])), k.x);
+                        if (NG == 2) v = fma_two(two(__uint_as_float(y[16 * (NG - 1)]), __uint_as_float(y[16 * (NG - 1) + 1])), k.y, v);
+                        sc[q][j] = v;
                     }
                 }
             }
-            const uint32_t gone = *reinterpret_cast<const volatile uint32_t *>(bad[st]);
+            const uint32_t gone = *reinterpret_cast<const volatile uint16_t *>(bad[st] + 2 * (i & 1));
             tc_before();
             __syncwarp();
             bar_arrive_if(s_read + 8 * w, lane == 0);         // scores, scales and `bad` are in registers
-            bar_arrive_if(k_read + 8 * st, lane == 0);
-            if (!(tok0 + kKeys <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
+            bar_arrive_if(k_read + 8 * st, lane == 0 && ((i & 1) || i + 1 == subs));
+            if (!(tok0 + kSub <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     int hi = 0x7fffffff, low = 0;       // a row of padding masks nothing
@@ -431,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     }
                     hi = min(hi, end);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < 4; ++j) {
                         float u, v;
                         apart(sc[q][j], u, v);
                         const int tok = tok0 + 8 * j + t2;
@@ -448,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             for (int q = 0; q < 4; ++q) {
                 top[q] = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 4; ++j) {
                     float u, v;
                     apart(sc[q][j], u, v);
                     top[q] = fmaxf(fmaxf(top[q], u), v);
@@ -467,14 +473,15 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     m[q] = now;
                     l[q] = mul_two(l[q], two(keep[q], keep[q]));
                 }
-                // (the scores of this tile were asked for after the last product with this group's probabilities was over)
                 if (i > 0) {
+                    if (!warp_wait(o_done + 16 * w + 8 * ((i - 1) & 1), (i - 1) >> 1 & 1, &failed)) goto done;
+                    tc_after();
+                    const float k0 = __shfl_sync(0xffffffffu, keep[0], (lane & 7) * 4), k1 = __shfl_sync(0xffffffffu, keep[1], (lane & 7) * 4);
+                    const float k2 = __shfl_sync(0xffffffffu, keep[2], (lane & 7) * 4), k3 = __shfl_sync(0xffffffffu, keep[3], (lane & 7) * 4);
+                    const float k = lane < 16 ? (lane < 8 ? k0 : k1) : (lane < 24 ? k2 : k3);
 #pragma unroll 1
                     for (int c0 = 0; c0 < NG * 64; c0 += 16) {
                         float v[16];
-                        const float k0 = __shfl_sync(0xffffffffu, keep[0], (lane & 7) * 4), k1 = __shfl_sync(0xffffffffu, keep[1], (lane & 7) * 4);
-                        const float k2 = __shfl_sync(0xffffffffu, keep[2], (lane & 7) * 4), k3 = __shfl_sync(0xffffffffu, keep[3], (lane & 7) * 4);
-                        const float k = lane < 16 ? (lane < 8 ? k0 : k1) : (lane < 24 ? k2 : k3);
                         acc_load16(out_at + c0, v);
 #pragma unroll
                         for (int x = 0; x < 16; ++x) v[x] *= k;
@@ -482,37 +489,34 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     }
                 }
             }
+            uint32_t p[NG][2][8];
 #pragma unroll
-            for (int j0 = 0; j0 < 8; j0 += 4) {
-                uint32_t p[NG][2][8];
+            for (int j = 0; j < 4; ++j) {
+                ulonglong2 f;
+                if (NG == 2) f = *reinterpret_cast<const ulonglong2 *>(vs + j * 8 * NG);
+                else f.x = *reinterpret_cast<const uint64_t *>(vs + j * 8 * NG), f.y = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    ulonglong2 f;
-                    if (NG == 2) f = *reinterpret_cast<const ulonglong2 *>(vs + (j0 + j) * 8 * NG);
-                    else f.x = *reinterpret_cast<const uint64_t *>(vs + (j0 + j) * 8 * NG), f.y = 0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float u, v;
-                        apart(add_two(sc[q][j0 + j], two(-m[q], -m[q])), u, v);
-                        const uint64_t e = two(power2(u), power2(v));
-                        l[q] = add_two(l[q], e);
-                        p[0][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.x));
-                        if (NG == 2) p[NG - 1][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.y));
-                    }
+                for (int q = 0; q < 4; ++q) {
+                    float u, v;
+                    apart(add_two(sc[q][j], two(-m[q], -m[q])), u, v);
+                    const uint64_t e = two(power2(u), power2(v));
+                    l[q] = add_two(l[q], e);
+                    p[0][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.x));
+                    if (NG == 2) p[NG - 1][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.y));
                 }
+            }
 #pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    pairs_store(sc_at + gr * 32 + j0 * 4, p[gr][0]);
-                    pairs_store(sc_at + gr * 32 + j0 * 4 + (16u << 16), p[gr][1]);
-                }
+            for (int gr = 0; gr < NG; ++gr) {
+                pairs_store(sc_at + 64 + (i & 1) * 32 + gr * 16, p[gr][0]);
+                pairs_store(sc_at + 64 + (i & 1) * 32 + gr * 16 + (16u << 16), p[gr][1]);
             }
             acc_stored();
             tc_before();
             __syncwarp();
-            bar_arrive_if(p_full + 8 * w, lane == 0);
+            bar_arrive_if(p_full + 16 * w + 8 * (i & 1), lane == 0);
         }
         // ---- the output: what is left in tensor memory, a row per thread, divided by the row's sum ----
-        if (n > 0 && !warp_wait(o_done + 8 * w, (n - 1) & 1, &failed)) goto done;
+        if (subs > 0 && !warp_wait(o_done + 16 * w + 8 * ((subs - 1) & 1), (subs - 1) >> 1 & 1, &failed)) goto done;
         tc_after();
         float sum = 0.0f;
 #pragma unroll
