@@ -126,14 +126,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     using S = Shape<D>;
     constexpr int NG = S::NG, kRow = S::kRow, kUnits = D / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[4 * kStages + 12];
+    __shared__ __align__(8) uint64_t bars[4 * kStages + 14];
     __shared__ int64_t warp_sum[kThreads / 32];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
     __shared__ uint32_t tmem_at;
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
-    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, k_read = v_empty + 8 * kStages, s_full = k_read + 8 * kStages, p_full = s_full + 16, o_done = p_full + 32, s_read = o_done + 32;
+    const uint32_t k_full = smem_addr(bars), v_full = k_full + 8 * kStages, v_empty = v_full + 8 * kStages, k_read = v_empty + 8 * kStages, s_full = k_read + 8 * kStages, p_full = s_full + 16, o_done = p_full + 32, s_read = o_done + 32, q_full = s_read + 16;
     // (p_full and o_done of a group: one for even, one for odd tiles.  A warp may be a tile ahead of the others' probabilities, and not every
     // product's end is waited for.)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_init(o_done + 16 * i, 1);
             bar_init(o_done + 16 * i + 8, 1);
             bar_init(s_read + 8 * i, 4);
+            bar_init(q_full + 8 * i, 4);
         }
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -209,43 +210,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     const int  lo  = a.window > 0 ? max(s.len - s.fresh + first_tok + 1 - a.window, 0) & ~15 : 0;
     const int  subs = end > lo ? (end - lo + kSub - 1) / kSub : 0, n = (subs + 1) / 2;
     if (tid == 0 && s.len > most) kv_record(a.status, seq, (int)most);
-
-    // ---- the queries: a row per thread; times 64 or 4, which the codes lack ----
-    if (warp < 8) {
-        const int r = tid & (kRows - 1), w = warp >> 2, row = block * kBlockRows + w * kRows + r;
-        const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
-        const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
-#pragma unroll
-        for (int cc = 0; cc < 2 * NG; ++cc) {
-            const int gr = cc >> 1, c = cc & 1;
-            uint4 v[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const __nv_bfloat16 *p = src + gr * 64 + c * 32 + t * 8;
-                v[t] = make_uint4(0, 0, 0, 0);
-                if (row < rows) {
-                    if (a.q_vec) {
-                        v[t] = *reinterpret_cast<const uint4 *>(p);
-                    } else {
-                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-                        v[t] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {              // sixteen bytes: channels 8 t + i and 8 t + i + 4
-                uint32_t x[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    x[t] = mul2(__byte_perm(i < 2 ? v[t].x : v[t].y, i < 2 ? v[t].z : v[t].w, i & 1 ? 0x7632 : 0x5410), i & 1 ? 0x40804080u : 0x42804280u);
-                *reinterpret_cast<uint4 *>(smem + S::kQ + (w * NG + gr) * S::kSlabQ + r * 128 + (((4 * c + i) ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-            }
-        }
-        to_engine();
-    }
-    tc_before();
-    __syncthreads();
-    tc_after();
 
     if (warp >= 8 && warp < 16) {
         registers_down<kRegsWorker>();
@@ -353,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                 commit(s_full + 8 * w);
             };
             if (subs > 0) {
-                if (!bar_wait(k_full, 0, &failed) || !bar_wait(v_full, 0, &failed)) goto done;
+                if (!bar_wait(q_full + 8 * w, 0, &failed) || !bar_wait(k_full, 0, &failed) || !bar_wait(v_full, 0, &failed)) goto done;
                 tc_after();
                 scores(0);
             }
@@ -390,6 +354,41 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         const int w = warp >> 2, row0 = block * kBlockRows + w * kRows, mine = row0 + (warp & 3) * 32 + (lane >> 2), t2 = (lane & 3) * 2;
         const uint32_t sc_at = tmem + ((uint32_t)(warp & 3) << 21) + w * 256, out_at = sc_at + 128;
         const int least_hi = row0 < rows ? s.len - s.fresh + by_share(a, row0) + 1 : 0x7fffffff, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
+        // ---- the queries: a row per thread; times 64 or 4, which the codes lack ----
+        {
+            const int r = tid & (kRows - 1), row = row0 + r, tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
+            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
+            uint4 v[NG * 8];
+#pragma unroll
+            for (int t = 0; t < NG * 8; ++t) {
+                v[t] = make_uint4(0, 0, 0, 0);
+                if (row < rows) {
+                    if (a.q_vec) {
+                        v[t] = *reinterpret_cast<const uint4 *>(src + t * 8);
+                    } else {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(src + t * 8);
+                        v[t] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                    }
+                }
+            }
+#pragma unroll
+            for (int cc = 0; cc < 2 * NG; ++cc) {
+                const int gr = cc >> 1, c = cc & 1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {              // sixteen bytes: channels 8 t + i and 8 t + i + 4
+                    uint32_t x[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint4 &y = v[cc * 4 + t];
+                        x[t] = mul2(__byte_perm(i < 2 ? y.x : y.y, i < 2 ? y.z : y.w, i & 1 ? 0x7632 : 0x5410), i & 1 ? 0x40804080u : 0x42804280u);
+                    }
+                    *reinterpret_cast<uint4 *>(smem + S::kQ + (w * NG + gr) * S::kSlabQ + r * 128 + (((4 * c + i) ^ (r & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                }
+            }
+            to_engine();
+            __syncwarp();
+            bar_arrive_if(q_full + 8 * w, lane == 0);
+        }
         float m[4] = {kNothing, kNothing, kNothing, kNothing};
         uint64_t l[4] = {0, 0, 0, 0};                   // of the thread's even and odd columns
 #pragma unroll 1
