@@ -16,11 +16,12 @@
 namespace symar {
 namespace {
 
-constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kSub = 32, kStages = 3, kRaw = 3;
+constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kSub = 32, kStages = 4, kRaw = 3;
 constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
-constexpr int kThreads = 32 * (8 + kWorkers + 4);      // two softmax groups of four warps, the workers, a warp for each group's products, two idle ones
-constexpr int kRegsSoftmax = 144, kRegsWorker = 72, kRegsRest = 48, kRegsLaunch = 96;
-static_assert(2 * kRegsSoftmax + 2 * kRegsWorker + kRegsRest <= 5 * kRegsLaunch, "the warpgroups' shares must not be above what a block is launched with");
+constexpr int kSoftmax = 16;                           // warps of the softmax: eight to a group of 128 rows, sixteen rows each
+constexpr int kThreads = 32 * (kSoftmax + kWorkers + 4);       // ... the workers, two warps for each group's products
+constexpr int kRegsSoftmax = 80, kRegsWorker = 72, kRegsRest = 40, kRegsLaunch = 72;
+static_assert(4 * kRegsSoftmax + 2 * kRegsWorker + kRegsRest <= 7 * kRegsLaunch, "the warpgroups' shares must not be above what a block is launched with");
 
 template <int D>
 struct Shape {
@@ -37,16 +38,6 @@ __device__ __forceinline__ void matrices_out(uint32_t addr, const uint32_t (&r)[
 {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-__device__ __forceinline__ void acc_store16(uint32_t addr, const float *v)
-{
-    uint32_t r[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-                 : "memory");
-}
 // Sixteen lanes and 32 columns, as the result of a matrix instruction lies in a warp: a thread has columns 8 j + 2 t and the next one of
 // lanes lane / 4 (v[4 j], v[4 j + 1]) and lane / 4 + 8 (v[4 j + 2], v[4 j + 3]), t = lane % 4.  Waited for later (acc_loaded).
 __device__ __forceinline__ void acc_ask_rows(uint32_t addr, uint32_t *r)
@@ -56,6 +47,13 @@ __device__ __forceinline__ void acc_ask_rows(uint32_t addr, uint32_t *r)
                    "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr));
 }
+__device__ __forceinline__ void acc_store_rows(uint32_t addr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
 // The same lanes, sixteen columns of pairs of bf16: a thread's pairs 4 j + t of lanes lane / 4 (v[2 j]) and lane / 4 + 8 (v[2 j + 1]).
 __device__ __forceinline__ void pairs_store(uint32_t addr, const uint32_t (&r)[8])
 {
@@ -63,22 +61,25 @@ __device__ __forceinline__ void pairs_store(uint32_t addr, const uint32_t (&r)[8
                  "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-// a product whose first operand is in tensor memory
-__device__ __forceinline__ void product_of(uint32_t acc, uint32_t a, uint64_t b, uint32_t how, uint32_t add)
+// Products and commits of the one lane that `on` names: the warp stays together, what it addresses stays in uniform registers.
+__device__ __forceinline__ void product_if(uint32_t acc, uint64_t a, uint64_t b, uint32_t how, uint32_t add, uint32_t on)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(acc),
-                 "r"(a), "l"(b), "r"(how), "r"(add) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(acc),
+                 "l"(a), "l"(b), "r"(how), "r"(add), "r"(on) : "memory");
+}
+// (the first operand in tensor memory)
+__device__ __forceinline__ void product_if(uint32_t acc, uint32_t a, uint64_t b, uint32_t how, uint32_t add, uint32_t on)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(acc),
+                 "r"(a), "l"(b), "r"(how), "r"(add), "r"(on) : "memory");
+}
+__device__ __forceinline__ void commit_if(uint32_t bar, uint32_t on)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+                 "r"(on) : "memory");
 }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-// sixteen columns, waited for later (acc_loaded)
-__device__ __forceinline__ void acc_ask16(uint32_t addr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(addr));
-}
 template <int N> __device__ __forceinline__ void acc_loaded(uint32_t (&r)[N])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -157,16 +158,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_init(k_full + 8 * i, kWorkers / 2);
             bar_init(v_full + 8 * i, kWorkers / 2);
             bar_init(v_empty + 8 * i, 2);
-            bar_init(k_read + 8 * i, 8);
+            bar_init(k_read + 8 * i, kSoftmax);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
-            bar_init(p_full + 16 * i, 4);
-            bar_init(p_full + 16 * i + 8, 4);
+            bar_init(p_full + 16 * i, kSoftmax / 2);
+            bar_init(p_full + 16 * i + 8, kSoftmax / 2);
             bar_init(o_done + 16 * i, 1);
             bar_init(o_done + 16 * i + 8, 1);
-            bar_init(s_read + 8 * i, 4);
-            bar_init(q_full + 8 * i, 4);
+            bar_init(s_read + 8 * i, kSoftmax / 2);
+            bar_init(q_full + 8 * i, kSoftmax / 2);
         }
         failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             flat += n;
         }
     }
-    if (warp == 16) {
+    if (warp == kSoftmax + kWorkers) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&tmem_at)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -211,10 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     const int  subs = end > lo ? (end - lo + kSub - 1) / kSub : 0, n = (subs + 1) / 2;
     if (tid == 0 && s.len > most) kv_record(a.status, seq, (int)most);
 
-    if (warp >= 8 && warp < 16) {
+    if (warp >= kSoftmax && warp < kSoftmax + kWorkers) {
         registers_down<kRegsWorker>();
         // ---- codes to operands ----
-        const int dw = warp - 8, c = dw & 3, side = dw >> 2, ps = 1 << a.c.page_shift, g = lane >> 2, t = lane & 3;
+        const int dw = warp - kSoftmax, c = dw & 3, side = dw >> 2, ps = 1 << a.c.page_shift, g = lane >> 2, t = lane & 3;
         unsigned char *raw = smem + S::kRawAt + dw * kRaw * S::kRawChunk;
         const uint32_t raw_addr = smem_addr(raw);
         int pages = -1;
@@ -295,72 +296,70 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_arrive_if((side ? v_full : k_full) + 8 * st, lane == 0);
         }
         copies_wait<0>();
-    } else if (warp >= 16) {
+    } else if (warp >= kSoftmax + kWorkers) {
         registers_down<kRegsRest>();
-        if (warp < 18 && elected()) {
-            // ---- a group's products, 32 keys at a time.  The next scores follow as soon as the softmax has read the ones before; there are two
-            // sets of probabilities.  (The softmax takes a set's place, and the scales of the values, without a wait of its own: when scores are
-            // there, the values are, and the products with the probabilities of two times before are over.) ----
-            constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
-            constexpr uint32_t kHowScores = kHow | ((uint32_t)(kSub / 8) << 17), kHowOut = kHow | (8u << 17);
-            const int w = warp - 16;
-            const uint32_t sc_at = tmem + w * 256, out_at = sc_at + 128;
-            auto scores = [&](int i) {
-                const int st = (i >> 1) % kStages;
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    const uint64_t q = operand(base + S::kQ + (w * NG + gr) * S::kSlabQ);
-                    const uint64_t k = operand(base + S::kKV + st * S::kStage + gr * S::kSlabK + (i & 1) * kSub * 128);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) product(sc_at + gr * kSub, q + 2 * x, k + 2 * x, kHowScores, x > 0);
-                }
-                commit(s_full + 8 * w);
-            };
-            if (subs > 0) {
-                if (!bar_wait(q_full + 8 * w, 0, &failed) || !bar_wait(k_full, 0, &failed) || !bar_wait(v_full, 0, &failed)) goto done;
-                tc_after();
-                scores(0);
-            }
+        // ---- products, 32 keys at a time: a warp for a group's scores, one for its outputs.  The next scores follow as soon as the softmax has
+        // read the ones before; there are two sets of probabilities.  (The softmax takes a set's place, and the scales of the values, without a
+        // wait of its own: when scores are there, the values are, and the product with the probabilities of two times before is over.) ----
+        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
+        constexpr uint32_t kHowScores = kHow | ((uint32_t)(kSub / 8) << 17), kHowOut = kHow | (8u << 17);
+        const int which = __shfl_sync(0xffffffffu, warp - (kSoftmax + kWorkers), 0), w = which & 1;
+        const uint32_t sc_at = __shfl_sync(0xffffffffu, tmem, 0) + w * 256, out_at = sc_at + 128, at = __shfl_sync(0xffffffffu, base, 0);
+        const uint32_t on = elected();
+        if (which < 2) {
+            if (subs > 0 && !warp_wait(q_full + 8 * w, 0, &failed)) goto done;
 #pragma unroll 1
             for (int i = 0; i < subs; ++i) {
                 const int st = (i >> 1) % kStages;
-                if (i + 1 < subs) {
-                    if (i & 1) {
-                        const int next = ((i + 1) >> 1) % kStages;
-                        const uint32_t round = (((i + 1) >> 1) / kStages) & 1;
-                        if (!bar_wait(k_full + 8 * next, round, &failed) || !bar_wait(v_full + 8 * next, round, &failed)) goto done;
-                    }
-                    if (!bar_wait(s_read + 8 * w, i & 1, &failed)) goto done;
-                    tc_after();
-                    scores(i + 1);
+                if (!(i & 1)) {
+                    const uint32_t round = ((i >> 1) / kStages) & 1;
+                    if (!warp_wait(k_full + 8 * st, round, &failed) || !warp_wait(v_full + 8 * st, round, &failed)) goto done;
                 }
-                if (!bar_wait(p_full + 16 * w + 8 * (i & 1), i >> 1 & 1, &failed)) goto done;
+                if (i > 1 && !warp_wait(o_done + 16 * w + 8 * (i & 1), (i >> 1) - 1 & 1, &failed)) goto done;
+                if (i > 0 && !warp_wait(s_read + 8 * w, (i - 1) & 1, &failed)) goto done;
                 tc_after();
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
-                    const uint64_t v = operand(base + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK) + 4 * (i & 1);
+                    const uint64_t q = operand(at + S::kQ + (w * NG + gr) * S::kSlabQ);
+                    const uint64_t k = operand(at + S::kKV + st * S::kStage + gr * S::kSlabK + (i & 1) * kSub * 128);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) product_if(sc_at + gr * kSub, q + 2 * x, k + 2 * x, kHowScores, x > 0, on);
+                }
+                commit_if(s_full + 8 * w, on);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < subs; ++i) {
+                const int st = (i >> 1) % kStages;
+                if (!(i & 1) && !warp_wait(v_full + 8 * st, ((i >> 1) / kStages) & 1, &failed)) goto done;
+                if (!warp_wait(p_full + 16 * w + 8 * (i & 1), i >> 1 & 1, &failed)) goto done;
+                tc_after();
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    const uint64_t v = operand(at + S::kKV + st * S::kStage + (NG + gr) * S::kSlabK) + 4 * (i & 1);
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
-                        product_of(out_at + gr * 64, sc_at + 64 + (i & 1) * 32 + gr * 16 + x * 8, v + 2 * x, kHowOut, i > 0 || x > 0);
+                        product_if(out_at + gr * 64, sc_at + 64 + (i & 1) * 32 + gr * 16 + x * 8, v + 2 * x, kHowOut, i > 0 || x > 0, on);
                 }
-                commit(o_done + 16 * w + 8 * (i & 1));
-                if ((i & 1) || i + 1 == subs) commit(v_empty + 8 * st);
+                commit_if(o_done + 16 * w + 8 * (i & 1), on);
+                if ((i & 1) || i + 1 == subs) commit_if(v_empty + 8 * st, on);
             }
         }
     } else {
-        // ---- softmax: a thread has four rows of its warp's 32 (8 q + lane / 4) and every eighth pair of columns, so that a scale that it
-        // loads serves four rows ----
+        // ---- softmax: a warp has sixteen rows of its quarter of tensor memory, a thread two of them (8 b + lane / 4) and every fourth pair of
+        // columns, so that a scale that it loads serves two rows ----
         registers_up<kRegsSoftmax>();
-        const int w = warp >> 2, row0 = block * kBlockRows + w * kRows, mine = row0 + (warp & 3) * 32 + (lane >> 2), t2 = (lane & 3) * 2;
-        const uint32_t sc_at = tmem + ((uint32_t)(warp & 3) << 21) + w * 256, out_at = sc_at + 128;
+        const int w = warp >> 3, half = warp >> 2 & 1, row0 = block * kBlockRows + w * kRows, t2 = (lane & 3) * 2;
+        const int mine = row0 + (warp & 3) * 32 + half * 16 + (lane >> 2);
+        const uint32_t sc_at = tmem + ((uint32_t)(2 * (warp & 3) + half) << 20) + w * 256, out_at = sc_at + 128;
         const int least_hi = row0 < rows ? s.len - s.fresh + by_share(a, row0) + 1 : 0x7fffffff, most_lo = a.window > 0 ? s.len - s.fresh + last_tok + 1 - a.window : 0;
-        // ---- the queries: a row per thread; times 64 or 4, which the codes lack ----
+        // ---- the queries: half a row per thread; times 64 or 4, which the codes lack ----
         {
-            const int r = tid & (kRows - 1), row = row0 + r, tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
-            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head;
-            uint4 v[NG * 8];
+            const int r = (tid & 255) >> 1, side = tid & 1, row = row0 + r, tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
+            const __nv_bfloat16 *src = a.q + (int64_t)(s.start + tok) * a.q_ld + (int64_t)(head * a.share + hh) * a.q_head + side * (D / 2);
+            uint4 v[NG * 4];
 #pragma unroll
-            for (int t = 0; t < NG * 8; ++t) {
+            for (int t = 0; t < NG * 4; ++t) {
                 v[t] = make_uint4(0, 0, 0, 0);
                 if (row < rows) {
                     if (a.q_vec) {
@@ -372,8 +371,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                 }
             }
 #pragma unroll
-            for (int cc = 0; cc < 2 * NG; ++cc) {
-                const int gr = cc >> 1, c = cc & 1;
+            for (int cc = 0; cc < NG; ++cc) {
+                const int gr = NG == 2 ? side : 0, c = NG == 2 ? cc : side;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {              // sixteen bytes: channels 8 t + i and 8 t + i + 4
                     uint32_t x[4];
@@ -389,35 +388,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             __syncwarp();
             bar_arrive_if(q_full + 8 * w, lane == 0);
         }
-        float m[4] = {kNothing, kNothing, kNothing, kNothing};
-        uint64_t l[4] = {0, 0, 0, 0};                   // of the thread's even and odd columns
+        float m[2] = {kNothing, kNothing};
+        uint64_t l[2] = {0, 0};                         // of the thread's even and odd columns
 #pragma unroll 1
         for (int i = 0; i < subs; ++i) {
             const int st = (i >> 1) % kStages, tok0 = lo + i * kSub;
             const float *ks = reinterpret_cast<const float *>(smem + S::kSc + st * S::kScales) + ((i & 1) * kSub + t2) * NG, *vs = ks + NG * kKeys;
             if (!warp_wait(s_full + 8 * w, i & 1, &failed)) goto done;
             tc_after();
-            uint64_t sc[4][4];                          // rows 8 q + lane / 4, columns 8 j + t2 and the next
+            uint64_t sc[2][4];                          // rows 8 b + lane / 4, columns 8 j + t2 and the next
             {
-                uint32_t x[2][16 * NG];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    acc_ask_rows(sc_at + ((uint32_t)h << 20), x[h]);
-                    if (NG == 2) acc_ask_rows(sc_at + ((uint32_t)h << 20) + kSub, x[h] + 16 * (NG - 1));
-                }
-                acc_loaded(x[0]);
-                acc_loaded(x[1]);
+                uint32_t x[16 * NG];
+                acc_ask_rows(sc_at, x);
+                if (NG == 2) acc_ask_rows(sc_at + kSub, x + 16 * (NG - 1));
+                acc_loaded(x);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     ulonglong2 k;
                     if (NG == 2) k = *reinterpret_cast<const ulonglong2 *>(ks + j * 8 * NG);
                     else k.x = *reinterpret_cast<const uint64_t *>(ks + j * 8 * NG), k.y = 0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t *y = x[q >> 1] + 4 * j + 2 * (q & 1);
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t *y = x + 4 * j + 2 * b;
                         uint64_t v = mul_two(two(__uint_as_float(y[0]), __uint_as_float(y[1])), k.x);
                         if (NG == 2) v = fma_two(two(__uint_as_float(y[16 * (NG - 1)]), __uint_as_float(y[16 * (NG - 1) + 1])), k.y, v);
-                        sc[q][j] = v;
+                        sc[b][j] = v;
                     }
                 }
             }
@@ -428,132 +423,125 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_arrive_if(k_read + 8 * st, lane == 0 && ((i & 1) || i + 1 == subs));
             if (!(tok0 + kSub <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int b = 0; b < 2; ++b) {
                     int hi = 0x7fffffff, low = 0;       // a row of padding masks nothing
-                    if (mine + 8 * q < rows) {
-                        hi  = s.len - s.fresh + by_share(a, mine + 8 * q) + 1;
+                    if (mine + 8 * b < rows) {
+                        hi  = s.len - s.fresh + by_share(a, mine + 8 * b) + 1;
                         low = a.window > 0 ? max(hi - a.window, 0) : 0;
                     }
                     hi = min(hi, end);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float u, v;
-                        apart(sc[q][j], u, v);
+                        apart(sc[b][j], u, v);
                         const int tok = tok0 + 8 * j + t2;
                         const bool lost = gone >> 8 * (j >> 1) & 1u;
                         if (tok >= hi || tok < low || lost) u = -INFINITY;
                         if (tok + 1 >= hi || tok + 1 < low || lost) v = -INFINITY;
-                        sc[q][j] = two(u, v);
+                        sc[b][j] = two(u, v);
                     }
                 }
             }
-            float top[4];
-            bool  more = false;
+            float top[2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                top[q] = -INFINITY;
+            for (int b = 0; b < 2; ++b) {
+                top[b] = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float u, v;
-                    apart(sc[q][j], u, v);
-                    top[q] = fmaxf(fmaxf(top[q], u), v);
+                    apart(sc[b][j], u, v);
+                    top[b] = fmaxf(fmaxf(top[b], u), v);
                 }
-                more |= top[q] > m[q] + 8.0f;
             }
             // (the maximum in use may lie up to 2^8 below the true one)
-            if (__any_sync(0xffffffffu, more)) {
-                float keep[4];
+            if (__any_sync(0xffffffffu, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+                float keep[2];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 1));
-                    top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], 2));
-                    const float now = fmaxf(top[q], m[q]);
-                    keep[q] = power2(m[q] - now);
-                    m[q] = now;
-                    l[q] = mul_two(l[q], two(keep[q], keep[q]));
+                for (int b = 0; b < 2; ++b) {
+                    top[b] = fmaxf(top[b], __shfl_xor_sync(0xffffffffu, top[b], 1));
+                    top[b] = fmaxf(top[b], __shfl_xor_sync(0xffffffffu, top[b], 2));
+                    const float now = fmaxf(top[b], m[b]);
+                    keep[b] = power2(m[b] - now);
+                    m[b] = now;
+                    l[b] = mul_two(l[b], two(keep[b], keep[b]));
                 }
                 if (i > 0) {
                     if (!warp_wait(o_done + 16 * w + 8 * ((i - 1) & 1), (i - 1) >> 1 & 1, &failed)) goto done;
                     tc_after();
-                    const float k0 = __shfl_sync(0xffffffffu, keep[0], (lane & 7) * 4), k1 = __shfl_sync(0xffffffffu, keep[1], (lane & 7) * 4);
-                    const float k2 = __shfl_sync(0xffffffffu, keep[2], (lane & 7) * 4), k3 = __shfl_sync(0xffffffffu, keep[3], (lane & 7) * 4);
-                    const float k = lane < 16 ? (lane < 8 ? k0 : k1) : (lane < 24 ? k2 : k3);
 #pragma unroll 1
-                    for (int c0 = 0; c0 < NG * 64; c0 += 16) {
-                        float v[16];
-                        acc_load16(out_at + c0, v);
+                    for (int c0 = 0; c0 < D; c0 += 32) {
+                        uint32_t v[16];
+                        acc_ask_rows(out_at + c0, v);
+                        acc_loaded(v);
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) v[x] *= k;
-                        acc_store16(out_at + c0, v);
+                        for (int x = 0; x < 16; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * keep[x >> 1 & 1]);
+                        acc_store_rows(out_at + c0, v);
                     }
                 }
             }
-            uint32_t p[NG][2][8];
+            uint32_t p[NG][8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 ulonglong2 f;
                 if (NG == 2) f = *reinterpret_cast<const ulonglong2 *>(vs + j * 8 * NG);
                 else f.x = *reinterpret_cast<const uint64_t *>(vs + j * 8 * NG), f.y = 0;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int b = 0; b < 2; ++b) {
                     float u, v;
-                    apart(add_two(sc[q][j], two(-m[q], -m[q])), u, v);
+                    apart(add_two(sc[b][j], two(-m[b], -m[b])), u, v);
                     const uint64_t e = two(power2(u), power2(v));
-                    l[q] = add_two(l[q], e);
-                    p[0][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.x));
-                    if (NG == 2) p[NG - 1][q >> 1][2 * j + (q & 1)] = pack_two(mul_two(e, f.y));
+                    l[b] = add_two(l[b], e);
+                    p[0][2 * j + b] = pack_two(mul_two(e, f.x));
+                    if (NG == 2) p[NG - 1][2 * j + b] = pack_two(mul_two(e, f.y));
                 }
             }
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                pairs_store(sc_at + 64 + (i & 1) * 32 + gr * 16, p[gr][0]);
-                pairs_store(sc_at + 64 + (i & 1) * 32 + gr * 16 + (16u << 16), p[gr][1]);
-            }
+            for (int gr = 0; gr < NG; ++gr) pairs_store(sc_at + 64 + (i & 1) * 32 + gr * 16, p[gr]);
             acc_stored();
             tc_before();
             __syncwarp();
             bar_arrive_if(p_full + 16 * w + 8 * (i & 1), lane == 0);
         }
-        // ---- the output: what is left in tensor memory, a row per thread, divided by the row's sum ----
+        // ---- the output: what is left in tensor memory, divided by the row's sum.  Column 8 j + g of 32 is channel 4 g + j: a thread has eight
+        // neighbouring channels of each of its rows ----
         if (subs > 0 && !warp_wait(o_done + 16 * w + 8 * ((subs - 1) & 1), (subs - 1) >> 1 & 1, &failed)) goto done;
         tc_after();
-        float sum = 0.0f;
+        float inv[2];
+        __nv_bfloat16 *out[2];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int b = 0; b < 2; ++b) {
             float u, v;
-            apart(l[q], u, v);
+            apart(l[b], u, v);
             u += v;
             u += __shfl_xor_sync(0xffffffffu, u, 1);
             u += __shfl_xor_sync(0xffffffffu, u, 2);
-            u = __shfl_sync(0xffffffffu, u, (lane & 7) * 4);
-            if (lane >> 3 == q) sum = u;
+            inv[b] = u > 0.0f ? 1.0f / u : (u == 0.0f ? 0.0f : u);
+            const int row = min(mine + 8 * b, rows - 1), tok = by_share(a, row);
+            out[b] = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + row - tok * a.share) * a.out_head + t2 * 4;
         }
-        const int row = row0 + (tid & (kRows - 1));
-        const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);
-        const int tok = by_share(a, min(row, rows - 1)), hh = min(row, rows - 1) - tok * a.share;
-        __nv_bfloat16 *out = a.out + (int64_t)(s.start + tok) * a.out_ld + (int64_t)(head * a.share + hh) * a.out_head;
 #pragma unroll 1
         for (int at = 0; at < D; at += 32) {
-            uint32_t v[32];
+            uint32_t v[16];
 #pragma unroll
-            for (int x = 0; x < 32; ++x) v[x] = 0;
-            if (n > 0) {
-                acc_ask16(out_at + at, *reinterpret_cast<uint32_t(*)[16]>(v));
-                acc_ask16(out_at + at + 16, *reinterpret_cast<uint32_t(*)[16]>(v + 16));
+            for (int x = 0; x < 16; ++x) v[x] = 0;
+            if (subs > 0) {
+                acc_ask_rows(out_at + at, v);
                 acc_loaded(v);
             }
-            if (row < rows) {
-                // column 8 i + g is channel 4 g + i
 #pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const uint32_t x = pack_bf16(64.0f * __uint_as_float(v[g]) * inv, 4.0f * __uint_as_float(v[8 + g]) * inv);
-                    const uint32_t y = pack_bf16(64.0f * __uint_as_float(v[16 + g]) * inv, 4.0f * __uint_as_float(v[24 + g]) * inv);
-                    __nv_bfloat16 *p = out + at + 4 * g;
+            for (int b = 0; b < 2; ++b) {
+                if (mine + 8 * b < rows) {
+                    auto of = [&](int j, int g) { return (j & 1 ? 4.0f : 64.0f) * __uint_as_float(v[4 * j + 2 * b + g]) * inv[b]; };
+                    const uint4 x = make_uint4(pack_bf16(of(0, 0), of(1, 0)), pack_bf16(of(2, 0), of(3, 0)), pack_bf16(of(0, 1), of(1, 1)), pack_bf16(of(2, 1), of(3, 1)));
+                    __nv_bfloat16 *to = out[b] + at;
                     if (a.out_vec) {
-                        *reinterpret_cast<uint2 *>(p) = make_uint2(x, y);
+                        *reinterpret_cast<uint2 *>(to) = make_uint2(x.x, x.y);
+                        *reinterpret_cast<uint2 *>(to + 4) = make_uint2(x.z, x.w);
                     } else {
-                        uint16_t *h = reinterpret_cast<uint16_t *>(p);
-                        h[0] = (uint16_t)x; h[1] = (uint16_t)(x >> 16); h[2] = (uint16_t)y; h[3] = (uint16_t)(y >> 16);
+                        uint16_t *h = reinterpret_cast<uint16_t *>(to);
+                        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) h[2 * z] = (uint16_t)y[z], h[2 * z + 1] = (uint16_t)(y[z] >> 16);
                     }
                 }
             }
@@ -572,7 +560,7 @@ done:
     tc_before();
     __syncthreads();
     tc_after();
-    if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == kSoftmax + kWorkers) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // items that the call has at most: a block each (blocks beyond the last item leave at once)
