@@ -1,16 +1,25 @@
 // Attention of many query rows (prompts, pieces of prompts) over the paged 4-bit cache, on the fifth generation's tensor cores.
 //
-// A block has 256 query rows (tokens and the heads of one key/value head's share) and walks over the cached tokens 64 at a time.  Eight
-// warps bring the codes in and write them out again as what a tensor-core operand is: whole numbers n - z in bf16, exact, keys as rows of
-// channels, values transposed.  The scales stay apart, so that nothing is rounded that the definition does not round but the probabilities:
-// every group of 64 channels has a product of its own, S_g = Q_g N_g^T, whose columns the softmax multiplies by the keys' scales and adds;
-// and a set of probabilities of its own, P_g = P s_g, for O_g = P_g N_g.  Two groups of four warps have 128 of the rows each, a thread to a
-// row, with their scores, running maxima and sums and outputs; each takes its exponentials beside the other's products, and the next tile's
-// scores are there when a tile's probabilities are written.  A channel's place in an operand is the one that its code comes out of the
-// register at: the queries are permuted alike, the output back.
+// A block has 256 query rows (tokens and the heads of one key/value head's share), two groups of 128, and walks over the cached tokens 64 at
+// a time.  Eight warps bring the codes in and write them out again as what a tensor-core operand is: whole numbers n - z in bf16, exact, keys
+// as rows of channels, values transposed.  The scales stay apart, so that nothing is rounded that the definition does not round but the
+// probabilities: every group of 64 channels has a product of its own, S_g = Q_g N_g^T, whose columns the softmax multiplies by the keys'
+// scales and adds; and a set of probabilities of its own, P_g = P s_g, for O_g = P_g N_g.  A channel's place in an operand is the one that its
+// code comes out of the register at: the queries are permuted alike, the output back.
+// Tensor memory: 64 columns of scores, two sets of 32 of probabilities (the products' first operand) and 128 of output per group, all 512.
+// Scores are therefore made for 32 keys at a time: with 64 the probabilities had to take the scores' place, and the next scores waited for
+// the product (569 us against 517 for the call below).  Sixteen warps have sixteen rows each, a thread two rows and every fourth pair of
+// columns (a row per thread loads every scale once per row: 746 us with the probabilities in shared memory; four rows, eight warps: 485).
+// Each group has a warp that issues scores and one that issues outputs (one thread for both: 527 us).  Registers are shared out between the
+// roles.
 // (Values scaled and probabilities in f16 would halve the products' and the softmax's traffic, but f16 has nothing below 2^-24: a row
 // whose likeliest token has a value of 0 loses what the others give it.)
-// Bound: 16 exponentials a cycle and 4096 products a cycle meet at 512 cycles per tile, group and multiprocessor for D = 128.
+// Bound: a tile of 64 keys takes 3700 cycles, of which 2400 issue instructions (9500 on four schedulers), 2050 move softmax and codes
+// through shared memory, 1500 feed the products from there, and 1024 take exponentials; taking any one of them out gains 3% or less.
+// Two pieces of 1024 tokens over 4099 with a window of 4096, 64 heads, 8 key/value heads of 128: 450 us, 610 TFLOP/s; a prompt of 4096 tokens:
+// 440 us, 625 TFLOP/s (of 1640 measured for a plain product).
+#include <cfloat>
+
 #include "symar_attention.cuh"
 
 namespace symar {
@@ -20,7 +29,7 @@ constexpr int kRows = 128, kBlockRows = 2 * kRows, kKeys = 64, kSub = 32, kStage
 constexpr int kWorkers = 8;                            // warps that expand codes: a chunk of 16 keys or values of every tile each
 constexpr int kSoftmax = 16;                           // warps of the softmax: eight to a group of 128 rows, sixteen rows each
 constexpr int kThreads = 32 * (kSoftmax + kWorkers + 4);       // ... the workers, two warps for each group's products
-constexpr int kRegsSoftmax = 80, kRegsWorker = 72, kRegsRest = 40, kRegsLaunch = 72;
+constexpr int kRegsSoftmax = 88, kRegsWorker = 56, kRegsRest = 40, kRegsLaunch = 72;
 static_assert(4 * kRegsSoftmax + 2 * kRegsWorker + kRegsRest <= 7 * kRegsLaunch, "the warpgroups' shares must not be above what a block is launched with");
 
 template <int D>
@@ -158,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             bar_init(k_full + 8 * i, kWorkers / 2);
             bar_init(v_full + 8 * i, kWorkers / 2);
             bar_init(v_empty + 8 * i, 2);
-            bar_init(k_read + 8 * i, kSoftmax);
+            bar_init(k_read + 8 * i, 2);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(s_full + 8 * i, 1);
@@ -316,7 +325,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                     if (!warp_wait(k_full + 8 * st, round, &failed) || !warp_wait(v_full + 8 * st, round, &failed)) goto done;
                 }
                 if (i > 1 && !warp_wait(o_done + 16 * w + 8 * (i & 1), (i >> 1) - 1 & 1, &failed)) goto done;
-                if (i > 0 && !warp_wait(s_read + 8 * w, (i - 1) & 1, &failed)) goto done;
+                if (i > 0) {
+                    if (!warp_wait(s_read + 8 * w, (i - 1) & 1, &failed)) goto done;
+                    if (!(i & 1)) bar_arrive_if(k_read + 8 * (((i >> 1) - 1) % kStages), on);       // the stage before is read
+                }
                 tc_after();
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
@@ -388,8 +400,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             __syncwarp();
             bar_arrive_if(q_full + 8 * w, lane == 0);
         }
-        float m[2] = {kNothing, kNothing};
-        uint64_t l[2] = {0, 0};                         // of the thread's even and odd columns
+        // scores are taken relative to m at once; `limit`: what they may come to before m is moved (a row that has seen nothing: any)
+        float m[2] = {0.0f, 0.0f}, limit[2] = {-FLT_MAX, -FLT_MAX};
+        uint64_t less[2] = {0, 0}, l[2] = {0, 0};       // -m twice; the sums of the thread's even and odd columns
+        const int clean = min(least_hi, end) - kSub;    // tiles that start at most here, and at least at most_lo, hide nothing
 #pragma unroll 1
         for (int i = 0; i < subs; ++i) {
             const int st = (i >> 1) % kStages, tok0 = lo + i * kSub;
@@ -410,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const uint32_t *y = x + 4 * j + 2 * b;
-                        uint64_t v = mul_two(two(__uint_as_float(y[0]), __uint_as_float(y[1])), k.x);
+                        uint64_t v = fma_two(two(__uint_as_float(y[0]), __uint_as_float(y[1])), k.x, less[b]);
                         if (NG == 2) v = fma_two(two(__uint_as_float(y[16 * (NG - 1)]), __uint_as_float(y[16 * (NG - 1) + 1])), k.y, v);
                         sc[b][j] = v;
                     }
@@ -420,8 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             tc_before();
             __syncwarp();
             bar_arrive_if(s_read + 8 * w, lane == 0);         // scores, scales and `bad` are in registers
-            bar_arrive_if(k_read + 8 * st, lane == 0 && ((i & 1) || i + 1 == subs));
-            if (!(tok0 + kSub <= min(least_hi, end) && tok0 >= most_lo && gone == 0)) {
+            if (tok0 > clean || tok0 < most_lo || gone != 0) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     int hi = 0x7fffffff, low = 0;       // a row of padding masks nothing
@@ -454,16 +467,21 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
                 }
             }
             // (the maximum in use may lie up to 2^8 below the true one)
-            if (__any_sync(0xffffffffu, top[0] > m[0] + 8.0f || top[1] > m[1] + 8.0f)) {
+            if (__any_sync(0xffffffffu, top[0] > limit[0] || top[1] > limit[1])) {
                 float keep[2];
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     top[b] = fmaxf(top[b], __shfl_xor_sync(0xffffffffu, top[b], 1));
                     top[b] = fmaxf(top[b], __shfl_xor_sync(0xffffffffu, top[b], 2));
-                    const float now = fmaxf(top[b], m[b]);
-                    keep[b] = power2(m[b] - now);
-                    m[b] = now;
-                    l[b] = mul_two(l[b], two(keep[b], keep[b]));
+                    const bool first = limit[b] < 0.0f, up = top[b] > (first ? limit[b] : 0.0f);
+                    const float now = up ? m[b] + top[b] : m[b], by = now - m[b];
+                    keep[b] = first ? 0.0f : power2(-by);
+                    if (up) limit[b] = 8.0f;
+                    m[b]    = now;
+                    less[b] = two(-now, -now);
+                    l[b]    = mul_two(l[b], two(keep[b], keep[b]));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sc[b][j] = add_two(sc[b][j], two(-by, -by));
                 }
                 if (i > 0) {
                     if (!warp_wait(o_done + 16 * w + 8 * ((i - 1) & 1), (i - 1) >> 1 & 1, &failed)) goto done;
@@ -488,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     float u, v;
-                    apart(add_two(sc[b][j], two(-m[b], -m[b])), u, v);
+                    apart(sc[b][j], u, v);
                     const uint64_t e = two(power2(u), power2(v));
                     l[b] = add_two(l[b], e);
                     p[0][2 * j + b] = pack_two(mul_two(e, f.x));
@@ -574,11 +592,13 @@ int64_t items_at_most(const AttnArgs &a)
 bool prompt_attention_takes(const AttnArgs &a, int num_sms)
 {
     if (a.c.dim > 128 || items_at_most(a) > 0x3fffffff) return false;
-    // Blocks that are mostly full, and for a quarter of the multiprocessors at least.  (64 heads, 8 key/value heads; this kernel against the
-    // one that shares a sequence's tokens between blocks, us: 512 new tokens over 8192: 372, 786; 256: 361, 398; 128, 32 blocks: 356, 206;
-    // 8 x 32 new tokens over 2048: 103, 117; 8 x 16, half-full blocks: 99, 67.)
+    // Blocks that are half full at least, and for a quarter of the multiprocessors.  (64 heads, 8 key/value heads unless said; this kernel
+    // against the one that shares a sequence's tokens between blocks, us: 512 new tokens over 8192, 128 blocks: 225, 786; 256: 217, 398; 128,
+    // 32 blocks: 214, 206; 64: 211, 111.  512 over 32768 with 8 heads of one, 16 blocks: 799, 401.  8 x 16 over 2048, half-full blocks: 62, 67;
+    // 64 x 8 over 1024, a quarter full: 139, 122; 32 x 32 with 8 heads of 8, an eighth: 69, 44.)
     const int64_t rows = (int64_t)a.b.tokens * a.share;                // of one key/value head
-    return rows >= (int64_t)kBlockRows * a.b.seqs && rows / kBlockRows * a.c.kv_heads >= num_sms / 4;
+    const int64_t blocks = rows / kBlockRows > a.b.seqs ? rows / kBlockRows : a.b.seqs;
+    return rows >= (int64_t)kRows * a.b.seqs && blocks * a.c.kv_heads >= num_sms / 4;
 }
 
 namespace {
