@@ -347,15 +347,13 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
             }
             uint4 u[kOf], next[kOf];
             int64_t byte = (int64_t)k_lo * 128 + c * 16;
+            // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece, which begins in the row)
             pieces<kOf>(u, at, how, byte, true, 4, ws, xs);
+            pieces<kOf>(next, at, how, byte + 128, a.k - k_lo * kSlice - c * 8 - kSlice + 8 > 0, 4, ws, xs);
+            byte += 128;
 #pragma unroll 2            // (the pieces on their way change places with those in hand without a copy, which would wait for them)
             for (int ks = k_lo; ks < k_hi; ++ks) {
-                // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece, which
-                // begins in the row)
-                byte += 128;
                 const int left = a.k - ks * kSlice - c * 8;
-                const bool more = left - kSlice + 8 > 0;
-                pieces<kOf>(next, at, how, byte, more, 4, ws, xs);
                 if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 unsigned char *dst = ring + st * S::kStage;
 #pragma unroll
@@ -366,6 +364,9 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                     if (j < 4 || to < NT) *reinterpret_cast<uint4 *>(dst + (j < 4 ? 0 : S::kA) + to * 128 + ((c ^ (to & 7)) << 4)) = v;
                     u[j] = next[j];
                 }
+                // asked for a whole slice before they are joined
+                byte += 128;
+                pieces<kOf>(next, at, how, byte, ks + 1 < k_hi && left - 2 * kSlice + 8 > 0, 4, ws, xs);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 bar_arrive(full + 8 * st);
                 if (++st == S::kStages) st = 0, ++round;
