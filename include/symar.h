@@ -436,7 +436,7 @@ const char *symar_last_cuda_error(void);
  *
  * Conventions.  Plain device pointers; every stride is in ELEMENTS of the tensor it belongs to and the
  * innermost axis is contiguous.  Strides are not negative; they may be larger than the extent they cover, and 0
- * where an operand is shared.  Calls enqueue on `cuda_stream`, return a status and may be captured in a CUDA graph; they
+ * where an operand is shared; rows that a call writes do not overlap.  Calls enqueue on `cuda_stream`, return a status and may be captured in a CUDA graph; they
  * allocate nothing.  Results are deterministic: no sum depends on the order in which blocks run.       */
 
 typedef enum {

@@ -624,6 +624,9 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     if (!(args->scale >= 0.0f) || std::isinf(args->scale)) return SYMAR_ERR_INVAL;
     if (batch->tokens == 0) return SYMAR_OK;
     if (!args->q || !args->out || ((uintptr_t)args->q | (uintptr_t)args->out) % 2) return SYMAR_ERR_INVAL;
+    if (args->q_ld < 0 || args->q_head < 0 || args->out_ld < 0 || args->out_head < 0 ||
+        kv_rows_meet(batch->tokens, args->q_heads, a.c.dim, args->out_ld, args->out_head))
+        return SYMAR_ERR_INVAL;
     a.q          = (const __nv_bfloat16 *)args->q;
     a.out        = (__nv_bfloat16 *)args->out;
     a.q_ld       = args->q_ld;

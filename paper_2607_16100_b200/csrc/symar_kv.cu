@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads) table_kernel(const TableArgs a)
 bool make_rows(Rows *r, const void *p, int64_t ld, int64_t head, int dtype)
 {
     const int64_t vec = dtype == SYMAR_F32 ? 4 : 8;
-    if ((uintptr_t)p % (dtype == SYMAR_F32 ? 4 : 2)) return false;
+    if ((uintptr_t)p % (dtype == SYMAR_F32 ? 4 : 2) || ld < 0 || head < 0) return false;
     r->p    = (char *)const_cast<void *>(p);
     r->ld   = ld;
     r->head = head;
@@ -619,7 +619,8 @@ int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_k
     if (!make_rows(&a.q, args->q, args->q_ld, args->q_head, args->dtype) ||
         !make_rows(&a.qo, args->q_out, args->q_out_ld, args->q_out_head, args->dtype) ||
         !make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
-        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype))
+        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype) ||
+        (a.q_heads > 0 && kv_rows_meet(batch->tokens, a.q_heads, a.c.dim, args->q_out_ld, args->q_out_head)))
         return SYMAR_ERR_INVAL;
     a.table       = (const float2 *)args->rotations;
     a.table_rows  = args->rotation_rows;
@@ -665,7 +666,9 @@ int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_
     if (!args || (args->dtype != SYMAR_F32 && args->dtype != SYMAR_BF16)) return SYMAR_ERR_INVAL;
     if (batch->tokens == 0 || (!args->k && !args->v)) return SYMAR_OK;
     if (!make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
-        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype))
+        !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype) ||
+        (args->k && kv_rows_meet(batch->tokens, a.c.kv_heads, a.c.dim, args->k_ld, args->k_head)) ||
+        (args->v && kv_rows_meet(batch->tokens, a.c.kv_heads, a.c.dim, args->v_ld, args->v_head)))
         return SYMAR_ERR_INVAL;
     a.status = kv->status;
     a.by_heads = reciprocal(2 * a.c.kv_heads);

@@ -82,6 +82,12 @@ inline cudaError_t allow_shared(const void *fn, int bytes, int device, std::atom
     return e;
 }
 
+// rows that a call would write twice
+inline bool kv_rows_meet(int tokens, int heads, int dim, int64_t ld, int64_t head)
+{
+    return (tokens > 1 && ld < dim) || (heads > 1 && head < dim);
+}
+
 // Argument checks shared by the calls on a cache; fills the views.
 int kv_check(const symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch, KvView *c, KvBatch *b);
 

@@ -101,6 +101,16 @@ def test_attention_refuses(lib):
     assert call(lib, "attention", args=dict(dtype=symar.F32)) == symar.ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("which,reads,writes", [("append", "q k v", "q_out"), ("read", "", "k v"), ("attention", "q", "out")])
+def test_strides_refused(lib, which, reads, writes):
+    for name in reads.split() + writes.split():
+        for bad in ({name + "_ld": -512}, {name + "_head": -128}):
+            assert call(lib, which, args=bad) == symar.ERR_INVAL, bad
+    for name in writes.split():                              # rows that would be written over one another
+        for bad in ({name + "_ld": 0}, {name + "_ld": 127}, {name + "_head": 0}, {name + "_head": 120}):
+            assert call(lib, which, args=bad) == symar.ERR_INVAL, bad
+
+
 def test_rope_table_refuses(lib):
     def rc(rows=16, table=SOME, **change):
         f = dict(base=1e4, factor=2.0, original=64.0, low=1.0, high=4.0, magnitude=1.0, kind=0, rot_dim=64)
