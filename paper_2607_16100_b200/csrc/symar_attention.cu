@@ -40,6 +40,13 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 // piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability before
 // it is rounded to bf16 (V), the one rounding that binary32 arithmetic would not have.
 // The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
+// Work is split over the cache as evenly as chunks allow, whatever the lengths: all chunks of all items lie in one order, every warp takes an
+// equal stretch of it, pieces of an item meet in the block and, where it crosses blocks, at the last block to come (in order, so that
+// results do not depend on which that is).
+// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 48.2 us, 3.2 TB/s of the
+// 6.5 measured for a copy; one sequence of 131072: 151 MB in 47.5 us.  Issue slots are 57% used, the pipe of integer and bit
+// operations (which turns codes into operands) 50%, tensor cores 15%, DRAM half its rate.  One token after 511 with one key/value head: 9.2 us, a chain of
+// lengths, page table, page and join, each a trip to memory.  D = 64: 32.7 us, D = 256 (lengths of 2048): 57.2 us.
 template <int D, int NB>
 struct Shape {
     static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;
