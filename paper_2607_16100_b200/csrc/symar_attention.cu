@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     auto result_of = [&](int i) { return reinterpret_cast<float *>(i & 1 ? smem + (i >> 1) * S::kRing : smem + kWarps * S::kRing + (i >> 1) * S::kPart); };
     const uint32_t mine_addr = smem_addr(mine);
 
+    wait_for_stream();
     // ---- shares: places [begin, end) of all items in order, kItemCost places and one per chunk each ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
@@ -609,8 +610,7 @@ cudaError_t launch(const AttnArgs &a, int num_sms, int device, cudaStream_t stre
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_shared((const void *)attention_kernel<D, NB>, S::kBytes, device, allowed);
     if (e != cudaSuccess) return e;
-    attention_kernel<D, NB><<<num_sms < kAttnMaxBlocks ? num_sms : kAttnMaxBlocks, 32 * S::kWarps, S::kBytes, stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(attention_kernel<D, NB>, dim3(num_sms < kAttnMaxBlocks ? num_sms : kAttnMaxBlocks), 32 * S::kWarps, S::kBytes, stream, a);
 }
 
 }  // namespace

@@ -307,6 +307,7 @@ __device__ __forceinline__ void queries(const AppendArgs &a, const Place *at, in
 template <typename T, bool kPaired>
 __global__ void __launch_bounds__(kThreads, 4) append_kernel(const AppendArgs a)
 {
+    wait_for_stream();
     __shared__ Place at[kMaxTokens];
     const int first = (int)blockIdx.x * a.tokens_per_block;
     const int mine  = min(a.tokens_per_block, a.b.tokens - first);
@@ -381,6 +382,7 @@ struct ReadArgs {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
 {
+    wait_for_stream();
     __shared__ Place at[kMaxTokens];
     const int first = (int)blockIdx.x * a.tokens_per_block;
     const int mine  = min(a.tokens_per_block, a.b.tokens - first);
@@ -650,14 +652,14 @@ int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_k
         grid.y += (unsigned)((per_block + kThreads - 1) / kThreads);
     }
     cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e;
     if (args->dtype == SYMAR_F32) {
-        if (paired) append_kernel<float, true><<<grid, kThreads, 0, s>>>(a);
-        else append_kernel<float, false><<<grid, kThreads, 0, s>>>(a);
+        if (paired) e = launch_early(append_kernel<float, true>, grid, kThreads, 0, s, a);
+        else e = launch_early(append_kernel<float, false>, grid, kThreads, 0, s, a);
     } else {
-        if (paired) append_kernel<__nv_bfloat16, true><<<grid, kThreads, 0, s>>>(a);
-        else append_kernel<__nv_bfloat16, false><<<grid, kThreads, 0, s>>>(a);
+        if (paired) e = launch_early(append_kernel<__nv_bfloat16, true>, grid, kThreads, 0, s, a);
+        else e = launch_early(append_kernel<__nv_bfloat16, false>, grid, kThreads, 0, s, a);
     }
-    cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_append");
 }
 
@@ -677,9 +679,9 @@ int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_
     a.status = kv->status;
     a.by_heads = reciprocal(2 * a.c.kv_heads);
     const dim3 grid = token_grid(batch->tokens, 2 * a.c.kv_heads, a.c.dim / 8, kv->num_sms, &a.tokens_per_block);
-    if (args->dtype == SYMAR_F32) read_kernel<float><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
-    else read_kernel<__nv_bfloat16><<<grid, kThreads, 0, (cudaStream_t)cuda_stream>>>(a);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e;
+    if (args->dtype == SYMAR_F32) e = launch_early(read_kernel<float>, grid, kThreads, 0, (cudaStream_t)cuda_stream, a);
+    else e = launch_early(read_kernel<__nv_bfloat16>, grid, kThreads, 0, (cudaStream_t)cuda_stream, a);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_read");
 }
 

@@ -303,6 +303,7 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
     tc_after();
     const uint32_t tmem = tmem_at;
 
+    wait_for_stream();
     // This block's slices of every one of its tiles: all of k, or its part where a cluster shares the tile.
     const int slices = (a.k + kSlice - 1) / kSlice, rank = a.split > 1 ? (int)blockIdx.x % a.split : 0;
     const int k_lo = (int)((int64_t)slices * rank / a.split), k_hi = (int)((int64_t)slices * (rank + 1) / a.split);
@@ -603,17 +604,20 @@ int launch(LinearArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, int g
     cudaError_t e = allow_shared((const void *)fn, S::kBytes, d.id, allowed);
     if (e != cudaSuccess) return cuda_fail(e, "symar_linear");
     cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     cfg.gridDim  = dim3((unsigned)(a.split > 1 ? tiles * a.split : (tiles < d.sms ? tiles : d.sms)));
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kBytes;
     cfg.stream   = stream;
     cfg.attrs    = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // (see wait_for_stream)
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
     if (a.split > 1) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)a.split;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)a.split;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
     }
     e = cudaLaunchKernelEx(&cfg, fn, wmap, xmap, a);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_linear");

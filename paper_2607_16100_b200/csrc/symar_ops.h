@@ -72,6 +72,31 @@ __device__ __forceinline__ int kv_page_of(const KvView &c, const KvBatch &b, int
 }
 #endif
 
+// The operators are launched before the kernel ahead of them on the stream has drained, and wait for its results here, before they read
+// or write anything; from then on the next kernel may be launched in the same way.
+#ifdef __CUDACC__
+__device__ __forceinline__ void wait_for_stream()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*fn)(P...), dim3 grid, unsigned threads, size_t shared, cudaStream_t stream, A... args)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, args...);
+}
+#endif
+
 // Dynamic shared memory of a kernel, allowed once per device (`done`: a bit per device, one word per kernel).
 inline cudaError_t allow_shared(const void *fn, int bytes, int device, std::atomic<uint64_t> &done)
 {

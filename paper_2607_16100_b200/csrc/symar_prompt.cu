@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- this block's item ----
+    wait_for_stream();
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
     auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kBlockRows - 1) / kBlockRows) * a.c.kv_heads; };
@@ -617,8 +618,7 @@ cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t 
     }
     const cudaError_t e = allow_shared((const void *)prompt_kernel<D>, Shape<D>::kBytes, device, allowed);
     if (e != cudaSuccess) return e;
-    prompt_kernel<D><<<blocks, kThreads, Shape<D>::kBytes, stream>>>(a);
-    return cudaGetLastError();
+    return launch_early(prompt_kernel<D>, dim3(blocks), kThreads, Shape<D>::kBytes, stream, a);
 }
 }  // namespace
 
