@@ -23,6 +23,14 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// the upper halves of two numbers, and what is left of each, rounded
+__device__ __forceinline__ uint32_t high_and_rest(float a, float b, uint32_t &rest)
+{
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    rest = pack_bf16(a - __uint_as_float(x & 0xffff0000u), b - __uint_as_float(y & 0xffff0000u));
+    return __byte_perm(x, y, 0x7632);
+}
+
 template <int R>
 __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 {
@@ -37,16 +45,19 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 // instruction and eight query rows its columns, so that the eight heads of a share fill it with one token.  A chunk's 16
 // tokens are one warp's own: it copies them to its shared memory four chunks ahead, turns codes into exact bf16
 // whole numbers (n - z) in registers, multiplies, and keeps its own running maximum and sum; warps meet once per
-// piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability before
-// it is rounded to bf16 (V), the one rounding that binary32 arithmetic would not have.
+// piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability (V), which
+// goes into the product as two bf16 numbers, its upper eight bits and what they leave: sixteen bits of it count.  (With the first alone, rounded, the
+// result's error is that of a second rounding of the output, 0.0024 instead of 0.0017 of its size, up to 0.0025 where it is small;
+// the second product costs 10%: 48.3 -> 53.2 us for the batch below.)
 // The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
 // Work is split over the cache as evenly as chunks allow, whatever the lengths: all chunks of all items lie in one order, every warp takes an
 // equal stretch of it, pieces of an item meet in the block and, where it crosses blocks, at the last block to come (in order, so that
 // results do not depend on which that is).
-// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 48.2 us, 3.2 TB/s of the
-// 6.5 measured for a copy; one sequence of 131072: 151 MB in 47.5 us.  Issue slots are 57% used, the pipe of integer and bit
+// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 53.2 us, 2.9 TB/s of the
+// 6.5 measured for a copy (14 us of it are start, joins and end; 256 such sequences ran at 4.7 TB/s before the second product); one
+// sequence of 131072: 151 MB in 52 us.  Issue slots are 57% used, the pipe of integer and bit
 // operations (which turns codes into operands) 50%, tensor cores 15%, DRAM half its rate.  One token after 511 with one key/value head: 9.2 us, a chain of
-// lengths, page table, page and join, each a trip to memory.  D = 64: 32.7 us, D = 256 (lengths of 2048): 57.2 us.
+// lengths, page table, page and join, each a trip to memory.  D = 64: 35.2 us, D = 256 (lengths of 2048): 59.6 us.
 template <int D, int NB>
 struct Shape {
     static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;
@@ -373,13 +384,15 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
             }
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                uint32_t r[4], pf[NB][2];
+                uint32_t r[4], pf[NB][2], pr[NB][2];
                 matrices_t(r, base + kCodes + mt * kRow + (((2 * gr + mc) ^ turn) << 4));
                 const float f0 = __uint_as_float(w0[gr]), f1 = __uint_as_float(w1[gr]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    pf[nb][0] = transposed(pack_bf16(sc[nb][0] * f0, sc[nb][1] * f0));
-                    pf[nb][1] = transposed(pack_bf16(sc[nb][2] * f1, sc[nb][3] * f1));
+                    pf[nb][0] = transposed(high_and_rest(sc[nb][0] * f0, sc[nb][1] * f0, pr[nb][0]));
+                    pf[nb][1] = transposed(high_and_rest(sc[nb][2] * f1, sc[nb][3] * f1, pr[nb][1]));
+                    pr[nb][0] = transposed(pr[nb][0]);
+                    pr[nb][1] = transposed(pr[nb][1]);
                 }
                 const uint32_t z0 = zeros_of(z2[0][gr], z2[1][gr]), z1 = zeros_of(z2[2][gr], z2[3][gr]);
                 const uint32_t y0 = mul2(z0, kSixteen), y1 = mul2(z1, kSixteen);
@@ -388,7 +401,10 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                     const uint32_t a0 = fma2(codes(r[0], i), kTwo127, i & 1 ? y0 : z0), a1 = fma2(codes(r[1], i), kTwo127, i & 1 ? y0 : z0);
                     const uint32_t a2 = fma2(codes(r[2], i), kTwo127, i & 1 ? y1 : z1), a3 = fma2(codes(r[3], i), kTwo127, i & 1 ? y1 : z1);
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
+                    for (int nb = 0; nb < NB; ++nb) {
+                        mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pf[nb][0], pf[nb][1]);
+                        mma(o[nb][gr * 4 + i], a0, a1, a2, a3, pr[nb][0], pr[nb][1]);
+                    }
                 }
             }
         }
