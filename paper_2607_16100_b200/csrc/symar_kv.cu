@@ -299,7 +299,7 @@ __device__ __forceinline__ void queries(const AppendArgs &a, const Place *at, in
 }
 
 // Bound: bytes.  16384 tokens of 64 query and 2 x 8 key/value heads of 128 in bf16: 720 MB in 147 us, 4.9 TB/s (0.74 of the measured copy
-// rate); of that 60 us for keys and values alone.  64 tokens 3.7 us, one token 2.9 us: the trip
+// rate); of that 60 us for keys and values alone.  64 tokens 3.5 us, one token 2.7 us: the trip
 // from the lengths to the page table to the page.  Ragged prompts of float32 (5 x up to 1501): 15.6 us.
 // Blocks with the first kv_blocks indexes in y store keys and values, the others turn queries.  (Where the queries' pairs do not come in
 // eights, kPaired is false and every block does both, a head of a token like another.)
@@ -378,7 +378,7 @@ struct ReadArgs {
     uint32_t by_heads;
 };
 
-// Bound: bytes; 16384 tokens 24.7 us (86 MB, 3.5 TB/s), one token 2.1 us.
+// Bound: bytes; 16384 tokens 24.7 us (86 MB, 3.5 TB/s), one token 2.0 us.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
 {

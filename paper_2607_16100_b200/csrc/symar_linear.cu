@@ -9,12 +9,12 @@
 // Where tiles are fewer than half the multiprocessors, clusters of two to eight blocks share a tile's k and add their parts up over
 // distributed shared memory in rank order (clusters of three left multiprocessors without one: 52 us instead of 37 for the odd case below).
 //
-// Bound and measured (B200, times within a CUDA graph).  Few tokens: the weights' bytes; 8 x 4 x 8192 x 1024 takes 25.8-27.2 us for 135 MB,
-// 5.2 TB/s (0.76-0.8 of the measured copy rate; the ring of ten stages holds 200 KB a multiprocessor in flight, the rest is
-// the start and the cluster's sum); 1 x 1024 x 1024 5.8 us, launch and latency.  Many: the tensor cores; 4096 x 8192 x 8192 takes 395 us,
+// Bound and measured (B200, times within a CUDA graph).  Few tokens: the weights' bytes; 8 x 4 x 8192 x 1024 takes 25.3 us for 135 MB,
+// 5.3 TB/s (0.81 of the measured copy rate; the ring of ten stages holds 200 KB a multiprocessor in flight, the rest is
+// the start and the cluster's sum); 1 x 1024 x 1024 4.9 us, launch and latency.  Many: the tensor cores; 4096 x 8192 x 8192 takes 395 us,
 // 1390 TFLOP/s (0.85 of the measured 1640; a library product 354), with bias, tanh-GELU and residual 450 us: the
 // epilogue's 33 M values are 55 us of work for eight warps and only partly hidden.  float32 results 680-715 us: their sums leave
-// the tensor cores every 128 products.  Rows on no 16-byte boundary: 2 x 333 x 1003 x 2049 takes 37 us where k = 2048 takes 14.4; the
+// the tensor cores every 128 products.  Rows on no 16-byte boundary: 2 x 333 x 1003 x 2049 takes 36 us where k = 2048 takes 13.9; the
 // eight loading warps issue most of a slice's 7600 instructions, to shift and join its 2048 pieces.
 #include <type_traits>
 
