@@ -43,6 +43,9 @@ CASES = [
     ([(512, 3000)], 24, 8, 128, 256, 1000),
     ([(2000, 2000)], 8, 8, 128, 64, 1),
     ([(900, 400), (300, 1)], 16, 8, 128, 16, 0),             # more new tokens than tokens: the first rows see nothing
+    ([(1200, 2111), (700, 700)], 8, 8, 64, 128, 100),        # a window shorter than a block's tokens, and many blocks
+    ([(16, 16 + 37 * i) for i in range(12)], 64, 8, 128, 16, 0),         # blocks that are half full, of unequal lengths
+    ([(40, 333), (1, 900), (150, 150), (64, 2000)], 64, 8, 128, 32, 77), # the same beside one token, under a window
 ]
 
 
