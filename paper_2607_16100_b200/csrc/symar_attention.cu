@@ -6,7 +6,7 @@
 namespace symar {
 namespace {
 
-constexpr int kStages   = 4;           // copies in flight per warp: three chunks ahead of the one in use
+constexpr int kStages   = 3;           // copies in flight per warp: two chunks ahead of the one in use (three: 51.7 us against 49.3 for one long sequence)
 constexpr int kMinChunks = 1;          // a warp's share of the work is at least this many chunks of 16 tokens
 constexpr int kItemCost  = 3;          // what an item costs a warp besides its chunks, in chunks
 
@@ -23,11 +23,13 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// the upper halves of two numbers, and what is left of each, rounded
-__device__ __forceinline__ uint32_t high_and_rest(float a, float b, uint32_t &rest)
+// the upper halves of a f and b f, and what is left of each, rounded
+__device__ __forceinline__ uint32_t high_and_rest(float a, float b, float f, uint32_t &rest)
 {
-    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-    rest = pack_bf16(a - __uint_as_float(x & 0xffff0000u), b - __uint_as_float(y & 0xffff0000u));
+    uint32_t x, y;
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %4};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "=r"(x), "=r"(y) : "f"(a), "f"(b), "f"(f));
+    rest = pack_bf16(__uint_as_float(x) - __uint_as_float(x & 0xffff0000u), __uint_as_float(y) - __uint_as_float(y & 0xffff0000u));
     return __byte_perm(x, y, 0x7632);
 }
 
@@ -43,21 +45,21 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 
 // S^T = K Q^T and O^T = V^T P^T: the cache's tokens (then its channels) are the sixteen rows of the matrix
 // instruction and eight query rows its columns, so that the eight heads of a share fill it with one token.  A chunk's 16
-// tokens are one warp's own: it copies them to its shared memory four chunks ahead, turns codes into exact bf16
+// tokens are one warp's own: it copies them to its shared memory two chunks ahead, turns codes into exact bf16
 // whole numbers (n - z) in registers, multiplies, and keeps its own running maximum and sum; warps meet once per
 // piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability (V), which
 // goes into the product as two bf16 numbers, its upper eight bits and what they leave: sixteen bits of it count.  (With the first alone, rounded, the
 // result's error is that of a second rounding of the output, 0.0024 instead of 0.0017 of its size, up to 0.0025 where it is small;
-// the second product costs 10%: 48.3 -> 53.2 us for the batch below.)
+// the second product costs 8%: 48.3 -> 52.2 us for the batch below.)
 // The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
 // Work is split over the cache as evenly as chunks allow, whatever the lengths: all chunks of all items lie in one order, every warp takes an
 // equal stretch of it, pieces of an item meet in the block and, where it crosses blocks, at the last block to come (in order, so that
 // results do not depend on which that is).
-// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 53.2 us, 2.9 TB/s of the
+// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 52.2 us, 3.0 TB/s of the
 // 6.5 measured for a copy (14 us of it are start, joins and end; 256 such sequences ran at 4.7 TB/s before the second product); one
-// sequence of 131072: 151 MB in 52 us.  Issue slots are 57% used, the pipe of integer and bit
-// operations (which turns codes into operands) 50%, tensor cores 15%, DRAM half its rate.  One token after 511 with one key/value head: 9.2 us, a chain of
-// lengths, page table, page and join, each a trip to memory.  D = 64: 35.2 us, D = 256 (lengths of 2048): 59.6 us.
+// sequence of 131072: 151 MB in 49.3 us.  Issue slots are 56% used, the pipe of integer and bit
+// operations (which turns codes into operands) 48%, tensor cores 21%, DRAM half its rate.  One token after 511 with one key/value head: 9.2 us, a chain of
+// lengths, page table, page and join, each a trip to memory.  D = 64: 35.5 us, D = 256 (lengths of 2048): 59.7 us.
 template <int D, int NB>
 struct Shape {
     static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;
@@ -389,8 +391,8 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
                 const float f0 = __uint_as_float(w0[gr]), f1 = __uint_as_float(w1[gr]);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    pf[nb][0] = transposed(high_and_rest(sc[nb][0] * f0, sc[nb][1] * f0, pr[nb][0]));
-                    pf[nb][1] = transposed(high_and_rest(sc[nb][2] * f1, sc[nb][3] * f1, pr[nb][1]));
+                    pf[nb][0] = transposed(high_and_rest(sc[nb][0], sc[nb][1], f0, pr[nb][0]));
+                    pf[nb][1] = transposed(high_and_rest(sc[nb][2], sc[nb][3], f1, pr[nb][1]));
                     pr[nb][0] = transposed(pr[nb][0]);
                     pr[nb][1] = transposed(pr[nb][1]);
                 }
