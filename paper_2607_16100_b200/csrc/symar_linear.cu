@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "symar_ops.h"
+#include "symar_rows.h"
 #include "symar_tc.cuh"
 
 namespace symar {
@@ -36,7 +37,7 @@ struct LinearArgs {
     unsigned *status;
 };
 
-constexpr int kRows = 128, kSlice = 64;    // channels of a tile; k of a stage: 128 bytes, one swizzled row
+constexpr int kRows = 128;                 // channels of a tile; a stage has kSlice of k: 128 bytes, one swizzled row
 constexpr int kMaxSplit = 8;
 
 __device__ __forceinline__ void cluster_sync()
@@ -184,10 +185,7 @@ __device__ __forceinline__ void finish(const LinearArgs &a, const Channels &c, i
 // Eight neighbouring lanes hold the eight aligned 16-byte pieces that a slice of a row begins in; the slice's own eight
 // pieces start `shift` bytes into them.  A lane takes the missing end of its piece from its neighbour, the eighth from the
 // first lane's piece of the next slice, which is on its way by then; so every piece is loaded once.
-struct Span {
-    const char *lo, *hi;         // the operand's bytes: nothing outside is read
-};
-__device__ __noinline__ uint4 edge_piece(const char *at, Span s)
+__device__ __noinline__ uint4 edge_piece(uintptr_t at, Span s)
 {
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -196,7 +194,7 @@ __device__ __noinline__ uint4 edge_piece(const char *at, Span s)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // (predicated, not a branch: the loads of all rows go out one after the other)
-__device__ __forceinline__ uint4 load_if(const char *at, bool on)
+__device__ __forceinline__ uint4 load_if(uintptr_t at, bool on)
 {
     uint4 v;
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
@@ -204,27 +202,24 @@ __device__ __forceinline__ uint4 load_if(const char *at, bool on)
                  : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(at), "r"((int)on));
     return v;
 }
-// One piece of each of N rows (of the first `split` of operand s0, the others of s1) where the row exists (bit 4 of how) and, for
-// what bit 5 does not vouch for, the piece lies in the operand; pieces that lie in it in part are put together element by element.
+// Piece c of a slice of each of N rows (of the first `split` of operand s0, the others of s1) where the row exists and the piece holds
+// some of its k elements; pieces that lie in the operand in part are put together element by element.
 template <int N>
-__device__ __forceinline__ void pieces(uint4 (&v)[N], const char *const (&at)[N], const int (&how)[N], int64_t byte, bool on, int split, Span s0, Span s1)
+__device__ __forceinline__ void pieces(uint4 (&v)[N], const uintptr_t (&at)[N], const int (&kind)[N], int k, int slice, int c, int split, Span s0, Span s1)
 {
+    const bool on = piece_wanted(k, slice, c);
+    const int64_t byte = (int64_t)slice * 128 + c * 16;
     bool rest = false;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        const Span &s = j < split ? s0 : s1;
-        const char *p = at[j] + byte;
-        const bool want = on && (how[j] & 16), safe = (how[j] & 32) || (p >= s.lo && p + 16 <= s.hi);
-        v[j] = load_if(p, want && safe);
-        rest |= want && !safe;
+        const bool want = on && (kind[j] & 16), whole = piece_whole(at[j] + byte, kind[j], j < split ? s0 : s1);
+        v[j] = load_if(at[j] + byte, want && whole);
+        rest |= want && !whole;
     }
     if (rest) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const Span &s = j < split ? s0 : s1;
-            const char *p = at[j] + byte;
-            if (on && (how[j] & 16) && !((how[j] & 32) || (p >= s.lo && p + 16 <= s.hi))) v[j] = edge_piece(p, s);
-        }
+        for (int j = 0; j < N; ++j)
+            if (on && (kind[j] & 16) && !piece_whole(at[j] + byte, kind[j], j < split ? s0 : s1)) v[j] = edge_piece(at[j] + byte, j < split ? s0 : s1);
     }
 }
 __device__ __forceinline__ uint4 joined(const uint4 &u, const uint4 &next, int shift, int c, int lane)
@@ -343,25 +338,21 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
         for (int tile = first; tile < a.tiles && k_lo < k_hi; tile += step) {
             int g, m0, n0;
             place(tile, g, m0, n0);
-            const char *w = reinterpret_cast<const char *>(a.w + g * a.w_group), *x = reinterpret_cast<const char *>(a.x + g * a.x_group);
+            const uintptr_t w = (uintptr_t)(a.w + g * a.w_group), x = (uintptr_t)(a.x + g * a.x_group);
             const Span ws{w, w + ((int64_t)(a.n - 1) * a.w_ld + a.k) * 2}, xs{x, x + ((int64_t)(a.m - 1) * a.x_ld + a.k) * 2};
-            const char *w_row = w + (int64_t)(n0 + r) * a.w_ld * 2, *x_row = x + (int64_t)(m0 + r) * a.x_ld * 2;
-            const char *at[kOf];                       // the aligned piece that the row begins in
-            int how[kOf];                              // byte shift of the row, + 16 where it exists, + 32 where it is inner
+            const uintptr_t w_row = w + (int64_t)(n0 + r) * a.w_ld * 2, x_row = x + (int64_t)(m0 + r) * a.x_ld * 2;
+            uintptr_t at[kOf];                         // the aligned piece that the row begins in
+            int kind[kOf];
 #pragma unroll
             for (int j = 0; j < kOf; ++j) {
-                const char *row = j < 4 ? w_row + j * 64 * a.w_ld : x_row + (j - 4) * 64 * a.x_ld;
+                const uintptr_t row = j < 4 ? w_row + j * 64 * a.w_ld : x_row + (j - 4) * 64 * a.x_ld;
                 const int i = j < 4 ? n0 + r + 32 * j : m0 + r + 32 * (j - 4), rows = j < 4 ? a.n : a.m;
-                at[j]  = reinterpret_cast<const char *>((uintptr_t)row & ~(uintptr_t)15);
-                how[j] = (int)((uintptr_t)row & 15) | (i < rows && (j < 4 || r + 32 * (j - 4) < NT) ? 16 : 0) |
-                         (row >= (j < 4 ? ws : xs).lo + 16 && row + 2 * a.k + 32 <= (j < 4 ? ws : xs).hi ? 32 : 0);
+                at[j]   = row & ~(uintptr_t)15;
+                kind[j] = row_kind(row, i < rows && (j < 4 || r + 32 * (j - 4) < NT), a.k, j < 4 ? ws : xs);
             }
             uint4 u[kOf], next[kOf];
-            int64_t byte = (int64_t)k_lo * 128 + c * 16;
-            // (a row's last piece may hold the last elements of a slice: one slice more, if only its first piece, which begins in the row)
-            pieces<kOf>(u, at, how, byte, true, 4, ws, xs);
-            pieces<kOf>(next, at, how, byte + 128, a.k - k_lo * kSlice - c * 8 - kSlice + 8 > 0, 4, ws, xs);
-            byte += 128;
+            pieces<kOf>(u, at, kind, a.k, k_lo, c, 4, ws, xs);
+            pieces<kOf>(next, at, kind, a.k, k_lo + 1, c, 4, ws, xs);
 #pragma unroll 2            // (the pieces on their way change places with those in hand without a copy, which would wait for them)
             for (int ks = k_lo; ks < k_hi; ++ks) {
                 const int left = a.k - ks * kSlice - c * 8;
@@ -369,15 +360,14 @@ linear_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ 
                 unsigned char *dst = ring + st * S::kStage;
 #pragma unroll
                 for (int j = 0; j < kOf; ++j) {
-                    uint4 v = joined(u[j], next[j], how[j], c, lane);
+                    uint4 v = joined(u[j], next[j], kind[j], c, lane);
                     if (left < 8) v = cut(v, left);
                     const int to = j < 4 ? r + 32 * j : r + 32 * (j - 4);
                     if (j < 4 || to < NT) *reinterpret_cast<uint4 *>(dst + (j < 4 ? 0 : S::kA) + to * 128 + ((c ^ (to & 7)) << 4)) = v;
                     u[j] = next[j];
                 }
-                // asked for a whole slice before they are joined
-                byte += 128;
-                pieces<kOf>(next, at, how, byte, ks + 1 < k_hi && left - 2 * kSlice + 8 > 0, 4, ws, xs);
+                // asked for a whole slice before they are joined (of the block's last slice's neighbour the slice after has no use)
+                pieces<kOf>(next, at, kind, a.k, ks + 1 < k_hi ? ks + 2 : slices + 1, c, 4, ws, xs);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 bar_arrive(full + 8 * st);
                 if (++st == S::kStages) st = 0, ++round;
