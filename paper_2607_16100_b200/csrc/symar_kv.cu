@@ -94,7 +94,7 @@ __device__ Place place_of(const KvView &c, const KvBatch &b, int *status, int to
             else lo = mid + 1;
         }
         p.seq = lo;
-        if (lo >= b.seqs) return p;                   // a row of no sequence
+        if (lo >= b.seqs || token < b.token_start[lo]) return p;      // a row of no sequence: behind the last, or before the first
         p.pos = b.lengths[lo] - (b.token_start[lo + 1] - token);
     } else {
         p.pos = b.lengths[token] - 1;
