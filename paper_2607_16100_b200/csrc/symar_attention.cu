@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     const uint32_t mine_addr = smem_addr(mine);
 
     wait_for_stream();
+    const RowRange rows_in = sequence_rows(a);
     // ---- shares: places [begin, end) of all items in order, kItemCost places and one per chunk each ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
@@ -113,6 +114,7 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     if (lane == 31) warp_sum[warp] = incl;
     if (tid < 2 * kWarps) piece[tid].chunks = 0;
     __syncthreads();
+    zero_other_rows(a, rows_in);
     int64_t total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {

@@ -143,6 +143,39 @@ __device__ __forceinline__ void store4(const AttnArgs &a, const Seq &s, int rows
     }
 }
 
+// The batch's rows: [first, end) are the sequences', the others zeros.
+struct RowRange {
+    int first, end;
+};
+__device__ __forceinline__ RowRange sequence_rows(const AttnArgs &a)
+{
+    RowRange r{0, a.b.tokens};
+    if (a.b.token_start) {
+        r.first = min(max(a.b.token_start[0], 0), a.b.tokens);
+        r.end   = max(min(a.b.token_start[a.b.seqs], a.b.tokens), r.first);
+    }
+    return r;
+}
+// (by all blocks of the grid)
+__device__ __forceinline__ void zero_other_rows(const AttnArgs &a, const RowRange &r)
+{
+    const int shift = 29 - __clz(a.c.dim), others = r.first + (a.b.tokens - r.end);         // 2^shift pieces of four channels
+#pragma unroll 1
+    for (int i = blockIdx.x; i < others; i += gridDim.x) {
+        __nv_bfloat16 *row = a.out + (int64_t)(i < r.first ? i : i - r.first + r.end) * a.out_ld;
+#pragma unroll 1
+        for (int e = threadIdx.x; e < a.q_heads << shift; e += blockDim.x) {
+            __nv_bfloat16 *p = row + (int64_t)(e >> shift) * a.out_head + ((e & ((1 << shift) - 1)) << 2);
+            if (a.out_vec) {
+                *reinterpret_cast<uint2 *>(p) = make_uint2(0, 0);
+            } else {
+                uint16_t *h = reinterpret_cast<uint16_t *>(p);
+                h[0] = h[1] = h[2] = h[3] = 0;
+            }
+        }
+    }
+}
+
 // One softmax over all work of an item, wherever it was done: unnormalised output relative to 2^m, and its sum.
 constexpr float kNothing = -3.402823466e38f;
 

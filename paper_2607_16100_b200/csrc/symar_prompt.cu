@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 
     // ---- this block's item ----
     wait_for_stream();
+    const RowRange rows_in = sequence_rows(a);
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
     auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kBlockRows - 1) / kBlockRows) * a.c.kv_heads; };
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         if (w == warp) incl += total;
         total += warp_sum[w];
     }
+    zero_other_rows(a, rows_in);
     if ((int64_t)blockIdx.x >= total) return;
     if ((int64_t)blockIdx.x >= incl - own && (int64_t)blockIdx.x < incl) {
         int64_t flat = incl - own;

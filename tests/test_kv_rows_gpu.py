@@ -1,10 +1,11 @@
-"""Which rows of q, k and v belong to which token of which sequence: rows before token_start[0] and behind token_start[seqs] (the padding
-of a call of a fixed size).  A row of no sequence: append stores nothing and copies its q, read gives zeros."""
+"""Which rows of q, k and v belong to which token of which sequence: rows before token_start[0], behind token_start[seqs] (the padding of
+a call of a fixed size).  A row of no sequence: append stores nothing and copies its q, read and attention give zeros."""
 import pytest
 import torch
 
 from paper_2607_16100_b200 import symar
 from test_kv_gpu import Setup, kv, normal      # noqa: F401  (kv is a fixture)
+from test_prompt_gpu import reference
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +49,29 @@ def test_append_and_read_leave_rows_of_no_sequence_alone(kv, seqs, hq, hkv, dim,
         for a, b in zip(kv.read(t.cache, batch, rows), kv.read(s.cache, s.batch, s.tokens)):
             assert torch.equal(a, padded(b, front, behind, 0.0))
     assert kv.status()[0] == symar.OK
+
+
+@pytest.mark.parametrize("front,behind", [(2, 0), (0, 3), (5, 300)])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("seqs,hq,hkv,dim,page", SIZES)
+def test_attention_of_rows_of_no_sequence_is_zero(kv, seqs, hq, hkv, dim, page, front, behind, offset):      # noqa: F811
+    s = Setup(seqs, hkv, dim, page, seed=2, single=False)
+    starts(s)
+    filled = s.fill(kv, seed=5)
+    q = normal(s.tokens, hq, dim, seed=6)
+    want, tol = reference(s, filled, q, dim ** -0.5, 0)
+    batch, rows = moved(s, front, behind)
+    room = torch.full((rows, hq * dim + 8 + offset), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = room[:, offset:offset + hq * dim].unflatten(1, (hq, dim))
+    kv.attention(s.cache, batch, padded(q, front, behind, 3.0), out=out)
+    assert ((out[front:front + s.tokens].double() - want).abs() <= tol).all()
+    assert (out[:front] == 0).all() and (out[front + s.tokens:] == 0).all()
+    assert (room[:, :offset] == 7.0).all() and (room[:, offset + hq * dim:] == 7.0).all()
+
+
+def test_a_batch_of_empty_sequences_gives_zeros(kv):      # noqa: F811
+    s = Setup([(0, 5), (0, 0)], 2, 128, 16, single=False)
+    q = normal(9, 8, 128, seed=1)
+    out = torch.full_like(q, 7.0)
+    kv.attention(s.cache, s.batch, q, out=out)
+    assert (out == 0).all()
