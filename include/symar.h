@@ -493,7 +493,8 @@ typedef struct {
  *   token_start [seqs + 1]   sequence b's new tokens are rows token_start[b] .. token_start[b+1]-1 of q, k and v, and
  *                            the last ones of the sequence; NULL: one new token per sequence, row b (tokens == seqs).  It rises; rows
  *                            before token_start[0] and from token_start[seqs] on belong to no sequence: nothing of them is stored,
- *                            their results are zeros (append's: q as it is)
+ *                            their results are zeros (append's: q as it is).  It may go beyond `tokens`: of a sequence's rows the first are there then,
+ *                            and they have the positions that token_start gives them
  *   page_table [seqs][table_ld]  token t of sequence b lies in page page_table[b][t / page_size]           */
 typedef struct {
     const int32_t *lengths;

@@ -98,15 +98,17 @@ __device__ __forceinline__ int by_share(const AttnArgs &a, int n) { return (int)
 // An item is `rows` query rows (a token and a head of the key/value head's share, tokens first) of one sequence and one
 // key/value head; its work is the chunks of 16 cached tokens that any of its rows sees, one at least.
 struct Seq {
-    int start, fresh, len;       // first row of q, new tokens, all tokens
+    int start, fresh, len;       // first row of q, new tokens, all tokens up to the last of them
 };
 __device__ __forceinline__ Seq sequence(const AttnArgs &a, int b)
 {
     Seq s;
     s.len = a.b.lengths[b];
     if (a.b.token_start) {
+        const int end = a.b.token_start[b + 1], last = min(end, a.b.tokens);
         s.start = max(a.b.token_start[b], 0);
-        s.fresh = max(min(a.b.token_start[b + 1], a.b.tokens) - s.start, 0);
+        s.fresh = max(last - s.start, 0);
+        s.len -= end - last;               // rows that the call does not have are tokens that none of its rows sees
     } else {
         s.start = b;
         s.fresh = 1;

@@ -1,5 +1,6 @@
 """Which rows of q, k and v belong to which token of which sequence: rows before token_start[0], behind token_start[seqs] (the padding of
-a call of a fixed size).  A row of no sequence: append stores nothing and copies its q, read and attention give zeros."""
+a call of a fixed size), and a token_start that goes beyond the call's rows.  A row of no sequence: append stores nothing and copies its
+q, read and attention give zeros."""
 import pytest
 import torch
 
@@ -75,3 +76,22 @@ def test_a_batch_of_empty_sequences_gives_zeros(kv):      # noqa: F811
     out = torch.full_like(q, 7.0)
     kv.attention(s.cache, s.batch, q, out=out)
     assert (out == 0).all()
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,dim,page", SIZES)
+def test_rows_that_a_call_does_not_have(kv, seqs, hq, hkv, dim, page):      # noqa: F811
+    """token_start may go beyond the call's rows: the rows that are there have the positions that token_start gives them."""
+    s, t = (Setup(seqs, hkv, dim, page, seed=3, single=False) for _ in range(2))
+    for x in (s, t):
+        starts(x)
+        x.fill(kv, seed=7)
+    q, k, v = (normal(s.tokens, h, dim, seed=i) for i, h in enumerate((hq, hkv, hkv)))
+    keep = max(1, s.tokens - 2)
+    table = symar.rope_table(2000, dim)
+    a = kv.append(s.cache, s.batch, k, v, q=q, rotations=table)
+    b = kv.append(t.cache, t.batch, k[:keep], v[:keep], q=q[:keep], rotations=table)
+    assert torch.equal(b, a[:keep])
+    x = t.whole()
+    k, v = (y.double().split([n for _, n in seqs]) for y in kv.read(t.cache, x.batch, x.tokens, dtype=torch.float32))
+    want, tol = reference(t, list(zip(k, v)), a, dim ** -0.5, 0)
+    assert ((kv.attention(t.cache, t.batch, b).double() - want[:keep]).abs() <= tol[:keep]).all()
