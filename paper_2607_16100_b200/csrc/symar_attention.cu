@@ -80,7 +80,7 @@ struct Piece {
 };
 
 template <int D, int NB>
-__global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel(const AttnArgs a)
+__device__ __forceinline__ void attention_block(const AttnArgs &a)
 {
     using S = Shape<D, NB>;
     constexpr int R = S::R, NG = S::NG, kRow = S::kRow, kUnits = D / 32, kWarps = S::kWarps, kThreads = 32 * kWarps;
@@ -98,7 +98,6 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     const uint32_t mine_addr = smem_addr(mine);
 
     wait_for_stream();
-    const RowRange rows_in = sequence_rows(a);
     // ---- shares: places [begin, end) of all items in order, kItemCost places and one per chunk each ----
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
@@ -114,7 +113,6 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
     if (lane == 31) warp_sum[warp] = incl;
     if (tid < 2 * kWarps) piece[tid].chunks = 0;
     __syncthreads();
-    zero_other_rows(a, rows_in);
     int64_t total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
@@ -621,6 +619,13 @@ __global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel
             __syncthreads();
         }
     }
+}
+
+template <int D, int NB>
+__global__ void __launch_bounds__(32 * Shape<D, NB>::kWarps, 1) attention_kernel(const AttnArgs a)
+{
+    attention_block<D, NB>(a);
+    zero_other_rows(a, blockIdx.x, gridDim.x, 32 * Shape<D, NB>::kWarps);
 }
 
 template <int D, int NB>

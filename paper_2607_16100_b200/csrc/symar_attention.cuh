@@ -145,28 +145,18 @@ __device__ __forceinline__ void store4(const AttnArgs &a, const Seq &s, int rows
     }
 }
 
-// The batch's rows: [first, end) are the sequences', the others zeros.
-struct RowRange {
-    int first, end;
-};
-__device__ __forceinline__ RowRange sequence_rows(const AttnArgs &a)
+// Rows before token_start[0] and from token_start[seqs] on are no sequence's: zeros, by the first `threads` threads of `blocks` blocks, of
+// which this one is `at`.  Blocks do this after their own work, or have no other (before it, it cost every call 1 to 2%, one without such rows too).
+__device__ __forceinline__ void zero_other_rows(const AttnArgs &a, int at, int blocks, int threads)
 {
-    RowRange r{0, a.b.tokens};
-    if (a.b.token_start) {
-        r.first = min(max(a.b.token_start[0], 0), a.b.tokens);
-        r.end   = max(min(a.b.token_start[a.b.seqs], a.b.tokens), r.first);
-    }
-    return r;
-}
-// (by all blocks of the grid)
-__device__ __forceinline__ void zero_other_rows(const AttnArgs &a, const RowRange &r)
-{
-    const int shift = 29 - __clz(a.c.dim), others = r.first + (a.b.tokens - r.end);         // 2^shift pieces of four channels
+    if (!a.b.token_start) return;
+    const int first = min(max(a.b.token_start[0], 0), a.b.tokens), end = max(min(a.b.token_start[a.b.seqs], a.b.tokens), first);
+    const int shift = 29 - __clz(a.c.dim);                     // 2^shift pieces of four channels
 #pragma unroll 1
-    for (int i = blockIdx.x; i < others; i += gridDim.x) {
-        __nv_bfloat16 *row = a.out + (int64_t)(i < r.first ? i : i - r.first + r.end) * a.out_ld;
+    for (int i = at; i < first + (a.b.tokens - end); i += blocks) {
+        __nv_bfloat16 *row = a.out + (int64_t)(i < first ? i : i - first + end) * a.out_ld;
 #pragma unroll 1
-        for (int e = threadIdx.x; e < a.q_heads << shift; e += blockDim.x) {
+        for (int e = threadIdx.x; e < a.q_heads << shift; e += threads) {
             __nv_bfloat16 *p = row + (int64_t)(e >> shift) * a.out_head + ((e & ((1 << shift) - 1)) << 2);
             if (a.out_vec) {
                 *reinterpret_cast<uint2 *>(p) = make_uint2(0, 0);

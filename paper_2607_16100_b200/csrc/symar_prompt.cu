@@ -150,7 +150,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 
     // ---- this block's item ----
     wait_for_stream();
-    const RowRange rows_in = sequence_rows(a);
     const int each = (a.b.seqs + kThreads - 1) / kThreads;
     const int s0 = min(tid * each, a.b.seqs), s1 = min(s0 + each, a.b.seqs);
     auto items_of = [&](const Seq &s) { return (int64_t)((s.fresh * a.share + kBlockRows - 1) / kBlockRows) * a.c.kv_heads; };
@@ -190,8 +189,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         if (w == warp) incl += total;
         total += warp_sum[w];
     }
-    zero_other_rows(a, rows_in);
-    if ((int64_t)blockIdx.x >= total) return;
+    if ((int64_t)blockIdx.x >= total) {                 // (there is one such block at least)
+        zero_other_rows(a, (int)((int64_t)blockIdx.x - total), (int)((int64_t)gridDim.x - total), kThreads);
+        return;
+    }
     if ((int64_t)blockIdx.x >= incl - own && (int64_t)blockIdx.x < incl) {
         int64_t flat = incl - own;
 #pragma unroll 1
@@ -584,7 +585,7 @@ done:
     if (warp == kSoftmax + kWorkers) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-// items that the call has at most: a block each (blocks beyond the last item leave at once)
+// items that the call has at most: a block each (blocks beyond the last item have only rows of no sequence to look at)
 int64_t items_at_most(const AttnArgs &a)
 {
     return ((int64_t)a.b.tokens * a.share / kBlockRows + (a.b.seqs < a.b.tokens ? a.b.seqs : a.b.tokens)) * a.c.kv_heads;
@@ -626,7 +627,7 @@ cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t 
 
 cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream)
 {
-    const unsigned blocks = (unsigned)items_at_most(a);
+    const unsigned blocks = (unsigned)items_at_most(a) + 1;
     return a.c.dim == 64 ? launch<64>(a, blocks, device, stream) : launch<128>(a, blocks, device, stream);
 }
 
