@@ -90,6 +90,7 @@ __device__ __forceinline__ void attention_block(const AttnArgs &a)
     __shared__ int     is_last[2];
     __shared__ Piece   piece[2 * kWarps];        // of each warp: the end of an item that began before, the beginning of one that goes on
     __shared__ float   row_sum[R];
+    __shared__ uint32_t odd_rows[kWarps][R];     // of a warp's item, bit gr: the row sees a value of group gr that is NaN, in a chunk that hides something
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     // this warp's ring; its unfinished first piece has a place of its own, its unfinished last piece that of the ring
@@ -112,6 +113,7 @@ __device__ __forceinline__ void attention_block(const AttnArgs &a)
     }
     if (lane == 31) warp_sum[warp] = incl;
     if (tid < 2 * kWarps) piece[tid].chunks = 0;
+    if (tid < kWarps * R) odd_rows[tid / R][tid % R] = 0;
     __syncthreads();
     int64_t total = 0;
 #pragma unroll
@@ -338,6 +340,21 @@ __device__ __forceinline__ void attention_block(const AttnArgs &a)
                         const int tok = tok0 + g + (j >> 1) * 8;
                         if (!paged || tok >= hi[nb][j & 1] || tok < lo[nb][j & 1] || tok >= s.len) sc[nb][j] = -INFINITY;
                     }
+                // What is hidden, or lies beyond the sequence's end, may be stored as anything: no scale that is NaN may meet its probability
+                // of 0.  Such a scale becomes 0, and the rows that see the value are noted.
+#pragma unroll 1
+                for (int x = lane; x < 16 * NG; x += 32) {
+                    uint32_t *w = reinterpret_cast<uint32_t *>(mine + at + 2 * kCodes) + 16 * NG + x;
+                    const bool bad = !(fabsf(__uint_as_float(*w)) < INFINITY);
+                    if (bad) *w = 0u;
+#pragma unroll 1
+                    for (uint32_t rest = __ballot_sync(NG == 1 ? 0xffffu : 0xffffffffu, bad); rest; rest &= rest - 1) {
+                        const int i = (x & ~31) + __ffs(rest) - 1, tok = tok0 + i / NG, r = block * R + lane;
+                        const int place = s.len - s.fresh + by_share(a, r);              // of this lane's row
+                        if (lane < R && r < rows && tok <= place && tok < s.len && (a.window == 0 || tok > place - a.window)) odd_rows[warp][lane] |= 1u << i % NG;
+                    }
+                }
+                __syncwarp();
             }
             bool rise = false;
 #pragma unroll
@@ -376,14 +393,6 @@ __device__ __forceinline__ void attention_block(const AttnArgs &a)
             load_words<NG>(w1, vw + (g + 8) * NG);
 #pragma unroll
             for (int j = 0; j < 4; ++j) load_words<NG>(z2[j], vw + (2 * t + (j >> 1) * 8 + (j & 1)) * NG);
-            if (!whole) {
-                // beyond the sequence's end a page holds anything: no scale from there may meet a probability of 0
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    w0[gr] = tok0 + g < s.len ? w0[gr] : 0u;
-                    w1[gr] = tok0 + g + 8 < s.len ? w1[gr] : 0u;
-                }
-            }
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
                 uint32_t r[4], pf[NB][2], pr[NB][2];
@@ -444,6 +453,14 @@ __device__ __forceinline__ void attention_block(const AttnArgs &a)
                                         64.0f * o[nb][gr * 4 + 2][j + 2 * half], 4.0f * o[nb][gr * 4 + 3][j + 2 * half]);
             }
         __syncwarp();
+        if (__any_sync(0xffffffffu, lane < R && odd_rows[warp][lane & (R - 1)])) {
+#pragma unroll 1
+            for (int e = lane; e < R * D; e += 32)
+                if (odd_rows[warp][e / D] >> (e % D / 64) & 1u) to[e / D * kOut + e % D] = __uint_as_float(0x7fc00000u);
+            __syncwarp();
+            if (lane < R) odd_rows[warp][lane] = 0;
+            __syncwarp();
+        }
         if (all) {
 #pragma unroll 1
             for (int e = lane; e < R * D / 4; e += 32) {

@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
     __shared__ __align__(8) uint64_t bars[4 * kStages + 14];
     __shared__ int64_t warp_sum[kThreads / 32];
     __shared__ __align__(4) unsigned char bad[kStages][4];          // chunks of a stage without a page
-    __shared__ uint32_t tmem_at;
+    __shared__ uint32_t tmem_at, odd_rows[kBlockRows];              // bit gr: the row sees a value of group gr that is NaN
     __shared__ int failed, at_seq, at_item;
     unsigned char *smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     const uint32_t base = smem_addr(smem);
@@ -163,6 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
         if (lane >= d) incl += o;
     }
     if (lane == 31) warp_sum[warp] = incl;
+    if (tid < kBlockRows) odd_rows[tid] = 0;
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
             bar_init(k_full + 8 * i, kWorkers / 2);
@@ -270,13 +271,29 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
             const uint32_t *words = reinterpret_cast<const uint32_t *>(raw + (j % kRaw) * S::kRawChunk + 16 * kRow);
             const uint32_t to = base + S::kKV + st * S::kStage + side * NG * S::kSlabK;
             const int mt = (lane >> 4) * 8 + (lane & 7), mc = lane >> 3 & 1, turn = D == 64 ? mt >> 2 & 1 : mt >> 1 & 3;
+            // what is hidden, or lies beyond the sequence's end, may be stored as anything, and a probability of 0 times a scale that is NaN would
+            // count: such a value's scale is 0 here, and the rows that see it are noted
+            uint32_t odd = 0;                           // bit gr: this lane's token
             if (lane < 16) {
-                // beyond the sequence's end a page holds anything: values from there count for nothing
                 float *scales = reinterpret_cast<float *>(smem + S::kSc + st * S::kScales) + side * NG * kKeys + (c * 8 + (lane >> 1)) * 2 * NG + (lane & 1);
 #pragma unroll
                 for (int gr = 0; gr < NG; ++gr) {
                     const float f = __uint_as_float(words[lane * NG + gr]);
-                    scales[gr * 2] = side ? (tok0 + lane < s.len ? f : 0.0f) : f * a.scale_log2;
+                    const bool fine = side == 0 || fabsf(f) < INFINITY;
+                    scales[gr * 2] = side ? (fine ? f : 0.0f) : f * a.scale_log2;
+                    if (!fine) odd |= 1u << gr;
+                }
+            }
+            if (side && __any_sync(0xffffffffu, odd != 0)) {
+#pragma unroll 1
+                for (uint32_t rest = __ballot_sync(0xffffffffu, odd != 0); rest; rest &= rest - 1) {
+                    const int of = __ffs(rest) - 1, tok = tok0 + of;
+                    const uint32_t groups = __shfl_sync(0xffffffffu, odd, of);
+#pragma unroll 1
+                    for (int row = lane; row < kBlockRows && block * kBlockRows + row < rows; row += 32) {
+                        const int at = s.len - s.fresh + by_share(a, block * kBlockRows + row);
+                        if (tok <= at && (a.window == 0 || tok > at - a.window)) atomicOr(&odd_rows[row], groups);
+                    }
                 }
             }
             if (side == 0 && lane == 0) bad[st][c] = !on && tok0 < end;
@@ -553,7 +570,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const AttnArgs a)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 if (mine + 8 * b < rows) {
-                    auto of = [&](int j, int g) { return (j & 1 ? 4.0f : 64.0f) * __uint_as_float(v[4 * j + 2 * b + g]) * inv[b]; };
+                    const float f = odd_rows[mine - block * kBlockRows + 8 * b] >> (at / 64) & 1u ? __uint_as_float(0x7fc00000u) : inv[b];
+                    auto of = [&](int j, int g) { return (j & 1 ? 4.0f : 64.0f) * __uint_as_float(v[4 * j + 2 * b + g]) * f; };
                     const uint4 x = make_uint4(pack_bf16(of(0, 0), of(1, 0)), pack_bf16(of(2, 0), of(3, 0)), pack_bf16(of(0, 1), of(1, 1)), pack_bf16(of(2, 1), of(3, 1)));
                     __nv_bfloat16 *to = out[b] + at;
                     if (a.out_vec) {
