@@ -686,7 +686,8 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     a.scale_log2 = (float)(scale * 1.4426950408889634);
     a.scale_code = std::ldexp(a.scale_log2, 69);
     a.q_heads    = args->q_heads;
-    a.window     = args->window;
+    // (a window that no sequence in the table is longer than hides nothing, and differences of positions and smaller ones stay in 32 bits)
+    a.window     = args->window < (batch->table_ld << a.c.page_shift) ? args->window : 0;
     a.status     = kv->status;
     a.share      = args->q_heads / cache->kv_heads;
     a.q_vec      = (uintptr_t)args->q % 16 == 0 && args->q_ld % 8 == 0 && args->q_head % 8 == 0;

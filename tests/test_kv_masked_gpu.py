@@ -1,5 +1,5 @@
 """What a row must not see does not reach it: tokens of the same sequence after it, and tokens before its window, whatever is stored
-for them."""
+for them.  And windows of any size."""
 import math
 
 import pytest
@@ -53,3 +53,15 @@ def test_hidden_tokens_may_hold_anything(kv, seqs, hq, hkv, dim, page, window, b
     assert torch.isnan(got[hit]).all()
     assert torch.isfinite(got[~hit]).all()
     assert torch.equal(got[~sees], clean[~sees])
+
+
+@pytest.mark.parametrize("seqs,hq,hkv,dim,page", [([(9, 3), (1, 30)], 8, 2, 128, 16), ([(20, 9)], 1, 1, 128, 16), ([(40, 20)], 5, 1, 256, 32),
+                                                   ([(900, 400), (300, 1)], 16, 8, 128, 16), ([(1500, 700)], 8, 8, 64, 16)])
+def test_a_window_of_any_size(kv, seqs, hq, hkv, dim, page):      # noqa: F811
+    """More new tokens than tokens, so that positions are negative; a window no smaller than the sequence hides nothing."""
+    s = Setup(seqs, hkv, dim, page, seed=4, single=False)
+    s.fill(kv, seed=13)
+    q = normal(s.tokens, hq, dim, seed=6)
+    want = kv.attention(s.cache, s.batch, q)
+    for window in (max(t for _, t in seqs), 100000, 2 ** 31 - 1):
+        assert torch.equal(kv.attention(s.cache, s.batch, q, window=window), want), window
