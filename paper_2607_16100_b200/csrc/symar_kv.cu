@@ -472,7 +472,7 @@ int kv_check(const symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv
     if (!kv || !cache || !batch) return SYMAR_ERR_INVAL;
     if (!symar_kv_page_bytes(cache->kv_heads, cache->head_dim, cache->page_size)) return SYMAR_ERR_UNSUPPORTED;
     if (!cache->pages || (uintptr_t)cache->pages % 16 || cache->num_pages < 1) return SYMAR_ERR_INVAL;
-    if (batch->seqs < 0 || batch->tokens < 0 || batch->table_ld < 0) return SYMAR_ERR_INVAL;
+    if (batch->seqs < 0 || batch->tokens < 0 || batch->table_ld < 0 || batch->table_ld >= 1ll << 48) return SYMAR_ERR_INVAL;
     if (batch->seqs > SYMAR_KV_MAX_SEQS) return SYMAR_ERR_UNSUPPORTED;
     if (batch->tokens > 0) {
         if (!batch->lengths || !batch->page_table || batch->seqs == 0) return SYMAR_ERR_INVAL;
