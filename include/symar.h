@@ -436,7 +436,7 @@ const char *symar_last_cuda_error(void);
  *
  * Conventions.  Plain device pointers; every stride is in ELEMENTS of the tensor it belongs to and the
  * innermost axis is contiguous.  Strides are not negative; they may be larger than the extent they cover, and 0
- * where an operand is shared; rows that a call writes do not overlap.  Calls enqueue on `cuda_stream`, return a status and may be captured in a CUDA graph; they
+ * where an operand is shared; rows that a call writes do not overlap (SYMAR_ERR_INVAL where they do).  Calls enqueue on `cuda_stream`, return a status and may be captured in a CUDA graph; they
  * allocate nothing.  Results are deterministic: no sum depends on the order in which blocks run.       */
 
 typedef enum {
@@ -453,7 +453,7 @@ typedef enum {
  * the tensor cores, whose additions truncate, are added up in IEEE binary32 every 128 products.
  * root: the one group that adds bias and residual; -1 = every group.  (Of P partial products that an AllReduce
  * will add, one rank carries the bias and the residual.)
- * group strides of 0 share an operand; an out_group of 0 is an error where groups > 1, as is an out_ld below n.  m, n
+ * group strides of 0 share an operand; rows of `out` that have an element in common are an error.  m, n
  * or k of 0 is allowed (k = 0: the product is 0).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
  * are read by the copy engine, others by the block's threads.
  * status: optional device word (may be NULL), cleared on the stream before the launch and set to SYMAR_ERR_TIMEOUT if a

@@ -674,7 +674,7 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     if (batch->tokens == 0) return SYMAR_OK;
     if (!args->q || !args->out || ((uintptr_t)args->q | (uintptr_t)args->out) % 2) return SYMAR_ERR_INVAL;
     if (args->q_ld < 0 || args->q_head < 0 || args->out_ld < 0 || args->out_head < 0 ||
-        kv_rows_meet(batch->tokens, args->q_heads, a.c.dim, args->out_ld, args->out_head))
+        rows_meet(batch->tokens, args->out_ld, args->q_heads, args->out_head, a.c.dim))
         return SYMAR_ERR_INVAL;
     a.q          = (const __nv_bfloat16 *)args->q;
     a.out        = (__nv_bfloat16 *)args->out;

@@ -626,7 +626,7 @@ int symar_kv_append(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_k
         !make_rows(&a.qo, args->q_out, args->q_out_ld, args->q_out_head, args->dtype) ||
         !make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
         !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype) ||
-        (a.q_heads > 0 && kv_rows_meet(batch->tokens, a.q_heads, a.c.dim, args->q_out_ld, args->q_out_head)))
+        (a.q_heads > 0 && rows_meet(batch->tokens, args->q_out_ld, a.q_heads, args->q_out_head, a.c.dim)))
         return SYMAR_ERR_INVAL;
     a.table       = (const float2 *)args->rotations;
     a.table_rows  = args->rotation_rows;
@@ -673,8 +673,8 @@ int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_
     if (batch->tokens == 0 || (!args->k && !args->v)) return SYMAR_OK;
     if (!make_rows(&a.k, args->k, args->k_ld, args->k_head, args->dtype) ||
         !make_rows(&a.v, args->v, args->v_ld, args->v_head, args->dtype) ||
-        (args->k && kv_rows_meet(batch->tokens, a.c.kv_heads, a.c.dim, args->k_ld, args->k_head)) ||
-        (args->v && kv_rows_meet(batch->tokens, a.c.kv_heads, a.c.dim, args->v_ld, args->v_head)))
+        (args->k && rows_meet(batch->tokens, args->k_ld, a.c.kv_heads, args->k_head, a.c.dim)) ||
+        (args->v && rows_meet(batch->tokens, args->v_ld, a.c.kv_heads, args->v_head, a.c.dim)))
         return SYMAR_ERR_INVAL;
     a.status = kv->status;
     a.by_heads = reciprocal(2 * a.c.kv_heads);

@@ -641,9 +641,8 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     const uintptr_t width = p.out_dtype == SYMAR_F32 ? 4 : 2;
     if (!p.out || (p.k > 0 && (!p.x || !p.w)) || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
     if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || ((uintptr_t)p.out | (uintptr_t)p.residual) % width) return SYMAR_ERR_INVAL;
-    if ((p.groups > 1 && p.out_group == 0) || (p.m > 1 && p.out_ld < p.n)) return SYMAR_ERR_INVAL;
     if (p.x_ld < 0 || p.x_group < 0 || p.w_ld < 0 || p.w_group < 0 || p.bias_group < 0 || p.residual_ld < 0 || p.residual_group < 0 ||
-        p.out_ld < 0 || p.out_group < 0)
+        p.out_ld < 0 || p.out_group < 0 || rows_meet(p.m, p.out_ld, p.groups, p.out_group, p.n))
         return SYMAR_ERR_INVAL;
     Device d;
     const int rc = device_info(&d);

@@ -8,6 +8,7 @@
 
 #include "symar.h"
 #include "symar_internal.h"
+#include "symar_rows.h"
 
 // The context of the cache operators (owned by symar_kv.cu).
 struct symar_kv {
@@ -105,12 +106,6 @@ inline cudaError_t allow_shared(const void *fn, int bytes, int device, std::atom
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
     return e;
-}
-
-// rows that a call would write twice
-inline bool kv_rows_meet(int tokens, int heads, int dim, int64_t ld, int64_t head)
-{
-    return (tokens > 1 && ld < dim) || (heads > 1 && head < dim);
 }
 
 // Argument checks shared by the calls on a cache; fills the views.
