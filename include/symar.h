@@ -528,7 +528,7 @@ size_t symar_kv_page_bytes(int kv_heads, int head_dim, int page_size);
  *   SYMAR_ROPE_BASE      base replaced by base * factor^(rot_dim / (rot_dim - 2))
  *   SYMAR_ROPE_BY_PARTS  with r = original / (2 pi / f_i) turns over the original context:
  *                        (1 - g) f_i / factor + g f_i,  g = clamp((r - low) / (high - low), 0, 1)
- * and cos and sin multiplied by `magnitude` (0 counts as 1).                                      */
+ * and cos and sin multiplied by `magnitude` (0 counts as 1).  All that a kind uses is finite, base and factor (and original) above 0. */
 typedef enum { SYMAR_ROPE_PLAIN = 0, SYMAR_ROPE_LINEAR = 1, SYMAR_ROPE_BASE = 2, SYMAR_ROPE_BY_PARTS = 3 } symar_rope_t;
 typedef struct {
     double  base, factor, original, low, high, magnitude;

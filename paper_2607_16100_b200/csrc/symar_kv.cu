@@ -584,9 +584,14 @@ int symar_rope_table(void *table, int64_t rows, const symar_rope_scaling_t *s, v
 {
     if (!s || rows < 0 || s->rot_dim < 2 || s->rot_dim % 2 || s->rot_dim > 256) return SYMAR_ERR_INVAL;
     if (!(s->base > 0.0) || s->kind < SYMAR_ROPE_PLAIN || s->kind > SYMAR_ROPE_BY_PARTS) return SYMAR_ERR_INVAL;
-    if (s->kind != SYMAR_ROPE_PLAIN && !(s->factor > 0.0)) return SYMAR_ERR_INVAL;
+    if (s->kind != SYMAR_ROPE_PLAIN && (!(s->factor > 0.0) || !std::isfinite(s->factor))) return SYMAR_ERR_INVAL;
     if (s->kind == SYMAR_ROPE_BASE && s->rot_dim < 4) return SYMAR_ERR_INVAL;
     if (s->kind == SYMAR_ROPE_BY_PARTS && (!(s->original > 0.0) || !(s->high > s->low))) return SYMAR_ERR_INVAL;
+    const double base = s->kind == SYMAR_ROPE_BASE ? s->base * std::pow(s->factor, (double)s->rot_dim / (s->rot_dim - 2)) : s->base;
+    const double inv_factor = s->kind == SYMAR_ROPE_PLAIN ? 1.0 : 1.0 / s->factor;
+    // (an infinite base has no f_0, and infinite ends have no place between them)
+    if (!(base > 0.0) || !std::isfinite(base) || !std::isfinite(inv_factor) || !std::isfinite(s->magnitude)) return SYMAR_ERR_INVAL;
+    if (s->kind == SYMAR_ROPE_BY_PARTS && (!std::isfinite(s->original) || !std::isfinite(s->high - s->low))) return SYMAR_ERR_INVAL;
     if (rows == 0) return SYMAR_OK;
     if (!table || (uintptr_t)table % 8) return SYMAR_ERR_INVAL;
     TableArgs a;
@@ -594,8 +599,7 @@ int symar_rope_table(void *table, int64_t rows, const symar_rope_scaling_t *s, v
     a.rows       = rows;
     a.half       = s->rot_dim / 2;
     a.kind       = s->kind;
-    a.inv_factor = s->kind == SYMAR_ROPE_PLAIN ? 1.0 : 1.0 / s->factor;
-    const double base = s->kind == SYMAR_ROPE_BASE ? s->base * std::pow(s->factor, (double)s->rot_dim / (s->rot_dim - 2)) : s->base;
+    a.inv_factor = inv_factor;
     a.log2_base  = std::log2(base);
     a.original   = s->original;
     a.low        = s->low;

@@ -1,4 +1,6 @@
 """Operators around the AllReduces: more of what the library refuses on the host (no GPU needed), beside test_operators_abi.py."""
+import ctypes
+import math
 import subprocess
 
 import pytest
@@ -59,3 +61,16 @@ def test_rows_that_share_an_element_are_refused(lib, na, a, nb, b):          # n
     for n in "kv":
         assert call(lib, "read", cache=dict(kv_heads=nb), batch=batch, args={n + "_ld": a, n + "_head": b}) == symar.ERR_INVAL
     assert lib.symar_linear(linear_args(m=na, out_ld=a, groups=nb, out_group=b, n=128), None) == symar.ERR_INVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(base=math.inf), dict(base=math.nan), dict(magnitude=math.nan), dict(magnitude=math.inf), dict(magnitude=-math.inf),
+    dict(kind=1, factor=math.nan), dict(kind=1, factor=math.inf), dict(kind=1, factor=5e-324), dict(kind=2, factor=math.inf), dict(kind=2, factor=1e300, base=1e300),
+    dict(kind=2, factor=1e-300, base=1e-300), dict(kind=3, original=math.inf), dict(kind=3, high=math.inf), dict(kind=3, low=-math.inf),
+    dict(kind=3, low=math.nan),
+], ids=lambda c: ",".join(f"{k}={v}" for k, v in c.items()))
+def test_rope_table_refuses_what_is_not_finite(lib, bad):        # noqa: F811
+    f = dict(base=1e4, factor=2.0, original=64.0, low=1.0, high=4.0, magnitude=1.0, kind=0, rot_dim=64)
+    f.update(bad)
+    assert lib.symar_rope_table(SOME, 16, ctypes.byref(symar.RopeScaling(**f)), None) == symar.ERR_INVAL
+    assert lib.symar_rope_table(None, 0, ctypes.byref(symar.RopeScaling(**f)), None) == symar.ERR_INVAL
