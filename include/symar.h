@@ -515,8 +515,9 @@ int symar_kv_destroy(symar_kv_t *kv);
 /* Clear the status word and the context's counters (asynchronous). */
 int symar_kv_reset(symar_kv_t *kv, void *cuda_stream);
 /* Synchronous read: *code is SYMAR_OK, or SYMAR_ERR_INVAL once a call met a page number outside the pool, a position
- * beyond the page table's row or beyond the table of rotations; *seq and *position say where first.  Such a token
- * is neither written nor seen; the calls themselves return normally.  Out pointers may be NULL.          */
+ * beyond the page table's row or beyond the table of rotations; *seq and *position say where first.  A token without
+ * a page is neither written nor seen; one beyond the table of rotations is stored as NaN, its q left as it is.  The calls
+ * themselves return normally.  Out pointers may be NULL.          */
 int symar_kv_status(symar_kv_t *kv, int *code, int *seq, int *position);
 /* Bytes of one page; 0 for an unsupported shape. */
 size_t symar_kv_page_bytes(int kv_heads, int head_dim, int page_size);

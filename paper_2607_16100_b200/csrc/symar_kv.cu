@@ -357,9 +357,9 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(const AppendArgs a)
         }
         __syncwarp();
         if (is_q) store8(reinterpret_cast<T *>(a.qo.p) + (int64_t)(first + f.t) * a.qo.ld + (int64_t)f.h * a.qo.head + c0, a.qo.vec, x);
-        uint32_t word;
-        const uint32_t codes = quantise8(x, word);
-        if (on && !is_q && p.page >= 0 && !(a.table && p.pos >= a.table_rows)) {
+        uint32_t word, codes = quantise8(x, word);
+        if (a.table && p.pos >= a.table_rows) word = 0x7fc00000u, codes = 0u;      // cannot be turned: NaN, not what the page held before
+        if (on && !is_q && p.page >= 0) {
             const int hh = f.h - q_heads - (is_k ? 0 : a.c.kv_heads), ps = 1 << a.c.page_shift, row = (is_k ? 0 : ps) + (p.pos & (ps - 1));
             unsigned char *base = a.c.pages + p.page * a.c.page_bytes + hh * a.c.head_bytes;
             *reinterpret_cast<uint32_t *>(base + row * (a.c.dim / 2) + lane * 4) = codes;
