@@ -505,14 +505,15 @@ typedef struct {
 } symar_kv_batch_t;
 
 /* Context of the cache operators: partial results of sequences that several blocks share, and a status word.
- * One stream and one host thread at a time, like a heap.  symar_kv_create() allocates (synchronously), the
- * _on form takes caller memory of symar_kv_required_bytes() bytes, 256-byte aligned.                   */
+ * One stream and one host thread at a time, like a heap; every call on it with the device current that was when
+ * it was made.  symar_kv_create() allocates (synchronously), the _on form takes caller memory of
+ * symar_kv_required_bytes() bytes, 256-byte aligned, that no kernel uses any more when it is given back.     */
 typedef struct symar_kv symar_kv_t;
 size_t symar_kv_required_bytes(void);
 int symar_kv_create(symar_kv_t **kv);
 int symar_kv_create_on(symar_kv_t **kv, void *device_mem, size_t device_bytes);
 int symar_kv_destroy(symar_kv_t *kv);
-/* Clear the status word and the context's counters (asynchronous). */
+/* Clear the status word and the context's counters (asynchronous): on the stream of the context's other calls. */
 int symar_kv_reset(symar_kv_t *kv, void *cuda_stream);
 /* Synchronous read: *code is SYMAR_OK, or SYMAR_ERR_INVAL once a call met a page number outside the pool, a position
  * beyond the page table's row or beyond the table of rotations; *seq and *position say where first.  A token without

@@ -620,6 +620,7 @@ class KVContext:
             _ck(self._lib.symar_kv_create(byref(self._h)), "symar_kv_create")
         else:
             _ck(self._lib.symar_kv_create_on(byref(self._h), device_mem, device_bytes), "symar_kv_create_on")
+        self.index = _device()
 
     @classmethod
     def on_torch(cls, device="cuda:0") -> "KVContext":
@@ -642,12 +643,16 @@ class KVContext:
         except Exception:
             pass
 
-    def reset(self, stream: int = 0) -> None:
-        _ck(self._lib.symar_kv_reset(self._h, stream), "symar_kv_reset")
+    def reset(self, stream=None) -> None:
+        """Clear the status and the counters, on torch's current stream unless another is given: behind this context's calls
+        there, and before those that follow."""
+        _call(self._lib.symar_kv_reset, "symar_kv_reset", self.index, stream, self._h)
 
     def status(self):
+        """(code, sequence, position) of the first offence since the last reset; waits for the device."""
         code, seq, position = c_int(), c_int(), c_int()
-        _ck(self._lib.symar_kv_status(self._h, byref(code), byref(seq), byref(position)), "symar_kv_status")
+        with _T.cuda.device(self.index):
+            _ck(self._lib.symar_kv_status(self._h, byref(code), byref(seq), byref(position)), "symar_kv_status")
         return code.value, seq.value, position.value
 
     @staticmethod

@@ -1,0 +1,57 @@
+"""The Python calls of the operators, without a GPU: which stream, device and memory they name to the library.  A stand-in for the library
+takes their arguments; tensors are torch's CPU ones, whose device index is -1."""
+import contextlib
+import types
+
+import pytest
+import torch
+
+from paper_2607_16100_b200 import symar
+
+
+class Library:
+    """Every function returns OK and notes its name and arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def fn(*args):
+            self.calls.append((name, args))
+            return symar.OK
+        return fn
+
+
+@pytest.fixture()
+def lib(monkeypatch):
+    symar._torch()
+    lib = Library()
+    monkeypatch.setattr(symar, "_raw_stream", lambda index: 1000 + index)
+    monkeypatch.setattr(symar, "_device", lambda: -1)
+    monkeypatch.setattr(symar, "_lib", lib)
+    return lib
+
+
+@contextlib.contextmanager
+def noted(log, index):
+    log.append(index)
+    yield
+
+
+def context(lib, index=-1, keepalive=None):
+    c = object.__new__(symar.KVContext)
+    c._lib, c._h, c._keepalive, c.index = lib, 77, keepalive, index
+    return c
+
+
+def test_reset_and_status_follow_the_current_stream_and_the_contexts_device(lib, monkeypatch):
+    entered = []
+    monkeypatch.setattr(torch.cuda, "device", lambda index: noted(entered, index))
+    c = context(lib, index=3)
+    c.reset()
+    assert lib.calls == [("symar_kv_reset", (77, 1003))] and entered == [3]
+    c.reset(5)
+    assert lib.calls[-1] == ("symar_kv_reset", (77, 5)) and entered == [3, 3]
+    assert c.status() == (0, 0, 0)
+    assert lib.calls[-1][0] == "symar_kv_status" and entered == [3, 3, 3]
+    c._h = None

@@ -1,0 +1,36 @@
+"""The Python calls of the operators on a GPU: streams, memory and status words that they take or make by themselves."""
+import pytest
+import torch
+
+from paper_2607_16100_b200 import symar
+from test_kv_gpu import Setup, normal
+
+pytestmark = pytest.mark.gpu
+
+
+def test_reset_is_one_of_the_streams_calls():
+    """Captured between a call that records an offence and one that does not, on a side stream, with no stream named anywhere."""
+    c = symar.KVContext.on_torch()
+    s = Setup([(1, 40), (1, 20)], 1, 128, 16, seed=7)
+    s.fill(c, seed=71)
+    q = normal(2, 8, 128, seed=1)
+    want = c.attention(s.cache, s.batch, q)
+    table = s.table.clone()
+    table[1, 1] = -1
+    bad = symar.KVBatch(s.lengths, table)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    out = torch.empty_like(q)
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        c.attention(s.cache, bad, q, out=out)
+        c.reset()
+        c.attention(s.cache, s.batch, q, out=out)
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert c.status()[0] == symar.OK
+        assert torch.equal(out, want)
+    c.attention(s.cache, bad, q)
+    assert c.status()[0] == symar.ERR_INVAL
+    c.destroy()
