@@ -456,6 +456,7 @@ _T = None               # torch, once a call needed it
 _raw_stream = None      # device index -> handle of torch's current stream
 _device = None          # -> index of the current device
 _CODES = {}             # torch dtype -> symar_dtype_t
+_late = []              # (device index, memory) of contexts that were given back during a capture
 
 
 def _torch():
@@ -632,9 +633,17 @@ class KVContext:
             return cls((buf.data_ptr() + 255) // 256 * 256, n, keepalive=buf)
 
     def destroy(self) -> None:
+        """Gives the context back; its memory, where that is torch's, once no kernel of any stream uses it."""
         if self._h:
             self._lib.symar_kv_destroy(self._h)
             self._h = c_void_p()
+            if self._keepalive is not None:
+                if _T.cuda.is_current_stream_capturing():
+                    _late.append((self.index, self._keepalive))     # (waiting would end the capture: kept until the next that may)
+                else:
+                    for index in sorted({self.index, *(i for i, _ in _late)}):
+                        _T.cuda.synchronize(index)
+                    _late.clear()
             self._keepalive = None
 
     def __del__(self):

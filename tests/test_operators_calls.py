@@ -55,3 +55,26 @@ def test_reset_and_status_follow_the_current_stream_and_the_contexts_device(lib,
     assert c.status() == (0, 0, 0)
     assert lib.calls[-1][0] == "symar_kv_status" and entered == [3, 3, 3]
     c._h = None
+
+
+def test_torchs_memory_is_kept_until_no_kernel_uses_it(lib, monkeypatch):
+    """The allocator knows nothing of the streams that the context's calls ran on."""
+    capturing, log = [False], []
+
+    class Memory:
+        def __del__(self):
+            log.append("freed")
+
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda index: log.append(("waited", index)))
+    context(lib, 2, Memory()).destroy()
+    assert lib.calls == [("symar_kv_destroy", (77,))] and log == [("waited", 2), "freed"]
+    log.clear()
+    capturing[0] = True                                          # where nothing may wait: by the next that may
+    context(lib, 2, Memory()).destroy()
+    assert log == []
+    capturing[0] = False
+    context(lib, 2, None).destroy()                              # (memory of the library's own: cudaFree waits)
+    assert log == []
+    context(lib, 1, Memory()).destroy()
+    assert log == [("waited", 1), ("waited", 2), "freed", "freed"]

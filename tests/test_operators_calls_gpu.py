@@ -34,3 +34,23 @@ def test_reset_is_one_of_the_streams_calls():
     c.attention(s.cache, bad, q)
     assert c.status()[0] == symar.ERR_INVAL
     c.destroy()
+
+
+def test_a_context_given_back_during_a_capture():
+    """Its memory stays as it is until something may wait; the capture goes on."""
+    c, other = symar.KVContext.on_torch(), symar.KVContext.on_torch()
+    s = Setup([(1, 40)], 1, 128, 16, seed=7)
+    s.fill(c, seed=71)
+    q = normal(1, 8, 128, seed=1)
+    want = c.attention(s.cache, s.batch, q)
+    out, graph, side = torch.empty_like(q), torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        other.destroy()
+        c.attention(s.cache, s.batch, q, out=out)
+    assert len(symar._late) == 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    c.destroy()
+    assert not symar._late
