@@ -397,6 +397,10 @@ def allreduce_static(in_ptr: int, out_ptr: int, rank_pitch_bytes: int, P: int, c
 #
 # These take torch tensors (device memory, strides, dtypes and the current stream); everything is computed in the
 # library's kernels.  Innermost axes must be contiguous; all other strides are free.
+#
+# ``stream``: a handle (an int), torch's current stream unless given.  A result that a call makes then comes from that stream's memory, as
+# if torch had made it there; tensors of other streams that it reads or writes are to be ready for it, and kept until it is
+# done with them (Tensor.record_stream), as with torch's own calls.
 
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
@@ -495,6 +499,15 @@ def _call(fn, where, index: int, stream, *args) -> None:
         raise SymarError(rc, where)
 
 
+def _new(like, shape, dtype, index: int, stream):
+    """An uninitialised result beside ``like``, of the pool of the stream that the call runs on: nothing that is still queued on
+    torch's current stream uses its memory."""
+    if stream is None or stream == _raw_stream(index):
+        return like.new_empty(shape, dtype=dtype)
+    with _T.cuda.stream(_T.cuda.ExternalStream(stream, device=index) if stream else _T.cuda.default_stream(index)):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, stream=None):
     """``act(x @ w.T + bias) + residual`` (``symar_linear``).
 
@@ -520,7 +533,7 @@ def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root:
     else:
         groups, shape = 1, (m, n)
     if out is None:
-        out = x.new_empty(shape, dtype=out_dtype or bf16)
+        out = _new(x, shape, out_dtype or bf16, index, stream)
         os = out.stride()
     else:
         os = out.stride()
@@ -556,9 +569,11 @@ def rope_table(rows: int, rot_dim: int, *, base: float = 10000.0, kind: str = "p
     torch = _torch()
     if kind not in ROPE_KINDS or rows < 0:
         _bad("symar_rope_table", f"rows {rows}, kind {kind!r}")
-    table = torch.empty(rows, rot_dim // 2, 2, dtype=torch.float32, device=device)
+    at = torch.device(device)
+    index = _device() if at.index is None else at.index
+    table = _new(torch.empty(0, dtype=torch.float32, device=at), (rows, rot_dim // 2, 2), torch.float32, index, stream)
     how = RopeScaling(base, factor, original, low, high, magnitude, ROPE_KINDS[kind], rot_dim)
-    _call(load().symar_rope_table, "symar_rope_table", table.get_device(), stream, table.data_ptr(), rows, byref(how))
+    _call(load().symar_rope_table, "symar_rope_table", index, stream, table.data_ptr(), rows, byref(how))
     return table
 
 
@@ -689,7 +704,7 @@ class KVContext:
             if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or q.dtype is not dtype or q.get_device() != index:
                 self._refuse(where, "q", q, (tokens, q_heads, dim), dtype)
             if q_out is None:
-                q_out = q.new_empty(shape)
+                q_out = _new(q, shape, dtype, index, stream)
                 os = (q_heads * dim, dim)
             else:
                 os = q_out.stride()
@@ -712,7 +727,7 @@ class KVContext:
         """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
         heads, dim = cache.kv_heads, cache.head_dim
         dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
-        k, v = cache.pages.new_empty(shape, dtype=dtype), cache.pages.new_empty(shape, dtype=dtype)
+        k, v = (_new(cache.pages, shape, dtype, batch.index, stream) for _ in range(2))
         args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(dtype, "symar_kv_read"))
         batch.args.tokens = tokens
         _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.ref, byref(args))
@@ -726,7 +741,7 @@ class KVContext:
         if len(shape) != 3 or shape[2] != cache.head_dim or qs[2] != 1 or q.get_device() != index:
             _bad(where, f"q is [tokens, q_heads, {cache.head_dim}] on the batch's device with contiguous channels, not {tuple(shape)}")
         if out is None:
-            out = q.new_empty(shape)
+            out = _new(q, shape, dtype, index, stream)
         os = out.stride()
         if out.shape != shape or os[2] != 1 or out.dtype is not dtype or out.get_device() != index:
             self._refuse(where, "out", out, shape, dtype)

@@ -78,3 +78,39 @@ def test_torchs_memory_is_kept_until_no_kernel_uses_it(lib, monkeypatch):
     assert log == []
     context(lib, 1, Memory()).destroy()
     assert log == [("waited", 1), ("waited", 2), "freed", "freed"]
+
+
+def setting(index=-1):
+    """A cache of two heads and a batch of three tokens, as the calls see them."""
+    cache = object.__new__(symar.PagedKV)
+    cache.pages, cache.head_dim, cache.page_size, cache.kv_heads = torch.empty(4, 2, 2304, dtype=torch.uint8), 128, 16, 2
+    cache.index, cache.args = index, symar.KVCacheArgs(0, 4, 2, 128, 16)
+    cache.ref = cache.args
+    batch = object.__new__(symar.KVBatch)
+    batch.index, batch.args = index, symar.KVBatchArgs(0, None, 0, 4, 3, 0)
+    batch.ref = batch.args
+    batch.last = (0, batch.args, batch.ref)
+    return cache, batch, torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 4, 128, dtype=torch.bfloat16)
+
+
+def test_results_come_from_the_memory_of_the_stream_that_is_named(lib, monkeypatch):
+    entered = []
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: noted(entered, s))
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device: (handle, device))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda index: (0, index))
+    cache, batch, k, q = setting()
+    c = context(lib)
+    for stream, want in ((None, []), (999, []), (5, [(5, -1)]), (0, [(0, -1)])):          # 999: the current one
+        for call, results in ((lambda: c.append(cache, batch, k, k, q=q, stream=stream), 1),
+                              (lambda: c.read(cache, batch, 3, stream=stream), 2),
+                              (lambda: c.attention(cache, batch, q, stream=stream), 1),
+                              (lambda: symar.rope_table(4, 64, device="cpu", stream=stream), 1)):
+            entered.clear()
+            call()
+            assert entered == want * results
+            assert lib.calls[-1][1][-1] == (999 if stream is None else stream)
+        entered.clear()
+        c.append(cache, batch, k, k, q=q, q_out=q, stream=stream)
+        c.attention(cache, batch, q, out=q, stream=stream)
+        assert entered == []
+    c._h = None

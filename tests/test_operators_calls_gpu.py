@@ -54,3 +54,31 @@ def test_a_context_given_back_during_a_capture():
     assert torch.equal(out, want)
     c.destroy()
     assert not symar._late
+
+
+def stream_of(t):
+    """The stream whose pool a tensor's memory is of."""
+    at = t.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+def test_results_are_of_the_stream_that_is_named():
+    c = symar.KVContext.on_torch()
+    s = Setup([(1, 40), (1, 20)], 2, 128, 16, seed=7)
+    s.fill(c, seed=71)
+    q, k = normal(2, 8, 128, seed=1), normal(2, 2, 128, seed=2)
+    x, w = normal(4, 128, seed=3), normal(64, 128, seed=4)
+    side = torch.cuda.Stream()
+    want = symar.linear(x, w), *c.read(s.cache, s.batch, 2), c.attention(s.cache, s.batch, q), symar.rope_table(9, 64)
+    torch.cuda.synchronize()
+    for handle, home in ((side.cuda_stream, side), (0, torch.cuda.default_stream())):
+        with torch.cuda.stream(torch.cuda.default_stream() if handle else side):         # the other one is current
+            got = (symar.linear(x, w, stream=handle), *c.read(s.cache, s.batch, 2, stream=handle),
+                   c.attention(s.cache, s.batch, q, stream=handle), symar.rope_table(9, 64, stream=handle))
+            turned = c.append(s.cache, s.batch, k, k, q=q, stream=handle)
+        torch.cuda.synchronize()
+        for t in (*got, turned):
+            assert stream_of(t) == home.cuda_stream
+        assert all(torch.equal(a, b) for a, b in zip(got[:1] + got[4:], want[:1] + want[4:]))
+    assert c.status()[0] == symar.OK
+    c.destroy()
