@@ -620,8 +620,16 @@ class KVBatch:
                 _bad("KVBatch", "token_start [seqs + 1] is a contiguous int32 CUDA tensor")
             start = token_start.data_ptr()
         self.lengths, self.page_table, self.token_start, self.seqs, self.index = lengths, page_table, token_start, seqs, index
-        self.args = KVBatchArgs(lengths.data_ptr(), start, page_table.data_ptr(), ps[1], seqs, 0)
-        self.ref = byref(self.args)
+        self._fields = lengths.data_ptr(), start, page_table.data_ptr(), ps[1], seqs
+        self._last = (None, None)
+
+    def of(self, tokens: int):
+        """What a call with that many rows hands to the library.  Nothing that is handed out changes any more: calls of several threads
+        may share a batch."""
+        last = self._last
+        if last[0] != tokens:
+            last = self._last = (tokens, byref(KVBatchArgs(*self._fields, tokens)))
+        return last[1]
 
 
 class KVContext:
@@ -719,8 +727,7 @@ class KVContext:
             rp, rows, rot = rotations.data_ptr(), rs[0], 2 * rs[1]
         args = KVAppendArgs(qp, qs[0], qs[1], op, os[0], os[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], rp, rows, rot,
                             1 if interleaved else 0, q_heads, code)
-        batch.args.tokens = tokens
-        _call(self._lib.symar_kv_append, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
+        _call(self._lib.symar_kv_append, where, index, stream, self._h, cache.ref, batch.of(tokens), byref(args))
         return q_out
 
     def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
@@ -729,8 +736,7 @@ class KVContext:
         dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
         k, v = (_new(cache.pages, shape, dtype, batch.index, stream) for _ in range(2))
         args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(dtype, "symar_kv_read"))
-        batch.args.tokens = tokens
-        _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.ref, byref(args))
+        _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.of(tokens), byref(args))
         return k, v
 
     def attention(self, cache: PagedKV, batch: KVBatch, q, *, out=None, scale: float = 0.0, window: int = 0, stream=None):
@@ -746,8 +752,7 @@ class KVContext:
         if out.shape != shape or os[2] != 1 or out.dtype is not dtype or out.get_device() != index:
             self._refuse(where, "out", out, shape, dtype)
         args = KVAttentionArgs(q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], scale, shape[1], window, code)
-        batch.args.tokens = shape[0]
-        _call(self._lib.symar_kv_attention, where, index, stream, self._h, cache.ref, batch.ref, byref(args))
+        _call(self._lib.symar_kv_attention, where, index, stream, self._h, cache.ref, batch.of(shape[0]), byref(args))
         return out
 
 

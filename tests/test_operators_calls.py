@@ -87,9 +87,7 @@ def setting(index=-1):
     cache.index, cache.args = index, symar.KVCacheArgs(0, 4, 2, 128, 16)
     cache.ref = cache.args
     batch = object.__new__(symar.KVBatch)
-    batch.index, batch.args = index, symar.KVBatchArgs(0, None, 0, 4, 3, 0)
-    batch.ref = batch.args
-    batch.last = (0, batch.args, batch.ref)
+    batch.index, batch._fields, batch._last = index, (0, None, 0, 4, 3), (None, None)
     return cache, batch, torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, 4, 128, dtype=torch.bfloat16)
 
 
@@ -113,4 +111,17 @@ def test_results_come_from_the_memory_of_the_stream_that_is_named(lib, monkeypat
         c.append(cache, batch, k, k, q=q, q_out=q, stream=stream)
         c.attention(cache, batch, q, out=q, stream=stream)
         assert entered == []
+    c._h = None
+
+
+def test_a_batch_may_be_shared_by_threads(lib):
+    """What one call hands to the library stays as it was while another is made with more rows."""
+    cache, batch, _, _ = setting()
+    c = context(lib)
+    for tokens in (3, 7, 7, 0, 3):
+        c.read(cache, batch, tokens)
+    handed = [args[2] for name, args in lib.calls]
+    assert [h._obj.tokens for h in handed] == [3, 7, 7, 0, 3]
+    assert all(h._obj.seqs == 3 and h._obj.table_ld == 4 for h in handed)
+    assert handed[1] is handed[2]                                # (a loop's calls make it once)
     c._h = None
