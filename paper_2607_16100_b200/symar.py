@@ -589,7 +589,7 @@ class PagedKV:
         if pages.dtype is not torch.uint8 or len(shape) != 3 or shape[2] != each or not pages.is_contiguous() or \
                 not pages.is_cuda:
             _bad("PagedKV", f"pages are a contiguous CUDA uint8 tensor [pages, kv_heads, {each}]")
-        self.pages, self.head_dim, self.page_size, self.kv_heads = pages, head_dim, page_size, shape[1]
+        self.pages, self.head_dim, self.page_size, self.kv_heads, self.index = pages, head_dim, page_size, shape[1], pages.get_device()
         self.args = KVCacheArgs(pages.data_ptr(), shape[0], shape[1], head_dim, page_size)
         self.ref = byref(self.args)
 
@@ -687,6 +687,10 @@ class KVContext:
             _ck(self._lib.symar_kv_status(self._h, byref(code), byref(seq), byref(position)), "symar_kv_status")
         return code.value, seq.value, position.value
 
+    def _one_device(self, where, cache, batch):
+        if cache.index != batch.index or self.index != batch.index:
+            _bad(where, f"the context is of device {self.index}, the cache of {cache.index}, the batch of {batch.index}")
+
     @staticmethod
     def _refuse(where, name, t, shape, dtype):
         _bad(where, f"{name} is {list(shape)} {dtype} on the batch's device with contiguous channels, not {tuple(t.shape)} {t.dtype} on "
@@ -698,6 +702,7 @@ class KVContext:
         where = "symar_kv_append"
         dtype, index, dim, ks, vs = k.dtype, batch.index, cache.head_dim, k.stride(), v.stride()
         code = _dtype_code(dtype, where)
+        self._one_device(where, cache, batch)
         tokens = k.shape[0]
         shape = (tokens, cache.kv_heads, dim)
         if k.shape != shape or ks[2] != 1 or k.get_device() != index:
@@ -732,6 +737,7 @@ class KVContext:
 
     def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
         """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
+        self._one_device("symar_kv_read", cache, batch)
         heads, dim = cache.kv_heads, cache.head_dim
         dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
         k, v = (_new(cache.pages, shape, dtype, batch.index, stream) for _ in range(2))
@@ -743,6 +749,7 @@ class KVContext:
         """Attention of the batch's new tokens over the cache (``symar_kv_attention``)."""
         where = "symar_kv_attention"
         shape, dtype, index = q.shape, q.dtype, batch.index
+        self._one_device(where, cache, batch)
         code, qs = _dtype_code(dtype, where), q.stride()
         if len(shape) != 3 or shape[2] != cache.head_dim or qs[2] != 1 or q.get_device() != index:
             _bad(where, f"q is [tokens, q_heads, {cache.head_dim}] on the batch's device with contiguous channels, not {tuple(shape)}")

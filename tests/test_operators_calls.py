@@ -125,3 +125,15 @@ def test_a_batch_may_be_shared_by_threads(lib):
     assert all(h._obj.seqs == 3 and h._obj.table_ld == 4 for h in handed)
     assert handed[1] is handed[2]                                # (a loop's calls make it once)
     c._h = None
+
+
+@pytest.mark.parametrize("of_context,of_cache,of_batch", [(0, -1, -1), (-1, 0, -1), (-1, -1, 0), (1, 1, 0), (0, 1, 1)])
+def test_context_cache_and_batch_are_of_one_device(lib, of_context, of_cache, of_batch):
+    cache, batch, k, q = setting()
+    c = context(lib, of_context)
+    cache.index, batch.index = of_cache, of_batch
+    for call in (lambda: c.append(cache, batch, k, k, q=q), lambda: c.read(cache, batch, 3), lambda: c.attention(cache, batch, q)):
+        with pytest.raises(symar.SymarError, match="device"):
+            call()
+    assert lib.calls == []
+    c._h = None
