@@ -515,7 +515,8 @@ int symar_kv_create_on(symar_kv_t **kv, void *device_mem, size_t device_bytes);
 int symar_kv_destroy(symar_kv_t *kv);
 /* Clear the status word and the context's counters (asynchronous): on the stream of the context's other calls. */
 int symar_kv_reset(symar_kv_t *kv, void *cuda_stream);
-/* Synchronous read: *code is SYMAR_OK, or SYMAR_ERR_INVAL once a call met a page number outside the pool, a position
+/* Synchronous read: *code is SYMAR_OK, SYMAR_ERR_TIMEOUT once a wait inside attention (for its own copies and products, four
+ * seconds at most) gave up, so that results are incomplete, or SYMAR_ERR_INVAL once a call met a page number outside the pool, a position
  * beyond the page table's row or beyond the table of rotations; *seq and *position say where first.  A token without
  * a page is neither written nor seen; one beyond the table of rotations is stored as NaN, its q left as it is.  The calls
  * themselves return normally.  Out pointers may be NULL.          */

@@ -508,13 +508,15 @@ def _new(like, shape, dtype, index: int, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
-def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, stream=None):
+def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, status=None,
+           stream=None):
     """``act(x @ w.T + bias) + residual`` (``symar_linear``).
 
     x [m, k] or [groups, m, k] and w [n, k] or [groups, n, k] bfloat16; bias [n] or [groups, n]; residual and the
     result [m, n] or [groups, m, n] of ``out_dtype`` (bfloat16 unless said or given by ``out``).  Operands of two
     dimensions (or expanded ones) are shared by all groups.  ``root``: the one group that adds bias and residual,
-    -1 = every group."""
+    -1 = every group.  ``status``: an int32 CUDA tensor of one element that the call sets, on its stream, to OK or, where a wait
+    inside the kernel gave up and the result is incomplete, to ERR_TIMEOUT; without it nothing says so."""
     torch = _T or _torch()
     where = "symar_linear"
     bf16 = torch.bfloat16
@@ -555,9 +557,14 @@ def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root:
                 residual.get_device() != index:
             _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
+    sp = 0
+    if status is not None:
+        if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != index:
+            _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
+        sp = status.data_ptr()
     args = LinearArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[0] if wd == 3 else 0, bp, bg, rp, rl,
                       rg, out.data_ptr(), os[-2], os[0] if len(os) == 3 else 0, groups, m, n, k,
-                      _dtype_code(out.dtype, where), act_code, root)
+                      _dtype_code(out.dtype, where), act_code, root, sp)
     _call((_lib or load()).symar_linear, where, index, stream, byref(args))
     return out
 

@@ -82,3 +82,14 @@ def test_results_are_of_the_stream_that_is_named():
         assert all(torch.equal(a, b) for a, b in zip(got[:1] + got[4:], want[:1] + want[4:]))
     assert c.status()[0] == symar.OK
     c.destroy()
+
+
+def test_a_product_reports_to_the_status_word_it_is_given():
+    x, w = normal(4, 128, seed=3), normal(64, 128, seed=4)
+    want = symar.linear(x, w)
+    words = torch.full((3,), 77, dtype=torch.int32, device="cuda")
+    assert torch.equal(symar.linear(x, w, status=words[1]), want)
+    assert words.tolist() == [77, symar.OK, 77]
+    for bad in (words, words[:0], words[:1].long(), words[:1].cpu(), words[:1].float()):
+        with pytest.raises(symar.SymarError):
+            symar.linear(x, w, status=bad)
