@@ -562,18 +562,14 @@ struct Device {
 };
 int device_info(Device *d)
 {
-    static Device known[64];
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
+    static std::atomic<int> known[64];                   // multiprocessors; 0: not asked yet (by any thread)
+    cudaError_t e = cudaGetDevice(&d->id);
     if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-    if (dev >= 0 && dev < 64 && known[dev].sms > 0) {
-        *d = known[dev];
-        return SYMAR_OK;
-    }
-    d->id = dev;
-    e     = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev);
+    const bool slot = d->id >= 0 && d->id < 64;
+    if (slot && (d->sms = known[d->id].load(std::memory_order_relaxed)) > 0) return SYMAR_OK;
+    e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->id);
     if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
-    if (dev >= 0 && dev < 64) known[dev] = *d;
+    if (slot) known[d->id].store(d->sms, std::memory_order_relaxed);
     return SYMAR_OK;
 }
 

@@ -1,4 +1,9 @@
 """The Python calls of the operators on a GPU: streams, memory and status words that they take or make by themselves."""
+import os
+import subprocess
+import sys
+from pathlib import Path
+
 import pytest
 import torch
 
@@ -93,3 +98,41 @@ def test_a_product_reports_to_the_status_word_it_is_given():
     for bad in (words, words[:0], words[:1].long(), words[:1].cpu(), words[:1].float()):
         with pytest.raises(symar.SymarError):
             symar.linear(x, w, status=bad)
+
+
+def test_threads_each_with_a_stream_and_a_context():
+    """Products need no context; cache calls of two threads share a cache and a batch, and have a context each.  In a process of its own, so
+    that the first call that the library sees comes from all threads at once."""
+    program = """
+import sys, threading
+import torch
+from paper_2607_16100_b200 import symar
+from test_kv_gpu import Setup, normal
+n = 6
+fill = symar.KVContext.on_torch()
+s = Setup([(1, 400), (1, 20), (1, 77)], 2, 128, 16, seed=7)
+q, x, w = normal(3, 8, 128, seed=1), normal(33, 328, seed=3), normal(64, 328, seed=4)
+s.fill(fill, seed=71)
+own = [(torch.cuda.Stream(), symar.KVContext.on_torch()) for _ in range(n)]
+torch.cuda.synchronize()
+got, gate = [None] * n, threading.Barrier(n)
+def work(i):
+    stream, c = own[i]
+    with torch.cuda.stream(stream):
+        gate.wait()
+        for _ in range(50):
+            got[i] = symar.linear(x, w), c.attention(s.cache, s.batch, q)
+        stream.synchronize()
+threads = [threading.Thread(target=work, args=(i,)) for i in range(n)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert all(torch.equal(a, b) for g in got for a, b in zip(g, got[0]))
+want = x.double() @ w.double().T
+assert ((got[0][0].double() - want).abs() <= 2.0 ** -8 * want.abs() + 328 * 2.0 ** -23 * (x.double().abs() @ w.double().abs().T)).all()
+assert torch.equal(got[0][1], fill.attention(s.cache, s.batch, q))
+assert all(c.status()[0] == symar.OK for _, c in own)
+print("threads agree")
+"""
+    run = subprocess.run([sys.executable, "-c", program], cwd=Path(__file__).parent, capture_output=True, text=True, timeout=300,
+                         env={**os.environ, "PYTHONPATH": str(Path(__file__).parent.parent)})
+    assert run.returncode == 0 and "threads agree" in run.stdout, run.stderr[-2000:]
