@@ -701,7 +701,7 @@ extern "C" int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache,
     if ((int64_t)a.b.tokens * a.share > 0x7fff0000) return SYMAR_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
-    if (prompt_attention_takes(a, kv->num_sms)) {
+    if (prompt_attention_takes(a, kv->num_sms, kv->device)) {
         e = launch_prompt_attention(a, kv->device, st);
         return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_kv_attention");
     }

@@ -172,7 +172,7 @@ __device__ __forceinline__ void zero_other_rows(const AttnArgs &a, int at, int b
 constexpr float kNothing = -3.402823466e38f;
 
 // Prompts: many query rows of a sequence (symar_prompt.cu).  False: not for this kernel.
-bool prompt_attention_takes(const AttnArgs &a, int num_sms);
+bool prompt_attention_takes(const AttnArgs &a, int num_sms, int device);
 cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream);
 
 }  // namespace symar

@@ -609,9 +609,29 @@ int64_t items_at_most(const AttnArgs &a)
     return ((int64_t)a.b.tokens * a.share / kBlockRows + (a.b.seqs < a.b.tokens ? a.b.seqs : a.b.tokens)) * a.c.kv_heads;
 }
 
+// The warpgroups share out what a block is launched with; with less than that they would wait for ever.
+template <int D>
+bool registers_suffice(int device)
+{
+    static std::atomic<uint64_t> known{0};
+    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (known.load(std::memory_order_relaxed) & bit) return true;
+    cudaFuncAttributes at;
+    if (cudaFuncGetAttributes(&at, (const void *)prompt_kernel<D>) != cudaSuccess || at.numRegs < kRegsLaunch) return false;
+    known.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+template <int D>
+cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t stream)
+{
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_shared((const void *)prompt_kernel<D>, Shape<D>::kBytes, device, allowed);
+    if (e != cudaSuccess) return e;
+    return launch_early(prompt_kernel<D>, dim3(blocks), kThreads, Shape<D>::kBytes, stream, a);
+}
 }  // namespace
 
-bool prompt_attention_takes(const AttnArgs &a, int num_sms)
+bool prompt_attention_takes(const AttnArgs &a, int num_sms, int device)
 {
     if (a.c.dim > 128 || items_at_most(a) > 0x3fffffff) return false;
     // Blocks that are half full at least, and for a quarter of the multiprocessors.  (64 heads, 8 key/value heads unless said; this kernel
@@ -620,28 +640,9 @@ bool prompt_attention_takes(const AttnArgs &a, int num_sms)
     // 64 x 8 over 1024, a quarter full: 139, 122; 32 x 32 with 8 heads of 8, an eighth: 69, 44.)
     const int64_t rows = (int64_t)a.b.tokens * a.share;                // of one key/value head
     const int64_t blocks = rows / kBlockRows > a.b.seqs ? rows / kBlockRows : a.b.seqs;
-    return rows >= (int64_t)kRows * a.b.seqs && blocks * a.c.kv_heads >= num_sms / 4;
+    if (rows < (int64_t)kRows * a.b.seqs || blocks * a.c.kv_heads < num_sms / 4) return false;
+    return a.c.dim == 64 ? registers_suffice<64>(device) : registers_suffice<128>(device);
 }
-
-namespace {
-template <int D>
-cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t stream)
-{
-    static std::atomic<uint64_t> allowed{0}, fits{0};
-    const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
-    if (!(fits.load(std::memory_order_relaxed) & bit)) {
-        // the warpgroups share out what a block is launched with; with less than that they would wait for ever
-        cudaFuncAttributes at;
-        const cudaError_t e = cudaFuncGetAttributes(&at, (const void *)prompt_kernel<D>);
-        if (e != cudaSuccess) return e;
-        if (at.numRegs < kRegsLaunch) return cudaErrorLaunchOutOfResources;
-        fits.fetch_or(bit, std::memory_order_relaxed);
-    }
-    const cudaError_t e = allow_shared((const void *)prompt_kernel<D>, Shape<D>::kBytes, device, allowed);
-    if (e != cudaSuccess) return e;
-    return launch_early(prompt_kernel<D>, dim3(blocks), kThreads, Shape<D>::kBytes, stream, a);
-}
-}  // namespace
 
 cudaError_t launch_prompt_attention(const AttnArgs &a, int device, cudaStream_t stream)
 {
