@@ -454,7 +454,7 @@ typedef enum {
  * root: the one group that adds bias and residual; -1 = every group.  (Of P partial products that an AllReduce
  * will add, one rank carries the bias and the residual.)
  * group strides of 0 share an operand; rows of `out` that have an element in common are an error.  m, n
- * or k of 0 is allowed (k = 0: the product is 0).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
+ * or k of 0 is allowed (k = 0: the product is 0), of more than 2^31 - 512 not (SYMAR_ERR_UNSUPPORTED).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
  * are read by the copy engine, others by the block's threads.
  * status: optional device word (may be NULL), cleared on the stream before the launch and set to SYMAR_ERR_TIMEOUT if a
  * wait inside the kernel (for its own copies and products, four seconds at most) gave up; `out` is then incomplete.   */

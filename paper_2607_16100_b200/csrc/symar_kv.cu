@@ -473,7 +473,7 @@ int kv_check(const symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv
     if (!symar_kv_page_bytes(cache->kv_heads, cache->head_dim, cache->page_size)) return SYMAR_ERR_UNSUPPORTED;
     if (!cache->pages || (uintptr_t)cache->pages % 16 || cache->num_pages < 1) return SYMAR_ERR_INVAL;
     if (batch->seqs < 0 || batch->tokens < 0 || batch->table_ld < 0 || batch->table_ld >= 1ll << 48) return SYMAR_ERR_INVAL;
-    if (batch->seqs > SYMAR_KV_MAX_SEQS) return SYMAR_ERR_UNSUPPORTED;
+    if (batch->seqs > SYMAR_KV_MAX_SEQS || batch->tokens > 0x7fffff00) return SYMAR_ERR_UNSUPPORTED;      // (a block's last token stays below 2^31)
     if (batch->tokens > 0) {
         if (!batch->lengths || !batch->page_table || batch->seqs == 0) return SYMAR_ERR_INVAL;
         if (((uintptr_t)batch->lengths | (uintptr_t)batch->page_table | (uintptr_t)batch->token_start) % 4) return SYMAR_ERR_INVAL;
@@ -582,7 +582,7 @@ int symar_kv_status(symar_kv_t *kv, int *code, int *seq, int *position)
 
 int symar_rope_table(void *table, int64_t rows, const symar_rope_scaling_t *s, void *cuda_stream)
 {
-    if (!s || rows < 0 || s->rot_dim < 2 || s->rot_dim % 2 || s->rot_dim > 256) return SYMAR_ERR_INVAL;
+    if (!s || rows < 0 || rows >= 1ll << 48 || s->rot_dim < 2 || s->rot_dim % 2 || s->rot_dim > 256) return SYMAR_ERR_INVAL;
     if (!(s->base > 0.0) || s->kind < SYMAR_ROPE_PLAIN || s->kind > SYMAR_ROPE_BY_PARTS) return SYMAR_ERR_INVAL;
     if (s->kind != SYMAR_ROPE_PLAIN && (!(s->factor > 0.0) || !std::isfinite(s->factor))) return SYMAR_ERR_INVAL;
     if (s->kind == SYMAR_ROPE_BASE && s->rot_dim < 4) return SYMAR_ERR_INVAL;

@@ -39,6 +39,7 @@ struct LinearArgs {
 
 constexpr int kRows = 128;                 // channels of a tile; a stage has kSlice of k: 128 bytes, one swizzled row
 constexpr int kMaxSplit = 8;
+constexpr int kMostRows = 0x7fffffff - 511;          // of m, n and k: the tile or slice that holds the last one ends below 2^31
 
 __device__ __forceinline__ void cluster_sync()
 {
@@ -633,6 +634,7 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     if (p.groups < 0 || p.m < 0 || p.n < 0 || p.k < 0 || p.act < SYMAR_ACT_NONE || p.act > SYMAR_ACT_SILU) return SYMAR_ERR_INVAL;
     if (p.out_dtype != SYMAR_F32 && p.out_dtype != SYMAR_BF16) return SYMAR_ERR_INVAL;
     if (p.root < -1 || (p.root >= p.groups && p.groups > 0)) return SYMAR_ERR_INVAL;
+    if (p.m > kMostRows || p.n > kMostRows || p.k > kMostRows) return SYMAR_ERR_UNSUPPORTED;
     if (p.groups == 0 || p.m == 0 || p.n == 0) return SYMAR_OK;
     const uintptr_t width = p.out_dtype == SYMAR_F32 ? 4 : 2;
     if (!p.out || (p.k > 0 && (!p.x || !p.w)) || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;

@@ -74,3 +74,15 @@ def test_rope_table_refuses_what_is_not_finite(lib, bad):        # noqa: F811
     f.update(bad)
     assert lib.symar_rope_table(SOME, 16, ctypes.byref(symar.RopeScaling(**f)), None) == symar.ERR_INVAL
     assert lib.symar_rope_table(None, 0, ctypes.byref(symar.RopeScaling(**f)), None) == symar.ERR_INVAL
+
+
+def test_sizes_whose_last_tile_would_pass_2_31(lib):             # noqa: F811
+    big = 2 ** 31 - 1
+    for bad in (dict(m=big), dict(n=big, out_ld=big), dict(k=big, x_ld=big, w_ld=big), dict(k=2 ** 31 - 511, x_ld=big, w_ld=big),
+                dict(m=big, n=0), dict(k=big, m=0)):
+        assert lib.symar_linear(linear_args(**bad), None) == symar.ERR_UNSUPPORTED, bad
+    for which in ("append", "read", "attention"):
+        assert call(lib, which, batch=dict(tokens=big, token_start=SOME)) == symar.ERR_UNSUPPORTED
+    f = dict(base=1e4, factor=2.0, original=64.0, low=1.0, high=4.0, magnitude=1.0, kind=0, rot_dim=64)
+    for rows in (1 << 48, (1 << 63) - 1):
+        assert lib.symar_rope_table(SOME, rows, ctypes.byref(symar.RopeScaling(**f)), None) == symar.ERR_INVAL
