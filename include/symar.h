@@ -456,7 +456,7 @@ typedef enum {
  * group strides of 0 share an operand; rows of `out` that have an element in common are an error.  m, n
  * or k of 0 is allowed (k = 0: the product is 0), of more than 2^31 - 512 not (SYMAR_ERR_UNSUPPORTED).  Operands of any alignment; rows on 16-byte boundaries (base, row and group stride)
  * are read by the copy engine, others by the block's threads.
- * status: optional device word (may be NULL), cleared on the stream before the launch and set to SYMAR_ERR_TIMEOUT if a
+ * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK and set to SYMAR_ERR_TIMEOUT if a
  * wait inside the kernel (for its own copies and products, four seconds at most) gave up; `out` is then incomplete.   */
 typedef struct {
     const void *x;        int64_t x_ld, x_group;

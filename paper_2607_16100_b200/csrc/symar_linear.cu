@@ -635,21 +635,23 @@ extern "C" int symar_linear(const symar_linear_t *args, void *cuda_stream)
     if (p.out_dtype != SYMAR_F32 && p.out_dtype != SYMAR_BF16) return SYMAR_ERR_INVAL;
     if (p.root < -1 || (p.root >= p.groups && p.groups > 0)) return SYMAR_ERR_INVAL;
     if (p.m > kMostRows || p.n > kMostRows || p.k > kMostRows) return SYMAR_ERR_UNSUPPORTED;
-    if (p.groups == 0 || p.m == 0 || p.n == 0) return SYMAR_OK;
+    if ((uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    auto clear = [&] {
+        const cudaError_t e = p.status ? cudaMemsetAsync(p.status, 0, sizeof(unsigned), s) : cudaSuccess;
+        return e == cudaSuccess ? (int)SYMAR_OK : cuda_fail(e, "cudaMemsetAsync");
+    };
+    if (p.groups == 0 || p.m == 0 || p.n == 0) return clear();
     const uintptr_t width = p.out_dtype == SYMAR_F32 ? 4 : 2;
-    if (!p.out || (p.k > 0 && (!p.x || !p.w)) || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
+    if (!p.out || (p.k > 0 && (!p.x || !p.w))) return SYMAR_ERR_INVAL;
     if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || ((uintptr_t)p.out | (uintptr_t)p.residual) % width) return SYMAR_ERR_INVAL;
     if (p.x_ld < 0 || p.x_group < 0 || p.w_ld < 0 || p.w_group < 0 || p.bias_group < 0 || p.residual_ld < 0 || p.residual_group < 0 ||
         p.out_ld < 0 || p.out_group < 0 || rows_meet(p.m, p.out_ld, p.groups, p.out_group, p.n))
         return SYMAR_ERR_INVAL;
     Device d;
-    const int rc = device_info(&d);
+    int rc = device_info(&d);
+    if (rc == SYMAR_OK) rc = clear();
     if (rc != SYMAR_OK) return rc;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (p.status) {
-        cudaError_t e = cudaMemsetAsync(p.status, 0, sizeof(unsigned), s);
-        if (e != cudaSuccess) return cuda_fail(e, "cudaMemsetAsync");
-    }
     LinearArgs a{};
     a.x = (const __nv_bfloat16 *)p.x;  a.x_ld = p.x_ld;  a.x_group = p.groups > 1 ? p.x_group : 0;
     a.w = (const __nv_bfloat16 *)p.w;  a.w_ld = p.w_ld;  a.w_group = p.groups > 1 ? p.w_group : 0;

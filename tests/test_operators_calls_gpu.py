@@ -95,6 +95,10 @@ def test_a_product_reports_to_the_status_word_it_is_given():
     words = torch.full((3,), 77, dtype=torch.int32, device="cuda")
     assert torch.equal(symar.linear(x, w, status=words[1]), want)
     assert words.tolist() == [77, symar.OK, 77]
+    for a, b in ((x[:0], w), (x, w[:0]), (x[:, :0], w[:, :0])):          # nothing to do is done: a word of an earlier call does not stay
+        words.fill_(77)
+        symar.linear(a, b, status=words[1])
+        assert words.tolist() == [77, symar.OK, 77]
     for bad in (words, words[:0], words[:1].long(), words[:1].cpu(), words[:1].float()):
         with pytest.raises(symar.SymarError):
             symar.linear(x, w, status=bad)
