@@ -710,7 +710,7 @@ class KVContext:
         dtype, index, dim, ks, vs = k.dtype, batch.index, cache.head_dim, k.stride(), v.stride()
         code = _dtype_code(dtype, where)
         self._one_device(where, cache, batch)
-        tokens = k.shape[0]
+        tokens = k.shape[0] if len(ks) else 0
         shape = (tokens, cache.kv_heads, dim)
         if k.shape != shape or ks[2] != 1 or k.get_device() != index:
             self._refuse(where, "k", k, shape, dtype)
@@ -720,7 +720,7 @@ class KVContext:
         qs = os = (0, 0)
         if q is not None:
             qs, shape = q.stride(), q.shape
-            q_heads = shape[1]
+            q_heads = shape[1] if len(shape) > 1 else 0
             if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or q.dtype is not dtype or q.get_device() != index:
                 self._refuse(where, "q", q, (tokens, q_heads, dim), dtype)
             if q_out is None:

@@ -137,3 +137,16 @@ def test_context_cache_and_batch_are_of_one_device(lib, of_context, of_cache, of
             call()
     assert lib.calls == []
     c._h = None
+
+
+def test_tensors_of_other_dimensions_are_refused(lib):
+    cache, batch, k, q = setting()
+    c = context(lib)
+    for call in (lambda t: c.append(cache, batch, t, k), lambda t: c.append(cache, batch, k, t), lambda t: c.append(cache, batch, k, k, q=t),
+                 lambda t: c.append(cache, batch, k, k, q=q, q_out=t), lambda t: c.attention(cache, batch, t),
+                 lambda t: c.attention(cache, batch, q, out=t)):
+        for t in (q[0, 0, 0], q[0, 0], q[0], q[None]):
+            with pytest.raises(symar.SymarError):
+                call(t)
+    assert lib.calls == []
+    c._h = None
