@@ -569,8 +569,12 @@ int symar_kv_read(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_
 /* Attention of the batch's new tokens (already stored) over the cache:
  *   out[t][h] = sum_j softmax_j(scale q[t][h] . K[j][h / share]) V[j][h / share],  share = q_heads / kv_heads,
  * over the tokens j up to t's own position and, where window > 0, more than position - window.  A row that sees no token
- * is zeros.  q, out [tokens][q_heads][D] bf16; scale 0 counts as 1 / sqrt(D).  Scores, softmax and sums are binary32; the
- * probabilities, times the scale of their V group, are rounded to bf16 for the tensor cores.               */
+ * is zeros; what a row does not see does not reach it, whatever is stored there.  q, out [tokens][q_heads][D] bf16; scale 0 counts
+ * as 1 / sqrt(D).  Scores, softmax and sums are binary32.  What is rounded to fewer bits for the tensor cores is the probability
+ * times the scale of its V group: to sixteen bits where sequences have few rows (new tokens times heads of a share), to eight, one bf16,
+ * where they have many.  (Scales are used with the zero point's bits in them, less than 2^-19 of the scale.)
+ * Sizes: values below 2^100; where rows are few, entries of q below 2^62 and keys below 2^60 (with scales up to 1): beyond
+ * them sums or products on the way may pass binary32 and the row be infinite or NaN.             */
 typedef struct {
     const void *q;   int64_t q_ld, q_head;
     void       *out; int64_t out_ld, out_head;
