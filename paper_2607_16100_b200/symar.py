@@ -500,7 +500,7 @@ def _call(fn, where, index: int, stream, *args) -> None:
 
 
 def _new(like, shape, dtype, index: int, stream):
-    """An uninitialised result beside ``like``, of the pool of the stream that the call runs on: nothing that is still queued on
+    """An uninitialised result beside ``like`` where a stream is named, of that stream's pool: nothing that is still queued on
     torch's current stream uses its memory."""
     if stream is None or stream == _raw_stream(index):
         return like.new_empty(shape, dtype=dtype)
@@ -535,7 +535,7 @@ def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root:
     else:
         groups, shape = 1, (m, n)
     if out is None:
-        out = _new(x, shape, out_dtype or bf16, index, stream)
+        out = x.new_empty(shape, dtype=out_dtype or bf16) if stream is None else _new(x, shape, out_dtype or bf16, index, stream)
         os = out.stride()
     else:
         os = out.stride()
@@ -589,14 +589,14 @@ class PagedKV:
 
     def __init__(self, pages, head_dim: int, page_size: int):
         torch = _T or _torch()
-        shape = pages.shape
+        shape, index = pages.shape, pages.get_device()
         each = page_size * head_dim + 8 * page_size * (head_dim // KV_GROUP)
         if head_dim not in (64, 128, 256) or page_size not in (16, 32, 64, 128, 256):
             raise SymarError(ERR_UNSUPPORTED, f"PagedKV: head_dim {head_dim}, page_size {page_size}")
         if pages.dtype is not torch.uint8 or len(shape) != 3 or shape[2] != each or not pages.is_contiguous() or \
-                not pages.is_cuda:
+                index < 0:
             _bad("PagedKV", f"pages are a contiguous CUDA uint8 tensor [pages, kv_heads, {each}]")
-        self.pages, self.head_dim, self.page_size, self.kv_heads, self.index = pages, head_dim, page_size, shape[1], pages.get_device()
+        self.pages, self.head_dim, self.page_size, self.kv_heads, self.index = pages, head_dim, page_size, shape[1], index
         self.args = KVCacheArgs(pages.data_ptr(), shape[0], shape[1], head_dim, page_size)
         self.ref = byref(self.args)
 
@@ -634,9 +634,12 @@ class KVBatch:
         """What a call with that many rows hands to the library.  Nothing that is handed out changes any more: calls of several threads
         may share a batch."""
         last = self._last
-        if last[0] != tokens:
-            last = self._last = (tokens, byref(KVBatchArgs(*self._fields, tokens)))
-        return last[1]
+        if last[0] == tokens:
+            return last[1]
+        lengths, start, table, columns, seqs = self._fields
+        ref = byref(KVBatchArgs(lengths, start, table, columns, seqs, tokens))
+        self._last = (tokens, ref)
+        return ref
 
 
 class KVContext:
@@ -694,9 +697,8 @@ class KVContext:
             _ck(self._lib.symar_kv_status(self._h, byref(code), byref(seq), byref(position)), "symar_kv_status")
         return code.value, seq.value, position.value
 
-    def _one_device(self, where, cache, batch):
-        if cache.index != batch.index or self.index != batch.index:
-            _bad(where, f"the context is of device {self.index}, the cache of {cache.index}, the batch of {batch.index}")
+    def _devices(self, where, cache, batch):
+        _bad(where, f"the context is of device {self.index}, the cache of {cache.index}, the batch of {batch.index}")
 
     @staticmethod
     def _refuse(where, name, t, shape, dtype):
@@ -709,7 +711,8 @@ class KVContext:
         where = "symar_kv_append"
         dtype, index, dim, ks, vs = k.dtype, batch.index, cache.head_dim, k.stride(), v.stride()
         code = _dtype_code(dtype, where)
-        self._one_device(where, cache, batch)
+        if cache.index != index or self.index != index:
+            self._devices(where, cache, batch)
         tokens = k.shape[0] if len(ks) else 0
         shape = (tokens, cache.kv_heads, dim)
         if k.shape != shape or ks[2] != 1 or k.get_device() != index:
@@ -724,7 +727,7 @@ class KVContext:
             if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or qs[2] != 1 or q.dtype is not dtype or q.get_device() != index:
                 self._refuse(where, "q", q, (tokens, q_heads, dim), dtype)
             if q_out is None:
-                q_out = _new(q, shape, dtype, index, stream)
+                q_out = q.new_empty(shape) if stream is None else _new(q, shape, dtype, index, stream)
                 os = (q_heads * dim, dim)
             else:
                 os = q_out.stride()
@@ -744,10 +747,14 @@ class KVContext:
 
     def read(self, cache: PagedKV, batch: KVBatch, tokens: int, *, dtype=None, stream=None):
         """(k, v) of the batch's new tokens as the cache holds them (``symar_kv_read``)."""
-        self._one_device("symar_kv_read", cache, batch)
+        if cache.index != batch.index or self.index != batch.index:
+            self._devices("symar_kv_read", cache, batch)
         heads, dim = cache.kv_heads, cache.head_dim
         dtype, shape = dtype or (_T or _torch()).bfloat16, (tokens, heads, dim)
-        k, v = (_new(cache.pages, shape, dtype, batch.index, stream) for _ in range(2))
+        if stream is None:
+            k, v = cache.pages.new_empty(shape, dtype=dtype), cache.pages.new_empty(shape, dtype=dtype)
+        else:
+            k, v = (_new(cache.pages, shape, dtype, batch.index, stream) for _ in range(2))
         args = KVReadArgs(k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim, dim, _dtype_code(dtype, "symar_kv_read"))
         _call(self._lib.symar_kv_read, "symar_kv_read", batch.index, stream, self._h, cache.ref, batch.of(tokens), byref(args))
         return k, v
@@ -756,12 +763,13 @@ class KVContext:
         """Attention of the batch's new tokens over the cache (``symar_kv_attention``)."""
         where = "symar_kv_attention"
         shape, dtype, index = q.shape, q.dtype, batch.index
-        self._one_device(where, cache, batch)
+        if cache.index != index or self.index != index:
+            self._devices(where, cache, batch)
         code, qs = _dtype_code(dtype, where), q.stride()
         if len(shape) != 3 or shape[2] != cache.head_dim or qs[2] != 1 or q.get_device() != index:
             _bad(where, f"q is [tokens, q_heads, {cache.head_dim}] on the batch's device with contiguous channels, not {tuple(shape)}")
         if out is None:
-            out = _new(q, shape, dtype, index, stream)
+            out = q.new_empty(shape) if stream is None else _new(q, shape, dtype, index, stream)
         os = out.stride()
         if out.shape != shape or os[2] != 1 or out.dtype is not dtype or out.get_device() != index:
             self._refuse(where, "out", out, shape, dtype)
