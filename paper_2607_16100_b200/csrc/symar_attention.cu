@@ -6,7 +6,7 @@
 namespace symar {
 namespace {
 
-constexpr int kStages   = 3;           // copies in flight per warp: two chunks ahead of the one in use (three: 51.7 us against 49.3 for one long sequence)
+constexpr int kStages   = 3;           // copies in flight per warp: two chunks ahead of the one in use (three ahead: 51.7 us against 49.3 for one long sequence)
 constexpr int kMinChunks = 1;          // a warp's share of the work is at least this many chunks of 16 tokens
 constexpr int kItemCost  = 3;          // what an item costs a warp besides its chunks, in chunks
 
@@ -50,16 +50,17 @@ __device__ __forceinline__ int64_t places_of(const AttnArgs &a, const Seq &s)
 // piece of work.  The scale of a token's group multiplies the group's partial score (K) and the probability (V), which
 // goes into the product as two bf16 numbers, its upper eight bits and what they leave: sixteen bits of it count.  (With the first alone, rounded, the
 // result's error is that of a second rounding of the output, 0.0024 instead of 0.0017 of its size, up to 0.0025 where it is small;
-// the second product costs 8%: 48.3 -> 52.2 us for the batch below.)
+// the second product costs 8%: 48.3 -> 52.2 us for the batch below when it came.)
 // The maximum in use may lie up to 2^8 below the true one: rescaling the output costs more than it is worth for less.
 // Work is split over the cache as evenly as chunks allow, whatever the lengths: all chunks of all items lie in one order, every warp takes an
 // equal stretch of it, pieces of an item meet in the block and, where it crosses blocks, at the last block to come (in order, so that
 // results do not depend on which that is).
-// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 52.2 us, 3.0 TB/s of the
+// Bound: instructions, not bytes.  64 sequences of about 4096 tokens, 64 heads, 8 key/value heads of 128: 155 MB in 52.9 us, 2.9 TB/s of the
 // 6.5 measured for a copy (14 us of it are start, joins and end; 256 such sequences ran at 4.7 TB/s before the second product); one
-// sequence of 131072: 151 MB in 49.3 us.  Issue slots are 56% used, the pipe of integer and bit
-// operations (which turns codes into operands) 48%, tensor cores 21%, DRAM half its rate.  One token after 511 with one key/value head: 9.2 us, a chain of
-// lengths, page table, page and join, each a trip to memory.  D = 64: 35.5 us, D = 256 (lengths of 2048): 59.7 us.
+// sequence of 131072: 151 MB in 49.4 us.  Issue slots are 56% used, the pipe of integer and bit
+// operations (which turns codes into operands) 48%, tensor cores 21%, DRAM half its rate.  One token after 511 with one key/value head: 9.4 us, a chain of
+// lengths, page table, page and join, each a trip to memory.  D = 64: 35.6 us, D = 256 (lengths of 2048): 60.2 us.
+// Spills (bytes stored, loaded): D = 128 with eight rows 24, 76, its 16 warps having 128 registers each; D = 256 with sixteen 412, 364; others none.
 template <int D, int NB>
 struct Shape {
     static constexpr int R = 8 * NB, NG = D / 64, kRow = D / 2;

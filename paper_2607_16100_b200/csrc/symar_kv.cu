@@ -298,9 +298,10 @@ __device__ __forceinline__ void queries(const AppendArgs &a, const Place *at, in
     }
 }
 
-// Bound: bytes.  16384 tokens of 64 query and 2 x 8 key/value heads of 128 in bf16: 720 MB in 147 us, 4.9 TB/s (0.74 of the measured copy
-// rate); of that 60 us for keys and values alone.  64 tokens 3.5 us, one token 2.7 us: the trip
-// from the lengths to the page table to the page.  Ragged prompts of float32 (5 x up to 1501): 15.6 us.
+// Bound: bytes.  16384 tokens of 64 query and 2 x 8 key/value heads of 128 in bf16: 631 MB in 145 us, 4.4 TB/s (0.67 of the measured copy
+// rate); keys and values alone take 60 us.  64 tokens 3.4 us, one token 2.6 us: the trip
+// from the lengths to the page table to the page.  Ragged prompts of float32 (5 x up to 1501): 15.7 us.  Paired queries of bf16 spill 32 bytes at 64
+// registers a thread, of float32 4.
 // Blocks with the first kv_blocks indexes in y store keys and values, the others turn queries.  (Where the queries' pairs do not come in
 // eights, kPaired is false and every block does both, a head of a token like another.)
 // (four blocks per multiprocessor: measured against three and five, with one, two or four heads' loads ahead)
@@ -378,7 +379,8 @@ struct ReadArgs {
     uint32_t by_heads;
 };
 
-// Bound: bytes; 16384 tokens 24.7 us (86 MB, 3.5 TB/s), one token 2.0 us.
+// Bytes: 16384 tokens 24.5 us for 86 MB, 3.5 TB/s (0.54 of the measured copy rate); bound by the loads in flight, of which a thread has four
+// bytes of codes and a word at a time.  One token 1.8 us.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
 {
@@ -420,6 +422,7 @@ struct TableArgs {
     double  log2_base, inv_factor, original, low, high, magnitude;
 };
 
+// Bound: binary64 arithmetic (exp2, sincos).  131072 positions of 128 channels 65 us, by parts 82 (67 MB, 1.0 TB/s); 4096 positions 3.8 and 4.3 us.
 __global__ void __launch_bounds__(kThreads) table_kernel(const TableArgs a)
 {
     const int64_t n = a.rows * a.half;

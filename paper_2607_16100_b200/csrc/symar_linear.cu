@@ -13,9 +13,10 @@
 // 5.3 TB/s (0.81 of the measured copy rate; the ring of ten stages holds 200 KB a multiprocessor in flight, the rest is
 // the start and the cluster's sum); 1 x 1024 x 1024 4.9 us, launch and latency.  Many: the tensor cores; 4096 x 8192 x 8192 takes 395 us,
 // 1390 TFLOP/s (0.85 of the measured 1640; a library product 354), with bias, tanh-GELU and residual 450 us: the
-// epilogue's 33 M values are 55 us of work for eight warps and only partly hidden.  float32 results 680-715 us: their sums leave
-// the tensor cores every 128 products.  Rows on no 16-byte boundary: 2 x 333 x 1003 x 2049 takes 36 us where k = 2048 takes 13.9; the
-// eight loading warps issue most of a slice's 7600 instructions, to shift and join its 2048 pieces.
+// epilogue's 33 M values are 55 us of work for eight warps and only partly hidden.  float32 results 610-680 us: their sums leave
+// the tensor cores every 128 products (see kChunk).  Rows on no 16-byte boundary: 2 x 333 x 1003 x 2049 takes 35.4 us where k = 2048 takes 13.9; the
+// eight loading warps issue most of a slice's 7600 instructions, to shift and join its 2048 pieces (these kernels spill 24 to 120 bytes at 96 registers; the
+// others nothing).
 #include <type_traits>
 
 #include "symar_ops.h"
@@ -259,7 +260,10 @@ struct Shape {
     static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
     static constexpr int kCols  = 2 * NT < 32 ? 32 : 2 * NT;      // two accumulators
 };
-constexpr int kChunk = 2;          // slices that a float32 result sums in the tensor cores at a time
+// Slices that a float32 result sums in the tensor cores at a time, whose additions truncate.  Error of the result (2-norm, of its own) at k = 1024, 8192,
+// 32768, and time of 4096 x 8192 x 8192: two slices 1.3, 1.5, 1.9 x 10^-7, 610 us; four 2.3, 2.4, 2.6, 538; eight 2.3, 4.8, 4.8, 504; all of k 2.3, 21, 91, 480.
+// A plain float32 product: 2.5, 9.5, 23.  (Partial sums of ranks are added up further; two is the nearest to one rounding, 0.3.)
+constexpr int kChunk = 2;
 
 // kWide: float32 results (and the sums of 128 products added up in registers)
 template <int NT, bool kWide, bool kTma>

@@ -16,8 +16,10 @@
 // whose likeliest token has a value of 0 loses what the others give it.)
 // Bound: a tile of 64 keys takes 3700 cycles, of which 2400 issue instructions (9500 on four schedulers), 2050 move softmax and codes
 // through shared memory, 1500 feed the products from there, and 1024 take exponentials; taking any one of them out gains 3% or less.
-// Two pieces of 1024 tokens over 4099 with a window of 4096, 64 heads, 8 key/value heads of 128: 450 us, 610 TFLOP/s; a prompt of 4096 tokens:
-// 440 us, 625 TFLOP/s (of 1640 measured for a plain product).
+// Two pieces of 1024 tokens over 4099 with a window of 4096, 64 heads, 8 key/value heads of 128: 459 us, 600 TFLOP/s; a prompt of 4096 tokens:
+// 445 us, 617 TFLOP/s (of 1640 measured for a plain product); the same with heads of 64 channels 338 us, 407 TFLOP/s: the softmax, the scales and the
+// waits of a tile are what they are at 128, its products half.  (These times follow the compiler's order of instructions: edits outside
+// the loops moved them by 2%, at D = 64 once by 10%.)  D = 256 has no form here: its output alone, 256 columns for each of two groups, is all of tensor memory.
 #include <cfloat>
 
 #include "symar_attention.cuh"
@@ -634,10 +636,11 @@ cudaError_t launch(const AttnArgs &a, unsigned blocks, int device, cudaStream_t 
 bool prompt_attention_takes(const AttnArgs &a, int num_sms, int device)
 {
     if (a.c.dim > 128 || items_at_most(a) > 0x3fffffff) return false;
-    // Blocks that are half full at least, and for a quarter of the multiprocessors.  (64 heads, 8 key/value heads unless said; this kernel
-    // against the one that shares a sequence's tokens between blocks, us: 512 new tokens over 8192, 128 blocks: 225, 786; 256: 217, 398; 128,
-    // 32 blocks: 214, 206; 64: 211, 111.  512 over 32768 with 8 heads of one, 16 blocks: 799, 401.  8 x 16 over 2048, half-full blocks: 62, 67;
-    // 64 x 8 over 1024, a quarter full: 139, 122; 32 x 32 with 8 heads of 8, an eighth: 69, 44.)
+    // Blocks that are half full at least, and for a quarter of the multiprocessors.  (64 heads, 8 key/value heads of 128 unless said; this kernel
+    // against the one that shares a sequence's tokens between blocks, us: 512 new tokens over 8192, 128 blocks: 230, 867; 256: 217, 438; 128,
+    // 32 blocks: 214, 226; 64: 214, 121.  512 over 32768 with 8 heads of one, 16 blocks: 817, 441.  8 x 16 over 2048, half-full blocks: 63, 73;
+    // 64 x 8 over 1024, a quarter full: 140, 134; 32 x 32 over 1024 with 8 heads of 8, an eighth: 70, 48.  Heads of 64: 512 over 8192: 185, 553; 128: 174, 149.)
+    // Lengths are on the device, so the rule knows averages alone: a batch of long pieces and single tokens goes to one kernel as a whole.
     const int64_t rows = (int64_t)a.b.tokens * a.share;                // of one key/value head
     const int64_t blocks = rows / kBlockRows > a.b.seqs ? rows / kBlockRows : a.b.seqs;
     if (rows < (int64_t)kRows * a.b.seqs || blocks * a.c.kv_heads < num_sms / 4) return false;
