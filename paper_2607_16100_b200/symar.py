@@ -577,6 +577,8 @@ def rope_table(rows: int, rot_dim: int, *, base: float = 10000.0, kind: str = "p
     if kind not in ROPE_KINDS or rows < 0:
         _bad("symar_rope_table", f"rows {rows}, kind {kind!r}")
     at = torch.device(device)
+    if at.type != "cuda":
+        _bad("symar_rope_table", f"a table on {at}")
     index = _device() if at.index is None else at.index
     table = _new(torch.empty(0, dtype=torch.float32, device=at), (rows, rot_dim // 2, 2), torch.float32, index, stream)
     how = RopeScaling(base, factor, original, low, high, magnitude, ROPE_KINDS[kind], rot_dim)

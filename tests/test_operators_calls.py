@@ -101,8 +101,7 @@ def test_results_come_from_the_memory_of_the_stream_that_is_named(lib, monkeypat
     for stream, want in ((None, []), (999, []), (5, [(5, -1)]), (0, [(0, -1)])):          # 999: the current one
         for call, results in ((lambda: c.append(cache, batch, k, k, q=q, stream=stream), 1),
                               (lambda: c.read(cache, batch, 3, stream=stream), 2),
-                              (lambda: c.attention(cache, batch, q, stream=stream), 1),
-                              (lambda: symar.rope_table(4, 64, device="cpu", stream=stream), 1)):
+                              (lambda: c.attention(cache, batch, q, stream=stream), 1)):
             entered.clear()
             call()
             assert entered == want * results
@@ -150,3 +149,12 @@ def test_tensors_of_other_dimensions_are_refused(lib):
                 call(t)
     assert lib.calls == []
     c._h = None
+
+
+def test_a_table_of_rotations_is_on_a_gpu(lib):
+    """(Its address goes to a kernel.)"""
+    for device in ("cpu", torch.device("cpu"), "meta"):
+        for stream in (None, 5):
+            with pytest.raises(symar.SymarError, match="table"):
+                symar.rope_table(4, 64, device=device, stream=stream)
+    assert lib.calls == []
