@@ -584,6 +584,43 @@ typedef struct {
 int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const symar_kv_batch_t *batch,
                        const symar_kv_attention_t *args, void *cuda_stream);
 
+/* ---- norms around the AllReduces, and a layer's mixture of experts ----------------
+ *
+ * The conventions are those of the operators above.                              */
+
+/* What follows a block's AllReduce, for every row of groups x m:
+ *     a = after(x),   r = residual_scale * residual + scale * act(gate) * a,   out = before(r)
+ * norms over a row's n channels:  SYMAR_NORM_RMS    v / sqrt(mean(v^2) + eps) * w + b
+ *                                 SYMAR_NORM_LAYER  (v - mean) / sqrt(mean((v - mean)^2) + eps) * w + b
+ *                                 SYMAR_NORM_NONE   v (`after`); no out (`before`)
+ * weight, bias [n] of the norm's own dtype, NULL: 1, 0; plus_one: the factor is 1 + w.
+ * x, gate, out of `dtype`; residual, residual_out of `stream_dtype`.  residual NULL: 0; gate NULL: act(gate) = 1;
+ * residual_out NULL: r is not stored; out is NULL where, and only where, `before` is SYMAR_NORM_NONE.  gate_step 1: a gate for
+ * every channel, 0: one number a row (strides of 0 share it among rows).  Everything is binary32, rounded once to what is stored: `before`
+ * sees r as it was before rounding.  Each of residual_out and out may be x or residual with the same layout and dtype; weights and gate
+ * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN.        */
+enum { SYMAR_NORM_MAX = 32768 };
+typedef enum { SYMAR_NORM_NONE = 0, SYMAR_NORM_RMS = 1, SYMAR_NORM_LAYER = 2 } symar_norm_kind_t;
+typedef enum { SYMAR_GATE_NONE = 0, SYMAR_GATE_SIGMOID = 1, SYMAR_GATE_TANH = 2 } symar_gate_t;
+typedef struct {
+    const void *weight, *bias;
+    float       eps;
+    int32_t     kind, dtype, plus_one;
+} symar_norm_side_t;
+typedef struct {
+    const void *x;            int64_t x_ld, x_group;
+    const void *residual;     int64_t residual_ld, residual_group;
+    const void *gate;         int64_t gate_ld, gate_group;
+    void       *residual_out; int64_t residual_out_ld, residual_out_group;
+    void       *out;          int64_t out_ld, out_group;
+    symar_norm_side_t after, before;
+    float       scale, residual_scale;
+    int32_t     groups, m, n;
+    int32_t     dtype, stream_dtype;      /* symar_dtype_t */
+    int32_t     gate_step, gate_act;
+} symar_norm_t;
+int symar_norm(const symar_norm_t *args, void *cuda_stream);
+
 /* ---- speed-of-light probes (Sec. VI: L_SoL = 2 L_L2_RTT + L_remote_store) ----
  *
  * Building blocks of the latency bound, measured on the box:

@@ -95,6 +95,7 @@ SIGNATURES = [
     ("symar_kv_append", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("symar_kv_read", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("symar_kv_attention", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    ("symar_norm", c_int, [c_void_p, c_void_p]),
     ("symar_probe_pingpong_blocks", c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int)]),
 ]
 
@@ -402,6 +403,8 @@ def allreduce_static(in_ptr: int, out_ptr: int, rank_pitch_bytes: int, P: int, c
 # if torch had made it there; tensors of other streams that it reads or writes are to be ready for it, and kept until it is
 # done with them (Tensor.record_stream), as with torch's own calls.
 
+NORM_KINDS = {"rms": 1, "layer": 2}
+GATES = {"none": 0, "sigmoid": 1, "tanh": 2}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 KV_GROUP, KV_MAX_SEQS = 64, 4096
@@ -454,6 +457,23 @@ class KVAttentionArgs(ctypes.Structure):
     _fields_ = [("q", c_void_p), ("q_ld", c_int64), ("q_head", c_int64),
                 ("out", c_void_p), ("out_ld", c_int64), ("out_head", c_int64),
                 ("scale", c_float), ("q_heads", c_int32), ("window", c_int32), ("dtype", c_int32)]
+
+
+class NormSide(ctypes.Structure):
+    _fields_ = [("weight", c_void_p), ("bias", c_void_p), ("eps", c_float), ("kind", c_int32), ("dtype", c_int32), ("plus_one", c_int32)]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = [
+        ("x", c_void_p), ("x_ld", c_int64), ("x_group", c_int64),
+        ("residual", c_void_p), ("residual_ld", c_int64), ("residual_group", c_int64),
+        ("gate", c_void_p), ("gate_ld", c_int64), ("gate_group", c_int64),
+        ("residual_out", c_void_p), ("residual_out_ld", c_int64), ("residual_out_group", c_int64),
+        ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
+        ("after", NormSide), ("before", NormSide), ("scale", c_float), ("residual_scale", c_float),
+        ("groups", c_int32), ("m", c_int32), ("n", c_int32), ("dtype", c_int32), ("stream_dtype", c_int32),
+        ("gate_step", c_int32), ("gate_act", c_int32),
+    ]
 
 
 _T = None               # torch, once a call needed it
@@ -778,6 +798,94 @@ class KVContext:
         args = KVAttentionArgs(q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], scale, shape[1], window, code)
         _call(self._lib.symar_kv_attention, where, index, stream, self._h, cache.ref, batch.of(shape[0]), byref(args))
         return out
+
+
+class Norm:
+    """One norm over a row's channels: kind "rms" or "layer", weight and bias [n] (None: 1 and 0; both of one dtype, float32 or bfloat16),
+    ``plus_one``: the factor is 1 + weight."""
+
+    def __init__(self, kind: str = "rms", weight=None, bias=None, *, eps: float = 1e-6, plus_one: bool = False):
+        _T or _torch()
+        where, some = "Norm", weight if weight is not None else bias
+        if kind not in NORM_KINDS:
+            _bad(where, f"kind {kind!r}, not one of " + ", ".join(NORM_KINDS))
+        for t in (weight, bias):
+            if t is not None and (t.dim() != 1 or t.shape != some.shape or t.dtype is not some.dtype or t.get_device() != some.get_device() or
+                                  some.get_device() < 0 or not t.is_contiguous()):
+                _bad(where, "weight and bias are contiguous CUDA tensors [n] of one dtype and device")
+        code = _dtype_code(some.dtype, where) if some is not None else F32
+        self.n, self.index = (some.shape[0], some.get_device()) if some is not None else (None, None)
+        self.weight, self.bias = weight, bias
+        self.args = NormSide(weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None, eps,
+                             NORM_KINDS[kind], code, 1 if plus_one else 0)
+
+
+_NO_NORM = NormSide()
+
+
+def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str = "none", scale: float = 1.0,
+         residual_scale: float = 1.0, out=None, residual_out=None, stream=None):
+    """(y, r) with ``r = residual_scale * residual + scale * act(gate) * after(x)`` and ``y = before(r)`` (``symar_norm``).
+
+    x [m, n] or [groups, m, n] float32 or bfloat16, y like it; residual of x's shape, float32 or bfloat16, r like it.  ``after`` and ``before``:
+    a :class:`Norm`, or None (a = x; no y, None in its place).  gate: of x's dtype and broadcastable to x's shape, a number for every channel
+    or (last extent 1) for a row; ``gate_act``: "none", "sigmoid" or "tanh".  Without a residual r is not stored (None) unless there is no y or
+    ``residual_out`` is given (r is then of its dtype).  ``out`` may be x, ``residual_out`` residual."""
+    torch = _T or _torch()
+    where = "symar_norm"
+    shape, xs, index, dtype = x.shape, x.stride(), x.get_device(), x.dtype
+    nd, act = len(shape), GATES.get(gate_act)
+    code = _dtype_code(dtype, where)
+    if index < 0 or nd not in (2, 3) or act is None or (shape[-1] > 1 and xs[-1] != 1):
+        _bad(where, "x is a CUDA tensor of two or three dimensions with contiguous channels, gate_act one of " + ", ".join(GATES))
+    m, n = shape[-2], shape[-1]
+    groups = shape[0] if nd == 3 else 1
+    rp = rl = rg = gp = gl = gg = step = op = ol = og = yp = yl = yg = 0
+    stream_dtype = None
+    if residual is not None:
+        s = residual.stride()
+        stream_dtype = residual.dtype
+        if residual.shape != shape or (n > 1 and s[-1] != 1) or residual.get_device() != index:
+            _bad(where, f"residual of shape {tuple(residual.shape)}")
+        rp, rl, rg = residual.data_ptr(), s[-2], s[0] if nd == 3 else 0
+    if residual_out is None:
+        if residual is not None or before is None:
+            stream_dtype = stream_dtype or dtype
+            residual_out = x.new_empty(shape, dtype=stream_dtype) if stream is None else _new(x, shape, stream_dtype, index, stream)
+    elif residual_out.shape != shape or (n > 1 and residual_out.stride(-1) != 1) or residual_out.get_device() != index or \
+            residual_out.dtype is not (stream_dtype or residual_out.dtype):
+        _bad(where, f"residual_out of shape {tuple(residual_out.shape)}, {residual_out.dtype}")
+    if residual_out is not None:
+        s = residual_out.stride()
+        stream_dtype = residual_out.dtype
+        op, ol, og = residual_out.data_ptr(), s[-2], s[0] if nd == 3 else 0
+    if before is not None:
+        if out is None:
+            out = x.new_empty(shape) if stream is None else _new(x, shape, dtype, index, stream)
+        s = out.stride()
+        if out.shape != shape or (n > 1 and s[-1] != 1) or out.dtype is not dtype or out.get_device() != index:
+            _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+        yp, yl, yg = out.data_ptr(), s[-2], s[0] if nd == 3 else 0
+    elif out is not None:
+        _bad(where, "out without a norm before the next block")
+    if gate is not None:
+        gs = gate.shape
+        if gate.dtype is not dtype or gate.get_device() != index or len(gs) > nd or \
+                any(a != b and a != 1 for a, b in zip(gs[::-1], shape[::-1])):
+            _bad(where, f"gate of shape {tuple(gs)}, {gate.dtype}")
+        step = 1 if len(gs) and gs[-1] != 1 else 0
+        s = gate.expand(shape).stride()
+        if step and n > 1 and s[-1] != 1:
+            _bad(where, "the gate's channels are contiguous")
+        gp, gl, gg = gate.data_ptr(), s[-2], s[0] if nd == 3 else 0
+    for side in (after, before):
+        if side is not None and side.n is not None and (side.n != n or side.index != index):
+            _bad(where, f"a norm of {side.n} channels on device {side.index} for x {tuple(shape)} on device {index}")
+    args = NormArgs(x.data_ptr(), xs[-2], xs[0] if nd == 3 else 0, rp, rl, rg, gp, gl, gg, op, ol, og, yp, yl, yg,
+                    after.args if after is not None else _NO_NORM, before.args if before is not None else _NO_NORM, scale, residual_scale,
+                    groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act)
+    _call((_lib or load()).symar_norm, where, index, stream, byref(args))
+    return out if before is not None else None, residual_out
 
 
 # -- probes --
