@@ -621,6 +621,50 @@ typedef struct {
 } symar_norm_t;
 int symar_norm(const symar_norm_t *args, void *cuda_stream);
 
+/* The experts of every token.  logits [tokens][experts] (rows `ld` apart) of `dtype`;
+ *     score = softmax over the token's logits, or sigmoid of each.
+ * A token's top_k experts are those with the largest logit, or with the largest score + bias where there is a bias [experts]
+ * (binary32), decided as exact arithmetic decides (in binary64 where binary32 leaves a doubt); of equal ones the lowest
+ * index first.  An expert whose logit is -inf or NaN, or whose score + bias is, is not to be had (and counts as 0 in a softmax); a
+ * token with fewer than top_k others has -1 and a weight of 0 in place of the rest.  weights = scores of the chosen,
+ * divided by their sum where renormalise is 1 (zeros where it is 0), times scale: binary32.
+ *   choice, weights [tokens][top_k]   in falling order
+ *   expert_start [experts + 1]        expert e's rows are expert_start[e] .. expert_start[e+1]-1, by token
+ *   row_token [tokens * top_k]        every row's token, -1 from expert_start[experts] on
+ *   token_row [tokens][top_k]         every choice's row, -1 where there is none
+ * Dense and 4-byte aligned.  workspace: symar_route_workspace(tokens, experts) bytes (0: none) that no other call uses meanwhile; what it holds
+ * before and after is of no account.  A logit of +inf makes a softmax NaN.
+ * Limits: 1024 experts, top_k 32 (SYMAR_ERR_UNSUPPORTED).                          */
+enum { SYMAR_ROUTE_MAX_EXPERTS = 1024, SYMAR_ROUTE_MAX_TOP = 32 };
+typedef enum { SYMAR_SCORE_SOFTMAX = 0, SYMAR_SCORE_SIGMOID = 1 } symar_score_t;
+typedef struct {
+    const void  *logits; int64_t ld;
+    const float *bias;
+    int32_t     *choice;
+    float       *weights;
+    int32_t     *expert_start, *row_token, *token_row;
+    void        *workspace; size_t workspace_bytes;
+    float        scale;
+    int32_t      tokens, experts, top_k, dtype, score, renormalise;
+} symar_route_t;
+size_t symar_route_workspace(int tokens, int experts);
+int symar_route(const symar_route_t *args, void *cuda_stream);
+
+/* out[g][t] = sum_j weights[t][j] y[g][token_row[t][j]] + residual[g][t]: the rows of a token's experts back in the tokens'
+ * order, for every rank g.  y [groups][rows][n] of dtype, out and residual (NULL: none) [groups][tokens][n] of out_dtype; weights NULL: 1.
+ * A token_row below 0 or from `rows` on is none, whatever its weight.  root: the one group that adds the residual, -1 = every
+ * group (a group stride of 0 shares it).  Sums are binary32 in the order of j, rounded once.  out may be residual with the same layout.  n up to 2^30. */
+typedef struct {
+    const void    *y;         int64_t y_ld, y_group;
+    const int32_t *token_row;
+    const float   *weights;
+    const void    *residual;  int64_t residual_ld, residual_group;
+    void          *out;       int64_t out_ld, out_group;
+    int32_t        groups, tokens, top_k, rows, n;
+    int32_t        dtype, out_dtype, root;
+} symar_combine_t;
+int symar_combine(const symar_combine_t *args, void *cuda_stream);
+
 /* ---- speed-of-light probes (Sec. VI: L_SoL = 2 L_L2_RTT + L_remote_store) ----
  *
  * Building blocks of the latency bound, measured on the box:

@@ -4,6 +4,7 @@
 // A row is read once, held in registers as binary32 through both norms and written once.  Sums go over a thread's own elements,
 // then over the row's threads by shuffles and, where they are several warps, by shared memory; a layer norm takes the mean first
 // and the squares of what is left after it, so that a large mean costs no digits.
+#include "symar_eights.cuh"
 #include "symar_ops.h"
 
 namespace symar {
@@ -24,81 +25,8 @@ struct NormArgs {
     int     x_wide, stream_wide, gate_step, gate_act;
 };
 
-// Eight elements as they were read: packed pairs (bf16 in one load) or one a word.
-struct Raw {
-    uint32_t w[8];
-};
-
-// Where a thread's eight elements of chunk c lie: side by side, or (rows on no 16-byte boundary) one in every T.
-template <int T, bool kVec> __device__ __forceinline__ int element(int c, int i, int j) { return kVec ? (c * T + i) * 8 + j : (c * 8 + j) * T + i; }
-
-template <int T, bool kVec>
-__device__ __forceinline__ Raw read8(const void *p, bool wide, int c, int i, int n)
-{
-    Raw r;
-    if (kVec) {
-        const int at = element<T, true>(c, i, 0);
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-        if (at < n) {
-            const char *q = static_cast<const char *>(p) + (int64_t)at * (wide ? 4 : 2);
-            lo = *reinterpret_cast<const uint4 *>(q);
-            if (wide) hi = *reinterpret_cast<const uint4 *>(q + 16);
-        }
-        r.w[0] = lo.x; r.w[1] = lo.y; r.w[2] = lo.z; r.w[3] = lo.w;
-        r.w[4] = hi.x; r.w[5] = hi.y; r.w[6] = hi.z; r.w[7] = hi.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int at = element<T, false>(c, i, j);
-            r.w[j] = 0;
-            if (at < n) r.w[j] = wide ? static_cast<const uint32_t *>(p)[at] : (uint32_t) static_cast<const uint16_t *>(p)[at] << 16;
-        }
-    }
-    return r;
-}
-template <bool kVec>
-__device__ __forceinline__ void values(const Raw &r, bool wide, float (&v)[8])
-{
-    if (kVec && !wide) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[2 * j]     = __uint_as_float(r.w[j] << 16);
-            v[2 * j + 1] = __uint_as_float(r.w[j] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j]);
-    }
-}
-template <int T, bool kVec>
-__device__ __forceinline__ void write8(void *p, bool wide, int c, int i, int n, const float *v)
-{
-    if (kVec) {
-        const int at = element<T, true>(c, i, 0);
-        if (at >= n) return;
-        char *q = static_cast<char *>(p) + (int64_t)at * (wide ? 4 : 2);
-        if (wide) {
-            *reinterpret_cast<float4 *>(q)      = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4 *>(q + 16) = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-                w[j] = *reinterpret_cast<uint32_t *>(&h);
-            }
-            *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int at = element<T, false>(c, i, j);
-            if (at >= n) continue;
-            if (wide) static_cast<float *>(p)[at] = v[j];
-            else static_cast<__nv_bfloat16 *>(p)[at] = __float2bfloat16_rn(v[j]);
-        }
-    }
-}
+// Where the eight elements of a thread's chunk c begin; on no 16-byte boundary they are T apart.
+template <int T, bool kVec> __device__ __forceinline__ int first(int c, int i) { return kVec ? (c * T + i) * 8 : c * 8 * T + i; }
 
 // Sum over a row's T threads, the same on every one of them; `room` is not in use by an earlier sum any more.
 template <int T>
@@ -130,7 +58,7 @@ __device__ __forceinline__ void norm_row(float (&v)[C][8], const Side &s, const 
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = element<T, kVec>(c, i, j) < n ? v[c][j] - mean : 0.0f;
+            for (int j = 0; j < 8; ++j) v[c][j] = first<T, kVec>(c, i) + (kVec ? j : j * T) < n ? v[c][j] - mean : 0.0f;
     }
     float sum = 0.0f;
 #pragma unroll
@@ -144,13 +72,13 @@ __device__ __forceinline__ void norm_row(float (&v)[C][8], const Side &s, const 
         for (int j = 0; j < 8; ++j) v[c][j] *= by;
         if (s.weight) {
             float w[8];
-            values<kVec>(C == 1 ? w0 : read8<T, kVec>(s.weight, s.wide, c, i, n), s.wide, w);
+            values<kVec>(C == 1 ? w0 : read8<kVec>(s.weight, s.wide, first<T, kVec>(c, i), T, n), s.wide, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] *= s.plus_one ? 1.0f + w[j] : w[j];
         }
         if (s.bias) {
             float b[8];
-            values<kVec>(C == 1 ? b0 : read8<T, kVec>(s.bias, s.wide, c, i, n), s.wide, b);
+            values<kVec>(C == 1 ? b0 : read8<kVec>(s.bias, s.wide, first<T, kVec>(c, i), T, n), s.wide, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] += b[j];
         }
@@ -178,16 +106,16 @@ __global__ void __launch_bounds__(T == 32 ? 32 * kSmall : T) norm_kernel(const _
 
     Raw in[C], old[C], none{}, wa = none, ba = none, wb = none, bb = none;
 #pragma unroll
-    for (int c = 0; c < C; ++c) in[c] = read8<T, kVec>(x, a.x_wide, c, i, n);
+    for (int c = 0; c < C; ++c) in[c] = read8<kVec>(x, a.x_wide, first<T, kVec>(c, i), T, n);
     if (a.residual) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) old[c] = read8<T, kVec>(res, a.stream_wide, c, i, n);
+        for (int c = 0; c < C; ++c) old[c] = read8<kVec>(res, a.stream_wide, first<T, kVec>(c, i), T, n);
     }
     if (C == 1) {                          // few rows: everything is asked for at once
-        if (a.after.weight) wa = read8<T, kVec>(a.after.weight, a.after.wide, 0, i, n);
-        if (a.after.bias) ba = read8<T, kVec>(a.after.bias, a.after.wide, 0, i, n);
-        if (a.before.weight) wb = read8<T, kVec>(a.before.weight, a.before.wide, 0, i, n);
-        if (a.before.bias) bb = read8<T, kVec>(a.before.bias, a.before.wide, 0, i, n);
+        if (a.after.weight) wa = read8<kVec>(a.after.weight, a.after.wide, first<T, kVec>(0, i), T, n);
+        if (a.after.bias) ba = read8<kVec>(a.after.bias, a.after.wide, first<T, kVec>(0, i), T, n);
+        if (a.before.weight) wb = read8<kVec>(a.before.weight, a.before.wide, first<T, kVec>(0, i), T, n);
+        if (a.before.bias) bb = read8<kVec>(a.before.bias, a.before.wide, first<T, kVec>(0, i), T, n);
     }
     float v[C][8];
 #pragma unroll
@@ -206,7 +134,7 @@ __global__ void __launch_bounds__(T == 32 ? 32 * kSmall : T) norm_kernel(const _
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 float w[8];
-                values<kVec>(read8<T, kVec>(gate, a.x_wide, c, i, n), a.x_wide, w);
+                values<kVec>(read8<kVec>(gate, a.x_wide, first<T, kVec>(c, i), T, n), a.x_wide, w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[c][j] *= a.scale * opened(w[j], a.gate_act);
             }
@@ -229,13 +157,13 @@ __global__ void __launch_bounds__(T == 32 ? 32 * kSmall : T) norm_kernel(const _
     if (a.residual_out) {
         char *to = static_cast<char *>(a.residual_out) + (g * a.residual_out_group + t * a.residual_out_ld) * (a.stream_wide ? 4 : 2);
 #pragma unroll
-        for (int c = 0; c < C; ++c) write8<T, kVec>(to, a.stream_wide, c, i, n, v[c]);
+        for (int c = 0; c < C; ++c) write8<kVec>(to, a.stream_wide, first<T, kVec>(c, i), T, n, v[c]);
     }
     if (a.out) {
         norm_row<T, C, kVec>(v, a.before, wb, bb, i, n, inv_n, room + 64);
         char *to = static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (a.x_wide ? 4 : 2);
 #pragma unroll
-        for (int c = 0; c < C; ++c) write8<T, kVec>(to, a.x_wide, c, i, n, v[c]);
+        for (int c = 0; c < C; ++c) write8<kVec>(to, a.x_wide, first<T, kVec>(c, i), T, n, v[c]);
     }
 }
 

@@ -96,6 +96,9 @@ SIGNATURES = [
     ("symar_kv_read", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("symar_kv_attention", c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("symar_norm", c_int, [c_void_p, c_void_p]),
+    ("symar_route_workspace", c_size_t, [c_int, c_int]),
+    ("symar_route", c_int, [c_void_p, c_void_p]),
+    ("symar_combine", c_int, [c_void_p, c_void_p]),
     ("symar_probe_pingpong_blocks", c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int)]),
 ]
 
@@ -404,6 +407,7 @@ def allreduce_static(in_ptr: int, out_ptr: int, rank_pitch_bytes: int, P: int, c
 # done with them (Tensor.record_stream), as with torch's own calls.
 
 NORM_KINDS = {"rms": 1, "layer": 2}
+SCORES = {"softmax": 0, "sigmoid": 1}
 GATES = {"none": 0, "sigmoid": 1, "tanh": 2}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 ROPE_KINDS = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
@@ -473,6 +477,24 @@ class NormArgs(ctypes.Structure):
         ("after", NormSide), ("before", NormSide), ("scale", c_float), ("residual_scale", c_float),
         ("groups", c_int32), ("m", c_int32), ("n", c_int32), ("dtype", c_int32), ("stream_dtype", c_int32),
         ("gate_step", c_int32), ("gate_act", c_int32),
+    ]
+
+
+class RouteArgs(ctypes.Structure):
+    _fields_ = [
+        ("logits", c_void_p), ("ld", c_int64), ("bias", c_void_p), ("choice", c_void_p), ("weights", c_void_p),
+        ("expert_start", c_void_p), ("row_token", c_void_p), ("token_row", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t),
+        ("scale", c_float), ("tokens", c_int32), ("experts", c_int32), ("top_k", c_int32), ("dtype", c_int32), ("score", c_int32),
+        ("renormalise", c_int32),
+    ]
+
+
+class CombineArgs(ctypes.Structure):
+    _fields_ = [
+        ("y", c_void_p), ("y_ld", c_int64), ("y_group", c_int64), ("token_row", c_void_p), ("weights", c_void_p),
+        ("residual", c_void_p), ("residual_ld", c_int64), ("residual_group", c_int64), ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
+        ("groups", c_int32), ("tokens", c_int32), ("top_k", c_int32), ("rows", c_int32), ("n", c_int32), ("dtype", c_int32),
+        ("out_dtype", c_int32), ("root", c_int32),
     ]
 
 
@@ -886,6 +908,93 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
                     groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act)
     _call((_lib or load()).symar_norm, where, index, stream, byref(args))
     return out if before is not None else None, residual_out
+
+
+class Routes:
+    """The experts of a call's tokens, as :func:`route` makes it: int32 CUDA tensors choice [tokens, top_k], expert_start [experts + 1],
+    row_token [tokens * top_k] and token_row [tokens, top_k], float32 weights [tokens, top_k], all contiguous."""
+
+    def __init__(self, choice, weights, expert_start, row_token, token_row):
+        torch = _T or _torch()
+        index, shape = weights.get_device(), weights.shape
+        if len(shape) != 2 or weights.dtype is not torch.float32 or index < 0 or not weights.is_contiguous():
+            _bad("Routes", "weights [tokens, top_k] are a contiguous float32 CUDA tensor")
+        for name, t, want in (("choice", choice, shape), ("token_row", token_row, shape), ("row_token", row_token, (shape[0] * shape[1],)),
+                              ("expert_start", expert_start, (expert_start.numel(),))):
+            if t.dtype is not torch.int32 or t.shape != want or t.get_device() != index or not t.is_contiguous():
+                _bad("Routes", f"{name} is a contiguous int32 tensor {list(want)} on the weights' device")
+        self._set(choice, weights, expert_start, row_token, token_row, shape, expert_start.shape[0] - 1, index)
+        if self.experts < 1:
+            _bad("Routes", "expert_start has an entry more than there are experts")
+
+    def _set(self, choice, weights, expert_start, row_token, token_row, shape, experts, index):
+        self.choice, self.weights, self.expert_start, self.row_token, self.token_row = choice, weights, expert_start, row_token, token_row
+        self.tokens, self.top_k = shape
+        self.experts, self.index, self.rows = experts, index, self.tokens * self.top_k
+
+
+def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, stream=None) -> Routes:
+    """The top_k experts of every token with their weights, and the lists that sort tokens by expert (``symar_route``).
+
+    logits [tokens, experts] float32 or bfloat16; ``score``: "softmax" or "sigmoid"; bias [experts] float32, which takes part in the choice and
+    not in the weights.  A token whose logits are all -inf (an idle slot) has no experts."""
+    torch = _T or _torch()
+    where = "symar_route"
+    shape, index, kind = logits.shape, logits.get_device(), SCORES.get(score)
+    code = _dtype_code(logits.dtype, where)
+    if len(shape) != 2 or index < 0 or kind is None or (shape[1] > 1 and logits.stride(1) != 1):
+        _bad(where, "logits are a CUDA tensor [tokens, experts] with contiguous rows, score one of " + ", ".join(SCORES))
+    tokens, experts = shape
+    if not 1 <= top_k <= experts:
+        _bad(where, f"top_k {top_k} of {experts} experts")
+    if bias is not None and (bias.shape != (experts,) or bias.dtype is not torch.float32 or bias.get_device() != index or
+                             not bias.is_contiguous()):
+        _bad(where, f"bias is a contiguous float32 tensor [{experts}], not {tuple(bias.shape)} {bias.dtype}")
+    lib = _lib or load()
+    rows, work = tokens * top_k, int(lib.symar_route_workspace(tokens, experts))
+    # lists and workspace in one piece
+    whole = _new(logits, (3 * rows + experts + 1 + work // 4,), torch.int32, index, stream)
+    weights = _new(logits, (tokens, top_k), torch.float32, index, stream)
+    at, start = whole.data_ptr(), 3 * rows
+    args = RouteArgs(logits.data_ptr(), logits.stride(0), bias.data_ptr() if bias is not None else None, at, weights.data_ptr(), at + 4 * start,
+                     at + 4 * rows, at + 8 * rows, at + 4 * (start + experts + 1) if work else None, work, scale, tokens, experts, top_k, code, kind,
+                     1 if renormalise else 0)
+    _call(lib.symar_route, where, index, stream, byref(args))
+    got = object.__new__(Routes)
+    got._set(whole[:rows].view(tokens, top_k), weights, whole[start:start + experts + 1], whole[rows:2 * rows],
+             whole[2 * rows:start].view(tokens, top_k), shape[:1] + (top_k,), experts, index)
+    return got
+
+
+def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_dtype=None, stream=None):
+    """The weighted sum of every token's rows (``symar_combine``): y [rows, n] or [ranks, rows, n] -> [tokens, n] or [ranks, tokens, n].
+
+    residual [tokens, n] or [ranks, tokens, n] of the result's dtype, added by rank ``root``, by all where that is -1."""
+    torch = _T or _torch()
+    where = "symar_combine"
+    shape, ys, index = y.shape, y.stride(), y.get_device()
+    nd = len(shape)
+    code = _dtype_code(y.dtype, where)
+    if nd not in (2, 3) or index != routes.index or shape[-2] != routes.rows or (shape[-1] > 1 and ys[-1] != 1):
+        _bad(where, f"y is [{routes.rows}, n] or [ranks, {routes.rows}, n] on the routes' device with contiguous channels, not {tuple(shape)}")
+    n, groups = shape[-1], shape[0] if nd == 3 else 1
+    want = (groups, routes.tokens, n) if nd == 3 else (routes.tokens, n)
+    if out is None:
+        out = _new(y, want, out_dtype or y.dtype, index, stream)
+    os = out.stride()
+    if out.shape != want or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and os[-1] != 1) or out.get_device() != index:
+        _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+    rp = rl = rg = 0
+    if residual is not None:
+        rs = residual.stride()
+        if residual.shape not in (want, want[-2:]) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or residual.get_device() != index:
+            _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
+        rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
+    args = CombineArgs(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes.token_row.data_ptr(), routes.weights.data_ptr(), rp, rl, rg,
+                       out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
+                       _dtype_code(out.dtype, where), root)
+    _call((_lib or load()).symar_combine, where, index, stream, byref(args))
+    return out
 
 
 # -- probes --

@@ -48,3 +48,57 @@ def test_norm_sizes(lib):
     assert norm_rc(lib, groups=1 << 16, m=1 << 15) == symar.ERR_UNSUPPORTED
     for empty in ("m", "n", "groups"):
         assert norm_rc(lib, **{empty: 0, "x": None, "residual": None}) == symar.OK
+
+
+def route_rc(lib, **change):
+    f = dict(logits=SOME, ld=64, bias=SOME, choice=SOME, weights=SOME, expert_start=SOME, row_token=SOME, token_row=SOME, workspace=SOME,
+             workspace_bytes=1 << 20, scale=1.0, tokens=400, experts=64, top_k=4, dtype=symar.F32, score=0, renormalise=1)
+    f.update(change)
+    return lib.symar_route(ctypes.byref(symar.RouteArgs(**f)), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(logits=None), dict(choice=None), dict(weights=None), dict(expert_start=None), dict(row_token=None), dict(token_row=None), dict(workspace=None),
+    dict(tokens=-1), dict(experts=0), dict(top_k=0), dict(top_k=65), dict(dtype=2), dict(score=2), dict(score=-1), dict(renormalise=2), dict(ld=-1),
+    dict(scale=math.nan), dict(scale=math.inf), dict(logits=SOME + 2), dict(logits=SOME + 1, dtype=symar.BF16), dict(bias=SOME + 2), dict(choice=SOME + 1),
+    dict(weights=SOME + 2), dict(expert_start=SOME + 3), dict(row_token=SOME + 2), dict(token_row=SOME + 2), dict(workspace=SOME + 2),
+    dict(tokens=0, expert_start=None),
+], ids=ids)
+def test_route_refuses(lib, change):
+    assert route_rc(lib, **change) == symar.ERR_INVAL
+
+
+def test_route_limits(lib):
+    assert lib.symar_route(None, None) == symar.ERR_INVAL
+    assert route_rc(lib, experts=1025) == symar.ERR_UNSUPPORTED
+    assert route_rc(lib, top_k=33) == symar.ERR_UNSUPPORTED
+    assert route_rc(lib, tokens=1 << 29) == symar.ERR_UNSUPPORTED
+    need = lib.symar_route_workspace(400, 64)
+    assert need > 0 and lib.symar_route_workspace(1, 64) == 0
+    assert route_rc(lib, workspace_bytes=need - 1) == symar.ERR_NOMEM
+    assert max(lib.symar_route_workspace(t, 1024) for t in (129, 5000, 1 << 30)) <= 148 * 4096
+
+
+def combine_rc(lib, **change):
+    f = {n + s: v for n in ("y", "residual", "out") for s, v in (("", SOME), ("_ld", 64), ("_group", 1024))}
+    f.update(token_row=SOME, weights=SOME, groups=2, tokens=8, top_k=2, rows=16, n=64, dtype=symar.BF16, out_dtype=symar.F32, root=0)
+    f.update(change)
+    return lib.symar_combine(ctypes.byref(symar.CombineArgs(**f)), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(y=None), dict(out=None), dict(token_row=None), dict(groups=-1), dict(tokens=-1), dict(top_k=-1), dict(rows=-1), dict(n=-1), dict(dtype=2),
+    dict(out_dtype=-1), dict(root=2), dict(root=-2), dict(y=SOME + 1), dict(out=SOME + 2), dict(residual=SOME + 2), dict(token_row=SOME + 2),
+    dict(weights=SOME + 2), dict(y_ld=-1), dict(y_group=-1), dict(residual_ld=-1), dict(residual_group=-1), dict(out_ld=63), dict(out_ld=0),
+    dict(out_group=0), dict(out_group=100), dict(out_group=-1),
+], ids=ids)
+def test_combine_refuses(lib, change):
+    assert combine_rc(lib, **change) == symar.ERR_INVAL
+
+
+def test_combine_sizes(lib):
+    assert lib.symar_combine(None, None) == symar.ERR_INVAL
+    assert combine_rc(lib, n=(1 << 30) + 1, out_ld=1 << 31, out_group=1 << 40) == symar.ERR_UNSUPPORTED
+    assert combine_rc(lib, n=1 << 30, tokens=1 << 20, out_ld=1 << 31, out_group=1 << 52) == symar.ERR_UNSUPPORTED
+    for empty in ("groups", "tokens", "n"):
+        assert combine_rc(lib, **{empty: 0, "y": None, "out": None, "token_row": None}) == symar.OK
