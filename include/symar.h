@@ -650,6 +650,32 @@ typedef struct {
 size_t symar_route_workspace(int tokens, int experts);
 int symar_route(const symar_route_t *args, void *cuda_stream);
 
+/* The experts' products: for every rank g and every row r of expert e (expert_start[e] <= r < expert_start[e+1])
+ *     out[g][r] = act(x w^T + bias)                              w = w[g][e] [n][k],  bias = bias[g][e] [n]
+ *     out[g][r] = act(x wg^T + bg) * (x wu^T + bu)  (gated)      w[g][e] [2n][k]: wg's n rows, then wu's; bias alike
+ * with x = x[g][row_token[r]], or x[g][r] where row_token is NULL.  x [groups][x_rows][k], w, bias (NULL: 0) bf16; sums and what follows them are
+ * binary32, rounded once to out_dtype (float32 results as in symar_linear).  Group strides of 0 share an operand.  The lists are symar_route()'s, on the
+ * device: starts are brought into 0 .. rows and into order before use; rows of nobody (behind the last expert's) are left as they were.
+ * A row_token outside x makes its row's result undefined and is reported.  Rows of x and w lie on 16-byte boundaries (base, and strides of axes longer than one:
+ * multiples of 8 elements, not 0), and a gathered x's x_group is a multiple of x_ld; SYMAR_ERR_UNSUPPORTED otherwise.  Sizes of 0 are
+ * allowed (k = 0: the product is 0); 1024 experts at most, other sizes up to 2^30.
+ * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_INVAL by a row_token
+ * outside x, or to SYMAR_ERR_TIMEOUT if a wait inside the kernel (for its own copies and products, four seconds at most) gave up;
+ * `out` is then incomplete.                                                         */
+enum { SYMAR_EXPERTS_MAX = 1024 };
+typedef struct {
+    const void    *x;    int64_t x_ld, x_group;
+    const void    *w;    int64_t w_ld, w_expert, w_group;
+    const void    *bias; int64_t bias_expert, bias_group;
+    void          *out;  int64_t out_ld, out_group;
+    const int32_t *expert_start;           /* [experts + 1] */
+    const int32_t *row_token;              /* [rows] or NULL */
+    int32_t        groups, experts, rows, x_rows, n, k;
+    int32_t        out_dtype, act, gated;
+    uint32_t      *status;
+} symar_experts_t;
+int symar_experts(const symar_experts_t *args, void *cuda_stream);
+
 /* out[g][t] = sum_j weights[t][j] y[g][token_row[t][j]] + residual[g][t]: the rows of a token's experts back in the tokens'
  * order, for every rank g.  y [groups][rows][n] of dtype, out and residual (NULL: none) [groups][tokens][n] of out_dtype; weights NULL: 1.
  * A token_row below 0 or from `rows` on is none, whatever its weight.  root: the one group that adds the residual, -1 = every

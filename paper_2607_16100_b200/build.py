@@ -13,7 +13,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libsymar.so"
 SOURCES = ["symar_kernels.cu", "symar_bulk.cu", "symar_host.cu", "symar_probe.cu", "symar_static.cu", "symar_coll.cu",
            "symar_atomic.cu", "symar_place.cu", "symar_linear.cu", "symar_kv.cu", "symar_attention.cu",
-           "symar_prompt.cu", "symar_norm.cu", "symar_route.cu", "symar_combine.cu"]
+           "symar_prompt.cu", "symar_norm.cu", "symar_route.cu", "symar_combine.cu", "symar_experts.cu"]
 
 LIB_SYS = PKG / "libsymar_sys.so"
 LIB_CHECK = PKG / "libsymar_check.so"

@@ -1,0 +1,464 @@
+// One product per expert over the rows of the tokens that chose it, for every rank (formulas in include/symar.h), on the fifth
+// generation's tensor cores.
+//
+// As in symar_linear.cu the weights are the 128 rows of every matrix instruction and the tokens its columns, so that experts with a token
+// or two still use all lanes.  Of a tile's 128 weights' rows 64 are the gate's and 64 up's where the activation is gated: both halves
+// of a result meet in one block.  How many rows an expert has is known on the device only: every block counts the
+// experts' tiles for itself and takes every so-many-th of them; the instruction's columns and what is copied of the tokens go with what a
+// tile has, in sixteens.  Tokens are gathered by the copy engine, four rows an instruction, so nothing is permuted beforehand.
+//
+// A block: one warp fills a ring of 64-wide slices of both operands, one thread issues the products, eight warps take finished accumulators
+// out of tensor memory while the next tile is summed in its other half.
+#include <type_traits>
+
+#include "symar_act.cuh"
+#include "symar_maps.h"
+#include "symar_ops.h"
+#include "symar_tc.cuh"
+
+namespace symar {
+namespace {
+
+struct ExpertsArgs {
+    const __nv_bfloat16 *bias;
+    const int32_t *expert_start, *row_token;
+    void    *out;
+    int64_t  bias_expert, bias_group, out_ld, out_group;
+    int      groups, experts, rows, x_rows, n, k, act, gated;
+    int      x_shared, w_shared;           // one for all groups
+    int      gather_step;                  // gathered rows: a group's first row in the map
+    int      n_tiles;                      // of 128 channels, or 64 gated ones
+    int      vec_out;
+    unsigned *status;
+};
+
+constexpr int kRows = 128, kHalf = 64, kSlice = 64;
+constexpr int kMaxExperts = SYMAR_EXPERTS_MAX;
+constexpr int kThreads = 384;
+constexpr int kChunk = 2;                  // slices that a float32 result sums in the tensor cores at a time (see symar_linear.cu)
+constexpr int kBand  = 16;                 // tiles of tokens that run through a column of weights before the next
+constexpr int kStep  = 32;                 // tokens that leave the accumulator at a time
+
+__device__ __forceinline__ void results_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+// four rows of a map whose box is one row
+__device__ __forceinline__ void tma_gather(uint32_t dst, const CUtensorMap *map, int x, int4 rows, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar) : "memory");
+}
+
+template <int NT, bool kWide>
+struct Shape {
+    static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
+    static constexpr int kHold = kStep * kRows * 4;
+    static constexpr int kStages = (212 * 1024 - kHold) / kStage;
+    static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
+    static constexpr int kCols  = 2 * NT;                               // two accumulators
+};
+
+// The experts' rows and tiles: first[e] is expert e's first row, tiles[e] the tiles of NT rows of the experts before it.
+struct Plan {
+    int first[kMaxExperts + 1], tiles[kMaxExperts + 1];
+};
+// by one warp: starts that fall or leave 0 .. rows are brought into order
+__device__ __forceinline__ void make_plan(Plan &p, const int32_t *start, int experts, int rows, int nt)
+{
+    const int lane = threadIdx.x & 31;
+    int most = 0, tiles = 0;               // so far
+    for (int e0 = 0; e0 <= experts; e0 += 32) {
+        const int e = e0 + lane;
+        int v = e <= experts ? max(0, min(start[e], rows)) : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v = max(v, u);
+        }
+        v = max(v, most);
+        int before = __shfl_up_sync(0xffffffffu, v, 1);
+        if (lane == 0) before = most;
+        // tiles of expert e - 1, which ends here
+        int t = e > 0 && e <= experts ? (v - before + nt - 1) / nt : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, t, d);
+            if (lane >= d) t += u;
+        }
+        t += tiles;
+        if (e <= experts) p.first[e] = v, p.tiles[e] = t;
+        most = __shfl_sync(0xffffffffu, v, 31), tiles = __shfl_sync(0xffffffffu, t, 31);
+    }
+}
+
+struct Tile {
+    int g, e, row, count, n0;              // its rows, of one expert, and its first channel
+};
+template <int NT>
+__device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int tile)
+{
+    Tile t;
+    const int per = p.tiles[a.experts] * a.n_tiles;
+    t.g = tile / per;
+    int i = tile - t.g * per;
+    const int m = i / a.n_tiles;           // the last expert whose tiles begin at or before
+    int lo = 0, hi = a.experts - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.tiles[mid] <= m) lo = mid;
+        else hi = mid - 1;
+    }
+    t.e = lo;
+    const int m_tiles = p.tiles[lo + 1] - p.tiles[lo];
+    i -= p.tiles[lo] * a.n_tiles;
+    const int b = i / (kBand * a.n_tiles), wide = min(kBand, m_tiles - kBand * b);
+    i -= b * kBand * a.n_tiles;
+    const int m0 = (kBand * b + i % wide) * NT;
+    t.row   = p.first[lo] + m0;
+    t.count = min(NT, p.first[lo + 1] - t.row);
+    t.n0    = i / wide * (a.gated ? kHalf : kRows);
+    return t;
+}
+
+// Four neighbouring channels, from n on (fewer at the row's end): what the tile's rows share.
+struct Channels {
+    float bias[4], up_bias[4];
+    int   n, count;
+};
+__device__ __forceinline__ Channels channels_of(const ExpertsArgs &a, const Tile &t, int n)
+{
+    Channels c;
+    c.n     = n;
+    c.count = max(0, min(4, a.n - n));
+    const __nv_bfloat16 *b = a.bias ? a.bias + t.g * a.bias_group + t.e * a.bias_expert : nullptr;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        c.bias[i]    = b && i < c.count ? __bfloat162float(b[n + i]) : 0.0f;
+        c.up_bias[i] = b && a.gated && i < c.count ? __bfloat162float(b[a.n + n + i]) : 0.0f;
+    }
+    return c;
+}
+template <typename O>
+__device__ __forceinline__ void store(const ExpertsArgs &a, const Channels &c, int g, int row, const float (&y)[4])
+{
+    O *p = static_cast<O *>(a.out) + g * a.out_group + row * a.out_ld + c.n;
+    if (a.vec_out && c.count == 4) {
+        put4(p, y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < c.count) put(p + i, y[i]);
+    }
+}
+
+template <int NT, bool kWide, bool kGather>
+__global__ void __launch_bounds__(kThreads, 1)
+experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertsArgs a)
+{
+    using S = Shape<NT, kWide>;
+    using O = typename std::conditional<kWide, float, __nv_bfloat16>::type;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Plan plan;
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed, bad;
+    unsigned char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    float *hold = reinterpret_cast<float *>(ring + S::kStages * S::kStage);
+    const uint32_t ring_addr = smem_addr(ring);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(acc_full + 8 * i, 1);
+            bar_init(acc_empty + 8 * i, 256);
+        }
+        failed = bad = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    wait_for_stream();
+    if (warp == 3) make_plan(plan, a.expert_start, a.experts, a.rows, NT);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_at;
+    const int slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
+
+    if (warp == 0) {
+        // ---- producer: one warp ----
+        int st = 0, round = 0;
+        for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
+            const Tile t = tile_of<NT>(plan, a, tile);
+            const int cols = (t.count + 15) & ~15, second = t.n0 + (a.gated ? a.n : kHalf);
+            constexpr int kGroups = kGather ? (NT + 127) / 128 : 1;       // fours of rows of a lane
+            int4 rows[kGroups];
+            if (kGather) {
+#pragma unroll
+                for (int i = 0; i < kGroups; ++i) {
+                    int r[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at = 4 * (lane + 32 * i) + j;
+                        r[j] = at < t.count ? a.row_token[t.row + at] : 0;      // (columns behind the last are computed and not kept)
+                        if (r[j] < 0 || r[j] >= a.x_rows) r[j] = 0, bad = 1;
+                        r[j] += t.g * a.gather_step;
+                    }
+                    rows[i] = make_int4(r[0], r[1], r[2], r[3]);
+                }
+            }
+            const uint32_t bytes = S::kA + (kGather ? cols : (cols + kStep - 1) / kStep * kStep) * kSlice * 2;
+            for (int ks = 0; ks < slices; ++ks) {
+                if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
+                if (lane == 0) {
+                    bar_expect(bar, bytes);
+                    tma_load4(at, &wmap, ks * kSlice, t.n0, t.e, a.w_shared ? 0 : t.g, bar);
+                    tma_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, a.w_shared ? 0 : t.g, bar);
+                    if (!kGather)
+                        for (int c = 0; c < cols; c += kStep) tma_load(at + S::kA + c * kSlice * 2, &xmap, ks * kSlice, t.row + c, a.x_shared ? 0 : t.g, bar);
+                }
+                __syncwarp();
+                if (kGather) {
+#pragma unroll
+                    for (int i = 0; i < kGroups; ++i) {
+                        const int c = 4 * (lane + 32 * i);
+                        if (c < cols) tma_gather(at + S::kA + c * kSlice * 2, &xmap, ks * kSlice, rows[i], bar);
+                    }
+                }
+                if (++st == S::kStages) st = 0, ++round;
+            }
+        }
+    } else if (warp == 1 && elected()) {
+        // ---- products: one thread ----
+        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
+        int st = 0, round = 0;
+        uint32_t turn = 0;                              // accumulators filled so far
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            const uint32_t how = kHow | (uint32_t)((tile_of<NT>(plan, a, tile).count + 15) / 16 * 2) << 17;
+            for (int ks = 0; ks < slices;) {
+                const int to = kWide ? min(ks + kChunk, slices) : slices;
+                const uint32_t buf = turn & 1, acc = tmem + buf * NT;
+                if (turn >= 2 && !bar_wait(acc_empty + 8 * buf, ((turn >> 1) - 1) & 1, &failed)) goto done;
+                tc_after();
+                for (uint32_t add = 0; ks < to; ++ks, add = 1) {
+                    if (!bar_wait(full + 8 * st, round & 1, &failed)) goto done;
+                    tc_after();
+                    const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
+                    product(acc, w, x, how, add);
+#pragma unroll
+                    for (int i = 1; i < kSlice / 16; ++i) product(acc, w + 2 * i, x + 2 * i, how, 1);
+                    commit(empty + 8 * st);
+                    if (++st == S::kStages) st = 0, ++round;
+                }
+                commit(acc_full + 8 * buf);
+                ++turn;
+            }
+        }
+    } else if (warp >= 4) {
+        // ---- results: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four neighbouring
+        // channels of one token, and up's beside the gate's
+        const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        const int per = a.gated ? 2 : 1, four = a.gated ? lane & 15 : lane;          // tokens that a warp finishes at once, its lanes' channels
+        uint32_t turn = 0;
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            const Tile t = tile_of<NT>(plan, a, tile);
+            const Channels c = channels_of(a, t, t.n0 + 4 * four);
+            constexpr int kOwn = kWide ? NT / 2 : 1;
+            float sum[kOwn];
+            if (kWide) {
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) sum[i] = 0.0f;
+                for (int ks = 0; ks < slices; ks += kChunk, ++turn) {
+                    const uint32_t buf = turn & 1;
+                    (void)warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
+                    tc_after();
+#pragma unroll
+                    for (int c0 = 0; c0 < kOwn; c0 += 16) {
+                        if (2 * c0 + 16 * side >= t.count) continue;
+                        float v[16];
+                        acc_load16(tmem + lanes + buf * NT + 2 * c0 + 16 * side, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[kWide ? c0 + i : 0] += v[i];
+                    }
+                    tc_before();
+                    bar_arrive(acc_empty + 8 * buf);
+                }
+            } else if (slices > 0) {
+                (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);
+                tc_after();
+            }
+#pragma unroll
+            for (int c0 = 0; c0 < NT; c0 += kStep) {
+                if (c0 >= t.count) break;
+                float v[16];
+                if (kWide) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = sum[kWide ? c0 / 2 + i : 0];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                    if (slices > 0 && c0 + 16 * side < t.count) acc_load16(tmem + lanes + (turn & 1) * NT + c0 + 16 * side, v);
+                    if (slices > 0 && c0 + kStep >= t.count) {       // the accumulator is free for the tile after the next
+                        tc_before();
+                        bar_arrive(acc_empty + 8 * (turn & 1));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) hold[(16 * side + i) * kRows + ch] = v[i];
+                results_sync();
+                const int count = min(kStep, t.count - c0);
+                for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < count; i += 8 * per) {
+                    const float4 y4 = reinterpret_cast<const float4 *>(hold + i * kRows)[four];
+                    float y[4] = {y4.x + c.bias[0], y4.y + c.bias[1], y4.z + c.bias[2], y4.w + c.bias[3]};
+                    activate4(y, a.act);
+                    if (a.gated) {
+                        const float4 u = reinterpret_cast<const float4 *>(hold + i * kRows + kHalf)[four];
+                        y[0] *= u.x + c.up_bias[0]; y[1] *= u.y + c.up_bias[1]; y[2] *= u.z + c.up_bias[2]; y[3] *= u.w + c.up_bias[3];
+                    }
+                    store<O>(a, c, t.g, t.row + c0 + i, y);
+                }
+                results_sync();
+            }
+            if (!kWide && slices > 0) ++turn;
+        }
+    }
+done:
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    if (failed) {
+        // copies and products may still be in flight: give them time to end before the memory is let go
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (tid == 0 && a.status && (failed || bad)) atomicCAS(a.status, 0u, (unsigned)(failed ? SYMAR_ERR_TIMEOUT : SYMAR_ERR_INVAL));
+    tc_after();
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kCols) : "memory");
+}
+
+// ---- host ---------------------------------------------------------------------------------
+constexpr int kMost = 1 << 30;             // of rows, channels and k: what a tile adds stays below 2^31
+
+// A map of 64-wide boxes over bf16 elements; axes of one element have any stride.
+bool encode(CUtensorMap *map, const void *p, int axes, const int64_t *extent, const int64_t *stride, int box)
+{
+    cuuint64_t dims[4], bytes[3];
+    const cuuint32_t boxes[4] = {kSlice, (cuuint32_t)box, 1, 1}, ones[4] = {1, 1, 1, 1};
+    int64_t last = (extent[0] + 7) / 8 * 8;
+    for (int i = 0; i < axes; ++i) {
+        dims[i] = (cuuint64_t)extent[i];
+        if (i == 0) continue;
+        if (extent[i] > 1) last = stride[i];
+        bytes[i - 1] = (cuuint64_t)last * 2;
+    }
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, axes, const_cast<void *>(p), dims, bytes, boxes, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Whether the copy engine can walk an axis: steps of 16 bytes, below 2^40 of them.
+bool engine_axis(int64_t extent, int64_t stride) { return extent <= 1 || (stride >= 8 && stride % 8 == 0 && stride < (1ll << 39)); }
+
+template <int NT, bool kWide, bool kGather>
+int launch(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)
+{
+    using S = Shape<NT, kWide>;
+    auto fn = experts_kernel<NT, kWide, kGather>;
+    const int64_t used = a.experts < a.rows ? a.experts : a.rows, tiles = (int64_t)a.groups * a.n_tiles * (a.rows / NT + used);      // at most
+    if (tiles > kMost || (int64_t)a.n_tiles * kBand > kMost) return SYMAR_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_shared((const void *)fn, S::kBytes, d.id, allowed);
+    if (e == cudaSuccess) e = launch_early(fn, dim3((unsigned)(tiles < d.sms ? tiles : d.sms)), kThreads, S::kBytes, stream, wmap, xmap, a);
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
+}
+template <int NT, bool kWide>
+int launch_as(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t s)
+{
+    return a.row_token ? launch<NT, kWide, true>(a, wmap, xmap, d, s) : launch<NT, kWide, false>(a, wmap, xmap, d, s);
+}
+
+}  // namespace
+}  // namespace symar
+
+using namespace symar;
+
+extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
+{
+    if (!args) return SYMAR_ERR_INVAL;
+    const symar_experts_t &p = *args;
+    if (p.groups < 0 || p.experts < 0 || p.rows < 0 || p.x_rows < 0 || p.n < 0 || p.k < 0 || p.act < SYMAR_ACT_NONE || p.act > SYMAR_ACT_SILU ||
+        p.gated < 0 || p.gated > 1 || (p.out_dtype != SYMAR_F32 && p.out_dtype != SYMAR_BF16) || (uintptr_t)p.status % 4)
+        return SYMAR_ERR_INVAL;
+    if (p.experts > kMaxExperts || p.rows > kMost || p.x_rows > kMost || p.n > kMost || p.k > kMost) return SYMAR_ERR_UNSUPPORTED;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    auto clear = [&] {
+        const cudaError_t e = p.status ? cudaMemsetAsync(p.status, 0, sizeof(unsigned), s) : cudaSuccess;
+        return e == cudaSuccess ? (int)SYMAR_OK : cuda_fail(e, "cudaMemsetAsync");
+    };
+    if (p.groups == 0 || p.experts == 0 || p.rows == 0 || p.n == 0) return clear();
+    const uintptr_t width = p.out_dtype == SYMAR_F32 ? 4 : 2;
+    if (!p.out || !p.expert_start || (p.k > 0 && (!p.x || !p.w || p.x_rows == 0))) return SYMAR_ERR_INVAL;
+    if (((uintptr_t)p.x | (uintptr_t)p.w | (uintptr_t)p.bias) % 2 || (uintptr_t)p.out % width || ((uintptr_t)p.expert_start | (uintptr_t)p.row_token) % 4)
+        return SYMAR_ERR_INVAL;
+    if (!p.row_token && p.x_rows < p.rows) return SYMAR_ERR_INVAL;
+    if (p.x_ld < 0 || p.x_group < 0 || p.w_ld < 0 || p.w_expert < 0 || p.w_group < 0 || p.bias_expert < 0 || p.bias_group < 0 || p.out_ld < 0 ||
+        p.out_group < 0 || rows_meet(p.rows, p.out_ld, p.groups, p.out_group, p.n))
+        return SYMAR_ERR_INVAL;
+    Device d;
+    ExpertsArgs a{};
+    a.bias = (const __nv_bfloat16 *)p.bias;  a.bias_expert = p.bias_expert;  a.bias_group = p.bias_group;
+    a.expert_start = p.expert_start;  a.row_token = p.row_token;
+    a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
+    a.groups = p.groups;  a.experts = p.experts;  a.rows = p.rows;  a.x_rows = p.x_rows;
+    a.n = p.n;  a.k = p.k;  a.act = p.act;  a.gated = p.gated;
+    a.x_shared = p.groups == 1 || p.x_group == 0;
+    a.w_shared = p.groups == 1 || p.w_group == 0;
+    a.n_tiles = p.gated ? (p.n + kHalf - 1) / kHalf : (p.n + kRows - 1) / kRows;
+    a.vec_out = (uintptr_t)p.out % (4 * width) == 0 && p.out_ld % 4 == 0 && p.out_group % 4 == 0 && p.n % 4 == 0;
+    a.status = p.status;
+    CUtensorMap wmap{}, xmap{};
+    if (p.k > 0) {
+        const int64_t w_rows = (int64_t)p.n * (p.gated ? 2 : 1);
+        const int64_t w_extent[4] = {p.k, w_rows, p.experts, a.w_shared ? 1 : p.groups}, w_stride[4] = {1, p.w_ld, p.w_expert, p.w_group};
+        int64_t x_extent[3] = {p.k, p.x_rows, a.x_shared ? 1 : p.groups}, x_stride[3] = {1, p.x_ld, p.x_group};
+        bool ok = encoder() && ((uintptr_t)p.x | (uintptr_t)p.w) % 16 == 0;
+        for (int i = 1; i < 4; ++i) ok = ok && engine_axis(w_extent[i], w_stride[i]);
+        for (int i = 1; i < 3; ++i) ok = ok && engine_axis(x_extent[i], x_stride[i]);
+        if (!ok) return SYMAR_ERR_UNSUPPORTED;
+        if (p.row_token) {                 // one list of rows for all groups
+            if (!a.x_shared) {
+                if (p.x_rows == 1) x_stride[1] = x_stride[2];
+                const int64_t step = x_stride[2] / x_stride[1];
+                if (x_stride[2] % x_stride[1] || step * (p.groups - 1) + p.x_rows > kMost) return SYMAR_ERR_UNSUPPORTED;
+                a.gather_step = (int)step;
+                x_extent[1] += step * (p.groups - 1);
+            }
+            ok = encode(&xmap, p.x, 2, x_extent, x_stride, 1);
+        } else {
+            ok = encode(&xmap, p.x, 3, x_extent, x_stride, kStep);
+        }
+        if (!ok || !encode(&wmap, p.w, 4, w_extent, w_stride, kHalf)) return SYMAR_ERR_UNSUPPORTED;
+    }
+    int rc = device_info(&d);
+    if (rc == SYMAR_OK) rc = clear();
+    if (rc != SYMAR_OK) return rc;
+    // Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
+    const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = p.rows / used;
+    const bool wide = p.out_dtype == SYMAR_F32;
+    if (each <= 32) return wide ? launch_as<64, true>(a, wmap, xmap, d, s) : launch_as<64, false>(a, wmap, xmap, d, s);
+    if (wide) return launch_as<128, true>(a, wmap, xmap, d, s);
+    if (each <= 96) return launch_as<128, false>(a, wmap, xmap, d, s);
+    return launch_as<256, false>(a, wmap, xmap, d, s);
+}

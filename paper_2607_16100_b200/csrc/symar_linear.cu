@@ -19,6 +19,8 @@
 // others nothing).
 #include <type_traits>
 
+#include "symar_act.cuh"
+#include "symar_maps.h"
 #include "symar_ops.h"
 #include "symar_rows.h"
 #include "symar_tc.cuh"
@@ -55,44 +57,6 @@ __device__ __forceinline__ float4 peer_load4(uint32_t addr, int rank)
     return v;
 }
 __device__ __forceinline__ void results_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
-// y / 2 (1 + tanh u) = y / (1 + exp(-2u)); the quotient's two units in the last place are far below the result's rounding
-__device__ __forceinline__ float gate(float y, float two_u) { return __fdividef(y, 1.0f + expf(-two_u)); }
-__device__ __forceinline__ void activate4(float (&y)[4], int act)
-{
-    if (act == SYMAR_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.0f ? 0.0f : y[i];
-    } else if (act == SYMAR_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = 0.5f * y[i] * (1.0f + erff(y[i] * 0.70710678118654752f));
-    } else if (act == SYMAR_ACT_GELU_TANH) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = gate(y[i], 1.5957691216057308f * (y[i] + 0.044715f * y[i] * y[i] * y[i]));
-    } else if (act == SYMAR_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = gate(y[i], y[i]);
-    }
-}
-__device__ __forceinline__ void put(float *p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
-__device__ __forceinline__ void load4(const float *p, float (&r)[4])
-{
-    const float4 v = *reinterpret_cast<const float4 *>(p);
-    r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&r)[4])
-{
-    const uint2 v = *reinterpret_cast<const uint2 *>(p);
-    r[0] = __uint_as_float(v.x << 16); r[1] = __uint_as_float(v.x & 0xffff0000u);
-    r[2] = __uint_as_float(v.y << 16); r[3] = __uint_as_float(v.y & 0xffff0000u);
-}
-__device__ __forceinline__ void put4(float *p, const float (&r)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(r[0], r[1], r[2], r[3]); }
-__device__ __forceinline__ void put4(__nv_bfloat16 *p, const float (&r)[4])
-{
-    __nv_bfloat162 lo = __floats2bfloat162_rn(r[0], r[1]), hi = __floats2bfloat162_rn(r[2], r[3]);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<uint32_t *>(&lo), *reinterpret_cast<uint32_t *>(&hi));
-}
 
 // What follows the sums: four neighbouring channels of one token, from `n` on (fewer at the row's end).
 template <typename O> struct Four;
@@ -529,21 +493,6 @@ done:
 }
 
 // ---- host ---------------------------------------------------------------------------------
-using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                              CUtensorMapFloatOOBfill);
-EncodeFn encoder()
-{
-    static EncodeFn fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    return fn;
-}
-
 // Rows that the copy engine can read: on 16-byte boundaries, rows that do not overlap.
 bool engine_rows(const void *p, int64_t ld, int64_t group, int rows, int groups, int k)
 {
@@ -560,22 +509,6 @@ bool encode(CUtensorMap *map, const void *p, int64_t ld, int64_t group, int rows
     return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, boxes, ones,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-struct Device {
-    int sms = 0, id = -1;
-};
-int device_info(Device *d)
-{
-    static std::atomic<int> known[64];                   // multiprocessors; 0: not asked yet (by any thread)
-    cudaError_t e = cudaGetDevice(&d->id);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaGetDevice");
-    const bool slot = d->id >= 0 && d->id < 64;
-    if (slot && (d->sms = known[d->id].load(std::memory_order_relaxed)) > 0) return SYMAR_OK;
-    e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->id);
-    if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
-    if (slot) known[d->id].store(d->sms, std::memory_order_relaxed);
-    return SYMAR_OK;
 }
 
 template <int NT, bool kWide, bool kTma>

@@ -98,6 +98,7 @@ SIGNATURES = [
     ("symar_norm", c_int, [c_void_p, c_void_p]),
     ("symar_route_workspace", c_size_t, [c_int, c_int]),
     ("symar_route", c_int, [c_void_p, c_void_p]),
+    ("symar_experts", c_int, [c_void_p, c_void_p]),
     ("symar_combine", c_int, [c_void_p, c_void_p]),
     ("symar_probe_pingpong_blocks", c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int)]),
 ]
@@ -486,6 +487,18 @@ class RouteArgs(ctypes.Structure):
         ("expert_start", c_void_p), ("row_token", c_void_p), ("token_row", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t),
         ("scale", c_float), ("tokens", c_int32), ("experts", c_int32), ("top_k", c_int32), ("dtype", c_int32), ("score", c_int32),
         ("renormalise", c_int32),
+    ]
+
+
+class ExpertsArgs(ctypes.Structure):
+    _fields_ = [
+        ("x", c_void_p), ("x_ld", c_int64), ("x_group", c_int64),
+        ("w", c_void_p), ("w_ld", c_int64), ("w_expert", c_int64), ("w_group", c_int64),
+        ("bias", c_void_p), ("bias_expert", c_int64), ("bias_group", c_int64),
+        ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
+        ("expert_start", c_void_p), ("row_token", c_void_p),
+        ("groups", c_int32), ("experts", c_int32), ("rows", c_int32), ("x_rows", c_int32), ("n", c_int32), ("k", c_int32),
+        ("out_dtype", c_int32), ("act", c_int32), ("gated", c_int32), ("status", c_void_p),
     ]
 
 
@@ -964,6 +977,58 @@ def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise:
     got._set(whole[:rows].view(tokens, top_k), weights, whole[start:start + experts + 1], whole[rows:2 * rows],
              whole[2 * rows:start].view(tokens, top_k), shape[:1] + (top_k,), experts, index)
     return got
+
+
+def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool = False, by_row: bool = False, out=None, out_dtype=None,
+            status=None, stream=None):
+    """Every expert's product over its tokens (``symar_experts``): ``act(x w_e^T + b_e)``, or gated ``act(gate) * up``.
+
+    x [tokens, k] or [ranks, tokens, k] bfloat16, with ``by_row`` a row for every choice as an earlier call left them ([rows, k] or [ranks, rows,
+    k]); w [experts, n, k] or [ranks, experts, n, k] and bias without k, of 2n rows where ``gated``: the gate's, then up's.  The result is
+    [rows, n], or [ranks, rows, n] where x or w has ranks, bfloat16 unless said or given by ``out``; its rows stand as ``routes`` sorts them, those of nobody
+    (behind the last expert's) are not written.  ``status``: as in :func:`linear`."""
+    torch = _T or _torch()
+    where = "symar_experts"
+    bf16 = torch.bfloat16
+    if x.dtype is not bf16 or w.dtype is not bf16 or (bias is not None and bias.dtype is not bf16):
+        raise SymarError(ERR_UNSUPPORTED, f"{where}: operands are bfloat16")
+    index, code = routes.index, ACTS.get(act)
+    xsh, wsh, xs, ws = x.shape, w.shape, x.stride(), w.stride()
+    xd, wd = len(xsh), len(wsh)
+    if xd not in (2, 3) or wd not in (3, 4) or code is None:
+        _bad(where, "x has two or three dimensions, w three or four, act is one of " + ", ".join(ACTS))
+    k, wide = xsh[-1], 2 if gated else 1
+    n = wsh[-2] // wide
+    ranked = xd == 3 or wd == 4
+    groups = (xsh[0] if xd == 3 else wsh[0]) if ranked else 1
+    x_rows = routes.rows if by_row else routes.tokens
+    if xsh[-2] != x_rows or wsh[-3:] != (routes.experts, n * wide, k) or (wd == 4 and wsh[0] != groups) or x.get_device() != index or \
+            w.get_device() != index:
+        _bad(where, f"shapes of x {tuple(xsh)} and w {tuple(wsh)} for {x_rows} rows and {routes.experts} experts, or not on the routes' device")
+    if k > 1 and (xs[-1] != 1 or ws[-1] != 1):
+        _bad(where, "the innermost axis is contiguous")
+    shape = (groups, routes.rows, n) if ranked else (routes.rows, n)
+    if out is None:
+        out = _new(x, shape, out_dtype or bf16, index, stream)
+    os = out.stride()
+    if out.shape != shape or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and os[-1] != 1) or out.get_device() != index:
+        _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+    bp = be = bg = sp = 0
+    if bias is not None:
+        bs = bias.stride()
+        if bias.shape not in ((routes.experts, n * wide), (groups, routes.experts, n * wide)) or (n * wide > 1 and bs[-1] != 1) or \
+                bias.get_device() != index:
+            _bad(where, f"bias of shape {tuple(bias.shape)}")
+        bp, be, bg = bias.data_ptr(), bs[-2], bs[0] if len(bs) == 3 else 0
+    if status is not None:
+        if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != index:
+            _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
+        sp = status.data_ptr()
+    args = ExpertsArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
+                       out.data_ptr(), os[-2], os[0] if ranked else 0, routes.expert_start.data_ptr(), None if by_row else routes.row_token.data_ptr(),
+                       groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
+    _call((_lib or load()).symar_experts, where, index, stream, byref(args))
+    return out
 
 
 def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_dtype=None, stream=None):

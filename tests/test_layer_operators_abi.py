@@ -102,3 +102,37 @@ def test_combine_sizes(lib):
     assert combine_rc(lib, n=1 << 30, tokens=1 << 20, out_ld=1 << 31, out_group=1 << 52) == symar.ERR_UNSUPPORTED
     for empty in ("groups", "tokens", "n"):
         assert combine_rc(lib, **{empty: 0, "y": None, "out": None, "token_row": None}) == symar.OK
+
+
+def experts_rc(lib, **change):
+    f = dict(x=SOME, x_ld=64, x_group=512, w=SOME, w_ld=64, w_expert=4096, w_group=1 << 15, bias=SOME, bias_expert=64, bias_group=512, out=SOME, out_ld=32,
+             out_group=1024, expert_start=SOME, row_token=SOME, groups=2, experts=8, rows=16, x_rows=8, n=32, k=64, out_dtype=symar.BF16, act=4, gated=1,
+             status=SOME)
+    f.update(change)
+    return lib.symar_experts(ctypes.byref(symar.ExpertsArgs(**f)), None)
+
+
+@pytest.mark.parametrize("change", [
+    dict(x=None), dict(w=None), dict(out=None), dict(expert_start=None), dict(groups=-1), dict(experts=-1), dict(rows=-1), dict(x_rows=-1), dict(n=-1),
+    dict(k=-1), dict(act=5), dict(act=-1), dict(gated=2), dict(gated=-1), dict(out_dtype=2), dict(x=SOME + 1), dict(w=SOME + 1), dict(bias=SOME + 1),
+    dict(out=SOME + 1), dict(out=SOME + 2, out_dtype=symar.F32), dict(expert_start=SOME + 2), dict(row_token=SOME + 2), dict(status=SOME + 2),
+    dict(row_token=None), dict(x_rows=0), dict(x_ld=-8), dict(x_group=-8), dict(w_ld=-8), dict(w_expert=-8), dict(w_group=-8), dict(bias_expert=-1),
+    dict(bias_group=-1), dict(out_ld=31), dict(out_ld=-32), dict(out_group=0), dict(out_group=500),
+], ids=ids)
+def test_experts_refuses(lib, change):
+    assert experts_rc(lib, **change) == symar.ERR_INVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(experts=1025), dict(rows=(1 << 30) + 1), dict(n=(1 << 30) + 1), dict(k=(1 << 30) + 1), dict(x_rows=(1 << 30) + 1), dict(x=SOME + 8), dict(w=SOME + 2),
+    dict(x_ld=68), dict(x_ld=0), dict(x_group=100), dict(x_group=520), dict(w_ld=12), dict(w_ld=0), dict(w_expert=4), dict(w_expert=0), dict(w_group=9),
+    dict(x_ld=1 << 39, x_group=1 << 39), dict(w_expert=1 << 40),
+], ids=ids)
+def test_experts_is_not_for(lib, change):
+    assert experts_rc(lib, **change) == symar.ERR_UNSUPPORTED
+
+
+def test_experts_without_work(lib):
+    assert lib.symar_experts(None, None) == symar.ERR_INVAL
+    for empty in ("groups", "experts", "rows", "n"):
+        assert experts_rc(lib, **{empty: 0, "x": None, "w": None, "out": None, "expert_start": None, "status": None}) == symar.OK
