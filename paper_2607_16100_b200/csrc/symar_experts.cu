@@ -5,7 +5,7 @@
 // or two still use all lanes.  Of a tile's 128 weights' rows 64 are the gate's and 64 up's where the activation is gated: both halves
 // of a result meet in one block.  How many rows an expert has is known on the device only: every block counts the
 // experts' tiles for itself and takes every so-many-th of them; the instruction's columns and what is copied of the tokens go with what a
-// tile has, in sixteens.  Tokens are gathered by the copy engine, four rows an instruction, so nothing is permuted beforehand.
+// tile has, in sixteens.  Four more warps gather the tokens' rows straight into the ring, so nothing is permuted beforehand.
 //
 // A block: one warp fills a ring of 64-wide slices of both operands, one thread issues the products, eight warps take finished accumulators
 // out of tensor memory while the next tile is summed in its other half.
@@ -20,13 +20,12 @@ namespace symar {
 namespace {
 
 struct ExpertsArgs {
-    const __nv_bfloat16 *bias;
+    const __nv_bfloat16 *bias, *x;         // (x: where its rows are gathered)
     const int32_t *expert_start, *row_token;
     void    *out;
-    int64_t  bias_expert, bias_group, out_ld, out_group;
+    int64_t  x_ld, x_group, bias_expert, bias_group, out_ld, out_group;
     int      groups, experts, rows, x_rows, n, k, act, gated;
     int      x_shared, w_shared;           // one for all groups
-    int      gather_step;                  // gathered rows: a group's first row in the map
     int      n_tiles;                      // of 128 channels, or 64 gated ones
     int      vec_out;
     unsigned *status;
@@ -34,7 +33,7 @@ struct ExpertsArgs {
 
 constexpr int kRows = 128, kHalf = 64, kSlice = 64;
 constexpr int kMaxExperts = SYMAR_EXPERTS_MAX;
-constexpr int kThreads = 384;
+constexpr int kLoaders = 128;                // threads that gather rows
 constexpr int kChunk = 2;                  // slices that a float32 result sums in the tensor cores at a time (see symar_linear.cu)
 constexpr int kBand  = 16;                 // tiles of tokens that run through a column of weights before the next
 constexpr int kStep  = 32;                 // tokens that leave the accumulator at a time
@@ -45,15 +44,17 @@ __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
-// four rows of a map whose box is one row
-__device__ __forceinline__ void tma_gather(uint32_t dst, const CUtensorMap *map, int x, int4 rows, uint32_t bar)
+// sixteen bytes of which the first `count` are read and the rest are zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t count)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w), "r"(bar) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(count) : "memory");
 }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-template <int NT, bool kWide>
+template <int NT, bool kWide, bool kGather>
 struct Shape {
+    static constexpr int kThreads = 384 + (kGather ? kLoaders : 0);
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
     static constexpr int kHold = kStep * kRows * 4;
     static constexpr int kStages = (212 * 1024 - kHold) / kStage;
@@ -155,10 +156,10 @@ __device__ __forceinline__ void store(const ExpertsArgs &a, const Channels &c, i
 }
 
 template <int NT, bool kWide, bool kGather>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Shape<NT, kWide, kGather>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertsArgs a)
 {
-    using S = Shape<NT, kWide>;
+    using S = Shape<NT, kWide, kGather>;
     using O = typename std::conditional<kWide, float, __nv_bfloat16>::type;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Plan plan;
@@ -173,7 +174,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
 
     if (tid == 0) {
         for (int i = 0; i < S::kStages; ++i) {
-            bar_init(full + 8 * i, 1);
+            bar_init(full + 8 * i, kGather ? 1 + kLoaders : 1);
             bar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -195,50 +196,72 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const uint32_t tmem = tmem_at;
     const int slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
 
-    if (warp == 0) {
-        // ---- producer: one warp ----
+    if (warp == 0 && elected()) {
+        // ---- producer: one thread.  A copy's own cost is what counts: a box of a whole tile's rows, whatever of them is used (boxes of 32 rows:
+        // 303 us instead of 203 for 16384 rows x 2048 x 4096), and no gathering by the copy engine (four rows an instruction: 1090 us)
         int st = 0, round = 0;
         for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
             const Tile t = tile_of<NT>(plan, a, tile);
-            const int cols = (t.count + 15) & ~15, second = t.n0 + (a.gated ? a.n : kHalf);
-            constexpr int kGroups = kGather ? (NT + 127) / 128 : 1;       // fours of rows of a lane
-            int4 rows[kGroups];
-            if (kGather) {
-#pragma unroll
-                for (int i = 0; i < kGroups; ++i) {
-                    int r[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int at = 4 * (lane + 32 * i) + j;
-                        r[j] = at < t.count ? a.row_token[t.row + at] : 0;      // (columns behind the last are computed and not kept)
-                        if (r[j] < 0 || r[j] >= a.x_rows) r[j] = 0, bad = 1;
-                        r[j] += t.g * a.gather_step;
-                    }
-                    rows[i] = make_int4(r[0], r[1], r[2], r[3]);
-                }
-            }
-            const uint32_t bytes = S::kA + (kGather ? cols : (cols + kStep - 1) / kStep * kStep) * kSlice * 2;
+            const int second = t.n0 + (a.gated ? a.n : kHalf), wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
             for (int ks = 0; ks < slices; ++ks) {
-                if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
-                if (lane == 0) {
-                    bar_expect(bar, bytes);
-                    tma_load4(at, &wmap, ks * kSlice, t.n0, t.e, a.w_shared ? 0 : t.g, bar);
-                    tma_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, a.w_shared ? 0 : t.g, bar);
-                    if (!kGather)
-                        for (int c = 0; c < cols; c += kStep) tma_load(at + S::kA + c * kSlice * 2, &xmap, ks * kSlice, t.row + c, a.x_shared ? 0 : t.g, bar);
-                }
-                __syncwarp();
-                if (kGather) {
-#pragma unroll
-                    for (int i = 0; i < kGroups; ++i) {
-                        const int c = 4 * (lane + 32 * i);
-                        if (c < cols) tma_gather(at + S::kA + c * kSlice * 2, &xmap, ks * kSlice, rows[i], bar);
-                    }
-                }
+                bar_expect(bar, S::kA + (kGather ? 0 : S::kB));
+                tma_load4(at, &wmap, ks * kSlice, t.n0, t.e, wg, bar);
+                tma_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, wg, bar);
+                if (!kGather) tma_load(at + S::kA, &xmap, ks * kSlice, t.row, xg, bar);
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
+    } else if (kGather && warp >= 12) {
+        // ---- gathered rows: four warps; a thread has one piece of every sixteenth row.  A stage is given away three stages after its copies
+        // were asked for, behind the fence that shows them to the tensor cores.
+        constexpr int kOf = kGather ? NT / 16 : 1, kAhead = 3;
+        static_assert(S::kStages > kAhead, "");
+        const int c = tid & 7, r = (tid - 384) >> 3;
+        int st = 0, round = 0, given = 0, asked = 0;     // stages
+        Tile t{};
+        int token[kOf], next[kOf];                       // of this tile's rows and, asked for a tile ahead, of the next one's
+        auto tokens_of = [&](int tile) {
+            if (tile >= tiles) return;
+            t = tile_of<NT>(plan, a, tile);
+#pragma unroll
+            for (int j = 0; j < kOf; ++j) next[j] = r + 16 * j < t.count ? a.row_token[t.row + r + 16 * j] : -1;      // (columns behind the last are zeros)
+        };
+        tokens_of(blockIdx.x);
+        for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
+            const __nv_bfloat16 *x = a.x + (a.x_shared ? 0 : t.g * a.x_group);
+            const int cols = (t.count + 15) & ~15;
+#pragma unroll
+            for (int j = 0; j < kOf; ++j) {
+                token[j] = next[j];
+                if (r + 16 * j < t.count && (uint32_t)token[j] >= (uint32_t)a.x_rows) token[j] = -1, bad = 1;
+            }
+            tokens_of(tile + gridDim.x);
+            for (int ks = 0; ks < slices; ++ks) {
+                if (asked - given == kAhead) {
+                    copies_wait<kAhead - 1>();
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    bar_arrive(full + 8 * (given % S::kStages));
+                    ++given;
+                }
+                if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                const int k0 = ks * kSlice + c * 8;
+                const uint32_t count = (uint32_t)max(0, min(8, a.k - k0)) * 2, dst = ring_addr + st * S::kStage + S::kA + r * 128 + ((c ^ (r & 7)) << 4);
+#pragma unroll
+                for (int j = 0; j < kOf; ++j) {
+                    if (16 * j >= cols) break;
+                    const bool on = token[j] >= 0 && count > 0;
+                    copy16(dst + j * 16 * 128, on ? x + (int64_t)token[j] * a.x_ld + k0 : a.x, on ? count : 0);
+                }
+                copies_end();
+                ++asked;
+                if (++st == S::kStages) st = 0, ++round;
+            }
+        }
+        copies_wait<0>();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (; given < asked; ++given) bar_arrive(full + 8 * (given % S::kStages));
     } else if (warp == 1 && elected()) {
         // ---- products: one thread ----
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
@@ -265,7 +288,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 ++turn;
             }
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 12) {
         // ---- results: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four neighbouring
         // channels of one token, and up's beside the gate's
         const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
@@ -374,13 +397,13 @@ bool engine_axis(int64_t extent, int64_t stride) { return extent <= 1 || (stride
 template <int NT, bool kWide, bool kGather>
 int launch(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)
 {
-    using S = Shape<NT, kWide>;
+    using S = Shape<NT, kWide, kGather>;
     auto fn = experts_kernel<NT, kWide, kGather>;
     const int64_t used = a.experts < a.rows ? a.experts : a.rows, tiles = (int64_t)a.groups * a.n_tiles * (a.rows / NT + used);      // at most
     if (tiles > kMost || (int64_t)a.n_tiles * kBand > kMost) return SYMAR_ERR_UNSUPPORTED;
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow_shared((const void *)fn, S::kBytes, d.id, allowed);
-    if (e == cudaSuccess) e = launch_early(fn, dim3((unsigned)(tiles < d.sms ? tiles : d.sms)), kThreads, S::kBytes, stream, wmap, xmap, a);
+    if (e == cudaSuccess) e = launch_early(fn, dim3((unsigned)(tiles < d.sms ? tiles : d.sms)), S::kThreads, S::kBytes, stream, wmap, xmap, a);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
 }
 template <int NT, bool kWide>
@@ -419,6 +442,7 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
     Device d;
     ExpertsArgs a{};
     a.bias = (const __nv_bfloat16 *)p.bias;  a.bias_expert = p.bias_expert;  a.bias_group = p.bias_group;
+    a.x = (const __nv_bfloat16 *)p.x;  a.x_ld = p.x_ld;  a.x_group = p.x_group;
     a.expert_start = p.expert_start;  a.row_token = p.row_token;
     a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
     a.groups = p.groups;  a.experts = p.experts;  a.rows = p.rows;  a.x_rows = p.x_rows;
@@ -429,36 +453,25 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
     a.vec_out = (uintptr_t)p.out % (4 * width) == 0 && p.out_ld % 4 == 0 && p.out_group % 4 == 0 && p.n % 4 == 0;
     a.status = p.status;
     CUtensorMap wmap{}, xmap{};
+    // Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
+    const bool wide = p.out_dtype == SYMAR_F32;
+    const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = p.rows / used;
+    const int nt = each <= 32 ? 64 : (each <= 96 || wide ? 128 : 256);
     if (p.k > 0) {
         const int64_t w_rows = (int64_t)p.n * (p.gated ? 2 : 1);
         const int64_t w_extent[4] = {p.k, w_rows, p.experts, a.w_shared ? 1 : p.groups}, w_stride[4] = {1, p.w_ld, p.w_expert, p.w_group};
-        int64_t x_extent[3] = {p.k, p.x_rows, a.x_shared ? 1 : p.groups}, x_stride[3] = {1, p.x_ld, p.x_group};
+        const int64_t x_extent[3] = {p.k, p.x_rows, a.x_shared ? 1 : p.groups}, x_stride[3] = {1, p.x_ld, p.x_group};
         bool ok = encoder() && ((uintptr_t)p.x | (uintptr_t)p.w) % 16 == 0;
         for (int i = 1; i < 4; ++i) ok = ok && engine_axis(w_extent[i], w_stride[i]);
         for (int i = 1; i < 3; ++i) ok = ok && engine_axis(x_extent[i], x_stride[i]);
         if (!ok) return SYMAR_ERR_UNSUPPORTED;
-        if (p.row_token) {                 // one list of rows for all groups
-            if (!a.x_shared) {
-                if (p.x_rows == 1) x_stride[1] = x_stride[2];
-                const int64_t step = x_stride[2] / x_stride[1];
-                if (x_stride[2] % x_stride[1] || step * (p.groups - 1) + p.x_rows > kMost) return SYMAR_ERR_UNSUPPORTED;
-                a.gather_step = (int)step;
-                x_extent[1] += step * (p.groups - 1);
-            }
-            ok = encode(&xmap, p.x, 2, x_extent, x_stride, 1);
-        } else {
-            ok = encode(&xmap, p.x, 3, x_extent, x_stride, kStep);
-        }
+        if (!p.row_token) ok = encode(&xmap, p.x, 3, x_extent, x_stride, nt);
         if (!ok || !encode(&wmap, p.w, 4, w_extent, w_stride, kHalf)) return SYMAR_ERR_UNSUPPORTED;
     }
     int rc = device_info(&d);
     if (rc == SYMAR_OK) rc = clear();
     if (rc != SYMAR_OK) return rc;
-    // Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
-    const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = p.rows / used;
-    const bool wide = p.out_dtype == SYMAR_F32;
-    if (each <= 32) return wide ? launch_as<64, true>(a, wmap, xmap, d, s) : launch_as<64, false>(a, wmap, xmap, d, s);
+    if (nt == 64) return wide ? launch_as<64, true>(a, wmap, xmap, d, s) : launch_as<64, false>(a, wmap, xmap, d, s);
     if (wide) return launch_as<128, true>(a, wmap, xmap, d, s);
-    if (each <= 96) return launch_as<128, false>(a, wmap, xmap, d, s);
-    return launch_as<256, false>(a, wmap, xmap, d, s);
+    return nt == 128 ? launch_as<128, false>(a, wmap, xmap, d, s) : launch_as<256, false>(a, wmap, xmap, d, s);
 }

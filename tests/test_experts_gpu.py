@@ -162,14 +162,7 @@ def test_strides(by_row):
         for out in (BF16, F32):
             room = torch.full((r.rows, 2, n + 8), 7.0, dtype=out, device="cuda")
             got = room[..., offset:offset + n].transpose(0, 1)
-            if by_row:
-                check(x, w, r, by_row=by_row, out_dtype=out, out=got)
-            else:
-                with pytest.raises(symar.SymarError) as err:         # (ranks of a token 208 elements apart, tokens 624)
-                    symar.experts(x, w, r, out=got)
-                assert err.value.code == symar.ERR_UNSUPPORTED
-                apart = normal(2, rows, k + 8, seed=3)[..., 8:]
-                check(apart, w, r, out_dtype=out, out=got)
+            check(x, w, r, by_row=by_row, out_dtype=out, out=got)
             assert (room[..., :offset] == 7).all() and (room[..., offset + n:] == 7).all()
     many = normal(5, 1, k, seed=4)                                   # one token of every rank
     one = lists([1, 2, 0, 1], 1)

@@ -125,7 +125,7 @@ def test_experts_refuses(lib, change):
 
 @pytest.mark.parametrize("change", [
     dict(experts=1025), dict(rows=(1 << 30) + 1), dict(n=(1 << 30) + 1), dict(k=(1 << 30) + 1), dict(x_rows=(1 << 30) + 1), dict(x=SOME + 8), dict(w=SOME + 2),
-    dict(x_ld=68), dict(x_ld=0), dict(x_group=100), dict(x_group=520), dict(w_ld=12), dict(w_ld=0), dict(w_expert=4), dict(w_expert=0), dict(w_group=9),
+    dict(x_ld=68), dict(x_ld=0), dict(x_group=100), dict(w_ld=12), dict(w_ld=0), dict(w_expert=4), dict(w_expert=0), dict(w_group=9),
     dict(x_ld=1 << 39, x_group=1 << 39), dict(w_expert=1 << 40),
 ], ids=ids)
 def test_experts_is_not_for(lib, change):
