@@ -660,7 +660,9 @@ int symar_route(const symar_route_t *args, void *cuda_stream);
  * multiples of 8 elements, not 0); SYMAR_ERR_UNSUPPORTED otherwise.  Sizes of 0 are allowed (k = 0: the product is 0); 1024 experts at most, other sizes up to 2^30.
  * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_INVAL by a row_token
  * outside x, or to SYMAR_ERR_TIMEOUT if a wait inside the kernel (for its own copies and products, four seconds at most) gave up;
- * `out` is then incomplete.                                                         */
+ * `out` is then incomplete.
+ * workspace: symar_experts_workspace(args) bytes (0 where rows are few, in order already or float32), 16-byte aligned, that no other call uses
+ * meanwhile: the gathered rows of x.  What it holds before and after is of no account.   */
 enum { SYMAR_EXPERTS_MAX = 1024 };
 typedef struct {
     const void    *x;    int64_t x_ld, x_group;
@@ -672,7 +674,9 @@ typedef struct {
     int32_t        groups, experts, rows, x_rows, n, k;
     int32_t        out_dtype, act, gated;
     uint32_t      *status;
+    void          *workspace; size_t workspace_bytes;
 } symar_experts_t;
+size_t symar_experts_workspace(const symar_experts_t *args);      /* by sizes, strides and whether row_token is NULL alone */
 int symar_experts(const symar_experts_t *args, void *cuda_stream);
 
 /* out[g][t] = sum_j weights[t][j] y[g][token_row[t][j]] + residual[g][t]: the rows of a token's experts back in the tokens'

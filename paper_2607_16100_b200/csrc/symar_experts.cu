@@ -49,8 +49,13 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t c
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(count) : "memory");
 }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+// An arrival of this thread once all its copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint32_t bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+// What other threads' copies have written, seen by the tensor cores behind this.
+__device__ __forceinline__ void copies_seen() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <int NT, bool kWide, bool kGather>
 struct Shape {
@@ -62,7 +67,7 @@ struct Shape {
     static constexpr int kCols  = 2 * NT;                               // two accumulators
 };
 
-// The experts' rows and tiles: first[e] is expert e's first row, tiles[e] the tiles of NT rows of the experts before it.
+// The experts' rows and tiles: first[e] is expert e's first row, tiles[e] the tiles of at most NT rows of the experts before it.
 struct Plan {
     int first[kMaxExperts + 1], tiles[kMaxExperts + 1];
 };
@@ -98,8 +103,8 @@ __device__ __forceinline__ void make_plan(Plan &p, const int32_t *start, int exp
 struct Tile {
     int g, e, row, count, n0;              // its rows, of one expert, and its first channel
 };
-template <int NT>
-__device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int tile)
+// (tiles of `channels` results)
+__device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int tile, int channels)
 {
     Tile t;
     const int per = p.tiles[a.experts] * a.n_tiles;
@@ -117,10 +122,11 @@ __device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int
     i -= p.tiles[lo] * a.n_tiles;
     const int b = i / (kBand * a.n_tiles), wide = min(kBand, m_tiles - kBand * b);
     i -= b * kBand * a.n_tiles;
-    const int m0 = (kBand * b + i % wide) * NT;
+    // an expert's tiles are of one size, in 32s: its last one's weights would cost as much for a few rows as for many
+    const int rows = p.first[lo + 1] - p.first[lo], size = ((rows + m_tiles - 1) / m_tiles + 31) & ~31, m0 = (kBand * b + i % wide) * size;
     t.row   = p.first[lo] + m0;
-    t.count = min(NT, p.first[lo + 1] - t.row);
-    t.n0    = i / wide * (a.gated ? kHalf : kRows);
+    t.count = min(size, rows - m0);
+    t.n0    = i / wide * channels;
     return t;
 }
 
@@ -153,6 +159,30 @@ __device__ __forceinline__ void store(const ExpertsArgs &a, const Channels &c, i
         for (int i = 0; i < 4; ++i)
             if (i < c.count) put(p + i, y[i]);
     }
+}
+
+// 32 tokens from c0 on of a tile: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four
+// neighbouring channels of one token, and up's beside the gate's.
+template <typename O>
+__device__ __forceinline__ void finish(const ExpertsArgs &a, const Tile &t, const Channels &c, int c0, const float (&v)[16], float *hold, int ew, int side,
+                                       int ch, int lane)
+{
+    const int per = a.gated ? 2 : 1, four = a.gated ? lane & 15 : lane;          // tokens that a warp finishes at once, its lanes' channels
+#pragma unroll
+    for (int i = 0; i < 16; ++i) hold[(16 * side + i) * kRows + ch] = v[i];
+    results_sync();
+    const int count = min(kStep, t.count - c0);
+    for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < count; i += 8 * per) {
+        const float4 y4 = reinterpret_cast<const float4 *>(hold + i * kRows)[four];
+        float y[4] = {y4.x + c.bias[0], y4.y + c.bias[1], y4.z + c.bias[2], y4.w + c.bias[3]};
+        activate4(y, a.act);
+        if (a.gated) {
+            const float4 u = reinterpret_cast<const float4 *>(hold + i * kRows + kHalf)[four];
+            y[0] *= u.x + c.up_bias[0]; y[1] *= u.y + c.up_bias[1]; y[2] *= u.z + c.up_bias[2]; y[3] *= u.w + c.up_bias[3];
+        }
+        store<O>(a, c, t.g, t.row + c0 + i, y);
+    }
+    results_sync();
 }
 
 template <int NT, bool kWide, bool kGather>
@@ -194,14 +224,14 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     __syncthreads();
     tc_after();
     const uint32_t tmem = tmem_at;
-    const int slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
+    const int channels = a.gated ? kHalf : kRows, slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
 
     if (warp == 0 && elected()) {
         // ---- producer: one thread.  A copy's own cost is what counts: a box of a whole tile's rows, whatever of them is used (boxes of 32 rows:
         // 303 us instead of 203 for 16384 rows x 2048 x 4096), and no gathering by the copy engine (four rows an instruction: 1090 us)
         int st = 0, round = 0;
         for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
-            const Tile t = tile_of<NT>(plan, a, tile);
+            const Tile t = tile_of(plan, a, tile, channels);
             const int second = t.n0 + (a.gated ? a.n : kHalf), wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
             for (int ks = 0; ks < slices; ++ks) {
                 if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
@@ -214,17 +244,16 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             }
         }
     } else if (kGather && warp >= 12) {
-        // ---- gathered rows: four warps; a thread has one piece of every sixteenth row.  A stage is given away three stages after its copies
-        // were asked for, behind the fence that shows them to the tensor cores.
-        constexpr int kOf = kGather ? NT / 16 : 1, kAhead = 3;
-        static_assert(S::kStages > kAhead, "");
+        // ---- gathered rows: four warps; a thread has one piece of every sixteenth row.  The copies themselves arrive at the stage's barrier; the
+        // fence that shows them to the tensor cores is behind the wait for it, as here it would wait for all copies on their way.
+        constexpr int kOf = kGather ? NT / 16 : 1;
         const int c = tid & 7, r = (tid - 384) >> 3;
-        int st = 0, round = 0, given = 0, asked = 0;     // stages
+        int st = 0, round = 0;
         Tile t{};
         int token[kOf], next[kOf];                       // of this tile's rows and, asked for a tile ahead, of the next one's
         auto tokens_of = [&](int tile) {
             if (tile >= tiles) return;
-            t = tile_of<NT>(plan, a, tile);
+            t = tile_of(plan, a, tile, channels);
 #pragma unroll
             for (int j = 0; j < kOf; ++j) next[j] = r + 16 * j < t.count ? a.row_token[t.row + r + 16 * j] : -1;      // (columns behind the last are zeros)
         };
@@ -239,12 +268,6 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             }
             tokens_of(tile + gridDim.x);
             for (int ks = 0; ks < slices; ++ks) {
-                if (asked - given == kAhead) {
-                    copies_wait<kAhead - 1>();
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    bar_arrive(full + 8 * (given % S::kStages));
-                    ++given;
-                }
                 if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const int k0 = ks * kSlice + c * 8;
                 const uint32_t count = (uint32_t)max(0, min(8, a.k - k0)) * 2, dst = ring_addr + st * S::kStage + S::kA + r * 128 + ((c ^ (r & 7)) << 4);
@@ -254,21 +277,17 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     const bool on = token[j] >= 0 && count > 0;
                     copy16(dst + j * 16 * 128, on ? x + (int64_t)token[j] * a.x_ld + k0 : a.x, on ? count : 0);
                 }
-                copies_end();
-                ++asked;
+                copies_arrive(full + 8 * st);
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
-        copies_wait<0>();
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        for (; given < asked; ++given) bar_arrive(full + 8 * (given % S::kStages));
     } else if (warp == 1 && elected()) {
         // ---- products: one thread ----
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
         int st = 0, round = 0;
         uint32_t turn = 0;                              // accumulators filled so far
         for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-            const uint32_t how = kHow | (uint32_t)((tile_of<NT>(plan, a, tile).count + 15) / 16 * 2) << 17;
+            const uint32_t how = kHow | (uint32_t)((tile_of(plan, a, tile, channels).count + 15) / 16 * 2) << 17;
             for (int ks = 0; ks < slices;) {
                 const int to = kWide ? min(ks + kChunk, slices) : slices;
                 const uint32_t buf = turn & 1, acc = tmem + buf * NT;
@@ -276,6 +295,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 tc_after();
                 for (uint32_t add = 0; ks < to; ++ks, add = 1) {
                     if (!bar_wait(full + 8 * st, round & 1, &failed)) goto done;
+                    if (kGather) copies_seen();
                     tc_after();
                     const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
                     product(acc, w, x, how, add);
@@ -289,15 +309,13 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             }
         }
     } else if (warp >= 4 && warp < 12) {
-        // ---- results: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four neighbouring
-        // channels of one token, and up's beside the gate's
+        // ---- results ----
         const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)quarter << 21;
-        const int per = a.gated ? 2 : 1, four = a.gated ? lane & 15 : lane;          // tokens that a warp finishes at once, its lanes' channels
         uint32_t turn = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-            const Tile t = tile_of<NT>(plan, a, tile);
-            const Channels c = channels_of(a, t, t.n0 + 4 * four);
+            const Tile t = tile_of(plan, a, tile, channels);
+            const Channels c = channels_of(a, t, t.n0 + 4 * (a.gated ? lane & 15 : lane));
             constexpr int kOwn = kWide ? NT / 2 : 1;
             float sum[kOwn];
             if (kWide) {
@@ -338,21 +356,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                         bar_arrive(acc_empty + 8 * (turn & 1));
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) hold[(16 * side + i) * kRows + ch] = v[i];
-                results_sync();
-                const int count = min(kStep, t.count - c0);
-                for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < count; i += 8 * per) {
-                    const float4 y4 = reinterpret_cast<const float4 *>(hold + i * kRows)[four];
-                    float y[4] = {y4.x + c.bias[0], y4.y + c.bias[1], y4.z + c.bias[2], y4.w + c.bias[3]};
-                    activate4(y, a.act);
-                    if (a.gated) {
-                        const float4 u = reinterpret_cast<const float4 *>(hold + i * kRows + kHalf)[four];
-                        y[0] *= u.x + c.up_bias[0]; y[1] *= u.y + c.up_bias[1]; y[2] *= u.z + c.up_bias[2]; y[3] *= u.w + c.up_bias[3];
-                    }
-                    store<O>(a, c, t.g, t.row + c0 + i, y);
-                }
-                results_sync();
+                finish<O>(a, t, c, c0, v, hold, ew, side, ch, lane);
             }
             if (!kWide && slices > 0) ++turn;
         }
@@ -370,6 +374,247 @@ done:
     tc_after();
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kCols) : "memory");
+}
+
+// ---- pairs of multiprocessors -------------------------------------------------------------
+// With many rows an expert, a cluster of two blocks has a tile of 256 weights' rows and up to 256 tokens: each block holds its 128 weights' rows and
+// half of the tokens, both read both halves of the tokens, and the first block's thread issues the products of both.  A block's copies are a third
+// fewer for the same products.  Rows by token are put in order by a kernel of their own first: gathered into the ring as above they come at 40 bytes a
+// cycle at best (16384 rows x 2 x 1024 x 4096: 304 us with four gathering warps a block, FIGURE with the rows in order beforehand, FIGURE2 where they are).
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    return there;
+}
+// (An address of at_rank.  What it orders is tensor memory alone, by tcgen05's own fences; a release of what the thread has stored would wait for
+// its results on their way.)
+__device__ __forceinline__ void far_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// A thread's wait for arrivals of both blocks
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    const uint64_t t0 = now_ns();
+    for (int i = 1;; ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if (i % 256 == 0 && (*failed || now_ns() - t0 > kWaitNs)) {
+            *failed = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ void pair_load3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_load4(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_product(uint32_t acc, uint64_t a, uint64_t b, uint32_t how, uint32_t add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(acc),
+                 "l"(a), "l"(b), "r"(how), "r"(add) : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint32_t bar)      // (the barrier at this address in both blocks)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+constexpr int kPair = 256;                 // tokens of a pair's tile
+struct PairShape {
+    static constexpr int kA = kRows * kSlice * 2, kB = kPair / 2 * kSlice * 2, kStage = kA + kB, kHold = kStep * kRows * 4;
+    static constexpr int kStages = (212 * 1024 - kHold) / kStage;
+    static constexpr int kBytes = kStages * kStage + kHold + 1024;
+};
+
+__global__ void __launch_bounds__(384, 1)
+pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertsArgs a)
+{
+    using S = PairShape;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Plan plan;
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed;
+    unsigned char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    float *hold = reinterpret_cast<float *>(ring + S::kStages * S::kStage);
+    const uint32_t ring_addr = smem_addr(ring);
+    const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const uint32_t full0 = at_rank(full, 0), acc_empty0 = at_rank(acc_empty, 0);       // the barriers that the products wait for are the first block's
+
+    if (tid == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(acc_full + 8 * i, 1);
+            bar_init(acc_empty + 8 * i, 2 * 8);
+        }
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(2 * kPair) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    wait_for_stream();
+    if (warp == 3) make_plan(plan, a.expert_start, a.experts, a.rows, kPair);
+    __syncwarp();
+    tc_before();
+    cluster_sync();                        // the other block's barriers are there
+    tc_after();
+    const uint32_t tmem = tmem_at;
+    const int own = a.gated ? kHalf : kRows, channels = 2 * own, slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
+    const int first = (int)blockIdx.x / 2, step = (int)gridDim.x / 2;
+
+    if (warp == 0 && elected()) {
+        // ---- producer: one thread of each block ----
+        int st = 0, round = 0;
+        for (int tile = first; tile < tiles && slices > 0; tile += step) {
+            const Tile t = tile_of(plan, a, tile, channels);
+            const int half = ((t.count + 31) & ~31) / 2, n0 = t.n0 + (int)rank * own, second = n0 + (a.gated ? a.n : kHalf);
+            const int wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
+            for (int ks = 0; ks < slices; ++ks) {
+                if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+                const uint32_t at = ring_addr + st * S::kStage, bar = full0 + 8 * st;
+                if (rank == 0) bar_expect(full + 8 * st, 2 * S::kStage);
+                pair_load4(at, &wmap, ks * kSlice, n0, t.e, wg, bar);
+                pair_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, wg, bar);
+                pair_load3(at + S::kA, &xmap, ks * kSlice, t.row + (int)rank * half, xg, bar);
+                if (++st == S::kStages) st = 0, ++round;
+            }
+        }
+        for (int i = 0; i < S::kStages; ++i) {           // the products' last arrivals, which come from the other block, find this one there
+            if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
+            if (++st == S::kStages) st = 0, ++round;
+        }
+    } else if (warp == 1 && rank == 0 && elected()) {
+        // ---- products of both blocks: one thread ----
+        constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(2 * kRows / 16) << 24);
+        int st = 0, round = 0;
+        uint32_t turn = 0;                              // accumulators filled so far
+        for (int tile = first; tile < tiles && slices > 0; tile += step) {
+            const uint32_t how = kHow | (uint32_t)((tile_of(plan, a, tile, channels).count + 31) / 32 * 4) << 17;
+            const uint32_t buf = turn & 1, acc = tmem + buf * kPair;
+            if (turn >= 2 && !pair_wait(acc_empty + 8 * buf, ((turn >> 1) - 1) & 1, &failed)) goto done;
+            tc_after();
+            for (int ks = 0; ks < slices; ++ks) {
+                if (!pair_wait(full + 8 * st, round & 1, &failed)) goto done;
+                tc_after();
+                const uint64_t w = operand(ring_addr + st * S::kStage), x = operand(ring_addr + st * S::kStage + S::kA);
+#pragma unroll
+                for (int i = 0; i < kSlice / 16; ++i) pair_product(acc, w + 2 * i, x + 2 * i, how, ks > 0 || i > 0);
+                pair_commit(empty + 8 * st);
+                if (++st == S::kStages) st = 0, ++round;
+            }
+            pair_commit(acc_full + 8 * buf);
+            ++turn;
+        }
+    } else if (warp >= 4 && warp < 12) {
+        // ---- results: this block's weights' rows, all tokens ----
+        const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)quarter << 21;
+        uint32_t turn = 0;
+        for (int tile = first; tile < tiles; tile += step) {
+            Tile t = tile_of(plan, a, tile, channels);
+            t.n0 += (int)rank * own;
+            const Channels c = channels_of(a, t, t.n0 + 4 * (a.gated ? lane & 15 : lane));
+            if (slices > 0) {
+                (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
+                tc_after();
+            }
+#pragma unroll 1
+            for (int c0 = 0; c0 < t.count; c0 += kStep) {
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                if (slices > 0 && c0 + 16 * side < t.count) acc_load16(tmem + lanes + (turn & 1) * kPair + c0 + 16 * side, v);
+                if (slices > 0 && c0 + kStep >= t.count) {       // the accumulator is free for the tile after the next
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) far_arrive(acc_empty0 + 8 * (turn & 1));
+                }
+                finish<__nv_bfloat16>(a, t, c, c0, v, hold, ew, side, ch, lane);
+            }
+            if (slices > 0) ++turn;
+        }
+    }
+done:
+    __syncwarp();
+    if (failed) {
+        // copies and products may still be in flight: give them time to end before the memory is let go
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+    __syncwarp();
+    tc_before();
+    cluster_sync();                        // neither block's memory is in use any more
+    tc_after();
+    if (tid == 0 && a.status && failed) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_TIMEOUT);
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(2 * kPair) : "memory");
+}
+
+// Rows of x in the lists' order: sixteen bytes a thread and step; rows of nobody are left out.
+struct GatherArgs {
+    const unsigned char *x;
+    unsigned char       *out;              // [groups][rows][pieces of 16 bytes]
+    const int32_t *expert_start, *row_token;
+    int64_t   x_ld, x_group;               // bytes
+    int       experts, rows, x_rows, groups, k, pieces;
+    unsigned *status;
+};
+constexpr int kGatherThreads = 256;
+
+__global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ GatherArgs a)
+{
+    wait_for_stream();
+    const int lane = threadIdx.x & 31;
+    int count = 0;                         // rows of somebody (see make_plan)
+    for (int e = lane; e <= a.experts; e += 32) count = max(count, a.expert_start[e]);
+    count = min(__reduce_max_sync(0xffffffffu, count), a.rows);
+    const int warps = kGatherThreads / 32 * (int)gridDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * (kGatherThreads / 32) + (threadIdx.x >> 5); i < (int64_t)a.groups * a.rows; i += warps) {
+        const int g = (int)(i / a.rows), row = (int)(i - (int64_t)g * a.rows);
+        if (row >= count) continue;
+        const int token = a.row_token[row];
+        const bool there = token >= 0 && token < a.x_rows;
+        if (!there && lane == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_INVAL);
+        const unsigned char *x = a.x + g * a.x_group + (there ? token : 0) * a.x_ld;
+        uint4 *out = reinterpret_cast<uint4 *>(a.out) + i * a.pieces;
+        const int whole = a.k / 8;
+        for (int c0 = 0; c0 < whole; c0 += 4 * 32) {
+            uint4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c0 + 32 * j + lane < whole) v[j] = *reinterpret_cast<const uint4 *>(x + 16ll * (c0 + 32 * j + lane));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c0 + 32 * j + lane < whole) out[c0 + 32 * j + lane] = there ? v[j] : make_uint4(0, 0, 0, 0);
+        }
+        for (int c = 8 * whole + lane; c < a.k; c += 32)
+            reinterpret_cast<uint16_t *>(out)[c] = there ? reinterpret_cast<const uint16_t *>(x)[c] : 0;
+    }
 }
 
 // ---- host ---------------------------------------------------------------------------------
@@ -412,10 +657,52 @@ int launch_as(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &
     return a.row_token ? launch<NT, kWide, true>(a, wmap, xmap, d, s) : launch<NT, kWide, false>(a, wmap, xmap, d, s);
 }
 
+int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)
+{
+    a.n_tiles = (a.n_tiles + 1) / 2;       // of both blocks' channels
+    const int64_t used = a.experts < a.rows ? a.experts : a.rows, tiles = (int64_t)a.groups * a.n_tiles * (a.rows / kPair + used);      // at most
+    if (tiles > kMost || (int64_t)a.n_tiles * kBand > kMost) return SYMAR_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_shared((const void *)pair_kernel, PairShape::kBytes, d.id, allowed);
+    if (e != cudaSuccess) return cuda_fail(e, "symar_experts");
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim  = dim3((unsigned)(2 * (tiles < d.sms / 2 ? tiles : d.sms / 2)));
+    cfg.blockDim = dim3(384);
+    cfg.dynamicSmemBytes = PairShape::kBytes;
+    cfg.stream   = stream;
+    cfg.attrs    = attr;
+    cfg.numAttrs = 2;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // (see wait_for_stream)
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    e = cudaLaunchKernelEx(&cfg, pair_kernel, wmap, xmap, a);
+    return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
+}
+
+// Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
+int tile_tokens(const symar_experts_t &p)
+{
+    const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = used > 0 ? p.rows / used : 0;
+    return each <= 32 ? 64 : (each <= 96 || p.out_dtype == SYMAR_F32 ? 128 : kPair);
+}
+bool in_order_first(const symar_experts_t &p) { return p.row_token && p.k > 0 && tile_tokens(p) == kPair; }
+int64_t pieces_of(int k) { return ((int64_t)k + 7) / 8; }
+
 }  // namespace
 }  // namespace symar
 
 using namespace symar;
+
+extern "C" size_t symar_experts_workspace(const symar_experts_t *p)
+{
+    if (!p || p->groups <= 0 || p->experts <= 0 || p->rows <= 0 || p->n <= 0 || p->k <= 0 || !in_order_first(*p)) return 0;
+    const int64_t groups = p->groups > 1 && p->x_group != 0 ? p->groups : 1;
+    const __int128 bytes = (__int128)groups * p->rows * pieces_of(p->k) * 16;
+    return bytes < ((__int128)1 << 62) ? (size_t)bytes : (size_t)1 << 62;
+}
 
 extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
 {
@@ -453,25 +740,40 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
     a.vec_out = (uintptr_t)p.out % (4 * width) == 0 && p.out_ld % 4 == 0 && p.out_group % 4 == 0 && p.n % 4 == 0;
     a.status = p.status;
     CUtensorMap wmap{}, xmap{};
-    // Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
-    const bool wide = p.out_dtype == SYMAR_F32;
-    const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = p.rows / used;
-    const int nt = each <= 32 ? 64 : (each <= 96 || wide ? 128 : 256);
+    const bool wide = p.out_dtype == SYMAR_F32, first = in_order_first(p);
+    const int nt = tile_tokens(p);
+    GatherArgs ga{};
     if (p.k > 0) {
         const int64_t w_rows = (int64_t)p.n * (p.gated ? 2 : 1);
         const int64_t w_extent[4] = {p.k, w_rows, p.experts, a.w_shared ? 1 : p.groups}, w_stride[4] = {1, p.w_ld, p.w_expert, p.w_group};
-        const int64_t x_extent[3] = {p.k, p.x_rows, a.x_shared ? 1 : p.groups}, x_stride[3] = {1, p.x_ld, p.x_group};
+        int64_t x_extent[3] = {p.k, p.x_rows, a.x_shared ? 1 : p.groups}, x_stride[3] = {1, p.x_ld, p.x_group};
         bool ok = encoder() && ((uintptr_t)p.x | (uintptr_t)p.w) % 16 == 0;
         for (int i = 1; i < 4; ++i) ok = ok && engine_axis(w_extent[i], w_stride[i]);
         for (int i = 1; i < 3; ++i) ok = ok && engine_axis(x_extent[i], x_stride[i]);
         if (!ok) return SYMAR_ERR_UNSUPPORTED;
-        if (!p.row_token) ok = encode(&xmap, p.x, 3, x_extent, x_stride, nt);
+        const void *x = p.x;
+        if (first) {
+            const size_t need = symar_experts_workspace(&p);
+            if (!p.workspace || (uintptr_t)p.workspace % 16) return SYMAR_ERR_INVAL;
+            if (p.workspace_bytes < need) return SYMAR_ERR_NOMEM;
+            ga = GatherArgs{(const unsigned char *)p.x, (unsigned char *)p.workspace, p.expert_start, p.row_token, 2 * p.x_ld, 2 * p.x_group, p.experts, p.rows,
+                            p.x_rows, (int)x_extent[2], p.k, (int)pieces_of(p.k), p.status};
+            x = p.workspace;
+            x_extent[1] = p.rows, x_stride[1] = 8 * pieces_of(p.k), x_stride[2] = x_stride[1] * p.rows;
+            ok = x_stride[2] < (1ll << 39);
+        }
+        if (ok && (!p.row_token || first)) ok = encode(&xmap, x, 3, x_extent, x_stride, nt < kPair ? nt : kPair / 2);
         if (!ok || !encode(&wmap, p.w, 4, w_extent, w_stride, kHalf)) return SYMAR_ERR_UNSUPPORTED;
     }
     int rc = device_info(&d);
     if (rc == SYMAR_OK) rc = clear();
     if (rc != SYMAR_OK) return rc;
     if (nt == 64) return wide ? launch_as<64, true>(a, wmap, xmap, d, s) : launch_as<64, false>(a, wmap, xmap, d, s);
-    if (wide) return launch_as<128, true>(a, wmap, xmap, d, s);
-    return nt == 128 ? launch_as<128, false>(a, wmap, xmap, d, s) : launch_as<256, false>(a, wmap, xmap, d, s);
+    if (nt == 128) return wide ? launch_as<128, true>(a, wmap, xmap, d, s) : launch_as<128, false>(a, wmap, xmap, d, s);
+    if (first) {
+        const int64_t blocks = ((int64_t)ga.groups * ga.rows + kGatherThreads / 32 - 1) / (kGatherThreads / 32), most = 8ll * d.sms;
+        const cudaError_t e = launch_early(gather_kernel, dim3((unsigned)(blocks < most ? blocks : most)), kGatherThreads, 0, s, ga);
+        if (e != cudaSuccess) return cuda_fail(e, "symar_experts");
+    }
+    return launch_pair(a, wmap, xmap, d, s);
 }

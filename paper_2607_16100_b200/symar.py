@@ -98,6 +98,7 @@ SIGNATURES = [
     ("symar_norm", c_int, [c_void_p, c_void_p]),
     ("symar_route_workspace", c_size_t, [c_int, c_int]),
     ("symar_route", c_int, [c_void_p, c_void_p]),
+    ("symar_experts_workspace", c_size_t, [c_void_p]),
     ("symar_experts", c_int, [c_void_p, c_void_p]),
     ("symar_combine", c_int, [c_void_p, c_void_p]),
     ("symar_probe_pingpong_blocks", c_int, [c_int, c_int, c_int, c_int, POINTER(c_double), POINTER(c_int)]),
@@ -498,7 +499,7 @@ class ExpertsArgs(ctypes.Structure):
         ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
         ("expert_start", c_void_p), ("row_token", c_void_p),
         ("groups", c_int32), ("experts", c_int32), ("rows", c_int32), ("x_rows", c_int32), ("n", c_int32), ("k", c_int32),
-        ("out_dtype", c_int32), ("act", c_int32), ("gated", c_int32), ("status", c_void_p),
+        ("out_dtype", c_int32), ("act", c_int32), ("gated", c_int32), ("status", c_void_p), ("workspace", c_void_p), ("workspace_bytes", c_size_t),
     ]
 
 
@@ -1027,7 +1028,13 @@ def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool =
     args = ExpertsArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
                        out.data_ptr(), os[-2], os[0] if ranked else 0, routes.expert_start.data_ptr(), None if by_row else routes.row_token.data_ptr(),
                        groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
-    _call((_lib or load()).symar_experts, where, index, stream, byref(args))
+    lib = _lib or load()
+    if not by_row:
+        need = lib.symar_experts_workspace(byref(args))
+        if need:
+            room = _new(x, (need,), torch.uint8, index, stream)
+            args.workspace, args.workspace_bytes = room.data_ptr(), need
+    _call(lib.symar_experts, where, index, stream, byref(args))
     return out
 
 
