@@ -4,8 +4,12 @@
 // A row is read once, held in registers as binary32 through both norms and written once.  Sums go over a thread's own elements,
 // then over the row's threads by shuffles and, where they are several warps, by shared memory; a layer norm takes the mean first
 // and the squares of what is left after it, so that a large mean costs no digits.
+#include <type_traits>
+
 #include "symar_eights.cuh"
+#include "symar_maps.h"
 #include "symar_ops.h"
+#include "symar_tc.cuh"
 
 namespace symar {
 namespace {
@@ -25,153 +29,419 @@ struct NormArgs {
     int     x_wide, stream_wide, gate_step, gate_act;
 };
 
-// Where the eight elements of a thread's chunk c begin; on no 16-byte boundary they are T apart.
-template <int T, bool kVec> __device__ __forceinline__ int first(int c, int i) { return kVec ? (c * T + i) * 8 : c * 8 * T + i; }
+// A row's share of one thread: C chunks of eight elements.  Where chunk c begins; in rows on no 16-byte boundary its elements are T apart.
+template <bool kVec> __device__ __forceinline__ int first(int c, int i, int T) { return kVec ? (c * T + i) * 8 : c * 8 * T + i; }
+template <bool kVec> __device__ __forceinline__ bool inside(int c, int j, int i, int T, int n) { return first<kVec>(c, i, T) + (kVec ? j : j * T) < n; }
 
-// Sum over a row's T threads, the same on every one of them; `room` is not in use by an earlier sum any more.
-template <int T>
-__device__ __forceinline__ float row_sum(float s, float *room)
+__device__ __forceinline__ float lanes_sum(float s, int lanes)
 {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (T == 32) return s;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) room[warp] = s;
-    __syncthreads();
-    s = lane < T / 32 ? room[lane] : 0.0f;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    for (int d = 16; d > 0; d >>= 1)
+        if (d < lanes) s += __shfl_xor_sync(0xffffffffu, s, d);
     return s;
 }
+// Sums over a row's threads, the same on every one of them: L lanes of a warp, or T threads (whole warps) that meet at a barrier.  No two sums of a row
+// use the same room.
+template <int L> struct LanesSum {
+    __device__ __forceinline__ float operator()(float s, int) const { return lanes_sum(s, L); }
+};
+struct ThreadsSum {
+    float *room;                           // [4][32]
+    int    warps, warp, barrier;
+    __device__ __forceinline__ float operator()(float s, int which) const
+    {
+        s = lanes_sum(s, 32);
+        if (warps == 1) return s;
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) room[32 * which + warp] = s;
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+        return lanes_sum(lane < warps ? room[32 * which + lane] : 0.0f, 32);
+    }
+};
 
-template <int T, int C, bool kVec>
-__device__ __forceinline__ void norm_row(float (&v)[C][8], const Side &s, const Raw &w0, const Raw &b0, int i, int n, float inv_n, float *room)
+// A side's weights and biases of chunk c as a kernel has them at hand: read for this row (kRead: already), or held as floats for all rows, where biases,
+// which few norms have, are read again.
+template <int C, bool kVec, bool kRead> struct ReadVectors {
+    Raw w[2][kRead ? C : 1], b[2][kRead ? C : 1];
+    int i, T;
+    __device__ __forceinline__ void read(const Side &s, int side, int n)
+    {
+        if (!kRead) return;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (s.weight) w[side][c] = read8<kVec>(s.weight, s.wide, first<kVec>(c, i, T), T, n);
+            if (s.bias) b[side][c] = read8<kVec>(s.bias, s.wide, first<kVec>(c, i, T), T, n);
+        }
+    }
+    __device__ __forceinline__ void weight(const Side &s, int side, int c, int n, float (&f)[8]) const
+    {
+        values<kVec>(kRead ? w[side][kRead ? c : 0] : read8<kVec>(s.weight, s.wide, first<kVec>(c, i, T), T, n), s.wide, f);
+        const float plus = s.plus_one ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] += plus;
+    }
+    __device__ __forceinline__ void bias(const Side &s, int side, int c, int n, float (&f)[8]) const
+    {
+        values<kVec>(kRead ? b[side][kRead ? c : 0] : read8<kVec>(s.bias, s.wide, first<kVec>(c, i, T), T, n), s.wide, f);
+    }
+};
+template <int C, bool kVec> struct HeldVectors {
+    float w[2][C][8];
+    int   i, T;
+    __device__ __forceinline__ void hold(const Side &s, int side, int n)
+    {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (!s.weight) continue;
+            values<kVec>(read8<kVec>(s.weight, s.wide, first<kVec>(c, i, T), T, n), s.wide, w[side][c]);
+            const float plus = s.plus_one ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[side][c][j] += plus;
+        }
+    }
+    __device__ __forceinline__ void weight(const Side &, int side, int c, int, float (&f)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = w[side][c][j];
+    }
+    __device__ __forceinline__ void bias(const Side &s, int, int c, int n, float (&f)[8]) const
+    {
+        values<kVec>(read8<kVec>(s.bias, s.wide, first<kVec>(c, i, T), T, n), s.wide, f);
+    }
+};
+
+template <int C, bool kVec, typename Vectors, typename Sum>
+__device__ __forceinline__ void norm_row(float (&v)[C][8], const Side &s, int side, const Vectors &vectors, int i, int T, int n, float inv_n, const Sum &sum)
 {
     if (s.kind == SYMAR_NORM_LAYER) {
-        float sum = 0.0f;
+        float all = 0.0f;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[c][j];                       // (elements beyond the row are zeros)
-        const float mean = row_sum<T>(sum, room) * inv_n;
-        room += 32;
+            for (int j = 0; j < 8; ++j) all += v[c][j];                       // (elements beyond the row are zeros)
+        const float mean = sum(all, 2 * side + 1) * inv_n;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = first<T, kVec>(c, i) + (kVec ? j : j * T) < n ? v[c][j] - mean : 0.0f;
+            for (int j = 0; j < 8; ++j) v[c][j] = inside<kVec>(c, j, i, T, n) ? v[c][j] - mean : 0.0f;
     }
-    float sum = 0.0f;
+    float all = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fmaf(v[c][j], v[c][j], sum);
-    const float by = 1.0f / sqrtf(fmaf(row_sum<T>(sum, room), inv_n, s.eps));
+        for (int j = 0; j < 8; ++j) all = fmaf(v[c][j], v[c][j], all);
+    const float by = 1.0f / sqrtf(fmaf(sum(all, 2 * side), inv_n, s.eps));
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[c][j] *= by;
         if (s.weight) {
             float w[8];
-            values<kVec>(C == 1 ? w0 : read8<kVec>(s.weight, s.wide, first<T, kVec>(c, i), T, n), s.wide, w);
+            vectors.weight(s, side, c, n, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] *= s.plus_one ? 1.0f + w[j] : w[j];
+            for (int j = 0; j < 8; ++j) v[c][j] *= w[j];
         }
         if (s.bias) {
             float b[8];
-            values<kVec>(C == 1 ? b0 : read8<kVec>(s.bias, s.wide, first<T, kVec>(c, i), T, n), s.wide, b);
+            vectors.bias(s, side, c, n, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] += b[j];
         }
     }
 }
-__device__ __forceinline__ float opened(float g, int act)
+__device__ __forceinline__ void open8(float (&g)[8], int act)
 {
-    if (act == SYMAR_GATE_SIGMOID) return 1.0f / (1.0f + expf(-g));
-    return act == SYMAR_GATE_TANH ? tanhf(g) : g;
+    if (act == SYMAR_GATE_SIGMOID) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = 1.0f / (1.0f + expf(-g[j]));
+    } else if (act == SYMAR_GATE_TANH) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = tanhf(g[j]);
+    }
 }
-
-constexpr int kSmall = 8;                  // rows of a block where a warp has one
-
-template <int T, int C, bool kVec>
-__global__ void __launch_bounds__(T == 32 ? 32 * kSmall : T) norm_kernel(const __grid_constant__ NormArgs a)
+template <typename P> __device__ __forceinline__ P *moved(P *p, int64_t elements, bool wide)
 {
-    __shared__ float room[4 * 32];         // two sums of each norm
-    wait_for_stream();
-    const int row = T == 32 ? (int)blockIdx.x * kSmall + (int)(threadIdx.x >> 5) : (int)blockIdx.x;
-    if (row >= a.rows) return;             // (a whole warp)
-    const int i = T == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, g = row / a.m, t = row - g * a.m, n = a.n;
-    const float inv_n = 1.0f / (float)n;
-    const char *x = static_cast<const char *>(a.x) + (g * a.x_group + t * a.x_ld) * (a.x_wide ? 4 : 2);
-    const char *res = static_cast<const char *>(a.residual) + (g * a.residual_group + t * a.residual_ld) * (a.stream_wide ? 4 : 2);
-
-    Raw in[C], old[C], none{}, wa = none, ba = none, wb = none, bb = none;
-#pragma unroll
-    for (int c = 0; c < C; ++c) in[c] = read8<kVec>(x, a.x_wide, first<T, kVec>(c, i), T, n);
-    if (a.residual) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) old[c] = read8<kVec>(res, a.stream_wide, first<T, kVec>(c, i), T, n);
-    }
-    if (C == 1) {                          // few rows: everything is asked for at once
-        if (a.after.weight) wa = read8<kVec>(a.after.weight, a.after.wide, first<T, kVec>(0, i), T, n);
-        if (a.after.bias) ba = read8<kVec>(a.after.bias, a.after.wide, first<T, kVec>(0, i), T, n);
-        if (a.before.weight) wb = read8<kVec>(a.before.weight, a.before.wide, first<T, kVec>(0, i), T, n);
-        if (a.before.bias) bb = read8<kVec>(a.before.bias, a.before.wide, first<T, kVec>(0, i), T, n);
-    }
+    return (P *)((char *)p + elements * (wide ? 4 : 2));
+}
+// A row's gate where it is one number, times the scale
+__device__ __forceinline__ float row_gate(const NormArgs &a, int g, int t)
+{
+    if (!a.gate || a.gate_step) return a.scale;
+    const void *p = moved(a.gate, g * a.gate_group + t * a.gate_ld, a.x_wide);
+    float v = a.x_wide ? *static_cast<const float *>(p) : __bfloat162float(*static_cast<const __nv_bfloat16 *>(p));
+    if (a.gate_act == SYMAR_GATE_SIGMOID) v = 1.0f / (1.0f + expf(-v));
+    else if (a.gate_act == SYMAR_GATE_TANH) v = tanhf(v);
+    return a.scale * v;
+}
+struct Gate {
+    const void *p;                         // a row's channels, where there is a gate for each
+    bool        wide;
+    int         act;
+    float       scale;
+};
+// One row from what in(c), old(c) give of x and residual to what is stored where it is to be kept.  `by`: row_gate(), of gates that are one number.
+// kX, kStream: x and the stream are float32.
+template <int C, bool kVec, bool kX, bool kStream, typename Vectors, typename Sum, typename In, typename Old>
+__device__ __forceinline__ void do_row(const NormArgs &a, const In &in, const Old &old, const Vectors &vectors, const Gate &gate, float by, int g, int t, bool keep,
+                                       int i, int T, float inv_n, const Sum &sum)
+{
+    const int n = a.n;
     float v[C][8];
 #pragma unroll
-    for (int c = 0; c < C; ++c) values<kVec>(in[c], a.x_wide, v[c]);
-    if (a.after.kind != SYMAR_NORM_NONE) norm_row<T, C, kVec>(v, a.after, wa, ba, i, n, inv_n, room);
-    if (a.gate) {
-        const char *gate = static_cast<const char *>(a.gate) + (g * a.gate_group + t * a.gate_ld) * (a.x_wide ? 4 : 2);
-        if (a.gate_step == 0) {
-            const float by = a.scale * opened(a.x_wide ? *reinterpret_cast<const float *>(gate)
-                                                       : __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(gate)), a.gate_act);
+    for (int c = 0; c < C; ++c) values<kVec>(in(c), kX, v[c]);
+    if (a.after.kind != SYMAR_NORM_NONE) norm_row<C, kVec>(v, a.after, 0, vectors, i, T, n, inv_n, sum);
+    if (a.gate && a.gate_step) {
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+            float w[8];
+            values<kVec>(read8<kVec>(gate.p, gate.wide, first<kVec>(c, i, T), T, n), gate.wide, w);
+            open8(w, gate.act);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] *= by;
-        } else {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float w[8];
-                values<kVec>(read8<kVec>(gate, a.x_wide, first<T, kVec>(c, i), T, n), a.x_wide, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] *= a.scale * opened(w[j], a.gate_act);
-            }
+            for (int j = 0; j < 8; ++j) v[c][j] *= gate.scale * w[j];
         }
     } else {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] *= a.scale;
+            for (int j = 0; j < 8; ++j) v[c][j] *= by;
     }
     if (a.residual) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             float h[8];
-            values<kVec>(old[c], a.stream_wide, h);
+            values<kVec>(old(c), kStream, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] = fmaf(a.residual_scale, h[j], v[c][j]);
         }
     }
-    if (a.residual_out) {
-        char *to = static_cast<char *>(a.residual_out) + (g * a.residual_out_group + t * a.residual_out_ld) * (a.stream_wide ? 4 : 2);
+    if (a.residual_out && keep) {
+        void *to = moved(a.residual_out, g * a.residual_out_group + t * a.residual_out_ld, kStream);
 #pragma unroll
-        for (int c = 0; c < C; ++c) write8<kVec>(to, a.stream_wide, first<T, kVec>(c, i), T, n, v[c]);
+        for (int c = 0; c < C; ++c) write8<kVec>(to, kStream, first<kVec>(c, i, T), T, n, v[c]);
     }
     if (a.out) {
-        norm_row<T, C, kVec>(v, a.before, wb, bb, i, n, inv_n, room + 64);
-        char *to = static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (a.x_wide ? 4 : 2);
+        norm_row<C, kVec>(v, a.before, 1, vectors, i, T, n, inv_n, sum);
+        if (!keep) return;
+        void *to = moved(a.out, g * a.out_group + t * a.out_ld, kX);
 #pragma unroll
-        for (int c = 0; c < C; ++c) write8<kVec>(to, a.x_wide, first<T, kVec>(c, i), T, n, v[c]);
+        for (int c = 0; c < C; ++c) write8<kVec>(to, kX, first<kVec>(c, i, T), T, n, v[c]);
     }
 }
 
-template <int T, int C>
-cudaError_t launch(const NormArgs &a, bool vec, cudaStream_t s)
+// ---- a block has a row: few rows, and long ones on no boundary ----
+template <int C, bool kVec, bool kX, bool kStream>
+__global__ void __launch_bounds__(1024) row_kernel(const __grid_constant__ NormArgs a)
 {
-    const unsigned blocks = T == 32 ? ((unsigned)a.rows + kSmall - 1) / kSmall : (unsigned)a.rows, threads = T == 32 ? 32 * kSmall : T;
-    return vec ? launch_early(norm_kernel<T, C, true>, dim3(blocks), threads, 0, s, a) : launch_early(norm_kernel<T, C, false>, dim3(blocks), threads, 0, s, a);
+    __shared__ float room[4 * 32];
+    wait_for_stream();
+    const int T = blockDim.x, i = threadIdx.x, row = blockIdx.x, g = row / a.m, t = row - g * a.m;
+    const void *x = moved(a.x, g * a.x_group + t * a.x_ld, kX);
+    Raw in[C], old[C] = {};
+#pragma unroll
+    for (int c = 0; c < C; ++c) in[c] = read8<kVec>(x, kX, first<kVec>(c, i, T), T, a.n);
+    if (a.residual) {
+        const void *h = moved(a.residual, g * a.residual_group + t * a.residual_ld, kStream);
+#pragma unroll
+        for (int c = 0; c < C; ++c) old[c] = read8<kVec>(h, kStream, first<kVec>(c, i, T), T, a.n);
+    }
+    ReadVectors<C, kVec, C == 1> vectors;  // (one trip to memory where registers allow it)
+    vectors.i = i, vectors.T = T;
+    vectors.read(a.after, 0, a.n), vectors.read(a.before, 1, a.n);
+    const float by = row_gate(a, g, t);
+    do_row<C, kVec, kX, kStream>(a, [&](int c) { return in[c]; }, [&](int c) { return old[c]; }, vectors,
+                                 Gate{moved(a.gate, g * a.gate_group + t * a.gate_ld, kX), kX, a.gate_act, a.scale}, by, g, t, true, i, T, 1.0f / (float)a.n, ThreadsSum{room, T / 32, i >> 5, 0});
+}
+
+// ---- L lanes of a warp have a row: short rows, U of them asked for before the first is computed ----
+constexpr int kShortThreads = 256;
+
+template <int L, int C, int U, bool kVec, bool kX, bool kStream>
+__global__ void __launch_bounds__(kShortThreads) short_kernel(const __grid_constant__ NormArgs a)
+{
+    wait_for_stream();
+    const int i = (int)threadIdx.x % L, slot = (int)(blockIdx.x * kShortThreads + threadIdx.x) / L, slots = (int)gridDim.x * (kShortThreads / L);
+    const float inv_n = 1.0f / (float)a.n;
+    typename std::conditional<C == 1, HeldVectors<C, kVec>, ReadVectors<C, kVec, false>>::type vectors;
+    vectors.i = i, vectors.T = L;
+    if constexpr (C == 1) vectors.hold(a.after, 0, a.n), vectors.hold(a.before, 1, a.n);
+    for (int64_t row0 = (int64_t)(slot / (32 / L)) * (32 / L) * U; row0 < a.rows; row0 += (int64_t)slots * U) {      // (whole warps go on together)
+        Raw in[U][C], old[U][C] = {};
+        int g[U], t[U];
+        float by[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (rows behind the last read the last one's and are not stored)
+            const int row = (int)min(row0 + u * (32 / L) + slot % (32 / L), (int64_t)a.rows - 1);
+            g[u] = row / a.m, t[u] = row - g[u] * a.m;
+            const void *x = moved(a.x, g[u] * a.x_group + t[u] * a.x_ld, kX);
+#pragma unroll
+            for (int c = 0; c < C; ++c) in[u][c] = read8<kVec>(x, kX, first<kVec>(c, i, L), L, a.n);
+            if (a.residual) {
+                const void *h = moved(a.residual, g[u] * a.residual_group + t[u] * a.residual_ld, kStream);
+#pragma unroll
+                for (int c = 0; c < C; ++c) old[u][c] = read8<kVec>(h, kStream, first<kVec>(c, i, L), L, a.n);
+            }
+            by[u] = row_gate(a, g[u], t[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            do_row<C, kVec, kX, kStream>(a, [&](int c) { return in[u][c]; }, [&](int c) { return old[u][c]; }, vectors,
+                                         Gate{moved(a.gate, g[u] * a.gate_group + t[u] * a.gate_ld, kX), kX, a.gate_act, a.scale}, by[u], g[u], t[u],
+                                         row0 + u * (32 / L) + slot % (32 / L) < a.rows, i, L, inv_n, LanesSum<L>{});
+    }
+}
+
+// ---- many long rows: a block for each multiprocessor, whose groups of threads have a row each; the copy engine brings a group's next rows into its
+// slots of shared memory meanwhile, so that reading never waits for the sums.  Weights and gates that all rows share lie in shared memory too. ----
+struct Ring {
+    int T, groups, slots;                  // threads of a group; groups; a group's slots
+    int x_bytes, old_bytes, gate_bytes;    // of a row in a slot: x, residual, gate (0: not in it)
+    int held;                              // bytes of what all rows share (0: read from memory)
+};
+constexpr int kRingThreads = 1024, kRingRoom = 208 * 1024, kMaxSlots = 8, kMaxGroups = 15, kRingMost = 16 * kRingThreads;
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+template <bool kX, bool kStream>
+__global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_constant__ NormArgs args, const __grid_constant__ Ring ring)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ __align__(8) uint64_t bars[kMaxGroups * kMaxSlots];
+    __shared__ float room[kMaxGroups * 2 * 4 * 32];            // a row's four sums, of every second row
+    __shared__ int failed;
+    NormArgs a = args;
+    const int T = ring.T, group = (int)threadIdx.x / T, i = (int)threadIdx.x - group * T, n = a.n;
+    if (threadIdx.x == 0) {
+        for (int b = 0; b < ring.groups * ring.slots; ++b) bar_init(smem_addr(bars + b), 1);
+        failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    wait_for_stream();
+    int at = 0;
+    auto hold = [&](const void *&p, bool wide) {
+        if (!p) return;
+        const int bytes = n * (wide ? 4 : 2);
+        for (int b = 16 * (int)threadIdx.x; b < bytes; b += 16 * (int)blockDim.x)
+            *reinterpret_cast<uint4 *>(smem + at + b) = *reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + b);
+        p = smem + at;
+        at += bytes;
+    };
+    Gate gate{a.gate, kX, a.gate_act, a.scale};
+    if (ring.held) {
+        hold(a.after.weight, a.after.wide), hold(a.after.bias, a.after.wide);
+        hold(a.before.weight, a.before.wide), hold(a.before.bias, a.before.wide);
+        if (a.gate && a.gate_step && !ring.gate_bytes) {       // with its function and the scale
+            float *to = reinterpret_cast<float *>(smem + at);
+            for (int c = 8 * (int)threadIdx.x; c < n; c += 8 * (int)blockDim.x) {
+                float f[8];
+                values<true>(read8<true>(a.gate, kX, c, 0, n), kX, f);
+                open8(f, a.gate_act);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] *= a.scale;
+                write8<true>(to, true, c, 0, n, f);
+            }
+            gate = Gate{to, true, SYMAR_GATE_NONE, 1.0f};
+        }
+    }
+    __syncthreads();
+    const int slot_bytes = ring.x_bytes + ring.old_bytes + ring.gate_bytes, step = (int)gridDim.x * ring.groups;
+    unsigned char *slots = smem + ring.held + (int64_t)group * ring.slots * slot_bytes;
+    const uint32_t bar0 = smem_addr(bars + group * ring.slots);
+    const float inv_n = 1.0f / (float)n;
+    auto ask = [&](int64_t row, int s) {   // (by one thread)
+        if (row >= a.rows) return;
+        const int g = (int)row / a.m, t = (int)row - g * a.m;
+        const uint32_t to = smem_addr(slots + s * slot_bytes), bar = bar0 + 8 * s;
+        bar_expect(bar, (uint32_t)slot_bytes);
+        bulk_load(to, moved(a.x, g * a.x_group + t * a.x_ld, kX), ring.x_bytes, bar);
+        if (ring.old_bytes) bulk_load(to + ring.x_bytes, moved(a.residual, g * a.residual_group + t * a.residual_ld, kStream), ring.old_bytes, bar);
+        if (ring.gate_bytes) bulk_load(to + ring.x_bytes + ring.old_bytes, moved(a.gate, g * a.gate_group + t * a.gate_ld, kX), ring.gate_bytes, bar);
+    };
+    int64_t row = (int64_t)blockIdx.x * ring.groups + group;
+    if (i == 0)
+        for (int s = 0; s < ring.slots; ++s) ask(row + (int64_t)s * step, s);
+    ReadVectors<2, true, false> vectors;
+    vectors.i = i, vectors.T = T;
+    auto gate_of = [&](int64_t r) { return r < a.rows ? row_gate(a, (int)r / a.m, (int)r % a.m) : 0.0f; };
+    float by = gate_of(row);
+    uint32_t turn = 0;
+    for (int s = 0, round = 0; row < a.rows; row += step, ++turn) {
+        const float next = gate_of(row + step);
+        const int g = (int)row / a.m, t = (int)row - g * a.m;
+        (void)warp_wait(bar0 + 8 * s, round & 1, &failed);     // (given up: on with what is there, the barriers count all)
+        const unsigned char *x = slots + s * slot_bytes, *h = x + ring.x_bytes;
+        do_row<2, true, kX, kStream>(a, [&](int c) { return read8<true>(x, kX, first<true>(c, i, T), T, n); },
+                                     [&](int c) { return read8<true>(h, kStream, first<true>(c, i, T), T, n); }, vectors,
+                                     ring.gate_bytes ? Gate{h + ring.old_bytes, kX, a.gate_act, a.scale} : gate, by, g, t, true, i, T, inv_n,
+                                     ThreadsSum{room + (group * 2 + (turn & 1)) * 4 * 32, T / 32, i >> 5, 1 + group});
+        // all of the slot has been read before the last sum, where there is one behind it
+        if (a.before.kind == SYMAR_NORM_NONE) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(T) : "memory");
+        if (i == 0) ask(row + (int64_t)ring.slots * step, s);
+        if (++s == ring.slots) s = 0, ++round;
+        by = next;
+    }
+}
+
+// How the ring divides shared memory; no group fits: T is 0.
+Ring ring_of(const NormArgs &a)
+{
+    Ring r{};
+    const int xw = a.x_wide ? 4 : 2;
+    r.x_bytes = a.n * xw;
+    r.old_bytes = a.residual ? a.n * (a.stream_wide ? 4 : 2) : 0;
+    r.gate_bytes = a.gate && a.gate_step && (a.gate_ld != 0 || a.gate_group != 0) ? a.n * xw : 0;
+    for (const Side *s : {&a.after, &a.before}) r.held += ((s->weight != nullptr) + (s->bias != nullptr)) * a.n * (s->wide ? 4 : 2);
+    if (a.gate && a.gate_step && !r.gate_bytes) r.held += a.n * 4;
+    if (r.held > 96 * 1024) r.held = 0;
+    const int threads = ((a.n + 15) / 16 + 31) / 32 * 32;  // sixteen elements each
+    for (int groups = kRingThreads / threads < kMaxGroups ? kRingThreads / threads : kMaxGroups; groups > 0; --groups) {
+        const int slots = (kRingRoom - r.held) / (groups * (r.x_bytes + r.old_bytes + r.gate_bytes));
+        if (slots < 2) continue;
+        r.T = threads, r.groups = groups, r.slots = slots < kMaxSlots ? slots : kMaxSlots;
+        break;
+    }
+    return r;
+}
+template <int L, int C, int U, bool kVec, bool kX, bool kStream>
+cudaError_t launch_short(const NormArgs &a, const Device &d, cudaStream_t s)
+{
+    const int64_t blocks = ((int64_t)a.rows * L + kShortThreads * U - 1) / (kShortThreads * U), most = 8ll * d.sms;
+    return launch_early(short_kernel<L, C, U, kVec, kX, kStream>, dim3((unsigned)(blocks < most ? blocks : most)), kShortThreads, 0, s, a);
+}
+template <bool kVec, bool kX, bool kStream>
+cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
+{
+    const bool many = a.rows > 4 * d.sms;
+    if (many && a.n <= 1024) {
+        if constexpr (kVec) {
+            if (a.n <= 64) return launch_short<8, 1, 4, true, kX, kStream>(a, d, s);
+            if (a.n <= 128) return launch_short<16, 1, 4, true, kX, kStream>(a, d, s);
+            if (a.n <= 256) return launch_short<32, 1, 4, true, kX, kStream>(a, d, s);
+        }
+        return launch_short<32, 4, 1, kVec, kX, kStream>(a, d, s);
+    }
+    if (kVec && many && a.n <= kRingMost && (a.after.kind != SYMAR_NORM_NONE || a.before.kind != SYMAR_NORM_NONE)) {
+        const Ring r = ring_of(a);
+        if (r.T) {
+            const int bytes = r.held + r.groups * r.slots * (r.x_bytes + r.old_bytes + r.gate_bytes);
+            static std::atomic<uint64_t> allowed{0};
+            const cudaError_t e = allow_shared((const void *)ring_kernel<kX, kStream>, kRingRoom, d.id, allowed);
+            return e != cudaSuccess ? e : launch_early(ring_kernel<kX, kStream>, dim3((unsigned)d.sms), (unsigned)(r.T * r.groups), (size_t)bytes, s, a, r);
+        }
+    }
+    const int chunks = a.n <= 8192 ? 1 : 4;
+    const unsigned threads = (unsigned)(((a.n + 8 * chunks - 1) / (8 * chunks) + 31) / 32 * 32);
+    return chunks == 1 ? launch_early(row_kernel<1, kVec, kX, kStream>, dim3((unsigned)a.rows), threads, 0, s, a)
+                       : launch_early(row_kernel<4, kVec, kX, kStream>, dim3((unsigned)a.rows), threads, 0, s, a);
+}
+template <bool kVec>
+cudaError_t launch_as(const NormArgs &a, const Device &d, cudaStream_t s)
+{
+    if (a.x_wide) return a.stream_wide ? launch<kVec, true, true>(a, d, s) : launch<kVec, true, false>(a, d, s);
+    return a.stream_wide ? launch<kVec, false, true>(a, d, s) : launch<kVec, false, false>(a, d, s);
 }
 
 bool dtype_ok(int d) { return d == SYMAR_F32 || d == SYMAR_BF16; }
@@ -207,7 +477,7 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
         if (strides[i] < 0) return SYMAR_ERR_INVAL;
         if (!(p.gate_step == 0 && (i == 4 || i == 5))) vec = vec && strides[i] % 8 == 0;
     }
-    if (p.n > SYMAR_NORM_MAX || (int64_t)p.groups * p.m > 0x7fffffff - kSmall) return SYMAR_ERR_UNSUPPORTED;
+    if (p.n > SYMAR_NORM_MAX || (int64_t)p.groups * p.m > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
     if (p.groups == 0 || p.m == 0 || p.n == 0) return SYMAR_OK;
     if ((p.out == nullptr) != (p.before.kind == SYMAR_NORM_NONE)) return SYMAR_ERR_INVAL;
     if (!p.x || (!p.out && !p.residual_out)) return SYMAR_ERR_INVAL;
@@ -226,15 +496,9 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
     a.m = p.m;  a.n = p.n;  a.rows = p.groups * p.m;
     a.x_wide = p.dtype == SYMAR_F32;  a.stream_wide = p.stream_dtype == SYMAR_F32;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    // Few rows: as many threads as there are eights of a row, so that a row is one trip to memory; many: thirty-two elements a thread
-    // and fewer threads to meet in a sum.
-    const bool few = a.rows <= 296;
-    cudaError_t e;
-    if (a.n <= 256) e = launch<32, 1>(a, vec, s);
-    else if (a.n <= 1024) e = few ? launch<128, 1>(a, vec, s) : launch<32, 4>(a, vec, s);
-    else if (a.n <= 4096) e = few ? launch<512, 1>(a, vec, s) : launch<128, 4>(a, vec, s);
-    else if (a.n <= 8192) e = few ? launch<1024, 1>(a, vec, s) : launch<256, 4>(a, vec, s);
-    else if (a.n <= 16384) e = launch<512, 4>(a, vec, s);
-    else e = launch<1024, 4>(a, vec, s);
+    Device d;
+    const int rc = device_info(&d);
+    if (rc != SYMAR_OK) return rc;
+    const cudaError_t e = vec ? launch_as<true>(a, d, s) : launch_as<false>(a, d, s);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_norm");
 }

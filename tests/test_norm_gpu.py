@@ -77,7 +77,7 @@ SIZES = [1, 2, 7, 8, 9, 64, 128, 250, 256, 257, 264, 1000, 1024, 1032, 2049, 409
 
 
 @pytest.mark.parametrize("n", SIZES)
-@pytest.mark.parametrize("rows", [1, 3, 300])
+@pytest.mark.parametrize("rows", [1, 3, 300, 700])
 def test_sizes(n, rows):
     x, res, w, w2 = normal(rows, n, seed=n), normal(rows, n, seed=1, scale=3), normal(n, seed=2), normal(n, seed=3, dtype=F32)
     check(x, res, before=("rms", w, None, 1e-6, 0))
@@ -87,9 +87,9 @@ def test_sizes(n, rows):
 @pytest.mark.parametrize("xt", [BF16, F32])
 @pytest.mark.parametrize("st", [BF16, F32])
 @pytest.mark.parametrize("gate", [None, "channel", "row", "all", "one"])
-@pytest.mark.parametrize("n", [136, 517, 3080])
-def test_types_gates_and_kinds(xt, st, gate, n):
-    m = 5
+@pytest.mark.parametrize("m,n", [(5, 136), (5, 517), (5, 3080), (700, 64), (613, 120), (1200, 256), (777, 136), (601, 300), (999, 1000), (599, 1032),
+                                 (1500, 2056), (650, 6400), (600, 9000), (594, 16384)])
+def test_types_gates_and_kinds(xt, st, gate, m, n):
     x, res = normal(m, n, seed=1, dtype=xt), normal(m, n, seed=2, dtype=st)
     g = {None: None, "channel": (n,), "row": (m, 1), "all": (m, n), "one": ()}[gate]
     g = normal(*g, seed=3, dtype=xt) if g is not None else None
@@ -129,8 +129,8 @@ def test_strides_groups_and_offsets(offset, n):
 
 
 def test_results_may_be_the_operands():
-    for n in (256, 1000, 2049, 8192):
-        x, res, w = normal(9, n, seed=1), normal(9, n, seed=2, dtype=F32), normal(n, seed=3)
+    for m, n in ((9, 256), (9, 1000), (9, 2049), (9, 8192), (1801, 128), (703, 1024), (1203, 2048), (601, 2050), (599, 8192)):
+        x, res, w = normal(m, n, seed=1), normal(m, n, seed=2, dtype=F32), normal(n, seed=3)
         y, r = symar.norm(x, res, before=symar.Norm("rms", w))
         a, b = x.clone(), res.clone()
         got = symar.norm(a, b, before=symar.Norm("rms", w), out=a, residual_out=b)
