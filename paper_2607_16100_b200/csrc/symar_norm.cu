@@ -55,7 +55,7 @@ struct ThreadsSum {
         const int lane = threadIdx.x & 31;
         if (lane == 0) room[32 * which + warp] = s;
         asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-        return lanes_sum(lane < warps ? room[32 * which + lane] : 0.0f, 32);
+        return lanes_sum(lane < warps ? room[32 * which + lane] : 0.0f, 32);       // (zeros behind the last: in every lane the same order)
     }
 };
 
@@ -296,23 +296,43 @@ __global__ void __launch_bounds__(kShortThreads) short_kernel(const __grid_const
 struct Ring {
     int T, groups, slots;                  // threads of a group; groups; a group's slots
     int x_bytes, old_bytes, gate_bytes;    // of a row in a slot: x, residual, gate (0: not in it)
-    int held;                              // bytes of what all rows share (0: read from memory)
+    int held;                              // bytes of what all rows share
 };
-constexpr int kRingThreads = 1024, kRingRoom = 208 * 1024, kMaxSlots = 8, kMaxGroups = 15, kRingMost = 16 * kRingThreads;
+constexpr int kRingThreads = 512, kRingRoom = 208 * 1024 - 32, kMaxSlots = 8, kMaxGroups = 15, kRingMost = 32 * kRingThreads;
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// eight values at a place in shared memory
+__device__ __forceinline__ void shared8(const unsigned char *p, bool wide, float (&v)[8])
+{
+    const uint4 lo = *reinterpret_cast<const uint4 *>(p);
+    Raw r;
+    r.w[0] = lo.x; r.w[1] = lo.y; r.w[2] = lo.z; r.w[3] = lo.w;
+    if (wide) {
+        const uint4 hi = *reinterpret_cast<const uint4 *>(p + 16);
+        r.w[4] = hi.x; r.w[5] = hi.y; r.w[6] = hi.z; r.w[7] = hi.w;
+    }
+    values<true>(r, wide, v);
+}
+// A vector that all rows share, in shared memory from this thread's first element on.
+struct Held {
+    int there, at, wide, step;             // step: bytes from a chunk to the next
+};
+
+// A thread has four chunks of eight elements: what it does once a row is then little beside what it does for every element, and that is
+// what this kernel is made of (the row kernel's code in its place, sixteen elements a thread: 57 instructions an element and 275 us
+// for 16384 x 8192 with two norms).
 template <bool kX, bool kStream>
-__global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_constant__ NormArgs args, const __grid_constant__ Ring ring)
+__global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Ring ring)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(8) uint64_t bars[kMaxGroups * kMaxSlots];
     __shared__ float room[kMaxGroups * 2 * 4 * 32];            // a row's four sums, of every second row
     __shared__ int failed;
-    NormArgs a = args;
+    constexpr int C = 4, kZero = 32, kXB = kX ? 4 : 2, kSB = kStream ? 4 : 2;
     const int T = ring.T, group = (int)threadIdx.x / T, i = (int)threadIdx.x - group * T, n = a.n;
     if (threadIdx.x == 0) {
         for (int b = 0; b < ring.groups * ring.slots; ++b) bar_init(smem_addr(bars + b), 1);
@@ -320,41 +340,41 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_cons
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     wait_for_stream();
-    int at = 0;
-    auto hold = [&](const void *&p, bool wide) {
-        if (!p) return;
-        const int bytes = n * (wide ? 4 : 2);
+    // chunks behind the row's end read zeros from the first 32 bytes, so that nothing branches
+    if (threadIdx.x < kZero / 4) reinterpret_cast<uint32_t *>(smem)[threadIdx.x] = 0;
+    int used = kZero;
+    auto hold = [&](const void *p, bool wide) {
+        const int width = wide ? 4 : 2, bytes = n * width, at = used;
+        if (!p) return Held{0, 0, 0, 0};
         for (int b = 16 * (int)threadIdx.x; b < bytes; b += 16 * (int)blockDim.x)
             *reinterpret_cast<uint4 *>(smem + at + b) = *reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + b);
-        p = smem + at;
-        at += bytes;
+        used += bytes;
+        return Held{1, at + 8 * i * width, wide, 8 * T * width};
     };
-    Gate gate{a.gate, kX, a.gate_act, a.scale};
-    if (ring.held) {
-        hold(a.after.weight, a.after.wide), hold(a.after.bias, a.after.wide);
-        hold(a.before.weight, a.before.wide), hold(a.before.bias, a.before.wide);
-        if (a.gate && a.gate_step && !ring.gate_bytes) {       // with its function and the scale
-            float *to = reinterpret_cast<float *>(smem + at);
-            for (int c = 8 * (int)threadIdx.x; c < n; c += 8 * (int)blockDim.x) {
-                float f[8];
-                values<true>(read8<true>(a.gate, kX, c, 0, n), kX, f);
-                open8(f, a.gate_act);
+    const Held w0 = hold(a.after.weight, a.after.wide), b0 = hold(a.after.bias, a.after.wide), w1 = hold(a.before.weight, a.before.wide),
+               b1 = hold(a.before.bias, a.before.wide);
+    Held gate{0, 0, 0, 0};
+    if (a.gate && a.gate_step && !ring.gate_bytes) {           // with its function and the scale
+        float *to = reinterpret_cast<float *>(smem + used);
+        for (int c = 8 * (int)threadIdx.x; c < n; c += 8 * (int)blockDim.x) {
+            float f[8];
+            values<true>(read8<true>(a.gate, kX, c, 0, n), kX, f);
+            open8(f, a.gate_act);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] *= a.scale;
-                write8<true>(to, true, c, 0, n, f);
-            }
-            gate = Gate{to, true, SYMAR_GATE_NONE, 1.0f};
+            for (int j = 0; j < 8; ++j) f[j] *= a.scale;
+            write8<true>(to, true, c, 0, n, f);
         }
+        gate = Held{1, used + 32 * i, 1, 32 * T};
     }
     __syncthreads();
     const int slot_bytes = ring.x_bytes + ring.old_bytes + ring.gate_bytes, step = (int)gridDim.x * ring.groups;
-    unsigned char *slots = smem + ring.held + (int64_t)group * ring.slots * slot_bytes;
+    const int slots = kZero + ring.held + group * ring.slots * slot_bytes;
     const uint32_t bar0 = smem_addr(bars + group * ring.slots);
     const float inv_n = 1.0f / (float)n;
     auto ask = [&](int64_t row, int s) {   // (by one thread)
         if (row >= a.rows) return;
         const int g = (int)row / a.m, t = (int)row - g * a.m;
-        const uint32_t to = smem_addr(slots + s * slot_bytes), bar = bar0 + 8 * s;
+        const uint32_t to = smem_addr(smem) + slots + s * slot_bytes, bar = bar0 + 8 * s;
         bar_expect(bar, (uint32_t)slot_bytes);
         bulk_load(to, moved(a.x, g * a.x_group + t * a.x_ld, kX), ring.x_bytes, bar);
         if (ring.old_bytes) bulk_load(to + ring.x_bytes, moved(a.residual, g * a.residual_group + t * a.residual_ld, kStream), ring.old_bytes, bar);
@@ -363,22 +383,113 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_cons
     int64_t row = (int64_t)blockIdx.x * ring.groups + group;
     if (i == 0)
         for (int s = 0; s < ring.slots; ++s) ask(row + (int64_t)s * step, s);
-    ReadVectors<2, true, false> vectors;
-    vectors.i = i, vectors.T = T;
+    bool on[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) on[c] = (c * T + i) * 8 < n;
+
+    float v[C][8];
+    auto normed = [&](const Side &s, const Held &w, const Held &b, const ThreadsSum &sum, int which) {
+        if (s.kind == SYMAR_NORM_LAYER) {
+            float all = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) all += v[c][j];                   // (elements beyond the row are zeros)
+            const float mean = sum(all, which + 1) * inv_n;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] = on[c] ? v[c][j] - mean : 0.0f;
+        }
+        float all = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) all = fmaf(v[c][j], v[c][j], all);
+        const float by = 1.0f / sqrtf(fmaf(sum(all, which), inv_n, s.eps));
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[c][j] *= by;
+            if (w.there) {
+                float f[8];
+                shared8(smem + (on[c] ? w.at + c * w.step : 0), w.wide, f);
+                if (s.plus_one) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] += 1.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] *= f[j];
+            }
+            if (b.there) {
+                float f[8];
+                shared8(smem + (on[c] ? b.at + c * b.step : 0), b.wide, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] += f[j];
+            }
+        }
+    };
     auto gate_of = [&](int64_t r) { return r < a.rows ? row_gate(a, (int)r / a.m, (int)r % a.m) : 0.0f; };
-    float by = gate_of(row);
+    const bool row_gates = a.gate && !a.gate_step;
+    float by = row_gates ? gate_of(row) : a.scale;
     uint32_t turn = 0;
     for (int s = 0, round = 0; row < a.rows; row += step, ++turn) {
-        const float next = gate_of(row + step);
-        const int g = (int)row / a.m, t = (int)row - g * a.m;
+        const float next = row_gates ? gate_of(row + step) : by;
+        const int g = a.m == a.rows ? 0 : (int)row / a.m, t = (int)row - g * a.m;
+        const ThreadsSum sum{room + (group * 2 + (turn & 1)) * 4 * 32, T / 32, i >> 5, 1 + group};
         (void)warp_wait(bar0 + 8 * s, round & 1, &failed);     // (given up: on with what is there, the barriers count all)
-        const unsigned char *x = slots + s * slot_bytes, *h = x + ring.x_bytes;
-        do_row<2, true, kX, kStream>(a, [&](int c) { return read8<true>(x, kX, first<true>(c, i, T), T, n); },
-                                     [&](int c) { return read8<true>(h, kStream, first<true>(c, i, T), T, n); }, vectors,
-                                     ring.gate_bytes ? Gate{h + ring.old_bytes, kX, a.gate_act, a.scale} : gate, by, g, t, true, i, T, inv_n,
-                                     ThreadsSum{room + (group * 2 + (turn & 1)) * 4 * 32, T / 32, i >> 5, 1 + group});
-        // all of the slot has been read before the last sum, where there is one behind it
-        if (a.before.kind == SYMAR_NORM_NONE) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(T) : "memory");
+        const int x = slots + s * slot_bytes + 8 * i * kXB, h = slots + s * slot_bytes + ring.x_bytes + 8 * i * kSB;
+#pragma unroll
+        for (int c = 0; c < C; ++c) shared8(smem + (on[c] ? x + c * 8 * T * kXB : 0), kX, v[c]);
+        if (a.after.kind != SYMAR_NORM_NONE) normed(a.after, w0, b0, sum, 0);
+        if (gate.there) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float f[8];
+                shared8(smem + (on[c] ? gate.at + c * gate.step : 0), true, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] *= f[j];
+            }
+        } else if (ring.gate_bytes) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float f[8];
+                shared8(smem + (on[c] ? x + ring.x_bytes + ring.old_bytes + c * 8 * T * kXB : 0), kX, f);
+                open8(f, a.gate_act);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] *= a.scale * f[j];
+            }
+        } else if (by != 1.0f) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] *= by;
+        }
+        if (ring.old_bytes) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float f[8];
+                shared8(smem + (on[c] ? h + c * 8 * T * kSB : 0), kStream, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] = fmaf(a.residual_scale, f[j], v[c][j]);
+            }
+        }
+        if (a.residual_out) {
+            void *to = moved(a.residual_out, g * a.residual_out_group + t * a.residual_out_ld + 8 * i, kStream);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (on[c]) write8<true>(to, kStream, c * 8 * T, 0, n, v[c]);
+        }
+        if (a.out) {
+            normed(a.before, w1, b1, sum, 2);
+            void *to = moved(a.out, g * a.out_group + t * a.out_ld + 8 * i, kX);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (on[c]) write8<true>(to, kX, c * 8 * T, 0, n, v[c]);
+        } else {
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(T) : "memory");
+        }
+        // all of the slot has been read before the row's last barrier
         if (i == 0) ask(row + (int64_t)ring.slots * step, s);
         if (++s == ring.slots) s = 0, ++round;
         by = next;
@@ -395,8 +506,8 @@ Ring ring_of(const NormArgs &a)
     r.gate_bytes = a.gate && a.gate_step && (a.gate_ld != 0 || a.gate_group != 0) ? a.n * xw : 0;
     for (const Side *s : {&a.after, &a.before}) r.held += ((s->weight != nullptr) + (s->bias != nullptr)) * a.n * (s->wide ? 4 : 2);
     if (a.gate && a.gate_step && !r.gate_bytes) r.held += a.n * 4;
-    if (r.held > 96 * 1024) r.held = 0;
-    const int threads = ((a.n + 15) / 16 + 31) / 32 * 32;  // sixteen elements each
+    if (r.held > kRingRoom) return r;
+    const int threads = ((a.n + 31) / 32 + 31) / 32 * 32;
     for (int groups = kRingThreads / threads < kMaxGroups ? kRingThreads / threads : kMaxGroups; groups > 0; --groups) {
         const int slots = (kRingRoom - r.held) / (groups * (r.x_bytes + r.old_bytes + r.gate_bytes));
         if (slots < 2) continue;
@@ -426,9 +537,9 @@ cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
     if (kVec && many && a.n <= kRingMost && (a.after.kind != SYMAR_NORM_NONE || a.before.kind != SYMAR_NORM_NONE)) {
         const Ring r = ring_of(a);
         if (r.T) {
-            const int bytes = r.held + r.groups * r.slots * (r.x_bytes + r.old_bytes + r.gate_bytes);
+            const int bytes = 32 + r.held + r.groups * r.slots * (r.x_bytes + r.old_bytes + r.gate_bytes);
             static std::atomic<uint64_t> allowed{0};
-            const cudaError_t e = allow_shared((const void *)ring_kernel<kX, kStream>, kRingRoom, d.id, allowed);
+            const cudaError_t e = allow_shared((const void *)ring_kernel<kX, kStream>, kRingRoom + 32, d.id, allowed);
             return e != cudaSuccess ? e : launch_early(ring_kernel<kX, kStream>, dim3((unsigned)d.sms), (unsigned)(r.T * r.groups), (size_t)bytes, s, a, r);
         }
     }
