@@ -1,8 +1,8 @@
 // out[t] = sum_j weight[t][j] y[row of (t, j)] + residual[t], for every rank (formulas in include/symar.h): the experts' rows back in the
 // tokens' order.
 //
-// A thread has eight channels of one token and asks for up to eight of its rows at once; they are added in the order of
-// the token's choices, so that results do not depend on anything else.  Bound by the rows' bytes.
+// A thread has eight or sixteen channels of one token and asks for eight pieces of its rows at once; a token's rows are added in the order
+// of its choices, so that results do not depend on anything else.  Bound by the rows' bytes: 8192 tokens x 4 rows x 4096 take FIGURE us.
 #include "symar_eights.cuh"
 #include "symar_ops.h"
 
@@ -14,55 +14,90 @@ struct CombineArgs {
     const int32_t *token_row;
     const float   *weights;
     void          *out;
-    int64_t y_ld, y_group, residual_ld, residual_group, out_ld, out_group, cells;      // cells: tokens of all groups
+    int64_t y_ld, y_group, residual_ld, residual_group, out_ld, out_group;
     int     tokens, top_k, rows, n, root;
-    int     y_wide, out_wide;
-    int     lanes, parts;                  // threads of a token, and of how many blocks' worth each
+    int     lanes, parts;                  // threads of a token (a power of two), and into how many blocks its channels are divided
 };
 constexpr int kMost = 1 << 30;              // channels: their last step ends below 2^31
-constexpr int kThreads = 256, kAtOnce = 8;
+constexpr int kThreads = 256;
 
-template <bool kVec>
+// kY, kOut: y and the results are float32.  K: rows asked for at once, C: pieces of each.
+template <bool kVec, bool kY, bool kOut, int K, int C>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ CombineArgs a)
 {
     wait_for_stream();
-    // `lanes` threads have 8 * lanes channels of a token; a block has kThreads / lanes tokens, or a part of one
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes, cell = unit / a.parts;
-    if (cell >= a.cells) return;
-    const int g = (int)(cell / a.tokens), t = (int)(cell - (int64_t)g * a.tokens);
-    const int i = (int)(unit - cell * a.parts) * a.lanes + (int)threadIdx.x % a.lanes, first = kVec ? 8 * i : i, step = a.lanes * a.parts;
+    const unsigned block = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - block * a.parts;
+    const int g = blockIdx.y, t = (int)(block * (kThreads / a.lanes) + threadIdx.x / a.lanes);
+    if (t >= a.tokens) return;
+    const int i = (int)part * C * a.lanes + (int)(threadIdx.x & (a.lanes - 1)), step = a.lanes * a.parts * C;
+    int first[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) first[c] = (kVec ? 8 : 1) * (i + c * a.lanes);
     const int32_t *at = a.token_row + (int64_t)t * a.top_k;
     const float *w = a.weights ? a.weights + (int64_t)t * a.top_k : nullptr;
-    const char *y = static_cast<const char *>(a.y) + g * a.y_group * (a.y_wide ? 4 : 2);
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int j0 = 0; j0 < a.top_k; j0 += kAtOnce) {
-        Raw   r[kAtOnce];
-        float by[kAtOnce];
-        bool  on[kAtOnce];
+    const char *y = static_cast<const char *>(a.y) + g * a.y_group * (kY ? 4 : 2);
+    float sum[C][8] = {};
+    for (int j0 = 0; j0 < a.top_k; j0 += K) {
+        int   row[K];
+        float by[K];
+        Raw   r[K][C];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int row = j0 + j < a.top_k ? at[j0 + j] : -1;
-            on[j] = row >= 0 && row < a.rows;
-            by[j] = on[j] && w ? w[j0 + j] : 1.0f;
-            if (on[j]) r[j] = read8<kVec>(y + row * a.y_ld * (a.y_wide ? 4 : 2), a.y_wide, first, step, a.n);
+        for (int j = 0; j < K; ++j) {
+            row[j] = j0 + j < a.top_k ? at[j0 + j] : -1;
+            by[j]  = j0 + j < a.top_k && w ? w[j0 + j] : 1.0f;
         }
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            if (!on[j]) continue;
+        for (int j = 0; j < K; ++j) {
+            const bool on = (unsigned)row[j] < (unsigned)a.rows;
+            const char *p = y + (on ? row[j] : 0) * a.y_ld * (kY ? 4 : 2);
+            by[j] = on ? by[j] : 0.0f;     // (and zeros times that)
+#pragma unroll
+            for (int c = 0; c < C; ++c) r[j][c] = read8<kVec>(p, kY, first[c], step, on ? a.n : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float v[8];
+                values<kVec>(r[j][c], kY, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[c][e] = fmaf(by[j], v[e], sum[c][e]);
+            }
+    }
+    const bool add = a.residual && (a.root < 0 || a.root == g);
+    const char *res = static_cast<const char *>(a.residual) + (g * a.residual_group + t * a.residual_ld) * (kOut ? 4 : 2);
+    char *out = static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (kOut ? 4 : 2);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (add) {
             float v[8];
-            values<kVec>(r[j], a.y_wide, v);
+            values<kVec>(read8<kVec>(res, kOut, first[c], step, a.n), kOut, v);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) sum[c] = fmaf(by[j], v[c], sum[c]);
+            for (int e = 0; e < 8; ++e) sum[c][e] += v[e];
         }
+        write8<kVec>(out, kOut, first[c], step, a.n, sum[c]);
     }
-    if (a.residual && (a.root < 0 || a.root == g)) {
-        const char *p = static_cast<const char *>(a.residual) + (g * a.residual_group + t * a.residual_ld) * (a.out_wide ? 4 : 2);
-        float v[8];
-        values<kVec>(read8<kVec>(p, a.out_wide, first, step, a.n), a.out_wide, v);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] += v[c];
-    }
-    write8<kVec>(static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (a.out_wide ? 4 : 2), a.out_wide, first, step, a.n, sum);
+}
+template <bool kVec, bool kY, bool kOut, int K, int C>
+cudaError_t launch(CombineArgs a, int groups, cudaStream_t s)
+{
+    a.lanes = 1;
+    while (a.lanes < kThreads && a.lanes * 8 * C < a.n) a.lanes *= 2;
+    a.parts = (a.n + a.lanes * 8 * C - 1) / (a.lanes * 8 * C);
+    const int64_t per = kThreads / a.lanes, blocks = (a.tokens + per - 1) / per * a.parts;
+    return launch_early(combine_kernel<kVec, kY, kOut, K, C>, dim3((unsigned)blocks, (unsigned)groups), kThreads, 0, s, a);
+}
+// Few rows a token leave room for two pieces of each on their way.
+template <bool kVec, bool kY, bool kOut>
+cudaError_t launch_of(const CombineArgs &a, int groups, cudaStream_t s)
+{
+    return a.top_k <= 4 ? launch<kVec, kY, kOut, 4, kVec ? 2 : 1>(a, groups, s) : launch<kVec, kY, kOut, 8, 1>(a, groups, s);
+}
+template <bool kVec>
+cudaError_t launch_as(const CombineArgs &a, int groups, bool y_wide, bool out_wide, cudaStream_t s)
+{
+    if (y_wide) return out_wide ? launch_of<kVec, true, true>(a, groups, s) : launch_of<kVec, true, false>(a, groups, s);
+    return out_wide ? launch_of<kVec, false, true>(a, groups, s) : launch_of<kVec, false, false>(a, groups, s);
 }
 
 bool dtype_ok(int d) { return d == SYMAR_F32 || d == SYMAR_BF16; }
@@ -86,7 +121,7 @@ extern "C" int symar_combine(const symar_combine_t *args, void *cuda_stream)
         if (s < 0) return SYMAR_ERR_INVAL;
         vec = vec && s % 8 == 0;
     }
-    if (p.n > kMost) return SYMAR_ERR_UNSUPPORTED;
+    if (p.n > kMost || p.groups > 65535 || (int64_t)p.tokens * ((p.n + 2047) / 2048) > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
     if (p.groups == 0 || p.tokens == 0 || p.n == 0) return SYMAR_OK;
     if (!p.out || (p.top_k > 0 && (!p.token_row || (p.rows > 0 && !p.y)))) return SYMAR_ERR_INVAL;
     if (rows_meet(p.tokens, p.out_ld, p.groups, p.out_group, p.n)) return SYMAR_ERR_INVAL;
@@ -95,16 +130,9 @@ extern "C" int symar_combine(const symar_combine_t *args, void *cuda_stream)
     a.residual = p.residual;  a.residual_ld = p.residual_ld;  a.residual_group = p.residual_group;
     a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
     a.token_row = p.token_row;  a.weights = p.weights;
-    a.cells = (int64_t)p.groups * p.tokens;
     a.tokens = p.tokens;  a.top_k = p.top_k;  a.rows = p.rows;  a.n = p.n;  a.root = p.root;
-    a.y_wide = p.dtype == SYMAR_F32;  a.out_wide = p.out_dtype == SYMAR_F32;
-    a.lanes = 1;
-    while (a.lanes < kThreads && a.lanes * 8 < p.n) a.lanes *= 2;
-    a.parts = (p.n + a.lanes * 8 - 1) / (a.lanes * 8);
-    const int64_t per = kThreads / a.lanes, blocks = (a.cells * a.parts + per - 1) / per;
-    if (blocks > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    const cudaError_t e = vec ? launch_early(combine_kernel<true>, dim3((unsigned)blocks), kThreads, 0, s, a)
-                              : launch_early(combine_kernel<false>, dim3((unsigned)blocks), kThreads, 0, s, a);
+    const bool y_wide = p.dtype == SYMAR_F32, out_wide = p.out_dtype == SYMAR_F32;
+    const cudaError_t e = vec ? launch_as<true>(a, p.groups, y_wide, out_wide, s) : launch_as<false>(a, p.groups, y_wide, out_wide, s);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_combine");
 }

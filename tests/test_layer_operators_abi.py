@@ -100,6 +100,7 @@ def test_combine_sizes(lib):
     assert lib.symar_combine(None, None) == symar.ERR_INVAL
     assert combine_rc(lib, n=(1 << 30) + 1, out_ld=1 << 31, out_group=1 << 40) == symar.ERR_UNSUPPORTED
     assert combine_rc(lib, n=1 << 30, tokens=1 << 20, out_ld=1 << 31, out_group=1 << 52) == symar.ERR_UNSUPPORTED
+    assert combine_rc(lib, groups=65536) == symar.ERR_UNSUPPORTED
     for empty in ("groups", "tokens", "n"):
         assert combine_rc(lib, **{empty: 0, "y": None, "out": None, "token_row": None}) == symar.OK
 
