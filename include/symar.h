@@ -683,7 +683,7 @@ int symar_experts(const symar_experts_t *args, void *cuda_stream);
  * order, for every rank g.  y [groups][rows][n] of dtype, out and residual (NULL: none) [groups][tokens][n] of out_dtype; weights NULL: 1.
  * A token_row below 0 or from `rows` on is none, whatever its weight.  root: the one group that adds the residual, -1 = every
  * group (a group stride of 0 shares it).  Sums are binary32 in the order of j, rounded once.  out may be residual with the same layout.  n up to
- * 2^30, 65535 ranks, tokens times n / 2048 below 2^31. */
+ * 2^30, 65535 ranks, tokens times n / 256 below 2^31. */
 typedef struct {
     const void    *y;         int64_t y_ld, y_group;
     const int32_t *token_row;

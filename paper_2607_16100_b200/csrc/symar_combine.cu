@@ -26,13 +26,18 @@ template <bool kVec, bool kY, bool kOut, int K, int C>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ CombineArgs a)
 {
     wait_for_stream();
-    const unsigned block = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - block * a.parts;
-    const int g = blockIdx.y, t = (int)(block * (kThreads / a.lanes) + threadIdx.x / a.lanes);
+    // a token's channels are divided into `parts` of 8 C a thread; on no boundary a warp has 256 in a row, a thread every thirty-second of them
+    constexpr int step = 32;
+    const unsigned lanes = kVec ? a.lanes : 32, per = kThreads / lanes, unit = blockIdx.x * per + threadIdx.x / lanes;
+    const unsigned block = kVec ? blockIdx.x / (unsigned)a.parts : 0, part = kVec ? blockIdx.x - block * a.parts : unit % (unsigned)a.parts;
+    const int g = blockIdx.y, t = (int)(kVec ? block * per + threadIdx.x / lanes : unit / (unsigned)a.parts);
     if (t >= a.tokens) return;
-    const int i = (int)part * C * a.lanes + (int)(threadIdx.x & (a.lanes - 1)), step = a.lanes * a.parts * C;
     int first[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) first[c] = (kVec ? 8 : 1) * (i + c * a.lanes);
+    for (int c = 0; c < C; ++c) {
+        const int i = (int)(part * C + c) * (int)lanes;
+        first[c] = 8 * i + (kVec ? 8 : 1) * (int)(threadIdx.x & (lanes - 1));
+    }
     const int32_t *at = a.token_row + (int64_t)t * a.top_k;
     const float *w = a.weights ? a.weights + (int64_t)t * a.top_k : nullptr;
     const char *y = static_cast<const char *>(a.y) + g * a.y_group * (kY ? 4 : 2);
@@ -81,10 +86,10 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
 template <bool kVec, bool kY, bool kOut, int K, int C>
 cudaError_t launch(CombineArgs a, int groups, cudaStream_t s)
 {
-    a.lanes = 1;
-    while (a.lanes < kThreads && a.lanes * 8 * C < a.n) a.lanes *= 2;
+    a.lanes = kVec ? 1 : 32;
+    while (kVec && a.lanes < kThreads && a.lanes * 8 * C < a.n) a.lanes *= 2;
     a.parts = (a.n + a.lanes * 8 * C - 1) / (a.lanes * 8 * C);
-    const int64_t per = kThreads / a.lanes, blocks = (a.tokens + per - 1) / per * a.parts;
+    const int64_t per = kThreads / a.lanes, blocks = kVec ? (a.tokens + per - 1) / per * a.parts : ((int64_t)a.tokens * a.parts + per - 1) / per;
     return launch_early(combine_kernel<kVec, kY, kOut, K, C>, dim3((unsigned)blocks, (unsigned)groups), kThreads, 0, s, a);
 }
 // Few rows a token leave room for two pieces of each on their way.
@@ -121,7 +126,7 @@ extern "C" int symar_combine(const symar_combine_t *args, void *cuda_stream)
         if (s < 0) return SYMAR_ERR_INVAL;
         vec = vec && s % 8 == 0;
     }
-    if (p.n > kMost || p.groups > 65535 || (int64_t)p.tokens * ((p.n + 2047) / 2048) > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
+    if (p.n > kMost || p.groups > 65535 || (int64_t)p.tokens * ((p.n + 255) / 256) > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
     if (p.groups == 0 || p.tokens == 0 || p.n == 0) return SYMAR_OK;
     if (!p.out || (p.top_k > 0 && (!p.token_row || (p.rows > 0 && !p.y)))) return SYMAR_ERR_INVAL;
     if (rows_meet(p.tokens, p.out_ld, p.groups, p.out_group, p.n)) return SYMAR_ERR_INVAL;

@@ -229,12 +229,14 @@ __device__ __forceinline__ void do_row(const NormArgs &a, const In &in, const Ol
 }
 
 // ---- a block has a row: few rows, and long ones on no boundary ----
-template <int C, bool kVec, bool kX, bool kStream>
-__global__ void __launch_bounds__(1024) row_kernel(const __grid_constant__ NormArgs a)
+// kT: threads of a block (0: as launched; on no boundary elements a known number apart need no arithmetic for each address).
+template <int C, int kT, bool kX, bool kStream>
+__global__ void __launch_bounds__(kT ? kT : 1024) row_kernel(const __grid_constant__ NormArgs a)
 {
+    constexpr bool kVec = kT == 0;
     __shared__ float room[4 * 32];
     wait_for_stream();
-    const int T = blockDim.x, i = threadIdx.x, row = blockIdx.x, g = row / a.m, t = row - g * a.m;
+    const int T = kT ? kT : blockDim.x, i = threadIdx.x, row = blockIdx.x, g = row / a.m, t = row - g * a.m;
     const void *x = moved(a.x, g * a.x_group + t * a.x_ld, kX);
     Raw in[C], old[C] = {};
 #pragma unroll
@@ -543,10 +545,18 @@ cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
             return e != cudaSuccess ? e : launch_early(ring_kernel<kX, kStream>, dim3((unsigned)d.sms), (unsigned)(r.T * r.groups), (size_t)bytes, s, a, r);
         }
     }
-    const int chunks = a.n <= 8192 ? 1 : 4;
-    const unsigned threads = (unsigned)(((a.n + 8 * chunks - 1) / (8 * chunks) + 31) / 32 * 32);
-    return chunks == 1 ? launch_early(row_kernel<1, kVec, kX, kStream>, dim3((unsigned)a.rows), threads, 0, s, a)
-                       : launch_early(row_kernel<4, kVec, kX, kStream>, dim3((unsigned)a.rows), threads, 0, s, a);
+    const dim3 rows((unsigned)a.rows);
+    if constexpr (kVec) {
+        const int chunks = a.n <= 8192 ? 1 : 4;
+        const unsigned threads = (unsigned)(((a.n + 8 * chunks - 1) / (8 * chunks) + 31) / 32 * 32);
+        return chunks == 1 ? launch_early(row_kernel<1, 0, kX, kStream>, rows, threads, 0, s, a) : launch_early(row_kernel<4, 0, kX, kStream>, rows, threads, 0, s, a);
+    } else {
+        if (a.n <= 1024) return launch_early(row_kernel<1, 128, kX, kStream>, rows, 128, 0, s, a);
+        if (a.n <= 2048) return launch_early(row_kernel<2, 128, kX, kStream>, rows, 128, 0, s, a);
+        if (a.n <= 4096) return launch_early(row_kernel<2, 256, kX, kStream>, rows, 256, 0, s, a);
+        if (a.n <= 8192) return launch_early(row_kernel<2, 512, kX, kStream>, rows, 512, 0, s, a);
+        return launch_early(row_kernel<4, 1024, kX, kStream>, rows, 1024, 0, s, a);
+    }
 }
 template <bool kVec>
 cudaError_t launch_as(const NormArgs &a, const Device &d, cudaStream_t s)
