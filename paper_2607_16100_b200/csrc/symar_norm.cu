@@ -66,7 +66,6 @@ template <int C, bool kVec, bool kRead> struct ReadVectors {
     int i, T;
     __device__ __forceinline__ void read(const Side &s, int side, int n)
     {
-        if (!kRead) return;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (s.weight) w[side][c] = read8<kVec>(s.weight, s.wide, first<kVec>(c, i, T), T, n);
@@ -248,7 +247,7 @@ __global__ void __launch_bounds__(kT ? kT : 1024) row_kernel(const __grid_consta
     }
     ReadVectors<C, kVec, C == 1> vectors;  // (one trip to memory where registers allow it)
     vectors.i = i, vectors.T = T;
-    vectors.read(a.after, 0, a.n), vectors.read(a.before, 1, a.n);
+    if constexpr (C == 1) vectors.read(a.after, 0, a.n), vectors.read(a.before, 1, a.n);
     const float by = row_gate(a, g, t);
     do_row<C, kVec, kX, kStream>(a, [&](int c) { return in[c]; }, [&](int c) { return old[c]; }, vectors,
                                  Gate{moved(a.gate, g * a.gate_group + t * a.gate_ld, kX), kX, a.gate_act, a.scale}, by, g, t, true, i, T, 1.0f / (float)a.n, ThreadsSum{room, T / 32, i >> 5, 0});

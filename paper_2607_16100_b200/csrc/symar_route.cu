@@ -1,13 +1,15 @@
 // The experts of every token, and the tokens of every expert (formulas in include/symar.h).
 //
-// A warp has one token at a time, a lane every thirty-second of its experts, as whole numbers in the order of the floats; a choice
-// is one maximum over the warp and one minimum over the indexes that have it.  Which row of the lists a choice gets is a
-// counting sort that keeps the tokens' order: every warp has tokens in a row and counts its choices per expert, the counts of
-// earlier warps and blocks and of smaller experts are added up, and the warp goes through its tokens once more.  Nothing depends on the order in which
-// blocks run.  Few tokens are one block and one launch; more are two launches, the blocks' counts between them in the workspace.
+// A warp has one token at a time, a lane every thirty-second of its experts, as whole numbers in the order of the floats whose lowest
+// bits give way to the expert's place in the lane.  A lane sorts its own; a choice is then the largest of the lanes' first ones.  Which row of the
+// lists a choice gets is a counting sort that keeps the tokens' order: every warp has tokens in a row and counts its choices per expert, the counts
+// of earlier warps and blocks and of smaller experts are added up, and the warp goes through its tokens once more.  Nothing depends on the order in
+// which blocks run.  Few tokens are one block and one launch; more are two launches, the blocks' counts between them in the workspace.
 //
-// Choices by score + bias have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order
-// found are nearer than the rounding of their keys, the token's choices are made again in binary64.
+// Choices have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order found are nearer than the rounding of
+// their keys, the token's choices are made again in binary64.
+//
+// Bound by instructions: FIGURES
 #include <math.h>
 
 #include "symar_ops.h"
@@ -58,7 +60,7 @@ __device__ __forceinline__ double warp_sum(double s)
     return s;
 }
 
-// The choices by score + bias in binary64: lane j gets the j-th expert, -1 for none.
+// The choices in binary64, by score + bias or by logit: lane j gets the j-th expert, -1 for none.
 template <int V>
 __device__ __noinline__ int choose_exactly(const RouteArgs &a, int64_t row, float top)
 {
@@ -68,14 +70,16 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int64_t row, floa
     for (int i = 0; i < V; ++i) {
         const int e = lane + 32 * i;
         const float v = e < a.experts ? logit_of(a, row, e) : -INFINITY;
-        key[i] = a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : exp((double)v - (double)top);
+        key[i] = !a.bias ? (double)v : a.sigmoid ? 1.0 / (1.0 + exp(-(double)v)) : exp((double)v - (double)top);
         if (!(v > -INFINITY)) key[i] = NAN;
         else sum += key[i];
     }
-    sum = warp_sum(sum);
+    if (a.bias) {
+        sum = warp_sum(sum);
 #pragma unroll 1
-    for (int i = 0; i < V; ++i)
-        if (lane + 32 * i < a.experts) key[i] = (a.sigmoid ? key[i] : key[i] / sum) + (double)a.bias[lane + 32 * i];
+        for (int i = 0; i < V; ++i)
+            if (lane + 32 * i < a.experts) key[i] = (a.sigmoid ? key[i] : key[i] / sum) + (double)a.bias[lane + 32 * i];
+    }
     int mine = -1;
     for (int j = 0; j < a.top_k; ++j) {
         double best = -INFINITY;
@@ -96,80 +100,100 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int64_t row, floa
     return mine;
 }
 
+// Falling order, by Batcher's odd-even merges
+template <int V>
+__device__ __forceinline__ void sort_falling(uint32_t (&key)[V])
+{
+#pragma unroll
+    for (int p = 1; p < V; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < V; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const uint32_t x = key[i + j], y = key[i + j + k];
+                        key[i + j] = max(x, y), key[i + j + k] = min(x, y);
+                    }
+}
+
 // Expert and weight of choice `lane` of token t (-1 and 0: none).  V: experts of a lane.
 template <int V>
 __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
 {
     const int lane = threadIdx.x & 31;
     const int64_t row = t * a.ld;
-    uint32_t key[V];
+    float v[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = lane + 32 * i < a.experts ? ordered(logit_of(a, row, lane + 32 * i)) : 0u;
+    for (int i = 0; i < V; ++i) v[i] = lane + 32 * i < a.experts ? logit_of(a, row, lane + 32 * i) : -INFINITY;
     float top = 0.0f, sum = 1.0f;
     if (!a.sigmoid) {
-        uint32_t most = 0;
+        float most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < V; ++i) most = max(most, key[i]);
-        most = __reduce_max_sync(0xffffffffu, most);
-        top = unordered(most);
+        for (int i = 0; i < V; ++i) most = fmaxf(most, v[i]);                 // (NaN counts as nothing)
+        const uint32_t whole = __reduce_max_sync(0xffffffffu, ordered(most));
+        top = whole ? unordered(whole) : 0.0f;
         if (a.bias || !a.renormalise) {    // (the weights' quotients need no sum over all)
             sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += key[i] ? expf(unordered(key[i]) - top) : 0.0f;
+            for (int i = 0; i < V; ++i) sum += v[i] > -INFINITY ? expf(v[i] - top) : 0.0f;
             sum = warp_sum(sum);
+            if (!whole) sum = 1.0f;
         }
-        if (most == 0) top = 0.0f, sum = 1.0f;
     }
-    if (a.bias) {
+    uint32_t key[V];
+    if (a.bias) {                          // (fast functions: what they round is in `margin`)
+        const float by = 1.0f / sum;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (key[i] == 0) continue;
-            const float v = unordered(key[i]);
-            const float score = a.sigmoid ? 1.0f / (1.0f + expf(-v)) : expf(v - top) / sum;
-            key[i] = ordered(score + a.bias[lane + 32 * i]);
+            const float score = a.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-v[i])) : __expf(v[i] - top) * by;
+            const bool there = lane + 32 * i < a.experts && v[i] > -INFINITY;
+            key[i] = there ? ordered(score + a.bias[lane + 32 * i]) : 0u;
         }
-    }
-    uint32_t best = 0;
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) best = max(best, key[i]);
-    // one choice more than asked for, where the border has to be looked at
-    const int more = a.bias ? min(a.top_k + 1, a.experts) : a.top_k;
+        for (int i = 0; i < V; ++i) key[i] = ordered(v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - i) : 0u;
+    sort_falling<V>(key);
+    // Two keys' errors together.  Score of a sigmoid s, x its logit: s (1 - s) (2 + 1.2 |x|) units of the fast exponential, a unit of the sum and one of
+    // the quotient, below 4 x 2^-23; of a softmax, of its largest one p: p (2 + 1.2 |x|) with p |x| < 0.4 of it, 37 additions of the sum.  Then a rounding of the
+    // sum with the bias, and the bits that the place takes.
+    const float step = a.sigmoid ? 0x1p-19f : 0x1p-17f / sum;
+    const int more = min(a.top_k + 1, a.experts);       // (the border has to be looked at)
     int mine = -1, last_at = -1;
     uint32_t last = 0;
     bool near = false;
-    // two keys' errors together: a score's (sigmoid: a function's two units, two roundings; softmax: of the largest one, the sum's 37
-    // additions more), and a rounding of the keys themselves
-    const float step = a.sigmoid ? 0x1p-20f : 0x1p-17f / sum;
     for (int j = 0; j < more; ++j) {
-        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+        const uint32_t most = __reduce_max_sync(0xffffffffu, key[0]);
         if (most == 0) break;
-        int at = kMaxExperts;
-        if (best == most) {
-#pragma unroll
-            for (int i = V - 1; i >= 0; --i) at = key[i] == most ? lane + 32 * i : at;
-        }
-        at = (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
+        // (the same place in several lanes: the lowest lane's is the lowest index)
+        const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == most)) - 1, at = winner + 32 * (V - 1 - (int)(most & (V - 1)));
         if (lane == j && j < a.top_k) mine = at;
-        if (a.bias) {
-            if (j > 0) {
-                const float was = unordered(last), is = unordered(most);
-                if (!(was - is > step + 0x1p-21f * fabsf(is)))
-                    near |= logit_of(a, row, at) != logit_of(a, row, last_at) || a.bias[at] != a.bias[last_at];
+        if (j > 0) {
+            bool close;
+            if (a.bias) {
+                const float was = unordered(last & ~(uint32_t)(V - 1)), is = unordered(most & ~(uint32_t)(V - 1));
+                close = !(was - is > step + (0x1p-21f + V * 0x1p-22f) * fmaxf(fabsf(was), fabsf(is)));
+            } else {
+                close = (last ^ most) < (uint32_t)V;
             }
-            last = most, last_at = at;
+            if (close) near |= logit_of(a, row, at) != logit_of(a, row, last_at) || (a.bias && a.bias[at] != a.bias[last_at]);
         }
-        best = 0;
+        last = most, last_at = at;
+        if (lane == winner) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (lane + 32 * i == at) key[i] = 0;
-            best = max(best, key[i]);
+            for (int i = 0; i + 1 < V; ++i) key[i] = key[i + 1];
+            key[V - 1] = 0;
         }
     }
     if (near) mine = choose_exactly<V>(a, row, top);
     weight = 0.0f;
     if (mine >= 0) {
-        const float v = logit_of(a, row, mine);
-        weight = a.sigmoid ? 1.0f / (1.0f + expf(-v)) : expf(v - top);
+        const float logit = logit_of(a, row, mine);
+        weight = a.sigmoid ? 1.0f / (1.0f + expf(-logit)) : expf(logit - top);
         if (!a.sigmoid && !a.renormalise) weight /= sum;
     }
     if (a.renormalise) {
@@ -216,36 +240,21 @@ __device__ __forceinline__ int exclusive(int v, int *room)
     return room[warp] + s - v;
 }
 
-// Rows of the warp's choices, once count[warp][e] holds its first row of expert e.
-__device__ __forceinline__ void place(const RouteArgs &a, Part tokens, int32_t *count)
-{
-    const int lane = threadIdx.x & 31;
-    for (int t = tokens.lo; t < tokens.hi; ++t) {
-        const int64_t at = (int64_t)t * a.top_k + lane;
-        const int e = lane < a.top_k ? a.choice[at] : -1;
-        int row = -1;
-        if (e >= 0) {                      // (a token's experts are different ones)
-            row = count[e]++;
-            a.row_token[row] = t;
-        }
-        if (lane < a.top_k) a.token_row[at] = row;
-        __syncwarp();
-    }
-}
-
-// kOnce: one block does it all.
+// kOnce: one block does it all.  Otherwise a choice's place among those of its block and expert goes to token_row, for place_kernel.
 template <int V, bool kOnce>
 __global__ void __launch_bounds__(kThreads, 1) choose_kernel(const __grid_constant__ RouteArgs a)
 {
     extern __shared__ int32_t count[];     // [kWarps][experts]
     __shared__ int room[33];
+    constexpr int kKept = 4;               // tokens whose choices stay in registers
     wait_for_stream();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     int32_t *own = count + warp * a.experts;
     for (int e = lane; e < a.experts; e += 32) own[e] = 0;
     __syncwarp();
     const Part mine = part(part({0, a.tokens}, blockIdx.x, gridDim.x), warp, kWarps);
-    for (int t = mine.lo; t < mine.hi; ++t) {
+    int kept[kKept];
+    auto take = [&](int t) {
         float weight;
         const int e = choose<V>(a, t, weight);
         if (lane < a.top_k) {
@@ -253,70 +262,99 @@ __global__ void __launch_bounds__(kThreads, 1) choose_kernel(const __grid_consta
             a.choice[at] = e;
             a.weights[at] = weight;
         }
-        if (e >= 0) ++own[e];
+        if (e >= 0) ++own[e];              // (a token's experts are different ones)
         __syncwarp();
+        return e;
+    };
+#pragma unroll
+    for (int u = 0; u < kKept; ++u) kept[u] = -1;
+    for (int t = mine.lo; t < mine.hi; ++t) {
+        const int e = take(t);
+#pragma unroll
+        for (int u = 0; u < kKept; ++u) kept[u] = t - mine.lo == u ? e : kept[u];
     }
     __syncthreads();
+    // count[w][e]: the choices of expert e by warps before w
     int all = 0;
-    if (tid < a.experts)
-        for (int w = 0; w < kWarps; ++w) all += count[w * a.experts + tid];
-    if (!kOnce) {
-        if (tid < a.experts) a.counts[(int64_t)blockIdx.x * a.experts + tid] = all;
-        return;
-    }
-    const int first = exclusive(all, room);
     if (tid < a.experts) {
-        a.expert_start[tid] = first;
-        int run = first;
+#pragma unroll 8
         for (int w = 0; w < kWarps; ++w) {
             const int c = count[w * a.experts + tid];
-            count[w * a.experts + tid] = run;
-            run += c;
+            count[w * a.experts + tid] = all;
+            all += c;
         }
     }
-    if (tid == 0) a.expert_start[a.experts] = room[32];
+    int *base = count + kWarps * a.experts;
+    int total = 0;
+    if (kOnce) {
+        const int first = exclusive(all, room);
+        total = room[32];
+        if (tid < a.experts) a.expert_start[tid] = base[tid] = first;
+        if (tid == 0) a.expert_start[a.experts] = total;
+    } else {
+        if (tid < a.experts) a.counts[(int64_t)blockIdx.x * a.experts + tid] = all;
+    }
     __syncthreads();
-    place(a, mine, own);
-    for (int64_t r = room[32] + tid; r < (int64_t)a.tokens * a.top_k; r += kThreads) a.row_token[r] = -1;
+    for (int t = mine.lo; t < mine.hi; ++t) {
+        const int64_t at = (int64_t)t * a.top_k + lane;
+        int e = -1, row = -1;
+        if (t - mine.lo < kKept) {
+#pragma unroll
+            for (int u = 0; u < kKept; ++u) e = t - mine.lo == u ? kept[u] : e;
+        } else if (lane < a.top_k) {
+            e = a.choice[at];
+        }
+        if (e >= 0) {
+            row = own[e]++;
+            if (kOnce) a.row_token[row += base[e]] = t;
+        }
+        if (lane < a.top_k) a.token_row[at] = row;
+        __syncwarp();
+    }
+    if (kOnce)
+        for (int64_t r = total + tid; r < (int64_t)a.tokens * a.top_k; r += kThreads) a.row_token[r] = -1;
 }
 
 __global__ void __launch_bounds__(kThreads, 1) place_kernel(const __grid_constant__ RouteArgs a)
 {
-    extern __shared__ int32_t count[];     // [kWarps][experts]
     __shared__ int room[33];
+    __shared__ int base[kMaxExperts], part_all[kThreads], part_before[kThreads];
     wait_for_stream();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int32_t *own = count + warp * a.experts;
-    for (int e = lane; e < a.experts; e += 32) own[e] = 0;
-    __syncwarp();
-    const Part mine = part(part({0, a.tokens}, blockIdx.x, gridDim.x), warp, kWarps);
-    for (int t = mine.lo; t < mine.hi; ++t) {
-        const int e = lane < a.top_k ? a.choice[(int64_t)t * a.top_k + lane] : -1;
-        if (e >= 0) ++own[e];
-        __syncwarp();
-    }
-    int before = 0, all = 0;               // of expert tid: in earlier blocks, in all
-    if (tid < a.experts) {
+    const int tid = threadIdx.x;
+    // several threads an expert: each has every so-manyth block's counts
+    int wide = 32;
+    while (wide < a.experts) wide *= 2;
+    const int e = tid & (wide - 1), shares = kThreads / wide;
+    int before = 0, all = 0;               // choices of expert e in earlier blocks, and in all
+    if (e < a.experts) {
 #pragma unroll 8
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-            const int c = a.counts[(int64_t)b * a.experts + tid];
+        for (int b = tid / wide; b < (int)gridDim.x; b += shares) {
+            const int c = a.counts[(int64_t)b * a.experts + e];
             all += c;
             before += b < (int)blockIdx.x ? c : 0;
         }
     }
-    const int first = exclusive(all, room);                    // (its barriers stand behind the counts of all warps)
+    part_all[tid] = all, part_before[tid] = before;
+    __syncthreads();
+    all = before = 0;
+    if (tid < a.experts)
+        for (int q = 0; q < shares; ++q) all += part_all[tid + q * wide], before += part_before[tid + q * wide];
+    const int first = exclusive(all, room);
     if (tid < a.experts) {
+        base[tid] = first + before;
         if (blockIdx.x == 0) a.expert_start[tid] = first;
-        int run = first + before;
-        for (int w = 0; w < kWarps; ++w) {
-            const int c = count[w * a.experts + tid];
-            count[w * a.experts + tid] = run;
-            run += c;
-        }
     }
     if (blockIdx.x == 0 && tid == 0) a.expert_start[a.experts] = room[32];
     __syncthreads();
-    place(a, mine, own);
+    const Part tokens = part({0, a.tokens}, blockIdx.x, gridDim.x);
+    const int hi = tokens.hi * a.top_k;    // (below 2^31 with a block's threads more)
+    for (int at = tokens.lo * a.top_k + tid; at < hi; at += kThreads) {
+        const int expert = a.choice[at];
+        if (expert < 0) continue;
+        const int row = base[expert] + a.token_row[at];
+        a.token_row[at] = row;
+        a.row_token[row] = (int)((unsigned)at / (unsigned)a.top_k);
+    }
     for (int64_t r = room[32] + (int64_t)blockIdx.x * kThreads + tid; r < (int64_t)a.tokens * a.top_k; r += (int64_t)gridDim.x * kThreads)
         a.row_token[r] = -1;
 }
@@ -326,17 +364,13 @@ int blocks_of(int tokens) { return tokens <= kAlone ? 1 : (int)((tokens + kWarps
 template <int V>
 int launch(const RouteArgs &a, int device, cudaStream_t s)
 {
-    const int shared = kWarps * a.experts * 4, blocks = blocks_of(a.tokens);
+    const int shared = (kWarps + 1) * a.experts * 4, blocks = blocks_of(a.tokens);
     static std::atomic<uint64_t> once{0}, many{0};
     const bool alone = blocks == 1;
     auto fn = alone ? choose_kernel<V, true> : choose_kernel<V, false>;
-    cudaError_t e = allow_shared((const void *)fn, kWarps * V * 32 * 4, device, alone ? once : many);
+    cudaError_t e = allow_shared((const void *)fn, (kWarps + 1) * V * 32 * 4, device, alone ? once : many);
     if (e == cudaSuccess) e = launch_early(fn, dim3((unsigned)blocks), kThreads, (size_t)shared, s, a);
-    if (e == cudaSuccess && !alone) {
-        static std::atomic<uint64_t> placed{0};
-        e = allow_shared((const void *)place_kernel, kWarps * kMaxExperts * 4, device, placed);
-        if (e == cudaSuccess) e = launch_early(place_kernel, dim3((unsigned)blocks), kThreads, (size_t)shared, s, a);
-    }
+    if (e == cudaSuccess && !alone) e = launch_early(place_kernel, dim3((unsigned)blocks), kThreads, 0, s, a);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_route");
 }
 
