@@ -26,11 +26,12 @@ struct RouteArgs {
     int64_t  ld;
     float    scale;
     int      tokens, experts, top_k, wide, sigmoid, renormalise;
+    int      of_block, of_warp;            // tokens
 };
 constexpr int kMaxExperts = SYMAR_ROUTE_MAX_EXPERTS, kMaxTop = SYMAR_ROUTE_MAX_TOP;
 constexpr int kWarps = 32, kThreads = 32 * kWarps;
 constexpr int kBlocks = 148;               // of the two launches
-constexpr int kAlone  = 128;               // tokens of one block
+constexpr int kAlone  = 48;                // tokens of one block
 static_assert(kThreads >= kMaxExperts && kMaxTop <= 32 && kMaxExperts <= 32 * 32, "");
 
 __device__ __forceinline__ float logit_of(const RouteArgs &a, int64_t row, int e)
@@ -100,33 +101,75 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int64_t row, floa
     return mine;
 }
 
-// Falling order, by Batcher's odd-even merges
-template <int V>
-__device__ __forceinline__ void sort_falling(uint32_t (&key)[V])
+// The D largest of V keys in falling order, by Batcher's odd-even merges of D at a time.
+template <int D>
+__device__ __forceinline__ void sort_falling(uint32_t *key)
 {
 #pragma unroll
-    for (int p = 1; p < V; p *= 2)
+    for (int p = 1; p < D; p *= 2)
 #pragma unroll
         for (int k = p; k >= 1; k /= 2)
 #pragma unroll
-            for (int j = k % p; j + k < V; j += 2 * k)
+            for (int j = k % p; j + k < D; j += 2 * k)
 #pragma unroll
                 for (int i = 0; i < k; ++i)
-                    if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                    if (i + j + k < D && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
                         const uint32_t x = key[i + j], y = key[i + j + k];
                         key[i + j] = max(x, y), key[i + j + k] = min(x, y);
                     }
+}
+template <int V, int D>
+__device__ __forceinline__ void largest(uint32_t (&key)[V])
+{
+    sort_falling<D>(key);
+#pragma unroll
+    for (int from = D; from < V; from += D) {
+        sort_falling<D>(key + from);
+        // the larger of the i-th largest here and the i-th smallest there are the D largest of both: they rise and fall, or fall and rise
+#pragma unroll
+        for (int i = 0; i < D; ++i) key[i] = max(key[i], key[from + D - 1 - i]);
+#pragma unroll
+        for (int k = D / 2; k >= 1; k /= 2)
+#pragma unroll
+            for (int i = 0; i < D; ++i)
+                if ((i & k) == 0) {
+                    const uint32_t x = key[i], y = key[i + k];
+                    key[i] = max(x, y), key[i + k] = min(x, y);
+                }
+    }
+}
+__device__ __forceinline__ float fast_exp(float x)             // 2^-22, and 2^-23 |x|
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+    return y;
+}
+__device__ __forceinline__ float fast_inverse(float x)         // one unit
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // Expert and weight of choice `lane` of token t (-1 and 0: none).  V: experts of a lane.
 template <int V>
 __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
 {
+    constexpr int kDeep = V < 8 ? V : 8;   // experts of a lane that are looked at; a token that wants more of one is done in binary64
+    constexpr uint32_t kPlace = V - 1;
     const int lane = threadIdx.x & 31;
     const int64_t row = t * a.ld;
+    const int left = a.experts - lane;     // expert lane + 32 i is there where 32 i < left
     float v[V];
+    if (a.wide) {
+        const float *p = static_cast<const float *>(a.logits) + row + lane;
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = lane + 32 * i < a.experts ? logit_of(a, row, lane + 32 * i) : -INFINITY;
+        for (int i = 0; i < V; ++i) v[i] = 32 * i < left ? p[32 * i] : -INFINITY;
+    } else {
+        const uint16_t *p = static_cast<const uint16_t *>(a.logits) + row + lane;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = 32 * i < left ? __uint_as_float((uint32_t)p[32 * i] << 16) : -INFINITY;
+    }
     float top = 0.0f, sum = 1.0f;
     if (!a.sigmoid) {
         float most = -INFINITY;
@@ -143,53 +186,58 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
         }
     }
     uint32_t key[V];
-    if (a.bias) {                          // (fast functions: what they round is in `margin`)
+    if (a.bias) {                          // (fast functions: what they round is in `step`)
         const float by = 1.0f / sum;
+        const float *b = a.bias + lane;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float score = a.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-v[i])) : __expf(v[i] - top) * by;
-            const bool there = lane + 32 * i < a.experts && v[i] > -INFINITY;
-            key[i] = there ? ordered(score + a.bias[lane + 32 * i]) : 0u;
+            const float score = a.sigmoid ? fast_inverse(1.0f + fast_exp(-v[i])) : fast_exp(v[i] - top) * by;
+            const float sought = 32 * i < left && v[i] > -INFINITY ? score + b[32 * i] : -INFINITY;
+            key[i] = ordered(sought + 0.0f);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = ordered(v[i]);
+        for (int i = 0; i < V; ++i) key[i] = ordered(v[i] + 0.0f);            // (-0 is 0)
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - i) : 0u;
-    sort_falling<V>(key);
-    // Two keys' errors together.  Score of a sigmoid s, x its logit: s (1 - s) (2 + 1.2 |x|) units of the fast exponential, a unit of the sum and one of
-    // the quotient, below 4 x 2^-23; of a softmax, of its largest one p: p (2 + 1.2 |x|) with p |x| < 0.4 of it, 37 additions of the sum.  Then a rounding of the
-    // sum with the bias, and the bits that the place takes.
-    const float step = a.sigmoid ? 0x1p-19f : 0x1p-17f / sum;
+    for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~kPlace) | (kPlace - i) : 0u;
+    largest<V, kDeep>(key);
     const int more = min(a.top_k + 1, a.experts);       // (the border has to be looked at)
-    int mine = -1, last_at = -1;
-    uint32_t last = 0;
-    bool near = false;
+    int mine = -1, behind = -1, deep = 0;  // choice `lane`; the one behind all; this lane's experts that were chosen
+    uint32_t found = 0, found_behind = 0;
     for (int j = 0; j < more; ++j) {
         const uint32_t most = __reduce_max_sync(0xffffffffu, key[0]);
         if (most == 0) break;
         // (the same place in several lanes: the lowest lane's is the lowest index)
-        const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == most)) - 1, at = winner + 32 * (V - 1 - (int)(most & (V - 1)));
-        if (lane == j && j < a.top_k) mine = at;
-        if (j > 0) {
-            bool close;
-            if (a.bias) {
-                const float was = unordered(last & ~(uint32_t)(V - 1)), is = unordered(most & ~(uint32_t)(V - 1));
-                close = !(was - is > step + (0x1p-21f + V * 0x1p-22f) * fmaxf(fabsf(was), fabsf(is)));
-            } else {
-                close = (last ^ most) < (uint32_t)V;
-            }
-            if (close) near |= logit_of(a, row, at) != logit_of(a, row, last_at) || (a.bias && a.bias[at] != a.bias[last_at]);
-        }
-        last = most, last_at = at;
-        if (lane == winner) {
+        const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == most)) - 1, at = winner + 32 * (int)(kPlace - (most & kPlace));
+        if (lane == j) mine = at, found = most;
+        if (j == a.top_k) behind = at, found_behind = most;
+        const bool won = lane == winner;
+        deep += won;
 #pragma unroll
-            for (int i = 0; i + 1 < V; ++i) key[i] = key[i + 1];
-            key[V - 1] = 0;
-        }
+        for (int i = 0; i + 1 < kDeep; ++i) key[i] = won ? key[i + 1] : key[i];
+        key[kDeep - 1] = won ? 0u : key[kDeep - 1];
     }
-    if (near) mine = choose_exactly<V>(a, row, top);
+    if (lane >= a.top_k) mine = -1;
+    // Neighbours in the order.  Two keys' errors together: of a sigmoid s, x its logit, s (1 - s) (2 + 1.2 |x|) units of the exponential, a unit of the sum
+    // and one of the quotient, below 4 x 2^-23; of a softmax, p its largest score, p (2 + 1.2 |x|) with p |x| < 0.4 of it, 37 additions of the sum; then a rounding
+    // of the sum with the bias, and the bits that the place takes.  Logits themselves are exact but for those bits.
+    const int next_at = __shfl_down_sync(0xffffffffu, mine, 1);
+    const uint32_t next = __shfl_down_sync(0xffffffffu, found, 1);
+    const bool border = lane == a.top_k - 1;
+    const int other = border ? behind : next_at;
+    const uint32_t under = border ? found_behind : next;
+    bool near = false;
+    if (mine >= 0 && other >= 0) {
+        if (a.bias) {
+            const float was = unordered(found & ~kPlace), is = unordered(under & ~kPlace), step = a.sigmoid ? 0x1p-19f : 0x1p-17f / sum;
+            near = !(was - is > step + (0x1p-21f + V * 0x1p-22f) * fmaxf(fabsf(was), fabsf(is)));
+        } else {
+            near = (found ^ under) <= kPlace;
+        }
+        if (near) near = logit_of(a, row, mine) != logit_of(a, row, other) || (a.bias && a.bias[mine] != a.bias[other]);
+    }
+    if (__any_sync(0xffffffffu, near || (kDeep < V && deep == kDeep))) mine = choose_exactly<V>(a, row, top);
     weight = 0.0f;
     if (mine >= 0) {
         const float logit = logit_of(a, row, mine);
@@ -208,10 +256,10 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
 struct Part {
     int lo, hi;
 };
-__device__ __forceinline__ Part part(Part of, int i, int n)
+__device__ __forceinline__ Part part(Part of, int i, int size)
 {
-    const int64_t count = of.hi - of.lo;
-    return {of.lo + (int)(count * i / n), of.lo + (int)(count * (i + 1) / n)};
+    const int lo = (int)min((int64_t)of.lo + (int64_t)i * size, (int64_t)of.hi);
+    return {lo, (int)min((int64_t)lo + size, (int64_t)of.hi)};
 }
 
 // Exclusive sums over the experts of what every thread e < experts holds; `room`: 33 words.
@@ -252,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) choose_kernel(const __grid_consta
     int32_t *own = count + warp * a.experts;
     for (int e = lane; e < a.experts; e += 32) own[e] = 0;
     __syncwarp();
-    const Part mine = part(part({0, a.tokens}, blockIdx.x, gridDim.x), warp, kWarps);
+    const Part mine = part(part({0, a.tokens}, blockIdx.x, a.of_block), warp, a.of_warp);
     int kept[kKept];
     auto take = [&](int t) {
         float weight;
@@ -346,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) place_kernel(const __grid_constan
     }
     if (blockIdx.x == 0 && tid == 0) a.expert_start[a.experts] = room[32];
     __syncthreads();
-    const Part tokens = part({0, a.tokens}, blockIdx.x, gridDim.x);
+    const Part tokens = part({0, a.tokens}, blockIdx.x, a.of_block);
     const int hi = tokens.hi * a.top_k;    // (below 2^31 with a block's threads more)
     for (int at = tokens.lo * a.top_k + tid; at < hi; at += kThreads) {
         const int expert = a.choice[at];
@@ -359,11 +407,20 @@ __global__ void __launch_bounds__(kThreads, 1) place_kernel(const __grid_constan
         a.row_token[r] = -1;
 }
 
-int blocks_of(int tokens) { return tokens <= kAlone ? 1 : (int)((tokens + kWarps - 1) / kWarps < kBlocks ? (tokens + kWarps - 1) / kWarps : kBlocks); }
+// Tokens of a block: as many for each of its warps.
+int tokens_of(int tokens)
+{
+    if (tokens <= kAlone) return tokens;
+    const int each = (tokens + kBlocks * kWarps - 1) / (kBlocks * kWarps);
+    return each * kWarps;
+}
+int blocks_of(int tokens) { return (int)(((int64_t)tokens + tokens_of(tokens) - 1) / tokens_of(tokens)); }
 
 template <int V>
-int launch(const RouteArgs &a, int device, cudaStream_t s)
+int launch(RouteArgs a, int device, cudaStream_t s)
 {
+    a.of_block = tokens_of(a.tokens);
+    a.of_warp = (a.of_block + kWarps - 1) / kWarps;
     const int shared = (kWarps + 1) * a.experts * 4, blocks = blocks_of(a.tokens);
     static std::atomic<uint64_t> once{0}, many{0};
     const bool alone = blocks == 1;
