@@ -202,42 +202,69 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key[i] ? (key[i] & ~kPlace) | (kPlace - i) : 0u;
     largest<V, kDeep>(key);
-    const int more = min(a.top_k + 1, a.experts);       // (the border has to be looked at)
-    int mine = -1, behind = -1, deep = 0;  // choice `lane`; the one behind all; this lane's experts that were chosen
-    uint32_t found = 0, found_behind = 0;
-    for (int j = 0; j < more; ++j) {
-        const uint32_t most = __reduce_max_sync(0xffffffffu, key[0]);
-        if (most == 0) break;
+    int mine = -1, deep = 0;               // choice `lane`; this lane's experts that were chosen
+    // the next choice: its expert, and its key for the caller; -1 where nothing is left
+    auto pick = [&](uint32_t &most) {
+        most = __reduce_max_sync(0xffffffffu, key[0]);
         // (the same place in several lanes: the lowest lane's is the lowest index)
-        const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == most)) - 1, at = winner + 32 * (int)(kPlace - (most & kPlace));
-        if (lane == j) mine = at, found = most;
-        if (j == a.top_k) behind = at, found_behind = most;
-        const bool won = lane == winner;
+        const int winner = __ffs(__ballot_sync(0xffffffffu, key[0] == most)) - 1;
+        const bool won = lane == winner && most != 0;
         deep += won;
 #pragma unroll
         for (int i = 0; i + 1 < kDeep; ++i) key[i] = won ? key[i + 1] : key[i];
         key[kDeep - 1] = won ? 0u : key[kDeep - 1];
+        return most ? winner + 32 * (int)(kPlace - (most & kPlace)) : -1;
+    };
+    // Two keys' errors together.  Of a sigmoid s, x its logit: s (1 - s) (2 + 1.2 |x|) units of the exponential, a unit of the sum and one of the quotient,
+    // below 4 x 2^-23; of a softmax, p its largest score: p (2 + 1.2 |x|) with p |x| < 0.4 of it, 37 additions of the sum; then a rounding of the sum with
+    // the bias, and the bits that the place takes.  Logits themselves are exact but for those bits.
+    const float step = !a.bias ? 0.0f : a.sigmoid ? 0x1p-19f : 0x1p-17f / sum;
+    auto apart = [&](uint32_t above, uint32_t below) {
+        const float was = unordered(above & ~kPlace), is = unordered(below & ~kPlace);
+        return was - is > step + (0x1p-21f + V * 0x1p-22f) * fmaxf(fabsf(was), fabsf(is));
+    };
+    uint32_t found = 0;
+    for (int j = 0; j < a.top_k; ++j) {
+        uint32_t most;
+        const int at = pick(most);
+        if (at < 0) break;
+        if (lane == j) mine = at, found = most;
     }
-    if (lane >= a.top_k) mine = -1;
-    // Neighbours in the order.  Two keys' errors together: of a sigmoid s, x its logit, s (1 - s) (2 + 1.2 |x|) units of the exponential, a unit of the sum
-    // and one of the quotient, below 4 x 2^-23; of a softmax, p its largest score, p (2 + 1.2 |x|) with p |x| < 0.4 of it, 37 additions of the sum; then a rounding
-    // of the sum with the bias, and the bits that the place takes.  Logits themselves are exact but for those bits.
-    const int next_at = __shfl_down_sync(0xffffffffu, mine, 1);
+    uint32_t under;
+    const int behind = pick(under);        // the border has to be looked at
+    const int next_at = __shfl_down_sync(0xffffffffu, mine, 1), other = lane == a.top_k - 1 ? behind : next_at;
     const uint32_t next = __shfl_down_sync(0xffffffffu, found, 1);
-    const bool border = lane == a.top_k - 1;
-    const int other = border ? behind : next_at;
-    const uint32_t under = border ? found_behind : next;
     bool near = false;
-    if (mine >= 0 && other >= 0) {
-        if (a.bias) {
-            const float was = unordered(found & ~kPlace), is = unordered(under & ~kPlace), step = a.sigmoid ? 0x1p-19f : 0x1p-17f / sum;
-            near = !(was - is > step + (0x1p-21f + V * 0x1p-22f) * fmaxf(fabsf(was), fabsf(is)));
+    if (mine >= 0 && other >= 0 && lane < a.top_k && !apart(found, lane == a.top_k - 1 ? under : next))
+        near = logit_of(a, row, mine) != logit_of(a, row, other) || (a.bias && a.bias[mine] != a.bias[other]);
+    if (__any_sync(0xffffffffu, near || (kDeep < V && deep == kDeep))) {
+        // Neighbours nearer than their errors: all that may be among the choices, in binary64.
+        const uint32_t last = __shfl_sync(0xffffffffu, found, a.top_k - 1);
+        int count = __popc(__ballot_sync(0xffffffffu, mine >= 0)), at = behind;
+        uint32_t most = under;
+        for (; at >= 0 && count < 32 && !apart(last, most); at = pick(most), ++count)
+            if (lane == count) mine = at;
+        if ((a.bias && !a.sigmoid) || (at >= 0 && !apart(last, most)) || (kDeep < V && __any_sync(0xffffffffu, deep == kDeep))) {
+            mine = choose_exactly<V>(a, row, top);
         } else {
-            near = (found ^ under) <= kPlace;
+            double exact = -INFINITY;
+            if (mine >= 0) {
+                exact = (double)logit_of(a, row, mine);
+                if (a.bias) exact = 1.0 / (1.0 + exp(-exact)) + (double)a.bias[mine];
+            }
+            int rank = 0, sorted = -1;
+            for (int j = 0; j < count; ++j) {
+                const double key_j = __shfl_sync(0xffffffffu, exact, j);
+                const int at_j = __shfl_sync(0xffffffffu, mine, j);
+                rank += key_j > exact || (key_j == exact && at_j < mine);
+            }
+            for (int j = 0; j < count; ++j) {
+                const int rank_j = __shfl_sync(0xffffffffu, rank, j), at_j = __shfl_sync(0xffffffffu, mine, j);
+                if (lane == rank_j) sorted = at_j;
+            }
+            mine = lane < a.top_k ? sorted : -1;
         }
-        if (near) near = logit_of(a, row, mine) != logit_of(a, row, other) || (a.bias && a.bias[mine] != a.bias[other]);
     }
-    if (__any_sync(0xffffffffu, near || (kDeep < V && deep == kDeep))) mine = choose_exactly<V>(a, row, top);
     weight = 0.0f;
     if (mine >= 0) {
         const float logit = logit_of(a, row, mine);
