@@ -71,6 +71,10 @@ struct Shape {
 struct Plan {
     int first[kMaxExperts + 1], tiles[kMaxExperts + 1];
 };
+// The same with the experts in another order: tiles[s] are those of the experts in places before s, expert[s] is the one in place s.
+struct OrderedPlan : Plan {
+    uint16_t expert[kMaxExperts];
+};
 // by one warp: starts that fall or leave 0 .. rows are brought into order
 __device__ __forceinline__ void make_plan(Plan &p, const int32_t *start, int experts, int rows, int nt)
 {
@@ -100,11 +104,51 @@ __device__ __forceinline__ void make_plan(Plan &p, const int32_t *start, int exp
     }
 }
 
+// An expert's tiles are of one size, in 32s: its last one's weights would cost as much for a few rows as for many.
+__device__ __forceinline__ int tile_size(int rows, int m_tiles) { return ((rows + m_tiles - 1) / m_tiles + 31) & ~31; }
+
+// By one warp: experts with large tiles first, so that the last tiles of all are short ones (4% of a prompt's products by the tiles' costs).  One pass over the
+// experts for each of eight sizes: not worth it for many of them.
+constexpr int kOrdered = 128;
+__device__ __forceinline__ void order_plan(OrderedPlan &p, int experts, int nt)
+{
+    const int lane = threadIdx.x & 31;
+    if (experts > kOrdered) {
+        for (int e = lane; e < experts; e += 32) p.expert[e] = (uint16_t)e;
+        return;
+    }
+    int place = 0, tiles = 0;
+    __syncwarp();
+    for (int size = nt; size >= 0; size -= 32) {
+        for (int e0 = 0; e0 < experts; e0 += 32) {
+            const int e = e0 + lane, rows = e < experts ? p.first[e + 1] - p.first[e] : 0, m_tiles = (rows + nt - 1) / nt;
+            const bool mine = e < experts && (rows ? tile_size(rows, m_tiles) : 0) == size;
+            const unsigned some = __ballot_sync(0xffffffffu, mine);
+            int t = mine ? m_tiles : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, t, d);
+                if (lane >= d) t += u;
+            }
+            if (mine) {
+                const int at = place + __popc(some & ((1u << lane) - 1));
+                p.expert[at] = (uint16_t)e;
+                p.tiles[at]  = tiles + t - m_tiles;
+            }
+            place += __popc(some), tiles += __shfl_sync(0xffffffffu, t, 31);
+        }
+    }
+    if (lane == 0) p.tiles[experts] = tiles;
+}
+
 struct Tile {
     int g, e, row, count, n0;              // its rows, of one expert, and its first channel
 };
+__device__ __forceinline__ int expert_at(const Plan &, int place) { return place; }
+__device__ __forceinline__ int expert_at(const OrderedPlan &p, int place) { return p.expert[place]; }
 // (tiles of `channels` results)
-__device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int tile, int channels)
+template <typename P>
+__device__ __forceinline__ Tile tile_of(const P &p, const ExpertsArgs &a, int tile, int channels)
 {
     Tile t;
     const int per = p.tiles[a.experts] * a.n_tiles;
@@ -117,48 +161,57 @@ __device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int
         if (p.tiles[mid] <= m) lo = mid;
         else hi = mid - 1;
     }
-    t.e = lo;
+    t.e = expert_at(p, lo);
     const int m_tiles = p.tiles[lo + 1] - p.tiles[lo];
     i -= p.tiles[lo] * a.n_tiles;
     const int b = i / (kBand * a.n_tiles), wide = min(kBand, m_tiles - kBand * b);
     i -= b * kBand * a.n_tiles;
-    // an expert's tiles are of one size, in 32s: its last one's weights would cost as much for a few rows as for many
-    const int rows = p.first[lo + 1] - p.first[lo], size = ((rows + m_tiles - 1) / m_tiles + 31) & ~31, m0 = (kBand * b + i % wide) * size;
-    t.row   = p.first[lo] + m0;
+    const int rows = p.first[t.e + 1] - p.first[t.e], size = tile_size(rows, m_tiles), m0 = (kBand * b + i % wide) * size;
+    t.row   = p.first[t.e] + m0;
     t.count = min(size, rows - m0);
     t.n0    = i / wide * channels;
     return t;
 }
 
-// Four neighbouring channels, from n on (fewer at the row's end): what the tile's rows share.
+// A thread's four channels: neighbours, or (rows on no boundary, where a warp's stores are to lie side by side) as many apart as there are threads to a
+// token.  What the tile's rows share of them:
 struct Channels {
     float bias[4], up_bias[4];
-    int   n, count;
+    int   in, step, n, count;              // the first one in the tile, to the next, the first one of all, how many there are
 };
-__device__ __forceinline__ Channels channels_of(const ExpertsArgs &a, const Tile &t, int n)
+__device__ __forceinline__ Channels channels_of(const ExpertsArgs &a, const Tile &t, int lane)
 {
     Channels c;
-    c.n     = n;
-    c.count = max(0, min(4, a.n - n));
+    const int threads = a.gated ? 16 : 32, i = lane & (threads - 1);
+    c.step  = a.vec_out ? 1 : threads;
+    c.in    = a.vec_out ? 4 * i : i;
+    c.n     = t.n0 + c.in;
+    c.count = max(0, min(4, (a.n - c.n + c.step - 1) / c.step));
     const __nv_bfloat16 *b = a.bias ? a.bias + t.g * a.bias_group + t.e * a.bias_expert : nullptr;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        c.bias[i]    = b && i < c.count ? __bfloat162float(b[n + i]) : 0.0f;
-        c.up_bias[i] = b && a.gated && i < c.count ? __bfloat162float(b[a.n + n + i]) : 0.0f;
+    for (int j = 0; j < 4; ++j) {
+        c.bias[j]    = b && j < c.count ? __bfloat162float(b[c.n + j * c.step]) : 0.0f;
+        c.up_bias[j] = b && a.gated && j < c.count ? __bfloat162float(b[a.n + c.n + j * c.step]) : 0.0f;
     }
     return c;
 }
+// (vec_out: rows and n on boundaries of four elements, so all four channels are there or none)
 template <typename O>
 __device__ __forceinline__ void store(const ExpertsArgs &a, const Channels &c, int g, int row, const float (&y)[4])
 {
     O *p = static_cast<O *>(a.out) + g * a.out_group + row * a.out_ld + c.n;
-    if (a.vec_out && c.count == 4) {
-        put4(p, y);
+    if (a.vec_out) {
+        if (c.count == 4) put4(p, y);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < c.count) put(p + i, y[i]);
+        for (int j = 0; j < 4; ++j)
+            if (j < c.count) put(p + j * c.step, y[j]);
     }
+}
+__device__ __forceinline__ float4 held4(const float *row, const Channels &c)
+{
+    if (c.step == 1) return *reinterpret_cast<const float4 *>(row + c.in);
+    return make_float4(row[c.in], row[c.in + c.step], row[c.in + 2 * c.step], row[c.in + 3 * c.step]);
 }
 
 // 32 tokens from c0 on of a tile: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four
@@ -167,17 +220,17 @@ template <typename O>
 __device__ __forceinline__ void finish(const ExpertsArgs &a, const Tile &t, const Channels &c, int c0, const float (&v)[16], float *hold, int ew, int side,
                                        int ch, int lane)
 {
-    const int per = a.gated ? 2 : 1, four = a.gated ? lane & 15 : lane;          // tokens that a warp finishes at once, its lanes' channels
+    const int per = a.gated ? 2 : 1;       // tokens that a warp finishes at once
 #pragma unroll
     for (int i = 0; i < 16; ++i) hold[(16 * side + i) * kRows + ch] = v[i];
     results_sync();
     const int count = min(kStep, t.count - c0);
     for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < count; i += 8 * per) {
-        const float4 y4 = reinterpret_cast<const float4 *>(hold + i * kRows)[four];
+        const float4 y4 = held4(hold + i * kRows, c);
         float y[4] = {y4.x + c.bias[0], y4.y + c.bias[1], y4.z + c.bias[2], y4.w + c.bias[3]};
         activate4(y, a.act);
         if (a.gated) {
-            const float4 u = reinterpret_cast<const float4 *>(hold + i * kRows + kHalf)[four];
+            const float4 u = held4(hold + i * kRows + kHalf, c);
             y[0] *= u.x + c.up_bias[0]; y[1] *= u.y + c.up_bias[1]; y[2] *= u.z + c.up_bias[2]; y[3] *= u.w + c.up_bias[3];
         }
         store<O>(a, c, t.g, t.row + c0 + i, y);
@@ -213,6 +266,10 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         }
         failed = bad = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+        if (!kGather) asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_at)), "n"(S::kCols) : "memory");
@@ -315,7 +372,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         uint32_t turn = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
             const Tile t = tile_of(plan, a, tile, channels);
-            const Channels c = channels_of(a, t, t.n0 + 4 * (a.gated ? lane & 15 : lane));
+            const Channels c = channels_of(a, t, lane);
             constexpr int kOwn = kWide ? NT / 2 : 1;
             float sum[kOwn];
             if (kWide) {
@@ -450,7 +507,7 @@ pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CU
 {
     using S = PairShape;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ Plan plan;
+    __shared__ OrderedPlan plan;
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
@@ -479,7 +536,10 @@ pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CU
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     wait_for_stream();
-    if (warp == 3) make_plan(plan, a.expert_start, a.experts, a.rows, kPair);
+    if (warp == 3) {
+        make_plan(plan, a.expert_start, a.experts, a.rows, kPair);
+        order_plan(plan, a.experts, kPair);
+    }
     __syncwarp();
     tc_before();
     cluster_sync();                        // the other block's barriers are there
@@ -539,7 +599,7 @@ pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CU
         for (int tile = first; tile < tiles; tile += step) {
             Tile t = tile_of(plan, a, tile, channels);
             t.n0 += (int)rank * own;
-            const Channels c = channels_of(a, t, t.n0 + 4 * (a.gated ? lane & 15 : lane));
+            const Channels c = channels_of(a, t, lane);
             if (slices > 0) {
                 (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
                 tc_after();

@@ -564,6 +564,13 @@ def _new(like, shape, dtype, index: int, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
+def _like(t, index: int, stream):
+    """An uninitialised tensor of t's shape and dtype, dense."""
+    if stream is None and t.is_contiguous():
+        return _T.empty_like(t)
+    return _new(t, t.shape, t.dtype, index, stream)
+
+
 def linear(x, w, *, bias=None, residual=None, out=None, act: str = "none", root: int = -1, out_dtype=None, status=None,
            stream=None):
     """``act(x @ w.T + bias) + residual`` (``symar_linear``).
@@ -886,8 +893,7 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
         rp, rl, rg = residual.data_ptr(), s[-2], s[0] if nd == 3 else 0
     if residual_out is None:
         if residual is not None or before is None:
-            stream_dtype = stream_dtype or dtype
-            residual_out = x.new_empty(shape, dtype=stream_dtype) if stream is None else _new(x, shape, stream_dtype, index, stream)
+            residual_out = _like(x if residual is None else residual, index, stream)
     elif residual_out.shape != shape or (n > 1 and residual_out.stride(-1) != 1) or residual_out.get_device() != index or \
             residual_out.dtype is not (stream_dtype or residual_out.dtype):
         _bad(where, f"residual_out of shape {tuple(residual_out.shape)}, {residual_out.dtype}")
@@ -897,7 +903,7 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
         op, ol, og = residual_out.data_ptr(), s[-2], s[0] if nd == 3 else 0
     if before is not None:
         if out is None:
-            out = x.new_empty(shape) if stream is None else _new(x, shape, dtype, index, stream)
+            out = _like(x, index, stream)
         s = out.stride()
         if out.shape != shape or (n > 1 and s[-1] != 1) or out.dtype is not dtype or out.get_device() != index:
             _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
@@ -937,14 +943,37 @@ class Routes:
                               ("expert_start", expert_start, (expert_start.numel(),))):
             if t.dtype is not torch.int32 or t.shape != want or t.get_device() != index or not t.is_contiguous():
                 _bad("Routes", f"{name} is a contiguous int32 tensor {list(want)} on the weights' device")
-        self._set(choice, weights, expert_start, row_token, token_row, shape, expert_start.shape[0] - 1, index)
-        if self.experts < 1:
+        if expert_start.shape[0] < 2:
             _bad("Routes", "expert_start has an entry more than there are experts")
+        self._lists = choice, expert_start, row_token, token_row
+        self._set(weights, shape, expert_start.shape[0] - 1, index, expert_start.data_ptr(), row_token.data_ptr(), token_row.data_ptr())
 
-    def _set(self, choice, weights, expert_start, row_token, token_row, shape, experts, index):
-        self.choice, self.weights, self.expert_start, self.row_token, self.token_row = choice, weights, expert_start, row_token, token_row
+    @classmethod
+    def _of(cls, whole, weights, shape, experts: int, index: int) -> "Routes":
+        """Lists side by side in one tensor: choice, row_token, token_row, expert_start (the calls go by addresses, tensors are made when they are asked for)."""
+        r = object.__new__(cls)
+        at, rows = whole.data_ptr(), shape[0] * shape[1]
+        r._lists, r._whole = None, whole
+        r._set(weights, shape, experts, index, at + 12 * rows, at + 4 * rows, at + 8 * rows)
+        return r
+
+    def _set(self, weights, shape, experts, index, start_ptr, row_token_ptr, token_row_ptr):
+        self.weights, self.experts, self.index = weights, experts, index
         self.tokens, self.top_k = shape
-        self.experts, self.index, self.rows = experts, index, self.tokens * self.top_k
+        self.rows = self.tokens * self.top_k
+        self._start_ptr, self._row_token_ptr, self._token_row_ptr = start_ptr, row_token_ptr, token_row_ptr
+
+    def _list(self, i: int):
+        if self._lists is None:
+            w, rows, shape, stride = self._whole, self.rows, (self.tokens, self.top_k), (self.top_k, 1)
+            self._lists = (w.as_strided(shape, stride, 0), w.as_strided((self.experts + 1,), (1,), 3 * rows), w.as_strided((rows,), (1,), rows),
+                           w.as_strided(shape, stride, 2 * rows))
+        return self._lists[i]
+
+    choice = property(lambda self: self._list(0))
+    expert_start = property(lambda self: self._list(1))
+    row_token = property(lambda self: self._list(2))
+    token_row = property(lambda self: self._list(3))
 
 
 def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, stream=None) -> Routes:
@@ -974,10 +1003,7 @@ def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise:
                      at + 4 * rows, at + 8 * rows, at + 4 * (start + experts + 1) if work else None, work, scale, tokens, experts, top_k, code, kind,
                      1 if renormalise else 0)
     _call(lib.symar_route, where, index, stream, byref(args))
-    got = object.__new__(Routes)
-    got._set(whole[:rows].view(tokens, top_k), weights, whole[start:start + experts + 1], whole[rows:2 * rows],
-             whole[2 * rows:start].view(tokens, top_k), shape[:1] + (top_k,), experts, index)
-    return got
+    return Routes._of(whole, weights, (tokens, top_k), experts, index)
 
 
 def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool = False, by_row: bool = False, out=None, out_dtype=None,
@@ -1026,7 +1052,7 @@ def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool =
             _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
         sp = status.data_ptr()
     args = ExpertsArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
-                       out.data_ptr(), os[-2], os[0] if ranked else 0, routes.expert_start.data_ptr(), None if by_row else routes.row_token.data_ptr(),
+                       out.data_ptr(), os[-2], os[0] if ranked else 0, routes._start_ptr, None if by_row else routes._row_token_ptr,
                        groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
     lib = _lib or load()
     if not by_row:
@@ -1062,7 +1088,7 @@ def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_d
         if residual.shape not in (want, want[-2:]) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or residual.get_device() != index:
             _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
-    args = CombineArgs(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes.token_row.data_ptr(), routes.weights.data_ptr(), rp, rl, rg,
+    args = CombineArgs(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes.weights.data_ptr(), rp, rl, rg,
                        out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
                        _dtype_code(out.dtype, where), root)
     _call((_lib or load()).symar_combine, where, index, stream, byref(args))

@@ -38,10 +38,9 @@ def lists(counts, tokens, seed=0, spare=0):
     g = torch.Generator().manual_seed(seed)
     row_token = torch.cat([torch.randint(0, tokens, (sum(counts),), generator=g), torch.full((spare,), -1)]).to(torch.int32).cuda()
     start = torch.tensor([0, *counts]).cumsum(0).to(torch.int32).cuda()
-    r = object.__new__(symar.Routes)
     one = torch.zeros(rows, 1, dtype=torch.int32, device="cuda")
-    r._set(one, one.float(), start, row_token, one, (tokens, 1), len(counts), 0)
-    r.rows = rows
+    r = symar.Routes(one, one.float(), start, row_token, one)
+    r.tokens = tokens                      # (rows of any tokens, not a choice of each)
     return r
 
 
