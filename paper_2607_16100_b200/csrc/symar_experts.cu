@@ -61,6 +61,7 @@ template <int NT, bool kWide, bool kGather>
 struct Shape {
     static constexpr int kThreads = 384 + (kGather ? kLoaders : 0);
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
+    static constexpr int kBox  = NT / 2;                                // rows of one copy of tokens
     static constexpr int kHold = kStep * kRows * 4;
     static constexpr int kStages = (212 * 1024 - kHold) / kStage;
     static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
@@ -71,84 +72,50 @@ struct Shape {
 struct Plan {
     int first[kMaxExperts + 1], tiles[kMaxExperts + 1];
 };
-// The same with the experts in another order: tiles[s] are those of the experts in places before s, expert[s] is the one in place s.
-struct OrderedPlan : Plan {
-    uint16_t expert[kMaxExperts];
-};
 // by one warp: starts that fall or leave 0 .. rows are brought into order
 __device__ __forceinline__ void make_plan(Plan &p, const int32_t *start, int experts, int rows, int nt)
 {
     const int lane = threadIdx.x & 31;
+    constexpr int kAtOnce = 4;             // loads on their way
     int most = 0, tiles = 0;               // so far
-    for (int e0 = 0; e0 <= experts; e0 += 32) {
-        const int e = e0 + lane;
-        int v = e <= experts ? max(0, min(start[e], rows)) : 0;
+    for (int e0 = 0; e0 <= experts; e0 += 32 * kAtOnce) {
+        int v[kAtOnce];
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, v, d);
-            if (lane >= d) v = max(v, u);
-        }
-        v = max(v, most);
-        int before = __shfl_up_sync(0xffffffffu, v, 1);
-        if (lane == 0) before = most;
-        // tiles of expert e - 1, which ends here
-        int t = e > 0 && e <= experts ? (v - before + nt - 1) / nt : 0;
+        for (int c = 0; c < kAtOnce; ++c) v[c] = e0 + 32 * c + lane <= experts ? max(0, min(start[e0 + 32 * c + lane], rows)) : 0;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int u = __shfl_up_sync(0xffffffffu, t, d);
-            if (lane >= d) t += u;
+        for (int c = 0; c < kAtOnce; ++c) {
+            const int e = e0 + 32 * c + lane;
+            if (e - lane > experts) break;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, v[c], d);
+                if (lane >= d) v[c] = max(v[c], u);
+            }
+            v[c] = max(v[c], most);
+            int before = __shfl_up_sync(0xffffffffu, v[c], 1);
+            if (lane == 0) before = most;
+            // tiles of expert e - 1, which ends here
+            int t = e > 0 && e <= experts ? (v[c] - before + nt - 1) / nt : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, t, d);
+                if (lane >= d) t += u;
+            }
+            t += tiles;
+            if (e <= experts) p.first[e] = v[c], p.tiles[e] = t;
+            most = __shfl_sync(0xffffffffu, v[c], 31), tiles = __shfl_sync(0xffffffffu, t, 31);
         }
-        t += tiles;
-        if (e <= experts) p.first[e] = v, p.tiles[e] = t;
-        most = __shfl_sync(0xffffffffu, v, 31), tiles = __shfl_sync(0xffffffffu, t, 31);
     }
 }
 
 // An expert's tiles are of one size, in 32s: its last one's weights would cost as much for a few rows as for many.
 __device__ __forceinline__ int tile_size(int rows, int m_tiles) { return ((rows + m_tiles - 1) / m_tiles + 31) & ~31; }
 
-// By one warp: experts with large tiles first, so that the last tiles of all are short ones (4% of a prompt's products by the tiles' costs).  One pass over the
-// experts for each of eight sizes: not worth it for many of them.
-constexpr int kOrdered = 128;
-__device__ __forceinline__ void order_plan(OrderedPlan &p, int experts, int nt)
-{
-    const int lane = threadIdx.x & 31;
-    if (experts > kOrdered) {
-        for (int e = lane; e < experts; e += 32) p.expert[e] = (uint16_t)e;
-        return;
-    }
-    int place = 0, tiles = 0;
-    __syncwarp();
-    for (int size = nt; size >= 0; size -= 32) {
-        for (int e0 = 0; e0 < experts; e0 += 32) {
-            const int e = e0 + lane, rows = e < experts ? p.first[e + 1] - p.first[e] : 0, m_tiles = (rows + nt - 1) / nt;
-            const bool mine = e < experts && (rows ? tile_size(rows, m_tiles) : 0) == size;
-            const unsigned some = __ballot_sync(0xffffffffu, mine);
-            int t = mine ? m_tiles : 0;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, t, d);
-                if (lane >= d) t += u;
-            }
-            if (mine) {
-                const int at = place + __popc(some & ((1u << lane) - 1));
-                p.expert[at] = (uint16_t)e;
-                p.tiles[at]  = tiles + t - m_tiles;
-            }
-            place += __popc(some), tiles += __shfl_sync(0xffffffffu, t, 31);
-        }
-    }
-    if (lane == 0) p.tiles[experts] = tiles;
-}
-
 struct Tile {
     int g, e, row, count, n0;              // its rows, of one expert, and its first channel
 };
-__device__ __forceinline__ int expert_at(const Plan &, int place) { return place; }
-__device__ __forceinline__ int expert_at(const OrderedPlan &p, int place) { return p.expert[place]; }
 // (tiles of `channels` results)
-template <typename P>
-__device__ __forceinline__ Tile tile_of(const P &p, const ExpertsArgs &a, int tile, int channels)
+__device__ __forceinline__ Tile tile_of(const Plan &p, const ExpertsArgs &a, int tile, int channels)
 {
     Tile t;
     const int per = p.tiles[a.experts] * a.n_tiles;
@@ -161,7 +128,7 @@ __device__ __forceinline__ Tile tile_of(const P &p, const ExpertsArgs &a, int ti
         if (p.tiles[mid] <= m) lo = mid;
         else hi = mid - 1;
     }
-    t.e = expert_at(p, lo);
+    t.e = lo;
     const int m_tiles = p.tiles[lo + 1] - p.tiles[lo];
     i -= p.tiles[lo] * a.n_tiles;
     const int b = i / (kBand * a.n_tiles), wide = min(kBand, m_tiles - kBand * b);
@@ -284,19 +251,21 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int channels = a.gated ? kHalf : kRows, slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
 
     if (warp == 0 && elected()) {
-        // ---- producer: one thread.  A copy's own cost is what counts: a box of a whole tile's rows, whatever of them is used (boxes of 32 rows:
-        // 303 us instead of 203 for 16384 rows x 2048 x 4096), and no gathering by the copy engine (four rows an instruction: 1090 us)
+        // ---- producer: one thread.  A copy's own cost counts as well as its bytes: one or two of half a tile's rows (eight of 32: 303 us instead
+        // of 203 for 16384 rows x 2048 x 4096), and no gathering by the copy engine (four rows an instruction: 1090 us)
         int st = 0, round = 0;
         for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
             const Tile t = tile_of(plan, a, tile, channels);
             const int second = t.n0 + (a.gated ? a.n : kHalf), wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
+            const bool two = t.count > S::kBox;
             for (int ks = 0; ks < slices; ++ks) {
                 if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
-                bar_expect(bar, S::kA + (kGather ? 0 : S::kB));
+                bar_expect(bar, S::kA + (kGather ? 0 : two ? S::kB : S::kB / 2));
                 tma_load4(at, &wmap, ks * kSlice, t.n0, t.e, wg, bar);
                 tma_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, wg, bar);
                 if (!kGather) tma_load(at + S::kA, &xmap, ks * kSlice, t.row, xg, bar);
+                if (!kGather && two) tma_load(at + S::kA + S::kB / 2, &xmap, ks * kSlice, t.row + S::kBox, xg, bar);
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
@@ -507,7 +476,7 @@ pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CU
 {
     using S = PairShape;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ OrderedPlan plan;
+    __shared__ Plan plan;
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
@@ -536,10 +505,7 @@ pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CU
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     wait_for_stream();
-    if (warp == 3) {
-        make_plan(plan, a.expert_start, a.experts, a.rows, kPair);
-        order_plan(plan, a.experts, kPair);
-    }
+    if (warp == 3) make_plan(plan, a.expert_start, a.experts, a.rows, kPair);
     __syncwarp();
     tc_before();
     cluster_sync();                        // the other block's barriers are there
@@ -742,11 +708,15 @@ int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap,
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
 }
 
-// Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.
+// Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.  Pairs take many
+// rows where their tiles are enough for all multiprocessors (a product's start costs them 3 us more: 1000 rows x 128 x 520 of seven experts 13.3 us instead
+// of 9.9; with 1003 channels on two ranks 17.9 instead of 19.3).
 int tile_tokens(const symar_experts_t &p)
 {
     const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = used > 0 ? p.rows / used : 0;
-    return each <= 32 ? 64 : (each <= 96 || p.out_dtype == SYMAR_F32 ? 128 : kPair);
+    const int64_t tiles = used * p.groups * (p.gated ? (p.n + kHalf - 1) / kHalf : (p.n + kRows - 1) / kRows);
+    if (each <= 32) return 64;
+    return each <= 96 || tiles < 148 || p.out_dtype == SYMAR_F32 ? 128 : kPair;
 }
 bool in_order_first(const symar_experts_t &p) { return p.row_token && p.k > 0 && tile_tokens(p) == kPair; }
 int64_t pieces_of(int k) { return ((int64_t)k + 7) / 8; }
@@ -822,7 +792,7 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
             x_extent[1] = p.rows, x_stride[1] = 8 * pieces_of(p.k), x_stride[2] = x_stride[1] * p.rows;
             ok = x_stride[2] < (1ll << 39);
         }
-        if (ok && (!p.row_token || first)) ok = encode(&xmap, x, 3, x_extent, x_stride, nt < kPair ? nt : kPair / 2);
+        if (ok && (!p.row_token || first)) ok = encode(&xmap, x, 3, x_extent, x_stride, nt / 2);
         if (!ok || !encode(&wmap, p.w, 4, w_extent, w_stride, kHalf)) return SYMAR_ERR_UNSUPPORTED;
     }
     int rc = device_info(&d);
