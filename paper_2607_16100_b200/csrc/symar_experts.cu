@@ -57,11 +57,14 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
 // What other threads' copies have written, seen by the tensor cores behind this.
 __device__ __forceinline__ void copies_seen() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// rows of one copy of a tile's tokens
+constexpr int box_of(int nt) { return nt == 64 ? 32 : nt == 128 ? 128 : nt / 2; }
+
 template <int NT, bool kWide, bool kGather>
 struct Shape {
     static constexpr int kThreads = 384 + (kGather ? kLoaders : 0);
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
-    static constexpr int kBox  = NT / 2;                                // rows of one copy of tokens
+    static constexpr int kBox  = box_of(NT);
     static constexpr int kHold = kStep * kRows * 4;
     static constexpr int kStages = (212 * 1024 - kHold) / kStage;
     static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
@@ -251,21 +254,22 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     const int channels = a.gated ? kHalf : kRows, slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
 
     if (warp == 0 && elected()) {
-        // ---- producer: one thread.  A copy's own cost counts as well as its bytes: one or two of half a tile's rows (eight of 32: 303 us instead
-        // of 203 for 16384 rows x 2048 x 4096), and no gathering by the copy engine (four rows an instruction: 1090 us)
+        // ---- producer: one thread.  A copy's own cost counts beside its bytes: one for the tokens, two where half of a small tile's are wanted (boxes of 32
+        // rows: 303 us instead of 203 for 16384 rows x 2048 x 4096; two boxes instead of one for 128 rows 13.3 instead of 9.9 us for 1000 x 128 x 520), and no
+        // gathering by the copy engine (four rows an instruction: 1090 instead of 203 us).  The weights' two halves in one copy of five axes were slower (15.0 us).
         int st = 0, round = 0;
         for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
             const Tile t = tile_of(plan, a, tile, channels);
             const int second = t.n0 + (a.gated ? a.n : kHalf), wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
-            const bool two = t.count > S::kBox;
+            const bool two = NT > S::kBox && t.count > S::kBox;
             for (int ks = 0; ks < slices; ++ks) {
                 if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
-                bar_expect(bar, S::kA + (kGather ? 0 : two ? S::kB : S::kB / 2));
+                bar_expect(bar, S::kA + (kGather ? 0 : two ? S::kB : S::kBox * kSlice * 2));
                 tma_load4(at, &wmap, ks * kSlice, t.n0, t.e, wg, bar);
                 tma_load4(at + S::kA / 2, &wmap, ks * kSlice, second, t.e, wg, bar);
                 if (!kGather) tma_load(at + S::kA, &xmap, ks * kSlice, t.row, xg, bar);
-                if (!kGather && two) tma_load(at + S::kA + S::kB / 2, &xmap, ks * kSlice, t.row + S::kBox, xg, bar);
+                if (!kGather && two) tma_load(at + S::kA + S::kBox * kSlice * 2, &xmap, ks * kSlice, t.row + S::kBox, xg, bar);
                 if (++st == S::kStages) st = 0, ++round;
             }
         }
@@ -714,7 +718,7 @@ int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap,
 int tile_tokens(const symar_experts_t &p)
 {
     const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = used > 0 ? p.rows / used : 0;
-    const int64_t tiles = used * p.groups * (p.gated ? (p.n + kHalf - 1) / kHalf : (p.n + kRows - 1) / kRows);
+    const int64_t tiles = (int64_t)p.groups * (p.gated ? (p.n + kHalf - 1) / kHalf : (p.n + kRows - 1) / kRows) * (p.rows / kPair + used);
     if (each <= 32) return 64;
     return each <= 96 || tiles < 148 || p.out_dtype == SYMAR_F32 ? 128 : kPair;
 }
@@ -792,7 +796,7 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
             x_extent[1] = p.rows, x_stride[1] = 8 * pieces_of(p.k), x_stride[2] = x_stride[1] * p.rows;
             ok = x_stride[2] < (1ll << 39);
         }
-        if (ok && (!p.row_token || first)) ok = encode(&xmap, x, 3, x_extent, x_stride, nt / 2);
+        if (ok && (!p.row_token || first)) ok = encode(&xmap, x, 3, x_extent, x_stride, box_of(nt));
         if (!ok || !encode(&wmap, p.w, 4, w_extent, w_stride, kHalf)) return SYMAR_ERR_UNSUPPORTED;
     }
     int rc = device_info(&d);
