@@ -623,27 +623,28 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
     int count = 0;                         // rows of somebody (see make_plan)
     for (int e = lane; e <= a.experts; e += 32) count = max(count, a.expert_start[e]);
     count = min(__reduce_max_sync(0xffffffffu, count), a.rows);
-    const int warps = kGatherThreads / 32 * (int)gridDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * (kGatherThreads / 32) + (threadIdx.x >> 5); i < (int64_t)a.groups * a.rows; i += warps) {
-        const int g = (int)(i / a.rows), row = (int)(i - (int64_t)g * a.rows);
-        if (row >= count) continue;
+    // a warp's unit: 128 pieces of a row, four of them a lane
+    const int parts = (a.pieces + 127) / 128, whole = a.k / 8;
+    const int64_t units = (int64_t)a.groups * count * parts;
+    for (int64_t i = (int64_t)blockIdx.x * (kGatherThreads / 32) + (threadIdx.x >> 5); i < units; i += (int64_t)(kGatherThreads / 32) * gridDim.x) {
+        const int64_t cell = i / parts;
+        const int c0 = (int)(i - cell * parts) * 128 + lane, g = (int)(cell / count), row = (int)(cell - (int64_t)g * count);
         const int token = a.row_token[row];
         const bool there = token >= 0 && token < a.x_rows;
-        if (!there && lane == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_INVAL);
+        if (!there && c0 == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_INVAL);
         const unsigned char *x = a.x + g * a.x_group + (there ? token : 0) * a.x_ld;
-        uint4 *out = reinterpret_cast<uint4 *>(a.out) + i * a.pieces;
-        const int whole = a.k / 8;
-        for (int c0 = 0; c0 < whole; c0 += 4 * 32) {
-            uint4 v[4];
+        uint4 *out = reinterpret_cast<uint4 *>(a.out) + ((int64_t)g * a.rows + row) * a.pieces;
+        uint4 v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c0 + 32 * j + lane < whole) v[j] = *reinterpret_cast<const uint4 *>(x + 16ll * (c0 + 32 * j + lane));
+        for (int j = 0; j < 4; ++j)
+            if (c0 + 32 * j < whole) v[j] = *reinterpret_cast<const uint4 *>(x + 16ll * (c0 + 32 * j));
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (c0 + 32 * j + lane < whole) out[c0 + 32 * j + lane] = there ? v[j] : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) {
+            const int c = c0 + 32 * j;
+            if (c < whole) out[c] = there ? v[j] : make_uint4(0, 0, 0, 0);
+            else if (c < a.pieces)             // the last one in part
+                for (int e = 8 * c; e < a.k; ++e) reinterpret_cast<uint16_t *>(out)[e] = there ? reinterpret_cast<const uint16_t *>(x)[e] : 0;
         }
-        for (int c = 8 * whole + lane; c < a.k; c += 32)
-            reinterpret_cast<uint16_t *>(out)[c] = there ? reinterpret_cast<const uint16_t *>(x)[c] : 0;
     }
 }
 
@@ -805,7 +806,7 @@ extern "C" int symar_experts(const symar_experts_t *args, void *cuda_stream)
     if (nt == 64) return wide ? launch_as<64, true>(a, wmap, xmap, d, s) : launch_as<64, false>(a, wmap, xmap, d, s);
     if (nt == 128) return wide ? launch_as<128, true>(a, wmap, xmap, d, s) : launch_as<128, false>(a, wmap, xmap, d, s);
     if (first) {
-        const int64_t blocks = ((int64_t)ga.groups * ga.rows + kGatherThreads / 32 - 1) / (kGatherThreads / 32), most = 8ll * d.sms;
+        const int64_t blocks = ((int64_t)ga.groups * ga.rows * ((ga.pieces + 127) / 128) + kGatherThreads / 32 - 1) / (kGatherThreads / 32), most = 8ll * d.sms;
         const cudaError_t e = launch_early(gather_kernel, dim3((unsigned)(blocks < most ? blocks : most)), kGatherThreads, 0, s, ga);
         if (e != cudaSuccess) return cuda_fail(e, "symar_experts");
     }
