@@ -28,6 +28,7 @@ struct ExpertsArgs {
     int      x_shared, w_shared;           // one for all groups
     int      n_tiles;                      // of 128 channels, or 64 gated ones
     int      vec_out;
+    int      split;                        // blocks of a cluster that share a tile's k
     unsigned *status;
 };
 
@@ -57,15 +58,64 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar)
 // What other threads' copies have written, seen by the tensor cores behind this.
 __device__ __forceinline__ void copies_seen() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ---- clusters ----
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+    return there;
+}
+// (An address of at_rank.  What it orders is tensor memory alone, by tcgen05's own fences; a release of what the thread has stored would wait for
+// its results on their way.)
+__device__ __forceinline__ void far_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// A thread's wait for what other blocks of its cluster do
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    const uint64_t t0 = now_ns();
+    for (int i = 1;; ++i) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if (i % 256 == 0 && (*failed || now_ns() - t0 > kWaitNs)) {
+            *failed = 1;
+            return false;
+        }
+    }
+}
+// (What the block has read of its shared memory is read before: the others may write there again.)
+__device__ __forceinline__ void used_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// a word into another block's shared memory (addresses of at_rank), counted by that block's barrier
+__device__ __forceinline__ void far_store(uint32_t at, float v, uint32_t bar)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(at), "r"(__float_as_uint(v)), "r"(bar) : "memory");
+}
+
 // rows of one copy of a tile's tokens
 constexpr int box_of(int nt) { return nt == 64 ? 32 : nt == 128 ? 128 : nt / 2; }
 
-template <int NT, bool kWide, bool kGather>
+template <int NT, bool kWide, bool kGather, bool kSplit>
 struct Shape {
     static constexpr int kThreads = 384 + (kGather ? kLoaders : 0);
     static constexpr int kA = kRows * kSlice * 2, kB = NT * kSlice * 2, kStage = kA + kB;
     static constexpr int kBox  = box_of(NT);
-    static constexpr int kHold = kStep * kRows * 4;
+    static constexpr int kHold = (kSplit ? NT : kStep) * kRows * 4;
     static constexpr int kStages = (212 * 1024 - kHold) / kStage;
     static constexpr int kBytes = kStages * kStage + kHold + 1024;      // (the ring starts on a 1 KiB boundary)
     static constexpr int kCols  = 2 * NT;                               // two accumulators
@@ -183,7 +233,17 @@ __device__ __forceinline__ float4 held4(const float *row, const Channels &c)
     if (c.step == 1) return *reinterpret_cast<const float4 *>(row + c.in);
     return make_float4(row[c.in], row[c.in + c.step], row[c.in + 2 * c.step], row[c.in + 3 * c.step]);
 }
-
+// What follows the sums of four channels of a tile's token.
+template <typename O>
+__device__ __forceinline__ void finish_row(const ExpertsArgs &a, const Tile &t, const Channels &c, int token, float4 sum, float4 up)
+{
+    float y[4] = {sum.x + c.bias[0], sum.y + c.bias[1], sum.z + c.bias[2], sum.w + c.bias[3]};
+    activate4(y, a.act);
+    if (a.gated) {
+        y[0] *= up.x + c.up_bias[0]; y[1] *= up.y + c.up_bias[1]; y[2] *= up.z + c.up_bias[2]; y[3] *= up.w + c.up_bias[3];
+    }
+    store<O>(a, c, t.g, t.row + token, y);
+}
 // 32 tokens from c0 on of a tile: out of tensor memory a thread holds one weights' row of many tokens; by way of shared memory it gets four
 // neighbouring channels of one token, and up's beside the gate's.
 template <typename O>
@@ -196,33 +256,28 @@ __device__ __forceinline__ void finish(const ExpertsArgs &a, const Tile &t, cons
     results_sync();
     const int count = min(kStep, t.count - c0);
     for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < count; i += 8 * per) {
-        const float4 y4 = held4(hold + i * kRows, c);
-        float y[4] = {y4.x + c.bias[0], y4.y + c.bias[1], y4.z + c.bias[2], y4.w + c.bias[3]};
-        activate4(y, a.act);
-        if (a.gated) {
-            const float4 u = held4(hold + i * kRows + kHalf, c);
-            y[0] *= u.x + c.up_bias[0]; y[1] *= u.y + c.up_bias[1]; y[2] *= u.z + c.up_bias[2]; y[3] *= u.w + c.up_bias[3];
-        }
-        store<O>(a, c, t.g, t.row + c0 + i, y);
+        const float4 y = held4(hold + i * kRows, c);
+        finish_row<O>(a, t, c, c0 + i, y, a.gated ? held4(hold + i * kRows + kHalf, c) : y);
     }
     results_sync();
 }
 
-template <int NT, bool kWide, bool kGather>
-__global__ void __launch_bounds__(Shape<NT, kWide, kGather>::kThreads, 1)
+template <int NT, bool kWide, bool kGather, bool kSplit>
+__global__ void __launch_bounds__(Shape<NT, kWide, kGather, kSplit>::kThreads, 1)
 experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ ExpertsArgs a)
 {
-    using S = Shape<NT, kWide, kGather>;
+    using S = Shape<NT, kWide, kGather, kSplit>;
     using O = typename std::conditional<kWide, float, __nv_bfloat16>::type;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Plan plan;
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 4];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 6];
     __shared__ uint32_t tmem_at;
     __shared__ int failed, bad;
     unsigned char *ring = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
     float *hold = reinterpret_cast<float *>(ring + S::kStages * S::kStage);
     const uint32_t ring_addr = smem_addr(ring);
     const uint32_t full = smem_addr(bars), empty = full + 8 * S::kStages, acc_full = empty + 8 * S::kStages, acc_empty = acc_full + 16;
+    const uint32_t parts_here = acc_empty + 16, parts_used = parts_here + 8;      // of a tile that several blocks share
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
@@ -234,6 +289,8 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             bar_init(acc_full + 8 * i, 1);
             bar_init(acc_empty + 8 * i, 256);
         }
+        bar_init(parts_here, 1);
+        bar_init(parts_used, kSplit ? a.split : 1);
         failed = bad = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -248,21 +305,30 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
     wait_for_stream();
     if (warp == 3) make_plan(plan, a.expert_start, a.experts, a.rows, NT);
     tc_before();
-    __syncthreads();
+    if (kSplit) {
+        __syncwarp();
+        cluster_sync();                    // the other blocks' barriers are there
+    } else {
+        __syncthreads();
+    }
     tc_after();
     const uint32_t tmem = tmem_at;
     const int channels = a.gated ? kHalf : kRows, slices = (a.k + kSlice - 1) / kSlice, tiles = a.groups * plan.tiles[a.experts] * a.n_tiles;
+    // this block's slices of every one of its tiles: all of k, or its part where a cluster shares the tile
+    const int rank = kSplit ? (int)blockIdx.x % a.split : 0, first = kSplit ? (int)blockIdx.x / a.split : (int)blockIdx.x;
+    const int step = kSplit ? (int)gridDim.x / a.split : (int)gridDim.x;
+    const int k_lo = kSplit ? (int)((int64_t)slices * rank / a.split) : 0, k_hi = kSplit ? (int)((int64_t)slices * (rank + 1) / a.split) : slices;
 
     if (warp == 0 && elected()) {
         // ---- producer: one thread.  A copy's own cost counts beside its bytes: one for the tokens, two where half of a small tile's are wanted (boxes of 32
         // rows: 303 us instead of 203 for 16384 rows x 2048 x 4096; two boxes instead of one for 128 rows 13.3 instead of 9.9 us for 1000 x 128 x 520), and no
         // gathering by the copy engine (four rows an instruction: 1090 instead of 203 us).  The weights' two halves in one copy of five axes were slower (15.0 us).
         int st = 0, round = 0;
-        for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
+        for (int tile = first; tile < tiles && slices > 0; tile += step) {
             const Tile t = tile_of(plan, a, tile, channels);
             const int second = t.n0 + (a.gated ? a.n : kHalf), wg = a.w_shared ? 0 : t.g, xg = a.x_shared ? 0 : t.g;
             const bool two = NT > S::kBox && t.count > S::kBox;
-            for (int ks = 0; ks < slices; ++ks) {
+            for (int ks = k_lo; ks < k_hi; ++ks) {
                 if (round > 0 && !bar_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const uint32_t at = ring_addr + st * S::kStage, bar = full + 8 * st;
                 bar_expect(bar, S::kA + (kGather ? 0 : two ? S::kB : S::kBox * kSlice * 2));
@@ -287,8 +353,8 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
 #pragma unroll
             for (int j = 0; j < kOf; ++j) next[j] = r + 16 * j < t.count ? a.row_token[t.row + r + 16 * j] : -1;      // (columns behind the last are zeros)
         };
-        tokens_of(blockIdx.x);
-        for (int tile = blockIdx.x; tile < tiles && slices > 0; tile += gridDim.x) {
+        tokens_of(first);
+        for (int tile = first; tile < tiles && slices > 0; tile += step) {
             const __nv_bfloat16 *x = a.x + (a.x_shared ? 0 : t.g * a.x_group);
             const int cols = (t.count + 15) & ~15;
 #pragma unroll
@@ -296,8 +362,8 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 token[j] = next[j];
                 if (r + 16 * j < t.count && (uint32_t)token[j] >= (uint32_t)a.x_rows) token[j] = -1, bad = 1;
             }
-            tokens_of(tile + gridDim.x);
-            for (int ks = 0; ks < slices; ++ks) {
+            tokens_of(tile + step);
+            for (int ks = k_lo; ks < k_hi; ++ks) {
                 if (round > 0 && !warp_wait(empty + 8 * st, (round - 1) & 1, &failed)) goto done;
                 const int k0 = ks * kSlice + c * 8;
                 const uint32_t count = (uint32_t)max(0, min(8, a.k - k0)) * 2, dst = ring_addr + st * S::kStage + S::kA + r * 128 + ((c ^ (r & 7)) << 4);
@@ -316,10 +382,10 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         constexpr uint32_t kHow = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows / 16) << 24);
         int st = 0, round = 0;
         uint32_t turn = 0;                              // accumulators filled so far
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        for (int tile = first; tile < tiles; tile += step) {
             const uint32_t how = kHow | (uint32_t)((tile_of(plan, a, tile, channels).count + 15) / 16 * 2) << 17;
-            for (int ks = 0; ks < slices;) {
-                const int to = kWide ? min(ks + kChunk, slices) : slices;
+            for (int ks = k_lo; ks < k_hi;) {
+                const int to = kWide ? min(ks + kChunk, k_hi) : k_hi;
                 const uint32_t buf = turn & 1, acc = tmem + buf * NT;
                 if (turn >= 2 && !bar_wait(acc_empty + 8 * buf, ((turn >> 1) - 1) & 1, &failed)) goto done;
                 tc_after();
@@ -342,8 +408,8 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         // ---- results ----
         const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)quarter << 21;
-        uint32_t turn = 0;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        uint32_t turn = 0, shared_tiles = 0;
+        for (int tile = first; tile < tiles; tile += step) {
             const Tile t = tile_of(plan, a, tile, channels);
             const Channels c = channels_of(a, t, lane);
             constexpr int kOwn = kWide ? NT / 2 : 1;
@@ -351,7 +417,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             if (kWide) {
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) sum[i] = 0.0f;
-                for (int ks = 0; ks < slices; ks += kChunk, ++turn) {
+                for (int ks = k_lo; ks < k_hi; ks += kChunk, ++turn) {
                     const uint32_t buf = turn & 1;
                     (void)warp_wait(acc_full + 8 * buf, (turn >> 1) & 1, &failed);     // (given up: on with what is there, the barriers count all)
                     tc_after();
@@ -370,6 +436,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);
                 tc_after();
             }
+            if (kSplit && shared_tiles > 0) (void)pair_wait(parts_used, (shared_tiles - 1) & 1, &failed);      // every block has used its parts of the tile before
 #pragma unroll
             for (int c0 = 0; c0 < NT; c0 += kStep) {
                 if (c0 >= t.count) break;
@@ -386,10 +453,43 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                         bar_arrive(acc_empty + 8 * (turn & 1));
                     }
                 }
-                finish<O>(a, t, c, c0, v, hold, ew, side, ch, lane);
+                if (kSplit) {
+                    // token i's sums are added up by block i % split, as its token i / split
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int token = c0 + 16 * side + i, to = token % a.split;
+                        if (token >= t.count) break;
+                        far_store(at_rank(smem_addr(hold + ((token / a.split) * a.split + rank) * kRows + ch), to), v[i], at_rank(parts_here, to));
+                    }
+                } else {
+                    finish<O>(a, t, c, c0, v, hold, ew, side, ch, lane);
+                }
+            }
+            if (kSplit) {
+                const int own = (t.count - rank + a.split - 1) / a.split;      // (0 or less: none)
+                if (tid == 128) bar_expect(parts_here, (uint32_t)(max(own, 0) * a.split * kRows * 4));
+                (void)pair_wait(parts_here, shared_tiles & 1, &failed);
+                const int per = a.gated ? 2 : 1;
+                for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < own; i += 8 * per) {
+                    float4 y4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), u = y4;
+                    for (int r = 0; r < a.split; ++r) {
+                        const float *row = hold + (i * a.split + r) * kRows;
+                        const float4 y = held4(row, c);
+                        y4.x += y.x; y4.y += y.y; y4.z += y.z; y4.w += y.w;
+                        if (a.gated) {
+                            const float4 w = held4(row + kHalf, c);
+                            u.x += w.x; u.y += w.y; u.z += w.z; u.w += w.w;
+                        }
+                    }
+                    finish_row<O>(a, t, c, rank + i * a.split, y4, u);
+                }
+                results_sync();
+                if (tid < 128 + a.split) used_arrive(at_rank(parts_used, (uint32_t)(tid - 128)));
+                ++shared_tiles;
             }
             if (!kWide && slices > 0) ++turn;
         }
+        if (kSplit && shared_tiles > 0) (void)pair_wait(parts_used, (shared_tiles - 1) & 1, &failed);
     }
 done:
     __syncwarp();
@@ -399,6 +499,10 @@ done:
         // copies and products may still be in flight: give them time to end before the memory is let go
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         __syncthreads();
+    }
+    if (kSplit) {
+        __syncwarp();
+        cluster_sync();                    // no block's memory is in use any more
     }
     if (tid == 0 && a.status && (failed || bad)) atomicCAS(a.status, 0u, (unsigned)(failed ? SYMAR_ERR_TIMEOUT : SYMAR_ERR_INVAL));
     tc_after();
@@ -411,43 +515,6 @@ done:
 // half of the tokens, both read both halves of the tokens, and the first block's thread issues the products of both.  A block's copies are a third
 // fewer for the same products.  Rows by token are put in order by a kernel of their own first: gathered into the ring as above they come at 40 bytes a
 // cycle at best (16384 rows x 2 x 1024 x 4096: 304 us with four gathering warps a block, FIGURE with the rows in order beforehand, FIGURE2 where they are).
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
-{
-    uint32_t there;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-    return there;
-}
-// (An address of at_rank.  What it orders is tensor memory alone, by tcgen05's own fences; a release of what the thread has stored would wait for
-// its results on their way.)
-__device__ __forceinline__ void far_arrive(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// A thread's wait for arrivals of both blocks
-__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int *failed)
-{
-    const uint64_t t0 = now_ns();
-    for (int i = 1;; ++i) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
-        if (i % 256 == 0 && (*failed || now_ns() - t0 > kWaitNs)) {
-            *failed = 1;
-            return false;
-        }
-    }
-}
 __device__ __forceinline__ void pair_load3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -670,22 +737,58 @@ bool encode(CUtensorMap *map, const void *p, int axes, const int64_t *extent, co
 // Whether the copy engine can walk an axis: steps of 16 bytes, below 2^40 of them.
 bool engine_axis(int64_t extent, int64_t stride) { return extent <= 1 || (stride >= 8 && stride % 8 == 0 && stride < (1ll << 39)); }
 
-template <int NT, bool kWide, bool kGather>
-int launch(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)
+// Clusters of s blocks that run at once.  The chip's groups of multiprocessors are no multiples of eight: of sixteen clusters of eight two waited for the
+// others (16 tiles over k = 4672 17.6 us instead of 9.4 for 14), so a few less are counted on.
+int clusters_of(int sms, int s) { return s == 8 ? sms / 8 * 3 / 4 : s == 4 ? sms / 4 * 9 / 10 : sms / s; }
+template <int NT, bool kWide, bool kGather, bool kSplit>
+int launch(const ExpertsArgs &a, int tiles, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)
 {
-    using S = Shape<NT, kWide, kGather>;
-    auto fn = experts_kernel<NT, kWide, kGather>;
-    const int64_t used = a.experts < a.rows ? a.experts : a.rows, tiles = (int64_t)a.groups * a.n_tiles * (a.rows / NT + used);      // at most
-    if (tiles > kMost || (int64_t)a.n_tiles * kBand > kMost) return SYMAR_ERR_UNSUPPORTED;
+    using S = Shape<NT, kWide, kGather, kSplit>;
+    auto fn = experts_kernel<NT, kWide, kGather, kSplit>;
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow_shared((const void *)fn, S::kBytes, d.id, allowed);
-    if (e == cudaSuccess) e = launch_early(fn, dim3((unsigned)(tiles < d.sms ? tiles : d.sms)), S::kThreads, S::kBytes, stream, wmap, xmap, a);
+    if (e != cudaSuccess) return cuda_fail(e, "symar_experts");
+    const int most = clusters_of(d.sms, a.split);
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim  = dim3((unsigned)(a.split * (tiles < most ? tiles : most)));
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kBytes;
+    cfg.stream   = stream;
+    cfg.attrs    = attr;
+    cfg.numAttrs = kSplit ? 2 : 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // (see wait_for_stream)
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    e = cudaLaunchKernelEx(&cfg, fn, wmap, xmap, a);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
 }
-template <int NT, bool kWide>
-int launch_as(const ExpertsArgs &a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t s)
+// Blocks that share a tile's k, where tiles are few: what a multiprocessor does then in slices, an exchange of parts counted as four.
+int split_of(int tiles, int slices, int sms)
 {
-    return a.row_token ? launch<NT, kWide, true>(a, wmap, xmap, d, s) : launch<NT, kWide, false>(a, wmap, xmap, d, s);
+    int best = 1;
+    int64_t least = (int64_t)((tiles + sms - 1) / sms) * (slices + 1);
+    for (int s = 2; s <= 8; s *= 2) {
+        const int clusters = clusters_of(sms, s);
+        const int64_t cost = (int64_t)((tiles + clusters - 1) / clusters) * ((slices + s - 1) / s + 4);
+        if (slices >= 2 * s && cost < least) least = cost, best = s;
+    }
+    return best;
+}
+template <int NT, bool kWide>
+int launch_as(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t s)
+{
+    const int64_t used = a.experts < a.rows ? a.experts : a.rows, tiles = (int64_t)a.groups * a.n_tiles * (a.rows / NT + used);      // at most
+    if (tiles > kMost || (int64_t)a.n_tiles * kBand > kMost) return SYMAR_ERR_UNSUPPORTED;
+    a.split = 1;
+    if constexpr (NT == 64) {
+        a.split = split_of((int)tiles, (a.k + kSlice - 1) / kSlice, d.sms);
+        if (a.split > 1)
+            return a.row_token ? launch<NT, kWide, true, true>(a, (int)tiles, wmap, xmap, d, s) : launch<NT, kWide, false, true>(a, (int)tiles, wmap, xmap, d, s);
+    }
+    return a.row_token ? launch<NT, kWide, true, false>(a, (int)tiles, wmap, xmap, d, s) : launch<NT, kWide, false, false>(a, (int)tiles, wmap, xmap, d, s);
 }
 
 int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap, const Device &d, cudaStream_t stream)

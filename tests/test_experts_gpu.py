@@ -267,3 +267,28 @@ def test_refusals():
             symar.experts(a, c, r)
     with pytest.raises(symar.SymarError):
         symar.experts(x, w[:, :15], r, gated=True)                   # rows of gate and up: not an even number
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("by_row", [False, True])
+@pytest.mark.parametrize("counts,n,k", [([1], 64, 4096), ([3], 200, 1000), ([1, 0, 2], 129, 2048), ([5, 64, 1, 0, 9], 24, 1536), ([70, 3], 100, 4104),
+                                        ([1, 2, 9, 1, 17, 0, 33, 64, 1, 5], 1280, 8192)], ids=lambda c: str(c).replace(" ", ""))
+def test_few_tiles_share_multiprocessors(counts, n, k, by_row, out, gated):
+    """Products of few tiles over a long k, which blocks divide; the last one has several tiles for each group of blocks."""
+    if gated and n == 1280:
+        n = 640
+    r = lists(counts, 30, spare=2)
+    x = whole(r.rows if by_row else 30, k, seed=1)
+    w = whole(len(counts), n * (1 + gated), k, seed=2)
+    if not gated:
+        got = symar.experts(x, w, r, by_row=by_row, out_dtype=out)
+        start = r.expert_start.tolist()
+        for e in range(len(counts)):
+            rows = slice(start[e], start[e + 1])
+            xe = x[rows] if by_row else x[r.row_token[rows].long()]
+            assert torch.equal(got[rows], (xe.double() @ w[e].double().T).float().to(out)), e
+    x, w = normal(*x.shape, seed=3), normal(*w.shape, seed=4, scale=k ** -0.5)
+    first = check(x, w, r, normal(len(counts), n * (1 + gated), seed=5), "silu", gated, by_row, out)
+    again = check(x, w, r, normal(len(counts), n * (1 + gated), seed=5), "silu", gated, by_row, out)
+    assert torch.equal(first, again)
