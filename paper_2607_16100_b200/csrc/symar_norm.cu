@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kT ? kT : 1024) row_kernel(const __grid_consta
 constexpr int kShortThreads = 256;
 
 template <int L, int C, int U, bool kVec, bool kX, bool kStream>
-__global__ void __launch_bounds__(kShortThreads) short_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(kShortThreads, C == 1 ? 4 : C == 2 ? 3 : 2) short_kernel(const __grid_constant__ NormArgs a)
 {
     wait_for_stream();
     const int i = (int)threadIdx.x % L, slot = (int)(blockIdx.x * kShortThreads + threadIdx.x) / L, slots = (int)gridDim.x * (kShortThreads / L);
@@ -526,15 +526,18 @@ cudaError_t launch_short(const NormArgs &a, const Device &d, cudaStream_t s)
 template <bool kVec, bool kX, bool kStream>
 cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
 {
-    const bool many = a.rows > 4 * d.sms;
-    if (many && a.n <= 1024) {
+    const bool many = a.rows > 4 * d.sms;  // more than what is resident at once of the row kernel
+    if (many && a.n <= (kVec ? 512 : 1024)) {
         if constexpr (kVec) {
-            if (a.n <= 64) return launch_short<8, 1, 4, true, kX, kStream>(a, d, s);
-            if (a.n <= 128) return launch_short<16, 1, 4, true, kX, kStream>(a, d, s);
-            if (a.n <= 256) return launch_short<32, 1, 4, true, kX, kStream>(a, d, s);
+            if (a.n <= 64) return launch_short<8, 1, 2, true, kX, kStream>(a, d, s);
+            if (a.n <= 128) return launch_short<16, 1, 2, true, kX, kStream>(a, d, s);
+            if (a.n <= 256) return launch_short<32, 1, 2, true, kX, kStream>(a, d, s);
+            return launch_short<32, 2, 1, true, kX, kStream>(a, d, s);     // (16384 x 512, two norms and a gate: 20.4 us, in the ring 26.6)
+        } else {
+            return launch_short<32, 4, 1, false, kX, kStream>(a, d, s);
         }
-        return launch_short<32, 4, 1, kVec, kX, kStream>(a, d, s);
     }
+    // (16384 x 1024: 29.9 us, with a warp a row in registers 34.6)
     if (kVec && many && a.n <= kRingMost && (a.after.kind != SYMAR_NORM_NONE || a.before.kind != SYMAR_NORM_NONE)) {
         const Ring r = ring_of(a);
         if (r.T) {
