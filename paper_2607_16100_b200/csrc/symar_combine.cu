@@ -96,6 +96,8 @@ cudaError_t launch(CombineArgs a, int groups, cudaStream_t s)
 template <bool kVec, bool kY, bool kOut>
 cudaError_t launch_of(const CombineArgs &a, int groups, cudaStream_t s)
 {
+    if constexpr (!kVec)
+        if (a.top_k <= 2) return launch<false, kY, kOut, 2, 1>(a, groups, s);
     return a.top_k <= 4 ? launch<kVec, kY, kOut, 4, kVec ? 2 : 1>(a, groups, s) : launch<kVec, kY, kOut, 8, 1>(a, groups, s);
 }
 template <bool kVec>

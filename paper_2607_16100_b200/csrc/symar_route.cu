@@ -244,13 +244,22 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
         uint32_t most = under;
         for (; at >= 0 && count < 32 && !apart(last, most); at = pick(most), ++count)
             if (lane == count) mine = at;
-        if ((a.bias && !a.sigmoid) || (at >= 0 && !apart(last, most)) || (kDeep < V && __any_sync(0xffffffffu, deep == kDeep))) {
+        if ((at >= 0 && !apart(last, most)) || (kDeep < V && __any_sync(0xffffffffu, deep == kDeep))) {
             mine = choose_exactly<V>(a, row, top);
         } else {
-            double exact = -INFINITY;
+            double exact = -INFINITY, all = 0.0;
+            if (a.bias && !a.sigmoid) {
+#pragma unroll 4
+                for (int e = lane; e < a.experts; e += 32) {
+                    const float l = logit_of(a, row, e);
+                    all += l > -INFINITY ? exp((double)l - (double)top) : 0.0;
+                }
+                all = warp_sum(all);
+            }
             if (mine >= 0) {
                 exact = (double)logit_of(a, row, mine);
-                if (a.bias) exact = 1.0 / (1.0 + exp(-exact)) + (double)a.bias[mine];
+                if (a.bias) exact = a.sigmoid ? 1.0 / (1.0 + exp(-exact)) : exp(exact - (double)top) / all;
+                if (a.bias) exact += (double)a.bias[mine];
             }
             int rank = 0, sorted = -1;
             for (int j = 0; j < count; ++j) {
