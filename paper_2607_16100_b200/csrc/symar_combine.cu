@@ -1,8 +1,9 @@
 // out[t] = sum_j weight[t][j] y[row of (t, j)] + residual[t], for every rank (formulas in include/symar.h): the experts' rows back in the
 // tokens' order.
 //
-// A thread has eight or sixteen channels of one token and asks for eight pieces of its rows at once; a token's rows are added in the order
-// of its choices, so that results do not depend on anything else.  Bound by the rows' bytes: 8192 tokens x 4 rows x 4096 take FIGURE us.
+// A thread has eight channels of one token and asks for its pieces of up to eight rows at once; a token's rows are added in the order
+// of its choices, so that results do not depend on anything else.  Bound by the rows' bytes: 8192 tokens x 4 rows x 4096 take 57.8 us for 333 MB
+// (5.75 TB/s, 0.88 of the measured copy rate); rows on no 16-byte boundary (4097) 143 us, whose elements are read and written one by one.
 #include "symar_eights.cuh"
 #include "symar_ops.h"
 
@@ -21,31 +22,30 @@ struct CombineArgs {
 constexpr int kMost = 1 << 30;              // channels: their last step ends below 2^31
 constexpr int kThreads = 256;
 
-// kY, kOut: y and the results are float32.  K: rows asked for at once, C: pieces of each.
-template <bool kVec, bool kY, bool kOut, int K, int C>
-__global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant__ CombineArgs a)
+// Blocks of a multiprocessor: more of them hide more of the two dependent trips to memory, until their registers no longer hold what is on its way (four
+// rows a token: 8 blocks 57.8 us, 5 62, as many as 54 registers allow 67; eight rows 5 blocks 50.4, 6 53).
+constexpr int blocks_for(bool vec, bool wide, int rows) { return !vec ? 6 : rows == 8 ? (wide ? 3 : 4) : rows == 4 ? (wide ? 5 : 8) : 6; }
+
+// kY, kOut: y and the results are float32.  K: rows asked for at once.
+template <bool kVec, bool kY, bool kOut, int K>
+__global__ void __launch_bounds__(kThreads, blocks_for(kVec, kY, K)) combine_kernel(const __grid_constant__ CombineArgs a)
 {
     wait_for_stream();
-    // a token's channels are divided into `parts` of 8 C a thread; on no boundary a warp has 256 in a row, a thread every thirty-second of them
+    // a token's channels are divided into `parts` of eight a thread; on no boundary a warp has 256 in a row, a thread every thirty-second of them
     constexpr int step = 32;
     const unsigned lanes = kVec ? a.lanes : 32, per = kThreads / lanes, unit = blockIdx.x * per + threadIdx.x / lanes;
     const unsigned block = kVec ? blockIdx.x / (unsigned)a.parts : 0, part = kVec ? blockIdx.x - block * a.parts : unit % (unsigned)a.parts;
     const int g = blockIdx.y, t = (int)(kVec ? block * per + threadIdx.x / lanes : unit / (unsigned)a.parts);
     if (t >= a.tokens) return;
-    int first[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int i = (int)(part * C + c) * (int)lanes;
-        first[c] = 8 * i + (kVec ? 8 : 1) * (int)(threadIdx.x & (lanes - 1));
-    }
+    const int first = 8 * (int)(part * lanes) + (kVec ? 8 : 1) * (int)(threadIdx.x & (lanes - 1));
     const int32_t *at = a.token_row + (int64_t)t * a.top_k;
     const float *w = a.weights ? a.weights + (int64_t)t * a.top_k : nullptr;
     const char *y = static_cast<const char *>(a.y) + g * a.y_group * (kY ? 4 : 2);
-    float sum[C][8] = {};
+    float sum[8] = {};
     for (int j0 = 0; j0 < a.top_k; j0 += K) {
         int   row[K];
         float by[K];
-        Raw   r[K][C];
+        Raw   r[K];
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             row[j] = j0 + j < a.top_k ? at[j0 + j] : -1;
@@ -54,51 +54,42 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const __grid_constant
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             const bool on = (unsigned)row[j] < (unsigned)a.rows;
-            const char *p = y + (on ? row[j] : 0) * a.y_ld * (kY ? 4 : 2);
             by[j] = on ? by[j] : 0.0f;     // (and zeros times that)
-#pragma unroll
-            for (int c = 0; c < C; ++c) r[j][c] = read8<kVec>(p, kY, first[c], step, on ? a.n : 0);
+            r[j] = read8<kVec>(y + (on ? row[j] : 0) * a.y_ld * (kY ? 4 : 2), kY, first, step, on ? a.n : 0);
         }
 #pragma unroll
-        for (int j = 0; j < K; ++j)
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float v[8];
-                values<kVec>(r[j][c], kY, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[c][e] = fmaf(by[j], v[e], sum[c][e]);
-            }
-    }
-    const bool add = a.residual && (a.root < 0 || a.root == g);
-    const char *res = static_cast<const char *>(a.residual) + (g * a.residual_group + t * a.residual_ld) * (kOut ? 4 : 2);
-    char *out = static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (kOut ? 4 : 2);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if (add) {
+        for (int j = 0; j < K; ++j) {
             float v[8];
-            values<kVec>(read8<kVec>(res, kOut, first[c], step, a.n), kOut, v);
+            values<kVec>(r[j], kY, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[c][e] += v[e];
+            for (int e = 0; e < 8; ++e) sum[e] = fmaf(by[j], v[e], sum[e]);
         }
-        write8<kVec>(out, kOut, first[c], step, a.n, sum[c]);
     }
+    if (a.residual && (a.root < 0 || a.root == g)) {
+        const char *res = static_cast<const char *>(a.residual) + (g * a.residual_group + t * a.residual_ld) * (kOut ? 4 : 2);
+        float v[8];
+        values<kVec>(read8<kVec>(res, kOut, first, step, a.n), kOut, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+    write8<kVec>(static_cast<char *>(a.out) + (g * a.out_group + t * a.out_ld) * (kOut ? 4 : 2), kOut, first, step, a.n, sum);
 }
-template <bool kVec, bool kY, bool kOut, int K, int C>
+template <bool kVec, bool kY, bool kOut, int K>
 cudaError_t launch(CombineArgs a, int groups, cudaStream_t s)
 {
     a.lanes = kVec ? 1 : 32;
-    while (kVec && a.lanes < kThreads && a.lanes * 8 * C < a.n) a.lanes *= 2;
-    a.parts = (a.n + a.lanes * 8 * C - 1) / (a.lanes * 8 * C);
+    while (kVec && a.lanes < kThreads && a.lanes * 8 < a.n) a.lanes *= 2;
+    a.parts = (a.n + a.lanes * 8 - 1) / (a.lanes * 8);
     const int64_t per = kThreads / a.lanes, blocks = kVec ? (a.tokens + per - 1) / per * a.parts : ((int64_t)a.tokens * a.parts + per - 1) / per;
-    return launch_early(combine_kernel<kVec, kY, kOut, K, C>, dim3((unsigned)blocks, (unsigned)groups), kThreads, 0, s, a);
+    return launch_early(combine_kernel<kVec, kY, kOut, K>, dim3((unsigned)blocks, (unsigned)groups), kThreads, 0, s, a);
 }
-// Few rows a token leave room for two pieces of each on their way.
 template <bool kVec, bool kY, bool kOut>
 cudaError_t launch_of(const CombineArgs &a, int groups, cudaStream_t s)
 {
-    if constexpr (!kVec)
-        if (a.top_k <= 2) return launch<false, kY, kOut, 2, 1>(a, groups, s);
-    return a.top_k <= 4 ? launch<kVec, kY, kOut, 4, kVec ? 2 : 1>(a, groups, s) : launch<kVec, kY, kOut, 8, 1>(a, groups, s);
+    if (a.top_k <= 2) return launch<kVec, kY, kOut, 2>(a, groups, s);
+    if constexpr (kVec)
+        if (a.top_k > 4) return launch<true, kY, kOut, 8>(a, groups, s);
+    return launch<kVec, kY, kOut, 4>(a, groups, s);
 }
 template <bool kVec>
 cudaError_t launch_as(const CombineArgs &a, int groups, bool y_wide, bool out_wide, cudaStream_t s)
