@@ -586,7 +586,7 @@ int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const syma
 
 /* ---- norms around the AllReduces, and a layer's mixture of experts ----------------
  *
- * The conventions are those of the operators above.                              */
+ * The conventions are those of the operators above.  What a call writes overlaps nothing that it reads but where it says so.  */
 
 /* What follows a block's AllReduce, for every row of groups x m:
  *     a = after(x),   r = residual_scale * residual + scale * act(gate) * a,   out = before(r)

@@ -8,7 +8,13 @@
 // tile has, in sixteens.  Four more warps gather the tokens' rows straight into the ring, so nothing is permuted beforehand.
 //
 // A block: one warp fills a ring of 64-wide slices of both operands, one thread issues the products, eight warps take finished accumulators
-// out of tensor memory while the next tile is summed in its other half.
+// out of tensor memory while the next tile is summed in its other half.  Many rows an expert go to pairs of blocks, few tiles over a long k to clusters that
+// share it.
+//
+// Bound and measured (B200, within a CUDA graph).  A few tokens: the weights' bytes; one token's eight experts of 2 x 768 x 2048 take 14.6 us for 50 MB (a start of
+// 6 us, then 6 TB/s), 64 tokens on four ranks of 64 experts of 2048 x 352 63 us for 376 MB (5.95 TB/s, 0.91 of the measured copy rate).  Many: the tensor cores (75% of the
+// cycles in 212 us of pair_kernel), the experts' uneven numbers of rows (a fifth of it), and putting rows in order.  Small ragged products: the start, a tile's
+// epilogue and two rounds of tiles (333 tokens, 7 experts of 1003 x 520 on two ranks, GELU and float32 results: 23.5 us).
 #include <type_traits>
 
 #include "symar_act.cuh"
@@ -294,7 +300,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         failed = bad = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid == 32) {
+    if (tid == 32 && a.k > 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
         if (!kGather) asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
     }
@@ -514,7 +520,8 @@ done:
 // With many rows an expert, a cluster of two blocks has a tile of 256 weights' rows and up to 256 tokens: each block holds its 128 weights' rows and
 // half of the tokens, both read both halves of the tokens, and the first block's thread issues the products of both.  A block's copies are a third
 // fewer for the same products.  Rows by token are put in order by a kernel of their own first: gathered into the ring as above they come at 40 bytes a
-// cycle at best (16384 rows x 2 x 1024 x 4096: 304 us with four gathering warps a block, FIGURE with the rows in order beforehand, FIGURE2 where they are).
+// cycle at best (16384 rows x 2 x 1024 x 4096 of 32 experts: 304 us with four gathering warps a block, 250 with the rows in order beforehand, of
+// which that takes 35; 215 where they are in order already, 177 for four experts of 4096 rows each: 1550 TFLOP/s).
 __device__ __forceinline__ void pair_load3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),

@@ -9,7 +9,9 @@
 // Choices have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order found are nearer than the rounding of
 // their keys, the token's choices are made again in binary64.
 //
-// Bound by instructions: FIGURES
+// Bound by instructions and, with few tokens, by latency (B200, within a CUDA graph): 16384 tokens x 256 experts, top 8 of sigmoid + bias, take 26.8 us (about
+// 20 and 7 for the two launches; 800 instructions of a warp a token, a third of them the eight choices), 64 x 128 9.1 us, one token 4.0 us.  A choice by
+// two reductions over unsorted lanes took 1420 instructions (49 us), all doubts in binary64 over all experts 33 us.
 #include <math.h>
 
 #include "symar_ops.h"
