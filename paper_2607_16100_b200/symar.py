@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import (POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint,
                     c_void_p)
 from pathlib import Path
@@ -512,6 +513,25 @@ class CombineArgs(ctypes.Structure):
     ]
 
 
+def _packer(cls):
+    """The fields of a structure as bytes laid out as C lays them out: what a call hands over, in a fifth of a ctypes structure's time."""
+    codes = {c_void_p: "P", c_int64: "q", c_int32: "i", c_float: "f", c_size_t: "N"}
+
+    def flat(c):
+        return "".join(codes[t] if t in codes else flat(t) for _, t in c._fields_)
+    made = struct.Struct("@" + flat(cls) + "0P")
+    assert made.size == ctypes.sizeof(cls)
+
+    def pack(*fields):
+        try:
+            return made.pack(*fields)
+        except (struct.error, OverflowError) as e:
+            raise SymarError(ERR_INVAL, f"{cls.__name__}: {e}") from None
+    return pack
+
+
+_pack_norm, _pack_route, _pack_experts, _pack_combine = (_packer(c) for c in (NormArgs, RouteArgs, ExpertsArgs, CombineArgs))
+
 _T = None               # torch, once a call needed it
 _raw_stream = None      # device index -> handle of torch's current stream
 _device = None          # -> index of the current device
@@ -859,11 +879,11 @@ class Norm:
         code = _dtype_code(some.dtype, where) if some is not None else F32
         self.n, self.index = (some.shape[0], some.get_device()) if some is not None else (None, None)
         self.weight, self.bias = weight, bias
-        self.args = NormSide(weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None, eps,
-                             NORM_KINDS[kind], code, 1 if plus_one else 0)
+        self.fields = (weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, eps,
+                       NORM_KINDS[kind], code, 1 if plus_one else 0)
 
 
-_NO_NORM = NormSide()
+_NO_NORM = (0, 0, 0.0, 0, 0, 0)
 
 
 def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str = "none", scale: float = 1.0,
@@ -904,9 +924,9 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
     if before is not None:
         if out is None:
             out = _like(x, index, stream)
-        s = out.stride()
-        if out.shape != shape or (n > 1 and s[-1] != 1) or out.dtype is not dtype or out.get_device() != index:
+        elif out.shape != shape or (n > 1 and out.stride(-1) != 1) or out.dtype is not dtype or out.get_device() != index:
             _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+        s = out.stride()
         yp, yl, yg = out.data_ptr(), s[-2], s[0] if nd == 3 else 0
     elif out is not None:
         _bad(where, "out without a norm before the next block")
@@ -923,10 +943,10 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
     for side in (after, before):
         if side is not None and side.n is not None and (side.n != n or side.index != index):
             _bad(where, f"a norm of {side.n} channels on device {side.index} for x {tuple(shape)} on device {index}")
-    args = NormArgs(x.data_ptr(), xs[-2], xs[0] if nd == 3 else 0, rp, rl, rg, gp, gl, gg, op, ol, og, yp, yl, yg,
-                    after.args if after is not None else _NO_NORM, before.args if before is not None else _NO_NORM, scale, residual_scale,
-                    groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act)
-    _call((_lib or load()).symar_norm, where, index, stream, byref(args))
+    args = _pack_norm(x.data_ptr(), xs[-2], xs[0] if nd == 3 else 0, rp, rl, rg, gp, gl, gg, op, ol, og, yp, yl, yg,
+                      *(after.fields if after is not None else _NO_NORM), *(before.fields if before is not None else _NO_NORM), scale, residual_scale,
+                      groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act)
+    _call((_lib or load()).symar_norm, where, index, stream, args)
     return out if before is not None else None, residual_out
 
 
@@ -999,10 +1019,10 @@ def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise:
     whole = _new(logits, (3 * rows + experts + 1 + work // 4,), torch.int32, index, stream)
     weights = _new(logits, (tokens, top_k), torch.float32, index, stream)
     at, start = whole.data_ptr(), 3 * rows
-    args = RouteArgs(logits.data_ptr(), logits.stride(0), bias.data_ptr() if bias is not None else None, at, weights.data_ptr(), at + 4 * start,
-                     at + 4 * rows, at + 8 * rows, at + 4 * (start + experts + 1) if work else None, work, scale, tokens, experts, top_k, code, kind,
-                     1 if renormalise else 0)
-    _call(lib.symar_route, where, index, stream, byref(args))
+    args = _pack_route(logits.data_ptr(), logits.stride(0), bias.data_ptr() if bias is not None else 0, at, weights.data_ptr(), at + 4 * start,
+                       at + 4 * rows, at + 8 * rows, at + 4 * (start + experts + 1) if work else 0, work, scale, tokens, experts, top_k, code, kind,
+                       1 if renormalise else 0)
+    _call(lib.symar_route, where, index, stream, args)
     return Routes._of(whole, weights, (tokens, top_k), experts, index)
 
 
@@ -1037,9 +1057,9 @@ def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool =
     shape = (groups, routes.rows, n) if ranked else (routes.rows, n)
     if out is None:
         out = _new(x, shape, out_dtype or bf16, index, stream)
-    os = out.stride()
-    if out.shape != shape or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and os[-1] != 1) or out.get_device() != index:
+    elif out.shape != shape or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and out.stride(-1) != 1) or out.get_device() != index:
         _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+    os = out.stride()
     bp = be = bg = sp = 0
     if bias is not None:
         bs = bias.stride()
@@ -1051,16 +1071,16 @@ def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool =
         if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != index:
             _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
         sp = status.data_ptr()
-    args = ExpertsArgs(x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
-                       out.data_ptr(), os[-2], os[0] if ranked else 0, routes._start_ptr, None if by_row else routes._row_token_ptr,
-                       groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
-    lib = _lib or load()
+    fields = (x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
+              out.data_ptr(), os[-2], os[0] if ranked else 0, routes._start_ptr, 0 if by_row else routes._row_token_ptr,
+              groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
+    lib, args = _lib or load(), _pack_experts(*fields, 0, 0)
     if not by_row:
-        need = lib.symar_experts_workspace(byref(args))
+        need = lib.symar_experts_workspace(args)
         if need:
             room = _new(x, (need,), torch.uint8, index, stream)
-            args.workspace, args.workspace_bytes = room.data_ptr(), need
-    _call(lib.symar_experts, where, index, stream, byref(args))
+            args = _pack_experts(*fields, room.data_ptr(), need)
+    _call(lib.symar_experts, where, index, stream, args)
     return out
 
 
@@ -1079,19 +1099,19 @@ def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_d
     want = (groups, routes.tokens, n) if nd == 3 else (routes.tokens, n)
     if out is None:
         out = _new(y, want, out_dtype or y.dtype, index, stream)
-    os = out.stride()
-    if out.shape != want or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and os[-1] != 1) or out.get_device() != index:
+    elif out.shape != want or (out_dtype is not None and out.dtype is not out_dtype) or (n > 1 and out.stride(-1) != 1) or out.get_device() != index:
         _bad(where, f"out of shape {tuple(out.shape)}, {out.dtype}")
+    os = out.stride()
     rp = rl = rg = 0
     if residual is not None:
         rs = residual.stride()
         if residual.shape not in (want, want[-2:]) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or residual.get_device() != index:
             _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
-    args = CombineArgs(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes.weights.data_ptr(), rp, rl, rg,
-                       out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
-                       _dtype_code(out.dtype, where), root)
-    _call((_lib or load()).symar_combine, where, index, stream, byref(args))
+    args = _pack_combine(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes.weights.data_ptr(), rp, rl, rg,
+                         out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
+                         _dtype_code(out.dtype, where), root)
+    _call((_lib or load()).symar_combine, where, index, stream, args)
     return out
 
 

@@ -156,7 +156,7 @@ def test_nothing_to_do_and_refusals():
     x, w = normal(4, 64, seed=1), normal(64, seed=2)
     n = symar.Norm("rms", w)
     for kw in (dict(residual=x[:, :32]), dict(gate=w.float()), dict(gate=w[:32]), dict(out=x[:2]), dict(gate_act="relu"), dict(residual_out=x.float(), residual=x),
-               dict(before=None, out=x), dict(out=x.float()), dict(residual=x.cpu()), dict(gate=x[:, ::2].repeat(1, 2).T), dict(scale=math.nan),
+               dict(before=None, out=x), dict(out=x.float()), dict(residual=x.cpu()), dict(gate=x[:, ::2].repeat(1, 2).T), dict(scale=math.nan), dict(scale=1e39), dict(residual_scale=None),
                dict(out=torch.empty(1, 64, device="cuda", dtype=BF16).expand(4, 64))):
         with pytest.raises(symar.SymarError):
             symar.norm(x, **{"before": n, **kw})
