@@ -823,15 +823,16 @@ int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap,
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_experts");
 }
 
-// Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often.  Pairs take many
-// rows where their tiles are enough for all multiprocessors (a product's start costs them 3 us more: 1000 rows x 128 x 520 of seven experts 13.3 us instead
-// of 9.9; with 1003 channels on two ranks 17.9 instead of 19.3).
+// Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often (64 or 128 with 32 experts of
+// 2 x 1024 x 4096: 25 rows each 96.6 and 100 us, 50 rows 118 and 111).  Pairs take many rows where their tiles are enough for all multiprocessors (a product's start costs
+// them 3 us more: 1000 rows x 128 x 520 of seven experts 13.3 us instead of 9.9; with 1003 channels on two ranks 17.9 instead of 19.3) and the gathering beforehand is
+// little beside the products (75 rows each of k = 4096: 112 us instead of 123, of k = 1024 25.3 instead of 22.9).
 int tile_tokens(const symar_experts_t &p)
 {
     const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = used > 0 ? p.rows / used : 0;
     const int64_t tiles = (int64_t)p.groups * (p.gated ? (p.n + kHalf - 1) / kHalf : (p.n + kRows - 1) / kRows) * (p.rows / kPair + used);
     if (each <= 32) return 64;
-    return each <= 96 || tiles < 148 || p.out_dtype == SYMAR_F32 ? 128 : kPair;
+    return each <= (p.k < 2048 ? 96 : 48) || tiles < 148 || p.out_dtype == SYMAR_F32 ? 128 : kPair;
 }
 bool in_order_first(const symar_experts_t &p) { return p.row_token && p.k > 0 && tile_tokens(p) == kPair; }
 int64_t pieces_of(int k) { return ((int64_t)k + 7) / 8; }

@@ -532,8 +532,10 @@ cudaError_t launch_short(const NormArgs &a, const Device &d, cudaStream_t s)
 template <bool kVec, bool kX, bool kStream>
 cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
 {
-    const bool many = a.rows > 4 * d.sms;  // more than what is resident at once of the row kernel
-    if (many && a.n <= (kVec ? 512 : 1024)) {
+    // Many long rows: more than what is resident at once of the row kernel (of 8192: 400 rows 12.5 us, in the ring 13.3; 800 rows 19.1 us, a row a block 25.8; of
+    // 2048: 800 rows 6.8 and 6.0).  Many short ones: a block a row has idle threads, but is over sooner (1080 heads of 128 2.2 us, several a warp 2.9).
+    const bool many = a.rows > 4 * d.sms;
+    if (a.rows > 16 * d.sms && a.n <= (kVec ? 512 : 1024)) {
         if constexpr (kVec) {
             if (a.n <= 64) return launch_short<8, 1, 2, true, kX, kStream>(a, d, s);
             if (a.n <= 128) return launch_short<16, 1, 2, true, kX, kStream>(a, d, s);
@@ -544,7 +546,7 @@ cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
         }
     }
     // (16384 x 1024: 29.9 us, with a warp a row in registers 34.6)
-    if (kVec && many && a.n <= kRingMost && (a.after.kind != SYMAR_NORM_NONE || a.before.kind != SYMAR_NORM_NONE)) {
+    if (kVec && many && a.n > 512 && a.n <= kRingMost && (a.after.kind != SYMAR_NORM_NONE || a.before.kind != SYMAR_NORM_NONE)) {
         const Ring r = ring_of(a);
         if (r.T) {
             const int bytes = 32 + r.held + r.groups * r.slots * (r.x_bytes + r.old_bytes + r.gate_bytes);
