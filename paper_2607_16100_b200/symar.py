@@ -965,35 +965,37 @@ class Routes:
                 _bad("Routes", f"{name} is a contiguous int32 tensor {list(want)} on the weights' device")
         if expert_start.shape[0] < 2:
             _bad("Routes", "expert_start has an entry more than there are experts")
-        self._lists = choice, expert_start, row_token, token_row
-        self._set(weights, shape, expert_start.shape[0] - 1, index, expert_start.data_ptr(), row_token.data_ptr(), token_row.data_ptr())
+        self._lists = choice, expert_start, row_token, token_row, weights
+        self._set(shape, expert_start.shape[0] - 1, index, expert_start.data_ptr(), row_token.data_ptr(), token_row.data_ptr(), weights.data_ptr())
 
     @classmethod
-    def _of(cls, whole, weights, shape, experts: int, index: int) -> "Routes":
-        """Lists side by side in one tensor: choice, row_token, token_row, expert_start (the calls go by addresses, tensors are made when they are asked for)."""
+    def _of(cls, whole, shape, experts: int, index: int) -> "Routes":
+        """Lists side by side in one tensor: choice, row_token, token_row, weights, expert_start (the calls go by addresses, tensors are made when they are
+        asked for)."""
         r = object.__new__(cls)
         at, rows = whole.data_ptr(), shape[0] * shape[1]
         r._lists, r._whole = None, whole
-        r._set(weights, shape, experts, index, at + 12 * rows, at + 4 * rows, at + 8 * rows)
+        r._set(shape, experts, index, at + 16 * rows, at + 4 * rows, at + 8 * rows, at + 12 * rows)
         return r
 
-    def _set(self, weights, shape, experts, index, start_ptr, row_token_ptr, token_row_ptr):
-        self.weights, self.experts, self.index = weights, experts, index
+    def _set(self, shape, experts, index, start_ptr, row_token_ptr, token_row_ptr, weights_ptr):
+        self.experts, self.index = experts, index
         self.tokens, self.top_k = shape
         self.rows = self.tokens * self.top_k
-        self._start_ptr, self._row_token_ptr, self._token_row_ptr = start_ptr, row_token_ptr, token_row_ptr
+        self._start_ptr, self._row_token_ptr, self._token_row_ptr, self._weights_ptr = start_ptr, row_token_ptr, token_row_ptr, weights_ptr
 
     def _list(self, i: int):
         if self._lists is None:
             w, rows, shape, stride = self._whole, self.rows, (self.tokens, self.top_k), (self.top_k, 1)
-            self._lists = (w.as_strided(shape, stride, 0), w.as_strided((self.experts + 1,), (1,), 3 * rows), w.as_strided((rows,), (1,), rows),
-                           w.as_strided(shape, stride, 2 * rows))
+            self._lists = (w.as_strided(shape, stride, 0), w.as_strided((self.experts + 1,), (1,), 4 * rows), w.as_strided((rows,), (1,), rows),
+                           w.as_strided(shape, stride, 2 * rows), w.view(_T.float32).as_strided(shape, stride, 3 * rows))
         return self._lists[i]
 
     choice = property(lambda self: self._list(0))
     expert_start = property(lambda self: self._list(1))
     row_token = property(lambda self: self._list(2))
     token_row = property(lambda self: self._list(3))
+    weights = property(lambda self: self._list(4))
 
 
 def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise: bool = True, scale: float = 1.0, stream=None) -> Routes:
@@ -1016,14 +1018,13 @@ def route(logits, top_k: int, *, bias=None, score: str = "softmax", renormalise:
     lib = _lib or load()
     rows, work = tokens * top_k, int(lib.symar_route_workspace(tokens, experts))
     # lists and workspace in one piece
-    whole = _new(logits, (3 * rows + experts + 1 + work // 4,), torch.int32, index, stream)
-    weights = _new(logits, (tokens, top_k), torch.float32, index, stream)
-    at, start = whole.data_ptr(), 3 * rows
-    args = _pack_route(logits.data_ptr(), logits.stride(0), bias.data_ptr() if bias is not None else 0, at, weights.data_ptr(), at + 4 * start,
+    whole = _new(logits, (4 * rows + experts + 1 + work // 4,), torch.int32, index, stream)
+    at, start = whole.data_ptr(), 4 * rows
+    args = _pack_route(logits.data_ptr(), logits.stride(0), bias.data_ptr() if bias is not None else 0, at, at + 12 * rows, at + 4 * start,
                        at + 4 * rows, at + 8 * rows, at + 4 * (start + experts + 1) if work else 0, work, scale, tokens, experts, top_k, code, kind,
                        1 if renormalise else 0)
     _call(lib.symar_route, where, index, stream, args)
-    return Routes._of(whole, weights, (tokens, top_k), experts, index)
+    return Routes._of(whole, (tokens, top_k), experts, index)
 
 
 def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool = False, by_row: bool = False, out=None, out_dtype=None,
@@ -1108,7 +1109,7 @@ def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_d
         if residual.shape not in (want, want[-2:]) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or residual.get_device() != index:
             _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
-    args = _pack_combine(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes.weights.data_ptr(), rp, rl, rg,
+    args = _pack_combine(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes._weights_ptr, rp, rl, rg,
                          out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
                          _dtype_code(out.dtype, where), root)
     _call((_lib or load()).symar_combine, where, index, stream, args)

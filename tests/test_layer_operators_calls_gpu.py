@@ -113,8 +113,12 @@ def test_lists_of_a_program_of_its_own():
     r = symar.Routes(choice, weights, start, (order // 2).to(torch.int32), row.view(6, 2))
     assert r.choice is choice and r.experts == 3 and r.rows == 12
     got = symar.combine(symar.experts(x, w, r, out_dtype=F32), r)
-    want = sum(weights[:, j, None].double() * torch.einsum("tk,tnk->tn", x.double(), w[choice[:, j].long()].double()) for j in range(2))
-    assert (got.double() - want).abs().max() < 1e-4
+    def summed(x, w):
+        return sum(weights[:, j, None].double() * torch.einsum("tk,tnk->tn", x, w[choice[:, j].long()]) for j in range(2))
+    # 64 truncating additions of 2^-23, one more sum, two weights and their sum, of the terms' sizes; the result's half step
+    size = summed(x.double().abs(), w.double().abs())
+    tol = (64 * 2.0 ** -23 + 8 * 2.0 ** -24) * size
+    assert ((got.double() - summed(x.double(), w.double())).abs() <= tol).all()
 
 
 def test_results_into_the_heap():
