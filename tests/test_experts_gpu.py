@@ -292,3 +292,20 @@ def test_few_tiles_share_multiprocessors(counts, n, k, by_row, out, gated):
     first = check(x, w, r, normal(len(counts), n * (1 + gated), seed=5), "silu", gated, by_row, out)
     again = check(x, w, r, normal(len(counts), n * (1 + gated), seed=5), "silu", gated, by_row, out)
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("experts", [31, 32, 33, 127, 128, 129, 500, 1024])
+@pytest.mark.parametrize("most", [3, 130])
+def test_numbers_of_experts(experts, most):
+    """Experts with and without rows at every place of the counting."""
+    g = torch.Generator().manual_seed(experts)
+    counts = (torch.randint(0, most, (experts,), generator=g) * (torch.rand(experts, generator=g) < 0.6)).tolist()
+    counts[-1] = 2
+    r = lists(counts, 60, seed=1, spare=2)
+    x, w = whole(60, 64, seed=1), whole(experts, 24, 64, seed=2)
+    for out in (BF16, F32):
+        got = symar.experts(x, w, r, out=torch.full((r.rows, 24), 7.0, dtype=out, device="cuda"))
+        e = torch.repeat_interleave(torch.arange(experts), torch.tensor(counts)).cuda()
+        used = len(e)
+        want = torch.einsum("rk,rnk->rn", x[r.row_token[:used].long()].double(), w[e].double())
+        assert torch.equal(got[:used], want.float().to(out)) and (got[used:] == 7).all()

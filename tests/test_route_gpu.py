@@ -91,6 +91,19 @@ def test_equal_keys_and_keys_next_to_each_other(tokens, score):
     check(y, 8, (0.25 - s).float(), score)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,top_k", [(40, 32), (700, 32), (300, 8), (1024, 20)])
+def test_many_choices_next_to_each_other(experts, top_k, score):
+    """More equal and nearly equal keys than are looked at together, also all of a lane's."""
+    x = (normal(60, experts, seed=1)).round()
+    y = normal(1, experts, seed=3).expand(60, experts) + normal(60, experts, seed=4, scale=1e-6)
+    s = torch.sigmoid(y[0].double()) if score == "sigmoid" else torch.softmax(y[0].double(), -1)
+    z = torch.full((60, experts), -3.0, device="cuda")
+    z[:, ::32] = normal(60, len(range(0, experts, 32)), seed=5)
+    for logits, bias in ((x, None), (x, torch.zeros(experts, device="cuda")), (x, x[0] / 64), (y, (0.25 - s).float()), (y * 1e-3, None), (z, None), (z, x[0] / 64)):
+        check(logits, top_k, bias, score)
+
+
 def test_masked_experts_and_tokens():
     for tokens in (20, 1000):
         x = normal(tokens, 64, seed=1)
