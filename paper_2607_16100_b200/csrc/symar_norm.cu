@@ -564,10 +564,15 @@ cudaError_t launch(const NormArgs &a, const Device &d, cudaStream_t s)
         return chunks == 2 ? launch_early(row_kernel<2, 0, kX, kStream>, rows, threads, 0, s, a) : launch_early(row_kernel<4, 0, kX, kStream>, rows, threads, 0, s, a);
     } else {
         if (a.n <= 1024) return launch_early(row_kernel<1, 128, kX, kStream>, rows, 128, 0, s, a);
-        if (a.n <= 1536) return launch_early(row_kernel<2, 96, kX, kStream>, rows, 96, 0, s, a);
-        if (a.n <= 2048) return launch_early(row_kernel<2, 128, kX, kStream>, rows, 128, 0, s, a);
-        if (a.n <= 2560) return launch_early(row_kernel<2, 160, kX, kStream>, rows, 160, 0, s, a);
-        if (a.n <= 4096) return launch_early(row_kernel<2, 256, kX, kStream>, rows, 256, 0, s, a);
+        // sixteen elements a thread, in as many warps as that takes (2049 in 160 threads 21.7 us, in 256 26.5)
+        switch ((a.n + 511) / 512) {
+            case 3: return launch_early(row_kernel<2, 96, kX, kStream>, rows, 96, 0, s, a);
+            case 4: return launch_early(row_kernel<2, 128, kX, kStream>, rows, 128, 0, s, a);
+            case 5: return launch_early(row_kernel<2, 160, kX, kStream>, rows, 160, 0, s, a);
+            case 6: return launch_early(row_kernel<2, 192, kX, kStream>, rows, 192, 0, s, a);
+            case 7: return launch_early(row_kernel<2, 224, kX, kStream>, rows, 224, 0, s, a);
+            case 8: return launch_early(row_kernel<2, 256, kX, kStream>, rows, 256, 0, s, a);
+        }
         if (a.n <= 8192) return launch_early(row_kernel<2, 512, kX, kStream>, rows, 512, 0, s, a);
         return launch_early(row_kernel<4, 1024, kX, kStream>, rows, 1024, 0, s, a);
     }

@@ -73,7 +73,7 @@ def check(x, residual=None, after=None, before=None, gate=None, gate_act="none",
     return got, got_r
 
 
-SIZES = [1, 2, 7, 8, 9, 64, 128, 250, 256, 257, 264, 1000, 1024, 1032, 2049, 4096, 4100, 4104, 8192, 8200, 11111, 16384, 16392, 32767, 32768]
+SIZES = [1, 2, 7, 8, 9, 64, 128, 250, 256, 257, 264, 1000, 1024, 1025, 1032, 1535, 1999, 2049, 2700, 3333, 3583, 4095, 4096, 4100, 4104, 8192, 8200, 11111, 16384, 16392, 32767, 32768]
 
 
 @pytest.mark.parametrize("n", SIZES)
