@@ -6,8 +6,8 @@
 // of earlier warps and blocks and of smaller experts are added up, and the warp goes through its tokens once more.  Nothing depends on the order in
 // which blocks run.  Few tokens are one block and one launch; more are two launches, the blocks' counts between them in the workspace.
 //
-// Choices have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order found are nearer than the rounding of
-// their keys, the token's choices are made again in binary64.
+// Choices have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order found, or the last choice and any expert
+// behind it, are nearer than the rounding of their keys and not the same, the token's choices are made again in binary64.
 //
 // Bound by instructions and, with few tokens, by latency (B200, within a CUDA graph): 16384 tokens x 256 experts, top 8 of sigmoid + bias, take 26.8 us (about
 // 20 and 7 for the two launches; 800 instructions of a warp a token, a third of them the eight choices), 64 x 128 9.1 us, one token 4.0 us.  A choice by
@@ -236,10 +236,27 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
     const int behind = pick(under);        // the border has to be looked at
     const int next_at = __shfl_down_sync(0xffffffffu, mine, 1), other = lane == a.top_k - 1 ? behind : next_at;
     const uint32_t next = __shfl_down_sync(0xffffffffu, found, 1);
-    bool near = false;
-    if (mine >= 0 && other >= 0 && lane < a.top_k && !apart(found, lane == a.top_k - 1 ? under : next))
-        near = logit_of(a, row, mine) != logit_of(a, row, other) || (a.bias && a.bias[mine] != a.bias[other]);
-    if (__any_sync(0xffffffffu, near || (kDeep < V && deep == kDeep))) {
+    const bool close = mine >= 0 && other >= 0 && lane < a.top_k && !apart(found, lane == a.top_k - 1 ? under : next);
+    bool doubt = __any_sync(0xffffffffu, close || (kDeep < V && deep == kDeep));
+    if (doubt) {
+        // None where neighbours are the same, and all that is no further from the last choice than its error, too: a lane's experts that are left.
+        auto unlike = [&](int x, int y) { return logit_of(a, row, x) != logit_of(a, row, y) || (a.bias && a.bias[x] != a.bias[y]); };
+        bool differs = (close && unlike(mine, other)) || (kDeep < V && deep == kDeep);
+        if (__shfl_sync(0xffffffffu, (int)close, a.top_k - 1)) {
+            const int last_at = __shfl_sync(0xffffffffu, mine, a.top_k - 1);
+            const uint32_t last = __shfl_sync(0xffffffffu, found, a.top_k - 1);
+            int as_near = deep;
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i)
+                if (key[i] && !apart(last, key[i])) {
+                    ++as_near;
+                    differs = differs || unlike(lane + 32 * (int)(kPlace - (key[i] & kPlace)), last_at);
+                }
+            differs = differs || (kDeep < V && as_near == kDeep);      // (nobody knows what comes behind these)
+        }
+        doubt = __any_sync(0xffffffffu, differs);
+    }
+    if (doubt) {
         // Neighbours nearer than their errors: all that may be among the choices, in binary64.
         const uint32_t last = __shfl_sync(0xffffffffu, found, a.top_k - 1);
         int count = __popc(__ballot_sync(0xffffffffu, mine >= 0)), at = behind;
