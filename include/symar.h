@@ -627,7 +627,8 @@ int symar_norm(const symar_norm_t *args, void *cuda_stream);
  * (binary32), decided as exact arithmetic decides (in binary64 where binary32 leaves a doubt); of equal ones the lowest
  * index first.  An expert whose logit is -inf or NaN, or whose score + bias is, is not to be had (and counts as 0 in a softmax); a
  * token with fewer than top_k others has -1 and a weight of 0 in place of the rest.  weights = scores of the chosen,
- * divided by their sum where renormalise is 1 (zeros where it is 0), times scale: binary32.
+ * divided by their sum where renormalise is 1, times scale: binary32, in binary64 and rounded once for a token with a chosen score below 2^-100,
+ * so that scores too small for either have their quotients.
  *   choice, weights [tokens][top_k]   in falling order
  *   expert_start [experts + 1]        expert e's rows are expert_start[e] .. expert_start[e+1]-1, by token
  *   row_token [tokens * top_k]        every row's token, -1 from expert_start[experts] on

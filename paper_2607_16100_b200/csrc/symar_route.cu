@@ -103,6 +103,25 @@ __device__ __noinline__ int choose_exactly(const RouteArgs &a, int64_t row, floa
     return mine;
 }
 
+// The weight of choice `lane` in binary64, divided by the largest chosen score first where only quotients count: those of scores below binary32's (or
+// binary64's) range are numbers like others.  sum: a softmax's, of exp(logit - top).
+__device__ __noinline__ float weigh_exactly(const RouteArgs &a, int64_t row, int mine, float top, float sum)
+{
+    const double x = mine >= 0 ? (double)logit_of(a, row, mine) : -INFINITY;
+    double from = a.sigmoid ? 0.0 : (double)top;
+    if (a.renormalise) {
+        from = x;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) from = fmax(from, __shfl_xor_sync(0xffffffffu, from, d));
+        if (a.sigmoid) from = fmin(from, 0.0);
+    }
+    double w = 0.0;                        // a sigmoid is exp(min(x, 0)) / (1 + exp(-|x|))
+    if (mine >= 0) w = a.sigmoid ? exp(fmin(x, 0.0) - from) / (1.0 + exp(-fabs(x))) : exp(x - from);
+    if (a.renormalise) w /= warp_sum(w);   // (called where there is a choice)
+    else if (!a.sigmoid) w /= (double)sum;
+    return (float)(w * (double)a.scale);
+}
+
 // The D largest of V keys in falling order, by Batcher's odd-even merges of D at a time.
 template <int D>
 __device__ __forceinline__ void sort_falling(uint32_t *key)
@@ -298,6 +317,10 @@ __device__ __forceinline__ int choose(const RouteArgs &a, int t, float &weight)
         const float logit = logit_of(a, row, mine);
         weight = a.sigmoid ? 1.0f / (1.0f + expf(-logit)) : expf(logit - top);
         if (!a.sigmoid && !a.renormalise) weight /= sum;
+    }
+    if (__any_sync(0xffffffffu, mine >= 0 && weight < 0x1p-100f)) {      // (its last digits, or all of it, may be below what binary32 holds)
+        weight = weigh_exactly(a, row, mine, top, sum);
+        return mine;
     }
     if (a.renormalise) {
         const float all = warp_sum(weight);
