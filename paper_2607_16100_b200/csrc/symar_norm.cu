@@ -14,17 +14,13 @@
 
 #include "symar_eights.cuh"
 #include "symar_maps.h"
+#include "symar_norm_side.h"
 #include "symar_ops.h"
 #include "symar_tc.cuh"
 
 namespace symar {
 namespace {
 
-struct Side {
-    const void *weight, *bias;
-    float eps;
-    int   kind, wide, plus_one;            // wide: weight and bias are float32
-};
 struct NormArgs {
     const void *x, *residual, *gate;
     void       *residual_out, *out;
@@ -630,8 +626,7 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
     a.residual_out = p.residual_out;  a.residual_out_ld = p.residual_out_ld;  a.residual_out_group = p.residual_out_group;
     a.out = p.out;  a.out_ld = p.out_ld;  a.out_group = p.out_group;
     a.gate = p.gate;  a.gate_ld = p.gate_ld;  a.gate_group = p.gate_group;  a.gate_step = p.gate_step;  a.gate_act = p.gate_act;
-    Side *to[2] = {&a.after, &a.before};
-    for (int i = 0; i < 2; ++i) *to[i] = Side{sides[i]->weight, sides[i]->bias, sides[i]->eps, sides[i]->kind, sides[i]->dtype == SYMAR_F32, sides[i]->plus_one};
+    a.after = side_of(p.after);  a.before = side_of(p.before);
     a.scale = p.scale;  a.residual_scale = p.residual_scale;
     a.m = p.m;  a.n = p.n;  a.rows = p.groups * p.m;
     a.x_wide = p.dtype == SYMAR_F32;  a.stream_wide = p.stream_dtype == SYMAR_F32;
