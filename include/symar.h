@@ -598,7 +598,9 @@ int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const syma
  * residual_out NULL: r is not stored; out is NULL where, and only where, `before` is SYMAR_NORM_NONE.  gate_step 1: a gate for
  * every channel, 0: one number a row (strides of 0 share it among rows).  Everything is binary32, rounded once to what is stored: `before`
  * sees r as it was before rounding.  Each of residual_out and out may be x or residual with the same layout and dtype; weights and gate
- * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN.        */
+ * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN.
+ * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_TIMEOUT if a wait
+ * inside the kernel (for its own copies, four seconds at most) gave up; what is written is then incomplete.        */
 enum { SYMAR_NORM_MAX = 32768 };
 typedef enum { SYMAR_NORM_NONE = 0, SYMAR_NORM_RMS = 1, SYMAR_NORM_LAYER = 2 } symar_norm_kind_t;
 typedef enum { SYMAR_GATE_NONE = 0, SYMAR_GATE_SIGMOID = 1, SYMAR_GATE_TANH = 2 } symar_gate_t;
@@ -618,6 +620,7 @@ typedef struct {
     int32_t     groups, m, n;
     int32_t     dtype, stream_dtype;      /* symar_dtype_t */
     int32_t     gate_step, gate_act;
+    uint32_t   *status;
 } symar_norm_t;
 int symar_norm(const symar_norm_t *args, void *cuda_stream);
 

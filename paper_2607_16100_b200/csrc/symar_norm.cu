@@ -29,6 +29,7 @@ struct NormArgs {
     float   scale, residual_scale;
     int     m, n, rows;
     int     x_wide, stream_wide, gate_step, gate_act;
+    unsigned *status;
 };
 
 // A row's share of one thread: C chunks of eight elements.  Where chunk c begins; in rows on no 16-byte boundary its elements are T apart.
@@ -436,11 +437,12 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_cons
     const bool row_gates = a.gate && !a.gate_step;
     float by = row_gates ? gate_of(row) : a.scale;
     uint32_t turn = 0;
+    bool whole = true;                     // no wait gave up: nothing more is asked for then, as slots may still be written
     for (int s = 0, round = 0; row < a.rows; row += step, ++turn) {
         const float next = row_gates ? gate_of(row + step) : by;
         const int g = a.m == a.rows ? 0 : (int)row / a.m, t = (int)row - g * a.m;
         const ThreadsSum sum{room + (group * 2 + (turn & 1)) * 4 * 32, T / 32, i >> 5, 1 + group};
-        (void)warp_wait(bar0 + 8 * s, round & 1, &failed);     // (given up: on with what is there, the barriers count all)
+        whole &= warp_wait(bar0 + 8 * s, round & 1, &failed);  // (given up: on with what is there, the barriers count all)
         const int x = slots + s * slot_bytes + 8 * i * kXB, h = slots + s * slot_bytes + ring.x_bytes + 8 * i * kSB;
 #pragma unroll
         for (int c = 0; c < C; ++c) shared8(smem + (on[c] ? x + c * 8 * T * kXB : 0), kX, v[c]);
@@ -493,9 +495,14 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_kernel(const __grid_cons
             asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(T) : "memory");
         }
         // all of the slot has been read before the row's last barrier
-        if (i == 0) ask(row + (int64_t)ring.slots * step, s);
+        if (i == 0 && whole) ask(row + (int64_t)ring.slots * step, s);
         if (++s == ring.slots) s = 0, ++round;
         by = next;
+    }
+    if (*static_cast<volatile int *>(&failed)) {
+        // copies may still be on their way: give them time to end before the memory is let go
+        for (int k = 0; k < 1000; ++k) __nanosleep(1000);
+        if (i == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_TIMEOUT);
     }
 }
 
@@ -592,7 +599,7 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
     if (!args) return SYMAR_ERR_INVAL;
     const symar_norm_t &p = *args;
     if (p.groups < 0 || p.m < 0 || p.n < 0 || !dtype_ok(p.dtype) || !dtype_ok(p.stream_dtype)) return SYMAR_ERR_INVAL;
-    if (p.gate_act < SYMAR_GATE_NONE || p.gate_act > SYMAR_GATE_TANH || p.gate_step < 0 || p.gate_step > 1) return SYMAR_ERR_INVAL;
+    if (p.gate_act < SYMAR_GATE_NONE || p.gate_act > SYMAR_GATE_TANH || p.gate_step < 0 || p.gate_step > 1 || (uintptr_t)p.status % 4) return SYMAR_ERR_INVAL;
     const uintptr_t xw = p.dtype == SYMAR_F32 ? 4 : 2, sw = p.stream_dtype == SYMAR_F32 ? 4 : 2;
     uintptr_t at = (uintptr_t)p.x | (uintptr_t)p.out | (uintptr_t)(p.gate_step ? p.gate : nullptr), st = (uintptr_t)p.residual | (uintptr_t)p.residual_out;
     if ((at | (uintptr_t)p.gate) % xw || st % sw) return SYMAR_ERR_INVAL;
@@ -614,7 +621,12 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
         if (!(p.gate_step == 0 && (i == 4 || i == 5))) vec = vec && strides[i] % 8 == 0;
     }
     if (p.n > SYMAR_NORM_MAX || (int64_t)p.groups * p.m > 0x7fffffff) return SYMAR_ERR_UNSUPPORTED;
-    if (p.groups == 0 || p.m == 0 || p.n == 0) return SYMAR_OK;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    auto clear = [&] {
+        const cudaError_t e = p.status ? cudaMemsetAsync(p.status, 0, sizeof(unsigned), s) : cudaSuccess;
+        return e == cudaSuccess ? (int)SYMAR_OK : cuda_fail(e, "cudaMemsetAsync");
+    };
+    if (p.groups == 0 || p.m == 0 || p.n == 0) return clear();
     if ((p.out == nullptr) != (p.before.kind == SYMAR_NORM_NONE)) return SYMAR_ERR_INVAL;
     if (!p.x || (!p.out && !p.residual_out)) return SYMAR_ERR_INVAL;
     if ((p.out && rows_meet(p.m, p.out_ld, p.groups, p.out_group, p.n)) ||
@@ -630,9 +642,10 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
     a.scale = p.scale;  a.residual_scale = p.residual_scale;
     a.m = p.m;  a.n = p.n;  a.rows = p.groups * p.m;
     a.x_wide = p.dtype == SYMAR_F32;  a.stream_wide = p.stream_dtype == SYMAR_F32;
-    cudaStream_t s = (cudaStream_t)cuda_stream;
+    a.status = p.status;
     Device d;
-    const int rc = device_info(&d);
+    int rc = device_info(&d);
+    if (rc == SYMAR_OK) rc = clear();
     if (rc != SYMAR_OK) return rc;
     const cudaError_t e = vec ? launch_as<true>(a, d, s) : launch_as<false>(a, d, s);
     return e == cudaSuccess ? SYMAR_OK : cuda_fail(e, "symar_norm");

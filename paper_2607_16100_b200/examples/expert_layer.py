@@ -41,7 +41,7 @@ class ExpertBlock:
         self.out_offset = self.heap.bytes_per_rank // 2
         self.partial = self.heap.view(0, (tokens, hidden), torch.bfloat16)
         self.summed = self.heap.view(self.out_offset, (tokens, hidden), torch.bfloat16)
-        self.word = torch.zeros(2, dtype=torch.int32, device=device)
+        self.word = torch.zeros(3, dtype=torch.int32, device=device)
 
     def __call__(self, x, stream, idle=None):
         """x [tokens, hidden] bf16, the normed stream; stream [tokens, hidden], the residual stream (bf16 or float32); idle [tokens, 1] bool: slots
@@ -52,10 +52,10 @@ class ExpertBlock:
             logits.masked_fill_(idle, -math.inf)
         self.routes = symar.route(logits, self.top_k, score="sigmoid", bias=self.bias)
         rows = symar.experts(x, self.w_in, self.routes, gated=True, act="silu", status=self.word[:1])
-        rows = symar.experts(rows, self.w_out, self.routes, by_row=True, status=self.word[1:])
+        rows = symar.experts(rows, self.w_out, self.routes, by_row=True, status=self.word[1:2])
         symar.combine(rows, self.routes, out=self.partial[:, :tokens])
         self.heap.allreduce(0, self.out_offset, tokens * self.hidden, symar.BF16, symar.AUTO, torch.cuda.current_stream().cuda_stream)
-        return symar.norm(self.summed[0, :tokens], stream, after=self.after, before=self.before)
+        return symar.norm(self.summed[0, :tokens], stream, after=self.after, before=self.before, status=self.word[2:])
 
     def check(self) -> None:
         """Raises if a call recorded an error on the device (synchronises)."""

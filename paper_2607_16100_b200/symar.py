@@ -479,7 +479,7 @@ class NormArgs(ctypes.Structure):
         ("out", c_void_p), ("out_ld", c_int64), ("out_group", c_int64),
         ("after", NormSide), ("before", NormSide), ("scale", c_float), ("residual_scale", c_float),
         ("groups", c_int32), ("m", c_int32), ("n", c_int32), ("dtype", c_int32), ("stream_dtype", c_int32),
-        ("gate_step", c_int32), ("gate_act", c_int32),
+        ("gate_step", c_int32), ("gate_act", c_int32), ("status", c_void_p),
     ]
 
 
@@ -887,13 +887,13 @@ _NO_NORM = (0, 0, 0.0, 0, 0, 0)
 
 
 def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str = "none", scale: float = 1.0,
-         residual_scale: float = 1.0, out=None, residual_out=None, stream=None):
+         residual_scale: float = 1.0, out=None, residual_out=None, status=None, stream=None):
     """(y, r) with ``r = residual_scale * residual + scale * act(gate) * after(x)`` and ``y = before(r)`` (``symar_norm``).
 
     x [m, n] or [groups, m, n] float32 or bfloat16, y like it; residual of x's shape, float32 or bfloat16, r like it.  ``after`` and ``before``:
     a :class:`Norm`, or None (a = x; no y, None in its place).  gate: of x's dtype and broadcastable to x's shape, a number for every channel
     or (last extent 1) for a row; ``gate_act``: "none", "sigmoid" or "tanh".  Without a residual r is not stored (None) unless there is no y or
-    ``residual_out`` is given (r is then of its dtype).  ``out`` may be x, ``residual_out`` residual."""
+    ``residual_out`` is given (r is then of its dtype).  ``out`` may be x, ``residual_out`` residual.  ``status``: as in :func:`linear`."""
     torch = _T or _torch()
     where = "symar_norm"
     shape, xs, index, dtype = x.shape, x.stride(), x.get_device(), x.dtype
@@ -943,9 +943,14 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
     for side in (after, before):
         if side is not None and side.n is not None and (side.n != n or side.index != index):
             _bad(where, f"a norm of {side.n} channels on device {side.index} for x {tuple(shape)} on device {index}")
+    sp = 0
+    if status is not None:
+        if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != index:
+            _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
+        sp = status.data_ptr()
     args = _pack_norm(x.data_ptr(), xs[-2], xs[0] if nd == 3 else 0, rp, rl, rg, gp, gl, gg, op, ol, og, yp, yl, yg,
                       *(after.fields if after is not None else _NO_NORM), *(before.fields if before is not None else _NO_NORM), scale, residual_scale,
-                      groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act)
+                      groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act, sp)
     _call((_lib or load()).symar_norm, where, index, stream, args)
     return out if before is not None else None, residual_out
 
