@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) place_kernel(const __grid_constan
 int tokens_of(int tokens)
 {
     if (tokens <= kAlone) return tokens;
-    const int each = (tokens + kBlocks * kWarps - 1) / (kBlocks * kWarps);
+    const int each = (int)(((int64_t)tokens + kBlocks * kWarps - 1) / (kBlocks * kWarps));
     return each * kWarps;
 }
 int blocks_of(int tokens) { return (int)(((int64_t)tokens + tokens_of(tokens) - 1) / tokens_of(tokens)); }
