@@ -597,7 +597,8 @@ int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const syma
  * x, gate, out of `dtype`; residual, residual_out of `stream_dtype`.  residual NULL: 0; gate NULL: act(gate) = 1;
  * residual_out NULL: r is not stored; out is NULL where, and only where, `before` is SYMAR_NORM_NONE.  gate_step 1: a gate for
  * every channel, 0: one number a row (strides of 0 share it among rows).  Everything is binary32, rounded once to what is stored: `before`
- * sees r as it was before rounding.  Each of residual_out and out may be x or residual with the same layout and dtype; weights and gate
+ * sees r as it was before rounding.  residual_out and out have no element in common (SYMAR_ERR_INVAL where they begin at one address); each of them
+ * may be x or residual with the same layout and dtype; weights and gate
  * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN.
  * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_TIMEOUT if a wait
  * inside the kernel (for its own copies, four seconds at most) gave up; what is written is then incomplete.        */

@@ -630,7 +630,7 @@ extern "C" int symar_norm(const symar_norm_t *args, void *cuda_stream)
     if ((p.out == nullptr) != (p.before.kind == SYMAR_NORM_NONE)) return SYMAR_ERR_INVAL;
     if (!p.x || (!p.out && !p.residual_out)) return SYMAR_ERR_INVAL;
     if ((p.out && rows_meet(p.m, p.out_ld, p.groups, p.out_group, p.n)) ||
-        (p.residual_out && rows_meet(p.m, p.residual_out_ld, p.groups, p.residual_out_group, p.n)))
+        (p.residual_out && rows_meet(p.m, p.residual_out_ld, p.groups, p.residual_out_group, p.n)) || (p.out && p.out == p.residual_out))
         return SYMAR_ERR_INVAL;
     NormArgs a{};
     a.x = p.x;  a.x_ld = p.x_ld;  a.x_group = p.x_group;

@@ -893,7 +893,7 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
     x [m, n] or [groups, m, n] float32 or bfloat16, y like it; residual of x's shape, float32 or bfloat16, r like it.  ``after`` and ``before``:
     a :class:`Norm`, or None (a = x; no y, None in its place).  gate: of x's dtype and broadcastable to x's shape, a number for every channel
     or (last extent 1) for a row; ``gate_act``: "none", "sigmoid" or "tanh".  Without a residual r is not stored (None) unless there is no y or
-    ``residual_out`` is given (r is then of its dtype).  ``out`` may be x, ``residual_out`` residual.  ``status``: as in :func:`linear`."""
+    ``residual_out`` is given (r is then of its dtype).  ``out`` may be x, ``residual_out`` residual, both not one.  ``status``: as in :func:`linear`."""
     torch = _T or _torch()
     where = "symar_norm"
     shape, xs, index, dtype = x.shape, x.stride(), x.get_device(), x.dtype

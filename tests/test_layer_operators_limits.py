@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2607_16100_b200 import build, symar
-from test_layer_operators_abi import route_rc
+from test_layer_operators_abi import SOME, norm_rc, route_rc
 
 MOST = 2 ** 31 - 1
 
@@ -23,3 +23,12 @@ def test_a_routers_blocks_are_counted_beyond_31_bits(lib, tokens):
         if experts > 1 and tokens <= MOST - 1024:
             assert route_rc(lib, tokens=tokens, experts=experts, top_k=1, workspace_bytes=need - 1) == symar.ERR_NOMEM
     assert route_rc(lib, tokens=MOST - 1023, experts=2, top_k=1) == symar.ERR_UNSUPPORTED
+
+
+def test_a_norms_two_results_are_two(lib):
+    """Both in x's or the residual's place: one of them would be lost."""
+    for change in ({}, dict(stream_dtype=symar.BF16), dict(out_ld=128, out_group=512)):
+        assert norm_rc(lib, **change) == symar.ERR_INVAL            # (everything at one address)
+    apart = dict(out=SOME + (1 << 16))
+    for change in (dict(out_ld=63), dict(out_group=0), dict(out_group=255), dict(residual_out_ld=0), dict(residual_out_group=32)):
+        assert norm_rc(lib, **{**apart, **change}) == symar.ERR_INVAL
