@@ -865,7 +865,7 @@ class KVContext:
 
 class Norm:
     """One norm over a row's channels: kind "rms" or "layer", weight and bias [n] (None: 1 and 0; both of one dtype, float32 or bfloat16),
-    ``plus_one``: the factor is 1 + weight."""
+    ``plus_one``: the factor is 1 + weight.  A call goes by the tensors as they are then: weights may be loaded, cast or moved in between."""
 
     def __init__(self, kind: str = "rms", weight=None, bias=None, *, eps: float = 1e-6, plus_one: bool = False):
         _T or _torch()
@@ -876,11 +876,23 @@ class Norm:
             if t is not None and (t.dim() != 1 or t.shape != some.shape or t.dtype is not some.dtype or t.get_device() != some.get_device() or
                                   some.get_device() < 0 or not t.is_contiguous()):
                 _bad(where, "weight and bias are contiguous CUDA tensors [n] of one dtype and device")
-        code = _dtype_code(some.dtype, where) if some is not None else F32
-        self.n, self.index = (some.shape[0], some.get_device()) if some is not None else (None, None)
-        self.weight, self.bias = weight, bias
-        self.fields = (weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, eps,
-                       NORM_KINDS[kind], code, 1 if plus_one else 0)
+        if some is not None:
+            _dtype_code(some.dtype, where)
+        self.weight, self.bias, self.eps, self.kind, self.plus_one = weight, bias, eps, kind, plus_one
+
+    def _fields(self, n: int, index: int, where: str):
+        """What a call hands over for rows of n channels: of the tensors as they are now, as a program may have given them other memory, type or size."""
+        weight, bias = self.weight, self.bias
+        some = bias if weight is None else weight
+        kind, plus = NORM_KINDS.get(self.kind), 1 if self.plus_one else 0
+        if some is None:
+            return 0, 0, self.eps, kind, F32, plus
+        shape, dtype = some.shape, some.dtype
+        if shape != (n,) or some.get_device() != index or not some.is_contiguous() or (some is weight and bias is not None and (
+                bias.shape != shape or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous())):
+            _bad(where, f"a norm of weight and bias {[(tuple(t.shape), t.dtype, t.device) for t in (weight, bias) if t is not None]} for {n} channels on device {index}")
+        return (weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, self.eps, kind,
+                _dtype_code(dtype, where), plus)
 
 
 _NO_NORM = (0, 0, 0.0, 0, 0, 0)
@@ -940,16 +952,14 @@ def norm(x, residual=None, *, after=None, before=None, gate=None, gate_act: str 
         if step and n > 1 and s[-1] != 1:
             _bad(where, "the gate's channels are contiguous")
         gp, gl, gg = gate.data_ptr(), s[-2], s[0] if nd == 3 else 0
-    for side in (after, before):
-        if side is not None and side.n is not None and (side.n != n or side.index != index):
-            _bad(where, f"a norm of {side.n} channels on device {side.index} for x {tuple(shape)} on device {index}")
     sp = 0
     if status is not None:
         if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != index:
             _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
         sp = status.data_ptr()
     args = _pack_norm(x.data_ptr(), xs[-2], xs[0] if nd == 3 else 0, rp, rl, rg, gp, gl, gg, op, ol, og, yp, yl, yg,
-                      *(after.fields if after is not None else _NO_NORM), *(before.fields if before is not None else _NO_NORM), scale, residual_scale,
+                      *(after._fields(n, index, where) if after is not None else _NO_NORM),
+                      *(before._fields(n, index, where) if before is not None else _NO_NORM), scale, residual_scale,
                       groups, m, n, code, code if stream_dtype is None else _dtype_code(stream_dtype, where), step, act, sp)
     _call((_lib or load()).symar_norm, where, index, stream, args)
     return out if before is not None else None, residual_out
