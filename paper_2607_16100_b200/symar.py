@@ -981,7 +981,7 @@ class Routes:
         if expert_start.shape[0] < 2:
             _bad("Routes", "expert_start has an entry more than there are experts")
         self._lists = choice, expert_start, row_token, token_row, weights
-        self._set(shape, expert_start.shape[0] - 1, index, expert_start.data_ptr(), row_token.data_ptr(), token_row.data_ptr(), weights.data_ptr())
+        self._set(shape, expert_start.shape[0] - 1, index, tuple(t.data_ptr() for t in self._lists))
 
     @classmethod
     def _of(cls, whole, shape, experts: int, index: int) -> "Routes":
@@ -990,14 +990,26 @@ class Routes:
         r = object.__new__(cls)
         at, rows = whole.data_ptr(), shape[0] * shape[1]
         r._lists, r._whole = None, whole
-        r._set(shape, experts, index, at + 16 * rows, at + 4 * rows, at + 8 * rows, at + 12 * rows)
+        r._set(shape, experts, index, (at, at + 16 * rows, at + 4 * rows, at + 8 * rows, at + 12 * rows))
         return r
 
-    def _set(self, shape, experts, index, start_ptr, row_token_ptr, token_row_ptr, weights_ptr):
+    def _set(self, shape, experts, index, addresses):
         self.experts, self.index = experts, index
         self.tokens, self.top_k = shape
         self.rows = self.tokens * self.top_k
-        self._start_ptr, self._row_token_ptr, self._token_row_ptr, self._weights_ptr = start_ptr, row_token_ptr, token_row_ptr, weights_ptr
+        self._addresses = addresses
+
+    def _at(self, i: int) -> int:
+        """The address of a list as it is now: a program may have given its tensor other memory."""
+        at = self._addresses[i]
+        if self._lists is not None:
+            t = self._lists[i]
+            now = t.data_ptr()
+            if now != at and (t.numel() != (self.experts + 1 if i == 1 else self.rows) or t.dtype is not (_T.float32 if i == 4 else _T.int32) or
+                              t.get_device() != self.index or not t.is_contiguous()):
+                _bad("Routes", f"a list that has become {list(t.shape)} {t.dtype} on {t.device}")
+            at = now
+        return at
 
     def _list(self, i: int):
         if self._lists is None:
@@ -1088,7 +1100,7 @@ def experts(x, w, routes: Routes, *, bias=None, act: str = "none", gated: bool =
             _bad(where, f"status is one int32 on x's device, not {tuple(status.shape)} {status.dtype} on {status.device}")
         sp = status.data_ptr()
     fields = (x.data_ptr(), xs[-2], xs[0] if xd == 3 else 0, w.data_ptr(), ws[-2], ws[-3], ws[0] if wd == 4 else 0, bp, be, bg,
-              out.data_ptr(), os[-2], os[0] if ranked else 0, routes._start_ptr, 0 if by_row else routes._row_token_ptr,
+              out.data_ptr(), os[-2], os[0] if ranked else 0, routes._at(1), 0 if by_row else routes._at(2),
               groups, routes.experts, routes.rows, x_rows, n, k, _dtype_code(out.dtype, where), code, 1 if gated else 0, sp)
     lib, args = _lib or load(), _pack_experts(*fields, 0, 0)
     if not by_row:
@@ -1124,7 +1136,7 @@ def combine(y, routes: Routes, *, residual=None, root: int = -1, out=None, out_d
         if residual.shape not in (want, want[-2:]) or residual.dtype is not out.dtype or (n > 1 and rs[-1] != 1) or residual.get_device() != index:
             _bad(where, f"residual of shape {tuple(residual.shape)}, {residual.dtype}")
         rp, rl, rg = residual.data_ptr(), rs[-2], rs[0] if len(rs) == 3 else 0
-    args = _pack_combine(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._token_row_ptr, routes._weights_ptr, rp, rl, rg,
+    args = _pack_combine(y.data_ptr(), ys[-2], ys[0] if nd == 3 else 0, routes._at(3), routes._at(4), rp, rl, rg,
                          out.data_ptr(), os[-2], os[0] if nd == 3 else 0, groups, routes.tokens, routes.top_k, routes.rows, n, code,
                          _dtype_code(out.dtype, where), root)
     _call((_lib or load()).symar_combine, where, index, stream, args)
