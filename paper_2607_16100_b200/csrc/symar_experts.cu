@@ -88,15 +88,32 @@ __device__ __forceinline__ void far_arrive(uint32_t bar)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // A thread's wait for what other blocks of its cluster do
+__device__ __forceinline__ bool pair_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, volatile int *failed)
 {
     const uint64_t t0 = now_ns();
     for (int i = 1;; ++i) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) return true;
+        if (pair_try(bar, parity)) return true;
         if (i % 256 == 0 && (*failed || now_ns() - t0 > kWaitNs)) {
+            *failed = 1;
+            return false;
+        }
+    }
+}
+// The same for a whole warp: all its lanes go on, or none.
+__device__ __forceinline__ bool pair_warp_wait(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    const uint64_t t0 = now_ns();
+#pragma unroll 1
+    for (int i = 1;; ++i) {
+        if (__all_sync(0xffffffffu, pair_try(bar, parity))) return true;
+        if (i % 256 == 0 && __any_sync(0xffffffffu, *failed || now_ns() - t0 > kWaitNs)) {
             *failed = 1;
             return false;
         }
@@ -265,6 +282,7 @@ __device__ __forceinline__ void finish(const ExpertsArgs &a, const Tile &t, cons
         const float4 y = held4(hold + i * kRows, c);
         finish_row<O>(a, t, c, c0 + i, y, a.gated ? held4(hold + i * kRows + kHalf, c) : y);
     }
+    __syncwarp();                          // (halves of a warp may have had different numbers of tokens; in results_sync itself it costs 3% of a decode batch)
     results_sync();
 }
 
@@ -442,7 +460,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);
                 tc_after();
             }
-            if (kSplit && shared_tiles > 0) (void)pair_wait(parts_used, (shared_tiles - 1) & 1, &failed);      // every block has used its parts of the tile before
+            if (kSplit && shared_tiles > 0) (void)pair_warp_wait(parts_used, (shared_tiles - 1) & 1, &failed);      // every block has used its parts of the tile before
 #pragma unroll
             for (int c0 = 0; c0 < NT; c0 += kStep) {
                 if (c0 >= t.count) break;
@@ -474,7 +492,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             if (kSplit) {
                 const int own = (t.count - rank + a.split - 1) / a.split;      // (0 or less: none)
                 if (tid == 128) bar_expect(parts_here, (uint32_t)(max(own, 0) * a.split * kRows * 4));
-                (void)pair_wait(parts_here, shared_tiles & 1, &failed);
+                (void)pair_warp_wait(parts_here, shared_tiles & 1, &failed);
                 const int per = a.gated ? 2 : 1;
                 for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < own; i += 8 * per) {
                     float4 y4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), u = y4;
@@ -489,13 +507,14 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                     }
                     finish_row<O>(a, t, c, rank + i * a.split, y4, u);
                 }
+                __syncwarp();
                 results_sync();
                 if (tid < 128 + a.split) used_arrive(at_rank(parts_used, (uint32_t)(tid - 128)));
                 ++shared_tiles;
             }
             if (!kWide && slices > 0) ++turn;
         }
-        if (kSplit && shared_tiles > 0) (void)pair_wait(parts_used, (shared_tiles - 1) & 1, &failed);
+        if (kSplit && shared_tiles > 0) (void)pair_warp_wait(parts_used, (shared_tiles - 1) & 1, &failed);
     }
 done:
     __syncwarp();
