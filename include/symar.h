@@ -660,7 +660,7 @@ int symar_route(const symar_route_t *args, void *cuda_stream);
  *     out[g][r] = act(x wg^T + bg) * (x wu^T + bu)  (gated)      w[g][e] [2n][k]: wg's n rows, then wu's; bias alike
  * with x = x[g][row_token[r]], or x[g][r] where row_token is NULL.  x [groups][x_rows][k], w, bias (NULL: 0) bf16; sums and what follows them are
  * binary32, rounded once to out_dtype (float32 results as in symar_linear).  Group strides of 0 share an operand.  The lists are symar_route()'s, on the
- * device: starts are brought into 0 .. rows and into order before use; rows of nobody (behind the last expert's) are left as they were.
+ * device: starts are brought into 0 .. rows and into order before use; rows of nobody (before the first expert's, behind the last one's) are left as they were.
  * A row_token outside x makes its row's result undefined and is reported.  Rows of x and w lie on 16-byte boundaries (base, and strides of axes longer than one:
  * multiples of 8 elements, not 0); SYMAR_ERR_UNSUPPORTED otherwise.  Sizes of 0 are allowed (k = 0: the product is 0); 1024 experts at most, other sizes up to 2^30.
  * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_INVAL by a row_token

@@ -713,15 +713,16 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
 {
     wait_for_stream();
     const int lane = threadIdx.x & 31;
-    int count = 0;                         // rows of somebody (see make_plan)
+    const int from = max(0, min(a.expert_start[0], a.rows));
+    int count = 0;                         // rows of somebody, from there on (see make_plan)
     for (int e = lane; e <= a.experts; e += 32) count = max(count, a.expert_start[e]);
-    count = min(__reduce_max_sync(0xffffffffu, count), a.rows);
+    count = max(0, min(__reduce_max_sync(0xffffffffu, count), a.rows) - from);
     // a warp's unit: 128 pieces of a row, four of them a lane
     const int parts = (a.pieces + 127) / 128, whole = a.k / 8;
     const int64_t units = (int64_t)a.groups * count * parts;
     for (int64_t i = (int64_t)blockIdx.x * (kGatherThreads / 32) + (threadIdx.x >> 5); i < units; i += (int64_t)(kGatherThreads / 32) * gridDim.x) {
         const int64_t cell = i / parts;
-        const int c0 = (int)(i - cell * parts) * 128 + lane, g = (int)(cell / count), row = (int)(cell - (int64_t)g * count);
+        const int c0 = (int)(i - cell * parts) * 128 + lane, g = (int)(cell / count), row = from + (int)(cell - (int64_t)g * count);
         const int token = a.row_token[row];
         const bool there = token >= 0 && token < a.x_rows;
         if (!there && c0 == 0 && a.status) atomicCAS(a.status, 0u, (unsigned)SYMAR_ERR_INVAL);
