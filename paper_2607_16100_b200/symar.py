@@ -878,21 +878,22 @@ class Norm:
                 _bad(where, "weight and bias are contiguous CUDA tensors [n] of one dtype and device")
         if some is not None:
             _dtype_code(some.dtype, where)
-        self.weight, self.bias, self.eps, self.kind, self.plus_one = weight, bias, eps, kind, plus_one
+        self.weight, self.bias = weight, bias
+        self._eps, self._kind, self._plus = eps, NORM_KINDS[kind], 1 if plus_one else 0
 
     def _fields(self, n: int, index: int, where: str):
         """What a call hands over for rows of n channels: of the tensors as they are now, as a program may have given them other memory, type or size."""
         weight, bias = self.weight, self.bias
         some = bias if weight is None else weight
-        kind, plus = NORM_KINDS.get(self.kind), 1 if self.plus_one else 0
         if some is None:
-            return 0, 0, self.eps, kind, F32, plus
-        shape, dtype = some.shape, some.dtype
-        if shape != (n,) or some.get_device() != index or not some.is_contiguous() or (some is weight and bias is not None and (
-                bias.shape != shape or bias.dtype is not dtype or bias.get_device() != index or not bias.is_contiguous())):
+            return 0, 0, self._eps, self._kind, F32, self._plus
+        dtype = some.dtype
+        if some.shape != (n,) or not some.is_contiguous() or some.get_device() != index or (some is not bias and bias is not None and (
+                bias.dtype is not dtype or bias.shape != (n,) or not bias.is_contiguous() or bias.get_device() != index)):
             _bad(where, f"a norm of weight and bias {[(tuple(t.shape), t.dtype, t.device) for t in (weight, bias) if t is not None]} for {n} channels on device {index}")
-        return (weight.data_ptr() if weight is not None else 0, bias.data_ptr() if bias is not None else 0, self.eps, kind,
-                _dtype_code(dtype, where), plus)
+        code = _CODES.get(dtype)
+        return (0 if weight is None else weight.data_ptr(), 0 if bias is None else bias.data_ptr(), self._eps, self._kind,
+                _dtype_code(dtype, where) if code is None else code, self._plus)
 
 
 _NO_NORM = (0, 0, 0.0, 0, 0, 0)
