@@ -599,7 +599,7 @@ int symar_kv_attention(symar_kv_t *kv, const symar_kv_cache_t *cache, const syma
  * every channel, 0: one number a row (strides of 0 share it among rows).  Everything is binary32, rounded once to what is stored: `before`
  * sees r as it was before rounding.  residual_out and out have no element in common (SYMAR_ERR_INVAL where they begin at one address); each of them
  * may be x or residual with the same layout and dtype; weights and gate
- * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN.
+ * are written by nothing of the call.  n up to SYMAR_NORM_MAX; values whose squares pass binary32 give zeros or NaN, squares below it count as 0.
  * status: optional device word (may be NULL), cleared on the stream by every call that returns SYMAR_OK, then set to SYMAR_ERR_TIMEOUT if a wait
  * inside the kernel (for its own copies, four seconds at most) gave up; what is written is then incomplete.        */
 enum { SYMAR_NORM_MAX = 32768 };
@@ -628,7 +628,7 @@ int symar_norm(const symar_norm_t *args, void *cuda_stream);
 /* The experts of every token.  logits [tokens][experts] (rows `ld` apart) of `dtype`;
  *     score = softmax over the token's logits, or sigmoid of each.
  * A token's top_k experts are those with the largest logit, or with the largest score + bias where there is a bias [experts]
- * (binary32), decided as exact arithmetic decides (in binary64 where binary32 leaves a doubt); of equal ones the lowest
+ * (binary32): logits as they are, sums as binary64 has them wherever binary32 leaves a doubt; of equal ones the lowest
  * index first.  An expert whose logit is -inf or NaN, or whose score + bias is, is not to be had (and counts as 0 in a softmax); a
  * token with fewer than top_k others has -1 and a weight of 0 in place of the rest.  weights = scores of the chosen,
  * divided by their sum where renormalise is 1, times scale: binary32, in binary64 and rounded once for a token with a chosen score below 2^-100,
@@ -659,7 +659,9 @@ int symar_route(const symar_route_t *args, void *cuda_stream);
  *     out[g][r] = act(x w^T + bias)                              w = w[g][e] [n][k],  bias = bias[g][e] [n]
  *     out[g][r] = act(x wg^T + bg) * (x wu^T + bu)  (gated)      w[g][e] [2n][k]: wg's n rows, then wu's; bias alike
  * with x = x[g][row_token[r]], or x[g][r] where row_token is NULL.  x [groups][x_rows][k], w, bias (NULL: 0) bf16; sums and what follows them are
- * binary32, rounded once to out_dtype (float32 results as in symar_linear).  Group strides of 0 share an operand.  The lists are symar_route()'s, on the
+ * binary32, rounded once to out_dtype.  bf16 results sum all of k (or a block's part of it) in the tensor cores, whose additions truncate: off by
+ * k 2^-23 of the sum of the products' sizes at most; float32 results leave them every 128 products, as in symar_linear.  Group strides of 0 share an
+ * operand.  The lists are symar_route()'s, on the
  * device: starts are brought into 0 .. rows and into order before use; rows of nobody (before the first expert's, behind the last one's) are left as they were.
  * A row_token outside x makes its row's result undefined and is reported.  Rows of x and w lie on 16-byte boundaries (base, and strides of axes longer than one:
  * multiples of 8 elements, not 0); SYMAR_ERR_UNSUPPORTED otherwise.  Sizes of 0 are allowed (k = 0: the product is 0); 1024 experts at most, other sizes up to 2^30.

@@ -5,7 +5,7 @@
 // or two still use all lanes.  Of a tile's 128 weights' rows 64 are the gate's and 64 up's where the activation is gated: both halves
 // of a result meet in one block.  How many rows an expert has is known on the device only: every block counts the
 // experts' tiles for itself and takes every so-many-th of them; the instruction's columns and what is copied of the tokens go with what a
-// tile has, in sixteens.  Four more warps gather the tokens' rows straight into the ring, so nothing is permuted beforehand.
+// tile has, in sixteens.  Four more warps gather the tokens' rows straight into the ring; only pairs of blocks (below) have them put in order beforehand.
 //
 // A block: one warp fills a ring of 64-wide slices of both operands, one thread issues the products, eight warps take finished accumulators
 // out of tensor memory while the next tile is summed in its other half.  Many rows an expert go to pairs of blocks, few tiles over a long k to clusters that
@@ -41,7 +41,9 @@ struct ExpertsArgs {
 constexpr int kRows = 128, kHalf = 64, kSlice = 64;
 constexpr int kMaxExperts = SYMAR_EXPERTS_MAX;
 constexpr int kLoaders = 128;                // threads that gather rows
-constexpr int kChunk = 2;                  // slices that a float32 result sums in the tensor cores at a time (see symar_linear.cu)
+constexpr int kChunk = 2;                  // slices that a float32 result sums in the tensor cores at a time (see symar_linear.cu).  A bf16 result sums all of its
+                                           // block's slices there: its own rounding hides what truncating additions lose (k = 4096: 0.00166 of the result off 64 bits with
+                                           // either, 0.2% more of its elements rounded the other way)
 constexpr int kBand  = 16;                 // tiles of tokens that run through a column of weights before the next
 constexpr int kStep  = 32;                 // tokens that leave the accumulator at a time
 
@@ -846,7 +848,8 @@ int launch_pair(ExpertsArgs a, const CUtensorMap &wmap, const CUtensorMap &xmap,
 // Tokens of a tile, by what an expert has of them on average: few leave room for more weights on their way, many read them less often (64 or 128 with 32 experts of
 // 2 x 1024 x 4096: 25 rows each 96.6 and 100 us, 50 rows 118 and 111).  Pairs take many rows where their tiles are enough for all multiprocessors (a product's start costs
 // them 3 us more: 1000 rows x 128 x 520 of seven experts 13.3 us instead of 9.9; with 1003 channels on two ranks 17.9 instead of 19.3) and the gathering beforehand is
-// little beside the products (75 rows each of k = 4096: 112 us instead of 123, of k = 1024 25.3 instead of 22.9).
+// little beside the products (75 rows each of k = 4096: 112 us instead of 123, of k = 1024 25.3 instead of 22.9).  148 is the chip's number of multiprocessors: the
+// workspace goes by the same rule and is asked for by sizes alone, without a device.
 int tile_tokens(const symar_experts_t &p)
 {
     const int64_t used = p.experts < p.rows ? p.experts : p.rows, each = used > 0 ? p.rows / used : 0;

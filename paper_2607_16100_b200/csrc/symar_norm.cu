@@ -7,9 +7,10 @@
 //
 // Bound and measured (B200, within a CUDA graph).  A few rows: latency; one of 8192 takes 2.9 us, of which the launch is most.  Many long
 // ones: bytes; 16384 x 8192 with norms on both sides and a gate a channel takes 200 us for 1.07 GB (5.4 TB/s, 0.82 of the measured copy rate), with the norm before
-// the next block alone 183-193 us; what keeps it from the copy's rate is the row's chain of two sums among half the warps a multiprocessor could have.  Short
-// ones: instructions; 73728 heads of 128 out of rows of 20 take 13.0 us (2.9 TB/s).  Rows on no 16-byte boundary: instructions, as every
-// element is read and written by itself; 1501 x 2049, two layer norms with bias and a float32 stream, takes 20.4 us where 2048 takes 17.7.
+// the next block alone 188 us, 16384 x 4096 of float32 189 and 175 us; what keeps it from the copy's rate is the row's chain of two sums among half the warps a multiprocessor could have.  Short
+// ones: instructions and their latency (61% of the issue slots at 44% of the warps); 73728 heads of 128 out of rows of 20 take 12.9 us (2.9 TB/s), of
+// float32 16.5.  Rows on no 16-byte boundary: the same (50% at 40%), as every element is read and written by itself; 1501 x 2049, two layer norms with bias
+// and a float32 stream, takes 19.9 us where 2048 takes 17.7.
 #include <type_traits>
 
 #include "symar_eights.cuh"

@@ -6,11 +6,11 @@
 // of earlier warps and blocks and of smaller experts are added up, and the warp goes through its tokens once more.  Nothing depends on the order in
 // which blocks run.  Few tokens are one block and one launch; more are two launches, the blocks' counts between them in the workspace.
 //
-// Choices have to be those of exact arithmetic, whatever binary32 rounds: where two neighbours in the order found, or the last choice and any expert
+// Choices have to be those of binary64, whatever binary32 rounds: where two neighbours in the order found, or the last choice and any expert
 // behind it, are nearer than the rounding of their keys and not the same, the token's choices are made again in binary64.
 //
-// Bound by instructions and, with few tokens, by latency (B200, within a CUDA graph): 16384 tokens x 256 experts, top 8 of sigmoid + bias, take 26.8 us (about
-// 20 and 7 for the two launches; 800 instructions of a warp a token, a third of them the eight choices), 64 x 128 9.1 us, one token 4.0 us.  A choice by
+// Bound by instructions and, with few tokens, by latency (B200, within a CUDA graph): 16384 tokens x 256 experts, top 8 of sigmoid + bias, take 27.2 us (about
+// 20 and 7 for the two launches; 900 instructions of a warp a token, a third of them the eight choices), 64 x 128 9.2 us, one token 3.9 us.  A choice by
 // two reductions over unsorted lanes took 1420 instructions (49 us), all doubts in binary64 over all experts 33 us.
 #include <math.h>
 
@@ -32,8 +32,8 @@ struct RouteArgs {
 };
 constexpr int kMaxExperts = SYMAR_ROUTE_MAX_EXPERTS, kMaxTop = SYMAR_ROUTE_MAX_TOP;
 constexpr int kWarps = 32, kThreads = 32 * kWarps;
-constexpr int kBlocks = 148;               // of the two launches
-constexpr int kAlone  = 64;                // tokens of one block: one launch costs the host half (64 x 128: 9.2 us alone, 7.9 in two)
+constexpr int kBlocks = 148;               // of the two launches: the chip's multiprocessors (the workspace is asked for without a device)
+constexpr int kAlone  = 64;                // tokens of one block: one launch costs the host half (64 x 128: 9.2 us alone, 8.1 in two)
 static_assert(kThreads >= kMaxExperts && kMaxTop <= 32 && kMaxExperts <= 32 * 32, "");
 
 __device__ __forceinline__ float logit_of(const RouteArgs &a, int64_t row, int e)
