@@ -631,7 +631,7 @@ int symar_norm(const symar_norm_t *args, void *cuda_stream);
  * (binary32): logits as they are, sums as binary64 has them wherever binary32 leaves a doubt; of equal ones the lowest
  * index first.  An expert whose logit is -inf or NaN, or whose score + bias is, is not to be had (and counts as 0 in a softmax); a
  * token with fewer than top_k others has -1 and a weight of 0 in place of the rest.  weights = scores of the chosen,
- * divided by their sum where renormalise is 1, times scale: binary32, in binary64 and rounded once for a token with a chosen score below 2^-100,
+ * divided by their sum where renormalise is 1, times scale: binary32, in binary64 and rounded once (a softmax's sum over all experts apart) for a token with a chosen score below 2^-100,
  * so that scores too small for either have their quotients.
  *   choice, weights [tokens][top_k]   in falling order
  *   expert_start [experts + 1]        expert e's rows are expert_start[e] .. expert_start[e+1]-1, by token
