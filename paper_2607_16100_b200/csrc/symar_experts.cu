@@ -435,6 +435,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
         const int quarter = warp & 3, side = (warp - 4) >> 2, ew = warp - 4, ch = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)quarter << 21;
         uint32_t turn = 0, shared_tiles = 0;
+        bool whole = true;                 // no wait for other blocks gave up: nothing more is sent or expected then, their barriers may be a phase behind
         for (int tile = first; tile < tiles; tile += step) {
             const Tile t = tile_of(plan, a, tile, channels);
             const Channels c = channels_of(a, t, lane);
@@ -462,7 +463,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
                 (void)warp_wait(acc_full + 8 * (turn & 1), (turn >> 1) & 1, &failed);
                 tc_after();
             }
-            if (kSplit && shared_tiles > 0) (void)pair_warp_wait(parts_used, (shared_tiles - 1) & 1, &failed);      // every block has used its parts of the tile before
+            if (kSplit && shared_tiles > 0) whole &= pair_warp_wait(parts_used, (shared_tiles - 1) & 1, &failed);   // every block has used its parts of the tile before
 #pragma unroll
             for (int c0 = 0; c0 < NT; c0 += kStep) {
                 if (c0 >= t.count) break;
@@ -484,7 +485,7 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int token = c0 + 16 * side + i, to = token % a.split;
-                        if (token >= t.count) break;
+                        if (token >= t.count || !whole) break;
                         far_store(at_rank(smem_addr(hold + ((token / a.split) * a.split + rank) * kRows + ch), to), v[i], at_rank(parts_here, to));
                     }
                 } else {
@@ -493,8 +494,8 @@ experts_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__
             }
             if (kSplit) {
                 const int own = (t.count - rank + a.split - 1) / a.split;      // (0 or less: none)
-                if (tid == 128) bar_expect(parts_here, (uint32_t)(max(own, 0) * a.split * kRows * 4));
-                (void)pair_warp_wait(parts_here, shared_tiles & 1, &failed);
+                if (tid == 128 && whole) bar_expect(parts_here, (uint32_t)(max(own, 0) * a.split * kRows * 4));
+                whole &= pair_warp_wait(parts_here, shared_tiles & 1, &failed);
                 const int per = a.gated ? 2 : 1;
                 for (int i = ew * per + (a.gated ? lane >> 4 : 0); i < own; i += 8 * per) {
                     float4 y4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f), u = y4;

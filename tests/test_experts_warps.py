@@ -27,3 +27,12 @@ def test_lanes_come_together_before_a_barrier():
     assert len(loops) == 2
     for loop in loops:
         assert loop.index("__syncwarp();") < loop.index("results_sync();")
+
+
+def test_nothing_is_sent_or_expected_once_a_wait_gave_up():
+    """A barrier whose phase never ended takes no other arrival, and other blocks' memory no more parts."""
+    results = part(TEXT[TEXT.index("experts_kernel(const"):], "// ---- results ----", "done:")
+    assert results.count("bar_expect(") == 1 and results.count("if (tid == 128 && whole) bar_expect(parts_here") == 1
+    assert results.count("far_store(") == 1 and "if (token >= t.count || !whole) break;" in results
+    loop = results[:results.rindex("pair_warp_wait(")]               # (behind the last tile nothing follows)
+    assert loop.count("pair_warp_wait(") == loop.count("whole &= pair_warp_wait(") == 2
